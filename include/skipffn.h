@@ -209,6 +209,27 @@ skipffn_status skipffn_summary_backward(const void *X, const int32_t *seg_offset
                                         int32_t dw_fp32, void *scratch, size_t scratch_bytes,
                                         void *stream);
 
+/* Layer normalisation of packed rows (the vision tower's blocks and its projector; the decoder's RMS norm
+ * is part of the pre-norm variant above).  Needs no handle.
+ *     forward :  y = (x - mean) rstd gamma + beta,  mean and variance over the C columns of a row,
+ *                rstd = 1 / sqrt(var + eps), eps >= 0
+ *     backward:  dx, and the column sums dgamma = sum_rows dy (x - mean) rstd, dbeta = sum_rows dy
+ *   x, y, dy, dx : [n_rows, C] device, dtype = skipffn_dtype; C a multiple of 8, at most 16384
+ *                  (EUNSUPPORTED); y may be x, dx may be dy or x; a partial overlap is EINVAL
+ *   gamma, beta  : [C] in dtype; beta may be NULL (zero)
+ *   mean, rstd   : [n_rows] fp32; written by the forward (either may be NULL), read by the backward
+ *   dgamma, dbeta: [C] in dtype, fp32 with dw_fp32 or when dtype is fp32; overwritten; either may be NULL
+ *   scratch      : device memory of skipffn_layernorm_scratch_bytes(C) bytes (EWORKSPACE if smaller)
+ * Arrays in dtype and the scratch start on 16-byte boundaries (EINVAL otherwise).  Statistics and sums are
+ * fp32 in a fixed order; outputs are rounded once. */
+skipffn_status skipffn_layernorm_forward(const void *x, const void *gamma, const void *beta, int64_t n_rows, int32_t C,
+                                         int32_t dtype, float eps, void *y, float *mean, float *rstd, void *stream);
+size_t skipffn_layernorm_scratch_bytes(int32_t C);
+skipffn_status skipffn_layernorm_backward(const void *dy, const void *x, const void *gamma, const float *mean,
+                                          const float *rstd, int64_t n_rows, int32_t C, int32_t dtype, void *dx,
+                                          void *dgamma, void *dbeta, int32_t dw_fp32, void *scratch,
+                                          size_t scratch_bytes, void *stream);
+
 /* Token merge of the skipped visual tokens (paper section 4.1): (1) cosine similarity between every
  * pair of the n tokens and an average similarity per token, (2) the k tokens with the LOWEST average
  * are kept, (3) each other token is merged into its most similar kept token.
@@ -237,6 +258,59 @@ skipffn_status skipffn_token_merge(const void *X, int64_t n, int32_t C, int32_t 
  * if its tensor-core kernel gave up on a wait, else SKIPFFN_OK. */
 skipffn_status skipffn_token_merge_poll(void *scratch, int64_t n, int32_t C, int32_t k, int32_t dtype,
                                         void *stream, int32_t *site_out);
+
+/* Packed attention: the other half of the decoder block (the sublayer whose output Eq. 4 / Eq. 5 take
+ * as h_attn) and the vision tower's.  Per sequence of a packed batch, with scale > 0:
+ *     s_ij = scale q_i . k_j,  p_i = softmax_j s_ij over j <= i (causal = 1) or all j (causal = 0),
+ *     out_i = sum_j p_ij v_j,  lse_i = log sum_j exp(s_ij)
+ * where query head h reads key / value head h / (heads_q / heads_kv).  The backward is the exact vjp; the
+ * gradient of a shared key / value head is the sum over its query heads.
+ *
+ * A handle holds the packing (the same for every layer of a step), checked on the host once:
+ *   cu_seqlens : HOST int32 [n_seq + 1], ascending, first 0; zero lengths are allowed.  N = its last entry.
+ *   plan       : device memory of skipffn_attention_plan_bytes(...) bytes, 16-byte aligned, owned by the
+ *                caller and alive as long as the handle; holds the work lists and a status block.
+ *                skipffn_attention_create copies them there and waits for `stream`, so it stays outside
+ *                stream captures (EINVAL inside one); forward and backward may be captured.
+ * Handles are read-only after creation: calls on different streams may share one.
+ *
+ * Arrays are [tokens, heads, head_dim] with contiguous heads and a token stride ld* in elements (so
+ * that slices of one fused projection can be passed); bases and strides are multiples of 16 bytes
+ * and a stride is at least heads x head_dim.  head_dim is a multiple of 8 up to 128 and a group
+ * (heads_q / heads_kv) has at most 64 heads, else EUNSUPPORTED.  Only rows 0 .. N-1 are read or written;
+ * lse is [N, heads_q] fp32, natural logarithm.  Outputs must not overlap inputs or each other (EINVAL).
+ * bf16: tensor-core kernels with fp32 accumulation; scores, softmax statistics and gradients of the
+ * scores are fp32, P and dS are rounded to bf16 as operands of the second products, results once.
+ * fp32, or path = SIMT: plain FMA.  All sums have a fixed order: equal calls give equal bits.
+ * A non-finite value spreads inside its own sequence only (a later token's inf or NaN in v, k, q or
+ * dout can reach earlier tokens' results there: 0 * inf is not masked); it never reaches another sequence.
+ * backward: `out` and `lse` are the forward's results; scratch: device memory of
+ * skipffn_attention_scratch_bytes(handle) bytes, 16-byte aligned, used by this call only.
+ * skipffn_attention_poll synchronises `stream` and reports SKIPFFN_ETIMEOUT with the wait site if a kernel
+ * gave up on a wait. */
+typedef struct {
+    int32_t heads_q, heads_kv, head_dim;
+    int32_t dtype;           /* skipffn_dtype */
+    int32_t causal;
+    int32_t path;            /* skipffn_path */
+    float scale;
+} skipffn_attention_config;
+typedef struct skipffn_attention skipffn_attention;
+size_t skipffn_attention_plan_bytes(const skipffn_attention_config *cfg, const int32_t *cu_seqlens, int32_t n_seq);
+skipffn_status skipffn_attention_create(skipffn_attention **attention, const skipffn_attention_config *cfg,
+                                        const int32_t *cu_seqlens, int32_t n_seq, void *plan, size_t plan_bytes,
+                                        void *stream);
+void skipffn_attention_destroy(skipffn_attention *attention);
+skipffn_status skipffn_attention_forward(const skipffn_attention *attention, const void *q, int64_t ldq,
+                                         const void *k, int64_t ldk, const void *v, int64_t ldv, void *out,
+                                         int64_t ldo, float *lse, void *stream);
+size_t skipffn_attention_scratch_bytes(const skipffn_attention *attention);
+skipffn_status skipffn_attention_backward(const skipffn_attention *attention, const void *dout, int64_t lddo,
+                                          const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v,
+                                          int64_t ldv, const void *out, int64_t ldo, const float *lse, void *dq,
+                                          int64_t lddq, void *dk, int64_t lddk, void *dv, int64_t lddv,
+                                          void *scratch, size_t scratch_bytes, void *stream);
+skipffn_status skipffn_attention_poll(const skipffn_attention *attention, void *stream, int32_t *site_out);
 
 /* Device addresses of the kept-row index list (int32, ascending) and of its length. */
 skipffn_status skipffn_get_kept(const skipffn_saved *saved, const int32_t **idx_dev,

@@ -22,7 +22,10 @@ EXPORTS = ["skipffn_workspace_bytes", "skipffn_saved_create", "skipffn_saved_des
            "skipffn_summary_forward", "skipffn_summary_backward", "skipffn_token_merge_scratch_bytes",
            "skipffn_token_merge", "skipffn_tune", "skipffn_saved_bytes", "skipffn_scratch_bytes",
            "skipffn_workspace_bytes_kept", "skipffn_saved_create_kept", "skipffn_saved_create_split",
-           "skipffn_token_merge_poll", "skipffn_schedule_plan_segment"]
+           "skipffn_token_merge_poll", "skipffn_schedule_plan_segment", "skipffn_attention_plan_bytes",
+           "skipffn_attention_create", "skipffn_attention_destroy", "skipffn_attention_forward",
+           "skipffn_attention_scratch_bytes", "skipffn_attention_backward", "skipffn_attention_poll",
+           "skipffn_layernorm_forward", "skipffn_layernorm_scratch_bytes", "skipffn_layernorm_backward"]
 STATIC_MAX_TOKENS = 65536   # SKIPFFN_STATIC_MAX_TOKENS
 
 TUNABLES = {"tile_n": 0, "streamk": 1, "stages": 2, "lose_handover": 3, "one_box": 4, "tma_stores": 5, "gather": 6,
@@ -42,6 +45,12 @@ class _Config(ctypes.Structure):
                 ("dense", ctypes.c_int32), ("grad_dtype_fp32", ctypes.c_int32),
                 ("accumulate_dw", ctypes.c_int32), ("path", ctypes.c_int32),
                 ("prenorm", ctypes.c_int32), ("debug", ctypes.c_int32), ("recompute", ctypes.c_int32)]
+
+
+class _AttentionConfig(ctypes.Structure):
+    _fields_ = [("heads_q", ctypes.c_int32), ("heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32), ("path", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
 
 
 def load_library() -> ctypes.CDLL:
@@ -113,6 +122,27 @@ def load_library() -> ctypes.CDLL:
     lib.skipffn_token_merge.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.skipffn_token_merge_poll.restype = i32
     lib.skipffn_token_merge_poll.argtypes = [vp, i64, i32, i32, i32, vp, ctypes.POINTER(i32)]
+    acfgp = ctypes.POINTER(_AttentionConfig)
+    lib.skipffn_attention_plan_bytes.restype = ctypes.c_size_t
+    lib.skipffn_attention_plan_bytes.argtypes = [acfgp, vp, i32]
+    lib.skipffn_attention_create.restype = i32
+    lib.skipffn_attention_create.argtypes = [ctypes.POINTER(vp), acfgp, vp, i32, vp, ctypes.c_size_t, vp]
+    lib.skipffn_attention_destroy.restype = None
+    lib.skipffn_attention_destroy.argtypes = [vp]
+    lib.skipffn_attention_forward.restype = i32
+    lib.skipffn_attention_forward.argtypes = [vp] + [vp, i64] * 4 + [vp, vp]
+    lib.skipffn_attention_scratch_bytes.restype = ctypes.c_size_t
+    lib.skipffn_attention_scratch_bytes.argtypes = [vp]
+    lib.skipffn_attention_backward.restype = i32
+    lib.skipffn_attention_backward.argtypes = [vp] + [vp, i64] * 5 + [vp] + [vp, i64] * 3 + [vp, ctypes.c_size_t, vp]
+    lib.skipffn_attention_poll.restype = i32
+    lib.skipffn_attention_poll.argtypes = [vp, vp, ctypes.POINTER(i32)]
+    lib.skipffn_layernorm_forward.restype = i32
+    lib.skipffn_layernorm_forward.argtypes = [vp, vp, vp, i64, i32, i32, ctypes.c_float, vp, vp, vp, vp]
+    lib.skipffn_layernorm_scratch_bytes.restype = ctypes.c_size_t
+    lib.skipffn_layernorm_scratch_bytes.argtypes = [i32]
+    lib.skipffn_layernorm_backward.restype = i32
+    lib.skipffn_layernorm_backward.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
     lib.skipffn_strerror.restype = ctypes.c_char_p
     lib.skipffn_strerror.argtypes = [i32]
     _lib = lib
@@ -216,6 +246,71 @@ def summary_backward(X, seg_offsets, w, probs, dxs, dw_fp32=False):
     return dX, dw
 
 
+def _on_device(fn, device, *args):
+    """Call a library function with `device` current and its current stream as the last argument."""
+    import torch
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        return fn(*args, stream)
+    with torch.cuda.device(device):
+        return fn(*args, stream)
+
+
+def _layernorm_rows(x, name, like=None):
+    """Checks a ``[..., C]`` tensor of packed rows; returns (dtype, rows, C)."""
+    import torch
+    if not x.is_cuda or not x.is_contiguous() or x.dim() < 1 or x.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"{name} must be a contiguous bf16 or fp32 CUDA tensor")
+    if like is not None and (x.shape != like.shape or x.dtype != like.dtype or x.device != like.device):
+        raise ValueError(f"{name} must have the shape, dtype and device of x")
+    C = x.shape[-1]
+    return BF16 if x.dtype == torch.bfloat16 else FP32, x.numel() // C if C else 0, C
+
+
+def _layernorm_vec(t, name, n, dtype, device):
+    if t.dtype != dtype or t.device != device or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} entries on {device}")
+    return t.data_ptr()
+
+
+def layernorm_forward(x, gamma, beta=None, eps: float = 1e-5, out=None):
+    """Layer normalisation of the rows of ``x [..., C]`` (``skipffn_layernorm_forward``): ``(y, mean, rstd)``,
+    the last two fp32 with one entry per row, which is what the backward needs.  ``out`` may be ``x``."""
+    import torch
+    dtype, n, C = _layernorm_rows(x, "x")
+    g = _layernorm_vec(gamma, "gamma", C, x.dtype, x.device)
+    b = None if beta is None else _layernorm_vec(beta, "beta", C, x.dtype, x.device)
+    y = torch.empty_like(x) if out is None else out
+    _layernorm_rows(y, "out", x)
+    mean, rstd = torch.empty((2, n), dtype=torch.float32, device=x.device).unbind(0)
+    st = _on_device(load_library().skipffn_layernorm_forward, x.device, x.data_ptr(), g, b, n, C, dtype, float(eps), y.data_ptr(),
+                    mean.data_ptr(), rstd.data_ptr())
+    if st != 0:
+        raise SkipFFNError(st, "skipffn_layernorm_forward")
+    return y, mean, rstd
+
+
+def layernorm_backward(dy, x, gamma, mean, rstd, dw_fp32: bool = False, dx=None):
+    """``(dx, dgamma, dbeta)`` of ``layernorm_forward`` (``skipffn_layernorm_backward``); ``dx`` may be ``dy``."""
+    import torch
+    lib = load_library()
+    dtype, n, C = _layernorm_rows(x, "x")
+    _layernorm_rows(dy, "dy", x)
+    g = _layernorm_vec(gamma, "gamma", C, x.dtype, x.device)
+    m = _layernorm_vec(mean, "mean", n, torch.float32, x.device)
+    r = _layernorm_vec(rstd, "rstd", n, torch.float32, x.device)
+    dx = torch.empty_like(x) if dx is None else dx
+    _layernorm_rows(dx, "dx", x)
+    dgamma, dbeta = torch.empty((2, C), dtype=torch.float32 if dw_fp32 else x.dtype, device=x.device).unbind(0)
+    nbytes = int(lib.skipffn_layernorm_scratch_bytes(C))
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    st = _on_device(lib.skipffn_layernorm_backward, x.device, dy.data_ptr(), x.data_ptr(), g, m, r, n, C, dtype, dx.data_ptr(),
+                    dgamma.data_ptr(), dbeta.data_ptr(), int(dw_fp32), scratch.data_ptr(), nbytes)
+    if st != 0:
+        raise SkipFFNError(st, "skipffn_layernorm_backward")
+    return dx, dgamma, dbeta
+
+
 def token_merge(X, k: int, poll: bool = False):
     """Token merge of section 4.1 (``skipffn_token_merge``): ``(kept [k], assign [n], merged [k, C])``
     for the tokens ``X [n, C]`` (bf16 or fp32 CUDA tensor).  ``poll=True`` synchronises the stream
@@ -241,6 +336,119 @@ def token_merge(X, k: int, poll: bool = False):
         if st != 0:
             raise SkipFFNError(st, f"skipffn_token_merge_poll (site {site.value})")
     return kept, assign, merged
+
+
+class PackedAttention:
+    """Attention over a packed batch (``skipffn_attention_*``), forward and backward.
+
+    ``cu_seqlens``: ascending host offsets ``[n_seq + 1]`` (list, tuple or CPU tensor), first 0; the packing is
+    checked and laid out once and serves every layer of a step.  ``q`` is ``[tokens, heads_q, head_dim]``,
+    ``k`` and ``v`` ``[tokens, heads_kv, head_dim]``, with at least ``cu_seqlens[-1]`` tokens (rows behind
+    the last sequence are neither read nor written), contiguous heads and any token stride that is a multiple of
+    16 bytes, so slices of one fused projection need no copy.  ``causal=False`` attends to the whole
+    sequence; ``scale`` defaults to ``head_dim ** -0.5``.  Work is enqueued on the current torch stream;
+    one object may serve several streams."""
+
+    def __init__(self, cu_seqlens, heads_q: int, heads_kv: int, head_dim: int, dtype: int = BF16, causal: bool = True,
+                 scale: Optional[float] = None, path: int = PATH_DEFAULT, device="cuda"):
+        import torch
+        if not torch.cuda.is_available():
+            raise RuntimeError("packed attention needs a CUDA device (sm_100a); there is no CPU path")
+        self._torch, self.lib = torch, load_library()
+        self.heads_q, self.heads_kv, self.head_dim = int(heads_q), int(heads_kv), int(head_dim)
+        self.torch_dtype = torch.bfloat16 if dtype == BF16 else torch.float32
+        self._align = 8 if dtype == BF16 else 4
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        vals = [int(v) for v in cu_seqlens]
+        if any(not 0 <= v < 1 << 31 for v in vals):
+            raise ValueError("cu_seqlens must be offsets that fit 32 bits")
+        n_seq = len(vals) - 1
+        self.tokens = vals[-1] if vals else 0
+        cu = (ctypes.c_int32 * max(len(vals), 1))(*vals)
+        cfg = _AttentionConfig(self.heads_q, self.heads_kv, self.head_dim, int(dtype), int(bool(causal)), int(path),
+                               float(head_dim) ** -0.5 if scale is None else float(scale))
+        self._handle = ctypes.c_void_p()
+        nbytes = int(self.lib.skipffn_attention_plan_bytes(ctypes.byref(cfg), cu, n_seq))
+        self._plan = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self.device)
+        with torch.cuda.device(self.device):
+            st = self.lib.skipffn_attention_create(ctypes.byref(self._handle), ctypes.byref(cfg), cu, n_seq, _ptr(self._plan),
+                                                   self._plan.numel(), self._stream())
+        if st != 0:
+            raise SkipFFNError(st, "skipffn_attention_create")
+        self.scratch_bytes = int(self.lib.skipffn_attention_scratch_bytes(self._handle))
+
+    def __del__(self):
+        if getattr(self, "_handle", None) and self._handle.value:
+            self.lib.skipffn_attention_destroy(self._handle)
+            self._handle = ctypes.c_void_p()
+
+    def _stream(self):
+        return self._torch.cuda.current_stream(self.device).cuda_stream
+
+    def _arg(self, t, name, heads):
+        """(address, token stride) of a [tokens, heads, head_dim] tensor, checked."""
+        shape = t.shape
+        if t.dtype != self.torch_dtype or t.device != self.device:
+            raise ValueError(f"{name} must be a {self.torch_dtype} tensor on {self.device}")
+        if len(shape) != 3 or shape[0] < self.tokens or shape[1] != heads or shape[2] != self.head_dim:
+            raise ValueError(f"{name} must have shape [>= {self.tokens}, {heads}, {self.head_dim}], got {list(shape)}")
+        ld, sh, sd = t.stride()
+        if sd != 1 or (heads > 1 and sh != self.head_dim):
+            raise ValueError(f"{name} must have contiguous heads")
+        return t.data_ptr(), ld if shape[0] > 1 else heads * self.head_dim
+
+    def _call(self, name, *args):
+        torch = self._torch
+        fn = getattr(self.lib, name)
+        if torch.cuda.current_device() == self.device.index:
+            st = fn(self._handle, *args, self._stream())
+        else:
+            with torch.cuda.device(self.device):
+                st = fn(self._handle, *args, self._stream())
+        if st != 0:
+            raise SkipFFNError(st, name)
+
+    def forward(self, q, k, v, out=None, lse=None):
+        """``(out [tokens, heads_q, head_dim], lse [tokens, heads_q] fp32)``.  ``out`` and ``lse`` may be given."""
+        torch = self._torch
+        args = self._arg(q, "q", self.heads_q) + self._arg(k, "k", self.heads_kv) + self._arg(v, "v", self.heads_kv)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        self._check_lse(lse)
+        self._call("skipffn_attention_forward", *args, *self._arg(out, "out", self.heads_q), lse.data_ptr())
+        return out, lse
+
+    def _check_lse(self, lse):
+        if (lse.dtype != self._torch.float32 or lse.device != self.device or lse.dim() != 2 or lse.shape[0] < self.tokens
+                or lse.shape[1] != self.heads_q or not lse.is_contiguous()):
+            raise ValueError(f"lse must be a contiguous float32 tensor [>= {self.tokens}, {self.heads_q}] on {self.device}")
+
+    def backward(self, dout, q, k, v, out, lse, dq=None, dk=None, dv=None):
+        """``(dq, dk, dv)`` from the forward's inputs and results; the three may be given (slices of one
+        fused gradient, say) but must not overlap the inputs."""
+        torch = self._torch
+        hq, hk = self.heads_q, self.heads_kv
+        args = (self._arg(dout, "dout", hq) + self._arg(q, "q", hq) + self._arg(k, "k", hk) + self._arg(v, "v", hk)
+                + self._arg(out, "out", hq))
+        self._check_lse(lse)
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+        dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
+        dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
+        scratch = torch.empty(max(self.scratch_bytes, 16), dtype=torch.uint8, device=self.device)
+        self._call("skipffn_attention_backward", *args, lse.data_ptr(), *self._arg(dq, "dq", hq), *self._arg(dk, "dk", hk),
+                   *self._arg(dv, "dv", hk), scratch.data_ptr(), scratch.numel())
+        return dq, dk, dv
+
+    def poll(self):
+        """Synchronise the stream and raise if a kernel reported a device-side problem."""
+        site = ctypes.c_int32(0)
+        st = self.lib.skipffn_attention_poll(self._handle, self._stream(), ctypes.byref(site))
+        if st != 0:
+            raise SkipFFNError(st, f"skipffn_attention_poll (site {site.value})")
 
 
 def skipffn_compact_static(skip_mask, idx, nk) -> None:

@@ -10,7 +10,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libskipffn.so")
 # the same library with per-role cycle counters in the tensor-core GEMM kernels (bench.py --role-cycles)
 LIB_ROLE_CYCLES = os.path.join(HERE, "libskipffn_role_cycles.so")
-SOURCES = ["api.cu", "compact.cu", "compact_static.cu", "kvcache.cu", "merge.cu", "prenorm.cu", "simt.cu", "summary.cu", "umma.cu"]
+SOURCES = ["api.cu", "attention.cu", "attention_simt.cu", "attention_tc.cu", "compact.cu", "compact_static.cu", "kvcache.cu",
+           "layernorm.cu", "merge.cu", "prenorm.cu", "simt.cu", "summary.cu", "umma.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC"]
 

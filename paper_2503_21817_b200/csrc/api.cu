@@ -641,6 +641,47 @@ skipffn_status skipffn_summary_backward(const void *X, const int32_t *seg_offset
                                    (float *)scratch, (cudaStream_t)stream) == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }
 
+static bool layernorm_args_ok(const void *x, const void *gamma, int64_t n_rows, int32_t C, int32_t dtype)
+{
+    return n_rows >= 0 && n_rows < ((int64_t)1 << 31) && C > 0 && (dtype == SKIPFFN_BF16 || dtype == SKIPFFN_FP32) && gamma &&
+           (n_rows == 0 || x) && aligned16(x) && aligned16(gamma);
+}
+
+// a and b are the same rows or share none of their bytes
+static bool same_or_apart(const void *a, const void *b, int64_t bytes)
+{
+    const char *p = (const char *)a, *q = (const char *)b;
+    return p == q || p + bytes <= q || q + bytes <= p;
+}
+
+skipffn_status skipffn_layernorm_forward(const void *x, const void *gamma, const void *beta, int64_t n_rows, int32_t C,
+                                         int32_t dtype, float eps, void *y, float *mean, float *rstd, void *stream)
+{
+    if (!layernorm_args_ok(x, gamma, n_rows, C, dtype) || !(eps >= 0.0f)) return SKIPFFN_EINVAL;
+    if (C % 8 || C > LN_MAX_C) return SKIPFFN_EUNSUPPORTED;
+    if ((n_rows > 0 && !y) || !aligned16(y) || !aligned16(beta)) return SKIPFFN_EINVAL;
+    if (!same_or_apart(x, y, n_rows * C * (dtype == SKIPFFN_BF16 ? 2 : 4))) return SKIPFFN_EINVAL;
+    return launch_layernorm_forward(x, gamma, beta, n_rows, C, dtype, eps, y, mean, rstd, (cudaStream_t)stream) == cudaSuccess
+               ? SKIPFFN_OK : SKIPFFN_ECUDA;
+}
+
+size_t skipffn_layernorm_scratch_bytes(int32_t C) { return C > 0 ? (size_t)LN_MAX_PARTS * 2 * C * sizeof(float) : 0; }
+
+skipffn_status skipffn_layernorm_backward(const void *dy, const void *x, const void *gamma, const float *mean, const float *rstd,
+                                          int64_t n_rows, int32_t C, int32_t dtype, void *dx, void *dgamma, void *dbeta,
+                                          int32_t dw_fp32, void *scratch, size_t scratch_bytes, void *stream)
+{
+    if (!layernorm_args_ok(x, gamma, n_rows, C, dtype)) return SKIPFFN_EINVAL;
+    if (C % 8 || C > LN_MAX_C) return SKIPFFN_EUNSUPPORTED;
+    if ((n_rows > 0 && (!dy || !dx || !mean || !rstd)) || !aligned16(dy) || !aligned16(dx) || !scratch || !aligned16(scratch))
+        return SKIPFFN_EINVAL;
+    const int64_t bytes = n_rows * C * (dtype == SKIPFFN_BF16 ? 2 : 4);
+    if (!same_or_apart(dx, x, bytes) || !same_or_apart(dx, dy, bytes)) return SKIPFFN_EINVAL;
+    if (scratch_bytes < skipffn_layernorm_scratch_bytes(C)) return SKIPFFN_EWORKSPACE;
+    return launch_layernorm_backward(dy, x, gamma, mean, rstd, n_rows, C, dtype, dx, dgamma, dbeta, dw_fp32, (float *)scratch,
+                                     (cudaStream_t)stream) == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
+}
+
 size_t skipffn_token_merge_scratch_bytes(int64_t n, int32_t C, int32_t k, int32_t dtype)
 {
     if (n <= 0 || C <= 0 || k <= 0 || k > n || (dtype != SKIPFFN_BF16 && dtype != SKIPFFN_FP32)) return 0;

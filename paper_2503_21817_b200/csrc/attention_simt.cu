@@ -1,0 +1,322 @@
+// Packed attention with plain fused multiply-adds (fp32, and bf16 as an on-device second opinion), and
+// the row statistics of the backward pass of both paths.
+#include "attention.cuh"
+
+namespace skipffn {
+
+namespace {
+
+constexpr int SR = AT_SIMT_ROWS, SK = AT_SIMT_KEYS;
+constexpr int ST_THREADS = 256;
+constexpr int PITCH = AT_MAX_D + 4, PPITCH = SK + 4;     // shared-memory row pitches (floats): no bank conflicts
+constexpr float LOG2E = 1.4426950408889634f;
+
+// Thread (ty, tx) of the 16 x 16 grid owns rows 4 ty .. 4 ty + 3 and columns tx + 16 j of a 64 x 64 product,
+// and rows 4 ty .. +3, columns 4 tx .. +3 and 64 + 4 tx .. +3 of a 64 x d accumulator.
+struct Tile { int ty, tx; };
+__device__ __forceinline__ Tile tile_of() { return {(int)threadIdx.x / 16, (int)threadIdx.x % 16}; }
+
+struct Item { int start, len, t0, base, h; };
+__device__ __forceinline__ Item item_of(const int4 *items, int hk)
+{
+    const int4 e = items[blockIdx.x / hk];
+    return {e.x, e.y, e.z, e.w, (int)(blockIdx.x % hk)};
+}
+
+// 64 rows of a [tokens, heads, d] array as fp32: tile row r is token `token` + r / group, head h group + r % group;
+// rows at or past `valid` read as zeros
+template <typename T>
+__device__ __forceinline__ void load_rows(float *dst, const T *src, int64_t ld, int64_t token, int head0, int group, int valid, int d)
+{
+    for (int i = threadIdx.x; i < SR * (AT_MAX_D / 4); i += ST_THREADS) {
+        const int r = i / (AT_MAX_D / 4), c = 4 * (i % (AT_MAX_D / 4));
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (r < valid && c < d) load4(src + (token + r / group) * ld + (int64_t)(head0 + r % group) * d + c, v);
+        store4(dst + r * PITCH + c, v);
+    }
+}
+// s[i][j] = sum_d a[4 ty + i][d] b[tx + 16 j][d]
+__device__ __forceinline__ void rows_rows(float (&s)[4][4], const float *a, const float *b, int d, Tile t)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] = 0.0f;
+    for (int c = 0; c < d; c += 4) {
+        float x[4][4], y[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { load4(a + (4 * t.ty + i) * PITCH + c, x[i]); load4(b + (t.tx + 16 * i) * PITCH + c, y[i]); }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[i][j] = fmaf(x[i][e], y[j][e], s[i][j]);
+    }
+}
+// acc[4 rows][8 columns] += w(row, k) b[k][columns]; TR: w is stored [k][row], else [row][k]
+template <bool TR>
+__device__ __forceinline__ void weights_rows(float (&acc)[4][8], const float *w, const float *b, int n, Tile t)
+{
+    for (int k = 0; k < n; ++k) {
+        float x[4], y[2][4];
+        if (TR) load4(w + k * PPITCH + 4 * t.ty, x);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = w[(4 * t.ty + i) * PPITCH + k];
+        load4(b + k * PITCH + 4 * t.tx, y[0]);
+        load4(b + k * PITCH + 64 + 4 * t.tx, y[1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(x[i], y[j / 4][j % 4], acc[i][j]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_acc(T *row, const float (&v)[8], float f, int d, Tile t)
+{
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+        if (64 * j + 4 * t.tx < d) {
+            const float o[4] = {v[4 * j] * f, v[4 * j + 1] * f, v[4 * j + 2] * f, v[4 * j + 3] * f};
+            store4(row + 64 * j + 4 * t.tx, o);
+        }
+}
+__device__ __forceinline__ float half_warp_max(float v)
+{
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+__device__ __forceinline__ float half_warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(ST_THREADS)
+k_attention_fwd_simt(const AttnArgs a)
+{
+    extern __shared__ float sm[];
+    float *qs = sm, *kv = qs + SR * PITCH, *ps = kv + SK * PITCH;
+    const Tile t = tile_of();
+    const Item it = item_of(a.fwd_items, a.hk);
+    const int valid = min(a.tokens, it.len - it.t0) * a.group;
+    const int end = a.causal ? min(it.t0 + a.tokens, it.len) : it.len;
+    load_rows(qs, (const T *)a.q, a.ldq, (int64_t)it.start + it.t0, it.h * a.group, a.group, valid, a.d);
+    float m[4], l[4] = {0.0f, 0.0f, 0.0f, 0.0f}, acc[4][8] = {};
+    int row_end[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        m[i] = -INFINITY;
+        row_end[i] = a.causal ? min(it.t0 + (4 * t.ty + i) / a.group + 1, it.len) : it.len;
+    }
+    for (int k0 = 0; k0 < end; k0 += SK) {
+        __syncthreads();
+        load_rows(kv, (const T *)a.k, a.ldk, (int64_t)it.start + k0, it.h, 1, min(SK, it.len - k0), a.d);
+        __syncthreads();
+        float s[4][4];
+        rows_rows(s, qs, kv, a.d, t);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float bm = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[i][j] = k0 + t.tx + 16 * j < row_end[i] ? s[i][j] * a.scale : -INFINITY;
+                bm = fmaxf(bm, s[i][j]);
+            }
+            const float mn = fmaxf(m[i], half_warp_max(bm)), f = k0 == 0 ? 0.0f : expf(m[i] - mn);
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float p = expf(s[i][j] - mn);
+                sum += p;
+                ps[(4 * t.ty + i) * PPITCH + t.tx + 16 * j] = p;
+            }
+            l[i] = l[i] * f + half_warp_sum(sum);
+            m[i] = mn;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[i][j] *= f;
+        }
+        __syncthreads();
+        load_rows(kv, (const T *)a.v, a.ldv, (int64_t)it.start + k0, it.h, 1, min(SK, it.len - k0), a.d);
+        __syncthreads();
+        weights_rows<false>(acc, ps, kv, min(SK, end - k0), t);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 4 * t.ty + i;
+        if (r >= valid) continue;
+        const int64_t tok = (int64_t)it.start + it.t0 + r / a.group;
+        const int head = it.h * a.group + r % a.group;
+        store_acc((T *)a.out + tok * a.ldo + (int64_t)head * a.d, acc[i], 1.0f / l[i], a.d, t);
+        if (t.tx == 0) a.lse[tok * a.hq + head] = m[i] + logf(l[i]);
+    }
+}
+
+// P and dS of one 64 x 64 tile into shared memory (rows = queries, columns = keys)
+__device__ __forceinline__ void grad_tile(float *ps, float *ds, const float *qs, const float *gs, const float *ks, const float *vs,
+                                          const float2 *stats, const AttnArgs &a, int t0, int len, int k0, Tile t)
+{
+    float s[4][4], dp[4][4];
+    rows_rows(s, qs, ks, a.d, t);
+    rows_rows(dp, gs, vs, a.d, t);
+    const float c2 = a.scale * LOG2E;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 4 * t.ty + i, row_end = a.causal ? min(t0 + r / a.group + 1, len) : len;
+        const float2 st = stats[r];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = t.tx + 16 * j;
+            const bool on = k0 + c < row_end;
+            const float p = on ? exp2f(fmaf(s[i][j], c2, -st.x)) : 0.0f;
+            ps[r * PPITCH + c] = p;
+            ds[r * PPITCH + c] = on ? p * (dp[i][j] - st.y) : 0.0f;
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(ST_THREADS)
+k_attention_bwd_kv_simt(const AttnArgs a)
+{
+    extern __shared__ float sm[];
+    float *ks = sm, *vs = ks + SK * PITCH, *qs = vs + SK * PITCH, *gs = qs + SR * PITCH, *ps = gs + SR * PITCH, *ds = ps + SR * PPITCH;
+    const Tile t = tile_of();
+    const Item it = item_of(a.key_items, a.hk);
+    const int k0 = it.t0, keys = min(SK, it.len - k0);
+    load_rows(ks, (const T *)a.k, a.ldk, (int64_t)it.start + k0, it.h, 1, keys, a.d);
+    load_rows(vs, (const T *)a.v, a.ldv, (int64_t)it.start + k0, it.h, 1, keys, a.d);
+    float dk[4][8] = {}, dv[4][8] = {};
+    for (int tile = a.causal ? k0 / a.tokens : 0; tile * a.tokens < it.len; ++tile) {
+        const int t0 = tile * a.tokens, valid = min(a.tokens, it.len - t0) * a.group;
+        __syncthreads();
+        load_rows(qs, (const T *)a.q, a.ldq, (int64_t)it.start + t0, it.h * a.group, a.group, valid, a.d);
+        load_rows(gs, (const T *)a.dout, a.lddo, (int64_t)it.start + t0, it.h * a.group, a.group, valid, a.d);
+        __syncthreads();
+        grad_tile(ps, ds, qs, gs, ks, vs, a.row_stats + ((int64_t)(it.base + tile) * a.hk + it.h) * SR, a, t0, it.len, k0, t);
+        __syncthreads();
+        weights_rows<true>(dv, ps, gs, valid, t);
+        weights_rows<true>(dk, ds, qs, valid, t);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int key = 4 * t.ty + i;
+        if (key >= keys) continue;
+        const int64_t tok = (int64_t)it.start + k0 + key;
+        store_acc((T *)a.dk + tok * a.lddk + (int64_t)it.h * a.d, dk[i], a.scale, a.d, t);
+        store_acc((T *)a.dv + tok * a.lddv + (int64_t)it.h * a.d, dv[i], 1.0f, a.d, t);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(ST_THREADS)
+k_attention_bwd_q_simt(const AttnArgs a)
+{
+    extern __shared__ float sm[];
+    float *ks = sm, *vs = ks + SK * PITCH, *qs = vs + SK * PITCH, *gs = qs + SR * PITCH, *ps = gs + SR * PITCH, *ds = ps + SR * PPITCH;
+    const Tile t = tile_of();
+    const Item it = item_of(a.row_items, a.hk);
+    const int valid = min(a.tokens, it.len - it.t0) * a.group, end = a.causal ? min(it.t0 + a.tokens, it.len) : it.len;
+    load_rows(qs, (const T *)a.q, a.ldq, (int64_t)it.start + it.t0, it.h * a.group, a.group, valid, a.d);
+    load_rows(gs, (const T *)a.dout, a.lddo, (int64_t)it.start + it.t0, it.h * a.group, a.group, valid, a.d);
+    const float2 *stats = a.row_stats + ((int64_t)(it.base + it.t0 / a.tokens) * a.hk + it.h) * SR;
+    float dq[4][8] = {};
+    for (int k0 = 0; k0 < end; k0 += SK) {
+        const int keys = min(SK, it.len - k0);
+        __syncthreads();
+        load_rows(ks, (const T *)a.k, a.ldk, (int64_t)it.start + k0, it.h, 1, keys, a.d);
+        load_rows(vs, (const T *)a.v, a.ldv, (int64_t)it.start + k0, it.h, 1, keys, a.d);
+        __syncthreads();
+        grad_tile(ps, ds, qs, gs, ks, vs, stats, a, it.t0, it.len, k0, t);
+        __syncthreads();
+        weights_rows<false>(dq, ds, ks, keys, t);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 4 * t.ty + i;
+        if (r >= valid) continue;
+        const int64_t tok = (int64_t)it.start + it.t0 + r / a.group;
+        store_acc((T *)a.dq + tok * a.lddq + (int64_t)(it.h * a.group + r % a.group) * a.d, dq[i], a.scale, a.d, t);
+    }
+}
+
+// (lse log2 e, delta = sum_d dout out) of every row of a row tile, one warp per row; rows that belong to no
+// token get (infinity, 0), which makes their P and dS zero.  Reads out and dout once: HBM-bound.
+template <typename T>
+__global__ void __launch_bounds__(ST_THREADS)
+k_attention_row_stats(const AttnArgs a, int rows)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const Item it = item_of(a.row_items, a.hk);
+    const int valid = min(a.tokens, it.len - it.t0) * a.group;
+    float2 *dst = a.row_stats + ((int64_t)(it.base + it.t0 / a.tokens) * a.hk + it.h) * rows;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll 4
+    for (int r = warp; r < rows; r += ST_THREADS / 32) {
+        float2 v = make_float2(INFINITY, 0.0f);
+        if (r < valid) {
+            const int64_t tok = (int64_t)it.start + it.t0 + r / a.group;
+            const int head = it.h * a.group + r % a.group;
+            float dot = 0.0f;
+            if (4 * lane < a.d) {
+                float x[4], y[4];
+                load4((const T *)a.out_in + tok * a.ldo + (int64_t)head * a.d + 4 * lane, x);
+                load4((const T *)a.dout + tok * a.lddo + (int64_t)head * a.d + 4 * lane, y);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dot = fmaf(x[e], y[e], dot);
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+            v = make_float2(a.lse[tok * a.hq + head] * LOG2E, dot);
+        }
+        if (lane == 0) dst[r] = v;
+    }
+}
+
+constexpr int FWD_SMEM = (SR * PITCH + SK * PITCH + SR * PPITCH) * 4;
+constexpr int BWD_SMEM = (2 * SR * PITCH + 2 * SK * PITCH + 2 * SR * PPITCH) * 4;
+
+template <typename Kernel>
+static cudaError_t launch(Kernel kern, int n, int smem, const AttnArgs &a, cudaStream_t s)
+{
+    if (n <= 0) return cudaSuccess;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    kern<<<(unsigned)n, ST_THREADS, smem, s>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_attention_simt_forward(const AttnArgs &a, int dtype, cudaStream_t s)
+{
+    return dtype == SKIPFFN_BF16 ? launch(k_attention_fwd_simt<bf16>, a.n_fwd * a.hk, FWD_SMEM, a, s)
+                                 : launch(k_attention_fwd_simt<float>, a.n_fwd * a.hk, FWD_SMEM, a, s);
+}
+
+cudaError_t launch_attention_row_stats(const AttnArgs &a, int dtype, int rows_per_tile, cudaStream_t s)
+{
+    const int n = a.n_rows * a.hk;
+    if (n <= 0) return cudaSuccess;
+    return dtype == SKIPFFN_BF16 ? launch_pdl(k_attention_row_stats<bf16>, dim3((unsigned)n), dim3(ST_THREADS), s, a, rows_per_tile)
+                                 : launch_pdl(k_attention_row_stats<float>, dim3((unsigned)n), dim3(ST_THREADS), s, a, rows_per_tile);
+}
+
+cudaError_t launch_attention_simt_backward(const AttnArgs &a, int dtype, cudaStream_t s)
+{
+    cudaError_t e = launch_attention_row_stats(a, dtype, SR, s);
+    if (e != cudaSuccess) return e;
+    const bool b = dtype == SKIPFFN_BF16;
+    e = b ? launch(k_attention_bwd_kv_simt<bf16>, a.n_keys * a.hk, BWD_SMEM, a, s)
+          : launch(k_attention_bwd_kv_simt<float>, a.n_keys * a.hk, BWD_SMEM, a, s);
+    if (e != cudaSuccess) return e;
+    return b ? launch(k_attention_bwd_q_simt<bf16>, a.n_rows * a.hk, BWD_SMEM, a, s)
+             : launch(k_attention_bwd_q_simt<float>, a.n_rows * a.hk, BWD_SMEM, a, s);
+}
+
+}  // namespace skipffn

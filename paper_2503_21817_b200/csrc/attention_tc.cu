@@ -1,0 +1,1048 @@
+// Packed attention on the tensor cores (bf16, sm_100a): forward, key / value gradient, query gradient.
+#include "attention.cuh"
+#include "ptx.cuh"
+
+namespace skipffn {
+
+namespace {
+
+constexpr int TILE = 128;                    // rows of a row tile = keys of a key tile
+constexpr int AT_TMEM_COLS = 512;
+constexpr int AT_THREADS = 384;              // 8 arithmetic warps, TMA, MMA, tail cleaner, one idle
+constexpr int W_TMA = 8, W_MMA = 9, W_TAIL = 10;
+// Registers: 384 x 168 at launch, moved from the four service warps to the eight arithmetic warps
+// (128 x 88 + 256 x 208 = the same 64512).
+constexpr int AT_REGS_SERVICE = 88, AT_REGS_ARITH = 208;
+constexpr float LOG2E = 1.4426950408889634f;
+
+template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// Bounded wait, inlined: a kernel that moves registers between its warps cannot call functions.
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status, int site)
+{
+    if (mbar_try_wait(bar, parity)) return true;
+    const unsigned long long t0 = globaltimer_ns();
+    for (uint32_t it = 1;; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((it & 0xf) == 0) {
+            if (*abort_flag) return false;
+            if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) {
+                *abort_flag = 1;
+                if (atomicCAS(&status[ST_STATUS], 0, (int)SKIPFFN_ETIMEOUT) == 0) status[ST_SITE] = site;
+                return false;
+            }
+        }
+    }
+}
+
+struct AtParams {
+    const int4 *items;
+    int32_t n_items;                         // list entries x kv heads
+    int32_t hq, hk, group, tokens, d, causal;
+    float scale, c2;                         // c2 = scale * log2 e
+    int64_t ld0, ld1;                        // token strides of the outputs
+    bf16 *out0, *out1;
+    float *lse;
+    const float2 *row_stats;
+    int32_t *status;
+};
+struct alignas(64) AtMaps { CUtensorMap q, k, v, g; };
+
+template <int DP> constexpr int tile_bytes() { return TILE * DP * 2; }
+
+// Work items are sorted by falling work; CTA b takes items b, 2 grid - 1 - b, 2 grid + b, ... (the
+// order of a round is reversed every other time), which evens out the sums.
+struct ItemLoop {
+    int round = 0, n;
+    __device__ explicit ItemLoop(int n_) : n(n_) {}
+    __device__ int next()
+    {
+        const int g = (int)gridDim.x, b = (int)blockIdx.x;
+        const int i = round * g + ((round & 1) ? g - 1 - b : b);
+        ++round;
+        return i < n ? i : -1;
+    }
+};
+
+__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+// columns of a 128-wide tile that an MMA has to cover when `valid` of them (>= 1) mean something
+__device__ __forceinline__ int mma_cols(int valid) { return valid >= TILE ? TILE : (valid + 15) & ~15; }
+
+// Row r of a stored 128-byte-swizzled tile keeps its 128 bytes inside the row, so rows can be zeroed
+// without undoing the swizzle.  One warp zeroes rows lo .. hi-1 of every 64-wide slab.
+template <int DP> __device__ __forceinline__ void zero_rows(uint32_t tile, int lo, int hi, int lane)
+{
+    for (int i = lane; i < (hi - lo) * 8; i += 32)
+#pragma unroll
+        for (int s = 0; s < DP / 64; ++s)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + s * (TILE * 128) + lo * 128 + i * 16), "r"(0)
+                         : "memory");
+}
+__device__ __forceinline__ void zero_smem(uint32_t addr, int bytes)
+{
+    for (int i = threadIdx.x * 16; i < bytes; i += AT_THREADS * 16)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(addr + i), "r"(0) : "memory");
+}
+
+// A tile of [rows][head][token] boxes: one TMA box per 64-wide slab (columns past d read as zeros).
+template <int DP>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, int head, int token, uint32_t bar)
+{
+#pragma unroll
+    for (int s = 0; s < DP / 64; ++s) tma_load_3d(dst + s * (TILE * 128), map, 64 * s, head, token, bar);
+}
+
+// D[128 x n] = A[128 x DP] B[n x DP]^T, both K-major in shared memory
+template <int DP> __device__ __forceinline__ void mma_rows_rows(uint32_t d_tmem, uint32_t a, uint32_t b, int n)
+{
+    const uint64_t da = make_desc(a, 16, 1024), db = make_desc(b, 16, 1024);
+    const uint32_t idesc = make_idesc(0, 0, 128, n);
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) {
+        const uint64_t off = (uint64_t)((k / 4) * (TILE * 128 >> 4) + (k % 4) * 2);
+        umma_bf16(d_tmem, da + off, db + off, idesc, k != 0);
+    }
+}
+// D[128 x DP] (+)= A[128 x rows] B[rows x DP], A in tensor memory (16 columns of A take 8 tensor-memory
+// columns; the second half of A starts at `a_hi`), B = a stored tile read across its rows (MN-major)
+template <int DP>
+__device__ __forceinline__ void mma_tmem_rows(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b, int rows, bool acc)
+{
+    const uint64_t db = make_desc(b, TILE * 128, 1024);
+    const uint32_t idesc = make_idesc(0, 1, 128, DP);
+#pragma unroll
+    for (int k = 0; k < TILE / 16; ++k)
+        if (16 * k < rows)
+            umma_bf16_ta(d_tmem, k < 4 ? a_lo + 8 * k : a_hi + 8 * (k - 4), db + (uint64_t)(k * (16 * 128 >> 4)), idesc, acc || k != 0);
+}
+
+// 32 fp32 values of one row times `f`, to bf16, to columns c .. c+31 (below d) of a global row
+__device__ __forceinline__ void store_row32(bf16 *row, const uint32_t (&v)[32], float f, int c, int d)
+{
+#pragma unroll
+    for (int i = 0; i < 32; i += 8)
+        if (c + i < d) {
+            uint4 w;
+            w.x = pack_bf16(__uint_as_float(v[i]) * f, __uint_as_float(v[i + 1]) * f);
+            w.y = pack_bf16(__uint_as_float(v[i + 2]) * f, __uint_as_float(v[i + 3]) * f);
+            w.z = pack_bf16(__uint_as_float(v[i + 4]) * f, __uint_as_float(v[i + 5]) * f);
+            w.w = pack_bf16(__uint_as_float(v[i + 6]) * f, __uint_as_float(v[i + 7]) * f);
+            *reinterpret_cast<uint4 *>(row + c + i) = w;
+        }
+}
+
+__device__ __forceinline__ uint32_t align_tiles(const uint8_t *raw) { return (smem_u32(raw) + 1023u) & ~1023u; }
+
+// Ends of every kernel: drain after an abort, give the tensor memory back.
+__device__ __forceinline__ void cta_teardown(volatile int *abort_flag, uint32_t tmem_base)
+{
+    if (*abort_flag) {
+        const unsigned long long t0 = globaltimer_ns();
+        while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if ((threadIdx.x >> 5) == W_MMA) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, AT_TMEM_COLS);
+    }
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------------------------ forward
+// One item = two row tiles (2 x 128 rows) of one kv head against the keys of their sequence, by one
+// CTA; both tiles use every key / value tile that arrives.
+//   warps 0..3 / 4..7  softmax of row tile 0 / 1, one row per thread: running maximum and sum in
+//                      registers, P = 2^(c2 s - c2 m) packed to bf16 over the scores it came from
+//   TMA warp           ring of key and value tiles, query tiles
+//   MMA warp           S = Q K^T, O += P V (P read from tensor memory)
+//   tail warp          zeroes value rows past the sequence's end inside the last 16-row step: their P is
+//                      zero, but 0 * inf of a neighbour's (or of never-written) memory is not
+// The output is rescaled only when the running maximum has grown by more than 2^8 since the last
+// time (P stays below 2^8, far inside the range of bf16 and fp32).
+template <int DP> struct FwdShape {
+    static constexpr int T_BYTES = tile_bytes<DP>();
+    static constexpr int SLOTS = DP == 128 ? 5 : 8;
+    static constexpr int SMEM = (2 + SLOTS) * T_BYTES + 1024 + 512;
+};
+struct alignas(8) FwdCtl {
+    uint64_t q_full[2], q_empty[2], kv_full[8], kv_empty[8], tail[8], s_full[2], p_full[2], o_full[2], o_free[2];
+    uint32_t tmem_base;
+    volatile int abort_flag;
+};
+
+struct FwdItem {
+    int start, len, t0, h, nb0, nb1, end0, end1;   // key blocks and first key past the keys of the two tiles
+    __device__ FwdItem(const AtParams &p, int i)
+    {
+        const int4 e = p.items[i / p.hk];
+        h = i % p.hk;
+        start = e.x; len = e.y; t0 = e.z;
+        end0 = p.causal ? min(t0 + p.tokens, len) : len;
+        end1 = t0 + p.tokens < len ? (p.causal ? min(t0 + 2 * p.tokens, len) : len) : 0;
+        nb0 = ceil_div(end0, TILE);
+        nb1 = ceil_div(end1, TILE);
+    }
+    __device__ int blocks() const { return max(nb0, nb1); }
+    // the last value tile holds rows past the sequence that an MMA step would read
+    __device__ bool dirty_tail() const { return (len & 15) != 0 && blocks() * TILE > len; }
+};
+
+template <int DP>
+__global__ void __launch_bounds__(AT_THREADS, 1)
+k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
+{
+    constexpr int T_BYTES = FwdShape<DP>::T_BYTES, SLOTS = FwdShape<DP>::SLOTS;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t tiles = align_tiles(smem_raw), q_tile = tiles, ring = tiles + 2 * T_BYTES;
+    FwdCtl *ctl = reinterpret_cast<FwdCtl *>(smem_raw + (tiles - smem_u32(smem_raw)) + (2 + SLOTS) * T_BYTES);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&ctl->q_full[i]), 1);
+            mbar_init(smem_u32(&ctl->q_empty[i]), 1);
+            mbar_init(smem_u32(&ctl->s_full[i]), 1);
+            mbar_init(smem_u32(&ctl->p_full[i]), 4);
+            mbar_init(smem_u32(&ctl->o_full[i]), 1);
+            mbar_init(smem_u32(&ctl->o_free[i]), 4);
+        }
+        for (int i = 0; i < SLOTS; ++i) {
+            mbar_init(smem_u32(&ctl->kv_full[i]), 1);
+            mbar_init(smem_u32(&ctl->kv_empty[i]), 1);
+            mbar_init(smem_u32(&ctl->tail[i]), 1);
+        }
+        ctl->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    const int used = p.group * p.tokens;     // rows of a tile that a box fills; the others stay zero
+    if (used < TILE) zero_smem(q_tile, 2 * T_BYTES);
+    fence_proxy_async_smem();
+    if (warp == W_MMA) { tmem_alloc(smem_u32(&ctl->tmem_base), AT_TMEM_COLS); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = ctl->tmem_base;
+    volatile int *ab = &ctl->abort_flag;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    ItemLoop loop(p.n_items);
+
+    if (warp >= W_TMA) regs_down<AT_REGS_SERVICE>();
+    if (warp == W_TMA) {
+        if (lane == 0) {
+            uint32_t pos = 0, nq[2] = {0, 0};
+            bool ok = true;
+            auto acquire = [&]() {           // next ring slot, free to be written
+                const uint32_t s = pos % SLOTS;
+                ok = ok && wait_bar(smem_u32(&ctl->kv_empty[s]), ((pos / SLOTS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                ++pos;
+                return s;
+            };
+            auto load_q = [&](const FwdItem &it, int g) {
+                ok = ok && wait_bar(smem_u32(&ctl->q_empty[g]), (nq[g] & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                if (!ok) return;
+                const uint32_t bar = smem_u32(&ctl->q_full[g]);
+                mbar_expect_tx(bar, (uint32_t)(used * DP * 2));
+                load_tile<DP>(q_tile + g * T_BYTES, &tm.q, it.h * p.group, it.start + it.t0 + g * p.tokens, bar);
+                ++nq[g];
+            };
+            for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
+                const FwdItem it(p, i);
+                const int n = it.blocks();
+                load_q(it, 0);
+                for (int j = 0; j < n && ok; ++j) {
+                    uint32_t s = acquire();
+                    if (!ok) break;
+                    uint32_t bar = smem_u32(&ctl->kv_full[s]);
+                    mbar_expect_tx(bar, T_BYTES);
+                    load_tile<DP>(ring + s * T_BYTES, &tm.k, it.h, it.start + j * TILE, bar);
+                    if (j == 0 && it.nb1) load_q(it, 1);
+                    s = acquire();
+                    if (!ok) break;
+                    // the tail warp passes a tile with rows to zero on to the MMA warp
+                    bar = smem_u32(j == n - 1 && it.dirty_tail() ? &ctl->tail[s] : &ctl->kv_full[s]);
+                    mbar_expect_tx(bar, T_BYTES);
+                    load_tile<DP>(ring + s * T_BYTES, &tm.v, it.h, it.start + j * TILE, bar);
+                }
+            }
+        }
+    } else if (warp == W_TAIL) {
+        uint32_t pos = 0, seen = 0;          // bit s: parity of the tail events of slot s
+        bool ok = true;
+        for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
+            const FwdItem it(p, i);
+            const int n = it.blocks();
+            pos += 2 * n;
+            if (!it.dirty_tail()) continue;
+            const uint32_t s = (pos - 1) % SLOTS;
+            ok = wait_bar(smem_u32(&ctl->tail[s]), (seen >> s) & 1, ab, p.status, SITE_PRODUCER_EMPTY);
+            if (!ok) break;
+            seen ^= 1u << s;
+            const int valid = it.len - (n - 1) * TILE;
+            zero_rows<DP>(ring + s * T_BYTES, valid, mma_cols(valid), lane);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctl->kv_full[s]));
+        }
+    } else if (warp == W_MMA) {
+        if (lane == 0) {
+            uint32_t base = 0, nq[2] = {0, 0}, np[2] = {0, 0};
+            bool ok = true;
+            auto wait_slot = [&](uint32_t n) {
+                ok = ok && wait_bar(smem_u32(&ctl->kv_full[n % SLOTS]), (n / SLOTS) & 1, ab, p.status, SITE_MMA_FULL);
+                return ring + (n % SLOTS) * T_BYTES;
+            };
+            for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
+                const FwdItem it(p, i);
+                const int n = it.blocks();
+                auto scores = [&](int g, int j, uint32_t k_tile) {
+                    const int end = g ? it.end1 : it.end0;
+                    mma_rows_rows<DP>(tmem + g * TILE, q_tile + g * T_BYTES, k_tile, mma_cols(end - j * TILE));
+                    umma_commit(smem_u32(&ctl->s_full[g]));
+                    if (j == (g ? it.nb1 : it.nb0) - 1) umma_commit(smem_u32(&ctl->q_empty[g]));
+                };
+                uint32_t kt = wait_slot(base);
+                for (int g = 0; g < 2 && ok; ++g) {
+                    if (g && !it.nb1) break;
+                    ok = wait_bar(smem_u32(&ctl->q_full[g]), nq[g] & 1, ab, p.status, SITE_MMA_FULL);
+                    if (!ok) break;
+                    ++nq[g];
+                    tc_fence_after();
+                    scores(g, 0, kt);
+                }
+                if (!ok) break;
+                umma_commit(smem_u32(&ctl->kv_empty[base % SLOTS]));
+                for (int j = 0; j < n && ok; ++j) {
+                    const uint32_t vt = wait_slot(base + 2 * j + 1);
+                    const bool more = j + 1 < n;
+                    kt = more ? wait_slot(base + 2 * j + 2) : 0;
+                    for (int g = 0; g < 2 && ok; ++g) {
+                        const int nb = g ? it.nb1 : it.nb0, end = g ? it.end1 : it.end0;
+                        if (j >= nb) continue;
+                        ok = wait_bar(smem_u32(&ctl->p_full[g]), np[g] & 1, ab, p.status, SITE_MMA_FULL);
+                        ++np[g];
+                        if (ok && j == 0)
+                            ok = wait_bar(smem_u32(&ctl->o_free[g]), (nq[g] - 1) & 1 ^ 1, ab, p.status, SITE_MMA_TMEM_EMPTY);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t pt = tmem + g * TILE;
+                        mma_tmem_rows<DP>(tmem + 2 * TILE + g * DP, pt, pt + 32, vt, mma_cols(end - j * TILE), j > 0);
+                        if (j == nb - 1) umma_commit(smem_u32(&ctl->o_full[g]));
+                        else scores(g, j + 1, kt);
+                    }
+                    if (!ok) break;
+                    umma_commit(smem_u32(&ctl->kv_empty[(base + 2 * j + 1) % SLOTS]));
+                    if (more) umma_commit(smem_u32(&ctl->kv_empty[(base + 2 * j + 2) % SLOTS]));
+                }
+                base += 2 * n;
+            }
+        }
+    } else if (warp < W_TMA) {
+        regs_up<AT_REGS_ARITH>();
+        const int g = warp >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t t_s = tmem + lanes + g * TILE, t_o = tmem + lanes + 2 * TILE + g * DP;
+        const uint32_t s_full = smem_u32(&ctl->s_full[g]), p_full = smem_u32(&ctl->p_full[g]);
+        uint32_t ns = 0, no = 0;
+        bool ok = true;
+        const int row_t = row / p.group, row_h = row - row_t * p.group;
+        for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
+            const FwdItem it(p, i);
+            const int nb = g ? it.nb1 : it.nb0, end = g ? it.end1 : it.end0, t0 = it.t0 + g * p.tokens;
+            if (nb == 0) continue;
+            const int token = t0 + row_t;
+            const int row_end = p.causal ? min(token + 1, it.len) : it.len;   // keys of this row
+            float m = -INFINITY, l = 0.0f;
+            for (int j = 0; j < nb; ++j) {
+                ok = wait_bar(s_full, ns & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ++ns;
+                if (!ok) break;
+                tc_fence_after();
+                const int cols = mma_cols(end - j * TILE);
+                uint32_t r[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (32 * c < cols) tmem_ld32(t_s + 32 * c, r[c]);
+                tmem_ld_wait();
+                // columns past the row's keys (or past the ones the MMA wrote) count as minus infinity
+                if (cols < TILE || j * TILE + TILE > (p.causal ? t0 + 1 : it.len)) {
+                    const int limit = row_end - j * TILE;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (32 * c + e >= limit) r[c][e] = 0xff800000u;
+                }
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2)
+                        mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(r[c][e])), __uint_as_float(r[c][e + 1]));
+                const float bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                if (j == 0) {
+                    m = bm;
+                } else if (__any_sync(0xffffffffu, (bm - m) * p.c2 > 8.0f)) {
+                    // S of this block was issued after the previous O += P V, so O is at rest
+                    const float mn = fmaxf(m, bm), f = fast_exp2((m - mn) * p.c2);
+                    m = mn;
+                    l *= f;
+#pragma unroll
+                    for (int c = 0; c < DP; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(t_o + c, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tmem_st32(t_o + c, o);
+                    }
+                }
+                const float mc = m * p.c2;
+                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if (32 * c < cols) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            const float a = fast_exp2(fmaf(__uint_as_float(r[c][e]), p.c2, -mc));
+                            const float b = fast_exp2(fmaf(__uint_as_float(r[c][e + 1]), p.c2, -mc));
+                            sum[e & 2 ? 1 : 0] += a;
+                            sum[e & 2 ? 3 : 2] += b;
+                            // P enters the second product in bf16: relative 2^-8 per term, averaged over the row
+                            pk[e / 2] = pack_bf16(a, b);
+                        }
+                        tmem_st16(t_s + 16 * c, pk);
+                    }
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full);
+            }
+            if (!ok) break;
+            ok = wait_bar(smem_u32(&ctl->o_full[g]), no & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+            ++no;
+            if (!ok) break;
+            tc_fence_after();
+            const bool live = row < used && token < it.len;
+            const float inv = 1.0f / l;
+            const int head = it.h * p.group + row_h;
+            const int64_t tok = (int64_t)it.start + token;
+            bf16 *dst = p.out0 + tok * p.ld0 + (int64_t)head * p.d;
+#pragma unroll
+            for (int c = 0; c < DP; c += 32) {
+                uint32_t o[32];
+                tmem_ld32(t_o + c, o);
+                tmem_ld_wait();
+                if (live) store_row32(dst, o, inv, c, p.d);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctl->o_free[g]));
+            if (live) p.lse[tok * p.hq + head] = fmaf(m, p.scale, logf(l));
+        }
+    }
+    cta_teardown(ab, tmem);
+}
+
+// ------------------------------------------------------------------------------------ dK, dV
+// One item = one key tile (128 keys) of one kv head against the row tiles that attend to it.  The
+// scores are computed transposed (keys on the accumulator rows), so that P^T and dS^T are already the
+// tensor-memory operands of dV += P^T dO and dK += dS^T Q.  The two warpgroups share the rows and
+// split the columns.  While the arithmetic warps turn scores into P, the tensor cores run the
+// previous dK and the next dP; while they turn dP into dS, dV and the next scores.
+// Sums over the query heads of a group are sums over tile rows: fixed order, no atomics.
+template <int DP> struct KvShape {
+    static constexpr int T_BYTES = tile_bytes<DP>();
+    static constexpr int STAGES = 2;
+    static constexpr int STAT_BYTES = TILE * 8;
+    static constexpr int SMEM = (2 + 2 * STAGES) * T_BYTES + STAGES * STAT_BYTES + 1024 + 512;
+};
+struct alignas(8) KvCtl {
+    uint64_t kv_full, kv_empty, q_full[2], g_full[2], empty[2], q_tail[2], g_tail[2];
+    uint64_t s_full, g_scores, p_ready, ds_ready, acc_full, acc_free;
+    uint32_t tmem_base;
+    volatile int abort_flag;
+};
+struct KvItem {
+    int start, len, k0, base, h, first, n;      // row tiles first .. first + n - 1 of the sequence
+    __device__ KvItem(const AtParams &p, int i)
+    {
+        const int4 e = p.items[i / p.hk];
+        h = i % p.hk;
+        start = e.x; len = e.y; k0 = e.z; base = e.w;
+        first = p.causal ? k0 / p.tokens : 0;
+        n = ceil_div(len, p.tokens) - first;
+    }
+    // tile rows that belong to tokens of the sequence (the others follow them)
+    __device__ int valid(const AtParams &p, int tile) const { return min(p.tokens, len - tile * p.tokens) * p.group; }
+    __device__ bool dirty(const AtParams &p, int tile) const
+    {
+        return len - tile * p.tokens < p.tokens && (valid(p, tile) & 15) != 0;
+    }
+};
+
+template <int DP>
+__global__ void __launch_bounds__(AT_THREADS, 1)
+k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
+{
+    using Sh = KvShape<DP>;
+    constexpr int T_BYTES = Sh::T_BYTES;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t tiles = align_tiles(smem_raw);
+    const uint32_t k_tile = tiles, v_tile = tiles + T_BYTES, q_ring = tiles + 2 * T_BYTES, g_ring = q_ring + 2 * T_BYTES;
+    const uint32_t stats = g_ring + 2 * T_BYTES;
+    uint8_t *after = smem_raw + (stats - smem_u32(smem_raw));
+    KvCtl *ctl = reinterpret_cast<KvCtl *>(after + Sh::STAGES * Sh::STAT_BYTES);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&ctl->q_full[i]), 1);
+            mbar_init(smem_u32(&ctl->g_full[i]), 1);
+            mbar_init(smem_u32(&ctl->q_tail[i]), 1);
+            mbar_init(smem_u32(&ctl->g_tail[i]), 1);
+            mbar_init(smem_u32(&ctl->empty[i]), 1);
+        }
+        mbar_init(smem_u32(&ctl->kv_full), 1);
+        mbar_init(smem_u32(&ctl->kv_empty), 1);
+        mbar_init(smem_u32(&ctl->s_full), 1);
+        mbar_init(smem_u32(&ctl->g_scores), 1);
+        mbar_init(smem_u32(&ctl->p_ready), 8);
+        mbar_init(smem_u32(&ctl->ds_ready), 8);
+        mbar_init(smem_u32(&ctl->acc_full), 1);
+        mbar_init(smem_u32(&ctl->acc_free), 8);
+        ctl->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    const int used = p.group * p.tokens;
+    if (used < TILE) zero_smem(q_ring, 4 * T_BYTES);
+    fence_proxy_async_smem();
+    if (warp == W_MMA) { tmem_alloc(smem_u32(&ctl->tmem_base), AT_TMEM_COLS); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = ctl->tmem_base;
+    volatile int *ab = &ctl->abort_flag;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    ItemLoop loop(p.n_items);
+    const uint32_t t_s = tmem, t_dp = tmem + TILE, t_dv = tmem + 2 * TILE, t_dk = t_dv + DP;
+
+    if (warp >= W_TMA) regs_down<AT_REGS_SERVICE>();
+    if (warp == W_TMA) {
+        if (lane == 0) {
+            uint32_t cnt = 0, items = 0;
+            bool ok = true;
+            for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
+                const KvItem it(p, i);
+                ok = wait_bar(smem_u32(&ctl->kv_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                if (!ok) break;
+                const uint32_t kvb = smem_u32(&ctl->kv_full);
+                mbar_expect_tx(kvb, 2 * T_BYTES);
+                load_tile<DP>(k_tile, &tm.k, it.h, it.start + it.k0, kvb);
+                load_tile<DP>(v_tile, &tm.v, it.h, it.start + it.k0, kvb);
+                for (int j = 0; j < it.n; ++j, ++cnt) {
+                    const uint32_t s = cnt & 1;
+                    ok = wait_bar(smem_u32(&ctl->empty[s]), ((cnt >> 1) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    if (!ok) break;
+                    const int tile = it.first + j, token = it.start + tile * p.tokens;
+                    const bool dirty = it.dirty(p, tile);
+                    const uint32_t qb = smem_u32(dirty ? &ctl->q_tail[s] : &ctl->q_full[s]);
+                    const uint32_t gb = smem_u32(dirty ? &ctl->g_tail[s] : &ctl->g_full[s]);
+                    mbar_expect_tx(qb, (uint32_t)(used * DP * 2) + Sh::STAT_BYTES);
+                    load_tile<DP>(q_ring + s * T_BYTES, &tm.q, it.h * p.group, token, qb);
+                    bulk_load(stats + s * Sh::STAT_BYTES, p.row_stats + ((int64_t)(it.base + tile) * p.hk + it.h) * TILE, Sh::STAT_BYTES, qb);
+                    mbar_expect_tx(gb, (uint32_t)(used * DP * 2));
+                    load_tile<DP>(g_ring + s * T_BYTES, &tm.g, it.h * p.group, token, gb);
+                }
+            }
+        }
+    } else if (warp == W_TAIL) {
+        uint32_t cnt = 0, seen = 0;
+        bool ok = true;
+        for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
+            const KvItem it(p, i);
+            cnt += it.n;
+            const int tile = it.first + it.n - 1;          // only a sequence's last row tile can be short
+            if (!it.dirty(p, tile)) continue;
+            const uint32_t s = (cnt - 1) & 1;
+            const int valid = it.valid(p, tile);
+            for (int w = 0; w < 2 && ok; ++w) {
+                ok = wait_bar(smem_u32(w ? &ctl->g_tail[s] : &ctl->q_tail[s]), (seen >> s) & 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                if (!ok) break;
+                zero_rows<DP>((w ? g_ring : q_ring) + s * T_BYTES, valid, min(mma_cols(valid), used), lane);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(w ? &ctl->g_full[s] : &ctl->q_full[s]));
+            }
+            seen ^= 1u << s;
+        }
+    } else if (warp == W_MMA) {
+        if (lane == 0) {
+            uint32_t cnt = 0, items = 0;
+            bool ok = true;
+            for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
+                const KvItem it(p, i);
+                auto cols_of = [&](int j) { return mma_cols(it.valid(p, it.first + j)); };
+                auto scores = [&](int j, uint32_t c) {
+                    ok = ok && wait_bar(smem_u32(&ctl->q_full[c & 1]), (c >> 1) & 1, ab, p.status, SITE_MMA_FULL);
+                    if (!ok) return;
+                    tc_fence_after();
+                    mma_rows_rows<DP>(t_s, k_tile, q_ring + (c & 1) * T_BYTES, cols_of(j));
+                    umma_commit(smem_u32(&ctl->s_full));
+                };
+                auto grad_scores = [&](int j, uint32_t c) {
+                    ok = ok && wait_bar(smem_u32(&ctl->g_full[c & 1]), (c >> 1) & 1, ab, p.status, SITE_MMA_FULL);
+                    if (!ok) return;
+                    tc_fence_after();
+                    mma_rows_rows<DP>(t_dp, v_tile, g_ring + (c & 1) * T_BYTES, cols_of(j));
+                    umma_commit(smem_u32(&ctl->g_scores));
+                };
+                ok = wait_bar(smem_u32(&ctl->kv_full), items & 1, ab, p.status, SITE_MMA_FULL);
+                scores(0, cnt);
+                grad_scores(0, cnt);
+                for (int j = 0; j < it.n && ok; ++j, ++cnt) {
+                    const uint32_t s = cnt & 1;
+                    ok = wait_bar(smem_u32(&ctl->p_ready), cnt & 1, ab, p.status, SITE_MMA_FULL);
+                    if (ok && j == 0)
+                        ok = wait_bar(smem_u32(&ctl->acc_free), (items & 1) ^ 1, ab, p.status, SITE_MMA_TMEM_EMPTY);
+                    if (!ok) break;
+                    tc_fence_after();
+                    mma_tmem_rows<DP>(t_dv, t_s, t_s + 64, g_ring + s * T_BYTES, cols_of(j), j > 0);
+                    if (j + 1 < it.n) scores(j + 1, cnt + 1);
+                    ok = ok && wait_bar(smem_u32(&ctl->ds_ready), cnt & 1, ab, p.status, SITE_MMA_FULL);
+                    if (!ok) break;
+                    tc_fence_after();
+                    mma_tmem_rows<DP>(t_dk, t_dp, t_dp + 64, q_ring + s * T_BYTES, cols_of(j), j > 0);
+                    umma_commit(smem_u32(&ctl->empty[s]));
+                    if (j + 1 < it.n) grad_scores(j + 1, cnt + 1);
+                }
+                if (!ok) break;
+                umma_commit(smem_u32(&ctl->acc_full));
+                umma_commit(smem_u32(&ctl->kv_empty));
+            }
+        }
+    } else if (warp < W_TMA) {
+        regs_up<AT_REGS_ARITH>();
+        const int g = warp >> 2, row = (warp & 3) * 32 + lane, c0 = 64 * g;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        uint32_t cnt = 0, items = 0;
+        bool ok = true;
+        for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
+            const KvItem it(p, i);
+            const int key = it.k0 + row;
+            for (int j = 0; j < it.n; ++j, ++cnt) {
+                const int tile = it.first + j, t0 = tile * p.tokens;
+                const int cols = mma_cols(it.valid(p, tile));
+                // causal: row (token, head) r of the tile sees this key if token >= key, r >= (key - t0) group
+                const bool mask = p.causal && t0 < it.k0 + TILE - 1;
+                const int from = mask ? (key - t0) * p.group - c0 : 0;
+                const uint32_t st = stats + (cnt & 1) * Sh::STAT_BYTES + c0 * 8;
+                ok = wait_bar(smem_u32(&ctl->s_full), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t r[2][32];
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (c0 + 32 * c < cols) tmem_ld32(t_s + lanes + c0 + 32 * c, r[c]);
+                tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (c0 + 32 * c < cols) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            float l0, d0, l1, d1;
+                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l0), "=f"(d0), "=f"(l1), "=f"(d1) : "r"(st + (32 * c + e) * 8));
+                            float a = fast_exp2(fmaf(__uint_as_float(r[c][e]), p.c2, -l0));
+                            float b = fast_exp2(fmaf(__uint_as_float(r[c][e + 1]), p.c2, -l1));
+                            if (mask) {
+                                a = 32 * c + e >= from ? a : 0.0f;
+                                b = 32 * c + e + 1 >= from ? b : 0.0f;
+                            }
+                            r[c][e] = __float_as_uint(a);
+                            r[c][e + 1] = __float_as_uint(b);
+                            pk[e / 2] = pack_bf16(a, b);
+                        }
+                        tmem_st16(t_s + lanes + c0 + 16 * c, pk);
+                    }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready));
+                ok = wait_bar(smem_u32(&ctl->g_scores), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t dp[2][32];
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (c0 + 32 * c < cols) tmem_ld32(t_dp + lanes + c0 + 32 * c, dp[c]);
+                tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (c0 + 32 * c < cols) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            float l0, d0, l1, d1;
+                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l0), "=f"(d0), "=f"(l1), "=f"(d1) : "r"(st + (32 * c + e) * 8));
+                            float a = __uint_as_float(r[c][e]) * (__uint_as_float(dp[c][e]) - d0);
+                            float b = __uint_as_float(r[c][e + 1]) * (__uint_as_float(dp[c][e + 1]) - d1);
+                            if (mask) {            // a masked product is zero even where dP is not finite
+                                a = 32 * c + e >= from ? a : 0.0f;
+                                b = 32 * c + e + 1 >= from ? b : 0.0f;
+                            }
+                            pk[e / 2] = pack_bf16(a, b);
+                        }
+                        tmem_st16(t_dp + lanes + c0 + 16 * c, pk);
+                    }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&ctl->ds_ready));
+            }
+            if (!ok) break;
+            ok = wait_bar(smem_u32(&ctl->acc_full), items & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+            if (!ok) break;
+            tc_fence_after();
+            const bool live = key < it.len;
+            bf16 *dst = (g ? p.out0 + ((int64_t)it.start + key) * p.ld0 : p.out1 + ((int64_t)it.start + key) * p.ld1) + (int64_t)it.h * p.d;
+#pragma unroll
+            for (int c = 0; c < DP; c += 32) {
+                uint32_t o[32];
+                tmem_ld32((g ? t_dk : t_dv) + lanes + c, o);
+                tmem_ld_wait();
+                if (live) store_row32(dst, o, g ? p.scale : 1.0f, c, p.d);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_free));
+        }
+    }
+    cta_teardown(ab, tmem);
+}
+
+// ------------------------------------------------------------------------------------ dQ
+// One item = one row tile of one kv head against the keys of its sequence: S = Q K^T (two buffers),
+// dP = dO V^T, dS packed to bf16 over the scores, dQ += dS K.
+template <int DP> struct QShape {
+    static constexpr int T_BYTES = tile_bytes<DP>();
+    static constexpr int KS = 3, VS = 2;
+    static constexpr int SMEM = (2 + KS + VS) * T_BYTES + 1024 + 512;
+};
+struct alignas(8) QCtl {
+    uint64_t q_full, q_empty, k_full[3], k_empty[3], k_tail[3], v_full[2], v_empty[2];
+    uint64_t s_full[2], g_scores, ds_ready, acc_full, acc_free;
+    uint32_t tmem_base;
+    volatile int abort_flag;
+};
+struct QItem {
+    int start, len, t0, tile, h, end, nb;
+    __device__ QItem(const AtParams &p, int i)
+    {
+        const int4 e = p.items[i / p.hk];
+        h = i % p.hk;
+        start = e.x; len = e.y; t0 = e.z; tile = e.w + t0 / p.tokens;
+        end = p.causal ? min(t0 + p.tokens, len) : len;
+        nb = ceil_div(end, TILE);
+    }
+    __device__ bool dirty_tail() const { return (len & 15) != 0 && nb * TILE > len; }
+};
+
+template <int DP>
+__global__ void __launch_bounds__(AT_THREADS, 1)
+k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
+{
+    using Sh = QShape<DP>;
+    constexpr int T_BYTES = Sh::T_BYTES, KS = Sh::KS, VS = Sh::VS;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t tiles = align_tiles(smem_raw);
+    const uint32_t q_tile = tiles, g_tile = tiles + T_BYTES, k_ring = tiles + 2 * T_BYTES, v_ring = k_ring + KS * T_BYTES;
+    QCtl *ctl = reinterpret_cast<QCtl *>(smem_raw + (tiles - smem_u32(smem_raw)) + (2 + KS + VS) * T_BYTES);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&ctl->q_full), 1);
+        mbar_init(smem_u32(&ctl->q_empty), 1);
+        for (int i = 0; i < KS; ++i) {
+            mbar_init(smem_u32(&ctl->k_full[i]), 1);
+            mbar_init(smem_u32(&ctl->k_empty[i]), 1);
+            mbar_init(smem_u32(&ctl->k_tail[i]), 1);
+        }
+        for (int i = 0; i < VS; ++i) {
+            mbar_init(smem_u32(&ctl->v_full[i]), 1);
+            mbar_init(smem_u32(&ctl->v_empty[i]), 1);
+        }
+        mbar_init(smem_u32(&ctl->s_full[0]), 1);
+        mbar_init(smem_u32(&ctl->s_full[1]), 1);
+        mbar_init(smem_u32(&ctl->g_scores), 1);
+        mbar_init(smem_u32(&ctl->ds_ready), 8);
+        mbar_init(smem_u32(&ctl->acc_full), 1);
+        mbar_init(smem_u32(&ctl->acc_free), 8);
+        ctl->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    const int used = p.group * p.tokens;
+    if (used < TILE) zero_smem(q_tile, 2 * T_BYTES);
+    fence_proxy_async_smem();
+    if (warp == W_MMA) { tmem_alloc(smem_u32(&ctl->tmem_base), AT_TMEM_COLS); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = ctl->tmem_base;
+    volatile int *ab = &ctl->abort_flag;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    ItemLoop loop(p.n_items);
+    const uint32_t t_dp = tmem + 2 * TILE, t_dq = tmem + 3 * TILE;
+
+    if (warp >= W_TMA) regs_down<AT_REGS_SERVICE>();
+    if (warp == W_TMA) {
+        if (lane == 0) {
+            uint32_t cnt = 0, items = 0;
+            bool ok = true;
+            for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
+                const QItem it(p, i);
+                ok = wait_bar(smem_u32(&ctl->q_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                if (!ok) break;
+                const uint32_t qb = smem_u32(&ctl->q_full);
+                mbar_expect_tx(qb, (uint32_t)(2 * used * DP * 2));
+                load_tile<DP>(q_tile, &tm.q, it.h * p.group, it.start + it.t0, qb);
+                load_tile<DP>(g_tile, &tm.g, it.h * p.group, it.start + it.t0, qb);
+                for (int j = 0; j < it.nb; ++j, ++cnt) {
+                    const uint32_t ks = cnt % KS, vs = cnt % VS;
+                    ok = wait_bar(smem_u32(&ctl->k_empty[ks]), ((cnt / KS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    if (!ok) break;
+                    const uint32_t kb = smem_u32(j == it.nb - 1 && it.dirty_tail() ? &ctl->k_tail[ks] : &ctl->k_full[ks]);
+                    mbar_expect_tx(kb, T_BYTES);
+                    load_tile<DP>(k_ring + ks * T_BYTES, &tm.k, it.h, it.start + j * TILE, kb);
+                    ok = wait_bar(smem_u32(&ctl->v_empty[vs]), ((cnt / VS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    if (!ok) break;
+                    const uint32_t vb = smem_u32(&ctl->v_full[vs]);
+                    mbar_expect_tx(vb, T_BYTES);
+                    load_tile<DP>(v_ring + vs * T_BYTES, &tm.v, it.h, it.start + j * TILE, vb);
+                }
+            }
+        }
+    } else if (warp == W_TAIL) {
+        uint32_t cnt = 0, seen = 0;
+        bool ok = true;
+        for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
+            const QItem it(p, i);
+            cnt += it.nb;
+            if (!it.dirty_tail()) continue;
+            const uint32_t s = (cnt - 1) % KS;
+            ok = wait_bar(smem_u32(&ctl->k_tail[s]), (seen >> s) & 1, ab, p.status, SITE_PRODUCER_EMPTY);
+            if (!ok) break;
+            seen ^= 1u << s;
+            const int valid = it.len - (it.nb - 1) * TILE;
+            zero_rows<DP>(k_ring + s * T_BYTES, valid, mma_cols(valid), lane);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctl->k_full[s]));
+        }
+    } else if (warp == W_MMA) {
+        if (lane == 0) {
+            uint32_t cnt = 0, items = 0;
+            bool ok = true;
+            for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
+                const QItem it(p, i);
+                auto cols_of = [&](int j) { return mma_cols(it.end - j * TILE); };
+                auto scores = [&](int j, uint32_t c) {
+                    ok = ok && wait_bar(smem_u32(&ctl->k_full[c % KS]), (c / KS) & 1, ab, p.status, SITE_MMA_FULL);
+                    if (!ok) return;
+                    tc_fence_after();
+                    mma_rows_rows<DP>(tmem + (c & 1) * TILE, q_tile, k_ring + (c % KS) * T_BYTES, cols_of(j));
+                    umma_commit(smem_u32(&ctl->s_full[c & 1]));
+                };
+                auto grad_scores = [&](int j, uint32_t c) {
+                    ok = ok && wait_bar(smem_u32(&ctl->v_full[c % VS]), (c / VS) & 1, ab, p.status, SITE_MMA_FULL);
+                    if (!ok) return;
+                    tc_fence_after();
+                    mma_rows_rows<DP>(t_dp, g_tile, v_ring + (c % VS) * T_BYTES, cols_of(j));
+                    umma_commit(smem_u32(&ctl->g_scores));
+                    umma_commit(smem_u32(&ctl->v_empty[c % VS]));
+                };
+                ok = wait_bar(smem_u32(&ctl->q_full), items & 1, ab, p.status, SITE_MMA_FULL);
+                scores(0, cnt);
+                grad_scores(0, cnt);
+                if (it.nb > 1) scores(1, cnt + 1);
+                for (int j = 0; j < it.nb && ok; ++j, ++cnt) {
+                    ok = wait_bar(smem_u32(&ctl->ds_ready), cnt & 1, ab, p.status, SITE_MMA_FULL);
+                    if (!ok) break;
+                    if (j + 1 < it.nb) grad_scores(j + 1, cnt + 1);
+                    if (ok && j == 0)
+                        ok = wait_bar(smem_u32(&ctl->acc_free), (items & 1) ^ 1, ab, p.status, SITE_MMA_TMEM_EMPTY);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t ds = tmem + (cnt & 1) * TILE;
+                    mma_tmem_rows<DP>(t_dq, ds, ds + 64, k_ring + (cnt % KS) * T_BYTES, cols_of(j), j > 0);
+                    umma_commit(smem_u32(&ctl->k_empty[cnt % KS]));
+                    if (j + 2 < it.nb) scores(j + 2, cnt + 2);
+                }
+                if (!ok) break;
+                umma_commit(smem_u32(&ctl->acc_full));
+                umma_commit(smem_u32(&ctl->q_empty));
+            }
+        }
+    } else if (warp < W_TMA) {
+        regs_up<AT_REGS_ARITH>();
+        const int g = warp >> 2, row = (warp & 3) * 32 + lane, c0 = 64 * g;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const int row_t = row / p.group, row_h = row - row_t * p.group;
+        uint32_t cnt = 0, items = 0;
+        bool ok = true;
+        for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
+            const QItem it(p, i);
+            const float2 st = p.row_stats[((int64_t)it.tile * p.hk + it.h) * TILE + row];
+            const int token = it.t0 + row_t, row_end = p.causal ? min(token + 1, it.len) : it.len;
+            for (int j = 0; j < it.nb; ++j, ++cnt) {
+                const int cols = mma_cols(it.end - j * TILE);
+                const bool mask = cols < TILE || j * TILE + TILE > (p.causal ? it.t0 + 1 : it.len);
+                const int limit = row_end - j * TILE - c0;
+                ok = wait_bar(smem_u32(&ctl->s_full[cnt & 1]), (cnt >> 1) & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = ok && wait_bar(smem_u32(&ctl->g_scores), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t t_s = tmem + lanes + (cnt & 1) * TILE + c0;
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (c0 + 32 * c < cols) {
+                        uint32_t r[32], dp[32], pk[16];
+                        tmem_ld32(t_s + 32 * c, r);
+                        tmem_ld32(t_dp + lanes + c0 + 32 * c, dp);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            float a = fast_exp2(fmaf(__uint_as_float(r[e]), p.c2, -st.x)) * (__uint_as_float(dp[e]) - st.y);
+                            float b = fast_exp2(fmaf(__uint_as_float(r[e + 1]), p.c2, -st.x)) * (__uint_as_float(dp[e + 1]) - st.y);
+                            if (mask) {
+                                a = 32 * c + e < limit ? a : 0.0f;
+                                b = 32 * c + e + 1 < limit ? b : 0.0f;
+                            }
+                            pk[e / 2] = pack_bf16(a, b);
+                        }
+                        tmem_st16(t_s + 16 * c, pk);
+                    }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&ctl->ds_ready));
+            }
+            if (!ok) break;
+            ok = wait_bar(smem_u32(&ctl->acc_full), items & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+            if (!ok) break;
+            tc_fence_after();
+            const bool live = row < used && token < it.len;
+            bf16 *dst = p.out0 + ((int64_t)it.start + token) * p.ld0 + (int64_t)(it.h * p.group + row_h) * p.d;
+#pragma unroll
+            for (int c = 0; c < DP / 2; c += 32) {
+                uint32_t o[32];
+                tmem_ld32(t_dq + lanes + g * (DP / 2) + c, o);
+                tmem_ld_wait();
+                if (live) store_row32(dst, o, p.scale, g * (DP / 2) + c, p.d);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_free));
+        }
+    }
+    cta_teardown(ab, tmem);
+}
+
+// ------------------------------------------------------------------------------------ host
+// [N, heads, d] bf16 with a token stride of `ld` elements; box = 64 columns x box_heads x box_tokens
+static bool head_map(CUtensorMap *m, const void *base, int d, int heads, int64_t N, int64_t ld, int box_heads, int box_tokens)
+{
+    EncodeTiledFn enc = get_encode();
+    if (!enc || !base) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)N};
+    cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)ld * 2};
+    cuuint32_t box[3] = {64u, (cuuint32_t)box_heads, (cuuint32_t)box_tokens}, es[3] = {1u, 1u, 1u};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, es,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int AT_MAX_DEVICES = 64;
+
+template <typename Kernel>
+static cudaError_t launch_at(Kernel kern, int *sms_by_dev, int smem, const AtMaps &tm, const AtParams &p, cudaStream_t s)
+{
+    if (p.n_items <= 0) return cudaSuccess;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= AT_MAX_DEVICES) return cudaErrorInvalidDevice;
+    if (sms_by_dev[dev] == 0) {
+        int n = 0;
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+        if (e != cudaSuccess) return e;
+        sms_by_dev[dev] = n;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(p.n_items < sms_by_dev[dev] ? p.n_items : sms_by_dev[dev]));
+    cfg.blockDim = dim3(AT_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, tm, p);
+}
+
+static AtParams params_of(const AttnArgs &a, const int4 *items, int n)
+{
+    AtParams p = {};
+    p.items = items; p.n_items = n * a.hk;
+    p.hq = a.hq; p.hk = a.hk; p.group = a.group; p.tokens = a.tokens; p.d = a.d; p.causal = a.causal;
+    p.scale = a.scale; p.c2 = a.scale * LOG2E;
+    p.status = a.status; p.row_stats = a.row_stats;
+    return p;
+}
+
+template <int DP> static cudaError_t forward_dp(const AttnArgs &a, cudaStream_t s)
+{
+    static int sms[AT_MAX_DEVICES];
+    AtMaps tm;
+    if (!head_map(&tm.q, a.q, a.d, a.hq, a.N, a.ldq, a.group, a.tokens) || !head_map(&tm.k, a.k, a.d, a.hk, a.N, a.ldk, 1, TILE) ||
+        !head_map(&tm.v, a.v, a.d, a.hk, a.N, a.ldv, 1, TILE))
+        return cudaErrorInvalidValue;
+    tm.g = tm.q;
+    AtParams p = params_of(a, a.fwd_items, a.n_fwd);
+    p.out0 = (bf16 *)a.out; p.ld0 = a.ldo; p.lse = a.lse;
+    return launch_at(k_attention_fwd<DP>, sms, FwdShape<DP>::SMEM, tm, p, s);
+}
+
+template <int DP> static cudaError_t backward_dp(const AttnArgs &a, cudaStream_t s)
+{
+    static int sms_kv[AT_MAX_DEVICES], sms_q[AT_MAX_DEVICES];
+    AtMaps tm;
+    if (!head_map(&tm.q, a.q, a.d, a.hq, a.N, a.ldq, a.group, a.tokens) || !head_map(&tm.k, a.k, a.d, a.hk, a.N, a.ldk, 1, TILE) ||
+        !head_map(&tm.v, a.v, a.d, a.hk, a.N, a.ldv, 1, TILE) || !head_map(&tm.g, a.dout, a.d, a.hq, a.N, a.lddo, a.group, a.tokens))
+        return cudaErrorInvalidValue;
+    cudaError_t e = launch_attention_row_stats(a, SKIPFFN_BF16, TILE, s);
+    if (e != cudaSuccess) return e;
+    AtParams p = params_of(a, a.key_items, a.n_keys);
+    p.out0 = (bf16 *)a.dk; p.ld0 = a.lddk; p.out1 = (bf16 *)a.dv; p.ld1 = a.lddv;
+    e = launch_at(k_attention_bwd_kv<DP>, sms_kv, KvShape<DP>::SMEM, tm, p, s);
+    if (e != cudaSuccess) return e;
+    p = params_of(a, a.row_items, a.n_rows);
+    p.out0 = (bf16 *)a.dq; p.ld0 = a.lddq;
+    return launch_at(k_attention_bwd_q<DP>, sms_q, QShape<DP>::SMEM, tm, p, s);
+}
+
+cudaError_t launch_attention_tc_forward(const AttnArgs &a, cudaStream_t s)
+{
+    return a.d <= 64 ? forward_dp<64>(a, s) : forward_dp<128>(a, s);
+}
+cudaError_t launch_attention_tc_backward(const AttnArgs &a, cudaStream_t s)
+{
+    return a.d <= 64 ? backward_dp<64>(a, s) : backward_dp<128>(a, s);
+}
+
+}  // namespace skipffn

@@ -184,6 +184,13 @@ cudaError_t launch_summary_forward(const void *X, const int32_t *off, int n_seg,
 cudaError_t launch_summary_backward(const void *X, const int32_t *off, int n_seg, int64_t n, int C, int dtype,
                                     const void *w, const float *probs, const void *dxs, void *dX, void *dw,
                                     int dw_fp32, float *scratch, cudaStream_t s);
+// layernorm.cu
+constexpr int LN_MAX_PARTS = 160, LN_MAX_C = 16384;   // partial rows of the gradients' column sums; longest row
+cudaError_t launch_layernorm_forward(const void *x, const void *gamma, const void *beta, int64_t rows, int C, int dtype, float eps,
+                                     void *y, float *mean, float *rstd, cudaStream_t s);
+cudaError_t launch_layernorm_backward(const void *dy, const void *x, const void *gamma, const float *mean, const float *rstd,
+                                      int64_t rows, int C, int dtype, void *dx, void *dgamma, void *dbeta, int dw_fp32, float *part,
+                                      cudaStream_t s);
 // merge.cu
 size_t merge_scratch_bytes(int64_t n, int C, int k, int dtype);
 int32_t *merge_status_ptr(void *scratch, int64_t n, int C, int k, int dtype);

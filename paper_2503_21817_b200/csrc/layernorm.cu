@@ -1,0 +1,415 @@
+// Layer normalisation of packed rows (the vision tower's blocks and its projector; the decoder's RMS norm is
+// fused into the routing, prenorm.cu):
+//   forward : mean, var over the C columns;  rstd = (var + eps)^-1/2;  y = (x - mean) rstd gamma + beta
+//   backward: xh = (x - mean) rstd, t = dy gamma;  dx = rstd (t - mean_c(t) - xh mean_c(t xh));
+//             dgamma = sum_rows dy xh;  dbeta = sum_rows dy
+// HBM-bound: a row is read once into registers (16-byte loads, at most four per thread), the variance is
+// the mean of squared deviations (a second look at the registers, not E[x^2] - mean^2), and the backward
+// reads x and dy once for both its results.  Statistics and sums are fp32 in a fixed order (no atomics).
+#include "common.cuh"
+
+namespace skipffn {
+
+namespace {
+
+constexpr int LN_NV = 4;                      // 16-byte vectors per thread
+
+template <typename T> struct Vec { static constexpr int N = 16 / (int)sizeof(T); };   // elements of a vector
+
+template <int N> __device__ __forceinline__ void unpack(const uint4 &q, float (&v)[N])
+{
+    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+    if constexpr (N == 8) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[2 * k] = __uint_as_float(u[k] << 16);
+            v[2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(u[k]);
+    }
+}
+template <int N> __device__ __forceinline__ uint4 pack(const float (&v)[N])
+{
+    uint32_t u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (N == 8) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+            u[k] = *reinterpret_cast<const uint32_t *>(&h);
+        } else {
+            u[k] = __float_as_uint(v[k]);
+        }
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+
+__device__ __forceinline__ float warp_add(float v)
+{
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+// Barrier of the `threads` threads of row group `id` (every group of a CTA has its own)
+__device__ __forceinline__ void group_sync(int id, int threads)
+{
+    asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "r"(threads) : "memory");
+}
+// Sum over a row group in a fixed order, valid in every thread.  `red` holds one float per warp of the
+// group and alternates between two halves from call to call, so one barrier per call is enough.
+__device__ __forceinline__ float group_add(float v, float *red, int id, int threads)
+{
+    v = warp_add(v);
+    if (threads == 32) return v;
+    const int w = threadIdx.x >> 5;
+    if ((threadIdx.x & 31) == 0) red[w] = v;
+    group_sync(id, threads);
+    float s = 0.0f;
+    for (int k = 0; k < threads / 32; ++k) s += red[k];
+    return s;
+}
+
+// One row per group of blockDim.x threads, blockDim.y groups per CTA.
+template <typename T>
+__global__ void __launch_bounds__(1024)
+k_layernorm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__restrict__ beta, int64_t rows, int C,
+                float eps, T *__restrict__ y, float *__restrict__ mean_out, float *__restrict__ rstd_out)
+{
+    constexpr int N = Vec<T>::N;
+    __shared__ float red[2][32];
+    pdl_enter();
+    const int tx = threadIdx.x, threads = blockDim.x, id = threadIdx.y, vecs = C / N;
+    const int64_t row = (int64_t)blockIdx.x * blockDim.y + id;
+    if (row >= rows) return;
+    const uint4 *src = reinterpret_cast<const uint4 *>(x + row * C);
+    float v[LN_NV][N];
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < LN_NV; ++k) {
+        const int i = tx + k * threads;
+        const uint4 q = i < vecs ? src[i] : make_uint4(0, 0, 0, 0);
+        unpack(q, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < LN_NV; ++k)
+#pragma unroll
+        for (int e = 0; e < N; ++e) s += v[k][e];
+    float *r0 = red[0] + id * (threads / 32), *r1 = red[1] + id * (threads / 32);
+    const float mean = group_add(s, r0, id, threads) / (float)C;
+    float ss = 0.0f;
+#pragma unroll
+    for (int k = 0; k < LN_NV; ++k)
+        if (tx + k * threads < vecs)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                v[k][e] -= mean;
+                ss = fmaf(v[k][e], v[k][e], ss);
+            }
+    const float rstd = 1.0f / sqrtf(group_add(ss, r1, id, threads) / (float)C + eps);
+    uint4 *dst = reinterpret_cast<uint4 *>(y + row * C);
+#pragma unroll
+    for (int k = 0; k < LN_NV; ++k) {
+        const int i = tx + k * threads;
+        if (i >= vecs) break;
+        float g[N], b[N], o[N];
+        unpack(__ldg(reinterpret_cast<const uint4 *>(gamma) + i), g);
+        unpack(beta ? __ldg(reinterpret_cast<const uint4 *>(beta) + i) : make_uint4(0, 0, 0, 0), b);
+#pragma unroll
+        for (int e = 0; e < N; ++e) o[e] = fmaf(v[k][e] * rstd, g[e], b[e]);
+        dst[i] = pack(o);
+    }
+    if (tx == 0) {
+        if (mean_out) mean_out[row] = mean;
+        if (rstd_out) rstd_out[row] = rstd;
+    }
+}
+
+// Backward: group g of CTA b walks rows b groups + g, + grid x groups, ...; dx row by row, dgamma and dbeta of
+// the group's rows in registers.  At the end the groups add up in order through shared memory and the
+// CTA leaves one partial row of each in part[b][2][C].
+template <typename T, int BOUND>
+__global__ void __launch_bounds__(BOUND, 1)
+k_layernorm_bwd(const T *dy, const T *x, const T *__restrict__ gamma, const float *__restrict__ mean_in,
+                const float *__restrict__ rstd_in, int64_t rows, int C, T *dx, float *__restrict__ part)
+{
+    constexpr int N = Vec<T>::N;
+    __shared__ float red[2][2][32];
+    extern __shared__ float sums[];            // [2][C] when the CTA has several groups
+    pdl_enter();
+    const int tx = threadIdx.x, threads = blockDim.x, id = threadIdx.y, groups = blockDim.y, vecs = C / N;
+    const int64_t step = (int64_t)gridDim.x * groups;
+    float dg[LN_NV][N], db[LN_NV][N];
+    uint4 gq[LN_NV], xq[LN_NV], yq[LN_NV];
+#pragma unroll
+    for (int k = 0; k < LN_NV; ++k) {
+        const int i = tx + k * threads;
+        gq[k] = i < vecs ? __ldg(reinterpret_cast<const uint4 *>(gamma) + i) : make_uint4(0, 0, 0, 0);
+        xq[k] = yq[k] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < N; ++e) dg[k][e] = db[k][e] = 0.0f;
+    }
+    auto fetch = [&](int64_t row) {
+        const uint4 *xs = reinterpret_cast<const uint4 *>(x + row * C), *ys = reinterpret_cast<const uint4 *>(dy + row * C);
+#pragma unroll
+        for (int k = 0; k < LN_NV; ++k) {
+            const int i = tx + k * threads;
+            if (i < vecs) { xq[k] = xs[i]; yq[k] = ys[i]; }
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * groups + id;
+    if (row < rows) fetch(row);
+    for (int turn = 0; row < rows; row += step, turn ^= 1) {
+        const float mean = mean_in[row], rstd = rstd_in[row];
+        uint4 xc[LN_NV], yc[LN_NV];
+#pragma unroll
+        for (int k = 0; k < LN_NV; ++k) { xc[k] = xq[k]; yc[k] = yq[k]; }
+        if (row + step < rows) fetch(row + step);          // in flight while this row is worked on
+        float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < LN_NV; ++k) {
+            if (tx + k * threads >= vecs) break;
+            float xv[N], yv[N], g[N];
+            unpack(xc[k], xv); unpack(yc[k], yv); unpack(gq[k], g);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float xh = (xv[e] - mean) * rstd, t = yv[e] * g[e];
+                s0 += t;
+                s1 = fmaf(t, xh, s1);
+                dg[k][e] = fmaf(yv[e], xh, dg[k][e]);
+                db[k][e] += yv[e];
+            }
+        }
+        float *r = red[turn][0] + id * (threads / 32), *r2 = red[turn][1] + id * (threads / 32);
+        s0 = warp_add(s0);
+        s1 = warp_add(s1);
+        if (threads > 32) {
+            if ((tx & 31) == 0) { r[tx >> 5] = s0; r2[tx >> 5] = s1; }
+            group_sync(id, threads);
+            s0 = s1 = 0.0f;
+            for (int k = 0; k < threads / 32; ++k) { s0 += r[k]; s1 += r2[k]; }
+        }
+        s0 /= (float)C;
+        s1 /= (float)C;
+        uint4 *dst = reinterpret_cast<uint4 *>(dx + row * C);
+#pragma unroll
+        for (int k = 0; k < LN_NV; ++k) {
+            const int i = tx + k * threads;
+            if (i >= vecs) break;
+            float xv[N], yv[N], g[N], o[N];
+            unpack(xc[k], xv); unpack(yc[k], yv); unpack(gq[k], g);
+#pragma unroll
+            for (int e = 0; e < N; ++e) o[e] = rstd * (fmaf(yv[e], g[e], -s0) - (xv[e] - mean) * rstd * s1);
+            dst[i] = pack(o);
+        }
+    }
+    if (part == nullptr) return;
+    float *out = part + (int64_t)blockIdx.x * 2 * C;
+    for (int g = 0; g < groups; ++g) {
+        if (groups > 1) __syncthreads();
+        if (g != id) continue;
+        float *acc = g == groups - 1 ? out : sums;
+#pragma unroll
+        for (int k = 0; k < LN_NV; ++k) {
+            const int i = tx + k * threads;
+            if (i >= vecs) break;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const int c = i * N + e;
+                acc[c] = dg[k][e] + (g ? sums[c] : 0.0f);
+                acc[C + c] = db[k][e] + (g ? sums[C + c] : 0.0f);
+            }
+        }
+    }
+}
+
+// Rows too long for the registers of the kernel above: dx alone, one CTA per row, sums first.
+constexpr int LN_LONG_THREADS = 512;
+template <typename T>
+__global__ void __launch_bounds__(LN_LONG_THREADS)
+k_layernorm_bwd_rows(const T *dy, const T *x, const T *__restrict__ gamma, const float *__restrict__ mean_in,
+                     const float *__restrict__ rstd_in, int C, T *dx)
+{
+    __shared__ float red[2][LN_LONG_THREADS / 32];
+    pdl_enter();
+    const int64_t row = blockIdx.x;
+    const float mean = mean_in[row], rstd = rstd_in[row];
+    const T *xs = x + row * C, *ys = dy + row * C;
+    float s0 = 0.0f, s1 = 0.0f;
+    for (int c = 4 * threadIdx.x; c < C; c += 4 * LN_LONG_THREADS) {
+        float xv[4], yv[4], g[4];
+        load4(xs + c, xv); load4(ys + c, yv); load4(gamma + c, g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            s0 = fmaf(yv[e], g[e], s0);
+            s1 = fmaf(yv[e] * g[e], (xv[e] - mean) * rstd, s1);
+        }
+    }
+    s0 = group_add(s0, red[0], 0, LN_LONG_THREADS) / (float)C;
+    s1 = group_add(s1, red[1], 0, LN_LONG_THREADS) / (float)C;
+    for (int c = 4 * threadIdx.x; c < C; c += 4 * LN_LONG_THREADS) {
+        float xv[4], yv[4], g[4], o[4];
+        load4(xs + c, xv); load4(ys + c, yv); load4(gamma + c, g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = rstd * (fmaf(yv[e], g[e], -s0) - (xv[e] - mean) * rstd * s1);
+        store4(dx + row * C + c, o);
+    }
+}
+// ... and the column sums of its rows, one column per lane, 8 row lanes added in order: part[chunk][2][C]
+constexpr int LN_COLS = 32, LN_LANES = 8;
+template <typename T>
+__global__ void __launch_bounds__(LN_COLS * LN_LANES)
+k_layernorm_bwd_cols(const T *dy, const T *x, const float *__restrict__ mean_in, const float *__restrict__ rstd_in,
+                     int64_t rows, int C, float *__restrict__ part)
+{
+    __shared__ float red[2][LN_LANES][LN_COLS];
+    pdl_enter();
+    const int64_t per = (rows + gridDim.y - 1) / gridDim.y, r0 = blockIdx.y * per, r1 = r0 + per < rows ? r0 + per : rows;
+    const int cl = threadIdx.x % LN_COLS, lane = threadIdx.x / LN_COLS, c = blockIdx.x * LN_COLS + cl;
+    float g = 0.0f, b = 0.0f;
+    if (c < C)
+#pragma unroll 4
+        for (int64_t r = r0 + lane; r < r1; r += LN_LANES) {
+            const float d = to_f32(dy[r * C + c]);
+            g = fmaf(d, (to_f32(x[r * C + c]) - mean_in[r]) * rstd_in[r], g);
+            b += d;
+        }
+    red[0][lane][cl] = g;
+    red[1][lane][cl] = b;
+    __syncthreads();
+    if (lane < 2 && c < C) {
+        float s = 0.0f;
+#pragma unroll
+        for (int l = 0; l < LN_LANES; ++l) s += red[lane][l][cl];
+        part[((int64_t)blockIdx.y * 2 + lane) * C + c] = s;
+    }
+}
+
+// Sum of the partial rows: LN_LANES lanes per column walk the parts, added in lane order.  blockIdx.y: 0 dgamma, 1 dbeta.
+template <typename TO>
+__global__ void __launch_bounds__(LN_COLS * LN_LANES)
+k_layernorm_sum_parts(const float *__restrict__ part, int parts, int C, TO *__restrict__ dgamma, TO *__restrict__ dbeta)
+{
+    __shared__ float red[LN_LANES][LN_COLS];
+    pdl_enter();
+    TO *dst = blockIdx.y ? dbeta : dgamma;
+    if (dst == nullptr) return;
+    const int cl = threadIdx.x % LN_COLS, lane = threadIdx.x / LN_COLS, c = blockIdx.x * LN_COLS + cl;
+    float s = 0.0f;
+    if (c < C)
+#pragma unroll 8
+        for (int k = lane; k < parts; k += LN_LANES) s += part[((int64_t)k * 2 + blockIdx.y) * C + c];
+    red[lane][cl] = s;
+    __syncthreads();
+    if (lane == 0 && c < C) {
+        s = 0.0f;
+#pragma unroll
+        for (int l = 0; l < LN_LANES; ++l) s += red[l][cl];
+        dst[c] = from_f32<TO>(s);
+    }
+}
+
+// threads of a row group: enough for LN_NV vectors each, a whole number of warps
+template <typename T> int group_threads(int C)
+{
+    const int vecs = C / Vec<T>::N;
+    return ((vecs + LN_NV - 1) / LN_NV + 31) / 32 * 32;
+}
+
+constexpr int LN_MAX_DEVICES = 64;
+cudaError_t device_sms(int &sms)
+{
+    static int by_dev[LN_MAX_DEVICES];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= LN_MAX_DEVICES) return cudaErrorInvalidDevice;
+    if (by_dev[dev] == 0) {
+        int n = 0;
+        const cudaError_t e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+        if (e != cudaSuccess) return e;
+        by_dev[dev] = n;
+    }
+    sms = by_dev[dev] < LN_MAX_PARTS ? by_dev[dev] : LN_MAX_PARTS;
+    return cudaSuccess;
+}
+
+template <typename KernelT, typename... Args>
+cudaError_t launch_smem(KernelT kern, dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
+template <typename T>
+cudaError_t fwd_t(const T *x, const T *gamma, const T *beta, int64_t rows, int C, float eps, T *y, float *mean, float *rstd,
+                  cudaStream_t s)
+{
+    const int t = group_threads<T>(C), groups = t >= 128 ? 1 : 128 / t;
+    return launch_pdl(k_layernorm_fwd<T>, dim3((unsigned)((rows + groups - 1) / groups)), dim3(t, groups), s, x, gamma, beta, rows, C,
+                      eps, y, mean, rstd);
+}
+
+template <typename T, int BOUND>
+cudaError_t bwd_t(const T *dy, const T *x, const T *gamma, const float *mean, const float *rstd, int64_t rows, int C, T *dx,
+                  void *dgamma, void *dbeta, int dw_fp32, float *part, cudaStream_t s)
+{
+    int sms = 0;
+    cudaError_t e = device_sms(sms);
+    if (e != cudaSuccess) return e;
+    const bool sums = dgamma != nullptr || dbeta != nullptr;
+    const int t = group_threads<T>(C);
+    int parts;
+    if (t <= BOUND) {
+        const int groups = BOUND / t;
+        const int64_t need = (rows + groups - 1) / groups;
+        parts = (int)(need < sms ? (need > 0 ? need : 1) : sms);
+        const size_t smem = groups > 1 ? (size_t)2 * C * sizeof(float) : 0;     // at most 48 KiB
+        if (smem > 32 * 1024) {                 // with the static arrays more than a launch gets unasked
+            e = cudaFuncSetAttribute(k_layernorm_bwd<T, BOUND>, cudaFuncAttributeMaxDynamicSharedMemorySize, 48 * 1024);
+            if (e != cudaSuccess) return e;
+        }
+        e = launch_smem(k_layernorm_bwd<T, BOUND>, dim3(parts), dim3(t, groups), smem, s, dy, x, gamma, mean, rstd, rows, C, dx,
+                        sums ? part : nullptr);
+        if (e != cudaSuccess) return e;
+    } else {
+        parts = DG_CHUNKS;
+        if (sums) {
+            e = launch_pdl(k_layernorm_bwd_cols<T>, dim3((C + LN_COLS - 1) / LN_COLS, parts), dim3(LN_COLS * LN_LANES), s, dy, x, mean,
+                           rstd, rows, C, part);
+            if (e != cudaSuccess) return e;
+        }
+        if (rows > 0) {
+            e = launch_pdl(k_layernorm_bwd_rows<T>, dim3((unsigned)rows), dim3(LN_LONG_THREADS), s, dy, x, gamma, mean, rstd, C, dx);
+            if (e != cudaSuccess) return e;
+        }
+    }
+    if (!sums) return cudaSuccess;
+    const dim3 grid((C + LN_COLS - 1) / LN_COLS, 2), block(LN_COLS * LN_LANES);
+    return dw_fp32 ? launch_pdl(k_layernorm_sum_parts<float>, grid, block, s, part, parts, C, (float *)dgamma, (float *)dbeta)
+                   : launch_pdl(k_layernorm_sum_parts<T>, grid, block, s, part, parts, C, (T *)dgamma, (T *)dbeta);
+}
+
+}  // namespace
+
+cudaError_t launch_layernorm_forward(const void *x, const void *gamma, const void *beta, int64_t rows, int C, int dtype, float eps,
+                                     void *y, float *mean, float *rstd, cudaStream_t s)
+{
+    if (rows <= 0) return cudaSuccess;
+    return dtype == SKIPFFN_BF16 ? fwd_t((const bf16 *)x, (const bf16 *)gamma, (const bf16 *)beta, rows, C, eps, (bf16 *)y, mean, rstd, s)
+                                 : fwd_t((const float *)x, (const float *)gamma, (const float *)beta, rows, C, eps, (float *)y, mean, rstd, s);
+}
+
+cudaError_t launch_layernorm_backward(const void *dy, const void *x, const void *gamma, const float *mean, const float *rstd,
+                                      int64_t rows, int C, int dtype, void *dx, void *dgamma, void *dbeta, int dw_fp32, float *part,
+                                      cudaStream_t s)
+{
+    return dtype == SKIPFFN_BF16
+               ? bwd_t<bf16, 384>((const bf16 *)dy, (const bf16 *)x, (const bf16 *)gamma, mean, rstd, rows, C, (bf16 *)dx, dgamma, dbeta, dw_fp32, part, s)
+               : bwd_t<float, 512>((const float *)dy, (const float *)x, (const float *)gamma, mean, rstd, rows, C, (float *)dx, dgamma, dbeta, 1, part, s);
+}
+
+}  // namespace skipffn
