@@ -380,9 +380,9 @@ class PackedAttention:
         self.scratch_bytes = int(self.lib.skipffn_attention_scratch_bytes(self._handle))
 
     def __del__(self):
-        if getattr(self, "_handle", None) and self._handle.value:
-            self.lib.skipffn_attention_destroy(self._handle)
-            self._handle = ctypes.c_void_p()
+        handle, self._handle = getattr(self, "_handle", None), None
+        if handle is not None and handle.value:
+            self.lib.skipffn_attention_destroy(handle)
 
     def _stream(self):
         return self._torch.cuda.current_stream(self.device).cuda_stream

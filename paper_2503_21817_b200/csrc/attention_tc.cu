@@ -7,25 +7,45 @@ namespace skipffn {
 namespace {
 
 constexpr int TILE = 128;                    // rows of a row tile = keys of a key tile
-constexpr int AT_TMEM_COLS = 512;
-constexpr int AT_THREADS = 384;              // 8 arithmetic warps, TMA, MMA, tail cleaner, one idle
-constexpr int W_TMA = 8, W_MMA = 9, W_TAIL = 10;
-// Registers: 384 x 168 at launch, moved from the four service warps to the eight arithmetic warps
-// (128 x 88 + 256 x 208 = the same 64512).
-constexpr int AT_REGS_SERVICE = 88, AT_REGS_ARITH = 208;
+constexpr int AT_TMEM_COLS = 512;            // all of it, so the allocation starts at address 0
+constexpr uint32_t tmem = 0;
+// Warps of a CTA: TMA, MMA, tail cleaner, an idle one, then ARITH arithmetic warps.  At launch every thread has
+// the same number of registers; the four service warps give some of theirs to the arithmetic warps.
+//   forward : 8 (a row per thread)    384 x 168 = 128 x 88 + 256 x 208
+//   backward: 16 (a quarter of a row) 640 x  96 = 128 x 64 + 512 x 104
+template <int ARITH> struct Warps {
+    static constexpr int THREADS = 32 * (ARITH + 4), TMA = 0, MMA = 1, TAIL = 2, FIRST = 4, COUNT = ARITH;   // FIRST: arithmetic warps
+    static constexpr int REGS_SERVICE = ARITH == 8 ? 88 : 64, REGS_ARITH = ARITH == 8 ? 208 : 104;
+};
+using FwdWarps = Warps<8>;
+using BwdWarps = Warps<16>;
 constexpr float LOG2E = 1.4426950408889634f;
-
 template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-// Bounded wait, inlined: a kernel that moves registers between its warps cannot call functions.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// Bounded waits, inlined: a kernel that moves registers between its warps cannot call functions.  SPIN (the
+// arithmetic and MMA warps, whose waits are on the critical path) polls; the others let the hardware park the warp.
+template <bool SPIN>
 __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status, int site)
 {
-    if (mbar_try_wait(bar, parity)) return true;
+    auto probe = [&] { return SPIN ? mbar_test(bar, parity) : mbar_try_wait(bar, parity); };
+    if (probe()) return true;
     const unsigned long long t0 = globaltimer_ns();
     for (uint32_t it = 1;; ++it) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if ((it & 0xf) == 0) {
+        if (probe()) return true;
+        if ((it & (SPIN ? 0x3ff : 0xf)) == 0) {
             if (*abort_flag) return false;
             if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) {
                 *abort_flag = 1;
@@ -34,6 +54,55 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile
             }
         }
     }
+}
+
+// The MMA warp's wait: the answer is the same in every lane and the compiler can tell (a vote), so that what
+// follows stays in uniform registers.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status, int site)
+{
+    if (__builtin_expect(__all_sync(0xffffffffu, mbar_test(bar, parity)), 1)) return true;
+    const unsigned long long t0 = globaltimer_ns();
+    for (uint32_t it = 1;; ++it) {
+        if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
+        if ((it & 0x3ff) == 0) {
+            const bool late = globaltimer_ns() - t0 > WAIT_LIMIT_NS;
+            if (__any_sync(0xffffffffu, late || *abort_flag)) {
+                if (late) {
+                    *abort_flag = 1;
+                    if (atomicCAS(&status[ST_STATUS], 0, (int)SKIPFFN_ETIMEOUT) == 0) status[ST_SITE] = site;
+                }
+                return false;
+            }
+        }
+    }
+}
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+
+// Two fp32 operations in one instruction (register pairs)
+__device__ __forceinline__ uint64_t pair2(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair2(uint64_t v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 struct AtParams {
@@ -82,7 +151,7 @@ template <int DP> __device__ __forceinline__ void zero_rows(uint32_t tile, int l
 }
 __device__ __forceinline__ void zero_smem(uint32_t addr, int bytes)
 {
-    for (int i = threadIdx.x * 16; i < bytes; i += AT_THREADS * 16)
+    for (int i = threadIdx.x * 16; i < bytes; i += blockDim.x * 16)
         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(addr + i), "r"(0) : "memory");
 }
 
@@ -94,28 +163,46 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, 
     for (int s = 0; s < DP / 64; ++s) tma_load_3d(dst + s * (TILE * 128), map, 64 * s, head, token, bar);
 }
 
-// D[128 x n] = A[128 x DP] B[n x DP]^T, both K-major in shared memory
-template <int DP> __device__ __forceinline__ void mma_rows_rows(uint32_t d_tmem, uint32_t a, uint32_t b, int n)
+// The issuer's instructions are what a tile waits for, so they are kept few: descriptors are built as a constant
+// upper word and a lower word that a stage or a K step moves by an addition (shared memory ends below 256 KiB,
+// no carry leaves the address field).
+constexpr uint32_t DESC_HI = (1024 >> 4) | 1u << 14 | 2u << 29;      // 8-row groups 1024 bytes apart, 128-byte swizzle
+__device__ __forceinline__ uint64_t desc64(uint32_t lo)
 {
-    const uint64_t da = make_desc(a, 16, 1024), db = make_desc(b, 16, 1024);
-    const uint32_t idesc = make_idesc(0, 0, 128, n);
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "n"(DESC_HI));
+    return d;
+}
+__device__ __forceinline__ uint32_t desc_rows(uint32_t tile) { return tile >> 4 | (16u >> 4) << 16; }              // K-major
+__device__ __forceinline__ uint32_t desc_across(uint32_t tile) { return tile >> 4 | (TILE * 128u >> 4) << 16; }    // MN-major
+__device__ __forceinline__ uint32_t idesc_rows(int n) { return make_idesc(0, 0, 128, 0) | (uint32_t)n << 14; }
+
+// D[128 x n] = A[128 x DP] B[n x DP]^T, both K-major in shared memory
+template <int DP> __device__ __forceinline__ void mma_rows_rows(uint32_t on, uint32_t d_tmem, uint32_t a, uint32_t b, uint32_t idesc)
+{
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k) {
-        const uint64_t off = (uint64_t)((k / 4) * (TILE * 128 >> 4) + (k % 4) * 2);
-        umma_bf16(d_tmem, da + off, db + off, idesc, k != 0);
+        const uint32_t off = (k / 4) * (TILE * 128 >> 4) + (k % 4) * 2;
+        umma_bf16_if(on, d_tmem, desc64(a + off), desc64(b + off), idesc, k != 0);
     }
 }
-// D[128 x DP] (+)= A[128 x rows] B[rows x DP], A in tensor memory (16 columns of A take 8 tensor-memory
-// columns; the second half of A starts at `a_hi`), B = a stored tile read across its rows (MN-major)
-template <int DP>
-__device__ __forceinline__ void mma_tmem_rows(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b, int rows, bool acc)
+// D[128 x DP] (+)= A[128 x 16 K0..16 (K0 + KN) - 1] B[those rows x DP]: A in tensor memory, 16 of its rows in 8
+// columns from `a` (every STRIDE steps 32 further on), B a stored tile read across its rows.  Steps at or past
+// `steps` are left out.
+template <int DP, int K0, int KN, int STRIDE>
+__device__ __forceinline__ void mma_tmem_rows(uint32_t on, uint32_t d_tmem, uint32_t a, uint32_t b, int steps, uint32_t acc)
 {
-    const uint64_t db = make_desc(b, TILE * 128, 1024);
-    const uint32_t idesc = make_idesc(0, 1, 128, DP);
+    constexpr uint32_t idesc = make_idesc(0, 1, 128, DP);
+    if (steps >= K0 + KN) {
 #pragma unroll
-    for (int k = 0; k < TILE / 16; ++k)
-        if (16 * k < rows)
-            umma_bf16_ta(d_tmem, k < 4 ? a_lo + 8 * k : a_hi + 8 * (k - 4), db + (uint64_t)(k * (16 * 128 >> 4)), idesc, acc || k != 0);
+        for (int k = K0; k < K0 + KN; ++k)
+            umma_bf16_ta_if(on, d_tmem, a + 32 * (k / STRIDE) + 8 * (k % STRIDE), desc64(b + k * (16 * 128 >> 4)), idesc, k == K0 ? acc : 1u);
+    } else {
+#pragma unroll
+        for (int k = K0; k < K0 + KN - 1; ++k)
+            if (k < steps)
+                umma_bf16_ta_if(on, d_tmem, a + 32 * (k / STRIDE) + 8 * (k % STRIDE), desc64(b + k * (16 * 128 >> 4)), idesc, k == K0 ? acc : 1u);
+    }
 }
 
 // 32 fp32 values of one row times `f`, to bf16, to columns c .. c+31 (below d) of a global row
@@ -133,10 +220,8 @@ __device__ __forceinline__ void store_row32(bf16 *row, const uint32_t (&v)[32], 
         }
 }
 
-__device__ __forceinline__ uint32_t align_tiles(const uint8_t *raw) { return (smem_u32(raw) + 1023u) & ~1023u; }
-
 // Ends of every kernel: drain after an abort, give the tensor memory back.
-__device__ __forceinline__ void cta_teardown(volatile int *abort_flag, uint32_t tmem_base)
+__device__ __forceinline__ void cta_teardown(volatile int *abort_flag, uint32_t tmem_base, int dealloc_warp)
 {
     if (*abort_flag) {
         const unsigned long long t0 = globaltimer_ns();
@@ -144,7 +229,7 @@ __device__ __forceinline__ void cta_teardown(volatile int *abort_flag, uint32_t 
     }
     tc_fence_before();
     __syncthreads();
-    if ((threadIdx.x >> 5) == W_MMA) {
+    if ((int)(threadIdx.x >> 5) == dealloc_warp) {
         tc_fence_after();
         tmem_dealloc(tmem_base, AT_TMEM_COLS);
     }
@@ -166,19 +251,168 @@ __device__ __forceinline__ void cta_teardown(volatile int *abort_flag, uint32_t 
 template <int DP> struct FwdShape {
     static constexpr int T_BYTES = tile_bytes<DP>();
     static constexpr int SLOTS = DP == 128 ? 5 : 8;
-    static constexpr int SMEM = (2 + SLOTS) * T_BYTES + 1024 + 512;
+    static constexpr int SMEM = (2 + SLOTS) * T_BYTES + 512;
 };
 struct alignas(8) FwdCtl {
-    uint64_t q_full[2], q_empty[2], kv_full[8], kv_empty[8], tail[8], s_full[2], p_full[2], o_full[2], o_free[2];
+    uint64_t q_full[2], q_empty[2], kv_full[8], kv_empty[8], tail[8], s_full[2], p_full[2][2], o_full[2], o_free[2];   // p_full[g][half]
     uint32_t tmem_base;
     volatile int abort_flag;
 };
 
+// 32 scores to P (bf16 pairs); columns at or past `limit` are minus infinity
+template <bool MASKED> __device__ __forceinline__ void mask_chunk(uint32_t (&r)[32], int limit)
+{
+    if (MASKED) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+            if (e >= limit) r[e] = 0xff800000u;
+    }
+}
+__device__ __forceinline__ float max_chunk(const uint32_t (&r)[32], float m)
+{
+    float a = m, b = __uint_as_float(r[0]);
+#pragma unroll
+    for (int e = 1; e < 29; e += 4) {
+        a = max3(a, __uint_as_float(r[e]), __uint_as_float(r[e + 1]));
+        b = max3(b, __uint_as_float(r[e + 2]), __uint_as_float(r[e + 3]));
+    }
+    return max3(max3(a, b, __uint_as_float(r[29])), __uint_as_float(r[30]), __uint_as_float(r[31]));
+}
+// 2^x for a pair without the special-function unit: round to the nearest integer n (Cody and Waite's range
+// reduction, by adding and subtracting 1.5 2^23), a polynomial in f = x - n on [-1/2, 1/2], n into the
+// exponent.  Coefficients: minimax of the relative error by Remez's exchange, 7.5e-8; x below -126 gives
+// 2^-126 at least, NaN stays non-finite.
+__device__ __forceinline__ void poly_exp2(uint64_t x, float &a, float &b)
+{
+    float lo, hi;
+    unpair2(x, lo, hi);
+    asm("max.NaN.f32 %0, %0, 0fC2FC0000;" : "+f"(lo));      // -126
+    asm("max.NaN.f32 %0, %0, 0fC2FC0000;" : "+f"(hi));
+    const uint64_t t = pair2(lo, hi), magic = pair2(12582912.0f, 12582912.0f), un = pair2(-12582912.0f, -12582912.0f);
+    const uint64_t n = add2(t, magic), f = fma2(add2(n, un), pair2(-1.0f, -1.0f), t);
+    uint64_t q = fma2(f, pair2(0.0013276472454890609f, 0.0013276472454890609f), pair2(0.009675540961325169f, 0.009675540961325169f));
+    q = fma2(q, f, pair2(0.05550713092088699f, 0.05550713092088699f));
+    q = fma2(q, f, pair2(0.24022120237350464f, 0.24022120237350464f));
+    q = fma2(q, f, pair2(0.6931469440460205f, 0.6931469440460205f));
+    q = fma2(q, f, pair2(1.0000001192092896f, 1.0000001192092896f));
+    float nl, nh;
+    unpair2(n, nl, nh);
+    unpair2(q, lo, hi);
+    a = __int_as_float(__float_as_int(lo) + (__float_as_int(nl) << 23));
+    b = __int_as_float(__float_as_int(hi) + (__float_as_int(nh) << 23));
+}
+
+// 32 scores of a row to P: 2^(c2 s - c2 m), summed, packed to bf16.  POLY of the 16 pairs take poly_exp2: the
+// special-function unit alone (4 lanes a cycle) would need as long as the two products of the tile.
+template <int POLY>
+__device__ __forceinline__ void exp_chunk(const uint32_t (&r)[32], uint64_t c2, uint64_t neg_mc, uint64_t (&sum)[2], uint32_t (&pk)[16])
+{
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const uint64_t t = fma2(pair2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, neg_mc);
+        float a, b;
+        if ((e + 1) * POLY / 16 != e * POLY / 16) {
+            poly_exp2(t, a, b);
+        } else {
+            unpair2(t, a, b);
+            a = fast_exp2(a);
+            b = fast_exp2(b);
+        }
+        sum[e & 1] = add2(sum[e & 1], pair2(a, b));
+        // P enters the second product in bf16: relative 2^-8 per term, averaged over the row
+        pk[e] = pack_bf16(a, b);
+    }
+}
+#ifndef AT_POLY
+#define AT_POLY 4
+#endif
+constexpr int POLY_PAIRS = AT_POLY;
+
+// One block of scores of one row per thread: running maximum m and sum l, P over the scores.  The second half
+// of the scores is read twice (for the maximum, then again), which keeps a row's registers below what would
+// spill.  P is handed over in two halves (p_full, p_full + 8), so that the second product starts while the
+// second half is made.
+template <int DP, bool MASKED>
+__device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, int cols, int limit, float c2, bool first, float &m,
+                                              float &l, uint32_t p_full, int lane)
+{
+    constexpr int POLY = MASKED ? 0 : POLY_PAIRS;     // a masked score has to give zero
+    uint32_t x[32], y[32], u[32], v[32];
+    const bool upper = !MASKED || cols > 64;
+    float bm = -INFINITY;
+    tmem_ld32(t_s, x);
+    tmem_ld32(t_s + 32, y);
+    if (upper) {
+        tmem_ld32(t_s + 64, u);
+        tmem_ld32(t_s + 96, v);
+    }
+    tmem_ld_wait(x);
+    tmem_ld_wait(y);
+    mask_chunk<MASKED>(x, limit);
+    mask_chunk<MASKED>(y, limit - 32);
+    bm = max_chunk(y, max_chunk(x, bm));
+    if (upper) {
+        tmem_ld_wait(u);
+        tmem_ld_wait(v);
+        mask_chunk<MASKED>(u, limit - 64);
+        mask_chunk<MASKED>(v, limit - 96);
+        bm = max_chunk(v, max_chunk(u, bm));
+    }
+    if (first) {
+        m = bm;
+    } else if (__any_sync(0xffffffffu, (bm - m) * c2 > 8.0f)) {
+        // the scores of this block were issued after the previous O += P V, so O is at rest
+        const float mn = fmaxf(m, bm), f = fast_exp2((m - mn) * c2);
+        m = mn;
+        l *= f;
+#pragma unroll
+        for (int c = 0; c < DP; c += 16) {
+            uint32_t o[16];
+            tmem_ld16(t_o + c, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            tmem_st16(t_o + c, o);
+        }
+    }
+    const uint64_t c2p = pair2(c2, c2), mcp = pair2(-m * c2, -m * c2);
+    uint64_t sum[2] = {0, 0};
+    uint32_t pk[16];
+    if (upper) tmem_ld32(t_s + 64, u);
+    exp_chunk<POLY>(x, c2p, mcp, sum, pk);
+    tmem_st16(t_s, pk);
+    exp_chunk<POLY>(y, c2p, mcp, sum, pk);
+    tmem_st16(t_s + 16, pk);
+    tmem_st_wait();
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(p_full);
+    if (upper) {
+        tmem_ld32(t_s + 96, v);
+        tmem_ld_wait(u);
+        mask_chunk<MASKED>(u, limit - 64);
+        exp_chunk<POLY>(u, c2p, mcp, sum, pk);
+        tmem_st16(t_s + 32, pk);
+        tmem_ld_wait(v);
+        mask_chunk<MASKED>(v, limit - 96);
+        exp_chunk<POLY>(v, c2p, mcp, sum, pk);
+        tmem_st16(t_s + 48, pk);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+    }
+    if (lane == 0) mbar_arrive(p_full + 8);
+    float a, b;
+    unpair2(add2(sum[0], sum[1]), a, b);
+    l += a + b;
+}
+
 struct FwdItem {
     int start, len, t0, h, nb0, nb1, end0, end1;   // key blocks and first key past the keys of the two tiles
-    __device__ FwdItem(const AtParams &p, int i)
+    __device__ FwdItem(const AtParams &p, int i, bool whole_warp = true)
     {
-        const int4 e = p.items[i / p.hk];
+        int4 e = p.items[i / p.hk];
+        if (whole_warp) e = make_int4(uniform(e.x), uniform(e.y), uniform(e.z), uniform(e.w));
         h = i % p.hk;
         start = e.x; len = e.y; t0 = e.z;
         end0 = p.causal ? min(t0 + p.tokens, len) : len;
@@ -192,20 +426,21 @@ struct FwdItem {
 };
 
 template <int DP>
-__global__ void __launch_bounds__(AT_THREADS, 1)
+__global__ void __launch_bounds__(FwdWarps::THREADS, 1)
 k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
 {
     constexpr int T_BYTES = FwdShape<DP>::T_BYTES, SLOTS = FwdShape<DP>::SLOTS;
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t tiles = align_tiles(smem_raw), q_tile = tiles, ring = tiles + 2 * T_BYTES;
-    FwdCtl *ctl = reinterpret_cast<FwdCtl *>(smem_raw + (tiles - smem_u32(smem_raw)) + (2 + SLOTS) * T_BYTES);
+    extern __shared__ __align__(1024) uint8_t smem_raw[];      // tiles need 1024 bytes
+    const uint32_t tiles = smem_u32(smem_raw), q_tile = tiles, ring = tiles + 2 * T_BYTES;
+    FwdCtl *ctl = reinterpret_cast<FwdCtl *>(smem_raw + (2 + SLOTS) * T_BYTES);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&ctl->q_full[i]), 1);
             mbar_init(smem_u32(&ctl->q_empty[i]), 1);
             mbar_init(smem_u32(&ctl->s_full[i]), 1);
-            mbar_init(smem_u32(&ctl->p_full[i]), 4);
+            mbar_init(smem_u32(&ctl->p_full[i][0]), 4);
+            mbar_init(smem_u32(&ctl->p_full[i][1]), 4);
             mbar_init(smem_u32(&ctl->o_full[i]), 1);
             mbar_init(smem_u32(&ctl->o_free[i]), 4);
         }
@@ -220,29 +455,28 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
     const int used = p.group * p.tokens;     // rows of a tile that a box fills; the others stay zero
     if (used < TILE) zero_smem(q_tile, 2 * T_BYTES);
     fence_proxy_async_smem();
-    if (warp == W_MMA) { tmem_alloc(smem_u32(&ctl->tmem_base), AT_TMEM_COLS); tmem_relinquish(); }
+    if (warp == FwdWarps::MMA) { tmem_alloc(smem_u32(&ctl->tmem_base), AT_TMEM_COLS); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = ctl->tmem_base;
     volatile int *ab = &ctl->abort_flag;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     ItemLoop loop(p.n_items);
 
-    if (warp >= W_TMA) regs_down<AT_REGS_SERVICE>();
-    if (warp == W_TMA) {
+    if (warp < FwdWarps::FIRST) regs_down<FwdWarps::REGS_SERVICE>();
+    if (warp == FwdWarps::TMA) {
         if (lane == 0) {
             uint32_t pos = 0, nq[2] = {0, 0};
             bool ok = true;
             auto acquire = [&]() {           // next ring slot, free to be written
                 const uint32_t s = pos % SLOTS;
-                ok = ok && wait_bar(smem_u32(&ctl->kv_empty[s]), ((pos / SLOTS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                ok = ok && wait_bar<false>(smem_u32(&ctl->kv_empty[s]), ((pos / SLOTS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                 ++pos;
                 return s;
             };
             auto load_q = [&](const FwdItem &it, int g) {
-                ok = ok && wait_bar(smem_u32(&ctl->q_empty[g]), (nq[g] & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                ok = ok && wait_bar<false>(smem_u32(&ctl->q_empty[g]), (nq[g] & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                 if (!ok) return;
                 const uint32_t bar = smem_u32(&ctl->q_full[g]);
                 mbar_expect_tx(bar, (uint32_t)(used * DP * 2));
@@ -250,7 +484,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
                 ++nq[g];
             };
             for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
-                const FwdItem it(p, i);
+                const FwdItem it(p, i, false);      // one lane
                 const int n = it.blocks();
                 load_q(it, 0);
                 for (int j = 0; j < n && ok; ++j) {
@@ -269,7 +503,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
                 }
             }
         }
-    } else if (warp == W_TAIL) {
+    } else if (warp == FwdWarps::TAIL) {
         uint32_t pos = 0, seen = 0;          // bit s: parity of the tail events of slot s
         bool ok = true;
         for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
@@ -278,7 +512,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             pos += 2 * n;
             if (!it.dirty_tail()) continue;
             const uint32_t s = (pos - 1) % SLOTS;
-            ok = wait_bar(smem_u32(&ctl->tail[s]), (seen >> s) & 1, ab, p.status, SITE_PRODUCER_EMPTY);
+            ok = wait_bar<false>(smem_u32(&ctl->tail[s]), (seen >> s) & 1, ab, p.status, SITE_PRODUCER_EMPTY);
             if (!ok) break;
             seen ^= 1u << s;
             const int valid = it.len - (n - 1) * TILE;
@@ -287,65 +521,82 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&ctl->kv_full[s]));
         }
-    } else if (warp == W_MMA) {
-        if (lane == 0) {
-            uint32_t base = 0, nq[2] = {0, 0}, np[2] = {0, 0};
-            bool ok = true;
-            auto wait_slot = [&](uint32_t n) {
-                ok = ok && wait_bar(smem_u32(&ctl->kv_full[n % SLOTS]), (n / SLOTS) & 1, ab, p.status, SITE_MMA_FULL);
-                return ring + (n % SLOTS) * T_BYTES;
+    } else if (warp == FwdWarps::MMA) {
+        const uint32_t on = elect_one();     // the warp walks as one, one thread issues
+        const uint32_t q_desc = desc_rows(q_tile), k_desc0 = desc_rows(ring), v_desc0 = desc_across(ring);
+        const uint32_t kv_full = smem_u32(&ctl->kv_full[0]), kv_empty = smem_u32(&ctl->kv_empty[0]);
+        uint32_t slot = 0, phase = 0, nq[2] = {0, 0}, np[2] = {0, 0};
+        bool ok = true;
+        auto wait_slot = [&]() { ok = ok && wait_warp(kv_full + 8 * slot, phase, ab, p.status, SITE_MMA_FULL); };
+        auto next_slot = [&]() {
+            const uint32_t s = slot;
+            if (++slot == SLOTS) { slot = 0; phase ^= 1; }
+            return s;
+        };
+        for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
+            const FwdItem it(p, i);
+            const int n = it.blocks();
+            const int nb[2] = {it.nb0, it.nb1};
+            const int last_cols[2] = {mma_cols(it.end0 - (it.nb0 - 1) * TILE), mma_cols(it.end1 - (it.nb1 - 1) * TILE)};
+            auto scores = [&](int g, int j, uint32_t k_slot) {
+                mma_rows_rows<DP>(on, tmem + g * TILE, q_desc + g * (T_BYTES >> 4), k_desc0 + k_slot * (T_BYTES >> 4),
+                                  idesc_rows(j == nb[g] - 1 ? last_cols[g] : TILE));
+                umma_commit_if(on, smem_u32(&ctl->s_full[g]));
             };
-            for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
-                const FwdItem it(p, i);
-                const int n = it.blocks();
-                auto scores = [&](int g, int j, uint32_t k_tile) {
-                    const int end = g ? it.end1 : it.end0;
-                    mma_rows_rows<DP>(tmem + g * TILE, q_tile + g * T_BYTES, k_tile, mma_cols(end - j * TILE));
-                    umma_commit(smem_u32(&ctl->s_full[g]));
-                    if (j == (g ? it.nb1 : it.nb0) - 1) umma_commit(smem_u32(&ctl->q_empty[g]));
-                };
-                uint32_t kt = wait_slot(base);
-                for (int g = 0; g < 2 && ok; ++g) {
-                    if (g && !it.nb1) break;
-                    ok = wait_bar(smem_u32(&ctl->q_full[g]), nq[g] & 1, ab, p.status, SITE_MMA_FULL);
+            wait_slot();
+            uint32_t ks = next_slot();
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                if (!ok || nb[g] == 0) break;
+                ok = wait_warp(smem_u32(&ctl->q_full[g]), nq[g] & 1, ab, p.status, SITE_MMA_FULL);
+                if (!ok) break;
+                ++nq[g];
+                tc_fence_after();
+                scores(g, 0, ks);
+                if (nb[g] == 1) umma_commit_if(on, smem_u32(&ctl->q_empty[g]));
+            }
+            if (!ok) break;
+            umma_commit_if(on, kv_empty + 8 * ks);
+            for (int j = 0; j < n; ++j) {
+                wait_slot();
+                const uint32_t vs = next_slot();
+                const bool more = j + 1 < n;
+                if (more) { wait_slot(); ks = next_slot(); }
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
                     if (!ok) break;
-                    ++nq[g];
+                    if (j >= nb[g]) continue;
+                    const uint32_t pt = tmem + g * TILE, ot = tmem + 2 * TILE + g * DP, vd = v_desc0 + vs * (T_BYTES >> 4);
+                    const bool last = j == nb[g] - 1;
+                    const int steps = last ? last_cols[g] / 16 : TILE / 16;
+                    if (j == 0) ok = wait_warp(smem_u32(&ctl->o_free[g]), (nq[g] - 1) & 1 ^ 1, ab, p.status, SITE_MMA_TMEM_EMPTY);
+                    ok = ok && wait_warp(smem_u32(&ctl->p_full[g][0]), np[g] & 1, ab, p.status, SITE_MMA_FULL);
+                    if (!ok) break;
                     tc_fence_after();
-                    scores(g, 0, kt);
+                    mma_tmem_rows<DP, 0, 4, 8>(on, ot, pt, vd, steps, j > 0);
+                    ok = wait_warp(smem_u32(&ctl->p_full[g][1]), np[g] & 1, ab, p.status, SITE_MMA_FULL);
+                    if (!ok) break;
+                    ++np[g];
+                    tc_fence_after();
+                    mma_tmem_rows<DP, 4, 4, 8>(on, ot, pt, vd, steps, 1);
+                    if (last) {
+                        umma_commit_if(on, smem_u32(&ctl->o_full[g]));
+                    } else {
+                        scores(g, j + 1, ks);
+                        if (j + 2 == nb[g]) umma_commit_if(on, smem_u32(&ctl->q_empty[g]));
+                    }
                 }
                 if (!ok) break;
-                umma_commit(smem_u32(&ctl->kv_empty[base % SLOTS]));
-                for (int j = 0; j < n && ok; ++j) {
-                    const uint32_t vt = wait_slot(base + 2 * j + 1);
-                    const bool more = j + 1 < n;
-                    kt = more ? wait_slot(base + 2 * j + 2) : 0;
-                    for (int g = 0; g < 2 && ok; ++g) {
-                        const int nb = g ? it.nb1 : it.nb0, end = g ? it.end1 : it.end0;
-                        if (j >= nb) continue;
-                        ok = wait_bar(smem_u32(&ctl->p_full[g]), np[g] & 1, ab, p.status, SITE_MMA_FULL);
-                        ++np[g];
-                        if (ok && j == 0)
-                            ok = wait_bar(smem_u32(&ctl->o_free[g]), (nq[g] - 1) & 1 ^ 1, ab, p.status, SITE_MMA_TMEM_EMPTY);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t pt = tmem + g * TILE;
-                        mma_tmem_rows<DP>(tmem + 2 * TILE + g * DP, pt, pt + 32, vt, mma_cols(end - j * TILE), j > 0);
-                        if (j == nb - 1) umma_commit(smem_u32(&ctl->o_full[g]));
-                        else scores(g, j + 1, kt);
-                    }
-                    if (!ok) break;
-                    umma_commit(smem_u32(&ctl->kv_empty[(base + 2 * j + 1) % SLOTS]));
-                    if (more) umma_commit(smem_u32(&ctl->kv_empty[(base + 2 * j + 2) % SLOTS]));
-                }
-                base += 2 * n;
+                umma_commit_if(on, kv_empty + 8 * vs);
+                if (more) umma_commit_if(on, kv_empty + 8 * ks);
             }
         }
-    } else if (warp < W_TMA) {
-        regs_up<AT_REGS_ARITH>();
-        const int g = warp >> 2, row = (warp & 3) * 32 + lane;
+    } else if (warp >= FwdWarps::FIRST) {
+        regs_up<FwdWarps::REGS_ARITH>();
+        const int g = (warp - FwdWarps::FIRST) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + lanes + g * TILE, t_o = tmem + lanes + 2 * TILE + g * DP;
-        const uint32_t s_full = smem_u32(&ctl->s_full[g]), p_full = smem_u32(&ctl->p_full[g]);
+        const uint32_t s_full = smem_u32(&ctl->s_full[g]), p_full = smem_u32(&ctl->p_full[g][0]);
         uint32_t ns = 0, no = 0;
         bool ok = true;
         const int row_t = row / p.group, row_h = row - row_t * p.group;
@@ -357,75 +608,19 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             const int row_end = p.causal ? min(token + 1, it.len) : it.len;   // keys of this row
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; j < nb; ++j) {
-                ok = wait_bar(s_full, ns & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = wait_bar<true>(s_full, ns & 1, ab, p.status, SITE_EPI_TMEM_FULL);
                 ++ns;
                 if (!ok) break;
                 tc_fence_after();
-                const int cols = mma_cols(end - j * TILE);
-                uint32_t r[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (32 * c < cols) tmem_ld32(t_s + 32 * c, r[c]);
-                tmem_ld_wait();
                 // columns past the row's keys (or past the ones the MMA wrote) count as minus infinity
-                if (cols < TILE || j * TILE + TILE > (p.causal ? t0 + 1 : it.len)) {
-                    const int limit = row_end - j * TILE;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (32 * c + e >= limit) r[c][e] = 0xff800000u;
-                }
-                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2)
-                        mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(r[c][e])), __uint_as_float(r[c][e + 1]));
-                const float bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                if (j == 0) {
-                    m = bm;
-                } else if (__any_sync(0xffffffffu, (bm - m) * p.c2 > 8.0f)) {
-                    // S of this block was issued after the previous O += P V, so O is at rest
-                    const float mn = fmaxf(m, bm), f = fast_exp2((m - mn) * p.c2);
-                    m = mn;
-                    l *= f;
-#pragma unroll
-                    for (int c = 0; c < DP; c += 32) {
-                        uint32_t o[32];
-                        tmem_ld32(t_o + c, o);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        tmem_st32(t_o + c, o);
-                    }
-                }
-                const float mc = m * p.c2;
-                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    if (32 * c < cols) {
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            const float a = fast_exp2(fmaf(__uint_as_float(r[c][e]), p.c2, -mc));
-                            const float b = fast_exp2(fmaf(__uint_as_float(r[c][e + 1]), p.c2, -mc));
-                            sum[e & 2 ? 1 : 0] += a;
-                            sum[e & 2 ? 3 : 2] += b;
-                            // P enters the second product in bf16: relative 2^-8 per term, averaged over the row
-                            pk[e / 2] = pack_bf16(a, b);
-                        }
-                        tmem_st16(t_s + 16 * c, pk);
-                    }
-                }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_full);
+                const int cols = mma_cols(end - j * TILE);
+                if (cols < TILE || j * TILE + TILE > (p.causal ? t0 + 1 : it.len))
+                    softmax_block<DP, true>(t_s, t_o, cols, row_end - j * TILE, p.c2, j == 0, m, l, p_full, lane);
+                else
+                    softmax_block<DP, false>(t_s, t_o, TILE, TILE, p.c2, j == 0, m, l, p_full, lane);
             }
             if (!ok) break;
-            ok = wait_bar(smem_u32(&ctl->o_full[g]), no & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+            ok = wait_bar<true>(smem_u32(&ctl->o_full[g]), no & 1, ab, p.status, SITE_EPI_TMEM_FULL);
             ++no;
             if (!ok) break;
             tc_fence_after();
@@ -438,7 +633,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             for (int c = 0; c < DP; c += 32) {
                 uint32_t o[32];
                 tmem_ld32(t_o + c, o);
-                tmem_ld_wait();
+                tmem_ld_wait(o);
                 if (live) store_row32(dst, o, inv, c, p.d);
             }
             tc_fence_before();
@@ -447,21 +642,21 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             if (live) p.lse[tok * p.hq + head] = fmaf(m, p.scale, logf(l));
         }
     }
-    cta_teardown(ab, tmem);
+    cta_teardown(ab, ctl->tmem_base, FwdWarps::MMA);
 }
 
 // ------------------------------------------------------------------------------------ dK, dV
 // One item = one key tile (128 keys) of one kv head against the row tiles that attend to it.  The
 // scores are computed transposed (keys on the accumulator rows), so that P^T and dS^T are already the
-// tensor-memory operands of dV += P^T dO and dK += dS^T Q.  The two warpgroups share the rows and
-// split the columns.  While the arithmetic warps turn scores into P, the tensor cores run the
+// tensor-memory operands of dV += P^T dO and dK += dS^T Q.  Four warpgroups share the rows, each
+// with a quarter of the columns.  While the arithmetic warps turn scores into P, the tensor cores run the
 // previous dK and the next dP; while they turn dP into dS, dV and the next scores.
 // Sums over the query heads of a group are sums over tile rows: fixed order, no atomics.
 template <int DP> struct KvShape {
     static constexpr int T_BYTES = tile_bytes<DP>();
     static constexpr int STAGES = 2;
     static constexpr int STAT_BYTES = TILE * 8;
-    static constexpr int SMEM = (2 + 2 * STAGES) * T_BYTES + STAGES * STAT_BYTES + 1024 + 512;
+    static constexpr int SMEM = (2 + 2 * STAGES) * T_BYTES + STAGES * STAT_BYTES + 512;
 };
 struct alignas(8) KvCtl {
     uint64_t kv_full, kv_empty, q_full[2], g_full[2], empty[2], q_tail[2], g_tail[2];
@@ -471,9 +666,10 @@ struct alignas(8) KvCtl {
 };
 struct KvItem {
     int start, len, k0, base, h, first, n;      // row tiles first .. first + n - 1 of the sequence
-    __device__ KvItem(const AtParams &p, int i)
+    __device__ KvItem(const AtParams &p, int i, bool whole_warp = true)
     {
-        const int4 e = p.items[i / p.hk];
+        int4 e = p.items[i / p.hk];
+        if (whole_warp) e = make_int4(uniform(e.x), uniform(e.y), uniform(e.z), uniform(e.w));
         h = i % p.hk;
         start = e.x; len = e.y; k0 = e.z; base = e.w;
         first = p.causal ? k0 / p.tokens : 0;
@@ -488,13 +684,13 @@ struct KvItem {
 };
 
 template <int DP>
-__global__ void __launch_bounds__(AT_THREADS, 1)
+__global__ void __launch_bounds__(BwdWarps::THREADS, 1)
 k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
 {
     using Sh = KvShape<DP>;
     constexpr int T_BYTES = Sh::T_BYTES;
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t tiles = align_tiles(smem_raw);
+    extern __shared__ __align__(1024) uint8_t smem_raw[];      // tiles need 1024 bytes
+    const uint32_t tiles = smem_u32(smem_raw);
     const uint32_t k_tile = tiles, v_tile = tiles + T_BYTES, q_ring = tiles + 2 * T_BYTES, g_ring = q_ring + 2 * T_BYTES;
     const uint32_t stats = g_ring + 2 * T_BYTES;
     uint8_t *after = smem_raw + (stats - smem_u32(smem_raw));
@@ -512,35 +708,34 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
         mbar_init(smem_u32(&ctl->kv_empty), 1);
         mbar_init(smem_u32(&ctl->s_full), 1);
         mbar_init(smem_u32(&ctl->g_scores), 1);
-        mbar_init(smem_u32(&ctl->p_ready), 8);
-        mbar_init(smem_u32(&ctl->ds_ready), 8);
+        mbar_init(smem_u32(&ctl->p_ready), BwdWarps::COUNT);
+        mbar_init(smem_u32(&ctl->ds_ready), BwdWarps::COUNT);
         mbar_init(smem_u32(&ctl->acc_full), 1);
-        mbar_init(smem_u32(&ctl->acc_free), 8);
+        mbar_init(smem_u32(&ctl->acc_free), BwdWarps::COUNT);
         ctl->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     const int used = p.group * p.tokens;
     if (used < TILE) zero_smem(q_ring, 4 * T_BYTES);
     fence_proxy_async_smem();
-    if (warp == W_MMA) { tmem_alloc(smem_u32(&ctl->tmem_base), AT_TMEM_COLS); tmem_relinquish(); }
+    if (warp == BwdWarps::MMA) { tmem_alloc(smem_u32(&ctl->tmem_base), AT_TMEM_COLS); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = ctl->tmem_base;
     volatile int *ab = &ctl->abort_flag;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     ItemLoop loop(p.n_items);
     const uint32_t t_s = tmem, t_dp = tmem + TILE, t_dv = tmem + 2 * TILE, t_dk = t_dv + DP;
 
-    if (warp >= W_TMA) regs_down<AT_REGS_SERVICE>();
-    if (warp == W_TMA) {
+    if (warp < BwdWarps::FIRST) regs_down<BwdWarps::REGS_SERVICE>();
+    if (warp == BwdWarps::TMA) {
         if (lane == 0) {
             uint32_t cnt = 0, items = 0;
             bool ok = true;
             for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
-                const KvItem it(p, i);
-                ok = wait_bar(smem_u32(&ctl->kv_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                const KvItem it(p, i, false);      // one lane
+                ok = wait_bar<false>(smem_u32(&ctl->kv_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                 if (!ok) break;
                 const uint32_t kvb = smem_u32(&ctl->kv_full);
                 mbar_expect_tx(kvb, 2 * T_BYTES);
@@ -548,7 +743,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 load_tile<DP>(v_tile, &tm.v, it.h, it.start + it.k0, kvb);
                 for (int j = 0; j < it.n; ++j, ++cnt) {
                     const uint32_t s = cnt & 1;
-                    ok = wait_bar(smem_u32(&ctl->empty[s]), ((cnt >> 1) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    ok = wait_bar<false>(smem_u32(&ctl->empty[s]), ((cnt >> 1) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                     if (!ok) break;
                     const int tile = it.first + j, token = it.start + tile * p.tokens;
                     const bool dirty = it.dirty(p, tile);
@@ -562,7 +757,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 }
             }
         }
-    } else if (warp == W_TAIL) {
+    } else if (warp == BwdWarps::TAIL) {
         uint32_t cnt = 0, seen = 0;
         bool ok = true;
         for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
@@ -573,7 +768,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
             const uint32_t s = (cnt - 1) & 1;
             const int valid = it.valid(p, tile);
             for (int w = 0; w < 2 && ok; ++w) {
-                ok = wait_bar(smem_u32(w ? &ctl->g_tail[s] : &ctl->q_tail[s]), (seen >> s) & 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                ok = wait_bar<false>(smem_u32(w ? &ctl->g_tail[s] : &ctl->q_tail[s]), (seen >> s) & 1, ab, p.status, SITE_PRODUCER_EMPTY);
                 if (!ok) break;
                 zero_rows<DP>((w ? g_ring : q_ring) + s * T_BYTES, valid, min(mma_cols(valid), used), lane);
                 fence_proxy_async_smem();
@@ -582,54 +777,55 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
             }
             seen ^= 1u << s;
         }
-    } else if (warp == W_MMA) {
-        if (lane == 0) {
-            uint32_t cnt = 0, items = 0;
-            bool ok = true;
-            for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
-                const KvItem it(p, i);
-                auto cols_of = [&](int j) { return mma_cols(it.valid(p, it.first + j)); };
-                auto scores = [&](int j, uint32_t c) {
-                    ok = ok && wait_bar(smem_u32(&ctl->q_full[c & 1]), (c >> 1) & 1, ab, p.status, SITE_MMA_FULL);
-                    if (!ok) return;
-                    tc_fence_after();
-                    mma_rows_rows<DP>(t_s, k_tile, q_ring + (c & 1) * T_BYTES, cols_of(j));
-                    umma_commit(smem_u32(&ctl->s_full));
-                };
-                auto grad_scores = [&](int j, uint32_t c) {
-                    ok = ok && wait_bar(smem_u32(&ctl->g_full[c & 1]), (c >> 1) & 1, ab, p.status, SITE_MMA_FULL);
-                    if (!ok) return;
-                    tc_fence_after();
-                    mma_rows_rows<DP>(t_dp, v_tile, g_ring + (c & 1) * T_BYTES, cols_of(j));
-                    umma_commit(smem_u32(&ctl->g_scores));
-                };
-                ok = wait_bar(smem_u32(&ctl->kv_full), items & 1, ab, p.status, SITE_MMA_FULL);
-                scores(0, cnt);
-                grad_scores(0, cnt);
-                for (int j = 0; j < it.n && ok; ++j, ++cnt) {
-                    const uint32_t s = cnt & 1;
-                    ok = wait_bar(smem_u32(&ctl->p_ready), cnt & 1, ab, p.status, SITE_MMA_FULL);
-                    if (ok && j == 0)
-                        ok = wait_bar(smem_u32(&ctl->acc_free), (items & 1) ^ 1, ab, p.status, SITE_MMA_TMEM_EMPTY);
-                    if (!ok) break;
-                    tc_fence_after();
-                    mma_tmem_rows<DP>(t_dv, t_s, t_s + 64, g_ring + s * T_BYTES, cols_of(j), j > 0);
-                    if (j + 1 < it.n) scores(j + 1, cnt + 1);
-                    ok = ok && wait_bar(smem_u32(&ctl->ds_ready), cnt & 1, ab, p.status, SITE_MMA_FULL);
-                    if (!ok) break;
-                    tc_fence_after();
-                    mma_tmem_rows<DP>(t_dk, t_dp, t_dp + 64, q_ring + s * T_BYTES, cols_of(j), j > 0);
-                    umma_commit(smem_u32(&ctl->empty[s]));
-                    if (j + 1 < it.n) grad_scores(j + 1, cnt + 1);
-                }
+    } else if (warp == BwdWarps::MMA) {
+        const uint32_t on = elect_one();
+        const uint32_t k_desc = desc_rows(k_tile), v_desc = desc_rows(v_tile), q_desc = desc_rows(q_ring), g_desc = desc_rows(g_ring);
+        const uint32_t q_across = desc_across(q_ring), g_across = desc_across(g_ring);
+        uint32_t cnt = 0, items = 0;
+        bool ok = true;
+        for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
+            const KvItem it(p, i);
+            auto cols_of = [&](int j) { return mma_cols(it.valid(p, it.first + j)); };
+            auto scores = [&](int j, uint32_t c) {
+                ok = ok && wait_warp(smem_u32(&ctl->q_full[c & 1]), (c >> 1) & 1, ab, p.status, SITE_MMA_FULL);
+                if (!ok) return;
+                tc_fence_after();
+                mma_rows_rows<DP>(on, t_s, k_desc, q_desc + (c & 1) * (T_BYTES >> 4), idesc_rows(cols_of(j)));
+                umma_commit_if(on, smem_u32(&ctl->s_full));
+            };
+            auto grad_scores = [&](int j, uint32_t c) {
+                ok = ok && wait_warp(smem_u32(&ctl->g_full[c & 1]), (c >> 1) & 1, ab, p.status, SITE_MMA_FULL);
+                if (!ok) return;
+                tc_fence_after();
+                mma_rows_rows<DP>(on, t_dp, v_desc, g_desc + (c & 1) * (T_BYTES >> 4), idesc_rows(cols_of(j)));
+                umma_commit_if(on, smem_u32(&ctl->g_scores));
+            };
+            ok = wait_warp(smem_u32(&ctl->kv_full), items & 1, ab, p.status, SITE_MMA_FULL);
+            scores(0, cnt);
+            grad_scores(0, cnt);
+            for (int j = 0; j < it.n && ok; ++j, ++cnt) {
+                const uint32_t s = cnt & 1;
+                ok = wait_warp(smem_u32(&ctl->p_ready), cnt & 1, ab, p.status, SITE_MMA_FULL);
+                if (ok && j == 0)
+                    ok = wait_warp(smem_u32(&ctl->acc_free), (items & 1) ^ 1, ab, p.status, SITE_MMA_TMEM_EMPTY);
                 if (!ok) break;
-                umma_commit(smem_u32(&ctl->acc_full));
-                umma_commit(smem_u32(&ctl->kv_empty));
+                tc_fence_after();
+                mma_tmem_rows<DP, 0, 8, 2>(on, t_dv, t_s, g_across + s * (T_BYTES >> 4), cols_of(j) / 16, j > 0);
+                if (j + 1 < it.n) scores(j + 1, cnt + 1);
+                ok = ok && wait_warp(smem_u32(&ctl->ds_ready), cnt & 1, ab, p.status, SITE_MMA_FULL);
+                if (!ok) break;
+                tc_fence_after();
+                mma_tmem_rows<DP, 0, 8, 2>(on, t_dk, t_dp, q_across + s * (T_BYTES >> 4), cols_of(j) / 16, j > 0);
+                umma_commit_if(on, smem_u32(&ctl->empty[s]));
+                if (j + 1 < it.n) grad_scores(j + 1, cnt + 1);
             }
+            if (!ok) break;
+            umma_commit_if(on, smem_u32(&ctl->acc_full));
+            umma_commit_if(on, smem_u32(&ctl->kv_empty));
         }
-    } else if (warp < W_TMA) {
-        regs_up<AT_REGS_ARITH>();
-        const int g = warp >> 2, row = (warp & 3) * 32 + lane, c0 = 64 * g;
+    } else if (warp >= BwdWarps::FIRST) {
+        regs_up<BwdWarps::REGS_ARITH>();
+        const int part = (warp - BwdWarps::FIRST) >> 2, row = (warp & 3) * 32 + lane, c0 = 32 * part;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         uint32_t cnt = 0, items = 0;
         bool ok = true;
@@ -638,93 +834,85 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
             const int key = it.k0 + row;
             for (int j = 0; j < it.n; ++j, ++cnt) {
                 const int tile = it.first + j, t0 = tile * p.tokens;
-                const int cols = mma_cols(it.valid(p, tile));
+                const bool some = c0 < mma_cols(it.valid(p, tile));
                 // causal: row (token, head) r of the tile sees this key if token >= key, r >= (key - t0) group
                 const bool mask = p.causal && t0 < it.k0 + TILE - 1;
                 const int from = mask ? (key - t0) * p.group - c0 : 0;
                 const uint32_t st = stats + (cnt & 1) * Sh::STAT_BYTES + c0 * 8;
-                ok = wait_bar(smem_u32(&ctl->s_full), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = wait_bar<false>(smem_u32(&ctl->s_full), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t r[2][32];
+                uint32_t r[32], pk[16];
+                if (some) {
+                    tmem_ld32(t_s + lanes + c0, r);
+                    tmem_ld_wait(r);
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    if (c0 + 32 * c < cols) tmem_ld32(t_s + lanes + c0 + 32 * c, r[c]);
-                tmem_ld_wait();
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    if (c0 + 32 * c < cols) {
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            float l0, d0, l1, d1;
-                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l0), "=f"(d0), "=f"(l1), "=f"(d1) : "r"(st + (32 * c + e) * 8));
-                            float a = fast_exp2(fmaf(__uint_as_float(r[c][e]), p.c2, -l0));
-                            float b = fast_exp2(fmaf(__uint_as_float(r[c][e + 1]), p.c2, -l1));
-                            if (mask) {
-                                a = 32 * c + e >= from ? a : 0.0f;
-                                b = 32 * c + e + 1 >= from ? b : 0.0f;
-                            }
-                            r[c][e] = __float_as_uint(a);
-                            r[c][e + 1] = __float_as_uint(b);
-                            pk[e / 2] = pack_bf16(a, b);
+                    for (int e = 0; e < 32; e += 2) {
+                        float l0, d0, l1, d1;
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l0), "=f"(d0), "=f"(l1), "=f"(d1) : "r"(st + e * 8));
+                        float a = fast_exp2(fmaf(__uint_as_float(r[e]), p.c2, -l0));
+                        float b = fast_exp2(fmaf(__uint_as_float(r[e + 1]), p.c2, -l1));
+                        if (mask) {
+                            a = e >= from ? a : 0.0f;
+                            b = e + 1 >= from ? b : 0.0f;
                         }
-                        tmem_st16(t_s + lanes + c0 + 16 * c, pk);
+                        r[e] = __float_as_uint(a);
+                        r[e + 1] = __float_as_uint(b);
+                        pk[e / 2] = pack_bf16(a, b);
                     }
-                tmem_st_wait();
+                    tmem_st16(t_s + lanes + c0, pk);
+                    tmem_st_wait();
+                }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready));
-                ok = wait_bar(smem_u32(&ctl->g_scores), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = wait_bar<false>(smem_u32(&ctl->g_scores), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t dp[2][32];
+                if (some) {
+                    uint32_t dp[32];
+                    tmem_ld32(t_dp + lanes + c0, dp);
+                    tmem_ld_wait(dp);
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    if (c0 + 32 * c < cols) tmem_ld32(t_dp + lanes + c0 + 32 * c, dp[c]);
-                tmem_ld_wait();
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    if (c0 + 32 * c < cols) {
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            float l0, d0, l1, d1;
-                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l0), "=f"(d0), "=f"(l1), "=f"(d1) : "r"(st + (32 * c + e) * 8));
-                            float a = __uint_as_float(r[c][e]) * (__uint_as_float(dp[c][e]) - d0);
-                            float b = __uint_as_float(r[c][e + 1]) * (__uint_as_float(dp[c][e + 1]) - d1);
-                            if (mask) {            // a masked product is zero even where dP is not finite
-                                a = 32 * c + e >= from ? a : 0.0f;
-                                b = 32 * c + e + 1 >= from ? b : 0.0f;
-                            }
-                            pk[e / 2] = pack_bf16(a, b);
+                    for (int e = 0; e < 32; e += 2) {
+                        float l0, d0, l1, d1;
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l0), "=f"(d0), "=f"(l1), "=f"(d1) : "r"(st + e * 8));
+                        float a = __uint_as_float(r[e]) * (__uint_as_float(dp[e]) - d0);
+                        float b = __uint_as_float(r[e + 1]) * (__uint_as_float(dp[e + 1]) - d1);
+                        if (mask) {                // a masked product is zero even where dP is not finite
+                            a = e >= from ? a : 0.0f;
+                            b = e + 1 >= from ? b : 0.0f;
                         }
-                        tmem_st16(t_dp + lanes + c0 + 16 * c, pk);
+                        pk[e / 2] = pack_bf16(a, b);
                     }
-                tmem_st_wait();
+                    tmem_st16(t_dp + lanes + c0, pk);
+                    tmem_st_wait();
+                }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&ctl->ds_ready));
             }
             if (!ok) break;
-            ok = wait_bar(smem_u32(&ctl->acc_full), items & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+            ok = wait_bar<false>(smem_u32(&ctl->acc_full), items & 1, ab, p.status, SITE_EPI_TMEM_FULL);
             if (!ok) break;
             tc_fence_after();
-            const bool live = key < it.len;
-            bf16 *dst = (g ? p.out0 + ((int64_t)it.start + key) * p.ld0 : p.out1 + ((int64_t)it.start + key) * p.ld1) + (int64_t)it.h * p.d;
+            // parts 0, 1: the column halves of dV; 2, 3: of dK
+            const bool live = key < it.len, is_k = part >= 2;
+            const int col = (part & 1) * (DP / 2);
+            bf16 *dst = (is_k ? p.out0 + ((int64_t)it.start + key) * p.ld0 : p.out1 + ((int64_t)it.start + key) * p.ld1) + (int64_t)it.h * p.d;
 #pragma unroll
-            for (int c = 0; c < DP; c += 32) {
+            for (int c = 0; c < DP / 2; c += 32) {
                 uint32_t o[32];
-                tmem_ld32((g ? t_dk : t_dv) + lanes + c, o);
-                tmem_ld_wait();
-                if (live) store_row32(dst, o, g ? p.scale : 1.0f, c, p.d);
+                tmem_ld32((is_k ? t_dk : t_dv) + lanes + col + c, o);
+                tmem_ld_wait(o);
+                if (live) store_row32(dst, o, is_k ? p.scale : 1.0f, col + c, p.d);
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_free));
         }
     }
-    cta_teardown(ab, tmem);
+    cta_teardown(ab, ctl->tmem_base, BwdWarps::MMA);
 }
 
 // ------------------------------------------------------------------------------------ dQ
@@ -733,7 +921,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
 template <int DP> struct QShape {
     static constexpr int T_BYTES = tile_bytes<DP>();
     static constexpr int KS = 3, VS = 2;
-    static constexpr int SMEM = (2 + KS + VS) * T_BYTES + 1024 + 512;
+    static constexpr int SMEM = (2 + KS + VS) * T_BYTES + 512;
 };
 struct alignas(8) QCtl {
     uint64_t q_full, q_empty, k_full[3], k_empty[3], k_tail[3], v_full[2], v_empty[2];
@@ -743,9 +931,10 @@ struct alignas(8) QCtl {
 };
 struct QItem {
     int start, len, t0, tile, h, end, nb;
-    __device__ QItem(const AtParams &p, int i)
+    __device__ QItem(const AtParams &p, int i, bool whole_warp = true)
     {
-        const int4 e = p.items[i / p.hk];
+        int4 e = p.items[i / p.hk];
+        if (whole_warp) e = make_int4(uniform(e.x), uniform(e.y), uniform(e.z), uniform(e.w));
         h = i % p.hk;
         start = e.x; len = e.y; t0 = e.z; tile = e.w + t0 / p.tokens;
         end = p.causal ? min(t0 + p.tokens, len) : len;
@@ -755,15 +944,15 @@ struct QItem {
 };
 
 template <int DP>
-__global__ void __launch_bounds__(AT_THREADS, 1)
+__global__ void __launch_bounds__(BwdWarps::THREADS, 1)
 k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
 {
     using Sh = QShape<DP>;
     constexpr int T_BYTES = Sh::T_BYTES, KS = Sh::KS, VS = Sh::VS;
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t tiles = align_tiles(smem_raw);
+    extern __shared__ __align__(1024) uint8_t smem_raw[];      // tiles need 1024 bytes
+    const uint32_t tiles = smem_u32(smem_raw);
     const uint32_t q_tile = tiles, g_tile = tiles + T_BYTES, k_ring = tiles + 2 * T_BYTES, v_ring = k_ring + KS * T_BYTES;
-    QCtl *ctl = reinterpret_cast<QCtl *>(smem_raw + (tiles - smem_u32(smem_raw)) + (2 + KS + VS) * T_BYTES);
+    QCtl *ctl = reinterpret_cast<QCtl *>(smem_raw + (2 + KS + VS) * T_BYTES);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&ctl->q_full), 1);
@@ -780,34 +969,33 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
         mbar_init(smem_u32(&ctl->s_full[0]), 1);
         mbar_init(smem_u32(&ctl->s_full[1]), 1);
         mbar_init(smem_u32(&ctl->g_scores), 1);
-        mbar_init(smem_u32(&ctl->ds_ready), 8);
+        mbar_init(smem_u32(&ctl->ds_ready), BwdWarps::COUNT);
         mbar_init(smem_u32(&ctl->acc_full), 1);
-        mbar_init(smem_u32(&ctl->acc_free), 8);
+        mbar_init(smem_u32(&ctl->acc_free), BwdWarps::COUNT);
         ctl->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     const int used = p.group * p.tokens;
     if (used < TILE) zero_smem(q_tile, 2 * T_BYTES);
     fence_proxy_async_smem();
-    if (warp == W_MMA) { tmem_alloc(smem_u32(&ctl->tmem_base), AT_TMEM_COLS); tmem_relinquish(); }
+    if (warp == BwdWarps::MMA) { tmem_alloc(smem_u32(&ctl->tmem_base), AT_TMEM_COLS); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = ctl->tmem_base;
     volatile int *ab = &ctl->abort_flag;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     ItemLoop loop(p.n_items);
     const uint32_t t_dp = tmem + 2 * TILE, t_dq = tmem + 3 * TILE;
 
-    if (warp >= W_TMA) regs_down<AT_REGS_SERVICE>();
-    if (warp == W_TMA) {
+    if (warp < BwdWarps::FIRST) regs_down<BwdWarps::REGS_SERVICE>();
+    if (warp == BwdWarps::TMA) {
         if (lane == 0) {
             uint32_t cnt = 0, items = 0;
             bool ok = true;
             for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
-                const QItem it(p, i);
-                ok = wait_bar(smem_u32(&ctl->q_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                const QItem it(p, i, false);      // one lane
+                ok = wait_bar<false>(smem_u32(&ctl->q_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                 if (!ok) break;
                 const uint32_t qb = smem_u32(&ctl->q_full);
                 mbar_expect_tx(qb, (uint32_t)(2 * used * DP * 2));
@@ -815,12 +1003,12 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 load_tile<DP>(g_tile, &tm.g, it.h * p.group, it.start + it.t0, qb);
                 for (int j = 0; j < it.nb; ++j, ++cnt) {
                     const uint32_t ks = cnt % KS, vs = cnt % VS;
-                    ok = wait_bar(smem_u32(&ctl->k_empty[ks]), ((cnt / KS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    ok = wait_bar<false>(smem_u32(&ctl->k_empty[ks]), ((cnt / KS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                     if (!ok) break;
                     const uint32_t kb = smem_u32(j == it.nb - 1 && it.dirty_tail() ? &ctl->k_tail[ks] : &ctl->k_full[ks]);
                     mbar_expect_tx(kb, T_BYTES);
                     load_tile<DP>(k_ring + ks * T_BYTES, &tm.k, it.h, it.start + j * TILE, kb);
-                    ok = wait_bar(smem_u32(&ctl->v_empty[vs]), ((cnt / VS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    ok = wait_bar<false>(smem_u32(&ctl->v_empty[vs]), ((cnt / VS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                     if (!ok) break;
                     const uint32_t vb = smem_u32(&ctl->v_full[vs]);
                     mbar_expect_tx(vb, T_BYTES);
@@ -828,7 +1016,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 }
             }
         }
-    } else if (warp == W_TAIL) {
+    } else if (warp == BwdWarps::TAIL) {
         uint32_t cnt = 0, seen = 0;
         bool ok = true;
         for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
@@ -836,7 +1024,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
             cnt += it.nb;
             if (!it.dirty_tail()) continue;
             const uint32_t s = (cnt - 1) % KS;
-            ok = wait_bar(smem_u32(&ctl->k_tail[s]), (seen >> s) & 1, ab, p.status, SITE_PRODUCER_EMPTY);
+            ok = wait_bar<false>(smem_u32(&ctl->k_tail[s]), (seen >> s) & 1, ab, p.status, SITE_PRODUCER_EMPTY);
             if (!ok) break;
             seen ^= 1u << s;
             const int valid = it.len - (it.nb - 1) * TILE;
@@ -845,53 +1033,54 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&ctl->k_full[s]));
         }
-    } else if (warp == W_MMA) {
-        if (lane == 0) {
-            uint32_t cnt = 0, items = 0;
-            bool ok = true;
-            for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
-                const QItem it(p, i);
-                auto cols_of = [&](int j) { return mma_cols(it.end - j * TILE); };
-                auto scores = [&](int j, uint32_t c) {
-                    ok = ok && wait_bar(smem_u32(&ctl->k_full[c % KS]), (c / KS) & 1, ab, p.status, SITE_MMA_FULL);
-                    if (!ok) return;
-                    tc_fence_after();
-                    mma_rows_rows<DP>(tmem + (c & 1) * TILE, q_tile, k_ring + (c % KS) * T_BYTES, cols_of(j));
-                    umma_commit(smem_u32(&ctl->s_full[c & 1]));
-                };
-                auto grad_scores = [&](int j, uint32_t c) {
-                    ok = ok && wait_bar(smem_u32(&ctl->v_full[c % VS]), (c / VS) & 1, ab, p.status, SITE_MMA_FULL);
-                    if (!ok) return;
-                    tc_fence_after();
-                    mma_rows_rows<DP>(t_dp, g_tile, v_ring + (c % VS) * T_BYTES, cols_of(j));
-                    umma_commit(smem_u32(&ctl->g_scores));
-                    umma_commit(smem_u32(&ctl->v_empty[c % VS]));
-                };
-                ok = wait_bar(smem_u32(&ctl->q_full), items & 1, ab, p.status, SITE_MMA_FULL);
-                scores(0, cnt);
-                grad_scores(0, cnt);
-                if (it.nb > 1) scores(1, cnt + 1);
-                for (int j = 0; j < it.nb && ok; ++j, ++cnt) {
-                    ok = wait_bar(smem_u32(&ctl->ds_ready), cnt & 1, ab, p.status, SITE_MMA_FULL);
-                    if (!ok) break;
-                    if (j + 1 < it.nb) grad_scores(j + 1, cnt + 1);
-                    if (ok && j == 0)
-                        ok = wait_bar(smem_u32(&ctl->acc_free), (items & 1) ^ 1, ab, p.status, SITE_MMA_TMEM_EMPTY);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t ds = tmem + (cnt & 1) * TILE;
-                    mma_tmem_rows<DP>(t_dq, ds, ds + 64, k_ring + (cnt % KS) * T_BYTES, cols_of(j), j > 0);
-                    umma_commit(smem_u32(&ctl->k_empty[cnt % KS]));
-                    if (j + 2 < it.nb) scores(j + 2, cnt + 2);
-                }
+    } else if (warp == BwdWarps::MMA) {
+        const uint32_t on = elect_one();
+        const uint32_t q_desc = desc_rows(q_tile), g_desc = desc_rows(g_tile), k_desc = desc_rows(k_ring), v_desc = desc_rows(v_ring);
+        const uint32_t k_across = desc_across(k_ring);
+        uint32_t cnt = 0, items = 0;
+        bool ok = true;
+        for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
+            const QItem it(p, i);
+            auto cols_of = [&](int j) { return mma_cols(it.end - j * TILE); };
+            auto scores = [&](int j, uint32_t c) {
+                ok = ok && wait_warp(smem_u32(&ctl->k_full[c % KS]), (c / KS) & 1, ab, p.status, SITE_MMA_FULL);
+                if (!ok) return;
+                tc_fence_after();
+                mma_rows_rows<DP>(on, tmem + (c & 1) * TILE, q_desc, k_desc + (c % KS) * (T_BYTES >> 4), idesc_rows(cols_of(j)));
+                umma_commit_if(on, smem_u32(&ctl->s_full[c & 1]));
+            };
+            auto grad_scores = [&](int j, uint32_t c) {
+                ok = ok && wait_warp(smem_u32(&ctl->v_full[c % VS]), (c / VS) & 1, ab, p.status, SITE_MMA_FULL);
+                if (!ok) return;
+                tc_fence_after();
+                mma_rows_rows<DP>(on, t_dp, g_desc, v_desc + (c % VS) * (T_BYTES >> 4), idesc_rows(cols_of(j)));
+                umma_commit_if(on, smem_u32(&ctl->g_scores));
+                umma_commit_if(on, smem_u32(&ctl->v_empty[c % VS]));
+            };
+            ok = wait_warp(smem_u32(&ctl->q_full), items & 1, ab, p.status, SITE_MMA_FULL);
+            scores(0, cnt);
+            grad_scores(0, cnt);
+            if (it.nb > 1) scores(1, cnt + 1);
+            for (int j = 0; j < it.nb && ok; ++j, ++cnt) {
+                ok = wait_warp(smem_u32(&ctl->ds_ready), cnt & 1, ab, p.status, SITE_MMA_FULL);
                 if (!ok) break;
-                umma_commit(smem_u32(&ctl->acc_full));
-                umma_commit(smem_u32(&ctl->q_empty));
+                if (j + 1 < it.nb) grad_scores(j + 1, cnt + 1);
+                if (ok && j == 0)
+                    ok = wait_warp(smem_u32(&ctl->acc_free), (items & 1) ^ 1, ab, p.status, SITE_MMA_TMEM_EMPTY);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t ds = tmem + (cnt & 1) * TILE;
+                mma_tmem_rows<DP, 0, 8, 2>(on, t_dq, ds, k_across + (cnt % KS) * (T_BYTES >> 4), cols_of(j) / 16, j > 0);
+                umma_commit_if(on, smem_u32(&ctl->k_empty[cnt % KS]));
+                if (j + 2 < it.nb) scores(j + 2, cnt + 2);
             }
+            if (!ok) break;
+            umma_commit_if(on, smem_u32(&ctl->acc_full));
+            umma_commit_if(on, smem_u32(&ctl->q_empty));
         }
-    } else if (warp < W_TMA) {
-        regs_up<AT_REGS_ARITH>();
-        const int g = warp >> 2, row = (warp & 3) * 32 + lane, c0 = 64 * g;
+    } else if (warp >= BwdWarps::FIRST) {
+        regs_up<BwdWarps::REGS_ARITH>();
+        const int part = (warp - BwdWarps::FIRST) >> 2, row = (warp & 3) * 32 + lane, c0 = 32 * part;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const int row_t = row / p.group, row_h = row - row_t * p.group;
         uint32_t cnt = 0, items = 0;
@@ -904,54 +1093,52 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 const int cols = mma_cols(it.end - j * TILE);
                 const bool mask = cols < TILE || j * TILE + TILE > (p.causal ? it.t0 + 1 : it.len);
                 const int limit = row_end - j * TILE - c0;
-                ok = wait_bar(smem_u32(&ctl->s_full[cnt & 1]), (cnt >> 1) & 1, ab, p.status, SITE_EPI_TMEM_FULL);
-                ok = ok && wait_bar(smem_u32(&ctl->g_scores), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = wait_bar<false>(smem_u32(&ctl->s_full[cnt & 1]), (cnt >> 1) & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = ok && wait_bar<false>(smem_u32(&ctl->g_scores), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t t_s = tmem + lanes + (cnt & 1) * TILE + c0;
+                if (c0 < cols) {
+                    const uint32_t t_s = tmem + lanes + (cnt & 1) * TILE + c0;
+                    uint32_t r[32], dp[32], pk[16];
+                    tmem_ld32(t_s, r);
+                    tmem_ld32(t_dp + lanes + c0, dp);
+                    tmem_ld_wait(r);
+                    tmem_ld_wait(dp);
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    if (c0 + 32 * c < cols) {
-                        uint32_t r[32], dp[32], pk[16];
-                        tmem_ld32(t_s + 32 * c, r);
-                        tmem_ld32(t_dp + lanes + c0 + 32 * c, dp);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            float a = fast_exp2(fmaf(__uint_as_float(r[e]), p.c2, -st.x)) * (__uint_as_float(dp[e]) - st.y);
-                            float b = fast_exp2(fmaf(__uint_as_float(r[e + 1]), p.c2, -st.x)) * (__uint_as_float(dp[e + 1]) - st.y);
-                            if (mask) {
-                                a = 32 * c + e < limit ? a : 0.0f;
-                                b = 32 * c + e + 1 < limit ? b : 0.0f;
-                            }
-                            pk[e / 2] = pack_bf16(a, b);
+                    for (int e = 0; e < 32; e += 2) {
+                        float a = fast_exp2(fmaf(__uint_as_float(r[e]), p.c2, -st.x)) * (__uint_as_float(dp[e]) - st.y);
+                        float b = fast_exp2(fmaf(__uint_as_float(r[e + 1]), p.c2, -st.x)) * (__uint_as_float(dp[e + 1]) - st.y);
+                        if (mask) {
+                            a = e < limit ? a : 0.0f;
+                            b = e + 1 < limit ? b : 0.0f;
                         }
-                        tmem_st16(t_s + 16 * c, pk);
+                        pk[e / 2] = pack_bf16(a, b);
                     }
-                tmem_st_wait();
+                    tmem_st16(t_s, pk);
+                    tmem_st_wait();
+                }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&ctl->ds_ready));
             }
             if (!ok) break;
-            ok = wait_bar(smem_u32(&ctl->acc_full), items & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+            ok = wait_bar<false>(smem_u32(&ctl->acc_full), items & 1, ab, p.status, SITE_EPI_TMEM_FULL);
             if (!ok) break;
             tc_fence_after();
             const bool live = row < used && token < it.len;
-            bf16 *dst = p.out0 + ((int64_t)it.start + token) * p.ld0 + (int64_t)(it.h * p.group + row_h) * p.d;
-#pragma unroll
-            for (int c = 0; c < DP / 2; c += 32) {
+            if (c0 < DP) {
                 uint32_t o[32];
-                tmem_ld32(t_dq + lanes + g * (DP / 2) + c, o);
-                tmem_ld_wait();
-                if (live) store_row32(dst, o, p.scale, g * (DP / 2) + c, p.d);
+                tmem_ld32(t_dq + lanes + c0, o);
+                tmem_ld_wait(o);
+                if (live)
+                    store_row32(p.out0 + ((int64_t)it.start + token) * p.ld0 + (int64_t)(it.h * p.group + row_h) * p.d, o, p.scale, c0, p.d);
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_free));
         }
     }
-    cta_teardown(ab, tmem);
+    cta_teardown(ab, ctl->tmem_base, BwdWarps::MMA);
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -971,7 +1158,7 @@ static bool head_map(CUtensorMap *m, const void *base, int d, int heads, int64_t
 constexpr int AT_MAX_DEVICES = 64;
 
 template <typename Kernel>
-static cudaError_t launch_at(Kernel kern, int *sms_by_dev, int smem, const AtMaps &tm, const AtParams &p, cudaStream_t s)
+static cudaError_t launch_at(Kernel kern, int threads, int *sms_by_dev, int smem, const AtMaps &tm, const AtParams &p, cudaStream_t s)
 {
     if (p.n_items <= 0) return cudaSuccess;
     int dev = 0;
@@ -985,7 +1172,7 @@ static cudaError_t launch_at(Kernel kern, int *sms_by_dev, int smem, const AtMap
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(p.n_items < sms_by_dev[dev] ? p.n_items : sms_by_dev[dev]));
-    cfg.blockDim = dim3(AT_THREADS);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
@@ -1015,7 +1202,7 @@ template <int DP> static cudaError_t forward_dp(const AttnArgs &a, cudaStream_t 
     tm.g = tm.q;
     AtParams p = params_of(a, a.fwd_items, a.n_fwd);
     p.out0 = (bf16 *)a.out; p.ld0 = a.ldo; p.lse = a.lse;
-    return launch_at(k_attention_fwd<DP>, sms, FwdShape<DP>::SMEM, tm, p, s);
+    return launch_at(k_attention_fwd<DP>, FwdWarps::THREADS, sms, FwdShape<DP>::SMEM, tm, p, s);
 }
 
 template <int DP> static cudaError_t backward_dp(const AttnArgs &a, cudaStream_t s)
@@ -1029,11 +1216,11 @@ template <int DP> static cudaError_t backward_dp(const AttnArgs &a, cudaStream_t
     if (e != cudaSuccess) return e;
     AtParams p = params_of(a, a.key_items, a.n_keys);
     p.out0 = (bf16 *)a.dk; p.ld0 = a.lddk; p.out1 = (bf16 *)a.dv; p.ld1 = a.lddv;
-    e = launch_at(k_attention_bwd_kv<DP>, sms_kv, KvShape<DP>::SMEM, tm, p, s);
+    e = launch_at(k_attention_bwd_kv<DP>, BwdWarps::THREADS, sms_kv, KvShape<DP>::SMEM, tm, p, s);
     if (e != cudaSuccess) return e;
     p = params_of(a, a.row_items, a.n_rows);
     p.out0 = (bf16 *)a.dq; p.ld0 = a.lddq;
-    return launch_at(k_attention_bwd_q<DP>, sms_q, QShape<DP>::SMEM, tm, p, s);
+    return launch_at(k_attention_bwd_q<DP>, BwdWarps::THREADS, sms_q, QShape<DP>::SMEM, tm, p, s);
 }
 
 cudaError_t launch_attention_tc_forward(const AttnArgs &a, cudaStream_t s)
