@@ -35,7 +35,7 @@ cudaError_t launch_attention_tc_backward(const AttnArgs &a, cudaStream_t s);
 // attention_simt.cu
 cudaError_t launch_attention_simt_forward(const AttnArgs &a, int dtype, cudaStream_t s);
 cudaError_t launch_attention_simt_backward(const AttnArgs &a, int dtype, cudaStream_t s);
-// row statistics of the backward pass (attention_simt.cu): delta = sum_d dout * out per row
-cudaError_t launch_attention_row_stats(const AttnArgs &a, int dtype, int rows_per_tile, cudaStream_t s);
+// row statistics of the tensor-core backward (attention_simt.cu)
+cudaError_t launch_attention_row_stats_tc(const AttnArgs &a, cudaStream_t s);
 
 }  // namespace skipffn

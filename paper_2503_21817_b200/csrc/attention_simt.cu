@@ -244,37 +244,50 @@ k_attention_bwd_q_simt(const AttnArgs a)
     }
 }
 
-// (lse log2 e, delta = sum_d dout out) of every row of a row tile, one warp per row; rows that belong to no
-// token get (infinity, 0), which makes their P and dS zero.  Reads out and dout once: HBM-bound.
-template <typename T>
+// (lse log2 e, delta = sum_d dout out) of every row of a row tile; rows that belong to no token get (infinity, 0),
+// which makes their P and dS zero.  Reads out and dout once: HBM-bound.  A row of at most 128 columns is 16 (bf16)
+// or 32 (fp32) lanes x 16 bytes; all loads of a lane's rows are in flight before the first is used.
+template <typename T, int ROWS>
 __global__ void __launch_bounds__(ST_THREADS)
-k_attention_row_stats(const AttnArgs a, int rows)
+k_attention_row_stats(const AttnArgs a)
 {
+    constexpr int LANES = 128 * (int)sizeof(T) / 16, EL = 16 / (int)sizeof(T), STEP = ST_THREADS / LANES, N = ROWS / STEP;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const Item it = item_of(a.row_items, a.hk);
     const int valid = min(a.tokens, it.len - it.t0) * a.group;
-    float2 *dst = a.row_stats + ((int64_t)(it.base + it.t0 / a.tokens) * a.hk + it.h) * rows;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-#pragma unroll 4
-    for (int r = warp; r < rows; r += ST_THREADS / 32) {
-        float2 v = make_float2(INFINITY, 0.0f);
-        if (r < valid) {
+    float2 *dst = a.row_stats + ((int64_t)(it.base + it.t0 / a.tokens) * a.hk + it.h) * ROWS;
+    const int first = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    uint4 x[N], y[N];
+    float l[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int r = first + k * STEP;
+        x[k] = y[k] = make_uint4(0, 0, 0, 0);
+        l[k] = 0.0f;
+        if (r < valid && EL * lane < a.d) {
             const int64_t tok = (int64_t)it.start + it.t0 + r / a.group;
             const int head = it.h * a.group + r % a.group;
-            float dot = 0.0f;
-            if (4 * lane < a.d) {
-                float x[4], y[4];
-                load4((const T *)a.out_in + tok * a.ldo + (int64_t)head * a.d + 4 * lane, x);
-                load4((const T *)a.dout + tok * a.lddo + (int64_t)head * a.d + 4 * lane, y);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) dot = fmaf(x[e], y[e], dot);
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-            v = make_float2(a.lse[tok * a.hq + head] * LOG2E, dot);
+            x[k] = *reinterpret_cast<const uint4 *>((const T *)a.out_in + tok * a.ldo + (int64_t)head * a.d + EL * lane);
+            y[k] = *reinterpret_cast<const uint4 *>((const T *)a.dout + tok * a.lddo + (int64_t)head * a.d + EL * lane);
+            if (lane == 0) l[k] = a.lse[tok * a.hq + head];
         }
-        if (lane == 0) dst[r] = v;
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int r = first + k * STEP;
+        float dot = 0.0f;
+#pragma unroll
+        for (int h = 0; h < EL / 4; ++h) {
+            float u[4], v[4];
+            load4(reinterpret_cast<const T *>(&x[k]) + 4 * h, u);
+            load4(reinterpret_cast<const T *>(&y[k]) + 4 * h, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dot = fmaf(u[e], v[e], dot);
+        }
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+        if (lane == 0) dst[r] = r < valid ? make_float2(l[k] * LOG2E, dot) : make_float2(INFINITY, 0.0f);
     }
 }
 
@@ -299,19 +312,18 @@ cudaError_t launch_attention_simt_forward(const AttnArgs &a, int dtype, cudaStre
                                  : launch(k_attention_fwd_simt<float>, a.n_fwd * a.hk, FWD_SMEM, a, s);
 }
 
-cudaError_t launch_attention_row_stats(const AttnArgs &a, int dtype, int rows_per_tile, cudaStream_t s)
+template <typename T, int ROWS> static cudaError_t row_stats(const AttnArgs &a, cudaStream_t s)
 {
     const int n = a.n_rows * a.hk;
-    if (n <= 0) return cudaSuccess;
-    return dtype == SKIPFFN_BF16 ? launch_pdl(k_attention_row_stats<bf16>, dim3((unsigned)n), dim3(ST_THREADS), s, a, rows_per_tile)
-                                 : launch_pdl(k_attention_row_stats<float>, dim3((unsigned)n), dim3(ST_THREADS), s, a, rows_per_tile);
+    return n <= 0 ? cudaSuccess : launch_pdl(k_attention_row_stats<T, ROWS>, dim3((unsigned)n), dim3(ST_THREADS), s, a);
 }
+cudaError_t launch_attention_row_stats_tc(const AttnArgs &a, cudaStream_t s) { return row_stats<bf16, AT_TC_ROWS>(a, s); }
 
 cudaError_t launch_attention_simt_backward(const AttnArgs &a, int dtype, cudaStream_t s)
 {
-    cudaError_t e = launch_attention_row_stats(a, dtype, SR, s);
-    if (e != cudaSuccess) return e;
     const bool b = dtype == SKIPFFN_BF16;
+    cudaError_t e = b ? row_stats<bf16, SR>(a, s) : row_stats<float, SR>(a, s);
+    if (e != cudaSuccess) return e;
     e = b ? launch(k_attention_bwd_kv_simt<bf16>, a.n_keys * a.hk, BWD_SMEM, a, s)
           : launch(k_attention_bwd_kv_simt<float>, a.n_keys * a.hk, BWD_SMEM, a, s);
     if (e != cudaSuccess) return e;

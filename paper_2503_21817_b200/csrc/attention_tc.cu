@@ -35,8 +35,8 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
         : "memory");
     return ok != 0;
 }
-// Bounded waits, inlined: a kernel that moves registers between its warps cannot call functions.  SPIN (the
-// arithmetic and MMA warps, whose waits are on the critical path) polls; the others let the hardware park the warp.
+// Bounded waits, inlined: a kernel that moves registers between its warps cannot call functions.  SPIN (the warps
+// on the critical path) polls; the others let the hardware park the warp.
 template <bool SPIN>
 __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status, int site)
 {
@@ -55,7 +55,6 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile
         }
     }
 }
-
 // The MMA warp's wait: the answer is the same in every lane and the compiler can tell (a vote), so that what
 // follows stays in uniform registers.
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status, int site)
@@ -259,14 +258,23 @@ struct alignas(8) FwdCtl {
     volatile int abort_flag;
 };
 
-// 32 scores to P (bf16 pairs); columns at or past `limit` are minus infinity
-template <bool MASKED> __device__ __forceinline__ void mask_chunk(uint32_t (&r)[32], int limit)
+// Minus infinity into the columns of a row's scores at or past `limit`, from column `from` (a uniform lower bound of
+// the warp's limits) up to `to`.  Done in tensor memory and as a loop: blocks that need it come once per item, and
+// a second, masked copy of the softmax below would have to be fetched from L2 each time (measured: thousands
+// of cycles on a busy memory system).
+__device__ __forceinline__ void mask_scores(uint32_t t_s, int from, int to, int limit)
 {
-    if (MASKED) {
+#pragma unroll 1
+    for (int c = max(from, 0) & ~15; c < to; c += 16) {
+        uint32_t r[16];
+        tmem_ld16(t_s + c, r);
+        tmem_ld_wait();
 #pragma unroll
-        for (int e = 0; e < 32; ++e)
-            if (e >= limit) r[e] = 0xff800000u;
+        for (int e = 0; e < 16; ++e)
+            if (c + e >= limit) r[e] = 0xff800000u;
+        tmem_st16(t_s + c, r);
     }
+    tmem_st_wait();
 }
 __device__ __forceinline__ float max_chunk(const uint32_t (&r)[32], float m)
 {
@@ -278,86 +286,45 @@ __device__ __forceinline__ float max_chunk(const uint32_t (&r)[32], float m)
     }
     return max3(max3(a, b, __uint_as_float(r[29])), __uint_as_float(r[30]), __uint_as_float(r[31]));
 }
-// 2^x for a pair without the special-function unit: round to the nearest integer n (Cody and Waite's range
-// reduction, by adding and subtracting 1.5 2^23), a polynomial in f = x - n on [-1/2, 1/2], n into the
-// exponent.  Coefficients: minimax of the relative error by Remez's exchange, 7.5e-8; x below -126 gives
-// 2^-126 at least, NaN stays non-finite.
-__device__ __forceinline__ void poly_exp2(uint64_t x, float &a, float &b)
-{
-    float lo, hi;
-    unpair2(x, lo, hi);
-    asm("max.NaN.f32 %0, %0, 0fC2FC0000;" : "+f"(lo));      // -126
-    asm("max.NaN.f32 %0, %0, 0fC2FC0000;" : "+f"(hi));
-    const uint64_t t = pair2(lo, hi), magic = pair2(12582912.0f, 12582912.0f), un = pair2(-12582912.0f, -12582912.0f);
-    const uint64_t n = add2(t, magic), f = fma2(add2(n, un), pair2(-1.0f, -1.0f), t);
-    uint64_t q = fma2(f, pair2(0.0013276472454890609f, 0.0013276472454890609f), pair2(0.009675540961325169f, 0.009675540961325169f));
-    q = fma2(q, f, pair2(0.05550713092088699f, 0.05550713092088699f));
-    q = fma2(q, f, pair2(0.24022120237350464f, 0.24022120237350464f));
-    q = fma2(q, f, pair2(0.6931469440460205f, 0.6931469440460205f));
-    q = fma2(q, f, pair2(1.0000001192092896f, 1.0000001192092896f));
-    float nl, nh;
-    unpair2(n, nl, nh);
-    unpair2(q, lo, hi);
-    a = __int_as_float(__float_as_int(lo) + (__float_as_int(nl) << 23));
-    b = __int_as_float(__float_as_int(hi) + (__float_as_int(nh) << 23));
-}
-
-// 32 scores of a row to P: 2^(c2 s - c2 m), summed, packed to bf16.  POLY of the 16 pairs take poly_exp2: the
-// special-function unit alone (4 lanes a cycle) would need as long as the two products of the tile.
-template <int POLY>
+// 32 scores of a row to P: 2^(c2 s - c2 m), summed, packed to bf16.  (Moving a quarter of the exponentials from
+// the special-function unit to a polynomial on the FMA pipe was 2 % slower: the tile waits for latencies, not for
+// that unit.)
 __device__ __forceinline__ void exp_chunk(const uint32_t (&r)[32], uint64_t c2, uint64_t neg_mc, uint64_t (&sum)[2], uint32_t (&pk)[16])
 {
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-        const uint64_t t = fma2(pair2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, neg_mc);
         float a, b;
-        if ((e + 1) * POLY / 16 != e * POLY / 16) {
-            poly_exp2(t, a, b);
-        } else {
-            unpair2(t, a, b);
-            a = fast_exp2(a);
-            b = fast_exp2(b);
-        }
+        unpair2(fma2(pair2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, neg_mc), a, b);
+        a = fast_exp2(a);
+        b = fast_exp2(b);
         sum[e & 1] = add2(sum[e & 1], pair2(a, b));
         // P enters the second product in bf16: relative 2^-8 per term, averaged over the row
         pk[e] = pack_bf16(a, b);
     }
 }
-#ifndef AT_POLY
-#define AT_POLY 4
-#endif
-constexpr int POLY_PAIRS = AT_POLY;
 
-// One block of scores of one row per thread: running maximum m and sum l, P over the scores.  The second half
-// of the scores is read twice (for the maximum, then again), which keeps a row's registers below what would
-// spill.  P is handed over in two halves (p_full, p_full + 8), so that the second product starts while the
-// second half is made.
-template <int DP, bool MASKED>
-__device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, int cols, int limit, float c2, bool first, float &m,
-                                              float &l, uint32_t p_full, int lane)
+// One block of scores of one row per thread: running maximum m and sum l, P over the scores.  Half of the
+// scores is read twice (for the maximum, then again), which keeps a row's registers below what would spill.  P
+// is handed over in two halves (p_full, p_full + 8), so that the second product starts while the second half
+// is made.  `upper`: the block has columns past 63.
+template <int DP>
+__device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, bool upper, float c2, bool first, float &m, float &l,
+                                              uint32_t p_full, int lane)
 {
-    constexpr int POLY = MASKED ? 0 : POLY_PAIRS;     // a masked score has to give zero
     uint32_t x[32], y[32], u[32], v[32];
-    const bool upper = !MASKED || cols > 64;
     float bm = -INFINITY;
     tmem_ld32(t_s, x);
     tmem_ld32(t_s + 32, y);
     if (upper) {
         tmem_ld32(t_s + 64, u);
         tmem_ld32(t_s + 96, v);
+        tmem_ld_wait(u);
+        tmem_ld_wait(v);
+        bm = max_chunk(v, max_chunk(u, bm));
     }
     tmem_ld_wait(x);
     tmem_ld_wait(y);
-    mask_chunk<MASKED>(x, limit);
-    mask_chunk<MASKED>(y, limit - 32);
     bm = max_chunk(y, max_chunk(x, bm));
-    if (upper) {
-        tmem_ld_wait(u);
-        tmem_ld_wait(v);
-        mask_chunk<MASKED>(u, limit - 64);
-        mask_chunk<MASKED>(v, limit - 96);
-        bm = max_chunk(v, max_chunk(u, bm));
-    }
     if (first) {
         m = bm;
     } else if (__any_sync(0xffffffffu, (bm - m) * c2 > 8.0f)) {
@@ -365,7 +332,7 @@ __device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, int co
         const float mn = fmaxf(m, bm), f = fast_exp2((m - mn) * c2);
         m = mn;
         l *= f;
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < DP; c += 16) {
             uint32_t o[16];
             tmem_ld16(t_o + c, o);
@@ -379,9 +346,9 @@ __device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, int co
     uint64_t sum[2] = {0, 0};
     uint32_t pk[16];
     if (upper) tmem_ld32(t_s + 64, u);
-    exp_chunk<POLY>(x, c2p, mcp, sum, pk);
+    exp_chunk(x, c2p, mcp, sum, pk);
     tmem_st16(t_s, pk);
-    exp_chunk<POLY>(y, c2p, mcp, sum, pk);
+    exp_chunk(y, c2p, mcp, sum, pk);
     tmem_st16(t_s + 16, pk);
     tmem_st_wait();
     tc_fence_before();
@@ -390,12 +357,10 @@ __device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, int co
     if (upper) {
         tmem_ld32(t_s + 96, v);
         tmem_ld_wait(u);
-        mask_chunk<MASKED>(u, limit - 64);
-        exp_chunk<POLY>(u, c2p, mcp, sum, pk);
+        exp_chunk(u, c2p, mcp, sum, pk);
         tmem_st16(t_s + 32, pk);
         tmem_ld_wait(v);
-        mask_chunk<MASKED>(v, limit - 96);
-        exp_chunk<POLY>(v, c2p, mcp, sum, pk);
+        exp_chunk(v, c2p, mcp, sum, pk);
         tmem_st16(t_s + 48, pk);
         tmem_st_wait();
         tc_fence_before();
@@ -471,12 +436,12 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             bool ok = true;
             auto acquire = [&]() {           // next ring slot, free to be written
                 const uint32_t s = pos % SLOTS;
-                ok = ok && wait_bar<false>(smem_u32(&ctl->kv_empty[s]), ((pos / SLOTS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                ok = ok && wait_bar<true>(smem_u32(&ctl->kv_empty[s]), ((pos / SLOTS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                 ++pos;
                 return s;
             };
             auto load_q = [&](const FwdItem &it, int g) {
-                ok = ok && wait_bar<false>(smem_u32(&ctl->q_empty[g]), (nq[g] & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                ok = ok && wait_bar<true>(smem_u32(&ctl->q_empty[g]), (nq[g] & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                 if (!ok) return;
                 const uint32_t bar = smem_u32(&ctl->q_full[g]);
                 mbar_expect_tx(bar, (uint32_t)(used * DP * 2));
@@ -613,11 +578,10 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
                 if (!ok) break;
                 tc_fence_after();
                 // columns past the row's keys (or past the ones the MMA wrote) count as minus infinity
-                const int cols = mma_cols(end - j * TILE);
-                if (cols < TILE || j * TILE + TILE > (p.causal ? t0 + 1 : it.len))
-                    softmax_block<DP, true>(t_s, t_o, cols, row_end - j * TILE, p.c2, j == 0, m, l, p_full, lane);
-                else
-                    softmax_block<DP, false>(t_s, t_o, TILE, TILE, p.c2, j == 0, m, l, p_full, lane);
+                const bool upper = end - j * TILE > 64;
+                const int from = (p.causal ? t0 + 1 : it.len) - j * TILE, to = upper ? TILE : 64;
+                if (from < to) mask_scores(t_s, from, to, row_end - j * TILE);
+                softmax_block<DP>(t_s, t_o, upper, p.c2, j == 0, m, l, p_full, lane);
             }
             if (!ok) break;
             ok = wait_bar<true>(smem_u32(&ctl->o_full[g]), no & 1, ab, p.status, SITE_EPI_TMEM_FULL);
@@ -735,7 +699,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
             bool ok = true;
             for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
                 const KvItem it(p, i, false);      // one lane
-                ok = wait_bar<false>(smem_u32(&ctl->kv_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                ok = wait_bar<true>(smem_u32(&ctl->kv_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                 if (!ok) break;
                 const uint32_t kvb = smem_u32(&ctl->kv_full);
                 mbar_expect_tx(kvb, 2 * T_BYTES);
@@ -743,7 +707,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 load_tile<DP>(v_tile, &tm.v, it.h, it.start + it.k0, kvb);
                 for (int j = 0; j < it.n; ++j, ++cnt) {
                     const uint32_t s = cnt & 1;
-                    ok = wait_bar<false>(smem_u32(&ctl->empty[s]), ((cnt >> 1) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    ok = wait_bar<true>(smem_u32(&ctl->empty[s]), ((cnt >> 1) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                     if (!ok) break;
                     const int tile = it.first + j, token = it.start + tile * p.tokens;
                     const bool dirty = it.dirty(p, tile);
@@ -839,7 +803,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 const bool mask = p.causal && t0 < it.k0 + TILE - 1;
                 const int from = mask ? (key - t0) * p.group - c0 : 0;
                 const uint32_t st = stats + (cnt & 1) * Sh::STAT_BYTES + c0 * 8;
-                ok = wait_bar<false>(smem_u32(&ctl->s_full), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = wait_bar<true>(smem_u32(&ctl->s_full), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
                 if (!ok) break;
                 tc_fence_after();
                 uint32_t r[32], pk[16];
@@ -866,7 +830,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready));
-                ok = wait_bar<false>(smem_u32(&ctl->g_scores), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = wait_bar<true>(smem_u32(&ctl->g_scores), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
                 if (!ok) break;
                 tc_fence_after();
                 if (some) {
@@ -893,7 +857,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 if (lane == 0) mbar_arrive(smem_u32(&ctl->ds_ready));
             }
             if (!ok) break;
-            ok = wait_bar<false>(smem_u32(&ctl->acc_full), items & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+            ok = wait_bar<true>(smem_u32(&ctl->acc_full), items & 1, ab, p.status, SITE_EPI_TMEM_FULL);
             if (!ok) break;
             tc_fence_after();
             // parts 0, 1: the column halves of dV; 2, 3: of dK
@@ -995,7 +959,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
             bool ok = true;
             for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
                 const QItem it(p, i, false);      // one lane
-                ok = wait_bar<false>(smem_u32(&ctl->q_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                ok = wait_bar<true>(smem_u32(&ctl->q_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                 if (!ok) break;
                 const uint32_t qb = smem_u32(&ctl->q_full);
                 mbar_expect_tx(qb, (uint32_t)(2 * used * DP * 2));
@@ -1003,12 +967,12 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 load_tile<DP>(g_tile, &tm.g, it.h * p.group, it.start + it.t0, qb);
                 for (int j = 0; j < it.nb; ++j, ++cnt) {
                     const uint32_t ks = cnt % KS, vs = cnt % VS;
-                    ok = wait_bar<false>(smem_u32(&ctl->k_empty[ks]), ((cnt / KS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    ok = wait_bar<true>(smem_u32(&ctl->k_empty[ks]), ((cnt / KS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                     if (!ok) break;
                     const uint32_t kb = smem_u32(j == it.nb - 1 && it.dirty_tail() ? &ctl->k_tail[ks] : &ctl->k_full[ks]);
                     mbar_expect_tx(kb, T_BYTES);
                     load_tile<DP>(k_ring + ks * T_BYTES, &tm.k, it.h, it.start + j * TILE, kb);
-                    ok = wait_bar<false>(smem_u32(&ctl->v_empty[vs]), ((cnt / VS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    ok = wait_bar<true>(smem_u32(&ctl->v_empty[vs]), ((cnt / VS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                     if (!ok) break;
                     const uint32_t vb = smem_u32(&ctl->v_full[vs]);
                     mbar_expect_tx(vb, T_BYTES);
@@ -1093,8 +1057,8 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 const int cols = mma_cols(it.end - j * TILE);
                 const bool mask = cols < TILE || j * TILE + TILE > (p.causal ? it.t0 + 1 : it.len);
                 const int limit = row_end - j * TILE - c0;
-                ok = wait_bar<false>(smem_u32(&ctl->s_full[cnt & 1]), (cnt >> 1) & 1, ab, p.status, SITE_EPI_TMEM_FULL);
-                ok = ok && wait_bar<false>(smem_u32(&ctl->g_scores), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = wait_bar<true>(smem_u32(&ctl->s_full[cnt & 1]), (cnt >> 1) & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = ok && wait_bar<true>(smem_u32(&ctl->g_scores), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
                 if (!ok) break;
                 tc_fence_after();
                 if (c0 < cols) {
@@ -1122,7 +1086,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 if (lane == 0) mbar_arrive(smem_u32(&ctl->ds_ready));
             }
             if (!ok) break;
-            ok = wait_bar<false>(smem_u32(&ctl->acc_full), items & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+            ok = wait_bar<true>(smem_u32(&ctl->acc_full), items & 1, ab, p.status, SITE_EPI_TMEM_FULL);
             if (!ok) break;
             tc_fence_after();
             const bool live = row < used && token < it.len;
@@ -1212,7 +1176,7 @@ template <int DP> static cudaError_t backward_dp(const AttnArgs &a, cudaStream_t
     if (!head_map(&tm.q, a.q, a.d, a.hq, a.N, a.ldq, a.group, a.tokens) || !head_map(&tm.k, a.k, a.d, a.hk, a.N, a.ldk, 1, TILE) ||
         !head_map(&tm.v, a.v, a.d, a.hk, a.N, a.ldv, 1, TILE) || !head_map(&tm.g, a.dout, a.d, a.hq, a.N, a.lddo, a.group, a.tokens))
         return cudaErrorInvalidValue;
-    cudaError_t e = launch_attention_row_stats(a, SKIPFFN_BF16, TILE, s);
+    cudaError_t e = launch_attention_row_stats_tc(a, s);
     if (e != cudaSuccess) return e;
     AtParams p = params_of(a, a.key_items, a.n_keys);
     p.out0 = (bf16 *)a.dk; p.ld0 = a.lddk; p.out1 = (bf16 *)a.dv; p.ld1 = a.lddv;

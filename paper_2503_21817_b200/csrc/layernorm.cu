@@ -70,58 +70,67 @@ __device__ __forceinline__ float group_add(float v, float *red, int id, int thre
     return s;
 }
 
-// One row per group of blockDim.x threads, blockDim.y groups per CTA.
-template <typename T>
-__global__ void __launch_bounds__(1024)
-k_layernorm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__restrict__ beta, int64_t rows, int C,
-                float eps, T *__restrict__ y, float *__restrict__ mean_out, float *__restrict__ rstd_out)
+// A row per group of blockDim.x threads, blockDim.y groups per CTA; a group walks rows with the grid's stride, and
+// the next row is on its way while the current one is worked on.
+template <typename T, int BOUND, int CTAS>
+__global__ void __launch_bounds__(BOUND, CTAS)
+k_layernorm_fwd(const T *x, const T *__restrict__ gamma, const T *__restrict__ beta, int64_t rows, int C, float eps, T *y,
+                float *__restrict__ mean_out, float *__restrict__ rstd_out)
 {
     constexpr int N = Vec<T>::N;
-    __shared__ float red[2][32];
-    pdl_enter();
+    __shared__ float red[2][2][32];
     const int tx = threadIdx.x, threads = blockDim.x, id = threadIdx.y, vecs = C / N;
-    const int64_t row = (int64_t)blockIdx.x * blockDim.y + id;
-    if (row >= rows) return;
-    const uint4 *src = reinterpret_cast<const uint4 *>(x + row * C);
-    float v[LN_NV][N];
-    float s = 0.0f;
+    const int64_t step = (int64_t)gridDim.x * blockDim.y;
+    int64_t row = (int64_t)blockIdx.x * blockDim.y + id;
+    pdl_enter();
+    uint4 xq[LN_NV];
+    auto fetch = [&](int64_t r) {
+        const uint4 *src = reinterpret_cast<const uint4 *>(x + r * C);
 #pragma unroll
-    for (int k = 0; k < LN_NV; ++k) {
-        const int i = tx + k * threads;
-        const uint4 q = i < vecs ? src[i] : make_uint4(0, 0, 0, 0);
-        unpack(q, v[k]);
-    }
+        for (int k = 0; k < LN_NV; ++k) {
+            const int i = tx + k * threads;
+            if (i < vecs) xq[k] = src[i];
+        }
+    };
 #pragma unroll
-    for (int k = 0; k < LN_NV; ++k)
+    for (int k = 0; k < LN_NV; ++k) xq[k] = make_uint4(0, 0, 0, 0);
+    if (row < rows) fetch(row);
+    for (int turn = 0; row < rows; row += step, turn ^= 1) {
+        float v[LN_NV][N];
+        float s = 0.0f, ss = 0.0f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) s += v[k][e];
-    float *r0 = red[0] + id * (threads / 32), *r1 = red[1] + id * (threads / 32);
-    const float mean = group_add(s, r0, id, threads) / (float)C;
-    float ss = 0.0f;
+        for (int k = 0; k < LN_NV; ++k) {
+            unpack(xq[k], v[k]);
 #pragma unroll
-    for (int k = 0; k < LN_NV; ++k)
-        if (tx + k * threads < vecs)
+            for (int e = 0; e < N; ++e) s += v[k][e];
+        }
+        if (row + step < rows) fetch(row + step);
+        const float mean = group_add(s, red[turn][0] + id * (threads / 32), id, threads) / (float)C;
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                v[k][e] -= mean;
-                ss = fmaf(v[k][e], v[k][e], ss);
-            }
-    const float rstd = 1.0f / sqrtf(group_add(ss, r1, id, threads) / (float)C + eps);
-    uint4 *dst = reinterpret_cast<uint4 *>(y + row * C);
+        for (int k = 0; k < LN_NV; ++k)
+            if (tx + k * threads < vecs)
 #pragma unroll
-    for (int k = 0; k < LN_NV; ++k) {
-        const int i = tx + k * threads;
-        if (i >= vecs) break;
-        float g[N], b[N], o[N];
-        unpack(__ldg(reinterpret_cast<const uint4 *>(gamma) + i), g);
-        unpack(beta ? __ldg(reinterpret_cast<const uint4 *>(beta) + i) : make_uint4(0, 0, 0, 0), b);
+                for (int e = 0; e < N; ++e) {
+                    v[k][e] -= mean;
+                    ss = fmaf(v[k][e], v[k][e], ss);
+                }
+        const float rstd = 1.0f / sqrtf(group_add(ss, red[turn][1] + id * (threads / 32), id, threads) / (float)C + eps);
+        uint4 *dst = reinterpret_cast<uint4 *>(y + row * C);
 #pragma unroll
-        for (int e = 0; e < N; ++e) o[e] = fmaf(v[k][e] * rstd, g[e], b[e]);
-        dst[i] = pack(o);
-    }
-    if (tx == 0) {
-        if (mean_out) mean_out[row] = mean;
-        if (rstd_out) rstd_out[row] = rstd;
+        for (int k = 0; k < LN_NV; ++k) {
+            const int i = tx + k * threads;
+            if (i >= vecs) break;
+            float g[N], b[N], o[N];
+            unpack(__ldg(reinterpret_cast<const uint4 *>(gamma) + i), g);
+            unpack(beta ? __ldg(reinterpret_cast<const uint4 *>(beta) + i) : make_uint4(0, 0, 0, 0), b);
+#pragma unroll
+            for (int e = 0; e < N; ++e) o[e] = fmaf(v[k][e] * rstd, g[e], b[e]);
+            dst[i] = pack(o);
+        }
+        if (tx == 0) {
+            if (mean_out) mean_out[row] = mean;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
     }
 }
 
@@ -344,13 +353,28 @@ cudaError_t launch_smem(KernelT kern, dim3 grid, dim3 block, size_t smem, cudaSt
     return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
+// Rows of up to 8 KiB (bf16: 4096 columns) take groups of at most 128 threads, eight such CTAs to an SM; longer
+// ones CTAs of up to 512 or 1024 threads, two or one.
+template <typename T, int BOUND, int CTAS>
+cudaError_t fwd_b(const T *x, const T *gamma, const T *beta, int64_t rows, int C, float eps, T *y, float *mean, float *rstd, int t,
+                  cudaStream_t s)
+{
+    int sms = 0;
+    const cudaError_t e = device_sms(sms);
+    if (e != cudaSuccess) return e;
+    const int groups = BOUND / t;
+    const int64_t need = (rows + groups - 1) / groups, most = (int64_t)sms * CTAS;
+    return launch_pdl(k_layernorm_fwd<T, BOUND, CTAS>, dim3((unsigned)(need < most ? need : most)), dim3(t, groups), s, x, gamma, beta,
+                      rows, C, eps, y, mean, rstd);
+}
 template <typename T>
 cudaError_t fwd_t(const T *x, const T *gamma, const T *beta, int64_t rows, int C, float eps, T *y, float *mean, float *rstd,
                   cudaStream_t s)
 {
-    const int t = group_threads<T>(C), groups = t >= 128 ? 1 : 128 / t;
-    return launch_pdl(k_layernorm_fwd<T>, dim3((unsigned)((rows + groups - 1) / groups)), dim3(t, groups), s, x, gamma, beta, rows, C,
-                      eps, y, mean, rstd);
+    const int t = group_threads<T>(C);
+    if (t <= 128) return fwd_b<T, 128, 6>(x, gamma, beta, rows, C, eps, y, mean, rstd, t, s);
+    if (t <= 512) return fwd_b<T, 512, 1>(x, gamma, beta, rows, C, eps, y, mean, rstd, t, s);
+    return fwd_b<T, 1024, 1>(x, gamma, beta, rows, C, eps, y, mean, rstd, t, s);
 }
 
 template <typename T, int BOUND>
