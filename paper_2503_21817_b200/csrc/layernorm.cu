@@ -70,62 +70,101 @@ __device__ __forceinline__ float group_add(float v, float *red, int id, int thre
     return s;
 }
 
-// A row per group of blockDim.x threads, blockDim.y groups per CTA; a group walks rows with the grid's stride, and
-// the next row is on its way while the current one is worked on.
-template <typename T, int BOUND, int CTAS>
-__global__ void __launch_bounds__(BOUND, CTAS)
+// 16 bytes of a row as fp32 pairs, and back
+template <int N> __device__ __forceinline__ void unpack2(const uint4 &q, uint64_t (&v)[N / 2])
+{
+    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+    if constexpr (N == 8) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = pair2(__uint_as_float(u[k] << 16), __uint_as_float(u[k] & 0xffff0000u));
+    } else {
+        v[0] = pair2(__uint_as_float(u[0]), __uint_as_float(u[1]));
+        v[1] = pair2(__uint_as_float(u[2]), __uint_as_float(u[3]));
+    }
+}
+template <int N> __device__ __forceinline__ uint4 pack2(const uint64_t (&v)[N / 2])
+{
+    float f[N];
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) unpair2(v[k], f[2 * k], f[2 * k + 1]);
+    return pack(f);
+}
+// Forward.  ONE_WARP: a row per warp, blockDim.y of them; else a row per CTA.  The CTA walks rows with the grid's
+// stride; the next row is on its way while the current one is worked on.  gamma and beta sit in shared memory in
+// their own type (as fp32 their reads alone, two-way conflicts included, took 17 of 39 us at 9376 x 4096),
+// arithmetic is on pairs (18 instructions per element before), and a CTA has one barrier (a named one per group
+// held an SM to four CTAs).  FULL: every thread owns LN_NV vectors.
+constexpr int LN_FWD_REGS = 80, LN_FWD_REGS_FP32 = 64;       // fp32: CTAs of up to 1024 threads
+template <typename T, bool ONE_WARP, bool FULL>
+__global__ void __maxnreg__(sizeof(T) == 2 ? LN_FWD_REGS : LN_FWD_REGS_FP32)
 k_layernorm_fwd(const T *x, const T *__restrict__ gamma, const T *__restrict__ beta, int64_t rows, int C, float eps, T *y,
                 float *__restrict__ mean_out, float *__restrict__ rstd_out)
 {
-    constexpr int N = Vec<T>::N;
+    constexpr int N = Vec<T>::N, P = N / 2;
     __shared__ float red[2][2][32];
-    const int tx = threadIdx.x, threads = blockDim.x, id = threadIdx.y, vecs = C / N;
-    const int64_t step = (int64_t)gridDim.x * blockDim.y;
-    int64_t row = (int64_t)blockIdx.x * blockDim.y + id;
+    extern __shared__ uint4 affine[];                      // gamma [C], beta [C]
+    const int tx = threadIdx.x, threads = ONE_WARP ? 32 : blockDim.x, vecs = C / N;
+    const int64_t step = (int64_t)gridDim.x * (ONE_WARP ? blockDim.y : 1);
+    int64_t row = (int64_t)blockIdx.x * (ONE_WARP ? blockDim.y : 1) + threadIdx.y;
+    auto owns = [&](int k) { return FULL || tx + k * threads < vecs; };
+    auto row_sum = [&](uint64_t v, float *r) {
+        float a, b;
+        unpair2(v, a, b);
+        a = warp_add(a + b);
+        if (ONE_WARP) return a;
+        if ((tx & 31) == 0) r[tx >> 5] = a;
+        __syncthreads();
+        a = 0.0f;
+        for (int k = 0; k < threads / 32; ++k) a += r[k];
+        return a;
+    };
     pdl_enter();
     uint4 xq[LN_NV];
     auto fetch = [&](int64_t r) {
-        const uint4 *src = reinterpret_cast<const uint4 *>(x + r * C);
+        const uint4 *src = reinterpret_cast<const uint4 *>(x + r * C) + tx;
 #pragma unroll
-        for (int k = 0; k < LN_NV; ++k) {
-            const int i = tx + k * threads;
-            if (i < vecs) xq[k] = src[i];
-        }
+        for (int k = 0; k < LN_NV; ++k)
+            if (owns(k)) xq[k] = src[k * threads];
     };
 #pragma unroll
     for (int k = 0; k < LN_NV; ++k) xq[k] = make_uint4(0, 0, 0, 0);
     if (row < rows) fetch(row);
+    for (int i = threadIdx.y * blockDim.x + tx; i < vecs; i += blockDim.x * blockDim.y) {
+        affine[i] = reinterpret_cast<const uint4 *>(gamma)[i];
+        affine[vecs + i] = beta ? reinterpret_cast<const uint4 *>(beta)[i] : make_uint4(0, 0, 0, 0);
+    }
+    __syncthreads();
     for (int turn = 0; row < rows; row += step, turn ^= 1) {
-        float v[LN_NV][N];
-        float s = 0.0f, ss = 0.0f;
+        uint64_t v[LN_NV][P], s = 0, ss = 0;
 #pragma unroll
         for (int k = 0; k < LN_NV; ++k) {
-            unpack(xq[k], v[k]);
+            unpack2<N>(xq[k], v[k]);
 #pragma unroll
-            for (int e = 0; e < N; ++e) s += v[k][e];
+            for (int e = 0; e < P; ++e) s = add2(s, v[k][e]);
         }
         if (row + step < rows) fetch(row + step);
-        const float mean = group_add(s, red[turn][0] + id * (threads / 32), id, threads) / (float)C;
+        const float mean = row_sum(s, red[turn][0]) / (float)C;
+        const uint64_t neg = pair2(-mean, -mean);
 #pragma unroll
         for (int k = 0; k < LN_NV; ++k)
-            if (tx + k * threads < vecs)
+            if (owns(k))
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    v[k][e] -= mean;
-                    ss = fmaf(v[k][e], v[k][e], ss);
+                for (int e = 0; e < P; ++e) {
+                    v[k][e] = add2(v[k][e], neg);
+                    ss = fma2(v[k][e], v[k][e], ss);
                 }
-        const float rstd = 1.0f / sqrtf(group_add(ss, red[turn][1] + id * (threads / 32), id, threads) / (float)C + eps);
-        uint4 *dst = reinterpret_cast<uint4 *>(y + row * C);
+        const float rstd = 1.0f / sqrtf(row_sum(ss, red[turn][1]) / (float)C + eps);
+        const uint64_t r2 = pair2(rstd, rstd);
+        uint4 *dst = reinterpret_cast<uint4 *>(y + row * C) + tx;
 #pragma unroll
         for (int k = 0; k < LN_NV; ++k) {
-            const int i = tx + k * threads;
-            if (i >= vecs) break;
-            float g[N], b[N], o[N];
-            unpack(__ldg(reinterpret_cast<const uint4 *>(gamma) + i), g);
-            unpack(beta ? __ldg(reinterpret_cast<const uint4 *>(beta) + i) : make_uint4(0, 0, 0, 0), b);
+            if (!owns(k)) break;
+            uint64_t g[P], b[P];
+            unpack2<N>(affine[tx + k * threads], g);
+            unpack2<N>(affine[vecs + tx + k * threads], b);
 #pragma unroll
-            for (int e = 0; e < N; ++e) o[e] = fmaf(v[k][e] * rstd, g[e], b[e]);
-            dst[i] = pack(o);
+            for (int e = 0; e < P; ++e) v[k][e] = fma2(mul2(v[k][e], r2), g[e], b[e]);
+            dst[k * threads] = pack2<N>(v[k]);
         }
         if (tx == 0) {
             if (mean_out) mean_out[row] = mean;
@@ -134,82 +173,94 @@ k_layernorm_fwd(const T *x, const T *__restrict__ gamma, const T *__restrict__ b
     }
 }
 
-// Backward: group g of CTA b walks rows b groups + g, + grid x groups, ...; dx row by row, dgamma and dbeta of
-// the group's rows in registers.  At the end the groups add up in order through shared memory and the
-// CTA leaves one partial row of each in part[b][2][C].
-template <typename T, int BOUND>
-__global__ void __launch_bounds__(BOUND, 1)
+// Backward: group g of CTA b walks rows b groups + g, + grid x groups, ...; dx row by row, dgamma and dbeta of the
+// group's rows in registers (16 columns per thread).  At the end the groups add up in order through shared
+// memory and the CTA leaves one partial row of each in part[b][2][C].
+constexpr int LN_BWD_THREADS = 640, LN_BWD_COLS = 16;
+template <typename T>
+__global__ void __launch_bounds__(LN_BWD_THREADS, 1)
 k_layernorm_bwd(const T *dy, const T *x, const T *__restrict__ gamma, const float *__restrict__ mean_in,
                 const float *__restrict__ rstd_in, int64_t rows, int C, T *dx, float *__restrict__ part)
 {
-    constexpr int N = Vec<T>::N;
-    __shared__ float red[2][2][32];
-    extern __shared__ float sums[];            // [2][C] when the CTA has several groups
-    pdl_enter();
+    constexpr int N = Vec<T>::N, P = N / 2, NV = LN_BWD_COLS / N;
+    __shared__ float red[2][2][LN_BWD_THREADS / 32];
+    extern __shared__ uint4 gam[];                     // gamma [C]; with several groups also their sums [2][C]
+    float *sums = reinterpret_cast<float *>(gam + C / N);
     const int tx = threadIdx.x, threads = blockDim.x, id = threadIdx.y, groups = blockDim.y, vecs = C / N;
     const int64_t step = (int64_t)gridDim.x * groups;
-    float dg[LN_NV][N], db[LN_NV][N];
-    uint4 gq[LN_NV], xq[LN_NV], yq[LN_NV];
+    uint64_t dg[NV][P], db[NV][P];
+    uint4 xq[NV], yq[NV];
+    float mean_next = 0.0f, rstd_next = 0.0f;
 #pragma unroll
-    for (int k = 0; k < LN_NV; ++k) {
-        const int i = tx + k * threads;
-        gq[k] = i < vecs ? __ldg(reinterpret_cast<const uint4 *>(gamma) + i) : make_uint4(0, 0, 0, 0);
+    for (int k = 0; k < NV; ++k) {
         xq[k] = yq[k] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int e = 0; e < N; ++e) dg[k][e] = db[k][e] = 0.0f;
+        for (int e = 0; e < P; ++e) dg[k][e] = db[k][e] = 0;
     }
     auto fetch = [&](int64_t row) {
-        const uint4 *xs = reinterpret_cast<const uint4 *>(x + row * C), *ys = reinterpret_cast<const uint4 *>(dy + row * C);
+        const uint4 *xs = reinterpret_cast<const uint4 *>(x + row * C) + tx, *ys = reinterpret_cast<const uint4 *>(dy + row * C) + tx;
 #pragma unroll
-        for (int k = 0; k < LN_NV; ++k) {
-            const int i = tx + k * threads;
-            if (i < vecs) { xq[k] = xs[i]; yq[k] = ys[i]; }
-        }
+        for (int k = 0; k < NV; ++k)
+            if (tx + k * threads < vecs) { xq[k] = xs[k * threads]; yq[k] = ys[k * threads]; }
+        mean_next = mean_in[row];
+        rstd_next = rstd_in[row];
     };
+    pdl_enter();
     int64_t row = (int64_t)blockIdx.x * groups + id;
     if (row < rows) fetch(row);
+    for (int i = id * threads + tx; i < vecs; i += threads * groups) gam[i] = reinterpret_cast<const uint4 *>(gamma)[i];
+    __syncthreads();
     for (int turn = 0; row < rows; row += step, turn ^= 1) {
-        const float mean = mean_in[row], rstd = rstd_in[row];
-        uint4 xc[LN_NV], yc[LN_NV];
+        const float rstd = rstd_next;
+        const uint64_t neg_mean = pair2(-mean_next, -mean_next), r2 = pair2(rstd, rstd);
+        uint4 xc[NV], yc[NV];
 #pragma unroll
-        for (int k = 0; k < LN_NV; ++k) { xc[k] = xq[k]; yc[k] = yq[k]; }
+        for (int k = 0; k < NV; ++k) { xc[k] = xq[k]; yc[k] = yq[k]; }
         if (row + step < rows) fetch(row + step);          // in flight while this row is worked on
-        float s0 = 0.0f, s1 = 0.0f;
+        uint64_t p0 = 0, p1 = 0;
 #pragma unroll
-        for (int k = 0; k < LN_NV; ++k) {
+        for (int k = 0; k < NV; ++k) {
             if (tx + k * threads >= vecs) break;
-            float xv[N], yv[N], g[N];
-            unpack(xc[k], xv); unpack(yc[k], yv); unpack(gq[k], g);
+            uint64_t xv[P], yv[P], g[P];
+            unpack2<N>(xc[k], xv); unpack2<N>(yc[k], yv);
+            unpack2<N>(gam[tx + k * threads], g);
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float xh = (xv[e] - mean) * rstd, t = yv[e] * g[e];
-                s0 += t;
-                s1 = fmaf(t, xh, s1);
-                dg[k][e] = fmaf(yv[e], xh, dg[k][e]);
-                db[k][e] += yv[e];
+            for (int e = 0; e < P; ++e) {
+                const uint64_t xh = mul2(add2(xv[e], neg_mean), r2), t = mul2(yv[e], g[e]);
+                p0 = add2(p0, t);
+                p1 = fma2(t, xh, p1);
+                dg[k][e] = fma2(yv[e], xh, dg[k][e]);
+                db[k][e] = add2(db[k][e], yv[e]);
             }
         }
-        float *r = red[turn][0] + id * (threads / 32), *r2 = red[turn][1] + id * (threads / 32);
-        s0 = warp_add(s0);
-        s1 = warp_add(s1);
+        float s0, s1, hi;
+        unpair2(p0, s0, hi);
+        s0 = warp_add(s0 + hi);
+        unpair2(p1, s1, hi);
+        s1 = warp_add(s1 + hi);
         if (threads > 32) {
-            if ((tx & 31) == 0) { r[tx >> 5] = s0; r2[tx >> 5] = s1; }
+            float *r = red[turn][0] + id * (threads / 32), *q = red[turn][1] + id * (threads / 32);
+            if ((tx & 31) == 0) { r[tx >> 5] = s0; q[tx >> 5] = s1; }
             group_sync(id, threads);
             s0 = s1 = 0.0f;
-            for (int k = 0; k < threads / 32; ++k) { s0 += r[k]; s1 += r2[k]; }
+            for (int k = 0; k < threads / 32; ++k) { s0 += r[k]; s1 += q[k]; }
         }
-        s0 /= (float)C;
-        s1 /= (float)C;
-        uint4 *dst = reinterpret_cast<uint4 *>(dx + row * C);
+        s0 /= -(float)C;
+        s1 /= -(float)C;
+        const uint64_t m0 = pair2(s0, s0), m1 = pair2(s1, s1);
+        uint4 *dst = reinterpret_cast<uint4 *>(dx + row * C) + tx;
 #pragma unroll
-        for (int k = 0; k < LN_NV; ++k) {
-            const int i = tx + k * threads;
-            if (i >= vecs) break;
-            float xv[N], yv[N], g[N], o[N];
-            unpack(xc[k], xv); unpack(yc[k], yv); unpack(gq[k], g);
+        for (int k = 0; k < NV; ++k) {
+            if (tx + k * threads >= vecs) break;
+            uint64_t xv[P], yv[P], g[P];
+            unpack2<N>(xc[k], xv); unpack2<N>(yc[k], yv);
+            unpack2<N>(gam[tx + k * threads], g);
 #pragma unroll
-            for (int e = 0; e < N; ++e) o[e] = rstd * (fmaf(yv[e], g[e], -s0) - (xv[e] - mean) * rstd * s1);
-            dst[i] = pack(o);
+            for (int e = 0; e < P; ++e) {
+                const uint64_t xh = mul2(add2(xv[e], neg_mean), r2);
+                xv[e] = mul2(r2, fma2(xh, m1, fma2(yv[e], g[e], m0)));
+            }
+            dst[k * threads] = pack2<N>(xv);
         }
     }
     if (part == nullptr) return;
@@ -219,14 +270,21 @@ k_layernorm_bwd(const T *dy, const T *x, const T *__restrict__ gamma, const floa
         if (g != id) continue;
         float *acc = g == groups - 1 ? out : sums;
 #pragma unroll
-        for (int k = 0; k < LN_NV; ++k) {
+        for (int k = 0; k < NV; ++k) {
             const int i = tx + k * threads;
             if (i >= vecs) break;
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const int c = i * N + e;
-                acc[c] = dg[k][e] + (g ? sums[c] : 0.0f);
-                acc[C + c] = db[k][e] + (g ? sums[C + c] : 0.0f);
+            for (int e = 0; e < P; ++e) {
+                const int c = i * N + 2 * e;
+                float2 a, b;
+                unpair2(dg[k][e], a.x, a.y);
+                unpair2(db[k][e], b.x, b.y);
+                if (g) {
+                    const float2 pa = *reinterpret_cast<const float2 *>(sums + c), pb = *reinterpret_cast<const float2 *>(sums + C + c);
+                    a.x += pa.x; a.y += pa.y; b.x += pb.x; b.y += pb.y;
+                }
+                *reinterpret_cast<float2 *>(acc + c) = a;
+                *reinterpret_cast<float2 *>(acc + C + c) = b;
             }
         }
     }
@@ -353,31 +411,40 @@ cudaError_t launch_smem(KernelT kern, dim3 grid, dim3 block, size_t smem, cudaSt
     return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
-// Rows of up to 8 KiB (bf16: 4096 columns) take groups of at most 128 threads, eight such CTAs to an SM; longer
-// ones CTAs of up to 512 or 1024 threads, two or one.
-template <typename T, int BOUND, int CTAS>
-cudaError_t fwd_b(const T *x, const T *gamma, const T *beta, int64_t rows, int C, float eps, T *y, float *mean, float *rstd, int t,
+// Resident CTAs of a forward launch: as many as registers and gamma and beta in shared memory allow.
+template <typename T, bool ONE_WARP, bool FULL>
+cudaError_t fwd_k(const T *x, const T *gamma, const T *beta, int64_t rows, int C, float eps, T *y, float *mean, float *rstd, int t,
                   cudaStream_t s)
 {
+    constexpr int WARP_ROWS = 8;
     int sms = 0;
-    const cudaError_t e = device_sms(sms);
+    cudaError_t e = device_sms(sms);
     if (e != cudaSuccess) return e;
-    const int groups = BOUND / t;
-    const int64_t need = (rows + groups - 1) / groups, most = (int64_t)sms * CTAS;
-    return launch_pdl(k_layernorm_fwd<T, BOUND, CTAS>, dim3((unsigned)(need < most ? need : most)), dim3(t, groups), s, x, gamma, beta,
-                      rows, C, eps, y, mean, rstd);
+    const int groups = ONE_WARP ? WARP_ROWS : 1, threads = t * groups;
+    const size_t smem = (size_t)2 * C * sizeof(T);
+    if (smem > 32 * 1024) {
+        e = cudaFuncSetAttribute(k_layernorm_fwd<T, ONE_WARP, FULL>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * LN_MAX_C * 4);
+        if (e != cudaSuccess) return e;
+    }
+    const int by_regs = 65536 / (threads * (sizeof(T) == 2 ? LN_FWD_REGS : LN_FWD_REGS_FP32)), by_smem = (int)(200 * 1024 / (smem + 2048));
+    const int ctas = by_regs < by_smem ? (by_regs > 0 ? by_regs : 1) : (by_smem > 0 ? by_smem : 1);
+    const int64_t need = (rows + groups - 1) / groups, most = (int64_t)sms * ctas;
+    return launch_smem(k_layernorm_fwd<T, ONE_WARP, FULL>, dim3((unsigned)(need < most ? need : most)), dim3(t, groups), smem, s, x, gamma,
+                       beta, rows, C, eps, y, mean, rstd);
 }
 template <typename T>
 cudaError_t fwd_t(const T *x, const T *gamma, const T *beta, int64_t rows, int C, float eps, T *y, float *mean, float *rstd,
                   cudaStream_t s)
 {
     const int t = group_threads<T>(C);
-    if (t <= 128) return fwd_b<T, 128, 6>(x, gamma, beta, rows, C, eps, y, mean, rstd, t, s);
-    if (t <= 512) return fwd_b<T, 512, 1>(x, gamma, beta, rows, C, eps, y, mean, rstd, t, s);
-    return fwd_b<T, 1024, 1>(x, gamma, beta, rows, C, eps, y, mean, rstd, t, s);
+    const bool full = C == t * LN_NV * Vec<T>::N;
+    if (t == 32) return full ? fwd_k<T, true, true>(x, gamma, beta, rows, C, eps, y, mean, rstd, t, s)
+                             : fwd_k<T, true, false>(x, gamma, beta, rows, C, eps, y, mean, rstd, t, s);
+    return full ? fwd_k<T, false, true>(x, gamma, beta, rows, C, eps, y, mean, rstd, t, s)
+                : fwd_k<T, false, false>(x, gamma, beta, rows, C, eps, y, mean, rstd, t, s);
 }
 
-template <typename T, int BOUND>
+template <typename T>
 cudaError_t bwd_t(const T *dy, const T *x, const T *gamma, const float *mean, const float *rstd, int64_t rows, int C, T *dx,
                   void *dgamma, void *dbeta, int dw_fp32, float *part, cudaStream_t s)
 {
@@ -385,18 +452,18 @@ cudaError_t bwd_t(const T *dy, const T *x, const T *gamma, const float *mean, co
     cudaError_t e = device_sms(sms);
     if (e != cudaSuccess) return e;
     const bool sums = dgamma != nullptr || dbeta != nullptr;
-    const int t = group_threads<T>(C);
+    const int t = (C + 32 * LN_BWD_COLS - 1) / (32 * LN_BWD_COLS) * 32;
     int parts;
-    if (t <= BOUND) {
-        const int groups = BOUND / t;
+    if (t <= LN_BWD_THREADS) {
+        const int groups = LN_BWD_THREADS / t;
         const int64_t need = (rows + groups - 1) / groups;
         parts = (int)(need < sms ? (need > 0 ? need : 1) : sms);
-        const size_t smem = groups > 1 ? (size_t)2 * C * sizeof(float) : 0;     // at most 48 KiB
+        const size_t smem = C * (sizeof(T) + (groups > 1 ? 2 * sizeof(float) : 0));   // several groups: C <= 5120
         if (smem > 32 * 1024) {                 // with the static arrays more than a launch gets unasked
-            e = cudaFuncSetAttribute(k_layernorm_bwd<T, BOUND>, cudaFuncAttributeMaxDynamicSharedMemorySize, 48 * 1024);
+            e = cudaFuncSetAttribute(k_layernorm_bwd<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024);
             if (e != cudaSuccess) return e;
         }
-        e = launch_smem(k_layernorm_bwd<T, BOUND>, dim3(parts), dim3(t, groups), smem, s, dy, x, gamma, mean, rstd, rows, C, dx,
+        e = launch_smem(k_layernorm_bwd<T>, dim3(parts), dim3(t, groups), smem, s, dy, x, gamma, mean, rstd, rows, C, dx,
                         sums ? part : nullptr);
         if (e != cudaSuccess) return e;
     } else {
@@ -432,8 +499,8 @@ cudaError_t launch_layernorm_backward(const void *dy, const void *x, const void 
                                       cudaStream_t s)
 {
     return dtype == SKIPFFN_BF16
-               ? bwd_t<bf16, 384>((const bf16 *)dy, (const bf16 *)x, (const bf16 *)gamma, mean, rstd, rows, C, (bf16 *)dx, dgamma, dbeta, dw_fp32, part, s)
-               : bwd_t<float, 512>((const float *)dy, (const float *)x, (const float *)gamma, mean, rstd, rows, C, (float *)dx, dgamma, dbeta, 1, part, s);
+               ? bwd_t<bf16>((const bf16 *)dy, (const bf16 *)x, (const bf16 *)gamma, mean, rstd, rows, C, (bf16 *)dx, dgamma, dbeta, dw_fp32, part, s)
+               : bwd_t<float>((const float *)dy, (const float *)x, (const float *)gamma, mean, rstd, rows, C, (float *)dx, dgamma, dbeta, 1, part, s);
 }
 
 }  // namespace skipffn
