@@ -173,96 +173,145 @@ k_layernorm_fwd(const T *x, const T *__restrict__ gamma, const T *__restrict__ b
     }
 }
 
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Sums of a and b over a warp with six shuffles instead of ten: the lanes' halves take one sum each.  Lanes 0..15
+// get the sum of a, lanes 16..31 that of b.
+__device__ __forceinline__ float warp_add_two(float a, float b)
+{
+    const bool high = (threadIdx.x & 16) != 0;
+    float v = high ? b : a;
+    v += __shfl_xor_sync(0xffffffffu, high ? a : b, 16);
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+
 // Backward: group g of CTA b walks rows b groups + g, + grid x groups, ...; dx row by row, dgamma and dbeta of the
-// group's rows in registers (16 columns per thread).  At the end the groups add up in order through shared
-// memory and the CTA leaves one partial row of each in part[b][2][C].
+// group's rows in registers (16 columns per thread).  A thread copies its own columns of the next rows to its own
+// words of shared memory asynchronously, so nothing but the two row sums needs a barrier and no registers wait for
+// loads.  At the end the groups add up in order through shared memory and the CTA leaves one partial row of each
+// in part[b][2][C].
 constexpr int LN_BWD_THREADS = 640, LN_BWD_COLS = 16;
-template <typename T>
+template <typename T> struct LnBwd {
+    static constexpr int N = Vec<T>::N, P = N / 2, NV = LN_BWD_COLS / N;
+    static constexpr int STAGES = sizeof(T) == 2 ? 3 : 2;                    // rows on their way, the current one included
+    static size_t smem(int C, int threads, int groups)
+    {
+        return (size_t)threads * groups * STAGES * 2 * NV * 16 + C * (sizeof(T) + (groups > 1 ? 2 * sizeof(float) : 0));
+    }
+};
+template <typename T, bool FULL>
 __global__ void __launch_bounds__(LN_BWD_THREADS, 1)
 k_layernorm_bwd(const T *dy, const T *x, const T *__restrict__ gamma, const float *__restrict__ mean_in,
                 const float *__restrict__ rstd_in, int64_t rows, int C, T *dx, float *__restrict__ part)
 {
-    constexpr int N = Vec<T>::N, P = N / 2, NV = LN_BWD_COLS / N;
-    __shared__ float red[2][2][LN_BWD_THREADS / 32];
-    extern __shared__ uint4 gam[];                     // gamma [C]; with several groups also their sums [2][C]
-    float *sums = reinterpret_cast<float *>(gam + C / N);
-    const int tx = threadIdx.x, threads = blockDim.x, id = threadIdx.y, groups = blockDim.y, vecs = C / N;
+    using L = LnBwd<T>;
+    constexpr int N = L::N, P = L::P, NV = L::NV, STAGES = L::STAGES;
+    __shared__ float2 red[2][LN_BWD_THREADS / 32];
+    extern __shared__ uint4 dyn[];
+    const int tx = threadIdx.x, threads = blockDim.x, id = threadIdx.y, groups = blockDim.y, vecs = C / N, all = threads * groups;
     const int64_t step = (int64_t)gridDim.x * groups;
+    uint4 *ring = dyn + id * threads + tx;             // [stage][x, dy][k][thread]
+    uint4 *gam = dyn + (size_t)all * STAGES * 2 * NV;  // gamma [C]; with several groups also their sums [2][C]
+    float *sums = reinterpret_cast<float *>(gam + vecs);
+    const float inv_c = 1.0f / (float)C;
     uint64_t dg[NV][P], db[NV][P];
-    uint4 xq[NV], yq[NV];
-    float mean_next = 0.0f, rstd_next = 0.0f;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        xq[k] = yq[k] = make_uint4(0, 0, 0, 0);
+    for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < P; ++e) dg[k][e] = db[k][e] = 0;
-    }
-    auto fetch = [&](int64_t row) {
-        const uint4 *xs = reinterpret_cast<const uint4 *>(x + row * C) + tx, *ys = reinterpret_cast<const uint4 *>(dy + row * C) + tx;
+    auto owns = [&](int k) { return FULL || tx + k * threads < vecs; };
+    auto slot = [&](int stage, int which, int k) { return ring + (size_t)((stage * 2 + which) * NV + k) * all; };
+    auto fetch = [&](int64_t row, int stage) {         // always one copy group, so that the waits can count
+        if (row < rows) {
+            const uint4 *xs = reinterpret_cast<const uint4 *>(x + row * C) + tx, *ys = reinterpret_cast<const uint4 *>(dy + row * C) + tx;
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (tx + k * threads < vecs) { xq[k] = xs[k * threads]; yq[k] = ys[k * threads]; }
-        mean_next = mean_in[row];
-        rstd_next = rstd_in[row];
+            for (int k = 0; k < NV; ++k)
+                if (owns(k)) {
+                    copy_async16((uint32_t)__cvta_generic_to_shared(slot(stage, 0, k)), xs + k * threads);
+                    copy_async16((uint32_t)__cvta_generic_to_shared(slot(stage, 1, k)), ys + k * threads);
+                }
+        }
+        copy_async_commit();
     };
     pdl_enter();
     int64_t row = (int64_t)blockIdx.x * groups + id;
-    if (row < rows) fetch(row);
-    for (int i = id * threads + tx; i < vecs; i += threads * groups) gam[i] = reinterpret_cast<const uint4 *>(gamma)[i];
+#pragma unroll
+    for (int k = 0; k < STAGES - 1; ++k) fetch(row + k * step, k);
+    float mean_next = row < rows ? mean_in[row] : 0.0f, rstd_next = row < rows ? rstd_in[row] : 0.0f;
+    for (int i = id * threads + tx; i < vecs; i += all) gam[i] = reinterpret_cast<const uint4 *>(gamma)[i];
     __syncthreads();
+    int stage = 0;
     for (int turn = 0; row < rows; row += step, turn ^= 1) {
         const float rstd = rstd_next;
         const uint64_t neg_mean = pair2(-mean_next, -mean_next), r2 = pair2(rstd, rstd);
-        uint4 xc[NV], yc[NV];
-#pragma unroll
-        for (int k = 0; k < NV; ++k) { xc[k] = xq[k]; yc[k] = yq[k]; }
-        if (row + step < rows) fetch(row + step);          // in flight while this row is worked on
-        uint64_t p0 = 0, p1 = 0;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (tx + k * threads >= vecs) break;
-            uint64_t xv[P], yv[P], g[P];
-            unpack2<N>(xc[k], xv); unpack2<N>(yc[k], yv);
+        if (row + step < rows) { mean_next = mean_in[row + step]; rstd_next = rstd_in[row + step]; }
+        fetch(row + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
+        copy_async_wait<STAGES - 1>();
+        // xh and t = dy gamma of vector k; made twice, because keeping them would spill
+        auto vectors = [&](int k, uint64_t (&xh)[P], uint64_t (&yv)[P], uint64_t (&t)[P]) {
+            uint64_t g[P];
+            unpack2<N>(*slot(stage, 0, k), xh);
+            unpack2<N>(*slot(stage, 1, k), yv);
             unpack2<N>(gam[tx + k * threads], g);
 #pragma unroll
             for (int e = 0; e < P; ++e) {
-                const uint64_t xh = mul2(add2(xv[e], neg_mean), r2), t = mul2(yv[e], g[e]);
-                p0 = add2(p0, t);
-                p1 = fma2(t, xh, p1);
-                dg[k][e] = fma2(yv[e], xh, dg[k][e]);
-                db[k][e] = add2(db[k][e], yv[e]);
+                xh[e] = mul2(add2(xh[e], neg_mean), r2);
+                t[e] = mul2(yv[e], g[e]);
             }
-        }
-        float s0, s1, hi;
-        unpair2(p0, s0, hi);
-        s0 = warp_add(s0 + hi);
-        unpair2(p1, s1, hi);
-        s1 = warp_add(s1 + hi);
+        };
+        uint64_t p0 = 0, p1 = 0;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (owns(k)) {
+                uint64_t xh[P], yv[P], t[P];
+                vectors(k, xh, yv, t);
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    p0 = add2(p0, t[e]);
+                    p1 = fma2(t[e], xh[e], p1);
+                    dg[k][e] = fma2(yv[e], xh[e], dg[k][e]);
+                    db[k][e] = add2(db[k][e], yv[e]);
+                }
+            }
+        float a, b, c, d;
+        unpair2(p0, a, b);
+        unpair2(p1, c, d);
+        float s = warp_add_two(a + b, c + d), s0, s1;
         if (threads > 32) {
-            float *r = red[turn][0] + id * (threads / 32), *q = red[turn][1] + id * (threads / 32);
-            if ((tx & 31) == 0) { r[tx >> 5] = s0; q[tx >> 5] = s1; }
+            float2 *r = red[turn] + id * (threads / 32);
+            if ((tx & 15) == 0) reinterpret_cast<float *>(r + (tx >> 5))[(tx >> 4) & 1] = s;
             group_sync(id, threads);
-            s0 = s1 = 0.0f;
-            for (int k = 0; k < threads / 32; ++k) { s0 += r[k]; s1 += q[k]; }
+            uint64_t sum = 0;
+#pragma unroll 5
+            for (int k = 0; k < threads / 32; ++k) sum = add2(sum, *reinterpret_cast<const uint64_t *>(r + k));
+            unpair2(sum, s0, s1);
+        } else {
+            s0 = __shfl_sync(0xffffffffu, s, 0);
+            s1 = __shfl_sync(0xffffffffu, s, 16);
         }
-        s0 /= -(float)C;
-        s1 /= -(float)C;
+        s0 *= -inv_c;
+        s1 *= -inv_c;
         const uint64_t m0 = pair2(s0, s0), m1 = pair2(s1, s1);
         uint4 *dst = reinterpret_cast<uint4 *>(dx + row * C) + tx;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (tx + k * threads >= vecs) break;
-            uint64_t xv[P], yv[P], g[P];
-            unpack2<N>(xc[k], xv); unpack2<N>(yc[k], yv);
-            unpack2<N>(gam[tx + k * threads], g);
+        for (int k = 0; k < NV; ++k)
+            if (owns(k)) {
+                uint64_t xh[P], yv[P], t[P];
+                vectors(k, xh, yv, t);
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const uint64_t xh = mul2(add2(xv[e], neg_mean), r2);
-                xv[e] = mul2(r2, fma2(xh, m1, fma2(yv[e], g[e], m0)));
+                for (int e = 0; e < P; ++e) xh[e] = mul2(r2, fma2(xh[e], m1, add2(t[e], m0)));
+                dst[k * threads] = pack2<N>(xh);
             }
-            dst[k * threads] = pack2<N>(xv);
-        }
+        if (++stage == STAGES) stage = 0;
     }
+    copy_async_wait<0>();
     if (part == nullptr) return;
     float *out = part + (int64_t)blockIdx.x * 2 * C;
     for (int g = 0; g < groups; ++g) {
@@ -458,12 +507,11 @@ cudaError_t bwd_t(const T *dy, const T *x, const T *gamma, const float *mean, co
         const int groups = LN_BWD_THREADS / t;
         const int64_t need = (rows + groups - 1) / groups;
         parts = (int)(need < sms ? (need > 0 ? need : 1) : sms);
-        const size_t smem = C * (sizeof(T) + (groups > 1 ? 2 * sizeof(float) : 0));   // several groups: C <= 5120
-        if (smem > 32 * 1024) {                 // with the static arrays more than a launch gets unasked
-            e = cudaFuncSetAttribute(k_layernorm_bwd<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024);
-            if (e != cudaSuccess) return e;
-        }
-        e = launch_smem(k_layernorm_bwd<T>, dim3(parts), dim3(t, groups), smem, s, dy, x, gamma, mean, rstd, rows, C, dx,
+        const size_t smem = LnBwd<T>::smem(C, t, groups);        // at most 225280 bytes: several groups only up to C = 5120
+        const auto kern = C == t * LN_BWD_COLS ? k_layernorm_bwd<T, true> : k_layernorm_bwd<T, false>;   // every thread owns its columns
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 225280);
+        if (e != cudaSuccess) return e;
+        e = launch_smem(kern, dim3(parts), dim3(t, groups), smem, s, dy, x, gamma, mean, rstd, rows, C, dx,
                         sums ? part : nullptr);
         if (e != cudaSuccess) return e;
     } else {
