@@ -12,10 +12,10 @@ constexpr uint32_t tmem = 0;
 // Warps of a CTA: TMA, MMA, tail cleaner, an idle one, then ARITH arithmetic warps.  At launch every thread has
 // the same number of registers; the four service warps give some of theirs to the arithmetic warps.
 //   forward : 8 (a row per thread)    384 x 168 = 128 x 88 + 256 x 208
-//   backward: 16 (a quarter of a row) 640 x  96 = 128 x 64 + 512 x 104
+//   backward: 16 (a quarter of a row) 640 x  96
 template <int ARITH> struct Warps {
-    static constexpr int THREADS = 32 * (ARITH + 4), TMA = 0, MMA = 1, TAIL = 2, FIRST = 4, COUNT = ARITH;   // FIRST: arithmetic warps
-    static constexpr int REGS_SERVICE = ARITH == 8 ? 88 : 64, REGS_ARITH = ARITH == 8 ? 208 : 104;
+    static constexpr int THREADS = 32 * (ARITH + 4), TMA = 0, MMA = 1, TAIL = 2, FIRST = 4, COUNT = ARITH;   // FIRST of COUNT arithmetic warps
+    static constexpr int REGS_SERVICE = ARITH == 8 ? 88 : 96, REGS_ARITH = ARITH == 8 ? 208 : 96;
 };
 using FwdWarps = Warps<8>;
 using BwdWarps = Warps<16>;
@@ -75,7 +75,6 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
         }
     }
 }
-__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
@@ -94,22 +93,38 @@ struct AtParams {
     float *lse;
     const float2 *row_stats;
     int32_t *status;
+    int32_t wide;                            // dQ: every 16 columns of a row start on 32 bytes
 };
 struct alignas(64) AtMaps { CUtensorMap q, k, v, g; };
 
 template <int DP> constexpr int tile_bytes() { return TILE * DP * 2; }
 
-// Work items are sorted by falling work; CTA b takes items b, 2 grid - 1 - b, 2 grid + b, ... (the
-// order of a round is reversed every other time), which evens out the sums.
-struct ItemLoop {
-    int round = 0, n;
-    __device__ explicit ItemLoop(int n_) : n(n_) {}
-    __device__ int next()
+// Work items are sorted by falling work; CTA b takes items b, 2 grid - 1 - b, 2 grid + b, ... (the order of a
+// round is reversed every other time), which evens out the sums.  The entry of the next item is fetched when
+// the current one is taken.  WARP: used by a whole warp, whose copies are made uniform for the compiler.
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+template <typename Item, bool WARP> struct Feed {
+    const AtParams &p;
+    int round = 0, idx = -1, h = 0;
+    int4 e = {};
+    __device__ explicit Feed(const AtParams &p_) : p(p_) { fetch(); }
+    __device__ void fetch()
     {
         const int g = (int)gridDim.x, b = (int)blockIdx.x;
-        const int i = round * g + ((round & 1) ? g - 1 - b : b);
+        idx = round * g + ((round & 1) ? g - 1 - b : b);
         ++round;
-        return i < n ? i : -1;
+        if (idx >= p.n_items) { idx = -1; return; }
+        const int t = idx / p.hk;
+        h = idx - t * p.hk;
+        e = p.items[t];
+    }
+    __device__ bool take(Item &it)
+    {
+        if (idx < 0) return false;
+        if (WARP) e = make_int4(uniform(e.x), uniform(e.y), uniform(e.z), uniform(e.w));
+        it.set(p, h, e);
+        fetch();
+        return true;
     }
 };
 
@@ -184,19 +199,39 @@ __device__ __forceinline__ void mma_tmem_rows(uint32_t on, uint32_t d_tmem, uint
     }
 }
 
-// 32 fp32 values of one row times `f`, to bf16, to columns c .. c+31 (below d) of a global row
-__device__ __forceinline__ void store_row32(bf16 *row, const uint32_t (&v)[32], float f, int c, int d)
+// 8 fp32 values times `f` as bf16
+__device__ __forceinline__ uint4 pack8(const uint32_t *v, float f)
+{
+    return make_uint4(pack_bf16(__uint_as_float(v[0]) * f, __uint_as_float(v[1]) * f), pack_bf16(__uint_as_float(v[2]) * f, __uint_as_float(v[3]) * f),
+                      pack_bf16(__uint_as_float(v[4]) * f, __uint_as_float(v[5]) * f), pack_bf16(__uint_as_float(v[6]) * f, __uint_as_float(v[7]) * f));
+}
+// Rows of a warp's accumulator to global memory: CHUNKS x 8 columns of one row per lane go through `stage`
+// (32 x 16 CHUNKS bytes, slots XOR-swizzled by row: no bank conflicts), so that CHUNKS neighbouring lanes write one
+// row's contiguous bytes.  Written straight from the lanes (32 rows, 16 bytes each per instruction) an
+// item's output took 5000 cycles.  dst: this lane's row at the first column, null for a row that is not written;
+// `chunks` of them lie inside the head.
+template <int CHUNKS>
+__device__ __forceinline__ void store_rows(uint32_t stage, int lane, const uint4 (&w)[CHUNKS], bf16 *dst, int chunks)
 {
 #pragma unroll
-    for (int i = 0; i < 32; i += 8)
-        if (c + i < d) {
-            uint4 w;
-            w.x = pack_bf16(__uint_as_float(v[i]) * f, __uint_as_float(v[i + 1]) * f);
-            w.y = pack_bf16(__uint_as_float(v[i + 2]) * f, __uint_as_float(v[i + 3]) * f);
-            w.z = pack_bf16(__uint_as_float(v[i + 4]) * f, __uint_as_float(v[i + 5]) * f);
-            w.w = pack_bf16(__uint_as_float(v[i + 6]) * f, __uint_as_float(v[i + 7]) * f);
-            *reinterpret_cast<uint4 *>(row + c + i) = w;
-        }
+    for (int c = 0; c < CHUNKS; ++c)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * (16 * CHUNKS) + ((c ^ (lane * CHUNKS / 8)) & (CHUNKS - 1)) * 16),
+                     "r"(w[c].x), "r"(w[c].y), "r"(w[c].z), "r"(w[c].w)
+                     : "memory");
+    __syncwarp();
+    const int c = lane & (CHUNKS - 1);
+#pragma unroll
+    for (int it = 0; it < CHUNKS; ++it) {
+        const int row = it * (32 / CHUNKS) + lane / CHUNKS;
+        uint4 v;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                     : "r"(stage + row * (16 * CHUNKS) + ((c ^ (row * CHUNKS / 8)) & (CHUNKS - 1)) * 16)
+                     : "memory");
+        bf16 *d = (bf16 *)__shfl_sync(0xffffffffu, (unsigned long long)dst, row);
+        if (d != nullptr && c < chunks) *reinterpret_cast<uint4 *>(d + 8 * c) = v;
+    }
+    __syncwarp();
 }
 
 // Ends of every kernel: drain after an abort, give the tensor memory back.
@@ -229,8 +264,9 @@ __device__ __forceinline__ void cta_teardown(volatile int *abort_flag, uint32_t 
 // time (P stays below 2^8, far inside the range of bf16 and fp32).
 template <int DP> struct FwdShape {
     static constexpr int T_BYTES = tile_bytes<DP>();
-    static constexpr int SLOTS = DP == 128 ? 5 : 8;
-    static constexpr int SMEM = (2 + SLOTS) * T_BYTES + 512;
+    static constexpr int SLOTS = DP == 128 ? 4 : 8;
+    static constexpr int STAGE = 32 * 128;            // a warp's output rows, 64 columns at a time
+    static constexpr int SMEM = (2 + SLOTS) * T_BYTES + 8 * STAGE + 512;
 };
 struct alignas(8) FwdCtl {
     uint64_t q_full[2], q_empty[2], kv_full[8], kv_empty[8], tail[8], s_full[2], p_full[2][2], o_full[2], o_free[2];   // p_full[g][half]
@@ -354,11 +390,9 @@ __device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, bool u
 
 struct FwdItem {
     int start, len, t0, h, nb0, nb1, end0, end1;   // key blocks and first key past the keys of the two tiles
-    __device__ FwdItem(const AtParams &p, int i, bool whole_warp = true)
+    __device__ void set(const AtParams &p, int head, const int4 &e)
     {
-        int4 e = p.items[i / p.hk];
-        if (whole_warp) e = make_int4(uniform(e.x), uniform(e.y), uniform(e.z), uniform(e.w));
-        h = i % p.hk;
+        h = head;
         start = e.x; len = e.y; t0 = e.z;
         end0 = p.causal ? min(t0 + p.tokens, len) : len;
         end1 = t0 + p.tokens < len ? (p.causal ? min(t0 + 2 * p.tokens, len) : len) : 0;
@@ -377,7 +411,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
     constexpr int T_BYTES = FwdShape<DP>::T_BYTES, SLOTS = FwdShape<DP>::SLOTS;
     extern __shared__ __align__(1024) uint8_t smem_raw[];      // tiles need 1024 bytes
     const uint32_t tiles = smem_u32(smem_raw), q_tile = tiles, ring = tiles + 2 * T_BYTES;
-    FwdCtl *ctl = reinterpret_cast<FwdCtl *>(smem_raw + (2 + SLOTS) * T_BYTES);
+    FwdCtl *ctl = reinterpret_cast<FwdCtl *>(smem_raw + (2 + SLOTS) * T_BYTES + 8 * FwdShape<DP>::STAGE);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
@@ -407,7 +441,6 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
     volatile int *ab = &ctl->abort_flag;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    ItemLoop loop(p.n_items);
 
     if (warp < FwdWarps::FIRST) regs_down<FwdWarps::REGS_SERVICE>();
     if (warp == FwdWarps::TMA) {
@@ -428,8 +461,9 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
                 load_tile<DP>(q_tile + g * T_BYTES, &tm.q, it.h * p.group, it.start + it.t0 + g * p.tokens, bar);
                 ++nq[g];
             };
-            for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
-                const FwdItem it(p, i, false);      // one lane
+            Feed<FwdItem, false> feed(p);
+            FwdItem it;
+            while (ok && feed.take(it)) {
                 const int n = it.blocks();
                 load_q(it, 0);
                 for (int j = 0; j < n && ok; ++j) {
@@ -451,8 +485,9 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
     } else if (warp == FwdWarps::TAIL) {
         uint32_t pos = 0, seen = 0;          // bit s: parity of the tail events of slot s
         bool ok = true;
-        for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
-            const FwdItem it(p, i);
+        Feed<FwdItem, true> feed(p);
+        FwdItem it;
+        while (ok && feed.take(it)) {
             const int n = it.blocks();
             pos += 2 * n;
             if (!it.dirty_tail()) continue;
@@ -478,8 +513,9 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             if (++slot == SLOTS) { slot = 0; phase ^= 1; }
             return s;
         };
-        for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
-            const FwdItem it(p, i);
+        Feed<FwdItem, true> feed(p);
+        FwdItem it;
+        while (ok && feed.take(it)) {
             const int n = it.blocks();
             const int nb[2] = {it.nb0, it.nb1};
             const int last_cols[2] = {mma_cols(it.end0 - (it.nb0 - 1) * TILE), mma_cols(it.end1 - (it.nb1 - 1) * TILE)};
@@ -545,8 +581,9 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
         uint32_t ns = 0, no = 0;
         bool ok = true;
         const int row_t = row / p.group, row_h = row - row_t * p.group;
-        for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
-            const FwdItem it(p, i);
+        Feed<FwdItem, true> feed(p);
+        FwdItem it;
+        while (ok && feed.take(it)) {
             const int nb = g ? it.nb1 : it.nb0, end = g ? it.end1 : it.end0, t0 = it.t0 + g * p.tokens;
             if (nb == 0) continue;
             const int token = t0 + row_t;
@@ -572,13 +609,20 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             const float inv = 1.0f / l;
             const int head = it.h * p.group + row_h;
             const int64_t tok = (int64_t)it.start + token;
-            bf16 *dst = p.out0 + tok * p.ld0 + (int64_t)head * p.d;
-#pragma unroll
-            for (int c = 0; c < DP; c += 32) {
+            bf16 *dst = live ? p.out0 + tok * p.ld0 + (int64_t)head * p.d : nullptr;
+            const uint32_t stage = ring + SLOTS * T_BYTES + (warp - FwdWarps::FIRST) * FwdShape<DP>::STAGE;
+#pragma unroll 1
+            for (int c = 0; c < DP; c += 64) {
                 uint32_t o[32];
-                tmem_ld32(t_o + c, o);
-                tmem_ld_wait(o);
-                if (live) store_row32(dst, o, inv, c, p.d);
+                uint4 w[8];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    tmem_ld32(t_o + c + 32 * h, o);
+                    tmem_ld_wait(o);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w[4 * h + k] = pack8(o + 8 * k, inv);
+                }
+                store_rows<8>(stage, lane, w, dst ? dst + c : nullptr, (p.d - c) / 8);
             }
             tc_fence_before();
             __syncwarp();
@@ -600,21 +644,20 @@ template <int DP> struct KvShape {
     static constexpr int T_BYTES = tile_bytes<DP>();
     static constexpr int STAGES = 2;
     static constexpr int STAT_BYTES = TILE * 8;
-    static constexpr int SMEM = (2 + 2 * STAGES) * T_BYTES + STAGES * STAT_BYTES + 512;
+    static constexpr int STAGE = 32 * 64;             // a warp's output rows, 32 columns at a time
+    static constexpr int SMEM = (2 + 2 * STAGES) * T_BYTES + STAGES * STAT_BYTES + BwdWarps::COUNT * STAGE + 512;
 };
 struct alignas(8) KvCtl {
-    uint64_t kv_full, kv_empty, q_full[2], g_full[2], empty[2], q_tail[2], g_tail[2];
+    uint64_t k_full, k_empty, v_full, v_empty, q_full[2], g_full[2], empty[2], q_tail[2], g_tail[2];
     uint64_t s_full, g_scores, p_ready, ds_ready, acc_full, acc_free;
     uint32_t tmem_base;
     volatile int abort_flag;
 };
 struct KvItem {
     int start, len, k0, base, h, first, n;      // row tiles first .. first + n - 1 of the sequence
-    __device__ KvItem(const AtParams &p, int i, bool whole_warp = true)
+    __device__ void set(const AtParams &p, int head, const int4 &e)
     {
-        int4 e = p.items[i / p.hk];
-        if (whole_warp) e = make_int4(uniform(e.x), uniform(e.y), uniform(e.z), uniform(e.w));
-        h = i % p.hk;
+        h = head;
         start = e.x; len = e.y; k0 = e.z; base = e.w;
         first = p.causal ? k0 / p.tokens : 0;
         n = ceil_div(len, p.tokens) - first;
@@ -638,7 +681,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
     const uint32_t k_tile = tiles, v_tile = tiles + T_BYTES, q_ring = tiles + 2 * T_BYTES, g_ring = q_ring + 2 * T_BYTES;
     const uint32_t stats = g_ring + 2 * T_BYTES;
     uint8_t *after = smem_raw + (stats - smem_u32(smem_raw));
-    KvCtl *ctl = reinterpret_cast<KvCtl *>(after + Sh::STAGES * Sh::STAT_BYTES);
+    KvCtl *ctl = reinterpret_cast<KvCtl *>(after + Sh::STAGES * Sh::STAT_BYTES + BwdWarps::COUNT * Sh::STAGE);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
@@ -648,8 +691,10 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
             mbar_init(smem_u32(&ctl->g_tail[i]), 1);
             mbar_init(smem_u32(&ctl->empty[i]), 1);
         }
-        mbar_init(smem_u32(&ctl->kv_full), 1);
-        mbar_init(smem_u32(&ctl->kv_empty), 1);
+        mbar_init(smem_u32(&ctl->k_full), 1);
+        mbar_init(smem_u32(&ctl->k_empty), 1);
+        mbar_init(smem_u32(&ctl->v_full), 1);
+        mbar_init(smem_u32(&ctl->v_empty), 1);
         mbar_init(smem_u32(&ctl->s_full), 1);
         mbar_init(smem_u32(&ctl->g_scores), 1);
         mbar_init(smem_u32(&ctl->p_ready), BwdWarps::COUNT);
@@ -669,7 +714,6 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
     volatile int *ab = &ctl->abort_flag;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    ItemLoop loop(p.n_items);
     const uint32_t t_s = tmem, t_dp = tmem + TILE, t_dv = tmem + 2 * TILE, t_dk = t_dv + DP;
 
     if (warp < BwdWarps::FIRST) regs_down<BwdWarps::REGS_SERVICE>();
@@ -677,35 +721,43 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
         if (lane == 0) {
             uint32_t cnt = 0, items = 0;
             bool ok = true;
-            for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
-                const KvItem it(p, i, false);      // one lane
-                ok = wait_bar<true>(smem_u32(&ctl->kv_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
-                if (!ok) break;
-                const uint32_t kvb = smem_u32(&ctl->kv_full);
-                mbar_expect_tx(kvb, 2 * T_BYTES);
-                load_tile<DP>(k_tile, &tm.k, it.h, it.start + it.k0, kvb);
-                load_tile<DP>(v_tile, &tm.v, it.h, it.start + it.k0, kvb);
+            Feed<KvItem, false> feed(p);
+            KvItem it;
+            for (; ok && feed.take(it); ++items) {
                 for (int j = 0; j < it.n; ++j, ++cnt) {
                     const uint32_t s = cnt & 1;
-                    ok = wait_bar<true>(smem_u32(&ctl->empty[s]), ((cnt >> 1) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
-                    if (!ok) break;
                     const int tile = it.first + j, token = it.start + tile * p.tokens;
                     const bool dirty = it.dirty(p, tile);
                     const uint32_t qb = smem_u32(dirty ? &ctl->q_tail[s] : &ctl->q_full[s]);
                     const uint32_t gb = smem_u32(dirty ? &ctl->g_tail[s] : &ctl->g_full[s]);
+                    if (j == 0) {
+                        ok = wait_bar<true>(smem_u32(&ctl->k_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                        if (!ok) break;
+                        mbar_expect_tx(smem_u32(&ctl->k_full), T_BYTES);
+                        load_tile<DP>(k_tile, &tm.k, it.h, it.start + it.k0, smem_u32(&ctl->k_full));
+                    }
+                    ok = wait_bar<true>(smem_u32(&ctl->empty[s]), ((cnt >> 1) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    if (!ok) break;
                     mbar_expect_tx(qb, (uint32_t)(used * DP * 2) + Sh::STAT_BYTES);
                     load_tile<DP>(q_ring + s * T_BYTES, &tm.q, it.h * p.group, token, qb);
                     bulk_load(stats + s * Sh::STAT_BYTES, p.row_stats + ((int64_t)(it.base + tile) * p.hk + it.h) * TILE, Sh::STAT_BYTES, qb);
                     mbar_expect_tx(gb, (uint32_t)(used * DP * 2));
                     load_tile<DP>(g_ring + s * T_BYTES, &tm.g, it.h * p.group, token, gb);
+                    if (j == 0) {
+                        ok = wait_bar<true>(smem_u32(&ctl->v_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                        if (!ok) break;
+                        mbar_expect_tx(smem_u32(&ctl->v_full), T_BYTES);
+                        load_tile<DP>(v_tile, &tm.v, it.h, it.start + it.k0, smem_u32(&ctl->v_full));
+                    }
                 }
             }
         }
     } else if (warp == BwdWarps::TAIL) {
         uint32_t cnt = 0, seen = 0;
         bool ok = true;
-        for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
-            const KvItem it(p, i);
+        Feed<KvItem, true> feed(p);
+        KvItem it;
+        while (ok && feed.take(it)) {
             cnt += it.n;
             const int tile = it.first + it.n - 1;          // only a sequence's last row tile can be short
             if (!it.dirty(p, tile)) continue;
@@ -727,8 +779,9 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
         const uint32_t q_across = desc_across(q_ring), g_across = desc_across(g_ring);
         uint32_t cnt = 0, items = 0;
         bool ok = true;
-        for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
-            const KvItem it(p, i);
+        Feed<KvItem, true> feed(p);
+        KvItem it;
+        for (; ok && feed.take(it); ++items) {
             auto cols_of = [&](int j) { return mma_cols(it.valid(p, it.first + j)); };
             auto scores = [&](int j, uint32_t c) {
                 ok = ok && wait_warp(smem_u32(&ctl->q_full[c & 1]), (c >> 1) & 1, ab, p.status, SITE_MMA_FULL);
@@ -736,6 +789,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 tc_fence_after();
                 mma_rows_rows<DP>(on, t_s, k_desc, q_desc + (c & 1) * (T_BYTES >> 4), idesc_rows(cols_of(j)));
                 umma_commit_if(on, smem_u32(&ctl->s_full));
+                if (j == it.n - 1) umma_commit_if(on, smem_u32(&ctl->k_empty));
             };
             auto grad_scores = [&](int j, uint32_t c) {
                 ok = ok && wait_warp(smem_u32(&ctl->g_full[c & 1]), (c >> 1) & 1, ab, p.status, SITE_MMA_FULL);
@@ -743,9 +797,11 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 tc_fence_after();
                 mma_rows_rows<DP>(on, t_dp, v_desc, g_desc + (c & 1) * (T_BYTES >> 4), idesc_rows(cols_of(j)));
                 umma_commit_if(on, smem_u32(&ctl->g_scores));
+                if (j == it.n - 1) umma_commit_if(on, smem_u32(&ctl->v_empty));
             };
-            ok = wait_warp(smem_u32(&ctl->kv_full), items & 1, ab, p.status, SITE_MMA_FULL);
+            ok = wait_warp(smem_u32(&ctl->k_full), items & 1, ab, p.status, SITE_MMA_FULL);
             scores(0, cnt);
+            ok = ok && wait_warp(smem_u32(&ctl->v_full), items & 1, ab, p.status, SITE_MMA_FULL);
             grad_scores(0, cnt);
             for (int j = 0; j < it.n && ok; ++j, ++cnt) {
                 const uint32_t s = cnt & 1;
@@ -765,7 +821,6 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
             }
             if (!ok) break;
             umma_commit_if(on, smem_u32(&ctl->acc_full));
-            umma_commit_if(on, smem_u32(&ctl->kv_empty));
         }
     } else if (warp >= BwdWarps::FIRST) {
         regs_up<BwdWarps::REGS_ARITH>();
@@ -773,8 +828,9 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         uint32_t cnt = 0, items = 0;
         bool ok = true;
-        for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
-            const KvItem it(p, i);
+        Feed<KvItem, true> feed(p);
+        KvItem it;
+        for (; ok && feed.take(it); ++items) {
             const int key = it.k0 + row;
             for (int j = 0; j < it.n; ++j, ++cnt) {
                 const int tile = it.first + j, t0 = tile * p.tokens;
@@ -844,12 +900,16 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
             const bool live = key < it.len, is_k = part >= 2;
             const int col = (part & 1) * (DP / 2);
             bf16 *dst = (is_k ? p.out0 + ((int64_t)it.start + key) * p.ld0 : p.out1 + ((int64_t)it.start + key) * p.ld1) + (int64_t)it.h * p.d;
-#pragma unroll
-            for (int c = 0; c < DP / 2; c += 32) {
+            const uint32_t stage = stats + Sh::STAGES * Sh::STAT_BYTES + (warp - BwdWarps::FIRST) * Sh::STAGE;
+#pragma unroll 1
+            for (int c = col; c < col + DP / 2; c += 32) {
                 uint32_t o[32];
-                tmem_ld32((is_k ? t_dk : t_dv) + lanes + col + c, o);
+                uint4 w[4];
+                tmem_ld32((is_k ? t_dk : t_dv) + lanes + c, o);
                 tmem_ld_wait(o);
-                if (live) store_row32(dst, o, is_k ? p.scale : 1.0f, col + c, p.d);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = pack8(o + 8 * k, is_k ? p.scale : 1.0f);
+                store_rows<4>(stage, lane, w, live ? dst + c : nullptr, (p.d - c) / 8);
             }
             tc_fence_before();
             __syncwarp();
@@ -868,18 +928,16 @@ template <int DP> struct QShape {
     static constexpr int SMEM = (2 + KS + VS) * T_BYTES + 512;
 };
 struct alignas(8) QCtl {
-    uint64_t q_full, q_empty, k_full[3], k_empty[3], k_tail[3], v_full[2], v_empty[2];
+    uint64_t q_full, q_empty, g_full, g_empty, k_full[3], k_empty[3], k_tail[3], v_full[2], v_empty[2];
     uint64_t s_full[2], g_scores, ds_ready, acc_full, acc_free;
     uint32_t tmem_base;
     volatile int abort_flag;
 };
 struct QItem {
     int start, len, t0, tile, h, end, nb;
-    __device__ QItem(const AtParams &p, int i, bool whole_warp = true)
+    __device__ void set(const AtParams &p, int head, const int4 &e)
     {
-        int4 e = p.items[i / p.hk];
-        if (whole_warp) e = make_int4(uniform(e.x), uniform(e.y), uniform(e.z), uniform(e.w));
-        h = i % p.hk;
+        h = head;
         start = e.x; len = e.y; t0 = e.z; tile = e.w + t0 / p.tokens;
         end = p.causal ? min(t0 + p.tokens, len) : len;
         nb = ceil_div(end, TILE);
@@ -901,6 +959,8 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&ctl->q_full), 1);
         mbar_init(smem_u32(&ctl->q_empty), 1);
+        mbar_init(smem_u32(&ctl->g_full), 1);
+        mbar_init(smem_u32(&ctl->g_empty), 1);
         for (int i = 0; i < KS; ++i) {
             mbar_init(smem_u32(&ctl->k_full[i]), 1);
             mbar_init(smem_u32(&ctl->k_empty[i]), 1);
@@ -929,7 +989,6 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
     volatile int *ab = &ctl->abort_flag;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    ItemLoop loop(p.n_items);
     const uint32_t t_dp = tmem + 2 * TILE, t_dq = tmem + 3 * TILE;
 
     if (warp < BwdWarps::FIRST) regs_down<BwdWarps::REGS_SERVICE>();
@@ -937,14 +996,13 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
         if (lane == 0) {
             uint32_t cnt = 0, items = 0;
             bool ok = true;
-            for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
-                const QItem it(p, i, false);      // one lane
+            Feed<QItem, false> feed(p);
+            QItem it;
+            for (; ok && feed.take(it); ++items) {
                 ok = wait_bar<true>(smem_u32(&ctl->q_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                 if (!ok) break;
-                const uint32_t qb = smem_u32(&ctl->q_full);
-                mbar_expect_tx(qb, (uint32_t)(2 * used * DP * 2));
-                load_tile<DP>(q_tile, &tm.q, it.h * p.group, it.start + it.t0, qb);
-                load_tile<DP>(g_tile, &tm.g, it.h * p.group, it.start + it.t0, qb);
+                mbar_expect_tx(smem_u32(&ctl->q_full), (uint32_t)(used * DP * 2));
+                load_tile<DP>(q_tile, &tm.q, it.h * p.group, it.start + it.t0, smem_u32(&ctl->q_full));
                 for (int j = 0; j < it.nb; ++j, ++cnt) {
                     const uint32_t ks = cnt % KS, vs = cnt % VS;
                     ok = wait_bar<true>(smem_u32(&ctl->k_empty[ks]), ((cnt / KS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
@@ -952,6 +1010,12 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                     const uint32_t kb = smem_u32(j == it.nb - 1 && it.dirty_tail() ? &ctl->k_tail[ks] : &ctl->k_full[ks]);
                     mbar_expect_tx(kb, T_BYTES);
                     load_tile<DP>(k_ring + ks * T_BYTES, &tm.k, it.h, it.start + j * TILE, kb);
+                    if (j == 0) {
+                        ok = wait_bar<true>(smem_u32(&ctl->g_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                        if (!ok) break;
+                        mbar_expect_tx(smem_u32(&ctl->g_full), (uint32_t)(used * DP * 2));
+                        load_tile<DP>(g_tile, &tm.g, it.h * p.group, it.start + it.t0, smem_u32(&ctl->g_full));
+                    }
                     ok = wait_bar<true>(smem_u32(&ctl->v_empty[vs]), ((cnt / VS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
                     if (!ok) break;
                     const uint32_t vb = smem_u32(&ctl->v_full[vs]);
@@ -963,8 +1027,9 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
     } else if (warp == BwdWarps::TAIL) {
         uint32_t cnt = 0, seen = 0;
         bool ok = true;
-        for (int i = loop.next(); i >= 0 && ok; i = loop.next()) {
-            const QItem it(p, i);
+        Feed<QItem, true> feed(p);
+        QItem it;
+        while (ok && feed.take(it)) {
             cnt += it.nb;
             if (!it.dirty_tail()) continue;
             const uint32_t s = (cnt - 1) % KS;
@@ -983,8 +1048,9 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
         const uint32_t k_across = desc_across(k_ring);
         uint32_t cnt = 0, items = 0;
         bool ok = true;
-        for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
-            const QItem it(p, i);
+        Feed<QItem, true> feed(p);
+        QItem it;
+        for (; ok && feed.take(it); ++items) {
             auto cols_of = [&](int j) { return mma_cols(it.end - j * TILE); };
             auto scores = [&](int j, uint32_t c) {
                 ok = ok && wait_warp(smem_u32(&ctl->k_full[c % KS]), (c / KS) & 1, ab, p.status, SITE_MMA_FULL);
@@ -992,6 +1058,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 tc_fence_after();
                 mma_rows_rows<DP>(on, tmem + (c & 1) * TILE, q_desc, k_desc + (c % KS) * (T_BYTES >> 4), idesc_rows(cols_of(j)));
                 umma_commit_if(on, smem_u32(&ctl->s_full[c & 1]));
+                if (j == it.nb - 1) umma_commit_if(on, smem_u32(&ctl->q_empty));
             };
             auto grad_scores = [&](int j, uint32_t c) {
                 ok = ok && wait_warp(smem_u32(&ctl->v_full[c % VS]), (c / VS) & 1, ab, p.status, SITE_MMA_FULL);
@@ -1000,9 +1067,11 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 mma_rows_rows<DP>(on, t_dp, g_desc, v_desc + (c % VS) * (T_BYTES >> 4), idesc_rows(cols_of(j)));
                 umma_commit_if(on, smem_u32(&ctl->g_scores));
                 umma_commit_if(on, smem_u32(&ctl->v_empty[c % VS]));
+                if (j == it.nb - 1) umma_commit_if(on, smem_u32(&ctl->g_empty));
             };
             ok = wait_warp(smem_u32(&ctl->q_full), items & 1, ab, p.status, SITE_MMA_FULL);
             scores(0, cnt);
+            ok = ok && wait_warp(smem_u32(&ctl->g_full), items & 1, ab, p.status, SITE_MMA_FULL);
             grad_scores(0, cnt);
             if (it.nb > 1) scores(1, cnt + 1);
             for (int j = 0; j < it.nb && ok; ++j, ++cnt) {
@@ -1020,7 +1089,6 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
             }
             if (!ok) break;
             umma_commit_if(on, smem_u32(&ctl->acc_full));
-            umma_commit_if(on, smem_u32(&ctl->q_empty));
         }
     } else if (warp >= BwdWarps::FIRST) {
         regs_up<BwdWarps::REGS_ARITH>();
@@ -1029,8 +1097,9 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
         const int row_t = row / p.group, row_h = row - row_t * p.group;
         uint32_t cnt = 0, items = 0;
         bool ok = true;
-        for (int i = loop.next(); i >= 0 && ok; i = loop.next(), ++items) {
-            const QItem it(p, i);
+        Feed<QItem, true> feed(p);
+        QItem it;
+        for (; ok && feed.take(it); ++items) {
             const float2 st = p.row_stats[((int64_t)it.tile * p.hk + it.h) * TILE + row];
             const int token = it.t0 + row_t, row_end = p.causal ? min(token + 1, it.len) : it.len;
             for (int j = 0; j < it.nb; ++j, ++cnt) {
@@ -1074,8 +1143,21 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 uint32_t o[32];
                 tmem_ld32(t_dq + lanes + c0, o);
                 tmem_ld_wait(o);
-                if (live)
-                    store_row32(p.out0 + ((int64_t)it.start + token) * p.ld0 + (int64_t)(it.h * p.group + row_h) * p.d, o, p.scale, c0, p.d);
+                bf16 *dst = p.out0 + ((int64_t)it.start + token) * p.ld0 + (int64_t)(it.h * p.group + row_h) * p.d + c0;
+#pragma unroll
+                for (int k = 0; k < 4; k += 2) {
+                    const uint4 a = pack8(o + 8 * k, p.scale), b = pack8(o + 8 * k + 8, p.scale);
+                    if (live && c0 + 8 * k < p.d) {
+                        if (p.wide)                  // 32 bytes per lane: whole sectors (there is no room to stage rows here)
+                            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 8 * k), "r"(a.x), "r"(a.y),
+                                         "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                                         : "memory");
+                        else {
+                            *reinterpret_cast<uint4 *>(dst + 8 * k) = a;
+                            if (c0 + 8 * k + 8 < p.d) *reinterpret_cast<uint4 *>(dst + 8 * k + 8) = b;
+                        }
+                    }
+                }
             }
             tc_fence_before();
             __syncwarp();
@@ -1164,6 +1246,7 @@ template <int DP> static cudaError_t backward_dp(const AttnArgs &a, cudaStream_t
     if (e != cudaSuccess) return e;
     p = params_of(a, a.row_items, a.n_rows);
     p.out0 = (bf16 *)a.dq; p.ld0 = a.lddq;
+    p.wide = ((uintptr_t)a.dq & 31u) == 0 && a.lddq % 16 == 0 && a.d % 16 == 0;
     return launch_at(k_attention_bwd_q<DP>, BwdWarps::THREADS, sms_q, QShape<DP>::SMEM, tm, p, s);
 }
 
