@@ -246,30 +246,32 @@ def summary_backward(X, seg_offsets, w, probs, dxs, dw_fp32=False):
     return dX, dw
 
 
-def _on_device(fn, device, *args):
-    """Call a library function with `device` current and its current stream as the last argument."""
+def _on_device(fn, index, *args):
+    """Call a library function with CUDA device `index` current and its current stream as the last argument.
+    (The raw getters cost a few hundred nanoseconds; ``torch.cuda.current_stream`` alone cost a third of a
+    small call.)"""
     import torch
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if torch.cuda.current_device() == device.index:
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if torch._C._cuda_getDevice() == index:
         return fn(*args, stream)
-    with torch.cuda.device(device):
+    with torch.cuda.device(index):
         return fn(*args, stream)
 
 
 def _layernorm_rows(x, name, like=None):
-    """Checks a ``[..., C]`` tensor of packed rows; returns (dtype, rows, C)."""
+    """Checks a ``[..., C]`` tensor of packed rows; returns (dtype, C)."""
     import torch
-    if not x.is_cuda or not x.is_contiguous() or x.dim() < 1 or x.dtype not in (torch.bfloat16, torch.float32):
+    dt = x.dtype
+    if not x.is_cuda or not x.is_contiguous() or x.dim() < 1 or (dt is not torch.bfloat16 and dt is not torch.float32):
         raise ValueError(f"{name} must be a contiguous bf16 or fp32 CUDA tensor")
-    if like is not None and (x.shape != like.shape or x.dtype != like.dtype or x.device != like.device):
+    if like is not None and (x.shape != like.shape or dt is not like.dtype or x.get_device() != like.get_device()):
         raise ValueError(f"{name} must have the shape, dtype and device of x")
-    C = x.shape[-1]
-    return BF16 if x.dtype == torch.bfloat16 else FP32, x.numel() // C if C else 0, C
+    return BF16 if dt is torch.bfloat16 else FP32, x.shape[-1]
 
 
-def _layernorm_vec(t, name, n, dtype, device):
-    if t.dtype != dtype or t.device != device or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} entries on {device}")
+def _layernorm_vec(t, name, n, dtype, index):
+    if t.dtype is not dtype or t.get_device() != index or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} entries on the device of x")
     return t.data_ptr()
 
 
@@ -277,35 +279,45 @@ def layernorm_forward(x, gamma, beta=None, eps: float = 1e-5, out=None):
     """Layer normalisation of the rows of ``x [..., C]`` (``skipffn_layernorm_forward``): ``(y, mean, rstd)``,
     the last two fp32 with one entry per row, which is what the backward needs.  ``out`` may be ``x``."""
     import torch
-    dtype, n, C = _layernorm_rows(x, "x")
-    g = _layernorm_vec(gamma, "gamma", C, x.dtype, x.device)
-    b = None if beta is None else _layernorm_vec(beta, "beta", C, x.dtype, x.device)
-    y = torch.empty_like(x) if out is None else out
-    _layernorm_rows(y, "out", x)
-    mean, rstd = torch.empty((2, n), dtype=torch.float32, device=x.device).unbind(0)
-    st = _on_device(load_library().skipffn_layernorm_forward, x.device, x.data_ptr(), g, b, n, C, dtype, float(eps), y.data_ptr(),
+    dtype, C = _layernorm_rows(x, "x")
+    index, dt = x.get_device(), x.dtype
+    n = x.numel() // C if C else 0
+    g = _layernorm_vec(gamma, "gamma", C, dt, index)
+    b = None if beta is None else _layernorm_vec(beta, "beta", C, dt, index)
+    if out is None:
+        out = torch.empty_like(x)
+    else:
+        _layernorm_rows(out, "out", x)
+    mean = x.new_empty(n, dtype=torch.float32)
+    rstd = x.new_empty(n, dtype=torch.float32)
+    st = _on_device(load_library().skipffn_layernorm_forward, index, x.data_ptr(), g, b, n, C, dtype, eps, out.data_ptr(),
                     mean.data_ptr(), rstd.data_ptr())
     if st != 0:
         raise SkipFFNError(st, "skipffn_layernorm_forward")
-    return y, mean, rstd
+    return out, mean, rstd
 
 
 def layernorm_backward(dy, x, gamma, mean, rstd, dw_fp32: bool = False, dx=None):
     """``(dx, dgamma, dbeta)`` of ``layernorm_forward`` (``skipffn_layernorm_backward``); ``dx`` may be ``dy``."""
     import torch
     lib = load_library()
-    dtype, n, C = _layernorm_rows(x, "x")
+    dtype, C = _layernorm_rows(x, "x")
     _layernorm_rows(dy, "dy", x)
-    g = _layernorm_vec(gamma, "gamma", C, x.dtype, x.device)
-    m = _layernorm_vec(mean, "mean", n, torch.float32, x.device)
-    r = _layernorm_vec(rstd, "rstd", n, torch.float32, x.device)
-    dx = torch.empty_like(x) if dx is None else dx
-    _layernorm_rows(dx, "dx", x)
-    dgamma, dbeta = torch.empty((2, C), dtype=torch.float32 if dw_fp32 else x.dtype, device=x.device).unbind(0)
-    nbytes = int(lib.skipffn_layernorm_scratch_bytes(C))
-    scratch = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
-    st = _on_device(lib.skipffn_layernorm_backward, x.device, dy.data_ptr(), x.data_ptr(), g, m, r, n, C, dtype, dx.data_ptr(),
-                    dgamma.data_ptr(), dbeta.data_ptr(), int(dw_fp32), scratch.data_ptr(), nbytes)
+    index, dt = x.get_device(), x.dtype
+    n = x.numel() // C if C else 0
+    g = _layernorm_vec(gamma, "gamma", C, dt, index)
+    m = _layernorm_vec(mean, "mean", n, torch.float32, index)
+    r = _layernorm_vec(rstd, "rstd", n, torch.float32, index)
+    if dx is None:
+        dx = torch.empty_like(x)
+    else:
+        _layernorm_rows(dx, "dx", x)
+    gdt = torch.float32 if dw_fp32 else dt
+    dgamma, dbeta = x.new_empty(C, dtype=gdt), x.new_empty(C, dtype=gdt)
+    nbytes = lib.skipffn_layernorm_scratch_bytes(C)
+    scratch = x.new_empty(nbytes, dtype=torch.uint8)
+    st = _on_device(lib.skipffn_layernorm_backward, index, dy.data_ptr(), x.data_ptr(), g, m, r, n, C, dtype, dx.data_ptr(),
+                    dgamma.data_ptr(), dbeta.data_ptr(), 1 if dw_fp32 else 0, scratch.data_ptr(), nbytes)
     if st != 0:
         raise SkipFFNError(st, "skipffn_layernorm_backward")
     return dx, dgamma, dbeta
@@ -357,10 +369,11 @@ class PackedAttention:
         self._torch, self.lib = torch, load_library()
         self.heads_q, self.heads_kv, self.head_dim = int(heads_q), int(heads_kv), int(head_dim)
         self.torch_dtype = torch.bfloat16 if dtype == BF16 else torch.float32
-        self._align = 8 if dtype == BF16 else 4
         self.device = torch.device(device)
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
+        self._forward, self._backward = self.lib.skipffn_attention_forward, self.lib.skipffn_attention_backward
         vals = [int(v) for v in cu_seqlens]
         if any(not 0 <= v < 1 << 31 for v in vals):
             raise ValueError("cu_seqlens must be offsets that fit 32 bits")
@@ -389,58 +402,51 @@ class PackedAttention:
 
     def _arg(self, t, name, heads):
         """(address, token stride) of a [tokens, heads, head_dim] tensor, checked."""
-        shape = t.shape
-        if t.dtype != self.torch_dtype or t.device != self.device:
+        if t.dtype is not self.torch_dtype or t.get_device() != self._index:
             raise ValueError(f"{name} must be a {self.torch_dtype} tensor on {self.device}")
-        if len(shape) != 3 or shape[0] < self.tokens or shape[1] != heads or shape[2] != self.head_dim:
-            raise ValueError(f"{name} must have shape [>= {self.tokens}, {heads}, {self.head_dim}], got {list(shape)}")
+        shape, d = t.shape, self.head_dim
+        if len(shape) != 3 or shape[0] < self.tokens or shape[1] != heads or shape[2] != d:
+            raise ValueError(f"{name} must have shape [>= {self.tokens}, {heads}, {d}], got {list(shape)}")
         ld, sh, sd = t.stride()
-        if sd != 1 or (heads > 1 and sh != self.head_dim):
+        if sd != 1 or (sh != d and heads > 1):
             raise ValueError(f"{name} must have contiguous heads")
-        return t.data_ptr(), ld if shape[0] > 1 else heads * self.head_dim
-
-    def _call(self, name, *args):
-        torch = self._torch
-        fn = getattr(self.lib, name)
-        if torch.cuda.current_device() == self.device.index:
-            st = fn(self._handle, *args, self._stream())
-        else:
-            with torch.cuda.device(self.device):
-                st = fn(self._handle, *args, self._stream())
-        if st != 0:
-            raise SkipFFNError(st, name)
+        return t.data_ptr(), ld if shape[0] > 1 else heads * d
 
     def forward(self, q, k, v, out=None, lse=None):
         """``(out [tokens, heads_q, head_dim], lse [tokens, heads_q] fp32)``.  ``out`` and ``lse`` may be given."""
-        torch = self._torch
-        args = self._arg(q, "q", self.heads_q) + self._arg(k, "k", self.heads_kv) + self._arg(v, "v", self.heads_kv)
+        hq, hk = self.heads_q, self.heads_kv
+        args = self._arg(q, "q", hq) + self._arg(k, "k", hk) + self._arg(v, "v", hk)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
         if lse is None:
-            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-        self._check_lse(lse)
-        self._call("skipffn_attention_forward", *args, *self._arg(out, "out", self.heads_q), lse.data_ptr())
+            lse = q.new_empty(q.shape[:2], dtype=self._torch.float32)
+        else:
+            self._check_lse(lse)
+        st = _on_device(self._forward, self._index, self._handle, *args, *self._arg(out, "out", hq), lse.data_ptr())
+        if st != 0:
+            raise SkipFFNError(st, "skipffn_attention_forward")
         return out, lse
 
     def _check_lse(self, lse):
-        if (lse.dtype != self._torch.float32 or lse.device != self.device or lse.dim() != 2 or lse.shape[0] < self.tokens
-                or lse.shape[1] != self.heads_q or not lse.is_contiguous()):
+        if (lse.dtype is not self._torch.float32 or lse.get_device() != self._index or lse.dim() != 2
+                or lse.shape[0] < self.tokens or lse.shape[1] != self.heads_q or not lse.is_contiguous()):
             raise ValueError(f"lse must be a contiguous float32 tensor [>= {self.tokens}, {self.heads_q}] on {self.device}")
 
     def backward(self, dout, q, k, v, out, lse, dq=None, dk=None, dv=None):
         """``(dq, dk, dv)`` from the forward's inputs and results; the three may be given (slices of one
         fused gradient, say) but must not overlap the inputs."""
-        torch = self._torch
         hq, hk = self.heads_q, self.heads_kv
         args = (self._arg(dout, "dout", hq) + self._arg(q, "q", hq) + self._arg(k, "k", hk) + self._arg(v, "v", hk)
                 + self._arg(out, "out", hq))
         self._check_lse(lse)
-        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-        dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
-        dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
-        scratch = torch.empty(max(self.scratch_bytes, 16), dtype=torch.uint8, device=self.device)
-        self._call("skipffn_attention_backward", *args, lse.data_ptr(), *self._arg(dq, "dq", hq), *self._arg(dk, "dk", hk),
-                   *self._arg(dv, "dv", hk), scratch.data_ptr(), scratch.numel())
+        dq = q.new_empty(q.shape) if dq is None else dq
+        dk = k.new_empty(k.shape) if dk is None else dk
+        dv = v.new_empty(v.shape) if dv is None else dv
+        scratch = q.new_empty(max(self.scratch_bytes, 16), dtype=self._torch.uint8)
+        st = _on_device(self._backward, self._index, self._handle, *args, lse.data_ptr(), *self._arg(dq, "dq", hq),
+                        *self._arg(dk, "dk", hk), *self._arg(dv, "dv", hk), scratch.data_ptr(), scratch.numel())
+        if st != 0:
+            raise SkipFFNError(st, "skipffn_attention_backward")
         return dq, dk, dv
 
     def poll(self):
