@@ -15,7 +15,7 @@ struct skipffn_attention {
     int64_t N;
     int32_t group, tokens;               // query heads per kv head, tokens of a row tile
     int32_t n_fwd, n_rows, n_keys;       // entries of the work lists
-    int32_t row_tiles;                   // row tiles of all sequences (n_rows)
+    int32_t max_len;                     // of the longest sequence
     int32_t *status;                     // device: status block, then the lists
     const int4 *fwd_items, *row_items, *key_items;
 };
@@ -85,7 +85,7 @@ void fill_args(const skipffn_attention *h, AttnArgs *a)
     *a = AttnArgs{};
     a->fwd_items = h->fwd_items; a->row_items = h->row_items; a->key_items = h->key_items;
     a->n_fwd = h->n_fwd; a->n_rows = h->n_rows; a->n_keys = h->n_keys;
-    a->N = h->N;
+    a->N = h->N; a->max_len = h->max_len;
     a->hq = h->cfg.heads_q; a->hk = h->cfg.heads_kv; a->group = h->group; a->tokens = h->tokens;
     a->d = h->cfg.head_dim; a->causal = h->cfg.causal; a->scale = h->cfg.scale;
     a->status = h->status;
@@ -121,6 +121,8 @@ skipffn_status skipffn_attention_create(skipffn_attention **out, const skipffn_a
     h->group = cfg->heads_q / cfg->heads_kv;
     h->tokens = tile_rows(cfg) / h->group;
     h->n_fwd = (int32_t)n.fwd; h->n_rows = (int32_t)n.rows; h->n_keys = (int32_t)n.keys;
+    h->max_len = 0;
+    for (int32_t i = 0; i < n_seq; ++i) h->max_len = std::max(h->max_len, cu_seqlens[i + 1] - cu_seqlens[i]);
     h->status = (int32_t *)plan;
     int4 *lists = (int4 *)((char *)plan + ST_WORDS * 4);
     h->fwd_items = lists; h->row_items = lists + n.fwd; h->key_items = lists + n.fwd + n.rows;

@@ -19,6 +19,7 @@ struct AttnArgs {
     const int4 *fwd_items, *row_items, *key_items;
     int32_t n_fwd, n_rows, n_keys;   // entries of the three lists
     int64_t N;                       // tokens of all sequences
+    int32_t max_len;                 // of the longest sequence
     int32_t hq, hk, group, tokens, d, causal;
     float scale;
     float2 *row_stats;               // scratch: [row tile][kv head][rows of a tile] (lse log2 e, delta)

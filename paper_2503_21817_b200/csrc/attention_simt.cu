@@ -1,8 +1,12 @@
 // Packed attention with plain fused multiply-adds (fp32, and bf16 as an on-device second opinion), and
 // the row statistics of the backward pass of both paths.
+#include <cooperative_groups.h>
+
 #include "attention.cuh"
 
 namespace skipffn {
+
+namespace cg = cooperative_groups;
 
 namespace {
 
@@ -17,10 +21,10 @@ struct Tile { int ty, tx; };
 __device__ __forceinline__ Tile tile_of() { return {(int)threadIdx.x / 16, (int)threadIdx.x % 16}; }
 
 struct Item { int start, len, t0, base, h; };
-__device__ __forceinline__ Item item_of(const int4 *items, int hk)
+__device__ __forceinline__ Item item_of(const int4 *items, int hk, int block)
 {
-    const int4 e = items[blockIdx.x / hk];
-    return {e.x, e.y, e.z, e.w, (int)(blockIdx.x % hk)};
+    const int4 e = items[block / hk];
+    return {e.x, e.y, e.z, e.w, block % hk};
 }
 
 // 64 rows of a [tokens, heads, d] array as fp32: tile row r is token `token` + r / group, head h group + r % group;
@@ -54,33 +58,69 @@ __device__ __forceinline__ void rows_rows(float (&s)[4][4], const float *a, cons
                 for (int e = 0; e < 4; ++e) s[i][j] = fmaf(x[i][e], y[j][e], s[i][j]);
     }
 }
-// acc[4 rows][8 columns] += w(row, k) b[k][columns]; TR: w is stored [k][row], else [row][k]
-template <bool TR>
-__device__ __forceinline__ void weights_rows(float (&acc)[4][8], const float *w, const float *b, int n, Tile t)
+// acc[4 rows][4 NC columns] += w(row, k) b[k][columns], k < n; TR: w is stored [k][row], else [row][k].
+// NC = 1 serves heads of up to 64 columns, 2 up to 128.
+template <bool TR, int NC>
+__device__ __forceinline__ void weights_rows(float (&acc)[4][4 * NC], const float *w, const float *b, int n, Tile t)
 {
+#pragma unroll 2
     for (int k = 0; k < n; ++k) {
-        float x[4], y[2][4];
+        float x[4], y[NC][4];
         if (TR) load4(w + k * PPITCH + 4 * t.ty, x);
         else
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] = w[(4 * t.ty + i) * PPITCH + k];
-        load4(b + k * PITCH + 4 * t.tx, y[0]);
-        load4(b + k * PITCH + 64 + 4 * t.tx, y[1]);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) load4(b + k * PITCH + 64 * c + 4 * t.tx, y[c]);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(x[i], y[j / 4][j % 4], acc[i][j]);
+            for (int j = 0; j < 4 * NC; ++j) acc[i][j] = fmaf(x[i], y[j / 4][j % 4], acc[i][j]);
     }
 }
-template <typename T>
-__device__ __forceinline__ void store_acc(T *row, const float (&v)[8], float f, int d, Tile t)
+template <typename T, int NC>
+__device__ __forceinline__ void store_acc(T *row, const float (&v)[4 * NC], float f, int d, Tile t)
 {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NC; ++j)
         if (64 * j + 4 * t.tx < d) {
             const float o[4] = {v[4 * j] * f, v[4 * j + 1] * f, v[4 * j + 2] * f, v[4 * j + 3] * f};
             store4(row + 64 * j + 4 * t.tx, o);
         }
+}
+// The CTAs of a cluster share one item, each with every size-th step of its sum; this adds the accumulators of all
+// ranks, in order, into every rank's own (through `buf`, 64 rows of shared memory per CTA that nothing else uses now).
+template <int NC>
+__device__ __forceinline__ void cluster_add(cg::cluster_group cl, float (&acc)[4][4 * NC], float *buf, Tile t)
+{
+    const int size = (int)cl.num_blocks();
+    if (size == 1) return;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            const float o[4] = {acc[i][4 * j], acc[i][4 * j + 1], acc[i][4 * j + 2], acc[i][4 * j + 3]};
+            store4(buf + (4 * t.ty + i) * PITCH + 64 * j + 4 * t.tx, o);
+        }
+    cl.sync();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4 * NC; ++j) acc[i][j] = 0.0f;
+    for (int r = 0; r < size; ++r) {
+        const float *src = cl.map_shared_rank(buf, r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+                float v[4];
+                load4(src + (4 * t.ty + i) * PITCH + 64 * j + 4 * t.tx, v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][4 * j + e] += v[e];
+            }
+    }
+    cl.sync();                               // nobody overwrites or leaves with a buffer that is still read
 }
 __device__ __forceinline__ float half_warp_max(float v)
 {
@@ -95,18 +135,18 @@ __device__ __forceinline__ float half_warp_sum(float v)
     return v;
 }
 
-template <typename T>
+template <typename T, int NC>
 __global__ void __launch_bounds__(ST_THREADS)
 k_attention_fwd_simt(const AttnArgs a)
 {
     extern __shared__ float sm[];
     float *qs = sm, *kv = qs + SR * PITCH, *ps = kv + SK * PITCH;
     const Tile t = tile_of();
-    const Item it = item_of(a.fwd_items, a.hk);
+    const Item it = item_of(a.fwd_items, a.hk, blockIdx.x);
     const int valid = min(a.tokens, it.len - it.t0) * a.group;
     const int end = a.causal ? min(it.t0 + a.tokens, it.len) : it.len;
     load_rows(qs, (const T *)a.q, a.ldq, (int64_t)it.start + it.t0, it.h * a.group, a.group, valid, a.d);
-    float m[4], l[4] = {0.0f, 0.0f, 0.0f, 0.0f}, acc[4][8] = {};
+    float m[4], l[4] = {0.0f, 0.0f, 0.0f, 0.0f}, acc[4][4 * NC] = {};
     int row_end[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -138,12 +178,12 @@ k_attention_fwd_simt(const AttnArgs a)
             l[i] = l[i] * f + half_warp_sum(sum);
             m[i] = mn;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[i][j] *= f;
+            for (int j = 0; j < 4 * NC; ++j) acc[i][j] *= f;
         }
         __syncthreads();
         load_rows(kv, (const T *)a.v, a.ldv, (int64_t)it.start + k0, it.h, 1, min(SK, it.len - k0), a.d);
         __syncthreads();
-        weights_rows<false>(acc, ps, kv, min(SK, end - k0), t);
+        weights_rows<false, NC>(acc, ps, kv, min(SK, end - k0), t);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -151,7 +191,7 @@ k_attention_fwd_simt(const AttnArgs a)
         if (r >= valid) continue;
         const int64_t tok = (int64_t)it.start + it.t0 + r / a.group;
         const int head = it.h * a.group + r % a.group;
-        store_acc((T *)a.out + tok * a.ldo + (int64_t)head * a.d, acc[i], 1.0f / l[i], a.d, t);
+        store_acc<T, NC>((T *)a.out + tok * a.ldo + (int64_t)head * a.d, acc[i], 1.0f / l[i], a.d, t);
         if (t.tx == 0) a.lse[tok * a.hq + head] = m[i] + logf(l[i]);
     }
 }
@@ -179,19 +219,23 @@ __device__ __forceinline__ void grad_tile(float *ps, float *ds, const float *qs,
     }
 }
 
-template <typename T>
+// dK, dV of 64 keys by a cluster (see cluster_add): with one CTA per key tile a few short sequences would keep most
+// of the GPU idle.
+template <typename T, int NC>
 __global__ void __launch_bounds__(ST_THREADS)
 k_attention_bwd_kv_simt(const AttnArgs a)
 {
     extern __shared__ float sm[];
     float *ks = sm, *vs = ks + SK * PITCH, *qs = vs + SK * PITCH, *gs = qs + SR * PITCH, *ps = gs + SR * PITCH, *ds = ps + SR * PPITCH;
     const Tile t = tile_of();
-    const Item it = item_of(a.key_items, a.hk);
+    cg::cluster_group cl = cg::this_cluster();
+    const int rank = (int)cl.block_rank(), size = (int)cl.num_blocks();
+    const Item it = item_of(a.key_items, a.hk, blockIdx.x / size);
     const int k0 = it.t0, keys = min(SK, it.len - k0);
     load_rows(ks, (const T *)a.k, a.ldk, (int64_t)it.start + k0, it.h, 1, keys, a.d);
     load_rows(vs, (const T *)a.v, a.ldv, (int64_t)it.start + k0, it.h, 1, keys, a.d);
-    float dk[4][8] = {}, dv[4][8] = {};
-    for (int tile = a.causal ? k0 / a.tokens : 0; tile * a.tokens < it.len; ++tile) {
+    float dk[4][4 * NC] = {}, dv[4][4 * NC] = {};
+    for (int tile = (a.causal ? k0 / a.tokens : 0) + rank; tile * a.tokens < it.len; tile += size) {
         const int t0 = tile * a.tokens, valid = min(a.tokens, it.len - t0) * a.group;
         __syncthreads();
         load_rows(qs, (const T *)a.q, a.ldq, (int64_t)it.start + t0, it.h * a.group, a.group, valid, a.d);
@@ -199,33 +243,38 @@ k_attention_bwd_kv_simt(const AttnArgs a)
         __syncthreads();
         grad_tile(ps, ds, qs, gs, ks, vs, a.row_stats + ((int64_t)(it.base + tile) * a.hk + it.h) * SR, a, t0, it.len, k0, t);
         __syncthreads();
-        weights_rows<true>(dv, ps, gs, valid, t);
-        weights_rows<true>(dk, ds, qs, valid, t);
+        weights_rows<true, NC>(dv, ps, gs, valid, t);
+        weights_rows<true, NC>(dk, ds, qs, valid, t);
     }
+    cluster_add<NC>(cl, dv, gs, t);
+    cluster_add<NC>(cl, dk, qs, t);
+    if (rank != 0) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int key = 4 * t.ty + i;
         if (key >= keys) continue;
         const int64_t tok = (int64_t)it.start + k0 + key;
-        store_acc((T *)a.dk + tok * a.lddk + (int64_t)it.h * a.d, dk[i], a.scale, a.d, t);
-        store_acc((T *)a.dv + tok * a.lddv + (int64_t)it.h * a.d, dv[i], 1.0f, a.d, t);
+        store_acc<T, NC>((T *)a.dk + tok * a.lddk + (int64_t)it.h * a.d, dk[i], a.scale, a.d, t);
+        store_acc<T, NC>((T *)a.dv + tok * a.lddv + (int64_t)it.h * a.d, dv[i], 1.0f, a.d, t);
     }
 }
 
-template <typename T>
+template <typename T, int NC>
 __global__ void __launch_bounds__(ST_THREADS)
 k_attention_bwd_q_simt(const AttnArgs a)
 {
     extern __shared__ float sm[];
     float *ks = sm, *vs = ks + SK * PITCH, *qs = vs + SK * PITCH, *gs = qs + SR * PITCH, *ps = gs + SR * PITCH, *ds = ps + SR * PPITCH;
     const Tile t = tile_of();
-    const Item it = item_of(a.row_items, a.hk);
+    cg::cluster_group cl = cg::this_cluster();
+    const int rank = (int)cl.block_rank(), size = (int)cl.num_blocks();
+    const Item it = item_of(a.row_items, a.hk, blockIdx.x / size);
     const int valid = min(a.tokens, it.len - it.t0) * a.group, end = a.causal ? min(it.t0 + a.tokens, it.len) : it.len;
     load_rows(qs, (const T *)a.q, a.ldq, (int64_t)it.start + it.t0, it.h * a.group, a.group, valid, a.d);
     load_rows(gs, (const T *)a.dout, a.lddo, (int64_t)it.start + it.t0, it.h * a.group, a.group, valid, a.d);
     const float2 *stats = a.row_stats + ((int64_t)(it.base + it.t0 / a.tokens) * a.hk + it.h) * SR;
-    float dq[4][8] = {};
-    for (int k0 = 0; k0 < end; k0 += SK) {
+    float dq[4][4 * NC] = {};
+    for (int k0 = rank * SK; k0 < end; k0 += size * SK) {
         const int keys = min(SK, it.len - k0);
         __syncthreads();
         load_rows(ks, (const T *)a.k, a.ldk, (int64_t)it.start + k0, it.h, 1, keys, a.d);
@@ -233,14 +282,16 @@ k_attention_bwd_q_simt(const AttnArgs a)
         __syncthreads();
         grad_tile(ps, ds, qs, gs, ks, vs, stats, a, it.t0, it.len, k0, t);
         __syncthreads();
-        weights_rows<false>(dq, ds, ks, keys, t);
+        weights_rows<false, NC>(dq, ds, ks, keys, t);
     }
+    cluster_add<NC>(cl, dq, ks, t);
+    if (rank != 0) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = 4 * t.ty + i;
         if (r >= valid) continue;
         const int64_t tok = (int64_t)it.start + it.t0 + r / a.group;
-        store_acc((T *)a.dq + tok * a.lddq + (int64_t)(it.h * a.group + r % a.group) * a.d, dq[i], a.scale, a.d, t);
+        store_acc<T, NC>((T *)a.dq + tok * a.lddq + (int64_t)(it.h * a.group + r % a.group) * a.d, dq[i], a.scale, a.d, t);
     }
 }
 
@@ -254,7 +305,7 @@ k_attention_row_stats(const AttnArgs a)
     constexpr int LANES = 128 * (int)sizeof(T) / 16, EL = 16 / (int)sizeof(T), STEP = ST_THREADS / LANES, N = ROWS / STEP;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const Item it = item_of(a.row_items, a.hk);
+    const Item it = item_of(a.row_items, a.hk, blockIdx.x);
     const int valid = min(a.tokens, it.len - it.t0) * a.group;
     float2 *dst = a.row_stats + ((int64_t)(it.base + it.t0 / a.tokens) * a.hk + it.h) * ROWS;
     const int first = threadIdx.x / LANES, lane = threadIdx.x % LANES;
@@ -294,22 +345,35 @@ k_attention_row_stats(const AttnArgs a)
 constexpr int FWD_SMEM = (SR * PITCH + SK * PITCH + SR * PPITCH) * 4;
 constexpr int BWD_SMEM = (2 * SR * PITCH + 2 * SK * PITCH + 2 * SR * PPITCH) * 4;
 
+// n items, each by a cluster of 1, 2, 4 or 8 CTAs: as many as keep the grid within two waves of 148, and no more than
+// the longest item has steps
 template <typename Kernel>
-static cudaError_t launch(Kernel kern, int n, int smem, const AttnArgs &a, cudaStream_t s)
+static cudaError_t launch(Kernel kern, int n, int steps, int smem, const AttnArgs &a, cudaStream_t s)
 {
     if (n <= 0) return cudaSuccess;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    kern<<<(unsigned)n, ST_THREADS, smem, s>>>(a);
-    return cudaGetLastError();
+    int size = 1;
+    while (size < 8 && 2 * size <= steps && (int64_t)n * 2 * size <= 296) size *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)n * size); cfg.blockDim = dim3(ST_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = size; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    cfg.attrs = at; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
 }  // namespace
 
+template <typename T> static cudaError_t forward_t(const AttnArgs &a, cudaStream_t s)
+{
+    return a.d <= 64 ? launch(k_attention_fwd_simt<T, 1>, a.n_fwd * a.hk, 1, FWD_SMEM, a, s)
+                     : launch(k_attention_fwd_simt<T, 2>, a.n_fwd * a.hk, 1, FWD_SMEM, a, s);
+}
 cudaError_t launch_attention_simt_forward(const AttnArgs &a, int dtype, cudaStream_t s)
 {
-    return dtype == SKIPFFN_BF16 ? launch(k_attention_fwd_simt<bf16>, a.n_fwd * a.hk, FWD_SMEM, a, s)
-                                 : launch(k_attention_fwd_simt<float>, a.n_fwd * a.hk, FWD_SMEM, a, s);
+    return dtype == SKIPFFN_BF16 ? forward_t<bf16>(a, s) : forward_t<float>(a, s);
 }
 
 template <typename T, int ROWS> static cudaError_t row_stats(const AttnArgs &a, cudaStream_t s)
@@ -319,16 +383,20 @@ template <typename T, int ROWS> static cudaError_t row_stats(const AttnArgs &a, 
 }
 cudaError_t launch_attention_row_stats_tc(const AttnArgs &a, cudaStream_t s) { return row_stats<bf16, AT_TC_ROWS>(a, s); }
 
+template <typename T> static cudaError_t backward_t(const AttnArgs &a, cudaStream_t s)
+{
+    cudaError_t e = row_stats<T, SR>(a, s);
+    if (e != cudaSuccess) return e;
+    const int row_steps = (a.max_len + a.tokens - 1) / a.tokens, key_steps = (a.max_len + SK - 1) / SK;
+    e = a.d <= 64 ? launch(k_attention_bwd_kv_simt<T, 1>, a.n_keys * a.hk, row_steps, BWD_SMEM, a, s)
+                  : launch(k_attention_bwd_kv_simt<T, 2>, a.n_keys * a.hk, row_steps, BWD_SMEM, a, s);
+    if (e != cudaSuccess) return e;
+    return a.d <= 64 ? launch(k_attention_bwd_q_simt<T, 1>, a.n_rows * a.hk, key_steps, BWD_SMEM, a, s)
+                     : launch(k_attention_bwd_q_simt<T, 2>, a.n_rows * a.hk, key_steps, BWD_SMEM, a, s);
+}
 cudaError_t launch_attention_simt_backward(const AttnArgs &a, int dtype, cudaStream_t s)
 {
-    const bool b = dtype == SKIPFFN_BF16;
-    cudaError_t e = b ? row_stats<bf16, SR>(a, s) : row_stats<float, SR>(a, s);
-    if (e != cudaSuccess) return e;
-    e = b ? launch(k_attention_bwd_kv_simt<bf16>, a.n_keys * a.hk, BWD_SMEM, a, s)
-          : launch(k_attention_bwd_kv_simt<float>, a.n_keys * a.hk, BWD_SMEM, a, s);
-    if (e != cudaSuccess) return e;
-    return b ? launch(k_attention_bwd_q_simt<bf16>, a.n_rows * a.hk, BWD_SMEM, a, s)
-             : launch(k_attention_bwd_q_simt<float>, a.n_rows * a.hk, BWD_SMEM, a, s);
+    return dtype == SKIPFFN_BF16 ? backward_t<bf16>(a, s) : backward_t<float>(a, s);
 }
 
 }  // namespace skipffn
