@@ -297,48 +297,56 @@ k_attention_bwd_q_simt(const AttnArgs a)
 
 // (lse log2 e, delta = sum_d dout out) of every row of a row tile; rows that belong to no token get (infinity, 0),
 // which makes their P and dS zero.  Reads out and dout once: HBM-bound.  A row of at most 128 columns is 16 (bf16)
-// or 32 (fp32) lanes x 16 bytes; all loads of a lane's rows are in flight before the first is used.
+// or 32 (fp32) lanes x 16 bytes; the loads of four rows of a lane are in flight at a time, with few enough registers
+// for eight CTAs on an SM.
 template <typename T, int ROWS>
-__global__ void __launch_bounds__(ST_THREADS)
+__global__ void __launch_bounds__(ST_THREADS, 5)
 k_attention_row_stats(const AttnArgs a)
 {
     constexpr int LANES = 128 * (int)sizeof(T) / 16, EL = 16 / (int)sizeof(T), STEP = ST_THREADS / LANES, N = ROWS / STEP;
+    constexpr int BATCH = N < 4 ? N : 4;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const Item it = item_of(a.row_items, a.hk, blockIdx.x);
     const int valid = min(a.tokens, it.len - it.t0) * a.group;
     float2 *dst = a.row_stats + ((int64_t)(it.base + it.t0 / a.tokens) * a.hk + it.h) * ROWS;
     const int first = threadIdx.x / LANES, lane = threadIdx.x % LANES;
-    uint4 x[N], y[N];
-    float l[N];
+    const bool even = STEP % a.group == 0;       // a lane's rows then belong to one head, STEP / group tokens apart
+    const int t_first = first / a.group, h_first = first - t_first * a.group, t_step = STEP / a.group;
+#pragma unroll 1
+    for (int k0 = 0; k0 < N; k0 += BATCH) {
+        uint4 x[BATCH], y[BATCH];
+        float l[BATCH];
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        const int r = first + k * STEP;
-        x[k] = y[k] = make_uint4(0, 0, 0, 0);
-        l[k] = 0.0f;
-        if (r < valid && EL * lane < a.d) {
-            const int64_t tok = (int64_t)it.start + it.t0 + r / a.group;
-            const int head = it.h * a.group + r % a.group;
-            x[k] = *reinterpret_cast<const uint4 *>((const T *)a.out_in + tok * a.ldo + (int64_t)head * a.d + EL * lane);
-            y[k] = *reinterpret_cast<const uint4 *>((const T *)a.dout + tok * a.lddo + (int64_t)head * a.d + EL * lane);
-            if (lane == 0) l[k] = a.lse[tok * a.hq + head];
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        const int r = first + k * STEP;
-        float dot = 0.0f;
-#pragma unroll
-        for (int h = 0; h < EL / 4; ++h) {
-            float u[4], v[4];
-            load4(reinterpret_cast<const T *>(&x[k]) + 4 * h, u);
-            load4(reinterpret_cast<const T *>(&y[k]) + 4 * h, v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) dot = fmaf(u[e], v[e], dot);
+        for (int k = 0; k < BATCH; ++k) {
+            const int r = first + (k0 + k) * STEP;
+            const int t = even ? t_first + (k0 + k) * t_step : r / a.group, h = even ? h_first : r - t * a.group;
+            x[k] = y[k] = make_uint4(0, 0, 0, 0);
+            l[k] = 0.0f;
+            if (r < valid && EL * lane < a.d) {
+                const int64_t tok = (int64_t)it.start + it.t0 + t;
+                const int head = it.h * a.group + h;
+                x[k] = __ldcs(reinterpret_cast<const uint4 *>((const T *)a.out_in + tok * a.ldo + (int64_t)head * a.d + EL * lane));
+                y[k] = __ldg(reinterpret_cast<const uint4 *>((const T *)a.dout + tok * a.lddo + (int64_t)head * a.d + EL * lane));
+                if (lane == 0) l[k] = a.lse[tok * a.hq + head];
+            }
         }
 #pragma unroll
-        for (int o = LANES / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-        if (lane == 0) dst[r] = r < valid ? make_float2(l[k] * LOG2E, dot) : make_float2(INFINITY, 0.0f);
+        for (int k = 0; k < BATCH; ++k) {
+            const int r = first + (k0 + k) * STEP;
+            float dot = 0.0f;
+#pragma unroll
+            for (int h = 0; h < EL / 4; ++h) {
+                float u[4], v[4];
+                load4(reinterpret_cast<const T *>(&x[k]) + 4 * h, u);
+                load4(reinterpret_cast<const T *>(&y[k]) + 4 * h, v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dot = fmaf(u[e], v[e], dot);
+            }
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+            if (lane == 0) dst[r] = r < valid ? make_float2(l[k] * LOG2E, dot) : make_float2(INFINITY, 0.0f);
+        }
     }
 }
 
