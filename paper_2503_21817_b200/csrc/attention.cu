@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -62,22 +63,21 @@ size_t plan_bytes(const Counts &n) { return (size_t)ST_WORDS * 4 + (size_t)(n.fw
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
-// A [tokens, heads, d] array: base, token stride in elements, bytes of a token's heads
+// A [tokens, heads, d] array: base, token stride and extent of a token's heads in bytes
 struct Array { const void *p; int64_t ld; int64_t width; };
 
-bool array_ok(const Array &a, int esize)
+bool array_ok(const Array &a)
 {
-    return a.p && aligned16(a.p) && a.ld * esize % 16 == 0 && a.ld * esize >= a.width && a.ld <= (int64_t)1 << 36;
+    return a.p && aligned16(a.p) && a.ld % 16 == 0 && a.ld >= a.width && a.ld <= (int64_t)1 << 38;
 }
 // Do two arrays of N tokens share a byte?  Exact for equal strides (slices of one fused array), else by range.
-bool overlap(const Array &x, const Array &y, int64_t N, int esize)
+bool overlap(const Array &x, const Array &y, int64_t N)
 {
     const intptr_t a = (intptr_t)x.p, b = (intptr_t)y.p;
-    const int64_t sx = x.ld * esize, sy = y.ld * esize;
-    if (a >= b + (N - 1) * sy + y.width || b >= a + (N - 1) * sx + x.width) return false;
-    if (sx != sy) return true;
-    const int64_t off = ((b - a) % sx + sx) % sx;      // y's columns relative to x's inside one stride
-    return off < x.width || off + y.width > sx;
+    if (a >= b + (N - 1) * y.ld + y.width || b >= a + (N - 1) * x.ld + x.width) return false;
+    if (x.ld != y.ld) return true;
+    const int64_t off = ((b - a) % x.ld + x.ld) % x.ld;      // y's columns relative to x's inside one stride
+    return off < x.width || off + y.width > x.ld;
 }
 
 void fill_args(const skipffn_attention *h, AttnArgs *a)
@@ -179,10 +179,14 @@ skipffn_status skipffn_attention_forward(const skipffn_attention *h, const void 
     if (!h) return SKIPFFN_EINVAL;
     if (h->N == 0) return SKIPFFN_OK;
     const int es = h->cfg.dtype == SKIPFFN_BF16 ? 2 : 4;
+    for (const int64_t ld : {ldq, ldk, ldv, ldo})
+        if (ld < 0 || ld > (int64_t)1 << 36) return SKIPFFN_EINVAL;
     const int64_t wq = (int64_t)h->cfg.heads_q * h->cfg.head_dim * es, wk = (int64_t)h->cfg.heads_kv * h->cfg.head_dim * es;
-    const Array Q{q, ldq, wq}, K{k, ldk, wk}, V{v, ldv, wk}, O{out, ldo, wq};
-    if (!array_ok(Q, es) || !array_ok(K, es) || !array_ok(V, es) || !array_ok(O, es) || !lse || ((uintptr_t)lse & 3u)) return SKIPFFN_EINVAL;
-    if (overlap(O, Q, h->N, es) || overlap(O, K, h->N, es) || overlap(O, V, h->N, es)) return SKIPFFN_EINVAL;
+    const int64_t wl = (int64_t)h->cfg.heads_q * 4;
+    const Array in[3] = {{q, ldq * es, wq}, {k, ldk * es, wk}, {v, ldv * es, wk}}, O{out, ldo * es, wq}, L{lse, wl, wl};
+    if (!array_ok(O) || !lse || ((uintptr_t)lse & 3u) || overlap(O, L, h->N)) return SKIPFFN_EINVAL;
+    for (const Array &x : in)
+        if (!array_ok(x) || overlap(O, x, h->N) || overlap(L, x, h->N)) return SKIPFFN_EINVAL;
     AttnArgs a;
     fill_args(h, &a);
     a.q = q; a.k = k; a.v = v; a.out = out; a.lse = lse;
@@ -205,17 +209,19 @@ skipffn_status skipffn_attention_backward(const skipffn_attention *h, const void
     if (!h) return SKIPFFN_EINVAL;
     if (h->N == 0) return SKIPFFN_OK;
     const int es = h->cfg.dtype == SKIPFFN_BF16 ? 2 : 4;
+    for (const int64_t ld : {lddo, ldq, ldk, ldv, ldo, lddq, lddk, lddv})
+        if (ld < 0 || ld > (int64_t)1 << 36) return SKIPFFN_EINVAL;
     const int64_t wq = (int64_t)h->cfg.heads_q * h->cfg.head_dim * es, wk = (int64_t)h->cfg.heads_kv * h->cfg.head_dim * es;
-    const Array in[5] = {{q, ldq, wq}, {k, ldk, wk}, {v, ldv, wk}, {out, ldo, wq}, {dout, lddo, wq}};
-    const Array res[3] = {{dq, lddq, wq}, {dk, lddk, wk}, {dv, lddv, wk}};
+    const Array in[5] = {{q, ldq * es, wq}, {k, ldk * es, wk}, {v, ldv * es, wk}, {out, ldo * es, wq}, {dout, lddo * es, wq}};
+    const Array res[3] = {{dq, lddq * es, wq}, {dk, lddk * es, wk}, {dv, lddv * es, wk}};
     for (const Array &x : in)
-        if (!array_ok(x, es)) return SKIPFFN_EINVAL;
+        if (!array_ok(x)) return SKIPFFN_EINVAL;
     for (int i = 0; i < 3; ++i) {
-        if (!array_ok(res[i], es)) return SKIPFFN_EINVAL;
+        if (!array_ok(res[i])) return SKIPFFN_EINVAL;
         for (const Array &x : in)
-            if (overlap(res[i], x, h->N, es)) return SKIPFFN_EINVAL;
+            if (overlap(res[i], x, h->N)) return SKIPFFN_EINVAL;
         for (int j = 0; j < i; ++j)
-            if (overlap(res[i], res[j], h->N, es)) return SKIPFFN_EINVAL;
+            if (overlap(res[i], res[j], h->N)) return SKIPFFN_EINVAL;
     }
     if (!lse || ((uintptr_t)lse & 3u) || !scratch || !aligned16(scratch)) return SKIPFFN_EINVAL;
     if (scratch_bytes < skipffn_attention_scratch_bytes(h)) return SKIPFFN_EWORKSPACE;
