@@ -91,7 +91,7 @@ struct AtParams {
     int64_t ld0, ld1;                        // token strides of the outputs
     bf16 *out0, *out1;
     float *lse;
-    const float2 *row_stats;
+    float2 *row_stats;
     int32_t *status;
     int32_t wide;                            // dQ: every 16 columns of a row start on 32 bytes
 };
@@ -921,15 +921,21 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
 
 // ------------------------------------------------------------------------------------ dQ
 // One item = one row tile of one kv head against the keys of its sequence: S = Q K^T (two buffers),
-// dP = dO V^T, dS packed to bf16 over the scores, dQ += dS K.
+// dP = dO V^T, dS over the scores, dQ += dS K.
+// Two roundings would add up in dQ: dS to bf16, and the one of `out` that delta = do . out carries into every
+// dS of the row (relative errors 1.6e-3 and 1.0e-3, next to 1.7e-3 of dQ's own rounding).  So dS enters the
+// product as the sum of two bf16 numbers (eight more MMAs a block), which leaves the second.  The first is left in
+// dK, whose kernel runs after this one, and the second is taken out there: the exact delta makes every row of
+// dS sum to zero, so the row sums found here are added to delta.
 template <int DP> struct QShape {
     static constexpr int T_BYTES = tile_bytes<DP>();
     static constexpr int KS = 3, VS = 2;
-    static constexpr int SMEM = (2 + KS + VS) * T_BYTES + 512;
+    static constexpr int SUM_BYTES = 4 * TILE * 4;    // row sums of dS: [part][row]
+    static constexpr int SMEM = (2 + KS + VS) * T_BYTES + SUM_BYTES + 512;
 };
 struct alignas(8) QCtl {
     uint64_t q_full, q_empty, g_full, g_empty, k_full[3], k_empty[3], k_tail[3], v_full[2], v_empty[2];
-    uint64_t s_full[2], g_scores, ds_ready, acc_full, acc_free;
+    uint64_t s_full[2], g_scores, ds_ready, acc_full, acc_free, sum_ready, sum_read;
     uint32_t tmem_base;
     volatile int abort_flag;
 };
@@ -954,7 +960,8 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
     extern __shared__ __align__(1024) uint8_t smem_raw[];      // tiles need 1024 bytes
     const uint32_t tiles = smem_u32(smem_raw);
     const uint32_t q_tile = tiles, g_tile = tiles + T_BYTES, k_ring = tiles + 2 * T_BYTES, v_ring = k_ring + KS * T_BYTES;
-    QCtl *ctl = reinterpret_cast<QCtl *>(smem_raw + (2 + KS + VS) * T_BYTES);
+    const uint32_t sums = v_ring + VS * T_BYTES;
+    QCtl *ctl = reinterpret_cast<QCtl *>(smem_raw + (2 + KS + VS) * T_BYTES + Sh::SUM_BYTES);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&ctl->q_full), 1);
@@ -974,6 +981,8 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
         mbar_init(smem_u32(&ctl->s_full[1]), 1);
         mbar_init(smem_u32(&ctl->g_scores), 1);
         mbar_init(smem_u32(&ctl->ds_ready), BwdWarps::COUNT);
+        mbar_init(smem_u32(&ctl->sum_ready), BwdWarps::COUNT);
+        mbar_init(smem_u32(&ctl->sum_read), 4);
         mbar_init(smem_u32(&ctl->acc_full), 1);
         mbar_init(smem_u32(&ctl->acc_free), BwdWarps::COUNT);
         ctl->abort_flag = 0;
@@ -1084,6 +1093,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 tc_fence_after();
                 const uint32_t ds = tmem + (cnt & 1) * TILE;
                 mma_tmem_rows<DP, 0, 8, 2>(on, t_dq, ds, k_across + (cnt % KS) * (T_BYTES >> 4), cols_of(j) / 16, j > 0);
+                mma_tmem_rows<DP, 0, 8, 2>(on, t_dq, ds + 16, k_across + (cnt % KS) * (T_BYTES >> 4), cols_of(j) / 16, 1);
                 umma_commit_if(on, smem_u32(&ctl->k_empty[cnt % KS]));
                 if (j + 2 < it.nb) scores(j + 2, cnt + 2);
             }
@@ -1100,7 +1110,9 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
         Feed<QItem, true> feed(p);
         QItem it;
         for (; ok && feed.take(it); ++items) {
-            const float2 st = p.row_stats[((int64_t)it.tile * p.hk + it.h) * TILE + row];
+            float2 *stats = p.row_stats + ((int64_t)it.tile * p.hk + it.h) * TILE + row;
+            const float2 st = *stats;
+            float sum = 0.0f;                // of this part's dS
             const int token = it.t0 + row_t, row_end = p.causal ? min(token + 1, it.len) : it.len;
             for (int j = 0; j < it.nb; ++j, ++cnt) {
                 const int cols = mma_cols(it.end - j * TILE);
@@ -1112,7 +1124,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 tc_fence_after();
                 if (c0 < cols) {
                     const uint32_t t_s = tmem + lanes + (cnt & 1) * TILE + c0;
-                    uint32_t r[32], dp[32], pk[16];
+                    uint32_t r[32], dp[32], hi[16], lo[16];
                     tmem_ld32(t_s, r);
                     tmem_ld32(t_dp + lanes + c0, dp);
                     tmem_ld_wait(r);
@@ -1125,9 +1137,12 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                             a = e < limit ? a : 0.0f;
                             b = e + 1 < limit ? b : 0.0f;
                         }
-                        pk[e / 2] = pack_bf16(a, b);
+                        sum += a + b;
+                        hi[e / 2] = pack_bf16(a, b);
+                        lo[e / 2] = pack_bf16(a - __uint_as_float(hi[e / 2] << 16), b - __uint_as_float(hi[e / 2] & 0xffff0000u));
                     }
-                    tmem_st16(t_s, pk);
+                    tmem_st16(t_s, hi);
+                    tmem_st16(t_s + 16, lo);
                     tmem_st_wait();
                 }
                 tc_fence_before();
@@ -1139,6 +1154,22 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
             if (!ok) break;
             tc_fence_after();
             const bool live = row < used && token < it.len;
+            // the parts' sums meet; part 0 puts the row's delta right for the kernel of dK and dV
+            ok = wait_bar<true>(smem_u32(&ctl->sum_read), (items & 1) ^ 1, ab, p.status, SITE_EPI_EXCHANGE);
+            if (!ok) break;
+            asm volatile("st.shared.f32 [%0], %1;" ::"r"(sums + (part * TILE + row) * 4), "f"(sum) : "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctl->sum_ready));
+            if (part == 0) {
+                ok = wait_bar<true>(smem_u32(&ctl->sum_ready), items & 1, ab, p.status, SITE_EPI_EXCHANGE);
+                if (!ok) break;
+                float s4[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s4[k]) : "r"(sums + (k * TILE + row) * 4) : "memory");
+                if (live) stats->y = st.y + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&ctl->sum_read));
+            }
             if (c0 < DP) {
                 uint32_t o[32];
                 tmem_ld32(t_dq + lanes + c0, o);
@@ -1240,14 +1271,14 @@ template <int DP> static cudaError_t backward_dp(const AttnArgs &a, cudaStream_t
         return cudaErrorInvalidValue;
     cudaError_t e = launch_attention_row_stats_tc(a, s);
     if (e != cudaSuccess) return e;
-    AtParams p = params_of(a, a.key_items, a.n_keys);
-    p.out0 = (bf16 *)a.dk; p.ld0 = a.lddk; p.out1 = (bf16 *)a.dv; p.ld1 = a.lddv;
-    e = launch_at(k_attention_bwd_kv<DP>, BwdWarps::THREADS, sms_kv, KvShape<DP>::SMEM, tm, p, s);
-    if (e != cudaSuccess) return e;
-    p = params_of(a, a.row_items, a.n_rows);
+    AtParams p = params_of(a, a.row_items, a.n_rows);
     p.out0 = (bf16 *)a.dq; p.ld0 = a.lddq;
     p.wide = ((uintptr_t)a.dq & 31u) == 0 && a.lddq % 16 == 0 && a.d % 16 == 0;
-    return launch_at(k_attention_bwd_q<DP>, BwdWarps::THREADS, sms_q, QShape<DP>::SMEM, tm, p, s);
+    e = launch_at(k_attention_bwd_q<DP>, BwdWarps::THREADS, sms_q, QShape<DP>::SMEM, tm, p, s);
+    if (e != cudaSuccess) return e;
+    p = params_of(a, a.key_items, a.n_keys);
+    p.out0 = (bf16 *)a.dk; p.ld0 = a.lddk; p.out1 = (bf16 *)a.dv; p.ld1 = a.lddv;
+    return launch_at(k_attention_bwd_kv<DP>, BwdWarps::THREADS, sms_kv, KvShape<DP>::SMEM, tm, p, s);
 }
 
 cudaError_t launch_attention_tc_forward(const AttnArgs &a, cudaStream_t s)
