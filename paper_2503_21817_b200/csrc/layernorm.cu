@@ -6,6 +6,9 @@
 // HBM-bound: a row is read once into registers (16-byte loads, at most four per thread), the variance is
 // the mean of squared deviations (a second look at the registers, not E[x^2] - mean^2), and the backward
 // reads x and dy once for both its results.  Statistics and sums are fp32 in a fixed order (no atomics).
+// Measured (B200, bf16): forward 9376 x 4096 in 26.5 us (5.8 TB/s, 0.89 of the copy rate), 577 x 1024 in 3 us;
+// backward 4927 x 5120 in 43 us (3.5 TB/s; rows 37, partial sums 6): bound by the instructions of a row
+// (about 20 per column and thread) and its barrier, with two rows at a time on an SM.
 #include "common.cuh"
 
 namespace skipffn {
