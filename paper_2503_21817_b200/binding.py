@@ -359,7 +359,8 @@ class PackedAttention:
     the last sequence are neither read nor written), contiguous heads and any token stride that is a multiple of
     16 bytes, so slices of one fused projection need no copy.  ``causal=False`` attends to the whole
     sequence; ``scale`` defaults to ``head_dim ** -0.5``.  Work is enqueued on the current torch stream;
-    one object may serve several streams."""
+    one object may serve several streams.  A captured call reads the object's work lists at every replay: keep the
+    object as long as the graph."""
 
     def __init__(self, cu_seqlens, heads_q: int, heads_kv: int, head_dim: int, dtype: int = BF16, causal: bool = True,
                  scale: Optional[float] = None, path: int = PATH_DEFAULT, device="cuda"):
@@ -391,6 +392,7 @@ class PackedAttention:
         if st != 0:
             raise SkipFFNError(st, "skipffn_attention_create")
         self.scratch_bytes = int(self.lib.skipffn_attention_scratch_bytes(self._handle))
+        self._made_on = torch._C._cuda_getCurrentRawStream(self._index)
 
     def __del__(self):
         handle, self._handle = getattr(self, "_handle", None), None
@@ -399,6 +401,11 @@ class PackedAttention:
 
     def _stream(self):
         return self._torch.cuda.current_stream(self.device).cuda_stream
+
+    def _on_this_stream(self):
+        """The work lists are read by calls on any stream: their memory must outlive those calls too."""
+        if self._torch._C._cuda_getCurrentRawStream(self._index) != self._made_on and not self._torch.cuda.is_current_stream_capturing():
+            self._plan.record_stream(self._torch.cuda.current_stream(self.device))
 
     def _arg(self, t, name, heads):
         """(address, token stride) of a [tokens, heads, head_dim] tensor, checked."""
@@ -422,6 +429,7 @@ class PackedAttention:
             lse = q.new_empty(q.shape[:2], dtype=self._torch.float32)
         else:
             self._check_lse(lse)
+        self._on_this_stream()
         st = _on_device(self._forward, self._index, self._handle, *args, *self._arg(out, "out", hq), lse.data_ptr())
         if st != 0:
             raise SkipFFNError(st, "skipffn_attention_forward")
@@ -443,6 +451,7 @@ class PackedAttention:
         dk = k.new_empty(k.shape) if dk is None else dk
         dv = v.new_empty(v.shape) if dv is None else dv
         scratch = q.new_empty(max(self.scratch_bytes, 16), dtype=self._torch.uint8)
+        self._on_this_stream()
         st = _on_device(self._backward, self._index, self._handle, *args, lse.data_ptr(), *self._arg(dq, "dq", hq),
                         *self._arg(dk, "dk", hk), *self._arg(dv, "dv", hk), scratch.data_ptr(), scratch.numel())
         if st != 0:

@@ -66,9 +66,10 @@ bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 // A [tokens, heads, d] array: base, token stride and extent of a token's heads in bytes
 struct Array { const void *p; int64_t ld; int64_t width; };
 
-bool array_ok(const Array &a)
+// strides are bounded by what a tensor map takes and so that N of them stay within 64 bits
+bool array_ok(const Array &a, int64_t N)
 {
-    return a.p && aligned16(a.p) && a.ld % 16 == 0 && a.ld >= a.width && a.ld <= (int64_t)1 << 38;
+    return a.p && aligned16(a.p) && a.ld % 16 == 0 && a.ld >= a.width && a.ld <= (int64_t)1 << 38 && a.ld <= ((int64_t)1 << 60) / N;
 }
 // Do two arrays of N tokens share a byte?  Exact for equal strides (slices of one fused array), else by range.
 bool overlap(const Array &x, const Array &y, int64_t N)
@@ -184,9 +185,9 @@ skipffn_status skipffn_attention_forward(const skipffn_attention *h, const void 
     const int64_t wq = (int64_t)h->cfg.heads_q * h->cfg.head_dim * es, wk = (int64_t)h->cfg.heads_kv * h->cfg.head_dim * es;
     const int64_t wl = (int64_t)h->cfg.heads_q * 4;
     const Array in[3] = {{q, ldq * es, wq}, {k, ldk * es, wk}, {v, ldv * es, wk}}, O{out, ldo * es, wq}, L{lse, wl, wl};
-    if (!array_ok(O) || !lse || ((uintptr_t)lse & 3u) || overlap(O, L, h->N)) return SKIPFFN_EINVAL;
+    if (!array_ok(O, h->N) || !lse || ((uintptr_t)lse & 3u) || overlap(O, L, h->N)) return SKIPFFN_EINVAL;
     for (const Array &x : in)
-        if (!array_ok(x) || overlap(O, x, h->N) || overlap(L, x, h->N)) return SKIPFFN_EINVAL;
+        if (!array_ok(x, h->N) || overlap(O, x, h->N) || overlap(L, x, h->N)) return SKIPFFN_EINVAL;
     AttnArgs a;
     fill_args(h, &a);
     a.q = q; a.k = k; a.v = v; a.out = out; a.lse = lse;
@@ -215,9 +216,9 @@ skipffn_status skipffn_attention_backward(const skipffn_attention *h, const void
     const Array in[5] = {{q, ldq * es, wq}, {k, ldk * es, wk}, {v, ldv * es, wk}, {out, ldo * es, wq}, {dout, lddo * es, wq}};
     const Array res[3] = {{dq, lddq * es, wq}, {dk, lddk * es, wk}, {dv, lddv * es, wk}};
     for (const Array &x : in)
-        if (!array_ok(x)) return SKIPFFN_EINVAL;
+        if (!array_ok(x, h->N)) return SKIPFFN_EINVAL;
     for (int i = 0; i < 3; ++i) {
-        if (!array_ok(res[i])) return SKIPFFN_EINVAL;
+        if (!array_ok(res[i], h->N)) return SKIPFFN_EINVAL;
         for (const Array &x : in)
             if (overlap(res[i], x, h->N)) return SKIPFFN_EINVAL;
         for (int j = 0; j < i; ++j)

@@ -198,6 +198,25 @@ def test_fused_gradients_other_stream_capture_and_replay():
     a.poll()
 
 
+def test_work_lists_outlive_calls_on_another_stream():
+    # the object is dropped while a call on a side stream has not run yet: its lists may not be handed out again
+    import torch
+    q, k, v, do, cu = _tensors(14, (64,) * 40, 4, 2, 64, "bf16")
+    a = _object(cu, 4, 2, 64, "bf16")
+    want, _ = a.forward(q, k, v)
+    address, size = a._plan.data_ptr(), a._plan.numel()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)                           # about 0.1 s
+        got, _ = a.forward(q, k, v)
+    del a
+    others = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    assert all(t.data_ptr() != address for t in others)
+    side.synchronize()
+    assert torch.equal(got, want)
+
+
 def test_refusals():
     import torch
     import paper_2503_21817_b200 as sk
@@ -227,6 +246,10 @@ def test_refusals():
             sk.PackedAttention(*bad)
     with pytest.raises(ValueError):
         sk.PackedAttention([0, 1 << 31], 4, 2, 64)
+    # a stride that would leave 64 bits, and one that is no multiple of 16 bytes, at the C entry
+    f, p = a.lib.skipffn_attention_forward, (q.data_ptr(), k.data_ptr(), v.data_ptr(), torch.empty_like(q).data_ptr(), lse.data_ptr())
+    call = lambda ld: f(a._handle, p[0], ld, p[1], 128, p[2], 128, p[3], 256, torch.empty_like(lse).data_ptr(), None)
+    assert [call(ld) for ld in (1 << 62, 1 << 40, -256, 0, 252, 248)] == [1] * 6
     # an empty batch is a batch
     e = sk.PackedAttention([0, 0], 4, 2, 64)
     o, l = e.forward(q[:0], k[:0], v[:0])
