@@ -278,7 +278,8 @@ skipffn_status skipffn_token_merge_poll(void *scratch, int64_t n, int32_t C, int
  * that slices of one fused projection can be passed); bases and strides are multiples of 16 bytes
  * and a stride is at least heads x head_dim.  head_dim is a multiple of 8 up to 128 and a group
  * (heads_q / heads_kv) has at most 64 heads, else EUNSUPPORTED.  Only rows 0 .. N-1 are read or written;
- * lse is [N, heads_q] fp32, natural logarithm.  Outputs must not overlap inputs or each other (EINVAL).
+ * lse is [N, heads_q] fp32, natural logarithm.  Outputs must not overlap inputs or each other,
+ * nor the scratch any of them (EINVAL).
  * bf16: tensor-core kernels with fp32 accumulation; scores, softmax statistics and gradients of the
  * scores are fp32, P and dS are rounded to bf16 as operands of the second products, results once.
  * fp32, or path = SIMT: plain FMA.  All sums have a fixed order: equal calls give equal bits.

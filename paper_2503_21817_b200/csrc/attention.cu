@@ -225,7 +225,20 @@ skipffn_status skipffn_attention_backward(const skipffn_attention *h, const void
             if (overlap(res[i], res[j], h->N)) return SKIPFFN_EINVAL;
     }
     if (!lse || ((uintptr_t)lse & 3u) || !scratch || !aligned16(scratch)) return SKIPFFN_EINVAL;
-    if (scratch_bytes < skipffn_attention_scratch_bytes(h)) return SKIPFFN_EWORKSPACE;
+    const size_t need = skipffn_attention_scratch_bytes(h);
+    if (scratch_bytes < need) return SKIPFFN_EWORKSPACE;
+    // the row statistics are written before the arrays are read, and read while the results are written
+    const int64_t wl = (int64_t)h->cfg.heads_q * 4;
+    const Array L{lse, wl, wl};
+    auto in_scratch = [&](const Array &x) {
+        const uintptr_t s0 = (uintptr_t)scratch, x0 = (uintptr_t)x.p;
+        return x0 < s0 + need && s0 < x0 + (h->N - 1) * x.ld + x.width;
+    };
+    if (in_scratch(L)) return SKIPFFN_EINVAL;
+    for (const Array &x : in)
+        if (in_scratch(x)) return SKIPFFN_EINVAL;
+    for (const Array &x : res)
+        if (in_scratch(x) || overlap(x, L, h->N)) return SKIPFFN_EINVAL;
     AttnArgs a;
     fill_args(h, &a);
     a.q = q; a.k = k; a.v = v; a.out_in = out; a.dout = dout; a.dq = dq; a.dk = dk; a.dv = dv;

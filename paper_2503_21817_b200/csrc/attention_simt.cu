@@ -301,7 +301,7 @@ k_attention_bwd_q_simt(const AttnArgs a)
 // (lse log2 e, delta = sum_d dout out) of every row of a row tile; rows that belong to no token get (infinity, 0),
 // which makes their P and dS zero.  Reads out and dout once: HBM-bound.  A row of at most 128 columns is 16 (bf16)
 // or 32 (fp32) lanes x 16 bytes; the loads of four rows of a lane are in flight at a time, with few enough registers
-// for eight CTAs on an SM.
+// for five CTAs on an SM.
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(ST_THREADS, 5)
 k_attention_row_stats(const AttnArgs a)

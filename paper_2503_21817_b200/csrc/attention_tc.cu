@@ -71,7 +71,8 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile
     }
 }
 // The MMA warp's wait: the answer is the same in every lane and the compiler can tell (a vote), so that what
-// follows stays in uniform registers.
+// follows stays in uniform registers.  Every lane polls and the warp walks on together: a form in which one lane
+// polled for the others ended in an illegal access.
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status, int site)
 {
     if (__builtin_expect(__all_sync(0xffffffffu, mbar_test(bar, parity)), 1)) return true;

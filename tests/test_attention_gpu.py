@@ -238,6 +238,17 @@ def test_refusals():
     for kw in (dict(dq=q), dict(dk=v), dict(dv=k), dict(dk=v.clone(), dv=None, dq=out)):
         with pytest.raises(sk.SkipFFNError):
             a.backward(do, q, k, v, out, lse, **kw)
+    # results on top of the statistics, at the C entry: dq, dk, dv on lse; scratch on any of the nine arrays
+    big = torch.empty(20, 4, 64, dtype=torch.bfloat16, device="cuda")
+    rows = [do, q, k, v, out, lse, big, torch.empty_like(k), torch.empty_like(k), torch.empty(a.scratch_bytes, dtype=torch.uint8, device="cuda")]
+    def at_c(i, p):
+        p = [t.data_ptr() if j != i else p for j, t in enumerate(rows)]
+        ld = [256, 256, 128, 128, 256, None, 256, 128, 128, None]
+        flat = [x for y, z in zip(p, ld) for x in ((y,) if z is None else (y, z))]
+        return a.lib.skipffn_attention_backward(a._handle, *flat, a.scratch_bytes, None)
+    assert [at_c(i, lse.data_ptr()) for i in (6, 7, 8)] == [1] * 3
+    assert [at_c(9, t.data_ptr()) for t in rows[:9]] == [1] * 9
+    assert at_c(9, rows[9].data_ptr() + 8) == 1
     same = torch.empty_like(k)
     with pytest.raises(sk.SkipFFNError):
         a.backward(do, q, k, v, out, lse, dk=same, dv=same)
