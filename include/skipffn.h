@@ -215,7 +215,8 @@ skipffn_status skipffn_summary_backward(const void *X, const int32_t *seg_offset
  *                rstd = 1 / sqrt(var + eps), eps >= 0
  *     backward:  dx, and the column sums dgamma = sum_rows dy (x - mean) rstd, dbeta = sum_rows dy
  *   x, y, dy, dx : [n_rows, C] device, dtype = skipffn_dtype; C a multiple of 8, at most 16384
- *                  (EUNSUPPORTED); y may be x, dx may be dy or x; a partial overlap is EINVAL
+ *                  (EUNSUPPORTED); y may be x, dx may be dy or x; any other overlap with or between outputs
+ *                  and scratch is EINVAL
  *   gamma, beta  : [C] in dtype; beta may be NULL (zero)
  *   mean, rstd   : [n_rows] fp32; written by the forward (either may be NULL), read by the backward
  *   dgamma, dbeta: [C] in dtype, fp32 with dw_fp32 or when dtype is fp32; overwritten; either may be NULL

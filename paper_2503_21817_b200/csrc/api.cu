@@ -654,13 +654,32 @@ static bool same_or_apart(const void *a, const void *b, int64_t bytes)
     return p == q || p + bytes <= q || q + bytes <= p;
 }
 
+// An array of a layer-norm call; no bytes at all if p is null
+struct Bytes { const void *p; int64_t n; };
+static bool apart(const Bytes &a, const Bytes &b)
+{
+    const uintptr_t p = (uintptr_t)a.p, q = (uintptr_t)b.p;
+    return !p || !q || p + a.n <= q || q + b.n <= p;
+}
+static bool aligned(const void *p, int n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
 skipffn_status skipffn_layernorm_forward(const void *x, const void *gamma, const void *beta, int64_t n_rows, int32_t C,
                                          int32_t dtype, float eps, void *y, float *mean, float *rstd, void *stream)
 {
     if (!layernorm_args_ok(x, gamma, n_rows, C, dtype) || !(eps >= 0.0f)) return SKIPFFN_EINVAL;
     if (C % 8 || C > LN_MAX_C) return SKIPFFN_EUNSUPPORTED;
     if ((n_rows > 0 && !y) || !aligned16(y) || !aligned16(beta)) return SKIPFFN_EINVAL;
-    if (!same_or_apart(x, y, n_rows * C * (dtype == SKIPFFN_BF16 ? 2 : 4))) return SKIPFFN_EINVAL;
+    if (!aligned(mean, 4) || !aligned(rstd, 4)) return SKIPFFN_EINVAL;
+    const int64_t es = dtype == SKIPFFN_BF16 ? 2 : 4;
+    if (!same_or_apart(x, y, n_rows * C * es)) return SKIPFFN_EINVAL;
+    const Bytes in[3] = {{x, n_rows * C * es}, {gamma, C * es}, {beta, C * es}};
+    const Bytes res[3] = {{y, n_rows * C * es}, {mean, n_rows * 4}, {rstd, n_rows * 4}};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = i == 0 ? 1 : 0; j < 3; ++j)                 // y may be x
+            if (!apart(res[i], in[j])) return SKIPFFN_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (!apart(res[i], res[j])) return SKIPFFN_EINVAL;
+    }
     return launch_layernorm_forward(x, gamma, beta, n_rows, C, dtype, eps, y, mean, rstd, (cudaStream_t)stream) == cudaSuccess
                ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }
@@ -675,9 +694,18 @@ skipffn_status skipffn_layernorm_backward(const void *dy, const void *x, const v
     if (C % 8 || C > LN_MAX_C) return SKIPFFN_EUNSUPPORTED;
     if ((n_rows > 0 && (!dy || !dx || !mean || !rstd)) || !aligned16(dy) || !aligned16(dx) || !scratch || !aligned16(scratch))
         return SKIPFFN_EINVAL;
-    const int64_t bytes = n_rows * C * (dtype == SKIPFFN_BF16 ? 2 : 4);
+    const int64_t es = dtype == SKIPFFN_BF16 ? 2 : 4, gs = dw_fp32 ? 4 : es, bytes = n_rows * C * es;
+    if (!aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dgamma, (int)gs) || !aligned(dbeta, (int)gs)) return SKIPFFN_EINVAL;
     if (!same_or_apart(dx, x, bytes) || !same_or_apart(dx, dy, bytes)) return SKIPFFN_EINVAL;
     if (scratch_bytes < skipffn_layernorm_scratch_bytes(C)) return SKIPFFN_EWORKSPACE;
+    const Bytes in[5] = {{dy, bytes}, {x, bytes}, {gamma, C * es}, {mean, n_rows * 4}, {rstd, n_rows * 4}};
+    const Bytes res[4] = {{dx, bytes}, {dgamma, C * gs}, {dbeta, C * gs}, {scratch, (int64_t)skipffn_layernorm_scratch_bytes(C)}};
+    for (int i = 0; i < 4; ++i) {
+        for (int j = i == 0 ? 2 : 0; j < 5; ++j)                 // dx may be dy or x
+            if (!apart(res[i], in[j])) return SKIPFFN_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (!apart(res[i], res[j])) return SKIPFFN_EINVAL;
+    }
     return launch_layernorm_backward(dy, x, gamma, mean, rstd, n_rows, C, dtype, dx, dgamma, dbeta, dw_fp32, (float *)scratch,
                                      (cudaStream_t)stream) == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }

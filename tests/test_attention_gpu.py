@@ -198,6 +198,28 @@ def test_fused_gradients_other_stream_capture_and_replay():
     a.poll()
 
 
+@pytest.mark.parametrize("path", [0, 1])
+def test_offsets_past_32_bits(path):
+    # tokens 2^21 elements apart: the last ones lie behind 2^31 elements.  Same bits as from packed arrays.
+    import torch
+    q, k, v, do, cu = _tensors(15, (700, 400), 4, 2, 64, "bf16")
+    a = _object(cu, 4, 2, 64, "bf16", path=path)
+    out, lse = a.forward(q, k, v)
+    grads = a.backward(do, q, k, v, out, lse)
+    far = torch.empty(1100, 1 << 21, dtype=torch.bfloat16, device="cuda")
+    places = iter(range(0, 1 << 21, 256))
+    def moved(t):
+        x = next(places)
+        w = far[:, x:x + t.shape[1] * t.shape[2]].view(1100, t.shape[1], t.shape[2])
+        return w.copy_(t)
+    Q, K, V, G = (moved(t) for t in (q, k, v, do))
+    O, dQ, dK, dV = (moved(torch.zeros_like(t)) for t in (q, q, k, v))
+    O, L = a.forward(Q, K, V, out=O)
+    a.backward(G, Q, K, V, O, L, dQ, dK, dV)
+    a.poll()
+    assert torch.equal(L, lse) and all(torch.equal(x, y) for x, y in zip((O, dQ, dK, dV), (out, *grads)))
+
+
 def test_work_lists_outlive_calls_on_another_stream():
     # the object is dropped while a call on a side stream has not run yet: its lists may not be handed out again
     import torch
@@ -235,6 +257,9 @@ def test_refusals():
             a.forward(*bad)
     with pytest.raises(sk.SkipFFNError):
         a.forward(q, k, v, out=q)
+    for spread in (do[:1].expand(20, 4, 64), do[:, :1].expand(20, 4, 64), do[..., :1].expand(20, 4, 64)):     # gradients of sums
+        with pytest.raises((sk.SkipFFNError, ValueError)):
+            a.backward(spread, q, k, v, out, lse)
     for kw in (dict(dq=q), dict(dk=v), dict(dv=k), dict(dk=v.clone(), dv=None, dq=out)):
         with pytest.raises(sk.SkipFFNError):
             a.backward(do, q, k, v, out, lse, **kw)

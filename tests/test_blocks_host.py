@@ -77,6 +77,28 @@ def test_layernorm_arguments_refused():
     assert lib.skipffn_layernorm_scratch_bytes(0) == 0 and lib.skipffn_layernorm_scratch_bytes(64) == 160 * 2 * 64 * 4
 
 
+def test_layernorm_overlaps_and_alignment_refused():
+    # every output on top of every other array of the call, but for the two pairs that may coincide
+    lib = _lib()
+    fwd = dict(x=1 << 20, gamma=2 << 20, beta=3 << 20, y=4 << 20, mean=5 << 20, rstd=6 << 20)
+    f = lambda **kw: (lambda a: lib.skipffn_layernorm_forward(P(a["x"]), P(a["gamma"]), P(a["beta"]), 4, 64, 0, 1e-5, P(a["y"]),
+                                                               P(a["mean"]), P(a["rstd"]), None))({**fwd, **kw})
+    for o in ("y", "mean", "rstd"):
+        for i in fwd:
+            if i != o and (o, i) != ("y", "x"):
+                assert f(**{o: fwd[i]}) == 1, (o, i)
+    assert f(mean=fwd["mean"] + 2) == f(rstd=fwd["rstd"] + 1) == 1
+    bwd = dict(dy=1 << 20, x=2 << 20, gamma=3 << 20, mean=4 << 20, rstd=5 << 20, dx=6 << 20, dgamma=7 << 20, dbeta=8 << 20, scratch=9 << 20)
+    b = lambda dw=0, **kw: (lambda a: lib.skipffn_layernorm_backward(
+        P(a["dy"]), P(a["x"]), P(a["gamma"]), P(a["mean"]), P(a["rstd"]), 4, 64, 0, P(a["dx"]), P(a["dgamma"]), P(a["dbeta"]), dw,
+        P(a["scratch"]), 1 << 24, None))({**bwd, **kw})
+    for o in ("dx", "dgamma", "dbeta", "scratch"):
+        for i in bwd:
+            if i != o and (o, i) not in (("dx", "dy"), ("dx", "x")):
+                assert b(**{o: bwd[i]}) == 1, (o, i)
+    assert b(dgamma=bwd["dgamma"] + 1) == b(dw=1, dbeta=bwd["dbeta"] + 2) == 1
+
+
 def test_no_cpu_path():
     import torch
     import paper_2503_21817_b200 as sk

@@ -97,6 +97,26 @@ def test_rows_stay_apart_and_no_rows():
     assert bool((y == 0.5).all()) and np.allclose(to_host(rstd), 1e-5 ** -0.5, rtol=1e-6)
 
 
+def test_elements_past_32_bits():
+    # 2^31 elements and some rows: the last rows are those of a call with only them; the others' gradient is zero
+    import torch
+    import paper_2503_21817_b200 as sk
+    n, C, k = (1 << 31) // 4096 + 5, 4096, 9
+    x, gamma, beta, dy = _case(4, k, C, "bf16")
+    big, d = (torch.zeros(n, C, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    big[-k:], d[-k:] = x, dy
+    y, mean, rstd = sk.layernorm_forward(x, gamma, beta)
+    Y, M, R = sk.layernorm_forward(big, gamma, beta)
+    assert torch.equal(Y[-k:], y) and torch.equal(M[-k:], mean) and torch.equal(R[-k:], rstd) and torch.equal(Y[0], beta)
+    del Y
+    dx, dg, db = sk.layernorm_backward(d, big, gamma, M, R, dw_fp32=True, dx=d)
+    want = sk.layernorm_backward(dy, x, gamma, mean, rstd)[0]
+    assert torch.equal(dx[-k:], want) and not dx[:-k].any()
+    refs, errs = blocks.layernorm_backward(*(to_host(t) for t in (dy, x, gamma, mean, rstd)), "bf16", "fp32")
+    for name, got, r, e in zip(("dgamma", "dbeta"), (dg, db), refs[1:], errs[1:]):       # sums of zeros add no error
+        _within(got, r, e, name)
+
+
 def test_refusals():
     import torch
     import paper_2503_21817_b200 as sk
