@@ -424,9 +424,9 @@ class PackedAttention:
         hq, hk = self.heads_q, self.heads_kv
         args = self._arg(q, "q", hq) + self._arg(k, "k", hk) + self._arg(v, "v", hk)
         if out is None:
-            out = q.new_empty(q.shape)
+            out = self._torch.empty_like(q)
         if lse is None:
-            lse = q.new_empty(q.shape[:2], dtype=self._torch.float32)
+            lse = q.new_empty(q.shape[0], hq, dtype=self._torch.float32)     # sizes as integers: a shape costs 1 us
         else:
             self._check_lse(lse)
         self._on_this_stream()
@@ -447,9 +447,10 @@ class PackedAttention:
         args = (self._arg(dout, "dout", hq) + self._arg(q, "q", hq) + self._arg(k, "k", hk) + self._arg(v, "v", hk)
                 + self._arg(out, "out", hq))
         self._check_lse(lse)
-        dq = q.new_empty(q.shape) if dq is None else dq
-        dk = k.new_empty(k.shape) if dk is None else dk
-        dv = v.new_empty(v.shape) if dv is None else dv
+        like = self._torch.empty_like
+        dq = like(q) if dq is None else dq
+        dk = like(k) if dk is None else dk
+        dv = like(v) if dv is None else dv
         scratch = q.new_empty(max(self.scratch_bytes, 16), dtype=self._torch.uint8)
         self._on_this_stream()
         st = _on_device(self._backward, self._index, self._handle, *args, lse.data_ptr(), *self._arg(dq, "dq", hq),
