@@ -7,8 +7,9 @@
 // the mean of squared deviations (a second look at the registers, not E[x^2] - mean^2), and the backward
 // reads x and dy once for both its results.  Statistics and sums are fp32 in a fixed order (no atomics).
 // Measured (B200, bf16): forward 9376 x 4096 in 26.5 us (5.8 TB/s, 0.89 of the copy rate), 577 x 1024 in 3 us;
-// backward 4927 x 5120 in 43 us (3.5 TB/s; rows 37, partial sums 6): bound by the instructions of a row
-// (about 20 per column and thread) and its barrier, with two rows at a time on an SM.
+// backward 4927 x 5120 in 42.8 us (3.5 TB/s; rows 37, partial sums 6): an SM has two rows in the air and 20 warps that
+// issue in 57 % of its cycles (latency of a row's chain: sums, barrier, results); the next row's sums before this row's
+// results (44.5 us) did not help, nor half the shared-memory reads (42.5).
 #include "common.cuh"
 
 namespace skipffn {
@@ -257,15 +258,16 @@ k_layernorm_bwd(const T *dy, const T *x, const T *__restrict__ gamma, const floa
         if (row + step < rows) { mean_next = mean_in[row + step]; rstd_next = rstd_in[row + step]; }
         fetch(row + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
         copy_async_wait<STAGES - 1>();
-        // xh and t = dy gamma of vector k; made twice, because keeping them would spill
-        auto vectors = [&](int k, uint64_t (&xh)[P], uint64_t (&yv)[P], uint64_t (&t)[P]) {
+        // x - mean, dy and dy gamma of vector k, read twice from shared memory: held in registers as read (24 for
+        // bf16) the row cost as much (42.5 for 42.8 us), held unpacked it spills
+        auto vectors = [&](int k, uint64_t (&xm)[P], uint64_t (&yv)[P], uint64_t (&t)[P]) {
             uint64_t g[P];
-            unpack2<N>(*slot(stage, 0, k), xh);
+            unpack2<N>(*slot(stage, 0, k), xm);
             unpack2<N>(*slot(stage, 1, k), yv);
             unpack2<N>(gam[tx + k * threads], g);
 #pragma unroll
             for (int e = 0; e < P; ++e) {
-                xh[e] = mul2(add2(xh[e], neg_mean), r2);
+                xm[e] = add2(xm[e], neg_mean);
                 t[e] = mul2(yv[e], g[e]);
             }
         };
@@ -273,13 +275,14 @@ k_layernorm_bwd(const T *dy, const T *x, const T *__restrict__ gamma, const floa
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (owns(k)) {
-                uint64_t xh[P], yv[P], t[P];
-                vectors(k, xh, yv, t);
+                uint64_t xm[P], yv[P], t[P];
+                vectors(k, xm, yv, t);
 #pragma unroll
                 for (int e = 0; e < P; ++e) {
+                    const uint64_t xh = mul2(xm[e], r2);
                     p0 = add2(p0, t[e]);
-                    p1 = fma2(t[e], xh[e], p1);
-                    dg[k][e] = fma2(yv[e], xh[e], dg[k][e]);
+                    p1 = fma2(t[e], xh, p1);
+                    dg[k][e] = fma2(yv[e], xh, dg[k][e]);
                     db[k][e] = add2(db[k][e], yv[e]);
                 }
             }
@@ -299,18 +302,19 @@ k_layernorm_bwd(const T *dy, const T *x, const T *__restrict__ gamma, const floa
             s0 = __shfl_sync(0xffffffffu, s, 0);
             s1 = __shfl_sync(0xffffffffu, s, 16);
         }
-        s0 *= -inv_c;
-        s1 *= -inv_c;
+        // dx = rstd t + (x - mean) rstd^2 m1 + rstd m0 with m0, m1 the means of -t and -t xh
+        s0 *= -inv_c * rstd;
+        s1 *= -inv_c * rstd * rstd;
         const uint64_t m0 = pair2(s0, s0), m1 = pair2(s1, s1);
         uint4 *dst = reinterpret_cast<uint4 *>(dx + row * C) + tx;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (owns(k)) {
-                uint64_t xh[P], yv[P], t[P];
-                vectors(k, xh, yv, t);
+                uint64_t xm[P], yv[P], t[P];
+                vectors(k, xm, yv, t);
 #pragma unroll
-                for (int e = 0; e < P; ++e) xh[e] = mul2(r2, fma2(xh[e], m1, add2(t[e], m0)));
-                dst[k * threads] = pack2<N>(xh);
+                for (int e = 0; e < P; ++e) xm[e] = fma2(xm[e], m1, fma2(t[e], r2, m0));
+                dst[k * threads] = pack2<N>(xm);
             }
         if (++stage == STAGES) stage = 0;
     }
