@@ -7,9 +7,10 @@
 // the mean of squared deviations (a second look at the registers, not E[x^2] - mean^2), and the backward
 // reads x and dy once for both its results.  Statistics and sums are fp32 in a fixed order (no atomics).
 // Measured (B200, bf16): forward 9376 x 4096 in 26.5 us (5.8 TB/s, 0.89 of the copy rate), 577 x 1024 in 3 us;
-// backward 4927 x 5120 in 42.8 us (3.5 TB/s; rows 37, partial sums 6): an SM has two rows in the air and 20 warps that
+// backward 4927 x 5120 in 40.6 us (3.7 TB/s; rows 37, partial sums 4): an SM has two rows at a time and 20 warps that
 // issue in 57 % of its cycles (latency of a row's chain: sums, barrier, results); the next row's sums before this row's
-// results (44.5 us) did not help, nor half the shared-memory reads (42.5).
+// results (44.5 us) did not help
+// (42.8 before), nor half the shared-memory reads (42.5).  Partial sums with eight lanes per column instead of 32 took 2 us more.
 #include "common.cuh"
 
 namespace skipffn {
@@ -408,28 +409,31 @@ k_layernorm_bwd_cols(const T *dy, const T *x, const float *__restrict__ mean_in,
     }
 }
 
-// Sum of the partial rows: LN_LANES lanes per column walk the parts, added in lane order.  blockIdx.y: 0 dgamma, 1 dbeta.
+// Sum of the partial rows, 32 columns per CTA: warp w adds parts w, w + 32, ... of every column (all its loads in flight),
+// then the warps' sums of column w.  blockIdx.y: 0 dgamma, 1 dbeta.
+constexpr int SUM_COLS = 32, SUM_LOADS = (LN_MAX_PARTS + 31) / 32;
 template <typename TO>
-__global__ void __launch_bounds__(LN_COLS * LN_LANES)
+__global__ void __launch_bounds__(SUM_COLS * 32)
 k_layernorm_sum_parts(const float *__restrict__ part, int parts, int C, TO *__restrict__ dgamma, TO *__restrict__ dbeta)
 {
-    __shared__ float red[LN_LANES][LN_COLS];
+    __shared__ float red[32][SUM_COLS + 1];
     pdl_enter();
     TO *dst = blockIdx.y ? dbeta : dgamma;
     if (dst == nullptr) return;
-    const int cl = threadIdx.x % LN_COLS, lane = threadIdx.x / LN_COLS, c = blockIdx.x * LN_COLS + cl;
-    float s = 0.0f;
-    if (c < C)
-#pragma unroll 8
-        for (int k = lane; k < parts; k += LN_LANES) s += part[((int64_t)k * 2 + blockIdx.y) * C + c];
-    red[lane][cl] = s;
-    __syncthreads();
-    if (lane == 0 && c < C) {
-        s = 0.0f;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * SUM_COLS + lane;
+    float v[SUM_LOADS], s = 0.0f;
 #pragma unroll
-        for (int l = 0; l < LN_LANES; ++l) s += red[l][cl];
-        dst[c] = from_f32<TO>(s);
+    for (int k = 0; k < SUM_LOADS; ++k) {
+        const int q = warp + 32 * k;
+        v[k] = q < parts && c < C ? part[((int64_t)q * 2 + blockIdx.y) * C + c] : 0.0f;
     }
+#pragma unroll
+    for (int k = 0; k < SUM_LOADS; ++k) s += v[k];
+    red[warp][lane] = s;
+    __syncthreads();
+    s = warp_add(red[lane][warp]);
+    const int out = blockIdx.x * SUM_COLS + warp;
+    if (lane == 0 && out < C) dst[out] = from_f32<TO>(s);
 }
 
 // threads of a row group: enough for LN_NV vectors each, a whole number of warps
@@ -534,7 +538,7 @@ cudaError_t bwd_t(const T *dy, const T *x, const T *gamma, const float *mean, co
         }
     }
     if (!sums) return cudaSuccess;
-    const dim3 grid((C + LN_COLS - 1) / LN_COLS, 2), block(LN_COLS * LN_LANES);
+    const dim3 grid((C + SUM_COLS - 1) / SUM_COLS, 2), block(SUM_COLS * 32);
     return dw_fp32 ? launch_pdl(k_layernorm_sum_parts<float>, grid, block, s, part, parts, C, (float *)dgamma, (float *)dbeta)
                    : launch_pdl(k_layernorm_sum_parts<T>, grid, block, s, part, parts, C, (T *)dgamma, (T *)dbeta);
 }
