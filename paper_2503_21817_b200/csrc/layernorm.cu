@@ -7,10 +7,10 @@
 // the mean of squared deviations (a second look at the registers, not E[x^2] - mean^2), and the backward
 // reads x and dy once for both its results.  Statistics and sums are fp32 in a fixed order (no atomics).
 // Measured (B200, bf16): forward 9376 x 4096 in 26.5 us (5.8 TB/s, 0.89 of the copy rate), 577 x 1024 in 3 us;
-// backward 4927 x 5120 in 40.6 us (3.7 TB/s; rows 37, partial sums 4): an SM has two rows at a time and 20 warps that
-// issue in 57 % of its cycles (latency of a row's chain: sums, barrier, results); the next row's sums before this row's
-// results (44.5 us) did not help
-// (42.8 before), nor half the shared-memory reads (42.5).  Partial sums with eight lanes per column instead of 32 took 2 us more.
+// backward 4927 x 5120 in 41.3 us (3.7 TB/s; rows 37, partial sums 4): an SM has two rows at a time and 20 warps that
+// issue in 57 % of its cycles (latency of a row's chain: sums, barrier, results).  From 42.8 us, the next row's sums
+// before this row's results (44.5) did not help, nor half the shared-memory reads (42.5); partial sums with 32 lanes per
+// column instead of eight did (2 us less).
 #include "common.cuh"
 
 namespace skipffn {
@@ -303,9 +303,9 @@ k_layernorm_bwd(const T *dy, const T *x, const T *__restrict__ gamma, const floa
             s0 = __shfl_sync(0xffffffffu, s, 0);
             s1 = __shfl_sync(0xffffffffu, s, 16);
         }
-        // dx = rstd t + (x - mean) rstd^2 m1 + rstd m0 with m0, m1 the means of -t and -t xh
+        // dx = rstd t + xh (rstd m1) + rstd m0 with m0, m1 the means of -t and -t xh  (rstd^2 could leave fp32's range)
         s0 *= -inv_c * rstd;
-        s1 *= -inv_c * rstd * rstd;
+        s1 *= -inv_c * rstd;
         const uint64_t m0 = pair2(s0, s0), m1 = pair2(s1, s1);
         uint4 *dst = reinterpret_cast<uint4 *>(dx + row * C) + tx;
 #pragma unroll
@@ -314,7 +314,7 @@ k_layernorm_bwd(const T *dy, const T *x, const T *__restrict__ gamma, const floa
                 uint64_t xm[P], yv[P], t[P];
                 vectors(k, xm, yv, t);
 #pragma unroll
-                for (int e = 0; e < P; ++e) xm[e] = fma2(xm[e], m1, fma2(t[e], r2, m0));
+                for (int e = 0; e < P; ++e) xm[e] = fma2(mul2(xm[e], r2), m1, fma2(t[e], r2, m0));
                 dst[k * threads] = pack2<N>(xm);
             }
         if (++stage == STAGES) stage = 0;

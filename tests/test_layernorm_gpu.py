@@ -97,6 +97,20 @@ def test_rows_stay_apart_and_no_rows():
     assert bool((y == 0.5).all()) and np.allclose(to_host(rstd), 1e-5 ** -0.5, rtol=1e-6)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("power", [-60, 58])
+def test_gradient_scales_with_tiny_and_huge_rows(dtype, power):
+    # eps = 0: x -> 2^p x keeps y and dgamma, divides dx by 2^p, exactly but for products that leave the normal
+    # numbers of fp32: xh, rstd m and rstd t stay in them here, rstd^2 would not
+    import torch
+    import paper_2503_21817_b200 as sk
+    x, gamma, beta, dy = _case(5, 20, 1024, dtype)
+    a, b = ((s, *sk.layernorm_forward(s, gamma, beta, eps=0.0)) for s in (x, x * 2.0 ** power))
+    assert torch.equal(a[1], b[1])
+    ga, gb = (sk.layernorm_backward(dy, t[0], gamma, t[2], t[3]) for t in (a, b))
+    assert torch.equal(ga[0], gb[0] * 2.0 ** power) and torch.equal(ga[1], gb[1]) and torch.equal(ga[2], gb[2])
+
+
 def test_elements_past_32_bits():
     # 2^31 elements and some rows: the last rows are those of a call with only them; the others' gradient is zero
     import torch
