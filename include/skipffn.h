@@ -286,6 +286,8 @@ skipffn_status skipffn_token_merge_poll(void *scratch, int64_t n, int32_t C, int
  * fp32, or path = SIMT: plain FMA.  All sums have a fixed order: equal calls give equal bits.
  * A non-finite value spreads inside its own sequence only (a later token's inf or NaN in v, k, q or
  * dout can reach earlier tokens' results there: 0 * inf is not masked); it never reaches another sequence.
+ * A score of minus infinity (an infinite key, a product that leaves fp32) is a key of probability zero; a row whose
+ * every score is minus infinity has no result (out NaN, lse minus infinity).
  * backward: `out` and `lse` are the forward's results; scratch: device memory of
  * skipffn_attention_scratch_bytes(handle) bytes, 16-byte aligned, used by this call only.
  * skipffn_attention_poll synchronises `stream` and reports SKIPFFN_ETIMEOUT with the wait site if a kernel

@@ -170,11 +170,12 @@ k_attention_fwd_simt(const AttnArgs a)
                 s[i][j] = k0 + t.tx + 16 * j < row_end[i] ? s[i][j] * a.scale : -INFINITY;
                 bm = fmaxf(bm, s[i][j]);
             }
-            const float mn = fmaxf(m[i], half_warp_max(bm)), f = k0 == 0 ? 0.0f : expf(m[i] - mn);
+            // base: the maximum, or zero while a row has met nothing but minus infinity (its P and sum are zero then)
+            const float mn = fmaxf(m[i], half_warp_max(bm)), base = mn == -INFINITY ? 0.0f : mn, f = expf(m[i] - base);
             float sum = 0.0f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float p = expf(s[i][j] - mn);
+                const float p = expf(s[i][j] - base);
                 sum += p;
                 ps[(4 * t.ty + i) * PPITCH + t.tx + 16 * j] = p;
             }

@@ -363,7 +363,7 @@ __device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, bool u
         m = bm;
     } else if (__any_sync(0xffffffffu, (bm - m) * c2 > 8.0f)) {
         // the scores of this block were issued after the previous O += P V, so O is at rest
-        const float mn = fmaxf(m, bm), f = fast_exp2((m - mn) * c2);
+        const float mn = fmaxf(m, bm), f = m == mn ? 1.0f : fast_exp2((m - mn) * c2);    // both may be minus infinity
         m = mn;
         l *= f;
 #pragma unroll 1
@@ -376,7 +376,9 @@ __device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, bool u
             tmem_st16(t_o + c, o);
         }
     }
-    const uint64_t c2p = pair2(c2, c2), mcp = pair2(-m * c2, -m * c2);
+    // a row that has met nothing but minus infinity has P = 2^(-inf - 0) = 0 so far, not 2^(-inf + inf)
+    const float neg_mc = m == -INFINITY ? 0.0f : -m * c2;
+    const uint64_t c2p = pair2(c2, c2), mcp = pair2(neg_mc, neg_mc);
     uint64_t sum[2] = {0, 0};
     uint32_t pk[16];
     if (upper) tmem_ld32(t_s + 64, u);
