@@ -89,6 +89,36 @@ def attention_backward(q, k, v, dout, cu, scale, causal, dtype="bf16", bound_out
     return tuple(res), tuple(err)
 
 
+def _bf16(x):
+    """Nearest bf16 value of each finite entry (ties to even), as float64."""
+    b = np.ascontiguousarray(x, dtype=np.float32).view(np.uint32)
+    return ((b + (0x7fff + ((b >> 16) & 1))) & np.uint32(0xffff0000)).view(np.float32).astype(np.float64)
+
+
+def attention_rounded(q, k, v, dout, cu, scale, causal, mistake=None):
+    """``(out, dq, dk, dv)`` in fp64 but for the roundings to bf16 that the tensor-core kernels document: P as operand
+    of out and dV, dS as operand of dK (in dQ it is the sum of two bf16 numbers: no rounding), delta from the rounded
+    out, put right by the row sums of dS before dK is formed, and each result.  Gives the size of error to expect.
+    `mistake` plants one: "dropped" / "negated" correction of delta, "one number": dS rounded in dQ too."""
+    hq, group = q.shape[1], q.shape[1] // k.shape[1]
+    out, dq, dk, dv = (np.zeros_like(t) for t in (q, q, k, v))
+    correct = {"dropped": 0.0, "negated": -1.0}.get(mistake, 1.0)
+    for a, b in _sequences(cu):
+        for h in range(hq):
+            hk = h // group
+            Q, K, V, G = q[a:b, h], k[a:b, hk], v[a:b, hk], dout[a:b, h]
+            p, _, _ = _probabilities(Q, K, scale, causal)
+            P, dp = _bf16(p), G @ V.T
+            out[a:b, h] = _bf16(P @ V)
+            delta = np.sum(G * out[a:b, h], axis=1, keepdims=True)
+            ds = p * (dp - delta)
+            dq[a:b, h] = scale * ((_bf16(ds) if mistake == "one number" else ds) @ K)
+            delta = delta + correct * ds.sum(axis=1, keepdims=True)
+            dk[a:b, hk] += scale * (_bf16(p * (dp - delta)).T @ Q)
+            dv[a:b, hk] += P.T @ G
+    return out, _bf16(dq), _bf16(dk), _bf16(dv)
+
+
 # A fp32 sum of C values: at most 40 additions one after the other in a thread, ten shuffle or shared-memory
 # levels of at most 32 more; 128 roundings bound every path, and the products around it.
 _G = 128 * 2.0 ** -24

@@ -1,0 +1,79 @@
+"""Relative Frobenius errors of packed attention: no larger than the roundings that the kernels document make them.  The
+elementwise bounds of the other tests cover the worst case of every term at once; a lost correction of delta or a lost
+half of dS stays far inside those, and outside these."""
+import numpy as np
+import pytest
+
+from oracle import blocks
+
+CASES = [((15, 16, 17), 8, 2, 128, True), ((616, 133), 8, 2, 128, True), ((127, 128, 129), 2, 2, 64, True),
+         ((300, 7), 10, 2, 96, True), ((70, 200), 64, 1, 32, True)]
+# The limit is 1.04 times the error of oracle.blocks.attention_rounded on the same inputs.  It rounds the same quantities
+# at the same places; the kernels round P before it is normalised, another draw of as many rounding errors.  The
+# smallest result here has 12288 entries, the sampling error of its root mean square is 1 / sqrt(2 x 12288) < 1 %
+# of each draw, and fp32 accumulation and the exponential (2^-22) add 1e-6 to 2e-3.
+SLACK = 1.04
+NAMES = ("out", "dq", "dk", "dv")
+
+
+def _host_case(lens, hq, hk, d):
+    import torch
+    g = torch.Generator().manual_seed(sum(lens) + hq)
+    n = sum(lens)
+    t = [torch.randn(n, h, d, generator=g).to(torch.bfloat16) for h in (hq, hk, hk, hq)]
+    return t, [0] + [int(c) for c in np.cumsum(lens)]
+
+
+def _errors(got, want):
+    return [np.linalg.norm(a - b) / np.linalg.norm(b) for a, b in zip(got, want)]
+
+
+def _exact(t, cu, scale, causal):
+    q, k, v, do = t
+    return (blocks.attention_forward(q, k, v, cu, scale, causal)[0], *blocks.attention_backward(q, k, v, do, cu, scale, causal)[0])
+
+
+@pytest.mark.parametrize("lens,hq,hk,d,causal", CASES)
+def test_limits_tell_planted_mistakes(lens, hq, hk, d, causal):
+    t, cu = _host_case(lens, hq, hk, d)
+    t = [x.double().numpy() for x in t]
+    want = _exact(t, cu, d ** -0.5, causal)
+    base = _errors(blocks.attention_rounded(*t, cu, d ** -0.5, causal), want)
+    assert all(1e-3 < e < 3e-3 for e in base)
+    for mistake, i in (("dropped", 2), ("negated", 2), ("one number", 1)):
+        e = _errors(blocks.attention_rounded(*t, cu, d ** -0.5, causal, mistake), want)
+        assert e[i] > SLACK * base[i], (mistake, e[i], base[i])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,hq,hk,d,causal", CASES)
+def test_errors_are_those_of_the_documented_roundings(lens, hq, hk, d, causal):
+    from gpu_util import to_host
+    from test_attention_gpu import _object
+    t, cu = _host_case(lens, hq, hk, d)
+    q, k, v, do = (x.cuda() for x in t)
+    a = _object(cu, hq, hk, d, "bf16", causal)
+    out, lse = a.forward(q, k, v)
+    got = [to_host(x) for x in (out, *a.backward(do, q, k, v, out, lse))]
+    a.poll()
+    t = [x.double().numpy() for x in t]
+    want = _exact(t, cu, d ** -0.5, causal)
+    limits = _errors(blocks.attention_rounded(*t, cu, d ** -0.5, causal), want)
+    for name, e, limit in zip(NAMES, _errors(got, want), limits):
+        assert e <= SLACK * limit, (name, e, limit)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,hq,hk,d,causal", CASES)
+def test_errors_in_fp32(lens, hq, hk, d, causal):
+    # the package's fp32 criterion: relative Frobenius error 1e-5
+    from gpu_util import to_host
+    from test_attention_gpu import _object
+    t, cu = _host_case(lens, hq, hk, d)
+    q, k, v, do = (x.float().cuda() for x in t)
+    a = _object(cu, hq, hk, d, "fp32", causal)
+    out, lse = a.forward(q, k, v)
+    got = [to_host(x) for x in (out, *a.backward(do, q, k, v, out, lse))]
+    t = [x.double().numpy() for x in t]
+    for name, e in zip(NAMES, _errors(got, _exact(t, cu, d ** -0.5, causal))):
+        assert e <= 1e-5, (name, e)
