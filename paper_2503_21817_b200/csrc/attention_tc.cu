@@ -340,9 +340,9 @@ __device__ __forceinline__ void exp_chunk(const uint32_t (&r)[32], uint64_t c2, 
 // One block of scores of one row per thread: running maximum m and sum l, P over the scores.  Half of the
 // scores is read twice (for the maximum, then again), which keeps a row's registers below what would spill.  P
 // is handed over in two halves (p_full, p_full + 8), so that the second product starts while the second half
-// is made.  `upper`: the block has columns past 63.
+// is made.  `upper`: the block has columns past 63; `live`: this row is a query of the sequence.
 template <int DP>
-__device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, bool upper, float c2, bool first, float &m, float &l,
+__device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, bool upper, bool live, float c2, bool first, float &m, float &l,
                                               uint32_t p_full, int lane)
 {
     uint32_t x[32], y[32], u[32], v[32];
@@ -361,7 +361,8 @@ __device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, bool u
     bm = max_chunk(y, max_chunk(x, bm));
     if (first) {
         m = bm;
-    } else if (__any_sync(0xffffffffu, (bm - m) * c2 > 8.0f)) {
+    } else if (__any_sync(0xffffffffu, live && (bm - m) * c2 > 8.0f)) {
+        // rows of other sequences in this tile have no say, so a sequence's bits depend on nothing else
         // the scores of this block were issued after the previous O += P V, so O is at rest
         const float mn = fmaxf(m, bm), f = m == mn ? 1.0f : fast_exp2((m - mn) * c2);    // both may be minus infinity
         m = mn;
@@ -608,6 +609,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             if (nb == 0) continue;
             const int token = t0 + row_t;
             const int row_end = p.causal ? min(token + 1, it.len) : it.len;   // keys of this row
+            const bool live = row < used && token < it.len;                   // a query of this sequence
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; j < nb; ++j) {
                 ok = wait_bar<true>(s_full, ns & 1, ab, p.status, SITE_EPI_TMEM_FULL);
@@ -618,14 +620,13 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
                 const bool upper = end - j * TILE > 64;
                 const int from = (p.causal ? t0 + 1 : it.len) - j * TILE, to = upper ? TILE : 64;
                 if (from < to) mask_scores(t_s, from, to, row_end - j * TILE);
-                softmax_block<DP>(t_s, t_o, upper, p.c2, j == 0, m, l, p_full, lane);
+                softmax_block<DP>(t_s, t_o, upper, live, p.c2, j == 0, m, l, p_full, lane);
             }
             if (!ok) break;
             ok = wait_bar<true>(smem_u32(&ctl->o_full[g]), no & 1, ab, p.status, SITE_EPI_TMEM_FULL);
             ++no;
             if (!ok) break;
             tc_fence_after();
-            const bool live = row < used && token < it.len;
             const float inv = 1.0f / l;
             const int head = it.h * p.group + row_h;
             const int64_t tok = (int64_t)it.start + token;

@@ -1,5 +1,5 @@
-"""Packed attention on the GPU: what one row's result may depend on.  Keys whose scores are minus infinity leave it
-as the definition has it."""
+"""Packed attention on the GPU: what one row's result may depend on.  Rows of other sequences that share a tile, and
+keys whose scores are minus infinity, leave it as the definition has it."""
 import numpy as np
 import pytest
 
@@ -7,6 +7,27 @@ from gpu_util import to_host
 from test_attention_gpu import _object, _tensors, _within, blocks
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype,path", [("bf16", 0), ("bf16", 1), ("fp32", 0)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_finite_values_of_a_neighbour_do_not_reach_the_bits_of_a_sequence(dtype, path, causal):
+    # the second sequence's first queries lie in the last row tile of the first one.  With queries along key 140 of
+    # the first sequence their running maximum jumps in its second key block, by far more than 2^8: the first
+    # sequence's rows in that tile must not notice.
+    import torch
+    lens, d = (150, 90), 64
+    q, k, v, do, cu = _tensors(21, lens, 2, 2, d, dtype)
+    a = _object(cu, 2, 2, d, dtype, causal, path=path)
+    out, lse = a.forward(q, k, v)
+    grads = a.backward(do, q, k, v, out, lse)
+    wild = q.clone()
+    wild[150:] = 100.0 * k[140]
+    out2, lse2 = a.forward(wild, k, v)
+    grads2 = a.backward(do, wild, k, v, out2, lse2)
+    a.poll()
+    for name, x, y in zip(("out", "lse", "dq", "dk", "dv"), (out, lse, *grads), (out2, lse2, *grads2)):
+        assert torch.equal(x[:150], y[:150]), name
 
 
 @pytest.mark.parametrize("dtype,path", [("bf16", 0), ("bf16", 1), ("fp32", 0)])
