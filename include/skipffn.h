@@ -273,7 +273,7 @@ skipffn_status skipffn_token_merge_poll(void *scratch, int64_t n, int32_t C, int
  *                caller and alive as long as the handle; holds the work lists and a status block.
  *                skipffn_attention_create copies them there and waits for `stream`, so it stays outside
  *                stream captures (EINVAL inside one); forward and backward may be captured.
- * Handles are read-only after creation: calls on different streams may share one.
+ * Handles are read-only after creation, but for skipffn_attention_tune: calls on different streams may share one.
  *
  * Arrays are [tokens, heads, head_dim] with contiguous heads and a token stride ld* in elements (so
  * that slices of one fused projection can be passed); bases and strides are multiples of 16 bytes
@@ -315,6 +315,15 @@ skipffn_status skipffn_attention_backward(const skipffn_attention *attention, co
                                           int64_t lddq, void *dk, int64_t lddk, void *dv, int64_t lddv,
                                           void *scratch, size_t scratch_bytes, void *stream);
 skipffn_status skipffn_attention_poll(const skipffn_attention *attention, void *stream, int32_t *site_out);
+
+/* Host-only knobs of an attention handle for the calls that follow (not while another thread makes one; none needed in
+ * normal use; EINVAL outside the ranges):
+ *   WAIT_US    limit of a wait inside the tensor-core kernels, 1 .. 4 000 000 us, default 1 000 000; a kernel in
+ *              which one runs out leaves results unfinished and returns, and skipffn_attention_poll reports it
+ *   LOSE_LOAD  1: every key tile announces bytes that never come, so that the waits run out -- the failure path can be
+ *              exercised without any fault; 0 (default) */
+typedef enum { SKIPFFN_ATTENTION_WAIT_US = 0, SKIPFFN_ATTENTION_LOSE_LOAD = 1, SKIPFFN_ATTENTION_TUNE_COUNT = 2 } skipffn_attention_tunable;
+skipffn_status skipffn_attention_tune(skipffn_attention *attention, int32_t what, int32_t value);
 
 /* Device addresses of the kept-row index list (int32, ascending) and of its length. */
 skipffn_status skipffn_get_kept(const skipffn_saved *saved, const int32_t **idx_dev,

@@ -24,12 +24,13 @@ EXPORTS = ["skipffn_workspace_bytes", "skipffn_saved_create", "skipffn_saved_des
            "skipffn_workspace_bytes_kept", "skipffn_saved_create_kept", "skipffn_saved_create_split",
            "skipffn_token_merge_poll", "skipffn_schedule_plan_segment", "skipffn_attention_plan_bytes",
            "skipffn_attention_create", "skipffn_attention_destroy", "skipffn_attention_forward",
-           "skipffn_attention_scratch_bytes", "skipffn_attention_backward", "skipffn_attention_poll",
+           "skipffn_attention_scratch_bytes", "skipffn_attention_backward", "skipffn_attention_poll", "skipffn_attention_tune",
            "skipffn_layernorm_forward", "skipffn_layernorm_scratch_bytes", "skipffn_layernorm_backward"]
 STATIC_MAX_TOKENS = 65536   # SKIPFFN_STATIC_MAX_TOKENS
 
 TUNABLES = {"tile_n": 0, "streamk": 1, "stages": 2, "lose_handover": 3, "one_box": 4, "tma_stores": 5, "gather": 6,
             "panel_sync": 7}
+ATTENTION_TUNABLES = {"wait_us": 0, "lose_load": 1}   # skipffn_attention_tunable
 PROFILE_SLOTS = ["compact", "route_x", "gateup", "down", "route_dout", "dh", "dw_down", "dw_gate",
                  "dw_up", "dx", "norm_bwd", "recompute"]
 
@@ -137,6 +138,8 @@ def load_library() -> ctypes.CDLL:
     lib.skipffn_attention_backward.argtypes = [vp] + [vp, i64] * 5 + [vp] + [vp, i64] * 3 + [vp, ctypes.c_size_t, vp]
     lib.skipffn_attention_poll.restype = i32
     lib.skipffn_attention_poll.argtypes = [vp, vp, ctypes.POINTER(i32)]
+    lib.skipffn_attention_tune.restype = i32
+    lib.skipffn_attention_tune.argtypes = [vp, i32, i32]
     lib.skipffn_layernorm_forward.restype = i32
     lib.skipffn_layernorm_forward.argtypes = [vp, vp, vp, i64, i32, i32, ctypes.c_float, vp, vp, vp, vp]
     lib.skipffn_layernorm_scratch_bytes.restype = ctypes.c_size_t
@@ -458,6 +461,13 @@ class PackedAttention:
         if st != 0:
             raise SkipFFNError(st, "skipffn_attention_backward")
         return dq, dk, dv
+
+    def tune(self, **knobs):
+        """``skipffn_attention_tune``: wait_us, lose_load (failure path)."""
+        for name, value in knobs.items():
+            st = self.lib.skipffn_attention_tune(self._handle, ATTENTION_TUNABLES[name], int(value))
+            if st != 0:
+                raise SkipFFNError(st, f"skipffn_attention_tune({name})")
 
     def poll(self):
         """Synchronise the stream and raise if a kernel reported a device-side problem."""

@@ -19,9 +19,12 @@ struct skipffn_attention {
     int32_t max_len;                     // of the longest sequence
     int32_t *status;                     // device: status block, then the lists
     const int4 *fwd_items, *row_items, *key_items;
+    int32_t tune[SKIPFFN_ATTENTION_TUNE_COUNT];
 };
 
 namespace {
+
+constexpr int32_t WAIT_US_DEFAULT = 1000000, WAIT_US_MAX = 4000000;      // the kernels count nanoseconds in 32 bits
 
 bool simt(const skipffn_attention_config *c) { return c->dtype == SKIPFFN_FP32 || c->path == SKIPFFN_PATH_SIMT; }
 int tile_rows(const skipffn_attention_config *c) { return simt(c) ? AT_SIMT_ROWS : AT_TC_ROWS; }
@@ -90,6 +93,7 @@ void fill_args(const skipffn_attention *h, AttnArgs *a)
     a->hq = h->cfg.heads_q; a->hk = h->cfg.heads_kv; a->group = h->group; a->tokens = h->tokens;
     a->d = h->cfg.head_dim; a->causal = h->cfg.causal; a->scale = h->cfg.scale;
     a->status = h->status;
+    a->wait_us = h->tune[SKIPFFN_ATTENTION_WAIT_US]; a->lose_load = h->tune[SKIPFFN_ATTENTION_LOSE_LOAD];
 }
 
 }  // namespace
@@ -118,6 +122,8 @@ skipffn_status skipffn_attention_create(skipffn_attention **out, const skipffn_a
     skipffn_attention *h = new (std::nothrow) skipffn_attention;
     if (!h) return SKIPFFN_EWORKSPACE;
     h->cfg = *cfg;
+    h->tune[SKIPFFN_ATTENTION_WAIT_US] = WAIT_US_DEFAULT;
+    h->tune[SKIPFFN_ATTENTION_LOSE_LOAD] = 0;
     h->N = n_seq > 0 ? cu_seqlens[n_seq] : 0;
     h->group = cfg->heads_q / cfg->heads_kv;
     h->tokens = tile_rows(cfg) / h->group;
@@ -169,6 +175,14 @@ skipffn_status skipffn_attention_create(skipffn_attention **out, const skipffn_a
     }
     if (st != SKIPFFN_OK) { delete h; return st; }
     *out = h;
+    return SKIPFFN_OK;
+}
+
+skipffn_status skipffn_attention_tune(skipffn_attention *h, int32_t what, int32_t value)
+{
+    if (!h || what < 0 || what >= SKIPFFN_ATTENTION_TUNE_COUNT) return SKIPFFN_EINVAL;
+    if (what == SKIPFFN_ATTENTION_WAIT_US ? value < 1 || value > WAIT_US_MAX : value != 0 && value != 1) return SKIPFFN_EINVAL;
+    h->tune[what] = value;
     return SKIPFFN_OK;
 }
 

@@ -24,6 +24,7 @@ struct AttnArgs {
     float scale;
     float2 *row_stats;               // scratch: [row tile][kv head][rows of a tile] (lse log2 e, delta)
     int32_t *status;
+    int32_t wait_us, lose_load;      // tensor-core kernels: see skipffn_attention_tune
 };
 
 constexpr int AT_TC_ROWS = 128, AT_TC_KEYS = 128;       // tile of the tensor-core kernels

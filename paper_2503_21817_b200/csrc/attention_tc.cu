@@ -50,42 +50,44 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
         : "memory");
     return ok != 0;
 }
-// Bounded waits, inlined: a kernel that moves registers between its warps cannot call functions.  SPIN (the warps
-// on the critical path) polls; the others let the hardware park the warp.
-template <bool SPIN>
-__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status, int site)
+// Bounded waits, inlined: a kernel that moves registers between its warps cannot call functions.  A wait that runs
+// out sets the CTA's abort flag and the status word; every other wait of the CTA then gives up as well.
+struct Waits { volatile int *abort_flag; int32_t *status; uint32_t limit_ns; };
+__device__ __forceinline__ void expire(const Waits &w, int site)
 {
-    auto probe = [&] { return SPIN ? mbar_test(bar, parity) : mbar_try_wait(bar, parity); };
-    if (probe()) return true;
+    *w.abort_flag = 1;
+    if (atomicCAS(&w.status[ST_STATUS], 0, (int)SKIPFFN_ETIMEOUT) == 0) w.status[ST_SITE] = site;
+}
+// of a single lane (the TMA issuer)
+__device__ __forceinline__ bool wait_lane(uint32_t bar, uint32_t parity, const Waits &w, int site)
+{
+    if (mbar_test(bar, parity)) return true;
+    const unsigned long long t0 = globaltimer_ns();
+    for (uint32_t it = 1;; ++it) {
+        if (mbar_test(bar, parity)) return true;
+        if ((it & 0x3ff) == 0) {
+            if (*w.abort_flag) return false;
+            if (globaltimer_ns() - t0 > w.limit_ns) { expire(w, site); return false; }
+        }
+    }
+}
+// of a whole warp.  Every lane polls and a vote decides, so the answer is the same in every lane, and the warp is
+// together, when whole-warp instructions follow (tcgen05.ld / st, votes, shuffles, the MMA warp's uniform registers):
+// lane by lane, one lane could find the barrier complete and another its time up.  A form in which one lane polled for the
+// others ended in an illegal access.  SPIN (the warps on the critical path) polls; the others let the hardware park
+// the warp.
+template <bool SPIN>
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const Waits &w, int site)
+{
+    auto probe = [&] { return __all_sync(0xffffffffu, SPIN ? mbar_test(bar, parity) : mbar_try_wait(bar, parity)); };
+    if (__builtin_expect(probe(), 1)) return true;
     const unsigned long long t0 = globaltimer_ns();
     for (uint32_t it = 1;; ++it) {
         if (probe()) return true;
         if ((it & (SPIN ? 0x3ff : 0xf)) == 0) {
-            if (*abort_flag) return false;
-            if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) {
-                *abort_flag = 1;
-                if (atomicCAS(&status[ST_STATUS], 0, (int)SKIPFFN_ETIMEOUT) == 0) status[ST_SITE] = site;
-                return false;
-            }
-        }
-    }
-}
-// The MMA warp's wait: the answer is the same in every lane and the compiler can tell (a vote), so that what
-// follows stays in uniform registers.  Every lane polls and the warp walks on together: a form in which one lane
-// polled for the others ended in an illegal access.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status, int site)
-{
-    if (__builtin_expect(__all_sync(0xffffffffu, mbar_test(bar, parity)), 1)) return true;
-    const unsigned long long t0 = globaltimer_ns();
-    for (uint32_t it = 1;; ++it) {
-        if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
-        if ((it & 0x3ff) == 0) {
-            const bool late = globaltimer_ns() - t0 > WAIT_LIMIT_NS;
-            if (__any_sync(0xffffffffu, late || *abort_flag)) {
-                if (late) {
-                    *abort_flag = 1;
-                    if (atomicCAS(&status[ST_STATUS], 0, (int)SKIPFFN_ETIMEOUT) == 0) status[ST_SITE] = site;
-                }
+            const bool late = globaltimer_ns() - t0 > w.limit_ns;
+            if (__any_sync(0xffffffffu, late || *w.abort_flag)) {
+                if (late) expire(w, site);
                 return false;
             }
         }
@@ -109,6 +111,8 @@ struct AtParams {
     float *lse;
     float2 *row_stats;
     int32_t *status;
+    uint32_t wait_ns;                        // limit of a wait
+    uint32_t lose;                           // bytes that key tiles announce and that never come (failure path)
     int32_t wide;                            // dQ: every 16 columns of a row start on 32 bytes
 };
 struct alignas(64) AtMaps { CUtensorMap q, k, v, g; };
@@ -459,7 +463,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    volatile int *ab = &ctl->abort_flag;
+    const Waits waits{&ctl->abort_flag, p.status, p.wait_ns};
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
@@ -470,12 +474,12 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             bool ok = true;
             auto acquire = [&]() {           // next ring slot, free to be written
                 const uint32_t s = pos % SLOTS;
-                ok = ok && wait_bar<true>(smem_u32(&ctl->kv_empty[s]), ((pos / SLOTS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                ok = ok && wait_lane(smem_u32(&ctl->kv_empty[s]), ((pos / SLOTS) & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
                 ++pos;
                 return s;
             };
             auto load_q = [&](const FwdItem &it, int g) {
-                ok = ok && wait_bar<true>(smem_u32(&ctl->q_empty[g]), (nq[g] & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                ok = ok && wait_lane(smem_u32(&ctl->q_empty[g]), (nq[g] & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
                 if (!ok) return;
                 const uint32_t bar = smem_u32(&ctl->q_full[g]);
                 mbar_expect_tx(bar, (uint32_t)(used * DP * 2));
@@ -491,7 +495,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
                     uint32_t s = acquire();
                     if (!ok) break;
                     uint32_t bar = smem_u32(&ctl->kv_full[s]);
-                    mbar_expect_tx(bar, T_BYTES);
+                    mbar_expect_tx(bar, T_BYTES + p.lose);
                     load_tile<DP>(ring + s * T_BYTES, &tm.k, it.h, it.start + j * TILE, bar);
                     if (j == 0 && it.nb1) load_q(it, 1);
                     s = acquire();
@@ -513,7 +517,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             pos += 2 * n;
             if (!it.dirty_tail()) continue;
             const uint32_t s = (pos - 1) % SLOTS;
-            ok = wait_bar<false>(smem_u32(&ctl->tail[s]), (seen >> s) & 1, ab, p.status, SITE_PRODUCER_EMPTY);
+            ok = wait_warp<false>(smem_u32(&ctl->tail[s]), (seen >> s) & 1, waits, SITE_PRODUCER_EMPTY);
             if (!ok) break;
             seen ^= 1u << s;
             const int valid = it.len - (n - 1) * TILE;
@@ -528,7 +532,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
         const uint32_t kv_full = smem_u32(&ctl->kv_full[0]), kv_empty = smem_u32(&ctl->kv_empty[0]);
         uint32_t slot = 0, phase = 0, nq[2] = {0, 0}, np[2] = {0, 0};
         bool ok = true;
-        auto wait_slot = [&]() { ok = ok && wait_warp(kv_full + 8 * slot, phase, ab, p.status, SITE_MMA_FULL); };
+        auto wait_slot = [&]() { ok = ok && wait_warp<true>(kv_full + 8 * slot, phase, waits, SITE_MMA_FULL); };
         auto next_slot = [&]() {
             const uint32_t s = slot;
             if (++slot == SLOTS) { slot = 0; phase ^= 1; }
@@ -550,7 +554,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
                 if (!ok || nb[g] == 0) break;
-                ok = wait_warp(smem_u32(&ctl->q_full[g]), nq[g] & 1, ab, p.status, SITE_MMA_FULL);
+                ok = wait_warp<true>(smem_u32(&ctl->q_full[g]), nq[g] & 1, waits, SITE_MMA_FULL);
                 if (!ok) break;
                 ++nq[g];
                 tc_fence_after();
@@ -571,12 +575,12 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
                     const uint32_t pt = tmem + g * TILE, ot = tmem + 2 * TILE + g * DP, vd = v_desc0 + vs * (T_BYTES >> 4);
                     const bool last = j == nb[g] - 1;
                     const int steps = last ? last_cols[g] / 16 : TILE / 16;
-                    if (j == 0) ok = wait_warp(smem_u32(&ctl->o_free[g]), (nq[g] - 1) & 1 ^ 1, ab, p.status, SITE_MMA_TMEM_EMPTY);
-                    ok = ok && wait_warp(smem_u32(&ctl->p_full[g][0]), np[g] & 1, ab, p.status, SITE_MMA_FULL);
+                    if (j == 0) ok = wait_warp<true>(smem_u32(&ctl->o_free[g]), (nq[g] - 1) & 1 ^ 1, waits, SITE_MMA_TMEM_EMPTY);
+                    ok = ok && wait_warp<true>(smem_u32(&ctl->p_full[g][0]), np[g] & 1, waits, SITE_MMA_FULL);
                     if (!ok) break;
                     tc_fence_after();
                     mma_tmem_rows<DP, 0, 4, 8>(on, ot, pt, vd, steps, j > 0);
-                    ok = wait_warp(smem_u32(&ctl->p_full[g][1]), np[g] & 1, ab, p.status, SITE_MMA_FULL);
+                    ok = wait_warp<true>(smem_u32(&ctl->p_full[g][1]), np[g] & 1, waits, SITE_MMA_FULL);
                     if (!ok) break;
                     ++np[g];
                     tc_fence_after();
@@ -612,7 +616,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             const bool live = row < used && token < it.len;                   // a query of this sequence
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; j < nb; ++j) {
-                ok = wait_bar<true>(s_full, ns & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = wait_warp<true>(s_full, ns & 1, waits, SITE_EPI_TMEM_FULL);
                 ++ns;
                 if (!ok) break;
                 tc_fence_after();
@@ -623,7 +627,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
                 softmax_block<DP>(t_s, t_o, upper, live, p.c2, j == 0, m, l, p_full, lane);
             }
             if (!ok) break;
-            ok = wait_bar<true>(smem_u32(&ctl->o_full[g]), no & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+            ok = wait_warp<true>(smem_u32(&ctl->o_full[g]), no & 1, waits, SITE_EPI_TMEM_FULL);
             ++no;
             if (!ok) break;
             tc_fence_after();
@@ -651,7 +655,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             if (live) p.lse[tok * p.hq + head] = fmaf(m, p.scale, logf(l));
         }
     }
-    cta_teardown(ab, ctl->tmem_base, FwdWarps::MMA);
+    cta_teardown(waits.abort_flag, ctl->tmem_base, FwdWarps::MMA);
 }
 
 // ------------------------------------------------------------------------------------ dK, dV
@@ -734,7 +738,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    volatile int *ab = &ctl->abort_flag;
+    const Waits waits{&ctl->abort_flag, p.status, p.wait_ns};
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t t_s = tmem, t_dp = tmem + TILE, t_dv = tmem + 2 * TILE, t_dk = t_dv + DP;
@@ -754,12 +758,12 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                     const uint32_t qb = smem_u32(dirty ? &ctl->q_tail[s] : &ctl->q_full[s]);
                     const uint32_t gb = smem_u32(dirty ? &ctl->g_tail[s] : &ctl->g_full[s]);
                     if (j == 0) {
-                        ok = wait_bar<true>(smem_u32(&ctl->k_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                        ok = wait_lane(smem_u32(&ctl->k_empty), (items & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
                         if (!ok) break;
-                        mbar_expect_tx(smem_u32(&ctl->k_full), T_BYTES);
+                        mbar_expect_tx(smem_u32(&ctl->k_full), T_BYTES + p.lose);
                         load_tile<DP>(k_tile, &tm.k, it.h, it.start + it.k0, smem_u32(&ctl->k_full));
                     }
-                    ok = wait_bar<true>(smem_u32(&ctl->empty[s]), ((cnt >> 1) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    ok = wait_lane(smem_u32(&ctl->empty[s]), ((cnt >> 1) & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
                     if (!ok) break;
                     mbar_expect_tx(qb, (uint32_t)(used * DP * 2) + Sh::STAT_BYTES);
                     load_tile<DP>(q_ring + s * T_BYTES, &tm.q, it.h * p.group, token, qb);
@@ -767,7 +771,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                     mbar_expect_tx(gb, (uint32_t)(used * DP * 2));
                     load_tile<DP>(g_ring + s * T_BYTES, &tm.g, it.h * p.group, token, gb);
                     if (j == 0) {
-                        ok = wait_bar<true>(smem_u32(&ctl->v_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                        ok = wait_lane(smem_u32(&ctl->v_empty), (items & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
                         if (!ok) break;
                         mbar_expect_tx(smem_u32(&ctl->v_full), T_BYTES);
                         load_tile<DP>(v_tile, &tm.v, it.h, it.start + it.k0, smem_u32(&ctl->v_full));
@@ -787,7 +791,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
             const uint32_t s = (cnt - 1) & 1;
             const int valid = it.valid(p, tile);
             for (int w = 0; w < 2 && ok; ++w) {
-                ok = wait_bar<false>(smem_u32(w ? &ctl->g_tail[s] : &ctl->q_tail[s]), (seen >> s) & 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                ok = wait_warp<false>(smem_u32(w ? &ctl->g_tail[s] : &ctl->q_tail[s]), (seen >> s) & 1, waits, SITE_PRODUCER_EMPTY);
                 if (!ok) break;
                 zero_rows<DP>((w ? g_ring : q_ring) + s * T_BYTES, valid, min(mma_cols(valid), used), lane);
                 fence_proxy_async_smem();
@@ -807,7 +811,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
         for (; ok && feed.take(it); ++items) {
             auto cols_of = [&](int j) { return mma_cols(it.valid(p, it.first + j)); };
             auto scores = [&](int j, uint32_t c) {
-                ok = ok && wait_warp(smem_u32(&ctl->q_full[c & 1]), (c >> 1) & 1, ab, p.status, SITE_MMA_FULL);
+                ok = ok && wait_warp<true>(smem_u32(&ctl->q_full[c & 1]), (c >> 1) & 1, waits, SITE_MMA_FULL);
                 if (!ok) return;
                 tc_fence_after();
                 mma_rows_rows<DP>(on, t_s, k_desc, q_desc + (c & 1) * (T_BYTES >> 4), idesc_rows(cols_of(j)));
@@ -815,27 +819,27 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 if (j == it.n - 1) umma_commit_if(on, smem_u32(&ctl->k_empty));
             };
             auto grad_scores = [&](int j, uint32_t c) {
-                ok = ok && wait_warp(smem_u32(&ctl->g_full[c & 1]), (c >> 1) & 1, ab, p.status, SITE_MMA_FULL);
+                ok = ok && wait_warp<true>(smem_u32(&ctl->g_full[c & 1]), (c >> 1) & 1, waits, SITE_MMA_FULL);
                 if (!ok) return;
                 tc_fence_after();
                 mma_rows_rows<DP>(on, t_dp, v_desc, g_desc + (c & 1) * (T_BYTES >> 4), idesc_rows(cols_of(j)));
                 umma_commit_if(on, smem_u32(&ctl->g_scores));
                 if (j == it.n - 1) umma_commit_if(on, smem_u32(&ctl->v_empty));
             };
-            ok = wait_warp(smem_u32(&ctl->k_full), items & 1, ab, p.status, SITE_MMA_FULL);
+            ok = wait_warp<true>(smem_u32(&ctl->k_full), items & 1, waits, SITE_MMA_FULL);
             scores(0, cnt);
-            ok = ok && wait_warp(smem_u32(&ctl->v_full), items & 1, ab, p.status, SITE_MMA_FULL);
+            ok = ok && wait_warp<true>(smem_u32(&ctl->v_full), items & 1, waits, SITE_MMA_FULL);
             grad_scores(0, cnt);
             for (int j = 0; j < it.n && ok; ++j, ++cnt) {
                 const uint32_t s = cnt & 1;
-                ok = wait_warp(smem_u32(&ctl->p_ready), cnt & 1, ab, p.status, SITE_MMA_FULL);
+                ok = wait_warp<true>(smem_u32(&ctl->p_ready), cnt & 1, waits, SITE_MMA_FULL);
                 if (ok && j == 0)
-                    ok = wait_warp(smem_u32(&ctl->acc_free), (items & 1) ^ 1, ab, p.status, SITE_MMA_TMEM_EMPTY);
+                    ok = wait_warp<true>(smem_u32(&ctl->acc_free), (items & 1) ^ 1, waits, SITE_MMA_TMEM_EMPTY);
                 if (!ok) break;
                 tc_fence_after();
                 mma_tmem_rows<DP, 0, 8, 2>(on, t_dv, t_s, g_across + s * (T_BYTES >> 4), cols_of(j) / 16, j > 0);
                 if (j + 1 < it.n) scores(j + 1, cnt + 1);
-                ok = ok && wait_warp(smem_u32(&ctl->ds_ready), cnt & 1, ab, p.status, SITE_MMA_FULL);
+                ok = ok && wait_warp<true>(smem_u32(&ctl->ds_ready), cnt & 1, waits, SITE_MMA_FULL);
                 if (!ok) break;
                 tc_fence_after();
                 mma_tmem_rows<DP, 0, 8, 2>(on, t_dk, t_dp, q_across + s * (T_BYTES >> 4), cols_of(j) / 16, j > 0);
@@ -862,7 +866,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 const bool mask = p.causal && t0 < it.k0 + TILE - 1;
                 const int from = mask ? (key - t0) * p.group - c0 : 0;
                 const uint32_t st = stats + (cnt & 1) * Sh::STAT_BYTES + c0 * 8;
-                ok = wait_bar<true>(smem_u32(&ctl->s_full), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = wait_warp<true>(smem_u32(&ctl->s_full), cnt & 1, waits, SITE_EPI_TMEM_FULL);
                 if (!ok) break;
                 tc_fence_after();
                 uint32_t r[32], pk[16];
@@ -889,7 +893,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready));
-                ok = wait_bar<true>(smem_u32(&ctl->g_scores), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = wait_warp<true>(smem_u32(&ctl->g_scores), cnt & 1, waits, SITE_EPI_TMEM_FULL);
                 if (!ok) break;
                 tc_fence_after();
                 if (some) {
@@ -916,7 +920,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 if (lane == 0) mbar_arrive(smem_u32(&ctl->ds_ready));
             }
             if (!ok) break;
-            ok = wait_bar<true>(smem_u32(&ctl->acc_full), items & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+            ok = wait_warp<true>(smem_u32(&ctl->acc_full), items & 1, waits, SITE_EPI_TMEM_FULL);
             if (!ok) break;
             tc_fence_after();
             // parts 0, 1: the column halves of dV; 2, 3: of dK
@@ -939,7 +943,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
             if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_free));
         }
     }
-    cta_teardown(ab, ctl->tmem_base, BwdWarps::MMA);
+    cta_teardown(waits.abort_flag, ctl->tmem_base, BwdWarps::MMA);
 }
 
 // ------------------------------------------------------------------------------------ dQ
@@ -1018,7 +1022,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    volatile int *ab = &ctl->abort_flag;
+    const Waits waits{&ctl->abort_flag, p.status, p.wait_ns};
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t t_dp = tmem + 2 * TILE, t_dq = tmem + 3 * TILE;
@@ -1031,24 +1035,24 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
             Feed<QItem, false> feed(p);
             QItem it;
             for (; ok && feed.take(it); ++items) {
-                ok = wait_bar<true>(smem_u32(&ctl->q_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                ok = wait_lane(smem_u32(&ctl->q_empty), (items & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
                 if (!ok) break;
                 mbar_expect_tx(smem_u32(&ctl->q_full), (uint32_t)(used * DP * 2));
                 load_tile<DP>(q_tile, &tm.q, it.h * p.group, it.start + it.t0, smem_u32(&ctl->q_full));
                 for (int j = 0; j < it.nb; ++j, ++cnt) {
                     const uint32_t ks = cnt % KS, vs = cnt % VS;
-                    ok = wait_bar<true>(smem_u32(&ctl->k_empty[ks]), ((cnt / KS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    ok = wait_lane(smem_u32(&ctl->k_empty[ks]), ((cnt / KS) & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
                     if (!ok) break;
                     const uint32_t kb = smem_u32(j == it.nb - 1 && it.dirty_tail() ? &ctl->k_tail[ks] : &ctl->k_full[ks]);
-                    mbar_expect_tx(kb, T_BYTES);
+                    mbar_expect_tx(kb, T_BYTES + p.lose);
                     load_tile<DP>(k_ring + ks * T_BYTES, &tm.k, it.h, it.start + j * TILE, kb);
                     if (j == 0) {
-                        ok = wait_bar<true>(smem_u32(&ctl->g_empty), (items & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                        ok = wait_lane(smem_u32(&ctl->g_empty), (items & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
                         if (!ok) break;
                         mbar_expect_tx(smem_u32(&ctl->g_full), (uint32_t)(used * DP * 2));
                         load_tile<DP>(g_tile, &tm.g, it.h * p.group, it.start + it.t0, smem_u32(&ctl->g_full));
                     }
-                    ok = wait_bar<true>(smem_u32(&ctl->v_empty[vs]), ((cnt / VS) & 1) ^ 1, ab, p.status, SITE_PRODUCER_EMPTY);
+                    ok = wait_lane(smem_u32(&ctl->v_empty[vs]), ((cnt / VS) & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
                     if (!ok) break;
                     const uint32_t vb = smem_u32(&ctl->v_full[vs]);
                     mbar_expect_tx(vb, T_BYTES);
@@ -1065,7 +1069,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
             cnt += it.nb;
             if (!it.dirty_tail()) continue;
             const uint32_t s = (cnt - 1) % KS;
-            ok = wait_bar<false>(smem_u32(&ctl->k_tail[s]), (seen >> s) & 1, ab, p.status, SITE_PRODUCER_EMPTY);
+            ok = wait_warp<false>(smem_u32(&ctl->k_tail[s]), (seen >> s) & 1, waits, SITE_PRODUCER_EMPTY);
             if (!ok) break;
             seen ^= 1u << s;
             const int valid = it.len - (it.nb - 1) * TILE;
@@ -1085,7 +1089,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
         for (; ok && feed.take(it); ++items) {
             auto cols_of = [&](int j) { return mma_cols(it.end - j * TILE); };
             auto scores = [&](int j, uint32_t c) {
-                ok = ok && wait_warp(smem_u32(&ctl->k_full[c % KS]), (c / KS) & 1, ab, p.status, SITE_MMA_FULL);
+                ok = ok && wait_warp<true>(smem_u32(&ctl->k_full[c % KS]), (c / KS) & 1, waits, SITE_MMA_FULL);
                 if (!ok) return;
                 tc_fence_after();
                 mma_rows_rows<DP>(on, tmem + (c & 1) * TILE, q_desc, k_desc + (c % KS) * (T_BYTES >> 4), idesc_rows(cols_of(j)));
@@ -1093,7 +1097,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 if (j == it.nb - 1) umma_commit_if(on, smem_u32(&ctl->q_empty));
             };
             auto grad_scores = [&](int j, uint32_t c) {
-                ok = ok && wait_warp(smem_u32(&ctl->v_full[c % VS]), (c / VS) & 1, ab, p.status, SITE_MMA_FULL);
+                ok = ok && wait_warp<true>(smem_u32(&ctl->v_full[c % VS]), (c / VS) & 1, waits, SITE_MMA_FULL);
                 if (!ok) return;
                 tc_fence_after();
                 mma_rows_rows<DP>(on, t_dp, g_desc, v_desc + (c % VS) * (T_BYTES >> 4), idesc_rows(cols_of(j)));
@@ -1101,17 +1105,17 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 umma_commit_if(on, smem_u32(&ctl->v_empty[c % VS]));
                 if (j == it.nb - 1) umma_commit_if(on, smem_u32(&ctl->g_empty));
             };
-            ok = wait_warp(smem_u32(&ctl->q_full), items & 1, ab, p.status, SITE_MMA_FULL);
+            ok = wait_warp<true>(smem_u32(&ctl->q_full), items & 1, waits, SITE_MMA_FULL);
             scores(0, cnt);
-            ok = ok && wait_warp(smem_u32(&ctl->g_full), items & 1, ab, p.status, SITE_MMA_FULL);
+            ok = ok && wait_warp<true>(smem_u32(&ctl->g_full), items & 1, waits, SITE_MMA_FULL);
             grad_scores(0, cnt);
             if (it.nb > 1) scores(1, cnt + 1);
             for (int j = 0; j < it.nb && ok; ++j, ++cnt) {
-                ok = wait_warp(smem_u32(&ctl->ds_ready), cnt & 1, ab, p.status, SITE_MMA_FULL);
+                ok = wait_warp<true>(smem_u32(&ctl->ds_ready), cnt & 1, waits, SITE_MMA_FULL);
                 if (!ok) break;
                 if (j + 1 < it.nb) grad_scores(j + 1, cnt + 1);
                 if (ok && j == 0)
-                    ok = wait_warp(smem_u32(&ctl->acc_free), (items & 1) ^ 1, ab, p.status, SITE_MMA_TMEM_EMPTY);
+                    ok = wait_warp<true>(smem_u32(&ctl->acc_free), (items & 1) ^ 1, waits, SITE_MMA_TMEM_EMPTY);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t ds = tmem + (cnt & 1) * TILE;
@@ -1141,8 +1145,8 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 const int cols = mma_cols(it.end - j * TILE);
                 const bool mask = cols < TILE || j * TILE + TILE > (p.causal ? it.t0 + 1 : it.len);
                 const int limit = row_end - j * TILE - c0;
-                ok = wait_bar<true>(smem_u32(&ctl->s_full[cnt & 1]), (cnt >> 1) & 1, ab, p.status, SITE_EPI_TMEM_FULL);
-                ok = ok && wait_bar<true>(smem_u32(&ctl->g_scores), cnt & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+                ok = wait_warp<true>(smem_u32(&ctl->s_full[cnt & 1]), (cnt >> 1) & 1, waits, SITE_EPI_TMEM_FULL);
+                ok = ok && wait_warp<true>(smem_u32(&ctl->g_scores), cnt & 1, waits, SITE_EPI_TMEM_FULL);
                 if (!ok) break;
                 tc_fence_after();
                 if (c0 < cols) {
@@ -1173,18 +1177,18 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 if (lane == 0) mbar_arrive(smem_u32(&ctl->ds_ready));
             }
             if (!ok) break;
-            ok = wait_bar<true>(smem_u32(&ctl->acc_full), items & 1, ab, p.status, SITE_EPI_TMEM_FULL);
+            ok = wait_warp<true>(smem_u32(&ctl->acc_full), items & 1, waits, SITE_EPI_TMEM_FULL);
             if (!ok) break;
             tc_fence_after();
             const bool live = row < used && token < it.len;
             // the parts' sums meet; part 0 puts the row's delta right for the kernel of dK and dV
-            ok = wait_bar<true>(smem_u32(&ctl->sum_read), (items & 1) ^ 1, ab, p.status, SITE_EPI_EXCHANGE);
+            ok = wait_warp<true>(smem_u32(&ctl->sum_read), (items & 1) ^ 1, waits, SITE_EPI_EXCHANGE);
             if (!ok) break;
             asm volatile("st.shared.f32 [%0], %1;" ::"r"(sums + (part * TILE + row) * 4), "f"(sum) : "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&ctl->sum_ready));
             if (part == 0) {
-                ok = wait_bar<true>(smem_u32(&ctl->sum_ready), items & 1, ab, p.status, SITE_EPI_EXCHANGE);
+                ok = wait_warp<true>(smem_u32(&ctl->sum_ready), items & 1, waits, SITE_EPI_EXCHANGE);
                 if (!ok) break;
                 float s4[4];
 #pragma unroll
@@ -1218,7 +1222,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
             if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_free));
         }
     }
-    cta_teardown(ab, ctl->tmem_base, BwdWarps::MMA);
+    cta_teardown(waits.abort_flag, ctl->tmem_base, BwdWarps::MMA);
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -1269,6 +1273,7 @@ static AtParams params_of(const AttnArgs &a, const int4 *items, int n)
     p.hq = a.hq; p.hk = a.hk; p.group = a.group; p.tokens = a.tokens; p.d = a.d; p.causal = a.causal;
     p.scale = a.scale; p.c2 = a.scale * LOG2E;
     p.status = a.status; p.row_stats = a.row_stats;
+    p.wait_ns = (uint32_t)a.wait_us * 1000u; p.lose = a.lose_load ? 16 : 0;
     return p;
 }
 
