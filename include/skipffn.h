@@ -318,8 +318,9 @@ skipffn_status skipffn_attention_poll(const skipffn_attention *attention, void *
 
 /* Host-only knobs of an attention handle for the calls that follow (not while another thread makes one; none needed in
  * normal use; EINVAL outside the ranges):
- *   WAIT_US    limit of a wait inside the tensor-core kernels, 1 .. 4 000 000 us, default 1 000 000; a kernel in
- *              which one runs out leaves results unfinished and returns, and skipffn_attention_poll reports it
+ *   WAIT_US    how long a wait inside the tensor-core kernels may see its CTA stand still, 1 .. 4 000 000 us, default
+ *              1 000 000 (a kernel may take longer); one in which a wait runs out leaves results unfinished and
+ *              returns, and skipffn_attention_poll reports it
  *   LOSE_LOAD  1: every key tile announces bytes that never come, so that the waits run out -- the failure path can be
  *              exercised without any fault; 0 (default) */
 typedef enum { SKIPFFN_ATTENTION_WAIT_US = 0, SKIPFFN_ATTENTION_LOSE_LOAD = 1, SKIPFFN_ATTENTION_TUNE_COUNT = 2 } skipffn_attention_tunable;

@@ -52,7 +52,11 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
 }
 // Bounded waits, inlined: a kernel that moves registers between its warps cannot call functions.  A wait that runs
 // out sets the CTA's abort flag and the status word; every other wait of the CTA then gives up as well.
-struct Waits { volatile int *abort_flag; int32_t *status; uint32_t limit_ns; };
+// A warp may have nothing to do for most of the kernel (the tail warp until an item has a tail, the second row tile's
+// softmax warps until an item has a second tile), so a warp's limit counts from the last tile that the TMA lane
+// issued: it runs out only when the CTA stands still.  The lane itself stands still within a few tiles of whatever it
+// waits for, and the tiles are finite, so every wait ends.
+struct Waits { volatile int *abort_flag; volatile uint32_t *issued; int32_t *status; uint32_t limit_ns; };
 __device__ __forceinline__ void expire(const Waits &w, int site)
 {
     *w.abort_flag = 1;
@@ -81,11 +85,14 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const W
 {
     auto probe = [&] { return __all_sync(0xffffffffu, SPIN ? mbar_test(bar, parity) : mbar_try_wait(bar, parity)); };
     if (__builtin_expect(probe(), 1)) return true;
-    const unsigned long long t0 = globaltimer_ns();
+    unsigned long long t0 = globaltimer_ns();
+    uint32_t seen = *w.issued;
     for (uint32_t it = 1;; ++it) {
         if (probe()) return true;
         if ((it & (SPIN ? 0x3ff : 0xf)) == 0) {
-            const bool late = globaltimer_ns() - t0 > w.limit_ns;
+            const unsigned long long now = globaltimer_ns();
+            if (*w.issued != seen) { seen = *w.issued; t0 = now; }
+            const bool late = now - t0 > w.limit_ns;
             if (__any_sync(0xffffffffu, late || *w.abort_flag)) {
                 if (late) expire(w, site);
                 return false;
@@ -294,6 +301,7 @@ struct alignas(8) FwdCtl {
     uint64_t q_full[2], q_empty[2], kv_full[8], kv_empty[8], tail[8], s_full[2], p_full[2][2], o_full[2], o_free[2];   // p_full[g][half]
     uint32_t tmem_base;
     volatile int abort_flag;
+    volatile uint32_t issued;        // tiles that the TMA lane has asked for
 };
 
 // Minus infinity into the columns of a row's scores at or past `limit`, from column `from` (a uniform lower bound of
@@ -454,6 +462,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
             mbar_init(smem_u32(&ctl->tail[i]), 1);
         }
         ctl->abort_flag = 0;
+        ctl->issued = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     const int used = p.group * p.tokens;     // rows of a tile that a box fills; the others stay zero
@@ -463,7 +472,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const Waits waits{&ctl->abort_flag, p.status, p.wait_ns};
+    const Waits waits{&ctl->abort_flag, &ctl->issued, p.status, p.wait_ns};
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
@@ -504,6 +513,7 @@ k_attention_fwd(const __grid_constant__ AtMaps tm, const AtParams p)
                     bar = smem_u32(j == n - 1 && it.dirty_tail() ? &ctl->tail[s] : &ctl->kv_full[s]);
                     mbar_expect_tx(bar, T_BYTES);
                     load_tile<DP>(ring + s * T_BYTES, &tm.v, it.h, it.start + j * TILE, bar);
+                    ctl->issued = pos;
                 }
             }
         }
@@ -679,6 +689,7 @@ struct alignas(8) KvCtl {
     uint64_t s_full, g_scores, p_ready, ds_ready, acc_full, acc_free;
     uint32_t tmem_base;
     volatile int abort_flag;
+    volatile uint32_t issued;        // tiles that the TMA lane has asked for
 };
 struct KvItem {
     int start, len, k0, base, h, first, n;      // row tiles first .. first + n - 1 of the sequence
@@ -729,6 +740,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
         mbar_init(smem_u32(&ctl->acc_full), 1);
         mbar_init(smem_u32(&ctl->acc_free), BwdWarps::COUNT);
         ctl->abort_flag = 0;
+        ctl->issued = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     const int used = p.group * p.tokens;
@@ -738,7 +750,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const Waits waits{&ctl->abort_flag, p.status, p.wait_ns};
+    const Waits waits{&ctl->abort_flag, &ctl->issued, p.status, p.wait_ns};
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t t_s = tmem, t_dp = tmem + TILE, t_dv = tmem + 2 * TILE, t_dk = t_dv + DP;
@@ -770,6 +782,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                     bulk_load(stats + s * Sh::STAT_BYTES, p.row_stats + ((int64_t)(it.base + tile) * p.hk + it.h) * TILE, Sh::STAT_BYTES, qb);
                     mbar_expect_tx(gb, (uint32_t)(used * DP * 2));
                     load_tile<DP>(g_ring + s * T_BYTES, &tm.g, it.h * p.group, token, gb);
+                    ctl->issued = cnt + 1;
                     if (j == 0) {
                         ok = wait_lane(smem_u32(&ctl->v_empty), (items & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
                         if (!ok) break;
@@ -965,6 +978,7 @@ struct alignas(8) QCtl {
     uint64_t s_full[2], g_scores, ds_ready, acc_full, acc_free, sum_ready, sum_read;
     uint32_t tmem_base;
     volatile int abort_flag;
+    volatile uint32_t issued;        // tiles that the TMA lane has asked for
 };
 struct QItem {
     int start, len, t0, tile, h, end, nb;
@@ -1013,6 +1027,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
         mbar_init(smem_u32(&ctl->acc_full), 1);
         mbar_init(smem_u32(&ctl->acc_free), BwdWarps::COUNT);
         ctl->abort_flag = 0;
+        ctl->issued = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     const int used = p.group * p.tokens;
@@ -1022,7 +1037,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const Waits waits{&ctl->abort_flag, p.status, p.wait_ns};
+    const Waits waits{&ctl->abort_flag, &ctl->issued, p.status, p.wait_ns};
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t t_dp = tmem + 2 * TILE, t_dq = tmem + 3 * TILE;
@@ -1057,6 +1072,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                     const uint32_t vb = smem_u32(&ctl->v_full[vs]);
                     mbar_expect_tx(vb, T_BYTES);
                     load_tile<DP>(v_ring + vs * T_BYTES, &tm.v, it.h, it.start + j * TILE, vb);
+                    ctl->issued = cnt + 1;
                 }
             }
         }

@@ -53,3 +53,30 @@ def test_knobs_outside_their_ranges_are_refused():
         a.tune(other=1)
     a.tune(wait_us=1)
     a.tune(wait_us=4000000, lose_load=0)
+
+
+@pytest.mark.parametrize("lens,hq,hk,d", [
+    # a long sequence and a short one with a part-filled 16-row step: the warp that zeroes tails has nothing to do
+    # until the CTA has been through the long one
+    ((32768, 7), 16, 16, 64),
+    # items of one row tile, then items of two: the second tile's softmax warps have nothing to do until then
+    ((32,) * 30000 + (64,) * 300, 16, 4, 8),
+])
+def test_a_wait_may_take_longer_than_its_limit_while_the_kernel_moves_on(lens, hq, hk, d):
+    import torch
+    q, k, v, do, cu = _tensors(32, lens, hq, hk, d, "bf16")
+    a = _object(cu, hq, hk, d, "bf16")
+    out, lse = a.forward(q, k, v)
+    grads = a.backward(do, q, k, v, out, lse)
+    a.poll()
+    limit = 0.5
+    t0, t1 = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    a.tune(wait_us=int(1000 * limit))
+    t0.record()
+    out2, lse2 = a.forward(q, k, v)
+    t1.record()
+    a.poll()
+    assert t0.elapsed_time(t1) > 2 * limit       # milliseconds: the limit did pass in the meantime
+    grads2 = a.backward(do, q, k, v, out2, lse2)
+    a.poll()
+    assert all(torch.equal(x, y) for x, y in zip((out, lse, *grads), (out2, lse2, *grads2)))
