@@ -314,7 +314,7 @@ __device__ __forceinline__ void mask_scores(uint32_t t_s, int from, int to, int 
     for (int c = max(from, 0) & ~15; c < to; c += 16) {
         uint32_t r[16];
         tmem_ld16(t_s + c, r);
-        tmem_ld_wait();
+        tmem_ld_wait(r);
 #pragma unroll
         for (int e = 0; e < 16; ++e)
             if (c + e >= limit) r[e] = 0xff800000u;
@@ -383,7 +383,7 @@ __device__ __forceinline__ void softmax_block(uint32_t t_s, uint32_t t_o, bool u
         for (int c = 0; c < DP; c += 16) {
             uint32_t o[16];
             tmem_ld16(t_o + c, o);
-            tmem_ld_wait();
+            tmem_ld_wait(o);
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
             tmem_st16(t_o + c, o);

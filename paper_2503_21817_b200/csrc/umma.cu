@@ -705,7 +705,7 @@ k_umma_gemm(const __grid_constant__ TmapSet tm, const UmmaParams p)
                     uint32_t r[32];
                     if (TOK) { tmem_ld_frag16(t_acc + col, r); tmem_ld_frag16(t_acc + (16u << 16) + col, r + 16); }
                     else tmem_ld32(t_acc + col, r);
-                    tmem_ld_wait();
+                    tmem_ld_wait(r);
                     float4 *dst = slot_ptr(my_slot, j);
 #pragma unroll
                     for (int v = 0; v < 8; ++v)
@@ -786,7 +786,7 @@ k_umma_gemm(const __grid_constant__ TmapSet tm, const UmmaParams p)
                 if (!zero_acc) {
                     if (TOK) { tmem_ld_frag16(t_row + col, r); tmem_ld_frag16(t_row + (16u << 16) + col, r + 16); }
                     else tmem_ld32(t_row + col, r);
-                    tmem_ld_wait();
+                    tmem_ld_wait(r);
                 } else {
 #pragma unroll
                     for (int q = 0; q < 32; ++q) r[q] = 0u;
