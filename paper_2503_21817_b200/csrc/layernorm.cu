@@ -21,20 +21,6 @@ constexpr int LN_NV = 4;                      // 16-byte vectors per thread
 
 template <typename T> struct Vec { static constexpr int N = 16 / (int)sizeof(T); };   // elements of a vector
 
-template <int N> __device__ __forceinline__ void unpack(const uint4 &q, float (&v)[N])
-{
-    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
-    if constexpr (N == 8) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            v[2 * k] = __uint_as_float(u[k] << 16);
-            v[2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(u[k]);
-    }
-}
 template <int N> __device__ __forceinline__ uint4 pack(const float (&v)[N])
 {
     uint32_t u[4];

@@ -15,3 +15,11 @@ def test_waits_for_tensor_memory_loads_name_the_registers():
             found += 1
             assert '"+r"' in m.group(1), name
     assert found >= 2
+
+
+def test_device_functions_of_the_blocks_around_the_sublayer_are_called():
+    code = {n: re.sub(r"//[^\n]*|/\*.*?\*/", "", t, flags=re.S) for n, t in SOURCES.items()}
+    everything = "\n".join(code.values())
+    for name in ("ptx.cuh", "layernorm.cu", "attention.cu", "attention_simt.cu", "attention_tc.cu"):
+        for f in re.findall(r"__device__ __forceinline__ [\w:<>\*& ]*?(\w+)\(", code[name]):
+            assert len(re.findall(rf"\b{f}\b", everything)) > 1, (name, f)
