@@ -50,18 +50,26 @@ KERNEL_NAMES = ["compact", "route_x", "gateup", "down", "route_dout", "dh", "dw_
                 "dw_up", "dx"]
 # DRAM bytes per launch (dram__bytes_read.sum + dram__bytes_write.sum) of each GEMM kernel at the
 # default workload, from the ncu captures summarised under profiles/; None until captured.
-NCU_TRAFFIC_BYTES = {"gateup": 416.5e6, "down": 224.8e6, "dh": 276.2e6, "dw_down": 501.2e6,
-                     "dx": 443.2e6, "route_x": 42.1e6, "route_dout": 41.8e6}
-# sha256 prefix of csrc/umma.cu when those counters were taken; once the kernel source differs the
-# counters no longer describe it and `traffic` is reported as null
-NCU_TRAFFIC_SOURCE_SHA = "247200ca0aab8d92"
+NCU_TRAFFIC_BYTES = {"gateup": 416.9e6, "down": 221.0e6, "dh": 273.4e6, "dw_down": 498.9e6,
+                     "dx": 440.1e6, "route_x": 40.5e6, "route_dout": 40.5e6}
+# sha256 prefix of these kernels' sources, headers included, when those counters were taken; once one of
+# them differs the counters no longer describe it and `traffic` is reported as null
+NCU_TRAFFIC_SOURCES = ("umma.cu", "compact.cu", "common.cuh", "ptx.cuh", "sched.cuh")
+NCU_TRAFFIC_SOURCE_SHA = "cc3e4efc621703f3"
 
 
-def ncu_traffic(kernel):
+def ncu_traffic_source_sha(csrc):
     import hashlib
-    src = os.path.join(ROOT, "paper_2503_21817_b200", "csrc", "umma.cu")
+    h = hashlib.sha256()
+    for name in NCU_TRAFFIC_SOURCES:
+        with open(os.path.join(csrc, name), "rb") as f:
+            h.update(f.read())
+    return h.hexdigest()[:16]
+
+
+def ncu_traffic(kernel, csrc=os.path.join(ROOT, "paper_2503_21817_b200", "csrc")):
     try:
-        cur = hashlib.sha256(open(src, "rb").read()).hexdigest()[:16]
+        cur = ncu_traffic_source_sha(csrc)
     except OSError:
         return None
     return NCU_TRAFFIC_BYTES.get(kernel) if cur == NCU_TRAFFIC_SOURCE_SHA else None
