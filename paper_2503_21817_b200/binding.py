@@ -374,6 +374,8 @@ class PackedAttention:
         self.heads_q, self.heads_kv, self.head_dim = int(heads_q), int(heads_kv), int(head_dim)
         self.torch_dtype = torch.bfloat16 if dtype == BF16 else torch.float32
         self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError(f"packed attention needs a CUDA device, got {self.device}")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index
