@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Optional
 
@@ -380,7 +381,7 @@ class PackedAttention:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index
         self._forward, self._backward = self.lib.skipffn_attention_forward, self.lib.skipffn_attention_backward
-        vals = [int(v) for v in cu_seqlens]
+        vals = [operator.index(v) for v in cu_seqlens]           # int() would cut fractions off
         if any(not 0 <= v < 1 << 31 for v in vals):
             raise ValueError("cu_seqlens must be offsets that fit 32 bits")
         n_seq = len(vals) - 1
