@@ -200,7 +200,8 @@ k_attention_fwd_simt(const AttnArgs a)
     }
 }
 
-// P and dS of one 64 x 64 tile into shared memory (rows = queries, columns = keys)
+// P and dS of one 64 x 64 tile into shared memory (rows = queries, columns = keys).  The delta of a row that sees one
+// key is that key's dP: its dS is zero (NaN where dP is not finite), not what two orders of summation differ by.
 __device__ __forceinline__ void grad_tile(float *ps, float *ds, const float *qs, const float *gs, const float *ks, const float *vs,
                                           const float2 *stats, const AttnArgs &a, int t0, int len, int k0, Tile t)
 {
@@ -218,7 +219,7 @@ __device__ __forceinline__ void grad_tile(float *ps, float *ds, const float *qs,
             const bool on = k0 + c < row_end;
             const float p = on ? exp2f(fmaf(s[i][j], c2, -st.x)) : 0.0f;
             ps[r * PPITCH + c] = p;
-            ds[r * PPITCH + c] = on ? p * (dp[i][j] - st.y) : 0.0f;
+            ds[r * PPITCH + c] = on ? p * (dp[i][j] - (row_end == 1 ? dp[i][j] : st.y)) : 0.0f;
         }
     }
 }

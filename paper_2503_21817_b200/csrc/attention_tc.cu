@@ -261,6 +261,17 @@ __device__ __forceinline__ void store_rows(uint32_t stage, int lane, const uint4
     __syncwarp();
 }
 
+// The first n of 32 packed columns times zero: zero, or NaN where they are not finite
+__device__ __forceinline__ void null_columns(uint32_t (&pk)[16], int n)
+{
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        float lo, hi;
+        unpack_bf16(pk[e], lo, hi);
+        pk[e] = pack_bf16(2 * e < n ? lo * 0.0f : lo, 2 * e + 1 < n ? hi * 0.0f : hi);
+    }
+}
+
 // Ends of every kernel: drain after an abort, give the tensor memory back.
 __device__ __forceinline__ void cta_teardown(volatile int *abort_flag, uint32_t tmem_base, int dealloc_warp)
 {
@@ -878,6 +889,8 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 // causal: row (token, head) r of the tile sees this key if token >= key, r >= (key - t0) group
                 const bool mask = p.causal && t0 < it.k0 + TILE - 1;
                 const int from = mask ? (key - t0) * p.group - c0 : 0;
+                // the first token's rows of a causal sequence, or of one of a single token, see key 0 alone: their dS is zero
+                const bool single = (p.causal || it.len == 1) && it.k0 == 0 && t0 == 0;
                 const uint32_t st = stats + (cnt & 1) * Sh::STAT_BYTES + c0 * 8;
                 ok = wait_warp<true>(smem_u32(&ctl->s_full), cnt & 1, waits, SITE_EPI_TMEM_FULL);
                 if (!ok) break;
@@ -925,6 +938,7 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                         }
                         pk[e / 2] = pack_bf16(a, b);
                     }
+                    if (single) null_columns(pk, key == 0 ? p.group - c0 : 0);
                     tmem_st16(t_dp + lanes + c0, pk);
                     tmem_st_wait();
                 }
@@ -1172,10 +1186,12 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                     tmem_ld32(t_dp + lanes + c0, dp);
                     tmem_ld_wait(r);
                     tmem_ld_wait(dp);
+                    // a row that sees one key: delta is that key's dP, so that dS is zero, not what two orders of summation differ by
+                    const float delta = row_end == 1 ? __uint_as_float(dp[0]) : st.y;
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
-                        float a = fast_exp2(fmaf(__uint_as_float(r[e]), p.c2, -st.x)) * (__uint_as_float(dp[e]) - st.y);
-                        float b = fast_exp2(fmaf(__uint_as_float(r[e + 1]), p.c2, -st.x)) * (__uint_as_float(dp[e + 1]) - st.y);
+                        float a = fast_exp2(fmaf(__uint_as_float(r[e]), p.c2, -st.x)) * (__uint_as_float(dp[e]) - delta);
+                        float b = fast_exp2(fmaf(__uint_as_float(r[e + 1]), p.c2, -st.x)) * (__uint_as_float(dp[e + 1]) - delta);
                         if (mask) {
                             a = e < limit ? a : 0.0f;
                             b = e + 1 < limit ? b : 0.0f;

@@ -66,3 +66,51 @@ def test_keys_whose_scores_are_minus_infinity(dtype, path, low, blind):
         _within(out[blind:, h], r_out, e_out, f"out of head {h}")
         _within(lse[blind:, h], r_lse, es[:, 0] + g + 2.0 ** -22 * (1 + np.abs(r_lse)), f"lse of head {h}")
     assert not np.isfinite(to_host(lse[:blind])).any()
+
+
+@pytest.mark.parametrize("dtype,path", [("bf16", 0), ("bf16", 1), ("fp32", 0)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("hq,hk,d", [(8, 2, 128), (3, 3, 40), (5, 1, 64), (64, 1, 32)])
+def test_a_row_that_sees_one_key_has_no_gradient_of_its_score(dtype, path, causal, hq, hk, d):
+    # P = 1 whatever the score: dq = 0, no contribution to dk, and dv gets dout as it is.  Exactly: what is left of
+    # dP - delta when the two are summed in different orders is no gradient.
+    import torch
+    lens = (1, 1, 0, 1)
+    q, k, v, do, cu = _tensors(23, lens, hq, hk, d, dtype)
+    a = _object(cu, hq, hk, d, dtype, causal, path=path)
+    out, lse = a.forward(q, k, v)
+    dq, dk, dv = a.backward(do, q, k, v, out, lse)
+    a.poll()
+    assert torch.equal(out, v.repeat_interleave(hq // hk, 1))
+    assert not dq.any() and not dk.any()
+    want = to_host(do).reshape(3, hk, hq // hk, d)
+    u = blocks.HALF_STEP[dtype]
+    # the group's sum: at most 64 additions in fp32 of values whose P is 1 to (1 + |lse|) 2^-22; one rounding
+    bound = (64 * 2.0 ** -24 + 2.0 ** -22 * (1 + np.abs(to_host(lse)).max())) * np.abs(want).sum(2) + u * np.abs(want.sum(2))
+    _within(dv, want.sum(2), bound, "dv")
+    # a longer causal sequence: its first token
+    if causal:
+        q, k, v, do, cu = _tensors(24, (200, 33), hq, hk, d, dtype)
+        a = _object(cu, hq, hk, d, dtype, causal, path=path)
+        out, lse = a.forward(q, k, v)
+        dq, dk, dv = a.backward(do, q, k, v, out, lse)
+        assert not dq[0].any() and not dq[200].any() and bool(dq[1].any())
+        # ... which adds nothing to dk: without its dout the same bits
+        none = do.clone()
+        none[0] = none[200] = 0
+        assert torch.equal(dk, a.backward(none, q, k, v, out, lse)[1])
+
+
+@pytest.mark.parametrize("dtype,path", [("bf16", 0), ("bf16", 1), ("fp32", 0)])
+def test_a_gradient_that_is_not_finite_shows_where_a_row_sees_one_key(dtype, path):
+    import torch
+    q, k, v, do, cu = _tensors(25, (1, 40), 4, 2, 64, dtype)
+    do[0, 0, 3] = float("nan")
+    do[1, 0, 3] = float("inf")
+    a = _object(cu, 4, 2, 64, dtype, path=path)
+    out, lse = a.forward(q, k, v)
+    dq, dk, dv = a.backward(do, q, k, v, out, lse)
+    a.poll()
+    for i in (0, 1):
+        assert not torch.isfinite(dq[i, 0]).any() and not torch.isfinite(dk[i, 0]).any() and not torch.isfinite(dv[i, 0, 3])
+        assert bool(torch.isfinite(dq[i, 2:]).all()) and bool(torch.isfinite(dk[:, 1]).all())
