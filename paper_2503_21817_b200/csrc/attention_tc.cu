@@ -261,17 +261,6 @@ __device__ __forceinline__ void store_rows(uint32_t stage, int lane, const uint4
     __syncwarp();
 }
 
-// The first n of 32 packed columns times zero: zero, or NaN where they are not finite
-__device__ __forceinline__ void null_columns(uint32_t (&pk)[16], int n)
-{
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        float lo, hi;
-        unpack_bf16(pk[e], lo, hi);
-        pk[e] = pack_bf16(2 * e < n ? lo * 0.0f : lo, 2 * e + 1 < n ? hi * 0.0f : hi);
-    }
-}
-
 // Ends of every kernel: drain after an abort, give the tensor memory back.
 __device__ __forceinline__ void cta_teardown(volatile int *abort_flag, uint32_t tmem_base, int dealloc_warp)
 {
@@ -889,8 +878,6 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                 // causal: row (token, head) r of the tile sees this key if token >= key, r >= (key - t0) group
                 const bool mask = p.causal && t0 < it.k0 + TILE - 1;
                 const int from = mask ? (key - t0) * p.group - c0 : 0;
-                // the first token's rows of a causal sequence, or of one of a single token, see key 0 alone: their dS is zero
-                const bool single = (p.causal || it.len == 1) && it.k0 == 0 && t0 == 0;
                 const uint32_t st = stats + (cnt & 1) * Sh::STAT_BYTES + c0 * 8;
                 ok = wait_warp<true>(smem_u32(&ctl->s_full), cnt & 1, waits, SITE_EPI_TMEM_FULL);
                 if (!ok) break;
@@ -938,7 +925,6 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
                         }
                         pk[e / 2] = pack_bf16(a, b);
                     }
-                    if (single) null_columns(pk, key == 0 ? p.group - c0 : 0);
                     tmem_st16(t_dp + lanes + c0, pk);
                     tmem_st_wait();
                 }
@@ -981,6 +967,8 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
 // product as the sum of two bf16 numbers (eight more MMAs a block), which leaves the second.  The first is left in
 // dK, whose kernel runs after this one, and the second is taken out there: the exact delta makes every row of
 // dS sum to zero, so the row sums found here are added to delta.
+// A row that sees one key has P = 1, and delta is that key's dP: its dS is zero, not the difference of two orders of
+// summation.  It gets that delta for the kernel of dK and dV, whose dP is the same sum in the same order.
 template <int DP> struct QShape {
     static constexpr int T_BYTES = tile_bytes<DP>();
     static constexpr int KS = 3, VS = 2;
@@ -1171,6 +1159,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
             const float2 st = *stats;
             float sum = 0.0f;                // of this part's dS
             const int token = it.t0 + row_t, row_end = p.causal ? min(token + 1, it.len) : it.len;
+            const bool live = row < used && token < it.len;
             for (int j = 0; j < it.nb; ++j, ++cnt) {
                 const int cols = mma_cols(it.end - j * TILE);
                 const bool mask = cols < TILE || j * TILE + TILE > (p.causal ? it.t0 + 1 : it.len);
@@ -1186,15 +1175,17 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                     tmem_ld32(t_dp + lanes + c0, dp);
                     tmem_ld_wait(r);
                     tmem_ld_wait(dp);
-                    // a row that sees one key: delta is that key's dP, so that dS is zero, not what two orders of summation differ by
-                    const float delta = row_end == 1 ? __uint_as_float(dp[0]) : st.y;
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
-                        float a = fast_exp2(fmaf(__uint_as_float(r[e]), p.c2, -st.x)) * (__uint_as_float(dp[e]) - delta);
-                        float b = fast_exp2(fmaf(__uint_as_float(r[e + 1]), p.c2, -st.x)) * (__uint_as_float(dp[e + 1]) - delta);
+                        float a = fast_exp2(fmaf(__uint_as_float(r[e]), p.c2, -st.x)) * (__uint_as_float(dp[e]) - st.y);
+                        float b = fast_exp2(fmaf(__uint_as_float(r[e + 1]), p.c2, -st.x)) * (__uint_as_float(dp[e + 1]) - st.y);
                         if (mask) {
                             a = e < limit ? a : 0.0f;
                             b = e + 1 < limit ? b : 0.0f;
+                        }
+                        if (e == 0 && row_end == 1) {        // dS is zero (NaN where dP is not finite); part 0's sum is the delta
+                            a *= 0.0f;
+                            sum = __uint_as_float(dp[0]);
                         }
                         sum += a + b;
                         hi[e / 2] = pack_bf16(a, b);
@@ -1212,7 +1203,6 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
             ok = wait_warp<true>(smem_u32(&ctl->acc_full), items & 1, waits, SITE_EPI_TMEM_FULL);
             if (!ok) break;
             tc_fence_after();
-            const bool live = row < used && token < it.len;
             // the parts' sums meet; part 0 puts the row's delta right for the kernel of dK and dV
             ok = wait_warp<true>(smem_u32(&ctl->sum_read), (items & 1) ^ 1, waits, SITE_EPI_EXCHANGE);
             if (!ok) break;
@@ -1225,7 +1215,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                 float s4[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s4[k]) : "r"(sums + (k * TILE + row) * 4) : "memory");
-                if (live) stats->y = st.y + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
+                if (live) stats->y = row_end == 1 ? s4[0] : st.y + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&ctl->sum_read));
             }
