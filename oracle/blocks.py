@@ -98,9 +98,11 @@ def _bf16(x):
 def attention_rounded(q, k, v, dout, cu, scale, causal, mistake=None):
     """``(out, dq, dk, dv)`` in fp64 but for the roundings to bf16 that the tensor-core kernels document: P as operand
     of out and dV, dS as operand of dK (in dQ it is the sum of two bf16 numbers: no rounding), delta from the rounded
-    out, put right by the row sums of dS before dK is formed, and each result.  Gives the size of error to expect.
+    out, put right by the row sums of dS before dK is formed (rows of a tile whose keys are one block of 128: the exact
+    delta), and each result.  Gives the size of error to expect.
     `mistake` plants one: "dropped" / "negated" correction of delta, "one number": dS rounded in dQ too."""
     hq, group = q.shape[1], q.shape[1] // k.shape[1]
+    tokens = 128 // group                        # of a row tile
     out, dq, dk, dv = (np.zeros_like(t) for t in (q, q, k, v))
     correct = {"dropped": 0.0, "negated": -1.0}.get(mistake, 1.0)
     for a, b in _sequences(cu):
@@ -110,7 +112,8 @@ def attention_rounded(q, k, v, dout, cu, scale, causal, mistake=None):
             p, _, _ = _probabilities(Q, K, scale, causal)
             P, dp = _bf16(p), G @ V.T
             out[a:b, h] = _bf16(P @ V)
-            delta = np.sum(G * out[a:b, h], axis=1, keepdims=True)
+            tile_end = np.minimum((np.arange(b - a) // tokens + 1) * tokens, b - a) if causal else np.full(b - a, b - a)
+            delta = np.where(tile_end <= 128, np.sum(p * dp, axis=1), np.sum(G * out[a:b, h], axis=1))[:, None]
             ds = p * (dp - delta)
             dq[a:b, h] = scale * ((_bf16(ds) if mistake == "one number" else ds) @ K)
             delta = delta + correct * ds.sum(axis=1, keepdims=True)

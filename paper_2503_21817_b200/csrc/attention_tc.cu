@@ -967,8 +967,10 @@ k_attention_bwd_kv(const __grid_constant__ AtMaps tm, const AtParams p)
 // product as the sum of two bf16 numbers (eight more MMAs a block), which leaves the second.  The first is left in
 // dK, whose kernel runs after this one, and the second is taken out there: the exact delta makes every row of
 // dS sum to zero, so the row sums found here are added to delta.
-// A row that sees one key has P = 1, and delta is that key's dP: its dS is zero, not the difference of two orders of
-// summation.  It gets that delta for the kernel of dK and dV, whose dP is the same sum in the same order.
+// A row whose keys are one block has all of P and dP at hand: its delta is their sum in fp32 (short sequences, where
+// the rounding of `out` was 1.6 to 5 times dQ's own), and where it sees one key, that key's dP: P = 1, and dS is zero
+// (NaN where dP is not finite), not the difference of two orders of summation.  The kernel of dK and dV, whose dP is
+// the same sum in the same order, gets these deltas too.
 template <int DP> struct QShape {
     static constexpr int T_BYTES = tile_bytes<DP>();
     static constexpr int KS = 3, VS = 2;
@@ -1025,7 +1027,7 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
         mbar_init(smem_u32(&ctl->g_scores), 1);
         mbar_init(smem_u32(&ctl->ds_ready), BwdWarps::COUNT);
         mbar_init(smem_u32(&ctl->sum_ready), BwdWarps::COUNT);
-        mbar_init(smem_u32(&ctl->sum_read), 4);
+        mbar_init(smem_u32(&ctl->sum_read), BwdWarps::COUNT);
         mbar_init(smem_u32(&ctl->acc_full), 1);
         mbar_init(smem_u32(&ctl->acc_free), BwdWarps::COUNT);
         ctl->abort_flag = 0;
@@ -1157,9 +1159,55 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
         for (; ok && feed.take(it); ++items) {
             float2 *stats = p.row_stats + ((int64_t)it.tile * p.hk + it.h) * TILE + row;
             const float2 st = *stats;
-            float sum = 0.0f;                // of this part's dS
+            float sum = 0.0f, delta = st.y;  // sum: of this part's dS
             const int token = it.t0 + row_t, row_end = p.causal ? min(token + 1, it.len) : it.len;
-            const bool live = row < used && token < it.len;
+            const bool live = row < used && token < it.len, whole = it.nb == 1;
+            // The four parts' values of a row meet in `sums`: put in and, when all are there, added up.
+            auto put = [&](float v) {
+                ok = ok && wait_warp<true>(smem_u32(&ctl->sum_read), (items & 1) ^ 1, waits, SITE_EPI_EXCHANGE);
+                if (!ok) return;
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(sums + (part * TILE + row) * 4), "f"(v) : "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&ctl->sum_ready));
+            };
+            auto total = [&]() {
+                ok = ok && wait_warp<true>(smem_u32(&ctl->sum_ready), items & 1, waits, SITE_EPI_EXCHANGE);
+                if (!ok) return 0.0f;
+                float s4[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s4[k]) : "r"(sums + (k * TILE + row) * 4) : "memory");
+                return (s4[0] + s4[1]) + (s4[2] + s4[3]);
+            };
+            auto done = [&]() {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&ctl->sum_read));
+            };
+            if (whole) {                     // ahead of the loop, which sees the same phases and looks at P and dP again
+                ok = wait_warp<true>(smem_u32(&ctl->s_full[cnt & 1]), (cnt >> 1) & 1, waits, SITE_EPI_TMEM_FULL);
+                ok = ok && wait_warp<true>(smem_u32(&ctl->g_scores), cnt & 1, waits, SITE_EPI_TMEM_FULL);
+                if (!ok) break;
+                tc_fence_after();
+                float t = 0.0f, first = 0.0f;
+#pragma unroll 1
+                for (int c = c0; c < min(c0 + 32, mma_cols(it.end)); c += 16) {
+                    uint32_t x[16], y[16];
+                    tmem_ld16(tmem + lanes + (cnt & 1) * TILE + c, x);
+                    tmem_ld16(t_dp + lanes + c, y);
+                    tmem_ld_wait(x);
+                    tmem_ld_wait(y);
+                    if (c == 0) first = __uint_as_float(y[0]);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float v = fast_exp2(fmaf(__uint_as_float(x[e]), p.c2, -st.x)) * __uint_as_float(y[e]);
+                        t += c + e < row_end ? v : 0.0f;
+                    }
+                }
+                put(t);
+                delta = total();
+                if (!ok) break;
+                done();
+                if (row_end == 1) delta = first;
+            }
             for (int j = 0; j < it.nb; ++j, ++cnt) {
                 const int cols = mma_cols(it.end - j * TILE);
                 const bool mask = cols < TILE || j * TILE + TILE > (p.causal ? it.t0 + 1 : it.len);
@@ -1177,15 +1225,11 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
                     tmem_ld_wait(dp);
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
-                        float a = fast_exp2(fmaf(__uint_as_float(r[e]), p.c2, -st.x)) * (__uint_as_float(dp[e]) - st.y);
-                        float b = fast_exp2(fmaf(__uint_as_float(r[e + 1]), p.c2, -st.x)) * (__uint_as_float(dp[e + 1]) - st.y);
+                        float a = fast_exp2(fmaf(__uint_as_float(r[e]), p.c2, -st.x)) * (__uint_as_float(dp[e]) - delta);
+                        float b = fast_exp2(fmaf(__uint_as_float(r[e + 1]), p.c2, -st.x)) * (__uint_as_float(dp[e + 1]) - delta);
                         if (mask) {
                             a = e < limit ? a : 0.0f;
                             b = e + 1 < limit ? b : 0.0f;
-                        }
-                        if (e == 0 && row_end == 1) {        // dS is zero (NaN where dP is not finite); part 0's sum is the delta
-                            a *= 0.0f;
-                            sum = __uint_as_float(dp[0]);
                         }
                         sum += a + b;
                         hi[e / 2] = pack_bf16(a, b);
@@ -1203,22 +1247,14 @@ k_attention_bwd_q(const __grid_constant__ AtMaps tm, const AtParams p)
             ok = wait_warp<true>(smem_u32(&ctl->acc_full), items & 1, waits, SITE_EPI_TMEM_FULL);
             if (!ok) break;
             tc_fence_after();
-            // the parts' sums meet; part 0 puts the row's delta right for the kernel of dK and dV
-            ok = wait_warp<true>(smem_u32(&ctl->sum_read), (items & 1) ^ 1, waits, SITE_EPI_EXCHANGE);
-            if (!ok) break;
-            asm volatile("st.shared.f32 [%0], %1;" ::"r"(sums + (part * TILE + row) * 4), "f"(sum) : "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&ctl->sum_ready));
-            if (part == 0) {
-                ok = wait_warp<true>(smem_u32(&ctl->sum_ready), items & 1, waits, SITE_EPI_EXCHANGE);
+            // part 0 puts the row's delta right for the kernel of dK and dV
+            if (!whole) {
+                put(sum);
+                if (part == 0) delta += total();
                 if (!ok) break;
-                float s4[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s4[k]) : "r"(sums + (k * TILE + row) * 4) : "memory");
-                if (live) stats->y = row_end == 1 ? s4[0] : st.y + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&ctl->sum_read));
+                done();
             }
+            if (part == 0 && live) stats->y = delta;
             if (c0 < DP) {
                 uint32_t o[32];
                 tmem_ld32(t_dq + lanes + c0, o);
