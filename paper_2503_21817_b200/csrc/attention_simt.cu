@@ -1,7 +1,7 @@
 // Packed attention with plain fused multiply-adds (fp32, and bf16 as an on-device second opinion), and
 // the row statistics of the backward pass of both paths.  64 x 64 tiles in shared memory, 4 x 4 products per thread;
 // the same row tiles as the tensor-core kernels (the heads of a group are rows), half as high.  Measured in fp32:
-// backward of sequences of 33, 1 and 200 tokens, 8 / 2 heads, d = 64: 82 us (271 us with a CTA per tile instead of a
+// backward of sequences of 33, 1 and 200 tokens, 8 / 2 heads, d = 64: 85 us a call (271 us with a CTA per tile instead of a
 // cluster); bound by the latency of a tile's steps.
 #include <cooperative_groups.h>
 

@@ -7,11 +7,12 @@
 // tile rows: no atomics, equal calls give equal bits.  The gradients take two kernels and seven products where
 // one with atomic adds into dQ would take five; that buys a fixed order and no fp32 dQ buffer to clear and convert.
 //
-// Measured (B200, d = 128, 32 / 8 heads, causal; floor = flops at 1662 TFLOP/s):
-//   forward   1 x 16381 tokens  1.95 ms (1.13 PFLOP/s, floor 1.32 ms; at the 1000 W cap, SM clock 1.6 GHz)
-//             8 x 616 tokens    42 us   (floor 15.5 us)
-//   backward  16 documents, 26 k tokens  1.77 ms for 1.06 TFLOP (floor 0.64 ms; at the power cap)
-//             8 x 616 tokens    145 us  (row statistics 16, dQ 68, dK / dV 67 us)
+// Measured (B200, d = 128, 32 / 8 heads, causal; floor = flops at 1662 TFLOP/s; calls through the Python entry point on
+// changing inputs, in brackets replays of a captured graph on the same ones):
+//   forward   1 x 16381 tokens  2.02 ms (1.09 PFLOP/s, floor 1.32 ms; at the 1000 W cap, SM clock 1.6 GHz)
+//             8 x 616 tokens    47 us   [41] (floor 15.5 us)
+//   backward  16 documents, 26 k tokens  1.92 ms [1.80] for 1.06 TFLOP (floor 0.64 ms; at the power cap)
+//             8 x 616 tokens    167 us  [144, row statistics 16 of it]
 // What bounds them now: the round trips between a product and its arithmetic (forward: 3500 cycles per block and pair of
 // tiles for 2048 cycles of products; dK / dV: 3300 for 2048), and the power limit on long sequences.
 #include "attention.cuh"

@@ -6,8 +6,9 @@
 // HBM-bound: a row is read once into registers (16-byte loads, at most four per thread), the variance is
 // the mean of squared deviations (a second look at the registers, not E[x^2] - mean^2), and the backward
 // reads x and dy once for both its results.  Statistics and sums are fp32 in a fixed order (no atomics).
-// Measured (B200, bf16): forward 9376 x 4096 in 26.5 us (5.8 TB/s, 0.89 of the copy rate), 577 x 1024 in 3 us;
-// backward 4927 x 5120 in 41.3 us (3.7 TB/s; rows 37, partial sums 4): an SM has two rows at a time and 20 warps that
+// Measured (B200, bf16, replayed from a graph): forward 9376 x 4096 in 25.9 us (5.9 TB/s, 0.90 of the copy rate),
+// 577 x 1024 in 2.4 us; backward 4927 x 5120 in 40.4 us (3.7 TB/s; rows 36, partial sums 4; fp32 77 us, 3.9 TB/s, with 92
+// bytes spilled), 4096 x 6144, one row per SM, 45 us (3.4 TB/s): an SM has two rows at a time and 20 warps that
 // issue in 57 % of its cycles (latency of a row's chain: sums, barrier, results).  From 42.8 us, the next row's sums
 // before this row's results (44.5) did not help, nor half the shared-memory reads (42.5); partial sums with 32 lanes per
 // column instead of eight did (2 us less).
