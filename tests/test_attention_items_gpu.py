@@ -32,3 +32,31 @@ def test_several_items_per_sm_against_64_bits(lens, hq, hk, d, causal, items):
     assert min(_items(lens, hq, hk)) >= items > 148
     q, k, v, do, cu = _tensors(len(lens) + hq, lens, hq, hk, d, "bf16")
     _check(_object(cu, hq, hk, d, "bf16", causal), q, k, v, do, cu, d ** -0.5, causal, "bf16")
+
+
+def test_calls_of_one_object_at_once_on_two_streams():
+    # both streams always have work, of this object and of the layer norm; each call has its own scratch
+    import torch
+    import paper_2503_21817_b200 as sk
+    lens, hq, hk, d = (300, 41, 577, 128, 5), 8, 2, 64
+    q, k, v, do, cu = _tensors(41, lens, hq, hk, d, "bf16")
+    a = _object(cu, hq, hk, d, "bf16")
+    gamma = torch.ones(hq * d, dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        out, lse = a.forward(q, k, v)
+        y, mean, rstd = sk.layernorm_forward(out.view(len(out), -1), gamma)
+        dx, dgamma, dbeta = sk.layernorm_backward(do.view(len(out), -1), out.view(len(out), -1), gamma, mean, rstd)
+        return (out, lse, y, dx, dgamma, dbeta, *a.backward(dx.view_as(out), q, k, v, out, lse))
+
+    want = step()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(25):
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append(step())
+    torch.cuda.synchronize()
+    a.poll()
+    assert all(torch.equal(x, y) for g in got for x, y in zip(g, want))
