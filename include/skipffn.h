@@ -283,8 +283,8 @@ skipffn_status skipffn_token_merge_poll(void *scratch, int64_t n, int32_t C, int
  * nor the scratch any of them (EINVAL).
  * bf16: tensor-core kernels with fp32 accumulation; scores, softmax statistics and gradients of the
  * scores are fp32, P and dS are rounded to bf16 as operands of the second products (dS of dq is the sum of two
- * bf16 numbers), results once; delta = sum_j p_j dp_j is summed in fp32 for rows whose keys are one block of 128, and
- * comes from the rounded `out` for the others.
+ * bf16 numbers), results once; delta = sum_j p_j dp_j is summed in fp32 for rows whose keys are one block of 128 (plain
+ * FMA: 64), and comes from the rounded `out` for the others.
  * fp32, or path = SIMT: plain FMA.  All sums have a fixed order: equal calls give equal bits.
  * A non-finite value spreads inside its own sequence only (a later token's inf or NaN in v, k, q or
  * dout can reach earlier tokens' results there: 0 * inf is not masked); it never reaches another sequence.

@@ -200,8 +200,9 @@ k_attention_fwd_simt(const AttnArgs a)
     }
 }
 
-// P and dS of one 64 x 64 tile into shared memory (rows = queries, columns = keys).  The delta of a row that sees one
-// key is that key's dP: its dS is zero (NaN where dP is not finite), not what two orders of summation differ by.
+// P and dS of one 64 x 64 tile into shared memory (rows = queries, columns = keys).  Where a row's keys are this one
+// tile its delta is summed here, without the rounding of a bf16 `out`; that of a row that sees one key is this key's dP:
+// its dS is zero (NaN where dP is not finite), not what two orders of summation differ by.
 __device__ __forceinline__ void grad_tile(float *ps, float *ds, const float *qs, const float *gs, const float *ks, const float *vs,
                                           const float2 *stats, const AttnArgs &a, int t0, int len, int k0, Tile t)
 {
@@ -209,17 +210,25 @@ __device__ __forceinline__ void grad_tile(float *ps, float *ds, const float *qs,
     rows_rows(s, qs, ks, a.d, t);
     rows_rows(dp, gs, vs, a.d, t);
     const float c2 = a.scale * LOG2E;
+    const bool whole = (a.causal ? min(t0 + a.tokens, len) : len) <= SK;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = 4 * t.ty + i, row_end = a.causal ? min(t0 + r / a.group + 1, len) : len;
         const float2 st = stats[r];
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool on = k0 + t.tx + 16 * j < row_end;
+            s[i][j] = on ? exp2f(fmaf(s[i][j], c2, -st.x)) : 0.0f;
+            if (!on) dp[i][j] = 0.0f;
+            sum = fmaf(s[i][j], dp[i][j], sum);
+        }
+        const float delta = whole ? half_warp_sum(sum) : st.y;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int c = t.tx + 16 * j;
-            const bool on = k0 + c < row_end;
-            const float p = on ? exp2f(fmaf(s[i][j], c2, -st.x)) : 0.0f;
-            ps[r * PPITCH + c] = p;
-            ds[r * PPITCH + c] = on ? p * (dp[i][j] - (row_end == 1 ? dp[i][j] : st.y)) : 0.0f;
+            ps[r * PPITCH + c] = s[i][j];
+            ds[r * PPITCH + c] = k0 + c < row_end ? s[i][j] * (dp[i][j] - (row_end == 1 ? dp[i][j] : delta)) : 0.0f;
         }
     }
 }

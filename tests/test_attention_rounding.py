@@ -81,19 +81,21 @@ def test_errors_in_fp32(lens, hq, hk, d, scale, causal):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("lens,hq,hk,d,causal", [
-    ((6,), 64, 8, 128, True), ((6,) * 30, 8, 1, 64, True), ((3,) * 50, 12, 4, 64, False), ((1, 2) * 40, 16, 16, 64, True),
-    ((40,), 32, 8, 128, True), ((128, 17, 100), 10, 2, 96, False), ((64, 128, 1, 33), 4, 4, 40, True),
+@pytest.mark.parametrize("lens,hq,hk,d,causal,path", [
+    ((6,), 64, 8, 128, True, 0), ((6,) * 30, 8, 1, 64, True, 0), ((3,) * 50, 12, 4, 64, False, 0), ((1, 2) * 40, 16, 16, 64, True, 0),
+    ((40,), 32, 8, 128, True, 0), ((128, 17, 100), 10, 2, 96, False, 0), ((64, 128, 1, 33), 4, 4, 40, True, 0),
+    ((6,) * 30, 8, 1, 64, True, 1), ((3,) * 50, 12, 4, 64, False, 1), ((40, 64, 17), 8, 2, 128, True, 1), ((64, 1, 33), 3, 3, 40, False, 1),
 ])
-def test_query_gradient_of_short_sequences_is_off_by_its_own_rounding(lens, hq, hk, d, causal):
-    # sequences of at most one block of keys: delta is summed from P and dP in fp32, dS enters as two bf16 numbers (2^-16),
-    # so that dq is the exact gradient, rounded once.  Its error is that rounding's, up to the share that fp32 sums
-    # and the exponential add (under 2^-16 of the terms of dS, which cancel to a tenth in the worst row: 2e-4 in all)
+def test_query_gradient_of_short_sequences_is_off_by_its_own_rounding(lens, hq, hk, d, causal, path):
+    # sequences of at most one block of keys (128, on plain FMA 64): delta is summed from P and dP in fp32, dS enters as
+    # two bf16 numbers (2^-16), so that dq is the exact gradient, rounded once.  Its error is that rounding's, up to the
+    # share that fp32 sums and the exponential add (under 2^-16 of the terms of dS, which cancel to a tenth in the worst
+    # row: 2e-4 in all)
     from gpu_util import to_host
     from test_attention_gpu import _object
     t, cu = _host_case(lens, hq, hk, d)
     q, k, v, do = (x.cuda() for x in t)
-    a = _object(cu, hq, hk, d, "bf16", causal)
+    a = _object(cu, hq, hk, d, "bf16", causal, path=path)
     out, lse = a.forward(q, k, v)
     dq = to_host(a.backward(do, q, k, v, out, lse)[0])
     a.poll()
