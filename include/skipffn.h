@@ -349,6 +349,130 @@ skipffn_status skipffn_kv_compact(const skipffn_saved *saved, const void *src, v
                                   const int32_t *cu_seqlens, int32_t n_seq,
                                   int32_t *kept_cu_seqlens, void *stream);
 
+/* Paged key / value cache: what a decoder answers from after its prompt.  Rows (one per token and kv head) stand in pages of
+ * `page_size` rows; a table per sequence lists its pages in order, so row j of sequence s is row j % page_size of page
+ * page_table[s][j / page_size].  Needs no handle; the caller owns every array and keeps it alive for the call.
+ *   k_pages, v_pages : device; row r of page p, head h starts at element p * page_stride + r * row_stride + h *
+ *                      head_stride of either (head_dim contiguous elements).  Any order of pages, rows and heads in
+ *                      memory, and keys and values interleaved at any level, as long as no two rows share a byte (EINVAL).
+ *                      Bases and strides are multiples of 16 bytes.
+ *   page_table       : device int32 [n_seq, table_stride], table_width entries of each row are read
+ *   cu_new           : device int32 [n_seq + 1], ascending, first 0: the new tokens of each sequence in this call's arrays
+ *   lens             : device int32 [n_seq]: rows of each sequence, its new tokens among them as the last ones
+ *   max_new          : bound of the new tokens of one sequence, known on the host
+ *   status           : device int32 [SKIPFFN_PAGED_STATUS_WORDS], zeroed once by the caller
+ * The three integer arrays may change between a call's launch and the next, so captured calls follow them.  They are not
+ * trusted: offsets outside the call's tokens, lengths beyond the table, more than max_new new tokens, page numbers
+ * outside 0 .. n_pages - 1 never lead to an access outside the arrays; such a sequence (or page) is left out or cut, and
+ * skipffn_paged_poll reports SKIPFFN_EINVAL with the site of one of the faults: 64 offsets, 65 length, 66 page, 67 no room for a row,
+ * 68 more rows than weights.
+ * head_dim is a multiple of 8 up to 128, page_size a multiple of 8, heads_q / heads_kv at most 64, else EUNSUPPORTED.
+ * All sums have a fixed order: equal calls give equal bits. */
+#define SKIPFFN_PAGED_STATUS_WORDS 64
+typedef struct {
+    int32_t heads_kv, head_dim;
+    int32_t dtype;           /* skipffn_dtype of the pages, and of the call's other arrays */
+    int32_t path;            /* skipffn_path */
+    int32_t page_size;
+    int32_t n_seq, table_width, max_new;
+    int64_t n_pages;
+    void *k_pages, *v_pages;
+    int64_t page_stride, row_stride, head_stride;   /* elements */
+    const int32_t *page_table;
+    int64_t table_stride;
+    const int32_t *cu_new, *lens;
+    int32_t *status;
+} skipffn_paged_cache;
+
+/* Attention of the new tokens over the cache, their own rows included: with n new tokens and `len` rows, token i of a
+ * sequence sees rows 0 .. len - n + i,
+ *     s_ij = scale q_i . k_j,  out_i = sum_j softmax_j(s_ij) v_j,  lse_i = log sum_j exp(s_ij),
+ * query head h with kv head h / (heads_q / heads_kv).  q, out: [n, heads_q, head_dim], contiguous heads, token strides ld*
+ * in elements (multiples of 16 bytes); lse: [n, heads_q] fp32.  A token that sees no row has out 0 and lse minus
+ * infinity.  Rows of q behind the last sequence are neither read nor written.  Outputs and scratch must not overlap each
+ * other, q or the cache (EINVAL).  scratch: device memory of skipffn_paged_attention_scratch_bytes(...) bytes, 16-byte
+ * aligned, used by this call only.
+ * Statistics and sums are fp32; bf16: the softmax weights are rounded to bf16 as operands of the second product, results once.
+ * What stands in the cache past a sequence's rows (unwritten memory, NaN) does not reach its results; inside a sequence a
+ * non-finite value of a new token can reach earlier tokens of the same call (0 * inf). */
+size_t skipffn_paged_attention_scratch_bytes(const skipffn_paged_cache *cache, int32_t heads_q, int64_t n);
+skipffn_status skipffn_paged_attention(const skipffn_paged_cache *cache, int32_t heads_q, float scale, int64_t n, const void *q,
+                                       int64_t ldq, void *out, int64_t ldo, float *lse, void *scratch, size_t scratch_bytes,
+                                       void *stream);
+
+/* Weight that the new tokens give to every row of the cache, per kv head: with q and lse of skipffn_paged_attention,
+ *     weights[s, h, j] = prior[s, h, j] + sum over new tokens i that see row j, and query heads g of kv head h,
+ *                        of exp(scale q_ig . k_j - lse_ig)                                    for j < lens[s], else 0.
+ * prior, weights: [n_seq, heads_kv, width] fp32; prior may be NULL (zero) or weights itself, else no overlap (EINVAL).
+ * Tokens whose lse is minus infinity give nothing.  n_seq is at most 65535 (EUNSUPPORTED).  All arithmetic fp32. */
+skipffn_status skipffn_paged_weights(const skipffn_paged_cache *cache, int32_t heads_q, float scale, int64_t n, const void *q,
+                                     int64_t ldq, const float *lse, const float *prior, float *weights, int32_t width, void *stream);
+
+/* Eviction: of every sequence and kv head with more than `budget` rows, keep the first `sinks`, the last `recent`, and of
+ * the others those with the largest weights, `budget` in all (sinks + recent <= budget, else EINVAL; equal weights: the
+ * lower row; NaN below everything); sequences of up to `budget` rows keep all.  The kept rows move, in their order, to the
+ * front of `into`'s pages (its page_table; the same heads, head_dim, dtype and n_seq; its cu_new and lens are not used),
+ * or of their own with into = NULL.  `into` must name other pages than `cache`, and a page that in-place eviction
+ * changes must not be another sequence's; neither is checked.
+ *   weights     : [n_seq, heads_kv, width] fp32
+ *   kept        : [n_seq, heads_kv, budget] int32 out, ascending former rows, -1 past the rows kept
+ *   lens_out    : [n_seq] int32 out, min(lens, budget)
+ *   weights_out : [n_seq, heads_kv, budget] fp32 out, the kept rows' weights, 0 past them
+ * cu_new and max_new are not used. */
+skipffn_status skipffn_paged_evict(const skipffn_paged_cache *cache, const skipffn_paged_cache *into, const float *weights,
+                                   int32_t width, int32_t budget, int32_t sinks, int32_t recent, int32_t *kept, int32_t *lens_out,
+                                   float *weights_out, void *stream);
+
+/* Writes rows of k and v ([n, heads_kv, head_dim], token strides in elements) into the cache: the new tokens of each
+ * sequence are its last rows.  The keys as they are; skipffn_rotary_append turns them first. */
+skipffn_status skipffn_paged_append(const skipffn_paged_cache *cache, int64_t n, const void *k, int64_t ldk, const void *v,
+                                    int64_t ldv, void *stream);
+
+/* Synchronises `stream` and reports (and clears) what a kernel found wrong with the integer arrays, see above. */
+skipffn_status skipffn_paged_poll(const skipffn_paged_cache *cache, void *stream, int32_t *site_out);
+
+/* Queries and keys normalised per head and rotated by position, in one pass:
+ *     n = x / sqrt(mean x^2 + eps) * gamma   (gamma NULL: n = x),
+ *     pair (a, b) of columns of n -> (a cos t - b sin t, b cos t + a sin t),  t = position[axis of the pair] * inv_freq
+ * Pair p of the rotary_dim / 2 pairs is columns (p, p + rotary_dim / 2), or (2p, 2p + 1) with interleaved = 1; columns
+ * from rotary_dim on are normalised only.  Every pair has its own frequency and one of up to four position axes
+ * (text: one; images and video: time, height, width).
+ *   inv_freq, axis : HOST arrays [rotary_dim / 2], copied at creation; radians per position; axis may be NULL (all 0)
+ *   head_dim       : a multiple of 8 up to 256;  rotary_dim : a multiple of 8 up to head_dim, 0 for no rotation
+ * A handle is host memory only and read-only: calls on any stream and device may share it.
+ * Angles are reduced modulo one turn exactly, so far positions are as accurate as near ones; any int32 position is legal.
+ *   q, k, results  : [n, heads, head_dim], contiguous heads, token strides in elements (multiples of 16 bytes)
+ *   positions      : device int32 [axes, ldpos], ldpos >= n
+ *   gamma_q, gamma_k : [head_dim], both or neither
+ * forward: a result may stand on its own input; backward (q, k: the forward's inputs; d*_out: gradients of its results): a
+ * gradient may stand on the upstream one or on the input; other overlaps are EINVAL.  dgamma_*: in dtype, fp32 with
+ * dw_fp32, overwritten, either may be NULL; scratch (only with gammas): skipffn_rotary_scratch_bytes(handle) bytes.
+ * append: the rotated keys and the values go to the rows of the cache that the new tokens are (cache->dtype is the dtype
+ * of the call), the rotated queries to q_out; tokens behind the last sequence are left alone.
+ * Arithmetic is fp32 in a fixed order, results are rounded once. */
+typedef struct {
+    int32_t heads_q, heads_kv, head_dim, rotary_dim;
+    int32_t interleaved, axes;
+    const double *inv_freq;
+    const int32_t *axis;
+    float eps;
+} skipffn_rotary_config;
+typedef struct skipffn_rotary skipffn_rotary;
+skipffn_status skipffn_rotary_create(skipffn_rotary **rotary, const skipffn_rotary_config *cfg);
+void skipffn_rotary_destroy(skipffn_rotary *rotary);
+skipffn_status skipffn_rotary_forward(const skipffn_rotary *rotary, int32_t dtype, int64_t n, const void *q, int64_t ldq, const void *k,
+                                      int64_t ldk, const int32_t *positions, int64_t ldpos, const void *gamma_q, const void *gamma_k,
+                                      void *q_out, int64_t ldqo, void *k_out, int64_t ldko, void *stream);
+size_t skipffn_rotary_scratch_bytes(const skipffn_rotary *rotary);
+skipffn_status skipffn_rotary_backward(const skipffn_rotary *rotary, int32_t dtype, int64_t n, const void *dq_out, int64_t lddqo,
+                                       const void *dk_out, int64_t lddko, const void *q, int64_t ldq, const void *k, int64_t ldk,
+                                       const int32_t *positions, int64_t ldpos, const void *gamma_q, const void *gamma_k, void *dq,
+                                       int64_t lddq, void *dk, int64_t lddk, void *dgamma_q, void *dgamma_k, int32_t dw_fp32,
+                                       void *scratch, size_t scratch_bytes, void *stream);
+skipffn_status skipffn_rotary_append(const skipffn_rotary *rotary, const skipffn_paged_cache *cache, int64_t n, const void *q, int64_t ldq,
+                                     const void *k, int64_t ldk, const void *v, int64_t ldv, const int32_t *positions, int64_t ldpos,
+                                     const void *gamma_q, const void *gamma_k, void *q_out, int64_t ldqo, void *stream);
+
 /* Device addresses of the compacted intermediates of the last forward / backward, each
  * [Nk, I] in cfg.dtype (rows Nk .. round_up(Nk,16)-1 are zero, later rows are unspecified):
  * which = 0 G, 1 U, 2 H, 3 dG, 4 dU;

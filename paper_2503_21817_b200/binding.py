@@ -26,7 +26,10 @@ EXPORTS = ["skipffn_workspace_bytes", "skipffn_saved_create", "skipffn_saved_des
            "skipffn_token_merge_poll", "skipffn_schedule_plan_segment", "skipffn_attention_plan_bytes",
            "skipffn_attention_create", "skipffn_attention_destroy", "skipffn_attention_forward",
            "skipffn_attention_scratch_bytes", "skipffn_attention_backward", "skipffn_attention_poll", "skipffn_attention_tune",
-           "skipffn_layernorm_forward", "skipffn_layernorm_scratch_bytes", "skipffn_layernorm_backward"]
+           "skipffn_layernorm_forward", "skipffn_layernorm_scratch_bytes", "skipffn_layernorm_backward",
+           "skipffn_rotary_create", "skipffn_rotary_destroy", "skipffn_rotary_forward", "skipffn_rotary_scratch_bytes",
+           "skipffn_rotary_backward", "skipffn_rotary_append", "skipffn_paged_append", "skipffn_paged_attention_scratch_bytes",
+           "skipffn_paged_attention", "skipffn_paged_weights", "skipffn_paged_evict", "skipffn_paged_poll"]
 STATIC_MAX_TOKENS = 65536   # SKIPFFN_STATIC_MAX_TOKENS
 
 TUNABLES = {"tile_n": 0, "streamk": 1, "stages": 2, "lose_handover": 3, "one_box": 4, "tma_stores": 5, "gather": 6,
@@ -149,6 +152,8 @@ def load_library() -> ctypes.CDLL:
     lib.skipffn_layernorm_backward.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
     lib.skipffn_strerror.restype = ctypes.c_char_p
     lib.skipffn_strerror.argtypes = [i32]
+    from . import cache
+    cache.bind(lib)
     _lib = lib
     return lib
 

@@ -1,0 +1,245 @@
+"""Attention over a paged cache and the weights of its rows on the GPU against their fp64 statements."""
+import numpy as np
+import pytest
+
+from cache_util import Batch, normal, within
+from gpu_util import to_host
+from oracle import cache as oc
+
+pytestmark = pytest.mark.gpu
+
+CASES = [
+    # new, lens, hq, hk, d, page
+    ((1,), (1,), 4, 1, 128, 16),                            # one token, one row
+    ((1, 1, 1, 1), (15, 16, 17, 64), 8, 2, 128, 16),        # around a page and a block
+    ((1, 1, 1), (63, 65, 300), 2, 2, 64, 8),
+    ((1, 0, 1, 0), (5, 7, 0, 0), 4, 2, 64, 24),             # nothing new; no rows at all; pages of 24 rows
+    ((3, 1, 4), (2, 1, 40), 4, 2, 64, 8),                   # more new tokens than rows: the first see nothing
+    ((2, 5, 3), (130, 70, 9), 8, 2, 128, 32),               # 20 rows: two groups of warps
+    ((9, 16, 1), (200, 16, 77), 8, 2, 96, 16),              # 64 rows, 96 columns
+    ((1, 1), (90, 400), 40, 1, 128, 64),                    # one kv head for 40
+    ((1, 1), (90, 129), 64, 1, 40, 16),                     # a group of 64, 40 columns
+    ((1,), (5000,), 8, 2, 80, 16),                          # one sequence over all SMs, 80 columns
+    ((1,) * 150, tuple(1 + 37 * i % 200 for i in range(150)), 4, 2, 64, 16),   # more sequences than threads of a CTA
+    ((17,), (17,), 8, 2, 128, 16),                          # a chunk that is the whole prompt
+    ((100, 1, 33, 0, 1), (300, 50, 33, 10, 700), 8, 2, 128, 16),   # chunks and single tokens
+    ((300,), (1100,), 12, 4, 64, 48),                       # pages that end inside a tile
+    ((130, 70), (130, 200), 4, 4, 128, 128),
+    ((128, 129, 127), (128, 129, 400), 2, 2, 64, 64),       # around a tile of one head
+    ((70, 40), (71, 45), 10, 2, 80, 16),                    # groups of 5
+    ((50, 60), (20, 60), 4, 2, 128, 8),                     # a chunk whose first tokens see nothing
+    ((20,), (100,), 64, 1, 32, 16),
+]
+
+
+@pytest.mark.parametrize("dtype,path", [("bf16", 0), ("bf16", 1), ("fp32", 0)])
+@pytest.mark.parametrize("new,lens,hq,hk,d,page", CASES)
+def test_attention_and_weights_against_64_bits(new, lens, hq, hk, d, page, dtype, path):
+    import torch
+    x = Batch(sum(lens), new, lens, hq, hk, d, page, dtype, path=path)
+    out, lse = x.cache.attention(x.q)
+    x.cache.poll()
+    r_out, r_lse, e_out, e_lse = x.want()
+    within(out, r_out, e_out, "out")
+    within(lse, r_lse, e_lse, "lse")
+    width = max(lens) + 5
+    prior = torch.rand(len(lens), hk, width, device="cuda")
+    w = x.cache.weights(x.q, lse, prior=prior)
+    x.cache.poll()
+    r_w, e_w = oc.weights(to_host(x.q), x.keys, to_host(lse), x.cu, lens, hk, x.scale, width, to_host(prior))
+    within(w, r_w, e_w, "weights")
+    # the same bits again, weights over their prior
+    out2, lse2 = x.cache.attention(x.q)
+    w2 = x.cache.weights(x.q, lse, prior=prior, out=prior)
+    assert torch.equal(out, out2) and torch.equal(lse, lse2) and torch.equal(w, w2) and w2 is prior
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("order", ["page,head,row", "pages of both", "rows of both"])
+def test_memory_orders_of_the_pages(order, dtype):
+    for new, lens in (((1, 1, 2), (70, 9, 130)), ((40, 1, 2), (70, 9, 130))):
+        x = Batch(1, new, lens, 8, 2, 64, 16, dtype, order)
+        out, lse = x.cache.attention(x.q)
+        r_out, r_lse, e_out, e_lse = x.want()
+        within(out, r_out, e_out, "out")
+        r_w, e_w = oc.weights(to_host(x.q), x.keys, to_host(lse), x.cu, lens, 2, x.scale, 130)
+        within(x.cache.weights(x.q, lse, width=130), r_w, e_w, "weights")
+        x.cache.poll()
+
+
+@pytest.mark.parametrize("dtype,path", [("bf16", 0), ("bf16", 1), ("fp32", 0)])
+def test_large_scores_and_other_scales(dtype, path):
+    # scores up to some hundreds: the running maximum moves block by block, the sums must follow
+    for new, lens in (((1, 3), (400, 129)), ((40, 100), (400, 129))):
+        x = Batch(2, new, lens, 8, 2, 64, 16, dtype, path=path)
+        for scale in (2.0, 0.01):
+            out, lse = x.cache.attention(x.q, scale=scale)
+            r_out, r_lse, e_out, e_lse = x.want(scale)
+            within(out, r_out, e_out, "out")
+            within(lse, r_lse, e_lse, "lse")
+
+
+@pytest.mark.parametrize("dtype,path", [("bf16", 0), ("bf16", 1), ("fp32", 0)])
+@pytest.mark.parametrize("new", [(1, 2, 1), (60, 2, 1), (60, 33, 40)])
+def test_neighbours_unowned_rows_and_rows_behind_the_batch(new, dtype, path):
+    # what no row of a sequence owns is NaN from the start; here the neighbours' rows become it too
+    import torch
+    lens, pad = (90, 45, 130), 5
+    x = Batch(3, new, lens, 8, 2, 64, 24, dtype, pad=pad, path=path)
+    n = x.cu[-1]
+    out, lse = x.cache.attention(x.q)
+    w = x.cache.weights(x.q, lse.nan_to_num(0.0), width=130)
+    for s in (0, 2):
+        for p in x.table[s][x.table[s] >= 0]:
+            x.k[int(p)] = float("inf")
+            x.v[int(p)] = float("nan")
+    x.q[:x.cu[1]] = float("nan")
+    x.q[x.cu[2]:] = float("nan")
+    out2, lse2 = x.cache.attention(x.q, out=torch.full_like(out, 7.0), lse=torch.full_like(lse, 7.0))
+    w2 = x.cache.weights(x.q, lse.nan_to_num(0.0), width=130)
+    x.cache.poll()
+    a, b = x.cu[1], x.cu[2]
+    assert torch.equal(out[a:b], out2[a:b]) and torch.equal(lse[a:b], lse2[a:b]) and torch.equal(w[1], w2[1])
+    assert bool((out2[n:] == 7.0).all()) and bool((lse2[n:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_lengths_offsets_and_pages_that_follow_a_replayed_graph(dtype):
+    import torch
+    hq, hk, d, page = 8, 2, 64, 16
+    for new, lens, new2, lens2 in (((1, 1, 1), (40, 100, 7), (1, 1, 1), (41, 101, 8)), ((50, 1, 0), (90, 100, 7), (2, 48, 1), (41, 101, 8))):
+        a, b = (Batch(s, m, l, hq, hk, d, page, dtype, max_new=50) for s, m, l in ((4, new, lens), (5, new2, lens2)))
+        x = Batch(4, new, lens, hq, hk, d, page, dtype, max_new=50)
+        x.cache.attention(x.q)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out, lse = x.cache.attention(x.q)
+        for y in (a, b, a):
+            pages = min(x.k.shape[0], y.k.shape[0])
+            assert max(y.table.max(), 0) < pages and y.table.shape == x.table.shape and y.q.shape == x.q.shape
+            x.k[:pages].copy_(y.k[:pages]), x.v[:pages].copy_(y.v[:pages]), x.q.copy_(y.q)
+            x.d_table.copy_(y.d_table), x.d_cu.copy_(y.d_cu), x.d_lens.copy_(y.d_lens)
+            graph.replay()
+            r_out, r_lse, e_out, e_lse = y.want()
+            within(out, r_out, e_out, "out")
+            within(lse, r_lse, e_lse, "lse")
+        x.cache.poll()
+
+
+@pytest.mark.parametrize("new", [(1, 1, 2), (70, 1, 40)])
+def test_calls_on_two_streams_at_once_and_two_graphs(new):
+    import torch
+    x = Batch(6, new, (3000, 900, 2000), 8, 2, 128, 16)
+    q2 = normal(77, *x.q.shape)
+    want = [x.cache.attention(q) for q in (x.q, q2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    res = []
+    for _ in range(4):
+        for s, q in zip(streams, (x.q, q2)):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                res.append(x.cache.attention(q))
+    torch.cuda.synchronize()
+    for i, (out, lse) in enumerate(res):
+        assert torch.equal(out, want[i % 2][0]) and torch.equal(lse, want[i % 2][1])
+    graphs = []
+    for q in (x.q, q2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            r = x.cache.attention(q)
+        graphs.append((g, r))
+    for _ in range(3):
+        for s, (g, r) in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for (g, r), w in zip(graphs, want):
+        assert torch.equal(r[0], w[0]) and torch.equal(r[1], w[1])
+    x.cache.poll()
+
+
+@pytest.mark.parametrize("dtype,path", [("bf16", 0), ("bf16", 1), ("fp32", 0)])
+@pytest.mark.parametrize("new", [(1, 2, 1), (60, 33, 40)])
+def test_wrong_integers_are_reported_and_leave_the_other_sequences_alone(new, dtype, path):
+    import torch
+    import paper_2503_21817_b200 as sk
+    lens = (90, 45, 130)
+    x = Batch(7, new, lens, 4, 2, 64, 16, dtype, path=path)      # the table's unused entries are -1
+    out, lse = x.cache.attention(x.q)
+    w = x.cache.weights(x.q, lse, width=130)
+    good = x.d_table.clone(), x.d_cu.clone(), x.d_lens.clone()
+    a, b = x.cu[1], x.cu[2]
+
+    def again(site, which=(0, 2), weigh=True):
+        o, l = x.cache.attention(x.q, out=torch.zeros_like(out), lse=torch.zeros_like(lse))
+        with pytest.raises(sk.SkipFFNError, match=f"site {site}"):
+            x.cache.poll()
+        if weigh:
+            w2 = x.cache.weights(x.q, lse, width=130)
+            with pytest.raises(sk.SkipFFNError, match=f"site {site}"):
+                x.cache.poll()
+        x.cache.poll()
+        for s in which:
+            r = slice(x.cu[s], x.cu[s + 1])
+            assert torch.equal(o[r], out[r]) and torch.equal(l[r], lse[r])
+            assert not weigh or torch.equal(w2[s], w[s])
+        for t, g in zip((x.d_table, x.d_cu, x.d_lens), good):
+            t.copy_(g)
+
+    for page in (-1, -2 ** 31, x.k.shape[0], 2 ** 31 - 1):       # a page that does not exist
+        x.d_table[1, 1] = page
+        again(66)
+    for length in (-3, 10 ** 6, 2 ** 31 - 1):                    # lengths that the table has no room for
+        x.d_lens[1] = length
+        again("65" if length < 0 else "6[56]")                   # cut to the table's width it reaches pages that are not there, too
+    x.d_cu[3] = 2 ** 31 - 1                                      # offsets past the call's tokens
+    again(64, (0, 1))
+    x.d_cu[1] = -5                                               # descending
+    again(64, (2,))
+    x.d_cu.copy_(torch.tensor([0, 0, 0, x.cu[-1]], dtype=torch.int32))   # more new tokens than max_new
+    if x.cu[-1] > max(new):
+        again(64, ())
+    else:
+        x.d_cu.copy_(good[1])
+
+
+def test_weights_of_more_rows_than_their_width_are_reported():
+    import paper_2503_21817_b200 as sk
+    x = Batch(8, (1,), (50,), 2, 2, 64, 16)
+    _, lse = x.cache.attention(x.q)
+    full = x.cache.weights(x.q, lse, width=64)
+    x.cache.poll()
+    part = x.cache.weights(x.q, lse, width=20)
+    with pytest.raises(sk.SkipFFNError, match="site 68"):
+        x.cache.poll()
+    assert bool((part == full[..., :20]).all())
+
+
+def test_long_cache_rows_against_64_bits():
+    x = Batch(9, (1, 70), (70001, 9000), 4, 1, 128, 64)
+    out, lse = x.cache.attention(x.q)
+    x.cache.poll()
+    r_out, r_lse, e_out, e_lse = x.want()
+    within(out, r_out, e_out, "out")
+    within(lse, r_lse, e_lse, "lse")
+
+
+def test_a_key_that_scores_minus_infinity_has_probability_zero():
+    import torch
+    for new in ((1,), (40,)):
+        x = Batch(10, new, (200,), 2, 1, 64, 16)
+        x.q.abs_()
+        page = x.d_table[0].long()
+        for j in (*range(0, 64), 100, 150):
+            x.k[page[j // 16], j % 16] = float("-inf")
+        x.keys[0][[*range(0, 64), 100, 150]] = -1e30
+        out, lse = x.cache.attention(x.q)
+        n = new[0]
+        k, v, q = x.keys[0][:, 0], x.values[0][:, 0], to_host(x.q)
+        for i in range(n):
+            for h in range(2):
+                s = x.scale * (k[:200 - n + i + 1] @ q[i, h])
+                p = np.exp(s - s.max())
+                p /= p.sum()
+                assert np.allclose(to_host(out)[i, h], p @ v[:p.size], atol=2.0 ** -7 * np.abs(v).max())
