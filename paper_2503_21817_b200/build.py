@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libskipffn.so")
 # the same library with per-role cycle counters in the tensor-core GEMM kernels (bench.py --role-cycles)
 LIB_ROLE_CYCLES = os.path.join(HERE, "libskipffn_role_cycles.so")
 SOURCES = ["api.cu", "attention.cu", "attention_simt.cu", "attention_tc.cu", "compact.cu", "compact_static.cu", "kvcache.cu",
-           "layernorm.cu", "merge.cu", "paged.cu", "paged_evict.cu", "paged_few.cu", "paged_simt.cu", "paged_weights.cu", "prenorm.cu", "rotary.cu",
+           "layernorm.cu", "merge.cu", "paged.cu", "paged_evict.cu", "paged_few.cu", "paged_simt.cu", "paged_tc.cu", "paged_weights.cu", "prenorm.cu", "rotary.cu",
            "simt.cu", "summary.cu", "umma.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC"]

@@ -44,7 +44,7 @@ skipffn_status paged_view(const skipffn_paged_cache *c, int64_t N, PagedView *v)
     v->table = c->page_table; v->cu = c->cu_new; v->lens = c->lens;
     v->table_stride = c->table_stride; v->n_pages = c->n_pages;
     v->n_seq = c->n_seq; v->heads = c->heads_kv; v->d = c->head_dim;
-    v->capacity = (int32_t)std::min<int64_t>((int64_t)c->table_width * c->page_size, INT_MAX - 4096);
+    v->capacity = c->n_pages == 0 ? 0 : (int32_t)std::min<int64_t>((int64_t)c->table_width * c->page_size, INT_MAX - 4096);
     v->N = N; v->max_new = c->max_new;
     v->page = make_divisor((uint32_t)c->page_size);
     v->status = c->status;
@@ -241,8 +241,10 @@ Scratch scratch_of(const skipffn_paged_cache *c, int group, int64_t N)
 {
     const int64_t most = std::min<int64_t>(c->max_new, N) * group;
     const bool few = !simt(c) && most <= 64;
-    const int64_t rows = simt(c) ? PG_SIMT_ROWS : few ? few_rows(most) : std::max(64, PG_SIMT_ROWS);
-    const int64_t tile = PG_SIMT_ROWS;
+    // the largest of the kernels that the call may launch
+    const int64_t slots = std::max<int64_t>(PG_MAX_RUNS * (simt(c) ? PG_SIMT_ROWS : few_rows(std::min<int64_t>(most, 64))),
+                                            simt(c) || few ? 0 : PG_TC_RUNS * PG_TC_ROWS);
+    const int64_t tile = simt(c) ? PG_SIMT_ROWS : 2 * (128 / group) * group;
     const int64_t pitch = !simt(c) && c->head_dim <= 64 ? 64 : 128;
     Scratch s;
     s.max_tiles = few ? 0 : N * group / tile + c->n_seq + 1;
@@ -252,8 +254,8 @@ Scratch scratch_of(const skipffn_paged_cache *c, int group, int64_t N)
     s.head = take(64);
     s.seq_tiles = take(((size_t)c->n_seq + 1) * 4);
     s.tiles = take((size_t)s.max_tiles * sizeof(PagedTile));
-    s.ml = take((size_t)2 * PG_MAX_RUNS * rows * sizeof(float2));
-    s.part = take((size_t)2 * PG_MAX_RUNS * rows * pitch * sizeof(float));
+    s.ml = take((size_t)2 * slots * sizeof(float2));
+    s.part = take((size_t)2 * slots * pitch * sizeof(float));
     s.total = at;
     return s;
 }
@@ -325,10 +327,12 @@ skipffn_status skipffn_paged_attention(const skipffn_paged_cache *cache, int32_t
         a.min_rows = 0;
         e = launch_paged_simt(a, s);
     } else {
-        // sequences of at most 64 rows read their keys once whatever a tile holds: the kernel for few rows has them
-        a.min_rows = 64;
-        e = launch_paged_few(a, few_rows(std::min<int64_t>(most, 64)), s);
-        if (e == cudaSuccess && most > 64) e = launch_paged_simt(a, s);
+        // sequences of at most 64 rows read their keys once whatever a tile holds: the kernel for few rows has them; a
+        // single sequence that may have more is not worth the launches that would find nothing to do
+        const bool both = most > 64 && a.c.n_seq > 1;
+        a.min_rows = both ? 64 : 0;
+        if (most <= 64 || both) e = launch_paged_few(a, few_rows(std::min<int64_t>(most, 64)), s);
+        if (e == cudaSuccess && most > 64) e = launch_paged_tc(a, s);
     }
     return e == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }

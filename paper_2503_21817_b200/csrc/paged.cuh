@@ -128,6 +128,7 @@ struct PagedEvictArgs {
 
 constexpr int PG_MAX_RUNS = 320;             // runs of one launch (sizes the scratch)
 constexpr int PG_SIMT_ROWS = 16, PG_SIMT_KEYS = 32;
+constexpr int PG_TC_RUNS = 160, PG_TC_ROWS = 256;     // tensor-core kernel: one run per SM, two row tiles
 
 // paged.cu
 // checks a cache for a call of N tokens and lays it out for the kernels
@@ -138,6 +139,8 @@ cudaError_t launch_paged_list(const PagedAttnArgs &a, int rows, int block, cudaS
 cudaError_t launch_paged_join(const PagedAttnArgs &a, int rows, int pitch, cudaStream_t s);
 // paged_few.cu: sequences of few rows, bf16
 cudaError_t launch_paged_few(const PagedAttnArgs &a, int tile_rows, cudaStream_t s);
+// paged_tc.cu: sequences of more rows than that, bf16
+cudaError_t launch_paged_tc(const PagedAttnArgs &a, cudaStream_t s);
 // paged_simt.cu: any number of rows, plain FMA
 cudaError_t launch_paged_simt(const PagedAttnArgs &a, cudaStream_t s);
 cudaError_t launch_paged_weights_simt(const PagedWeightsArgs &a, cudaStream_t s);
