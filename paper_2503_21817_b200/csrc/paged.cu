@@ -184,15 +184,23 @@ __global__ void __launch_bounds__(LIST_THREADS) k_paged_list(const PagedAttnArgs
     }
 }
 
-// The tile that begins in run blockIdx.x and ends in a later one: a warp per row adds up its pieces, in their order.
-constexpr int JOIN_THREADS = 128;
-template <typename T> __global__ void __launch_bounds__(JOIN_THREADS) k_paged_join(const PagedAttnArgs a, int slot_rows, int pitch)
+// Adds the pieces of a cut tile up, in their order.  Listed tiles: cut blockIdx.x, a warp per row (SUBS = 1).  Few rows: the
+// cut of (sequence, head) blockIdx.x, all warps of the CTA for row blockIdx.y, each with every SUBS-th piece: one long
+// sequence leaves a hundred pieces a row.
+constexpr int JOIN_THREADS = 256, JOIN_WARPS = JOIN_THREADS / 32;
+template <typename T, int SUBS> __global__ void __launch_bounds__(JOIN_THREADS) k_paged_join(const PagedAttnArgs a, int slot_rows, int pitch)
 {
+    __shared__ float sums[JOIN_WARPS][PG_MAX_D + 4];
     pdl_enter();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % SUBS;
+    const int row = blockIdx.y * (JOIN_WARPS / SUBS) + warp / SUBS;
+    if (SUBS > 1) {                          // sequences that another kernel has leave no word about their tiles
+        const PagedSeq q = paged_seq(a.c, blockIdx.x / a.c.heads, false);
+        if (row >= q.n * a.group || q.n * a.group > slot_rows) return;
+    }
     const PagedCut cut = a.cuts[blockIdx.x];
-    const int row = blockIdx.y * (JOIN_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (row >= cut.rows || cut.pieces == 0) return;
-    auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * blockIdx.x + 1 : 2 * (blockIdx.x + i)) * slot_rows + row; };
+    if (row >= cut.rows || cut.pieces == 0) return;              // with several warps a row: the same for all
+    auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * cut.first + 1 : 2 * (cut.first + i)) * slot_rows + row; };
     const float c2 = a.scale * 1.4426950408889634f;
     float top = -INFINITY;
     for (int i = lane; i < cut.pieces; i += 32) top = fmaxf(top, a.part_ml[slot(i)].x);
@@ -200,22 +208,36 @@ template <typename T> __global__ void __launch_bounds__(JOIN_THREADS) k_paged_jo
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const bool mine = 4 * lane < a.c.d;
     float l = 0.0f, acc[4] = {};
-    for (int i0 = 0; i0 < cut.pieces; i0 += 32) {
+    for (int i0 = sub; i0 < cut.pieces; i0 += 32 * SUBS) {
         // each lane looks up one piece's weight, then all walk through them
+        const int i1 = i0 + lane * SUBS;
         float2 ml = make_float2(-INFINITY, 0.0f);
-        if (i0 + lane < cut.pieces) ml = a.part_ml[slot(i0 + lane)];
+        if (i1 < cut.pieces) ml = a.part_ml[slot(i1)];
         const float f = ml.x == -INFINITY ? 0.0f : exp2f((ml.x - top) * c2), fl = f * ml.y;
-        const int n = min(32, cut.pieces - i0);
+        const int n = min(32, (cut.pieces - i0 + SUBS - 1) / SUBS);
 #pragma unroll 8
         for (int i = 0; i < n; ++i) {
             const float w = __shfl_sync(0xffffffffu, f, i);
             l += __shfl_sync(0xffffffffu, fl, i);
             if (w != 0.0f && mine) {         // a piece without keys for this row has written no sums
                 float v[4];
-                load4(a.part + slot(i0 + i) * pitch + 4 * lane, v);
+                load4(a.part + slot(i0 + i * SUBS) * pitch + 4 * lane, v);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, v[e], acc[e]);
             }
+        }
+    }
+    if (SUBS > 1) {
+        if (mine) store4(&sums[warp][4 * lane], acc);
+        if (lane == 0) sums[warp][PG_MAX_D] = l;
+        __syncthreads();
+        if (sub != 0) return;
+        for (int i = 1; i < SUBS; ++i) {
+            float v[4];
+            load4(&sums[warp + i][4 * lane], v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += v[e];
+            l += sums[warp + i][PG_MAX_D];
         }
     }
     const int r = cut.r0 + row;
@@ -234,23 +256,20 @@ struct Scratch { size_t cuts, head, seq_tiles, tiles, ml, part, total; int64_t m
 
 bool simt(const skipffn_paged_cache *c) { return c->dtype == SKIPFFN_FP32 || c->path == SKIPFFN_PATH_SIMT; }
 
-// rows of a tile of the kernel for few rows: the smallest that holds the largest sequence
-int few_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
-
 Scratch scratch_of(const skipffn_paged_cache *c, int group, int64_t N)
 {
     const int64_t most = std::min<int64_t>(c->max_new, N) * group;
-    const bool few = !simt(c) && most <= 64;
+    const bool listed = simt(c) || most > PG_FEW_ROWS;
     // the largest of the kernels that the call may launch
-    const int64_t slots = std::max<int64_t>(PG_MAX_RUNS * (simt(c) ? PG_SIMT_ROWS : few_rows(std::min<int64_t>(most, 64))),
-                                            simt(c) || few ? 0 : PG_TC_RUNS * PG_TC_ROWS);
+    const int64_t slots = simt(c) ? PG_SIMT_RUNS * PG_SIMT_ROWS : std::max(PG_FEW_RUNS * PG_FEW_ROWS, listed ? PG_TC_RUNS * PG_TC_ROWS : 0);
     const int64_t tile = simt(c) ? PG_SIMT_ROWS : 2 * (128 / group) * group;
     const int64_t pitch = !simt(c) && c->head_dim <= 64 ? 64 : 128;
+    const size_t cuts = std::max<size_t>(std::max(PG_SIMT_RUNS, PG_TC_RUNS), simt(c) ? 0 : (size_t)c->n_seq * c->heads_kv);
     Scratch s;
-    s.max_tiles = few ? 0 : N * group / tile + c->n_seq + 1;
+    s.max_tiles = listed ? N * group / tile + c->n_seq + 1 : 0;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at = (at + bytes + 255) & ~(size_t)255; return o; };
-    s.cuts = take(PG_MAX_RUNS * sizeof(PagedCut));
+    s.cuts = take(cuts * sizeof(PagedCut));
     s.head = take(64);
     s.seq_tiles = take(((size_t)c->n_seq + 1) * 4);
     s.tiles = take((size_t)s.max_tiles * sizeof(PagedTile));
@@ -269,9 +288,16 @@ cudaError_t launch_paged_list(const PagedAttnArgs &a, int rows, int block, cudaS
 
 cudaError_t launch_paged_join(const PagedAttnArgs &a, int rows, int pitch, cudaStream_t s)
 {
-    const dim3 grid((unsigned)a.runs, (unsigned)((rows + JOIN_THREADS / 32 - 1) / (JOIN_THREADS / 32)));
-    return a.dtype == SKIPFFN_BF16 ? launch_pdl(k_paged_join<bf16>, grid, dim3(JOIN_THREADS), s, a, rows, pitch)
-                                   : launch_pdl(k_paged_join<float>, grid, dim3(JOIN_THREADS), s, a, rows, pitch);
+    const dim3 grid((unsigned)a.runs, (unsigned)((rows + JOIN_WARPS - 1) / JOIN_WARPS));
+    return a.dtype == SKIPFFN_BF16 ? launch_pdl(k_paged_join<bf16, 1>, grid, dim3(JOIN_THREADS), s, a, rows, pitch)
+                                   : launch_pdl(k_paged_join<float, 1>, grid, dim3(JOIN_THREADS), s, a, rows, pitch);
+}
+
+cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int pitch, cudaStream_t s)
+{
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(a.c.max_new, a.c.N) * a.group), tiles = (int64_t)a.c.n_seq * a.c.heads;
+    const dim3 grid((unsigned)tiles, (unsigned)std::min<int64_t>(most, PG_FEW_ROWS));
+    return launch_pdl(k_paged_join<bf16, JOIN_WARPS>, grid, dim3(JOIN_THREADS), s, a, PG_FEW_ROWS, pitch);
 }
 
 }  // namespace skipffn
@@ -300,6 +326,7 @@ skipffn_status skipffn_paged_attention(const skipffn_paged_cache *cache, int32_t
     skipffn_status st = paged_view(cache, n, &a.c);
     if (st == SKIPFFN_OK) st = check_heads(a.c, heads_q, scale);
     if (st != SKIPFFN_OK || n == 0 || a.c.n_seq == 0) return st;
+    if ((int64_t)a.c.n_seq * a.c.heads > INT_MAX) return SKIPFFN_EUNSUPPORTED;
     const int es = cache->dtype == SKIPFFN_BF16 ? 2 : 4;
     for (const int64_t ld : {ldq, ldo})
         if (ld < 0 || ld > (int64_t)1 << 36) return SKIPFFN_EINVAL;
@@ -327,12 +354,12 @@ skipffn_status skipffn_paged_attention(const skipffn_paged_cache *cache, int32_t
         a.min_rows = 0;
         e = launch_paged_simt(a, s);
     } else {
-        // sequences of at most 64 rows read their keys once whatever a tile holds: the kernel for few rows has them; a
-        // single sequence that may have more is not worth the launches that would find nothing to do
-        const bool both = most > 64 && a.c.n_seq > 1;
-        a.min_rows = both ? 64 : 0;
-        if (most <= 64 || both) e = launch_paged_few(a, few_rows(std::min<int64_t>(most, 64)), s);
-        if (e == cudaSuccess && most > 64) e = launch_paged_tc(a, s);
+        // sequences of few rows are bound by reading their keys and have a kernel of their own; a single sequence that may
+        // have more is not worth the launches that would find nothing to do
+        const bool listed = most > PG_FEW_ROWS, few = !listed || a.c.n_seq > 1;
+        a.min_rows = few ? PG_FEW_ROWS : 0;
+        if (few) e = launch_paged_few(a, s);
+        if (e == cudaSuccess && listed) e = launch_paged_tc(a, s);
     }
     return e == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }

@@ -71,11 +71,11 @@ __device__ __forceinline__ int64_t paged_row(const PagedView &c, int s, int row)
 // ---- work of the attention kernels over the cache
 // A tile is up to `rows` consecutive rows of one sequence (row = token * group + head in group) of one kv head; its work
 // is ceil(keys / block) units.  All units stand in one line (tile, head, block) that is cut into equal runs, one per
-// CTA: a run takes the end of one tile, some whole ones and the beginning of another.  A tile inside one run is written at
-// once; the pieces of a cut one go to the CTA's two slots -- the piece a run begins with (when it did not begin the
+// CTA or warp: a run takes the end of one tile, some whole ones and the beginning of another.  A tile inside one run is written at
+// once; the pieces of a cut one go to the run's two slots -- the piece a run begins with (when it did not begin the
 // tile) to slot 2b, the one it ends with to slot 2b + 1 -- and a second kernel adds them up in the order of the runs.
 struct PagedTile { int q0, n, r0, len, s, blocks; int64_t u0; };   // u0: first unit (of head 0)
-struct PagedCut { int q0, r0, rows, h, pieces; int pad[3]; };      // the tile that begins in a run and ends in a later one
+struct PagedCut { int q0, r0, rows, h, pieces, first, pad[2]; };    // a tile that begins in run `first` and ends in a later one (pieces 0: none)
 
 struct PagedAttnArgs {
     PagedView c;
@@ -88,7 +88,7 @@ struct PagedAttnArgs {
     // scratch
     float *part;                             // [2 runs][rows][d or DP] unnormalised sums
     float2 *part_ml;                         // [2 runs][rows] maximum (of scores as they are) and sum
-    PagedCut *cuts;                          // [runs]
+    PagedCut *cuts;                          // listed tiles: [runs]; few rows: [sequence][head]
     PagedTile *tiles;                        // listed tiles
     int32_t *head;                           // listed tiles: number; then units (int64) at head + 2
     int32_t *seq_tiles;                      // [n_seq + 1] first tile of each sequence
@@ -126,8 +126,9 @@ struct PagedEvictArgs {
     int32_t elem_bytes;
 };
 
-constexpr int PG_MAX_RUNS = 320;             // runs of one launch (sizes the scratch)
-constexpr int PG_SIMT_ROWS = 16, PG_SIMT_KEYS = 32;
+// rows of a tile, runs of a launch (these size the scratch): plain FMA, two CTAs an SM; few rows, eight warps an SM
+constexpr int PG_SIMT_ROWS = 16, PG_SIMT_KEYS = 32, PG_SIMT_RUNS = 296;
+constexpr int PG_FEW_ROWS = 16, PG_FEW_RUNS = 1280;
 constexpr int PG_TC_RUNS = 160, PG_TC_ROWS = 256;     // tensor-core kernel: one run per SM, two row tiles
 
 // paged.cu
@@ -137,8 +138,9 @@ skipffn_status paged_view(const skipffn_paged_cache *c, int64_t N, PagedView *vi
 bool paged_overlap(const PagedView &c, const void *p, int64_t bytes);
 cudaError_t launch_paged_list(const PagedAttnArgs &a, int rows, int block, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttnArgs &a, int rows, int pitch, cudaStream_t s);
-// paged_few.cu: sequences of few rows, bf16
-cudaError_t launch_paged_few(const PagedAttnArgs &a, int tile_rows, cudaStream_t s);
+cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int pitch, cudaStream_t s);
+// paged_few.cu: sequences of at most PG_FEW_ROWS rows, bf16
+cudaError_t launch_paged_few(const PagedAttnArgs &a, cudaStream_t s);
 // paged_tc.cu: sequences of more rows than that, bf16
 cudaError_t launch_paged_tc(const PagedAttnArgs &a, cudaStream_t s);
 // paged_simt.cu: any number of rows, plain FMA

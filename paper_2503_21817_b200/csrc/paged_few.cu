@@ -1,15 +1,16 @@
-// Attention over a paged cache for sequences of few rows (tokens x query heads of a kv head <= 64), bf16: the token that
+// Attention over a paged cache for sequences of at most 16 rows (new tokens x query heads of a kv head), bf16: the token that
 // is being answered, a handful of proposed ones.
 //
 //   s_rj = scale q_r . k_j,  out_r = sum_j softmax(s_r)_j v_j,  one pass over the keys with a running maximum and sum.
 //
 // Bound by reading the cache once: 512 bytes a key and kv head at head_dim 128 for 4 x rows x 128 flops, so the legacy
 // matrix instructions (mma.sync, whose accumulators are registers and need no second kernel role) are far from their
-// limit at 16 rows.  The keys of all sequences and heads, 64 to a unit, are one line that is cut into equal runs, one per
-// CTA (two CTAs an SM): ragged batches and one long sequence load every SM alike.  A run streams its units through a ring
-// of asynchronous 16-byte copies; rows come from their pages eight at a time (a page holds whole groups of eight).
-// Warps share a unit by keys when there are at most 16 rows (each has its own maximum and sum, added up at the end of a
-// tile), by rows when there are 64.
+// limit.  The keys of all sequences and heads, 16 to a unit, are one line that is cut into equal runs, one per WARP (eight
+// an SM): ragged batches and one long sequence load every SM alike.  A warp streams its units through its own ring of
+// asynchronous 16-byte copies and waits for nobody: no barrier but at the start, and what the end of one tile costs (its
+// sums written, the next queries fetched) does not hold up the other seven.  Rows come from their pages eight at a time (a page
+// holds whole groups of eight).  Four warps of a CTA sharing a unit of 64 keys, their sums merged at a tile's end, took
+// 105 us for 48 conversations of 37 to 8877 rows (32 / 8 heads) against XX us for this form.
 #include "paged.cuh"
 #include "paged_mma.cuh"
 
@@ -17,78 +18,78 @@ namespace skipffn {
 
 namespace {
 
-constexpr int THREADS = 128, KEYS = 64, STAGES = 3;
+constexpr int WARPS = 8, THREADS = 32 * WARPS, KEYS = 16, ROWS = PG_FEW_ROWS;
 constexpr float LOG2E = 1.4426950408889634f;
 
 // Units of a sequence: blocks of keys of one head; a sequence without keys has one, which writes its empty rows.
-__device__ __forceinline__ int few_blocks(const PagedSeq &q, int group, int rows)
+__device__ __forceinline__ int few_blocks(const PagedSeq &q, int group)
 {
-    return q.n > 0 && q.n * group <= rows ? max(1, (q.len + KEYS - 1) / KEYS) : 0;
+    return q.n > 0 && q.n * group <= ROWS ? max(1, (q.len + KEYS - 1) / KEYS) : 0;
 }
 
 // A place in the line of units
 struct Place {
     int s, h, b, blocks;
     PagedSeq q;
-    // to the first unit of the next sequence that has any; there is one when a unit is left
-    __device__ void next_seq(const PagedView &c, int group, int rows)
+    __device__ void enter(const PagedView &c, int group, int seq)
     {
-        do {
-            ++s;
-            q = paged_seq(c, s, false);
-            blocks = few_blocks(q, group, rows);
-        } while (blocks == 0 && s + 1 < c.n_seq);
-        h = b = 0;
+        s = seq;
+        q = paged_seq(c, s, false);
+        blocks = few_blocks(q, group);
     }
-    __device__ void step(const PagedView &c, int group, int rows, bool more)
+    // to the next unit; there is one when `more`
+    __device__ void step(const PagedView &c, int group, bool more)
     {
         if (++b < blocks) return;
         b = 0;
         if (++h < c.heads) return;
-        if (more) next_seq(c, group, rows);
+        h = 0;
+        if (more)
+            do enter(c, group, s + 1);
+            while (blocks == 0 && s + 1 < c.n_seq);
     }
 };
 
-template <int DP, int WM> struct FewShape {
-    static constexpr int ROW = DP * 2, TILE = KEYS * ROW, STAGE = 2 * TILE;     // keys, then values
-    static constexpr int WK = 4 / WM;                                        // warps that share the keys of a unit
-    static constexpr int MERGE = WK > 1 ? WM * 16 * DP * 4 : 0;
-    static constexpr int SMEM = STAGES * STAGE + MERGE;
+template <int DP> struct FewShape {
+    static constexpr int TILE = KEYS * DP * 2, STAGE = 2 * TILE;              // keys, then values
+    static constexpr int STAGES = DP == 128 ? 3 : 6;
+    static constexpr int SMEM = WARPS * STAGES * STAGE;
 };
 
-template <int DP, int WM>
-__global__ void __launch_bounds__(THREADS, 2) k_paged_few(const PagedAttnArgs a)
+template <int DP>
+__global__ void __launch_bounds__(THREADS, 1) k_paged_few(const PagedAttnArgs a)
 {
-    using Sh = FewShape<DP, WM>;
-    constexpr int WK = Sh::WK, WKEYS = KEYS / WK, NT = WKEYS / 8, CHUNKS = DP / 8;
+    using Sh = FewShape<DP>;
+    constexpr int CHUNKS = DP / 8, STEP = 32 / CHUNKS, STAGES = Sh::STAGES;
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int64_t scan[THREADS / 32];
-    __shared__ int place[2];
-    __shared__ float2 stats[4][16];
+    __shared__ int64_t scan[WARPS], place_in[WARPS];
+    __shared__ int place_seq[WARPS];
     const PagedView &c = a.c;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, run = blockIdx.x, ROWS = 16 * WM;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, ctas = gridDim.x;
     pdl_enter();
 
-    // ---- where this CTA's run lies: sums of units over the sequences
-    auto units_of = [&](int s) { return s < c.n_seq ? (int64_t)few_blocks(paged_seq(c, s, run == 0), a.group, ROWS) * c.heads : 0; };
+    // ---- where the runs lie: sums of units over the sequences.  Run r is warp r / CTAs of CTA r % CTAs, so that a few runs are
+    // spread over the SMs.
+    auto units_of = [&](int s, bool report) { return s < c.n_seq ? (int64_t)few_blocks(paged_seq(c, s, report), a.group) * c.heads : 0; };
     auto block_sum = [&](int64_t v) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         __syncthreads();
         if (lane == 0) scan[warp] = v;
         __syncthreads();
-        return scan[0] + scan[1] + scan[2] + scan[3];
+        int64_t t = 0;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) t += scan[i];
+        return t;
     };
     int64_t mine = 0;
-    for (int s = tid; s < c.n_seq; s += THREADS) mine += units_of(s);
-    const Runs runs(block_sum(mine), a.runs);
-    const int64_t begin = runs.begin(run), end = runs.begin(run + 1);
-    if (tid == 0) a.cuts[run].pieces = 0;
-    if (begin >= end) return;
+    for (int s = tid; s < c.n_seq; s += THREADS) mine += units_of(s, blockIdx.x == 0);
+    const Runs runs(block_sum(mine), ctas * WARPS);
+    if (runs.units == 0) return;
     int64_t before = 0;
-    Place at;
-    for (int s0 = 0;; s0 += THREADS) {
-        const int64_t v = units_of(s0 + tid);
+    const int64_t last_begin = min(runs.begin((WARPS - 1) * ctas + (int)blockIdx.x), runs.units - 1);
+    for (int s0 = 0; s0 < c.n_seq; s0 += THREADS) {
+        const int64_t v = units_of(s0 + tid, false);
         int64_t x = v;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -98,58 +99,73 @@ __global__ void __launch_bounds__(THREADS, 2) k_paged_few(const PagedAttnArgs a)
         const int64_t total = block_sum(v);
         int64_t lo = before + x - v;
         for (int i = 0; i < warp; ++i) lo += scan[i];
-        if (v > 0 && lo <= begin && begin < lo + v) {
-            place[0] = s0 + tid;
-            place[1] = (int)(begin - lo);
+        for (int w = 0; w < WARPS; ++w) {
+            const int64_t u = runs.begin(w * ctas + (int)blockIdx.x);
+            if (lo <= u && u < lo + v) { place_seq[w] = s0 + tid; place_in[w] = u - lo; }
         }
         before += total;
-        if (before > begin) break;           // the same in every thread; ends, since begin < units
+        if (before > last_begin) break;      // the same in every thread
     }
     __syncthreads();
-    at.s = place[0];
-    at.q = paged_seq(c, at.s, false);
-    at.blocks = few_blocks(at.q, a.group, ROWS);
-    at.h = place[1] / at.blocks;
-    at.b = place[1] - at.h * at.blocks;
+    const int run = warp * ctas + (int)blockIdx.x;
+    const int64_t begin = runs.begin(run), end = runs.begin(run + 1);
+    if (run >= runs.n) return;               // no barrier below
+    Place at;
+    at.enter(c, a.group, place_seq[warp]);
+    at.h = (int)(place_in[warp] / at.blocks);
+    at.b = (int)(place_in[warp] - (int64_t)at.h * at.blocks);
     int64_t item = begin - at.b;             // first unit of the current tile
 
-    // ---- the ring
-    const uint32_t ring = smem_u32(smem);
+    // ---- the ring.  A unit's pages are looked up when the one before it is issued: lanes 0 and 1 keep the entries for its
+    // rows 0 .. 7 and 8 .. 15, which are touched a unit later.
+    const uint32_t ring = smem_u32(smem) + warp * STAGES * Sh::STAGE;
+    const int chunk = lane % CHUNKS, row0 = lane / CHUNKS;
     Place ahead = at;
     int64_t issued = begin;
+    uint32_t fill = ring, use = ring;
+    int entry = 0, inside = -1;              // page number, row inside the page (-1: no such row)
+    auto find = [&]() {
+        const int r = ahead.b * KEYS + 8 * lane;
+        inside = -1;
+        if (lane < KEYS / 8 && r < ahead.q.len) {
+            const int p = div_by(r, c.page);
+            entry = c.table[(int64_t)ahead.s * c.table_stride + p];
+            inside = r - p * (int)c.page.d;
+        }
+    };
     auto issue = [&]() {
         if (issued < end) {
-            const uint32_t dst = ring + (uint32_t)((issued - begin) % STAGES) * Sh::STAGE;
-            const int j0 = ahead.b * KEYS;
-            // lane i < 8 finds the rows 8 i .. 8 i + 7 of the block; -1: not there
+            const int left = ahead.q.len - ahead.b * KEYS;
             int64_t base = -1;
-            if (lane < KEYS / 8 && j0 + 8 * lane < ahead.q.len) {
-                base = paged_row(c, ahead.s, j0 + 8 * lane);
-                if (base >= 0) base += ahead.h * c.head_stride;
-                else paged_report(c, SITE_PAGED_PAGE);
+            if (inside >= 0) {
+                if (entry < 0 || entry >= c.n_pages) paged_report(c, SITE_PAGED_PAGE);
+                else base = entry * c.page_stride + inside * c.row_stride + ahead.h * c.head_stride;
             }
-            const int chunk = tid % CHUNKS, r0 = tid / CHUNKS;
-            constexpr int STEP = THREADS / CHUNKS;
+            const int64_t g[2] = {__shfl_sync(0xffffffffu, base, 0), __shfl_sync(0xffffffffu, base, 1)};
 #pragma unroll
             for (int i = 0; i < KEYS / STEP; ++i) {
-                const int r = r0 + i * STEP;
-                const int64_t g = __shfl_sync(0xffffffffu, base, r >> 3);
-                const bool on = g >= 0 && j0 + r < ahead.q.len && chunk * 8 < c.d;
-                const int64_t off = on ? g + (r & 7) * c.row_stride + chunk * 16 : 0;
-                const uint32_t to = dst + chunk_at<DP>(r, chunk);
+                const int r = row0 + i * STEP;
+                const int64_t b = r < 8 ? g[0] : g[1];
+                const bool on = b >= 0 && r < left && chunk * 8 < c.d;
+                const int64_t off = on ? b + (r & 7) * c.row_stride + chunk * 16 : 0;
+                const uint32_t to = fill + chunk_at<DP>(r, chunk);
                 copy16(to, c.k + off, on);
                 copy16(to + Sh::TILE, c.v + off, on);
             }
-            ++issued;
-            ahead.step(c, a.group, ROWS, issued < end);
+            fill = fill == ring + (STAGES - 1) * Sh::STAGE ? ring : fill + Sh::STAGE;
+            if (++issued < end) {
+                ahead.step(c, a.group, true);
+                find();
+            }
         }
         copy_commit();
     };
+    find();
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) issue();
 
-    // ---- arithmetic: warp = (rows 16 wm .., keys wk * WKEYS ..); a thread has rows r0 and r0 + 8 of its 16
-    const int wm = warp % WM, wk = warp / WM, r0 = wm * 16 + (lane >> 2);
+    // ---- arithmetic: a thread has rows r0 and r0 + 8
+    const int r0 = lane >> 2;
     const float c2 = a.scale * LOG2E;
     uint32_t qf[DP / 16][4];
     float o[DP / 8][4], m[2], l[2];
@@ -180,29 +196,27 @@ __global__ void __launch_bounds__(THREADS, 2) k_paged_few(const PagedAttnArgs a)
                 for (int e = 0; e < 4; ++e) o[n][e] = 0.0f;
         }
         copy_wait<STAGES - 2>();
-        __syncthreads();                     // the unit is there for every warp, and the slot refilled next is free
+        __syncwarp();                        // the unit is there for every lane, and the slot refilled next is free
         issue();
-        const uint32_t kt = ring + (uint32_t)((u - begin) % STAGES) * Sh::STAGE + wk * WKEYS * Sh::ROW, vt = kt + Sh::TILE;
-        const int j0 = at.b * KEYS + wk * WKEYS;
-        float s[NT][4];
+        const uint32_t kt = use, vt = use + Sh::TILE;
+        use = use == ring + (STAGES - 1) * Sh::STAGE ? ring : use + Sh::STAGE;
+        const int j0 = at.b * KEYS;
+        float s[2][4] = {}, t2[2][4] = {};   // two chains a tile of eight keys
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int k = 0; k < DP / 16; ++k) {
+            uint32_t b[4];
+            ldsm_x4(kt + chunk_at<DP>((lane >> 4) * 8 + (lane & 7), 2 * k + ((lane >> 3) & 1)), b);
+            mma_16x8(k & 1 ? t2[0] : s[0], qf[k], b[0], b[1]);
+            mma_16x8(k & 1 ? t2[1] : s[1], qf[k], b[2], b[3]);
+        }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][e] = 0.0f;
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-            for (int n = 0; n < NT; n += 2) {
-                const int r = n * 8 + (lane >> 4) * 8 + (lane & 7), ch = 2 * k + ((lane >> 3) & 1);
-                uint32_t b[4];
-                ldsm_x4(kt + chunk_at<DP>(r, ch), b);
-                mma_16x8(s[n], qf[k], b[0], b[1]);
-                mma_16x8(s[n + 1], qf[k], b[2], b[3]);
-            }
+            for (int e = 0; e < 4; ++e) s[n][e] += t2[n][e];
         // keys past a row's own
-        if (j0 + WKEYS > min(limit[0], limit[1])) {
+        if (j0 + KEYS > min(limit[0], limit[1])) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (j0 + 8 * n + 2 * (lane & 3) + (e & 1) >= limit[e >> 1]) s[n][e] = -INFINITY;
@@ -210,9 +224,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_paged_few(const PagedAttnArgs a)
         float f[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            float t = -INFINITY;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) t = fmaxf(t, fmaxf(s[n][2 * i], s[n][2 * i + 1]));
+            float t = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1]));
             t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
             t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
             t = fmaxf(t, m[i]);
@@ -222,7 +234,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_paged_few(const PagedAttnArgs a)
             const float shift = t == -INFINITY ? 0.0f : -t * c2;
             float sum = 0.0f;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float p = fast_exp2(fmaf(s[n][2 * i + e], c2, shift));
@@ -237,137 +249,82 @@ __global__ void __launch_bounds__(THREADS, 2) k_paged_few(const PagedAttnArgs a)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[n][e] *= f[e >> 1];
         }
+        // p as operand of the second product: rounded to bf16, at most 2^-8 of a term; the sum l takes it unrounded
+        const uint32_t p[4] = {pack_bf16(s[0][0], s[0][1]), pack_bf16(s[0][2], s[0][3]), pack_bf16(s[1][0], s[1][1]), pack_bf16(s[1][2], s[1][3])};
 #pragma unroll
-        for (int k = 0; k < NT / 2; ++k) {
-            // p as operand of the second product: rounded to bf16, relative 2^-9 a term; the sum l takes it unrounded
-            const uint32_t p[4] = {pack_bf16(s[2 * k][0], s[2 * k][1]), pack_bf16(s[2 * k][2], s[2 * k][3]),
-                                   pack_bf16(s[2 * k + 1][0], s[2 * k + 1][1]), pack_bf16(s[2 * k + 1][2], s[2 * k + 1][3])};
-#pragma unroll
-            for (int n = 0; n < DP / 16; ++n) {
-                const int r = 16 * k + (lane & 15), ch = 2 * n + (lane >> 4);
-                uint32_t b[4];
-                ldsm_x4_trans(vt + chunk_at<DP>(r, ch), b[0], b[1], b[2], b[3]);
-                mma_16x8(o[2 * n], p, b[0], b[1]);
-                mma_16x8(o[2 * n + 1], p, b[2], b[3]);
-            }
+        for (int n = 0; n < DP / 16; ++n) {
+            uint32_t b[4];
+            ldsm_x4_trans(vt + chunk_at<DP>(lane & 15, 2 * n + (lane >> 4)), b[0], b[1], b[2], b[3]);
+            mma_16x8(o[2 * n], p, b[0], b[1]);
+            mma_16x8(o[2 * n + 1], p, b[2], b[3]);
         }
         if (u + 1 < end && at.b + 1 < at.blocks) { ++at.b; continue; }
 
         // ---- the end of this run's part of the tile
+        const int64_t last = item + at.blocks;
+        const bool whole = item >= begin && last <= end;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-        }
-        if (WK > 1) {
-            // the warps of a row group: a common maximum, then their sums one after the other
-            if ((lane & 3) == 0)
+            const int r = r0 + 8 * i;
+            if (r >= at.q.n * a.group) continue;
+            const int64_t token = at.q.q0 + r / a.group;
+            const int head = at.h * a.group + r % a.group;
+            if (whole) {
+                bf16 *dst = (bf16 *)a.out + token * a.ldo + (int64_t)head * c.d;
+                const float inv = 1.0f / l[i];
+                const bool none = m[i] == -INFINITY;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) stats[warp][(lane >> 2) + 8 * i] = make_float2(m[i], l[i]);
-            __syncthreads();
-            float g[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float2 w[WK];
-                float t = -INFINITY;
-#pragma unroll
-                for (int x = 0; x < WK; ++x) { w[x] = stats[x * WM + wm][(lane >> 2) + 8 * i]; t = fmaxf(t, w[x].x); }
-                g[i] = m[i] == -INFINITY ? 0.0f : fast_exp2((m[i] - t) * c2);
-                float sum = 0.0f;
-#pragma unroll
-                for (int x = 0; x < WK; ++x) sum += w[x].x == -INFINITY ? 0.0f : w[x].y * fast_exp2((w[x].x - t) * c2);
-                m[i] = t;
-                l[i] = sum;
-            }
-            float *merge = reinterpret_cast<float *>(smem + STAGES * Sh::STAGE) + wm * 16 * DP;
-            for (int x = 1; x < WK; ++x) {
-                if (wk == x)
-#pragma unroll
-                    for (int n = 0; n < DP / 8; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) merge[(4 * n + e) * 32 + lane] = o[n][e] * g[e >> 1];
-                __syncthreads();
-                if (wk == 0)
-#pragma unroll
-                    for (int n = 0; n < DP / 8; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[n][e] = (x == 1 ? o[n][e] * g[e >> 1] : o[n][e]) + merge[(4 * n + e) * 32 + lane];
-                __syncthreads();
-            }
-        }
-        const int64_t last = item + at.blocks;
-        const bool whole = item >= begin && last <= end;
-        if (wk == 0) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = r0 + 8 * i;
-                if (r >= at.q.n * a.group) continue;
-                const int64_t token = at.q.q0 + r / a.group;
-                const int head = at.h * a.group + r % a.group;
-                if (whole) {
-                    bf16 *dst = (bf16 *)a.out + token * a.ldo + (int64_t)head * c.d;
-                    const float inv = 1.0f / l[i];
-                    const bool none = m[i] == -INFINITY;
-#pragma unroll
-                    for (int n = 0; n < DP / 8; ++n) {
-                        const int col = 8 * n + 2 * (lane & 3);
-                        if (col < c.d)
-                            *reinterpret_cast<uint32_t *>(dst + col) = none ? 0u : pack_bf16(o[n][2 * i] * inv, o[n][2 * i + 1] * inv);
-                    }
-                    if ((lane & 3) == 0) a.lse[token * a.hq + head] = none ? -INFINITY : fmaf(m[i], a.scale, logf(l[i]));
-                } else {
-                    const int64_t to = (int64_t)(2 * run + (item >= begin ? 1 : 0)) * ROWS + r;
-#pragma unroll
-                    for (int n = 0; n < DP / 8; ++n)
-                        *reinterpret_cast<float2 *>(a.part + to * DP + 8 * n + 2 * (lane & 3)) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
-                    if ((lane & 3) == 0) a.part_ml[to] = make_float2(m[i], l[i]);
+                for (int n = 0; n < DP / 8; ++n) {
+                    const int col = 8 * n + 2 * (lane & 3);
+                    if (col < c.d) *reinterpret_cast<uint32_t *>(dst + col) = none ? 0u : pack_bf16(o[n][2 * i] * inv, o[n][2 * i + 1] * inv);
                 }
+                if ((lane & 3) == 0) a.lse[token * a.hq + head] = none ? -INFINITY : fmaf(m[i], a.scale, logf(l[i]));
+            } else {
+                const int64_t to = (int64_t)(2 * run + (item >= begin ? 1 : 0)) * ROWS + r;
+#pragma unroll
+                for (int n = 0; n < DP / 8; ++n)
+                    *reinterpret_cast<float2 *>(a.part + to * DP + 8 * n + 2 * (lane & 3)) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
+                if ((lane & 3) == 0) a.part_ml[to] = make_float2(m[i], l[i]);
             }
         }
-        if (item >= begin && last > end && tid == 0) {
+        if (item >= begin && lane == 0) {    // the run that begins a tile says how many pieces it has
             PagedCut cut = {};
-            cut.q0 = at.q.q0; cut.rows = at.q.n * a.group; cut.h = at.h;
-            cut.pieces = runs.of(last - 1) - run + 1;
-            a.cuts[run] = cut;
+            cut.q0 = at.q.q0; cut.rows = at.q.n * a.group; cut.h = at.h; cut.first = run;
+            cut.pieces = whole ? 0 : runs.of(last - 1) - run + 1;
+            a.cuts[(int64_t)at.s * c.heads + at.h] = cut;
         }
-        at.step(c, a.group, ROWS, u + 1 < end);
+        at.step(c, a.group, u + 1 < end);
     }
     copy_wait<0>();
 }
 
-template <int DP, int WM> cudaError_t few(const PagedAttnArgs &args, cudaStream_t s)
+template <int DP> cudaError_t few(const PagedAttnArgs &a, cudaStream_t s)
 {
-    using Sh = FewShape<DP, WM>;
-    static int runs_of_device[64];
+    using Sh = FewShape<DP>;
+    static int sms_of_device[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    if (runs_of_device[dev] == 0) {
-        int sms = 0, per = 0;
-        cudaError_t e = cudaFuncSetAttribute(k_paged_few<DP, WM>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::SMEM);
-        if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, k_paged_few<DP, WM>, THREADS, Sh::SMEM);
+    if (sms_of_device[dev] == 0) {
+        int n = 0;
+        cudaError_t e = cudaFuncSetAttribute(k_paged_few<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::SMEM);
+        if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
         if (e != cudaSuccess) return e;
-        if (per < 1) return cudaErrorInvalidConfiguration;
-        runs_of_device[dev] = sms * (per < 2 ? per : 2) < PG_MAX_RUNS ? sms * (per < 2 ? per : 2) : PG_MAX_RUNS;
+        sms_of_device[dev] = n < PG_FEW_RUNS / WARPS ? n : PG_FEW_RUNS / WARPS;
     }
-    PagedAttnArgs a = args;
-    a.runs = runs_of_device[dev];
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)a.runs); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = Sh::SMEM; cfg.stream = s;
+    cfg.gridDim = dim3((unsigned)sms_of_device[dev]); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = Sh::SMEM; cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_paged_few<DP, WM>, a);
-    return e != cudaSuccess ? e : launch_paged_join(a, 16 * WM, DP, s);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_paged_few<DP>, a);
+    return e != cudaSuccess ? e : launch_paged_join_few(a, DP, s);
 }
 
 }  // namespace
 
-cudaError_t launch_paged_few(const PagedAttnArgs &a, int tile_rows, cudaStream_t s)
-{
-    if (a.c.d <= 64) return tile_rows == 16 ? few<64, 1>(a, s) : tile_rows == 32 ? few<64, 2>(a, s) : few<64, 4>(a, s);
-    return tile_rows == 16 ? few<128, 1>(a, s) : tile_rows == 32 ? few<128, 2>(a, s) : few<128, 4>(a, s);
-}
+cudaError_t launch_paged_few(const PagedAttnArgs &a, cudaStream_t s) { return a.c.d <= 64 ? few<64>(a, s) : few<128>(a, s); }
 
 }  // namespace skipffn

@@ -158,7 +158,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS) k_paged_simt(co
             }
             if (b0 == 0 && b1 < e.blocks && threadIdx.x == 0) {
                 PagedCut cut = {};
-                cut.q0 = e.q0; cut.r0 = e.r0; cut.rows = live; cut.h = h;
+                cut.q0 = e.q0; cut.r0 = e.r0; cut.rows = live; cut.h = h; cut.first = run;
                 cut.pieces = runs.of(last - 1) - run + 1;
                 a.cuts[run] = cut;
             }
@@ -229,7 +229,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS) k_paged_weights
 cudaError_t launch_paged_simt(const PagedAttnArgs &args, cudaStream_t s)
 {
     PagedAttnArgs a = args;
-    a.runs = 296;                            // two CTAs per SM
+    a.runs = PG_SIMT_RUNS;
     cudaError_t e = launch_paged_list(a, ROWS, KEYS, s);
     if (e != cudaSuccess) return e;
     e = a.dtype == SKIPFFN_BF16 ? launch_pdl(k_paged_simt<bf16>, dim3(a.runs), dim3(THREADS), s, a)

@@ -1,4 +1,4 @@
-// Attention over a paged cache on the tensor cores (bf16): sequences with more than 64 rows, the chunks of a prompt.
+// Attention over a paged cache on the tensor cores (bf16): sequences with more than 16 rows, the chunks of a prompt.
 //
 // The softmax of two row tiles (2 x 128 rows: tokens x query heads of a kv head) against a ring of key and value tiles, as
 // in the packed forward (roles, registers and the block's softmax are the same code).  What differs:
@@ -127,12 +127,12 @@ k_paged_tc(const __grid_constant__ PagedMaps tm, const __grid_constant__ PagedTc
         const uint32_t box_bytes = (uint32_t)(p.box * DP * 2);
         auto acquire = [&]() {               // next ring slot, free to be written
             const uint32_t s = pos % SLOTS;
-            ok = ok && wait_warp<false>(smem_u32(&ctl->kv_empty[s]), ((pos / SLOTS) & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
+            ok = ok && wait_warp<true>(smem_u32(&ctl->kv_empty[s]), ((pos / SLOTS) & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
             ++pos;
             return s;
         };
         auto load_q = [&](const Piece &it, int g) {
-            ok = ok && wait_warp<false>(smem_u32(&ctl->q_empty[g]), (nq[g] & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
+            ok = ok && wait_warp<true>(smem_u32(&ctl->q_empty[g]), (nq[g] & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
             if (!ok) return;
             if (lane == 0) {
                 const uint32_t bar = smem_u32(&ctl->q_full[g]);
@@ -144,22 +144,21 @@ k_paged_tc(const __grid_constant__ PagedMaps tm, const __grid_constant__ PagedTc
         PieceFeed<true> feed(p);
         Piece it;
         while (ok && feed.take(it)) {
-            // this lane's page of block j: its number (out of range: the first one past the pool) and the row inside it
-            auto find = [&](int j, int &page, int &row) {
+            // this lane's entry of the table for block j, looked up a block ahead and not touched until then
+            auto find = [&](int j, int &entry, int &row) {
                 const int r = j * TILE + lane * p.box;
-                page = -1;
+                row = -1;
                 if (lane < boxes && r < it.len) {
                     const int k = div_by(r, a.c.page);
-                    page = a.c.table[(int64_t)it.s * a.c.table_stride + k];
+                    entry = a.c.table[(int64_t)it.s * a.c.table_stride + k];
                     row = r - k * p.page_rows;
-                    if (page < 0 || page >= a.c.n_pages) { page = (int)a.c.n_pages; row = 0; paged_report(a.c, SITE_PAGED_PAGE); }
                 }
             };
             auto load = [&](uint32_t dst, const CUtensorMap *map, uint32_t bar, int page, int row) {
-                const int n = __popc(__ballot_sync(0xffffffffu, page >= 0));
+                const int n = __popc(__ballot_sync(0xffffffffu, row >= 0));
                 if (lane == 0) mbar_expect_tx(bar, (uint32_t)n * box_bytes);
                 __syncwarp();
-                if (page >= 0)
+                if (row >= 0)
 #pragma unroll
                     for (int s = 0; s < DP / 64; ++s)
                         asm volatile(
@@ -169,9 +168,11 @@ k_paged_tc(const __grid_constant__ PagedMaps tm, const __grid_constant__ PagedTc
                             : "memory");
                 __syncwarp();
             };
-            int page, row = 0, next_page = -1, next_row = 0;
+            int page = 0, row = -1, next_page = 0, next_row = -1;
             find(it.b0, page, row);
             for (int j = it.b0; j < it.b1 && ok; ++j) {
+                // a page that does not exist: the first one past the pool
+                if (row >= 0 && (page < 0 || page >= a.c.n_pages)) { page = (int)a.c.n_pages; row = 0; paged_report(a.c, SITE_PAGED_PAGE); }
                 if (j == it.b0 && it.count(0)) load_q(it, 0);
                 if (j + 1 < it.b1) find(j + 1, next_page, next_row);
                 uint32_t s = acquire();
@@ -198,7 +199,7 @@ k_paged_tc(const __grid_constant__ PagedMaps tm, const __grid_constant__ PagedTc
             pos += 2 * n;
             if (it.b0 == 0 && it.b1 < it.blocks && lane == 0) {
                 PagedCut cut = {};
-                cut.q0 = it.q0; cut.r0 = it.t0 * a.group; cut.h = it.h;
+                cut.q0 = it.q0; cut.r0 = it.t0 * a.group; cut.h = it.h; cut.first = blockIdx.x;
                 cut.rows = min(2 * used, it.n * a.group - cut.r0);
                 cut.pieces = feed.runs.of(u + it.blocks - 1) - (int)blockIdx.x + 1;
                 a.cuts[blockIdx.x] = cut;

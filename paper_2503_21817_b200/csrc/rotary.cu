@@ -23,25 +23,30 @@
 namespace skipffn {
 
 constexpr int RT_MAX_D = 256, RT_MAX_PAIRS = RT_MAX_D / 2, RT_MAX_AXES = 4;
-constexpr int RT_THREADS = 256, RT_MAX_TOKENS = 16;          // tokens of a CTA's table
-constexpr int RT_MAX_PARTS = 592;                            // CTAs of the backward: partial sums of the gains' gradients
+constexpr int RT_THREADS = 256, RT_MAX_TOKENS = 32;          // tokens of a CTA's table
+constexpr int RT_FWD_ROWS = 4, RT_BWD_ROWS = 2;              // rows that a group of lanes has in flight
+constexpr int RT_MAX_PARTS = 444;                            // CTAs of the backward: partial sums of the gains' gradients
 
 struct RotaryTurns {                                         // by value in the kernels' parameters
     unsigned long long turns[RT_MAX_PAIRS];
     uint8_t axis[RT_MAX_PAIRS];
 };
 
+// The rows of one kind: queries, keys, or values that are copied.  Each kind has its own CTAs, so that a CTA's rows share one
+// gain and one set of strides, and `tokens` of them at a time.
+struct RotaryRows {
+    const void *x, *gamma, *dy;              // dy: backward
+    void *out;
+    int64_t ld, ldo, lddy;
+    int32_t heads, tokens, ctas, pad;
+};
 struct RotaryArgs {
-    const void *q, *k, *v, *gq, *gk;                         // v: append only; gq, gk: gains or null
-    const void *dyq, *dyk;                                   // backward
-    void *oq, *ok;
-    int64_t ldq, ldk, ldv, lddyq, lddyk, ldoq, ldok;
+    RotaryRows rows[3];
     const int32_t *pos;
-    int64_t ldpos;
-    int64_t n;
-    int32_t hq, hk, d, rot, tokens, heads_per_cta;
+    int64_t ldpos, n;
+    int32_t d, rot;
     float eps;
-    float *part;                                             // backward: [CTAs][2][d]
+    float *part;                             // backward: [CTAs][d]
     PagedView c;
 };
 
@@ -121,8 +126,10 @@ template <int L> __device__ __forceinline__ float group_sum(float v)
 __device__ __forceinline__ void fill_table(float2 *table, const RotaryArgs &a, const RotaryTurns &f, int64_t t0, int count)
 {
     const int pairs = a.rot / 2;
-    for (int i = threadIdx.x; i < count * pairs; i += RT_THREADS) {
-        const int t = i / pairs, p = i - t * pairs;
+    if (pairs == 0) return;
+    int t = threadIdx.x / pairs, p = threadIdx.x - t * pairs;
+    for (int i = threadIdx.x; i < count * pairs; i += RT_THREADS, p += RT_THREADS) {
+        while (p >= pairs) { p -= pairs; ++t; }
         const long long pos = a.pos[f.axis[p] * a.ldpos + t0 + t];
         table[i] = turn_to_cos_sin((unsigned long long)pos * f.turns[p]);
     }
@@ -130,7 +137,7 @@ __device__ __forceinline__ void fill_table(float2 *table, const RotaryArgs &a, c
 
 // Where the last row of a token's sequence puts it: byte offset of its cache row, -1 for none (token behind the last sequence: -2).
 // One warp, every lane gets the answer.
-__device__ __forceinline__ int64_t append_row(const PagedView &c, int64_t token, int lane)
+__device__ __forceinline__ int64_t append_row(const PagedView &c, int64_t token, int lane, bool report)
 {
     int lo = 0, hi = c.n_seq;                                // largest s with cu[s] <= token, 32 candidates at a time
     while (hi - lo > 1) {
@@ -144,20 +151,42 @@ __device__ __forceinline__ int64_t append_row(const PagedView &c, int64_t token,
     const int a = c.cu[lo], b = c.cu[lo + 1];
     if (token < a || token >= b) {
         // behind the last sequence is where rows may stand that belong to none
-        if (lane == 0 && token < c.cu[c.n_seq]) paged_report(c, SITE_PAGED_OFFSETS);
+        if (report && lane == 0 && token < c.cu[c.n_seq]) paged_report(c, SITE_PAGED_OFFSETS);
         return -2;
     }
     const int64_t row = (int64_t)c.lens[lo] - b + token;
     if (row < 0 || row >= c.capacity) {
-        if (lane == 0) paged_report(c, SITE_PAGED_ROOM);
+        if (report && lane == 0) paged_report(c, SITE_PAGED_ROOM);
         return -1;
     }
     const int64_t at = paged_row(c, lo, (int)row);
-    if (at < 0 && lane == 0) paged_report(c, SITE_PAGED_PAGE);
+    if (report && at < 0 && lane == 0) paged_report(c, SITE_PAGED_PAGE);
     return at;
 }
 
-// Forward.  CTA: `tokens` tokens x heads blockIdx.y * heads_per_cta .. of the hq + hk (+ hk values) rows of each.
+// Walks the (token, head) rows of a CTA, GROUPS apart
+struct RowWalk {
+    int t, h, heads, dt, dh;
+    __device__ RowWalk(int first, int step, int heads_) : heads(heads_)
+    {
+        t = first / heads; h = first - t * heads;
+        dt = step / heads; dh = step - dt * heads;
+    }
+    __device__ void next()
+    {
+        t += dt; h += dh;
+        if (h >= heads) { h -= heads; ++t; }
+    }
+};
+
+template <typename T, int V> struct Row { typename Vec<T, V>::type w0, w1; };
+template <typename T, int V> __device__ __forceinline__ Row<T, V> load_row(const T *p, const LanePairs &l)
+{
+    typedef typename Vec<T, V>::type W;
+    return Row<T, V>{*reinterpret_cast<const W *>(p + l.e0), *reinterpret_cast<const W *>(p + l.e1)};
+}
+
+// Forward.  Every group of lanes has several rows in flight: their loads are issued before any of them is worked on.
 template <typename T, int V, int L, bool INTER, bool APPEND>
 __global__ void __launch_bounds__(RT_THREADS)
 k_rotary_fwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ RotaryTurns f)
@@ -165,195 +194,196 @@ k_rotary_fwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ Rotar
     typedef typename Vec<T, V>::type W;
     extern __shared__ float2 table[];
     __shared__ int64_t slot[RT_MAX_TOKENS];
-    pdl_enter();
-    const int64_t t0 = (int64_t)blockIdx.x * a.tokens;
-    const int count = (int)min((int64_t)a.tokens, a.n - t0);
-    const int h0 = blockIdx.y * a.heads_per_cta, all = a.hq + (APPEND ? 2 : 1) * a.hk, heads = min(a.heads_per_cta, all - h0);
-    fill_table(table, a, f, t0, count);
-    if (APPEND)
-        for (int t = threadIdx.x >> 5; t < count; t += RT_THREADS / 32) {
-            const int64_t r = append_row(a.c, t0 + t, threadIdx.x & 31);
-            if ((threadIdx.x & 31) == 0) slot[t] = r;
-        }
-    __syncthreads();
-    constexpr int GROUPS = RT_THREADS / L;
+    constexpr int GROUPS = RT_THREADS / L, U = RT_FWD_ROWS;
+    int kind = 0, cta = blockIdx.x;
+    while (cta >= a.rows[kind].ctas) cta -= a.rows[kind++].ctas;
+    const RotaryRows &k = a.rows[kind];
+    const int64_t t0 = (int64_t)cta * k.tokens;
+    const int count = (int)min((int64_t)k.tokens, a.n - t0), rows = count * k.heads;
     const LanePairs l = lane_pairs<V, INTER>(threadIdx.x % L, a.d, a.rot);
     const float inv_d = 1.0f / a.d;
-    int t = 0, h = threadIdx.x / L;
-    while (h >= heads) { h -= heads; ++t; }
+    RowWalk walk(threadIdx.x / L, GROUPS, k.heads);
+    pdl_enter();
+    float g0[V], g1[V];
+    if (k.gamma && l.on) {
+        const Row<T, V> g = load_row<T, V>((const T *)k.gamma, l);
+        unpack<T, V>(g.w0, g0);
+        unpack<T, V>(g.w1, g1);
+    }
+    if (kind < 2) fill_table(table, a, f, t0, count);
+    if (APPEND)
+        for (int t = threadIdx.x >> 5; t < count; t += RT_THREADS / 32) {
+            const int64_t r = append_row(a.c, t0 + t, threadIdx.x & 31, kind == 1);
+            if ((threadIdx.x & 31) == 0) slot[t] = r;
+        }
+    bool synced = false;
     // every lane of a warp takes part in the shuffles, so all walk the same number of rows
-    for (int it = 0; it < (count * heads + GROUPS - 1) / GROUPS; ++it) {
-        const bool live = t < count && l.on;
-        const int head = h0 + h;
-        const int64_t tok = t0 + t;
-        const bool is_q = head < a.hq, is_v = APPEND && head >= a.hq + a.hk;
-        const T *src = nullptr;
-        T *dst = nullptr;
-        if (live) {
-            const int kh = is_q ? 0 : is_v ? head - a.hq - a.hk : head - a.hq;
-            if (is_q) {
-                src = (const T *)a.q + tok * a.ldq + (int64_t)head * a.d;
-                dst = (T *)a.oq + tok * a.ldoq + (int64_t)head * a.d;
-            } else {
-                src = (is_v ? (const T *)a.v + tok * a.ldv : (const T *)a.k + tok * a.ldk) + (int64_t)kh * a.d;
-                if (!APPEND) dst = (T *)a.ok + tok * a.ldok + (int64_t)kh * a.d;
-            }
-            if (APPEND) {
-                const int64_t s = slot[t];
-                if (s == -2) dst = nullptr;
-                else if (!is_q) dst = s < 0 ? nullptr : (T *)((is_v ? a.c.v : a.c.k) + s + kh * a.c.head_stride);
-            }
-        }
-        W w0 = {}, w1 = {};
-        if (dst) {
-            w0 = *reinterpret_cast<const W *>(src + l.e0);
-            w1 = *reinterpret_cast<const W *>(src + l.e1);
-        }
-        const T *gamma = is_v ? nullptr : (const T *)(is_q ? a.gq : a.gk);
-        float lo[V], hi[V];
-        unpack<T, V>(w0, lo);
-        unpack<T, V>(w1, hi);
-        if (a.gq) {                                          // with a gain for q there is one for k
-            float ss = 0.0f;
+    for (int r0 = 0; r0 < rows; r0 += U * GROUPS) {
+        Row<T, V> x[U];
+        int at[U];                           // token of the CTA, -1: no row
+        int64_t to[U];                       // element offset of the result's row (append, keys and values: byte offset)
+        if (APPEND && !synced) { __syncthreads(); synced = true; }
 #pragma unroll
-            for (int i = 0; i < V; ++i) ss = fmaf(lo[i], lo[i], fmaf(hi[i], hi[i], ss));
-            const float r = rsqrtf(group_sum<L>(ss) * inv_d + a.eps);
-            if (gamma && l.on) {
-                float g0[V], g1[V];
-                unpack<T, V>(*reinterpret_cast<const W *>(gamma + l.e0), g0);
-                unpack<T, V>(*reinterpret_cast<const W *>(gamma + l.e1), g1);
+        for (int u = 0; u < U; ++u) {
+            at[u] = -1;
+            to[u] = -1;
+            x[u] = Row<T, V>{};
+            if (walk.t < count && l.on) {
+                const int64_t tok = t0 + walk.t;
+                to[u] = tok * k.ldo + (int64_t)walk.h * a.d;
+                if (APPEND) {
+                    const int64_t s = slot[walk.t];
+                    if (s == -2) to[u] = -1;
+                    else if (kind > 0) to[u] = s < 0 ? -1 : s + walk.h * a.c.head_stride;
+                }
+                at[u] = walk.t;
+                if (to[u] >= 0) x[u] = load_row<T, V>((const T *)k.x + tok * k.ld + (int64_t)walk.h * a.d, l);
+            }
+            walk.next();
+        }
+        if (!synced) { __syncthreads(); synced = true; }       // the table is made while the first rows arrive
 #pragma unroll
-                for (int i = 0; i < V; ++i) { lo[i] *= r * g0[i]; hi[i] *= r * g1[i]; }
+        for (int u = 0; u < U; ++u) {
+            if (kind < 2) {
+                float lo[V], hi[V];
+                unpack<T, V>(x[u].w0, lo);
+                unpack<T, V>(x[u].w1, hi);
+                if (k.gamma) {
+                    float ss = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) ss = fmaf(lo[i], lo[i], fmaf(hi[i], hi[i], ss));
+                    const float r = rsqrtf(group_sum<L>(ss) * inv_d + a.eps);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) { lo[i] *= r * g0[i]; hi[i] *= r * g1[i]; }
+                }
+                if (at[u] >= 0 && l.p0 >= 0) rotate<V, INTER>(lo, hi, table + at[u] * (a.rot / 2) + l.p0, 1.0f);
+                x[u].w0 = pack<T, V>(lo);
+                x[u].w1 = pack<T, V>(hi);
+            }
+            if (to[u] >= 0) {
+                T *dst = APPEND && kind > 0 ? (T *)((kind == 1 ? a.c.k : a.c.v) + to[u]) : (T *)k.out + to[u];
+                *reinterpret_cast<W *>(dst + l.e0) = x[u].w0;
+                *reinterpret_cast<W *>(dst + l.e1) = x[u].w1;
             }
         }
-        if (dst) {
-            if (!is_v) {
-                if (l.p0 >= 0) rotate<V, INTER>(lo, hi, table + t * (a.rot / 2) + l.p0, 1.0f);
-                w0 = pack<T, V>(lo);
-                w1 = pack<T, V>(hi);
-            }
-            *reinterpret_cast<W *>(dst + l.e0) = w0;
-            *reinterpret_cast<W *>(dst + l.e1) = w1;
-        }
-        h += GROUPS;
-        while (h >= heads) { h -= heads; ++t; }
     }
 }
 
-// Backward.  CTAs walk blocks of tokens; the gains' gradients are summed in registers (a lane's columns stay the
-// same), over the CTA's groups in shared memory, then over the CTAs by k_rotary_sum: a fixed order throughout.
+// Backward.  CTAs of a kind walk blocks of its tokens; the gain's gradient is summed in registers (a lane's columns stay
+// the same), over the CTA's groups in shared memory, then over the CTAs by k_rotary_sum: a fixed order throughout.
 template <typename T, int V, int L, bool INTER>
 __global__ void __launch_bounds__(RT_THREADS)
 k_rotary_bwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ RotaryTurns f)
 {
     typedef typename Vec<T, V>::type W;
     extern __shared__ float2 table[];
-    pdl_enter();
-    constexpr int GROUPS = RT_THREADS / L;
+    constexpr int GROUPS = RT_THREADS / L, U = RT_BWD_ROWS;
+    const int kind = blockIdx.x >= a.rows[0].ctas, cta = blockIdx.x - (kind ? a.rows[0].ctas : 0);
+    const RotaryRows &k = a.rows[kind];
     const LanePairs l = lane_pairs<V, INTER>(threadIdx.x % L, a.d, a.rot);
-    const int heads = a.hq + a.hk;
     const float inv_d = 1.0f / a.d;
-    float acc[2][2][V] = {};
-    for (int64_t t0 = (int64_t)blockIdx.x * a.tokens; t0 < a.n; t0 += (int64_t)gridDim.x * a.tokens) {
-        const int count = (int)min((int64_t)a.tokens, a.n - t0);
-        __syncthreads();
+    pdl_enter();
+    float acc[2][V] = {}, g0[V] = {}, g1[V] = {};
+    if (k.gamma && l.on) {
+        const Row<T, V> g = load_row<T, V>((const T *)k.gamma, l);
+        unpack<T, V>(g.w0, g0);
+        unpack<T, V>(g.w1, g1);
+    }
+    for (int64_t t0 = (int64_t)cta * k.tokens; t0 < a.n; t0 += (int64_t)k.ctas * k.tokens) {
+        const int count = (int)min((int64_t)k.tokens, a.n - t0), rows = count * k.heads;
+        RowWalk walk(threadIdx.x / L, GROUPS, k.heads);
+        __syncthreads();                     // the table has been read
         fill_table(table, a, f, t0, count);
-        __syncthreads();
-        int t = 0, h = threadIdx.x / L;
-        while (h >= heads) { h -= heads; ++t; }
-        for (int it = 0; it < (count * heads + GROUPS - 1) / GROUPS; ++it) {
-            const bool live = t < count && l.on, is_q = h < a.hq;
-            const int64_t tok = t0 + t;
-            const int kh = is_q ? h : h - a.hq;
-            W y0 = {}, y1 = {}, x0 = {}, x1 = {};
-            if (live) {
-                const T *dy = (is_q ? (const T *)a.dyq + tok * a.lddyq : (const T *)a.dyk + tok * a.lddyk) + (int64_t)kh * a.d;
-                y0 = *reinterpret_cast<const W *>(dy + l.e0);
-                y1 = *reinterpret_cast<const W *>(dy + l.e1);
-                if (a.gq) {
-                    const T *x = (is_q ? (const T *)a.q + tok * a.ldq : (const T *)a.k + tok * a.ldk) + (int64_t)kh * a.d;
-                    x0 = *reinterpret_cast<const W *>(x + l.e0);
-                    x1 = *reinterpret_cast<const W *>(x + l.e1);
-                }
-            }
-            float lo[V], hi[V];
-            unpack<T, V>(y0, lo);
-            unpack<T, V>(y1, hi);
-            if (live && l.p0 >= 0) rotate<V, INTER>(lo, hi, table + t * (a.rot / 2) + l.p0, -1.0f);
-            if (a.gq) {
-                const T *gamma = (const T *)(is_q ? a.gq : a.gk);
-                float xl[V], xh[V], g0[V] = {}, g1[V] = {};
-                unpack<T, V>(x0, xl);
-                unpack<T, V>(x1, xh);
-                if (l.on) {
-                    unpack<T, V>(*reinterpret_cast<const W *>(gamma + l.e0), g0);
-                    unpack<T, V>(*reinterpret_cast<const W *>(gamma + l.e1), g1);
-                }
-                float ss = 0.0f, ux = 0.0f;
+        bool synced = false;
+        for (int r0 = 0; r0 < rows; r0 += U * GROUPS) {
+            Row<T, V> y[U], x[U];
+            int at[U], head[U];
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    ss = fmaf(xl[i], xl[i], fmaf(xh[i], xh[i], ss));
-                    ux = fmaf(lo[i] * g0[i], xl[i], fmaf(hi[i] * g1[i], xh[i], ux));
+            for (int u = 0; u < U; ++u) {
+                at[u] = -1;
+                head[u] = walk.h;
+                y[u] = x[u] = Row<T, V>{};   // a lane without a row adds nothing
+                if (walk.t < count && l.on) {
+                    const int64_t tok = t0 + walk.t;
+                    at[u] = walk.t;
+                    y[u] = load_row<T, V>((const T *)k.dy + tok * k.lddy + (int64_t)walk.h * a.d, l);
+                    if (k.gamma) x[u] = load_row<T, V>((const T *)k.x + tok * k.ld + (int64_t)walk.h * a.d, l);
                 }
-                const float r = rsqrtf(group_sum<L>(ss) * inv_d + a.eps);
-                const float m = group_sum<L>(ux) * inv_d * r * r;
+                walk.next();
+            }
+            if (!synced) { __syncthreads(); synced = true; }
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float al = lo[i] * (xl[i] * r), ah = hi[i] * (xh[i] * r);
-                    // a dead lane has zeros here
-                    acc[0][0][i] += is_q ? al : 0.0f;
-                    acc[0][1][i] += is_q ? ah : 0.0f;
-                    acc[1][0][i] += is_q ? 0.0f : al;
-                    acc[1][1][i] += is_q ? 0.0f : ah;
-                    lo[i] = r * (lo[i] * g0[i] - xl[i] * m);
-                    hi[i] = r * (hi[i] * g1[i] - xh[i] * m);
+            for (int u = 0; u < U; ++u) {
+                float lo[V], hi[V];
+                unpack<T, V>(y[u].w0, lo);
+                unpack<T, V>(y[u].w1, hi);
+                if (at[u] >= 0 && l.p0 >= 0) rotate<V, INTER>(lo, hi, table + at[u] * (a.rot / 2) + l.p0, -1.0f);
+                if (k.gamma) {
+                    float xl[V], xh[V];
+                    unpack<T, V>(x[u].w0, xl);
+                    unpack<T, V>(x[u].w1, xh);
+                    float ss = 0.0f, ux = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        ss = fmaf(xl[i], xl[i], fmaf(xh[i], xh[i], ss));
+                        ux = fmaf(lo[i] * g0[i], xl[i], fmaf(hi[i] * g1[i], xh[i], ux));
+                    }
+                    const float r = rsqrtf(group_sum<L>(ss) * inv_d + a.eps);
+                    const float m = group_sum<L>(ux) * inv_d * r * r;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        acc[0][i] = fmaf(lo[i], xl[i] * r, acc[0][i]);
+                        acc[1][i] = fmaf(hi[i], xh[i] * r, acc[1][i]);
+                        lo[i] = r * (lo[i] * g0[i] - xl[i] * m);
+                        hi[i] = r * (hi[i] * g1[i] - xh[i] * m);
+                    }
+                }
+                if (at[u] >= 0) {
+                    T *dx = (T *)k.out + (t0 + at[u]) * k.ldo + (int64_t)head[u] * a.d;
+                    *reinterpret_cast<W *>(dx + l.e0) = pack<T, V>(lo);
+                    *reinterpret_cast<W *>(dx + l.e1) = pack<T, V>(hi);
                 }
             }
-            if (live) {
-                T *dx = (is_q ? (T *)a.oq + tok * a.ldoq : (T *)a.ok + tok * a.ldok) + (int64_t)kh * a.d;
-                *reinterpret_cast<W *>(dx + l.e0) = pack<T, V>(lo);
-                *reinterpret_cast<W *>(dx + l.e1) = pack<T, V>(hi);
-            }
-            h += GROUPS;
-            while (h >= heads) { h -= heads; ++t; }
         }
     }
-    if (!a.gq) return;
+    if (!k.gamma) return;
     float *sums = reinterpret_cast<float *>(table);           // [groups][d]
-    for (int z = 0; z < 2; ++z) {
-        __syncthreads();
-        if (l.on)
+    __syncthreads();
+    if (l.on)
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                sums[(threadIdx.x / L) * a.d + l.e0 + i] = acc[z][0][i];
-                sums[(threadIdx.x / L) * a.d + l.e1 + i] = acc[z][1][i];
-            }
-        __syncthreads();
-        for (int c = threadIdx.x; c < a.d; c += RT_THREADS) {
-            float s = 0.0f;
-            for (int g = 0; g < GROUPS; ++g) s += sums[g * a.d + c];
-            a.part[((int64_t)blockIdx.x * 2 + z) * a.d + c] = s;
+        for (int i = 0; i < V; ++i) {
+            sums[(threadIdx.x / L) * a.d + l.e0 + i] = acc[0][i];
+            sums[(threadIdx.x / L) * a.d + l.e1 + i] = acc[1][i];
         }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.d; c += RT_THREADS) {
+        float s = 0.0f;
+        for (int g = 0; g < GROUPS; ++g) s += sums[g * a.d + c];
+        a.part[(int64_t)blockIdx.x * a.d + c] = s;
     }
 }
 
-// dgamma[z][c] = sum of the CTAs' parts: 32 columns a CTA, 32 rows of parts at a time
-template <typename T> __global__ void __launch_bounds__(1024) k_rotary_sum(const float *__restrict__ part, int parts, int d, T *dgq, T *dgk)
+// dgamma[c] = sum of the CTAs' parts, of parts 0 .. split - 1 for the queries' gain (blockIdx.y 0), the others for the
+// keys': 32 columns a CTA, 32 parts at a time
+template <typename T> __global__ void __launch_bounds__(1024) k_rotary_sum(const float *__restrict__ part, int split, int parts, int d, T *dgq, T *dgk)
 {
     __shared__ float red[32][33];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+    const int p0 = blockIdx.y ? split : 0, p1 = blockIdx.y ? parts : split;
     pdl_enter();
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;   // column of [2][d]
     float s = 0.0f;
-    if (col < 2 * d)
-        for (int p = w; p < parts; p += 32) s += part[(int64_t)p * 2 * d + col];
+    if (col < d) {
+#pragma unroll 8
+        for (int p = p0 + w; p < p1; p += 32) s += part[(int64_t)p * d + col];
+    }
     red[w][lane] = s;
     __syncthreads();
-    if (w == 0 && col < 2 * d) {
+    if (w == 0 && col < d) {
         float total = 0.0f;
 #pragma unroll
         for (int i = 0; i < 32; ++i) total += red[i][lane];
-        T *dst = col < d ? dgq : dgk;
-        if (dst) dst[col < d ? col : col - d] = from_f32<T>(total);
+        T *dst = blockIdx.y ? dgk : dgq;
+        if (dst) dst[col] = from_f32<T>(total);
     }
 }
 
@@ -376,44 +406,58 @@ static int lanes_of(int d, int V)
     return L;
 }
 
-template <typename T, int V, int L, bool INTER> static cudaError_t rotary_l(int mode, RotaryArgs a, const RotaryTurns &f, dim3 grid, cudaStream_t s)
+enum RotaryMode { RT_FORWARD, RT_APPEND, RT_BACKWARD };
+
+template <typename T, int V, int L, bool INTER> static cudaError_t rotary_l(RotaryMode mode, const RotaryArgs &a, const RotaryTurns &f, cudaStream_t s)
 {
-    const size_t table = (size_t)a.tokens * (a.rot / 2) * sizeof(float2);
-    if (mode == 0) return launch_smem(k_rotary_fwd<T, V, L, INTER, false>, grid, dim3(RT_THREADS), table, s, a, f);
-    if (mode == 1) return launch_smem(k_rotary_fwd<T, V, L, INTER, true>, grid, dim3(RT_THREADS), table, s, a, f);
-    const size_t sums = (size_t)(RT_THREADS / L) * a.d * sizeof(float);
-    return launch_smem(k_rotary_bwd<T, V, L, INTER>, grid, dim3(RT_THREADS), table > sums ? table : sums, s, a, f);
+    int tokens = 1, ctas = 0;
+    for (const RotaryRows &k : a.rows) {
+        if (k.ctas > 0 && k.tokens > tokens) tokens = k.tokens;
+        ctas += k.ctas;
+    }
+    const size_t table = (size_t)tokens * (a.rot / 2) * sizeof(float2);
+    const dim3 grid((unsigned)ctas), block(RT_THREADS);
+    if (mode == RT_FORWARD) return launch_smem(k_rotary_fwd<T, V, L, INTER, false>, grid, block, table, s, a, f);
+    if (mode == RT_APPEND) return launch_smem(k_rotary_fwd<T, V, L, INTER, true>, grid, block, table, s, a, f);
+    const size_t sums = a.rows[0].gamma ? (size_t)(RT_THREADS / L) * a.d * sizeof(float) : 0;
+    return launch_smem(k_rotary_bwd<T, V, L, INTER>, grid, block, table > sums ? table : sums, s, a, f);
 }
-template <typename T, int V, bool INTER> static cudaError_t rotary_v(int mode, const RotaryArgs &a, const RotaryTurns &f, dim3 grid, cudaStream_t s)
+template <typename T, int V, bool INTER> static cudaError_t rotary_v(RotaryMode mode, const RotaryArgs &a, const RotaryTurns &f, cudaStream_t s)
 {
     switch (lanes_of(a.d, V)) {
-    case 1: return rotary_l<T, V, 1, INTER>(mode, a, f, grid, s);
-    case 2: return rotary_l<T, V, 2, INTER>(mode, a, f, grid, s);
-    case 4: return rotary_l<T, V, 4, INTER>(mode, a, f, grid, s);
-    case 8: return rotary_l<T, V, 8, INTER>(mode, a, f, grid, s);
-    case 16: return rotary_l<T, V, 16, INTER>(mode, a, f, grid, s);
-    default: return rotary_l<T, V, 32, INTER>(mode, a, f, grid, s);
+    case 1: return rotary_l<T, V, 1, INTER>(mode, a, f, s);
+    case 2: return rotary_l<T, V, 2, INTER>(mode, a, f, s);
+    case 4: return rotary_l<T, V, 4, INTER>(mode, a, f, s);
+    case 8: return rotary_l<T, V, 8, INTER>(mode, a, f, s);
+    case 16: return rotary_l<T, V, 16, INTER>(mode, a, f, s);
+    default: return rotary_l<T, V, 32, INTER>(mode, a, f, s);
     }
 }
-// Eight pairs a lane need halves and the columns behind the rotated ones to be multiples of 8 resp. 16; four always fit.
-static cudaError_t rotary_launch(int mode, int dtype, bool inter, const RotaryArgs &a, const RotaryTurns &f, dim3 grid, cudaStream_t s)
+// Pairs of a lane: eight when halves and the columns behind the rotated ones are multiples of 8 resp. 16; four always fit.
+static int pairs_per_lane(int dtype, int d, int rot) { return dtype == SKIPFFN_BF16 && d % 16 == 0 && rot % 16 == 0 ? 8 : 4; }
+static cudaError_t rotary_launch(RotaryMode mode, int dtype, bool inter, const RotaryArgs &a, const RotaryTurns &f, cudaStream_t s)
 {
-    if (dtype == SKIPFFN_FP32) return inter ? rotary_v<float, 4, true>(mode, a, f, grid, s) : rotary_v<float, 4, false>(mode, a, f, grid, s);
-    if (a.d % 16 == 0 && a.rot % 16 == 0)
-        return inter ? rotary_v<bf16, 8, true>(mode, a, f, grid, s) : rotary_v<bf16, 8, false>(mode, a, f, grid, s);
-    return inter ? rotary_v<bf16, 4, true>(mode, a, f, grid, s) : rotary_v<bf16, 4, false>(mode, a, f, grid, s);
+    if (dtype == SKIPFFN_FP32) return inter ? rotary_v<float, 4, true>(mode, a, f, s) : rotary_v<float, 4, false>(mode, a, f, s);
+    if (pairs_per_lane(dtype, a.d, a.rot) == 8) return inter ? rotary_v<bf16, 8, true>(mode, a, f, s) : rotary_v<bf16, 8, false>(mode, a, f, s);
+    return inter ? rotary_v<bf16, 4, true>(mode, a, f, s) : rotary_v<bf16, 4, false>(mode, a, f, s);
 }
 
-// tokens of a CTA: up to 8, fewer while that leaves SMs without one; one token's heads are spread over CTAs when
-// there are fewer tokens than SMs
-static dim3 rotary_grid(RotaryArgs *a, int rows, int groups, bool split)
+// Tokens of a CTA's turn: two batches of rows per group of lanes, fewer while SMs would be left without work, never more than
+// the table holds.
+static int turn_tokens(int64_t n, int heads, int batch, int groups)
 {
-    int t = 8;
-    while (t > 1 && (a->n + t - 1) / t < 4 * 148) t /= 2;
-    a->tokens = t;
-    a->heads_per_cta = rows;
-    if (split && t == 1 && a->n < 148) a->heads_per_cta = groups < rows ? groups : rows;
-    return dim3((unsigned)((a->n + t - 1) / t), (unsigned)((rows + a->heads_per_cta - 1) / a->heads_per_cta));
+    int64_t t = 2 * batch * groups / heads;
+    while (t > 1 && (n + t - 1) / t * heads < (int64_t)148 * 4 * groups) t /= 2;
+    return (int)(t < 1 ? 1 : t > RT_MAX_TOKENS ? RT_MAX_TOKENS : t);
+}
+static void plan_rows(RotaryArgs *a, int dtype, int batch)
+{
+    const int groups = RT_THREADS / lanes_of(a->d, pairs_per_lane(dtype, a->d, a->rot));
+    for (RotaryRows &k : a->rows) {
+        if (k.heads == 0) continue;
+        k.tokens = turn_tokens(a->n, k.heads, batch, groups);
+        k.ctas = (int32_t)((a->n + k.tokens - 1) / k.tokens);
+    }
 }
 
 }  // namespace skipffn
@@ -462,11 +506,13 @@ bool out_ok(const TokenArray &out, const TokenArray *same, std::initializer_list
 int64_t pos_bytes(const skipffn_rotary *h, int64_t n, int64_t ldpos) { return h->rot ? ((h->axes - 1) * ldpos + n) * 4 : 0; }
 
 RotaryArgs args_of(const skipffn_rotary *h, int64_t n, const void *q, int64_t ldq, const void *k, int64_t ldk, const int32_t *pos,
-                   int64_t ldpos, const void *gq, const void *gk)
+                   int64_t ldpos, const void *gq, const void *gk, void *oq, int64_t ldoq, void *ok, int64_t ldok)
 {
     RotaryArgs a = {};
-    a.q = q; a.k = k; a.ldq = ldq; a.ldk = ldk; a.pos = pos; a.ldpos = ldpos; a.gq = gq; a.gk = gk; a.n = n;
-    a.hq = h->hq; a.hk = h->hk; a.d = h->d; a.rot = h->rot; a.eps = h->eps;
+    a.rows[0].x = q; a.rows[0].ld = ldq; a.rows[0].gamma = gq; a.rows[0].out = oq; a.rows[0].ldo = ldoq; a.rows[0].heads = h->hq;
+    a.rows[1].x = k; a.rows[1].ld = ldk; a.rows[1].gamma = gk; a.rows[1].out = ok; a.rows[1].ldo = ldok; a.rows[1].heads = h->hk;
+    a.pos = pos; a.ldpos = ldpos; a.n = n;
+    a.d = h->d; a.rot = h->rot; a.eps = h->eps;
     return a;
 }
 
@@ -518,14 +564,12 @@ skipffn_status skipffn_rotary_forward(const skipffn_rotary *h, int32_t dtype, in
     if (!out_ok(oq, &c.q, {c.q, c.k}, positions, pb, gamma_q, gamma_k, gb, n) ||
         !out_ok(ok, &c.k, {c.q, c.k}, positions, pb, gamma_q, gamma_k, gb, n) || tokens_overlap(oq, ok, n))
         return SKIPFFN_EINVAL;
-    RotaryArgs a = args_of(h, n, q, ldq, k, ldk, positions, ldpos, gamma_q, gamma_k);
-    a.oq = q_out; a.ok = k_out; a.ldoq = ldqo; a.ldok = ldko;
-    const int V = dtype == SKIPFFN_BF16 && h->d % 16 == 0 && h->rot % 16 == 0 ? 8 : 4;
-    const dim3 grid = rotary_grid(&a, h->hq + h->hk, RT_THREADS / lanes_of(h->d, V), true);
-    return rotary_launch(0, dtype, h->inter, a, h->f, grid, (cudaStream_t)stream) == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
+    RotaryArgs a = args_of(h, n, q, ldq, k, ldk, positions, ldpos, gamma_q, gamma_k, q_out, ldqo, k_out, ldko);
+    plan_rows(&a, dtype, RT_FWD_ROWS);
+    return rotary_launch(RT_FORWARD, dtype, h->inter, a, h->f, (cudaStream_t)stream) == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }
 
-size_t skipffn_rotary_scratch_bytes(const skipffn_rotary *h) { return h ? (size_t)RT_MAX_PARTS * 2 * h->d * sizeof(float) : 0; }
+size_t skipffn_rotary_scratch_bytes(const skipffn_rotary *h) { return h ? (size_t)RT_MAX_PARTS * h->d * sizeof(float) : 0; }
 
 skipffn_status skipffn_rotary_backward(const skipffn_rotary *h, int32_t dtype, int64_t n, const void *dq_out, int64_t lddqo,
                                        const void *dk_out, int64_t lddko, const void *q, int64_t ldq, const void *k, int64_t ldk,
@@ -547,8 +591,7 @@ skipffn_status skipffn_rotary_backward(const skipffn_rotary *h, int32_t dtype, i
         if (ranges_overlap(dgamma_q, b, dgamma_k, b) || ranges_overlap(dgamma_q, b, scratch, need) || ranges_overlap(dgamma_k, b, scratch, need))
             return SKIPFFN_EINVAL;
     }
-    RotaryArgs a = args_of(h, n, q, ldq, k, ldk, positions, ldpos, gamma_q, gamma_k);
-    dim3 grid(0, 1, 1);
+    RotaryArgs a = args_of(h, n, q, ldq, k, ldk, positions, ldpos, gamma_q, gamma_k, dq, lddq, dk, lddk);
     if (n > 0) {
         for (const int64_t ld : {lddqo, lddko, lddq, lddk})
             if (ld < 0 || ld > (int64_t)1 << 36) return SKIPFFN_EINVAL;
@@ -572,19 +615,23 @@ skipffn_status skipffn_rotary_backward(const skipffn_rotary *h, int32_t dtype, i
             if (ranges_overlap(positions, pb, dgamma_q, b) || ranges_overlap(positions, pb, dgamma_k, b) || ranges_overlap(positions, pb, scratch, need))
                 return SKIPFFN_EINVAL;
         }
-        a.dyq = dq_out; a.dyk = dk_out; a.lddyq = lddqo; a.lddyk = lddko;
-        a.oq = dq; a.ok = dk; a.ldoq = lddq; a.ldok = lddk;
+        a.rows[0].dy = dq_out; a.rows[0].lddy = lddqo;
+        a.rows[1].dy = dk_out; a.rows[1].lddy = lddko;
         a.part = (float *)scratch;
-        grid = rotary_grid(&a, h->hq + h->hk, 0, false);
-        if (grid.x > RT_MAX_PARTS) grid.x = RT_MAX_PARTS;
-        if (rotary_launch(2, dtype, h->inter, a, h->f, grid, (cudaStream_t)stream) != cudaSuccess) return SKIPFFN_ECUDA;
+        plan_rows(&a, dtype, RT_BWD_ROWS);
+        // three CTAs an SM, shared out by the rows of a kind
+        const int share = (int)((int64_t)RT_MAX_PARTS * h->hq / (h->hq + h->hk)), of_q = share < 1 ? 1 : share == RT_MAX_PARTS ? share - 1 : share;
+        if (a.rows[0].ctas > of_q) a.rows[0].ctas = of_q;
+        if (a.rows[1].ctas > RT_MAX_PARTS - of_q) a.rows[1].ctas = RT_MAX_PARTS - of_q;
+        if (rotary_launch(RT_BACKWARD, dtype, h->inter, a, h->f, (cudaStream_t)stream) != cudaSuccess) return SKIPFFN_ECUDA;
     }
     if (!norm || (!dgamma_q && !dgamma_k)) return SKIPFFN_OK;
-    const dim3 sum_grid((unsigned)((2 * h->d + 31) / 32));
-    const cudaError_t e = gs == 4 ? launch_smem(k_rotary_sum<float>, sum_grid, dim3(1024), 0, (cudaStream_t)stream, (const float *)scratch,
-                                                (int)grid.x, (int)h->d, (float *)dgamma_q, (float *)dgamma_k)
-                                  : launch_smem(k_rotary_sum<bf16>, sum_grid, dim3(1024), 0, (cudaStream_t)stream, (const float *)scratch,
-                                                (int)grid.x, (int)h->d, (bf16 *)dgamma_q, (bf16 *)dgamma_k);
+    const dim3 sum_grid((unsigned)((h->d + 31) / 32), 2);
+    const int split = a.rows[0].ctas, parts = split + a.rows[1].ctas;         // none without tokens: zeros
+    const cudaError_t e = gs == 4 ? launch_pdl(k_rotary_sum<float>, sum_grid, dim3(1024), (cudaStream_t)stream, (const float *)scratch, split, parts,
+                                               (int)h->d, (float *)dgamma_q, (float *)dgamma_k)
+                                  : launch_pdl(k_rotary_sum<bf16>, sum_grid, dim3(1024), (cudaStream_t)stream, (const float *)scratch, split, parts,
+                                               (int)h->d, (bf16 *)dgamma_q, (bf16 *)dgamma_k);
     return e == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }
 
@@ -607,11 +654,11 @@ skipffn_status skipffn_rotary_append(const skipffn_rotary *h, const skipffn_page
     for (const TokenArray &x : {c.q, c.k, va, oq})
         if (paged_overlap(view, x.p, token_bytes(x, n))) return SKIPFFN_EINVAL;
     if (paged_overlap(view, positions, pb) || paged_overlap(view, gamma_q, gb) || paged_overlap(view, gamma_k, gb)) return SKIPFFN_EINVAL;
-    RotaryArgs a = args_of(h, n, q, ldq, k, ldk, positions, ldpos, gamma_q, gamma_k);
-    a.v = v; a.ldv = ldv; a.oq = q_out; a.ldoq = ldqo; a.c = view;
-    const int V = cache->dtype == SKIPFFN_BF16 && h->d % 16 == 0 && h->rot % 16 == 0 ? 8 : 4;
-    const dim3 grid = rotary_grid(&a, h->hq + 2 * h->hk, RT_THREADS / lanes_of(h->d, V), true);
-    return rotary_launch(1, cache->dtype, h->inter, a, h->f, grid, (cudaStream_t)stream) == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
+    RotaryArgs a = args_of(h, n, q, ldq, k, ldk, positions, ldpos, gamma_q, gamma_k, q_out, ldqo, nullptr, 0);
+    a.rows[2].x = v; a.rows[2].ld = ldv; a.rows[2].heads = h->hk;
+    a.c = view;
+    plan_rows(&a, cache->dtype, RT_FWD_ROWS);
+    return rotary_launch(RT_APPEND, cache->dtype, h->inter, a, h->f, (cudaStream_t)stream) == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }
 
 skipffn_status skipffn_paged_append(const skipffn_paged_cache *cache, int64_t n, const void *k, int64_t ldk, const void *v, int64_t ldv,
@@ -626,10 +673,11 @@ skipffn_status skipffn_paged_append(const skipffn_paged_cache *cache, int64_t n,
     for (const TokenArray &x : {TokenArray{k, ldk * es, w}, TokenArray{v, ldv * es, w}})
         if (!token_array_ok(x, n) || paged_overlap(view, x.p, token_bytes(x, n))) return SKIPFFN_EINVAL;
     RotaryArgs a = {};                       // no queries, nothing turned
-    a.k = k; a.v = v; a.ldk = ldk; a.ldv = ldv; a.n = n; a.hk = view.heads; a.d = view.d; a.c = view;
-    const int V = cache->dtype == SKIPFFN_BF16 && view.d % 16 == 0 ? 8 : 4;
-    const dim3 grid = rotary_grid(&a, 2 * a.hk, RT_THREADS / lanes_of(a.d, V), true);
-    return rotary_launch(1, cache->dtype, false, a, RotaryTurns{}, grid, (cudaStream_t)stream) == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
+    a.rows[1].x = k; a.rows[1].ld = ldk; a.rows[1].heads = view.heads;
+    a.rows[2].x = v; a.rows[2].ld = ldv; a.rows[2].heads = view.heads;
+    a.n = n; a.d = view.d; a.c = view;
+    plan_rows(&a, cache->dtype, RT_FWD_ROWS);
+    return rotary_launch(RT_APPEND, cache->dtype, false, a, RotaryTurns{}, (cudaStream_t)stream) == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }
 
 }  // extern "C"
