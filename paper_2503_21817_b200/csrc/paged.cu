@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(LIST_THREADS) k_paged_list(const PagedAttnArgs
                 else empty_rows<float>(a, e, live);
             }
         }
-        const int64_t before = block_exclusive((int64_t)e.blocks * c.heads, warp_sums, total);
+        const int64_t before = block_exclusive(e.blocks ? (int64_t)(e.blocks + PG_TILE_COST) * c.heads : 0, warp_sums, total);
         e.u0 = units + before;
         if (t < tiles) a.tiles[t] = e;
         units += total;
@@ -261,7 +261,7 @@ Scratch scratch_of(const skipffn_paged_cache *c, int group, int64_t N)
     const int64_t most = std::min<int64_t>(c->max_new, N) * group;
     const bool listed = simt(c) || most > PG_FEW_ROWS;
     // the largest of the kernels that the call may launch
-    const int64_t slots = simt(c) ? PG_SIMT_RUNS * PG_SIMT_ROWS : std::max(PG_FEW_RUNS * PG_FEW_ROWS, listed ? PG_TC_RUNS * PG_TC_ROWS : 0);
+    const int64_t slots = simt(c) ? 2 * PG_SIMT_RUNS * PG_SIMT_ROWS : std::max(PG_FEW_SLOTS, listed ? 2 * PG_TC_RUNS * PG_TC_ROWS : 0);
     const int64_t tile = simt(c) ? PG_SIMT_ROWS : 2 * (128 / group) * group;
     const int64_t pitch = !simt(c) && c->head_dim <= 64 ? 64 : 128;
     const size_t cuts = std::max<size_t>(std::max(PG_SIMT_RUNS, PG_TC_RUNS), simt(c) ? 0 : (size_t)c->n_seq * c->heads_kv);
@@ -273,8 +273,8 @@ Scratch scratch_of(const skipffn_paged_cache *c, int group, int64_t N)
     s.head = take(64);
     s.seq_tiles = take(((size_t)c->n_seq + 1) * 4);
     s.tiles = take((size_t)s.max_tiles * sizeof(PagedTile));
-    s.ml = take((size_t)2 * slots * sizeof(float2));
-    s.part = take((size_t)2 * slots * pitch * sizeof(float));
+    s.ml = take((size_t)slots * sizeof(float2));
+    s.part = take((size_t)slots * pitch * sizeof(float));
     s.total = at;
     return s;
 }
@@ -293,11 +293,11 @@ cudaError_t launch_paged_join(const PagedAttnArgs &a, int rows, int pitch, cudaS
                                    : launch_pdl(k_paged_join<float, 1>, grid, dim3(JOIN_THREADS), s, a, rows, pitch);
 }
 
-cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int pitch, cudaStream_t s)
+cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int rows, int pitch, cudaStream_t s)
 {
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(a.c.max_new, a.c.N) * a.group), tiles = (int64_t)a.c.n_seq * a.c.heads;
-    const dim3 grid((unsigned)tiles, (unsigned)std::min<int64_t>(most, PG_FEW_ROWS));
-    return launch_pdl(k_paged_join<bf16, JOIN_WARPS>, grid, dim3(JOIN_THREADS), s, a, PG_FEW_ROWS, pitch);
+    const dim3 grid((unsigned)tiles, (unsigned)std::min<int64_t>(most, rows));
+    return launch_pdl(k_paged_join<bf16, JOIN_WARPS>, grid, dim3(JOIN_THREADS), s, a, rows, pitch);
 }
 
 }  // namespace skipffn
@@ -354,11 +354,12 @@ skipffn_status skipffn_paged_attention(const skipffn_paged_cache *cache, int32_t
         a.min_rows = 0;
         e = launch_paged_simt(a, s);
     } else {
-        // sequences of few rows are bound by reading their keys and have a kernel of their own; a single sequence that may
-        // have more is not worth the launches that would find nothing to do
+        // Sequences of few rows are bound by reading their keys and have a kernel of their own.  Next to chunks these are
+        // single tokens (16 rows, the fastest form; what has more joins the chunks); a single sequence that may be a chunk
+        // is not worth the launches that would find nothing to do.
         const bool listed = most > PG_FEW_ROWS, few = !listed || a.c.n_seq > 1;
-        a.min_rows = few ? PG_FEW_ROWS : 0;
-        if (few) e = launch_paged_few(a, s);
+        a.min_rows = few ? 16 : 0;
+        if (few) e = launch_paged_few(a, listed ? 16 : (int)most, s);
         if (e == cudaSuccess && listed) e = launch_paged_tc(a, s);
     }
     return e == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;

@@ -70,10 +70,14 @@ __device__ __forceinline__ int64_t paged_row(const PagedView &c, int s, int row)
 
 // ---- work of the attention kernels over the cache
 // A tile is up to `rows` consecutive rows of one sequence (row = token * group + head in group) of one kv head; its work
-// is ceil(keys / block) units.  All units stand in one line (tile, head, block) that is cut into equal runs, one per
-// CTA or warp: a run takes the end of one tile, some whole ones and the beginning of another.  A tile inside one run is written at
-// once; the pieces of a cut one go to the run's two slots -- the piece a run begins with (when it did not begin the
-// tile) to slot 2b, the one it ends with to slot 2b + 1 -- and a second kernel adds them up in the order of the runs.
+// is ceil(keys / block) blocks.  A line of units, PG_TILE_COST and then one for each block for every (tile, head), is cut into
+// equal runs, one per CTA or group of warps: a run takes the end of one tile, some whole ones and the beginning of another.
+// The units in front of a tile's blocks stand for what a tile costs beside them (measured about one block: without them
+// the run that fell to a chunk of 500 tokens over 500 rows, 64 tiles of 1 to 4 blocks, took 150 us longer than the others).
+// A tile inside one run is written at once; the pieces of a cut one go to the run's two slots -- the piece a run begins
+// with (when it did not begin the tile) to slot 2b, the one it ends with to slot 2b + 1 -- and a second kernel adds them up
+// in the order of the runs, from the one that holds the first block to the one that holds the last.
+constexpr int PG_TILE_COST = 1;
 struct PagedTile { int q0, n, r0, len, s, blocks; int64_t u0; };   // u0: first unit (of head 0)
 struct PagedCut { int q0, r0, rows, h, pieces, first, pad[2]; };    // a tile that begins in run `first` and ends in a later one (pieces 0: none)
 
@@ -128,7 +132,7 @@ struct PagedEvictArgs {
 
 // rows of a tile, runs of a launch (these size the scratch): plain FMA, two CTAs an SM; few rows, eight warps an SM
 constexpr int PG_SIMT_ROWS = 16, PG_SIMT_KEYS = 32, PG_SIMT_RUNS = 296;
-constexpr int PG_FEW_ROWS = 16, PG_FEW_RUNS = 1280;
+constexpr int PG_FEW_ROWS = 64, PG_FEW_SMS = 160, PG_FEW_SLOTS = 2 * PG_FEW_SMS * 8 * 16;
 constexpr int PG_TC_RUNS = 160, PG_TC_ROWS = 256;     // tensor-core kernel: one run per SM, two row tiles
 
 // paged.cu
@@ -138,9 +142,9 @@ skipffn_status paged_view(const skipffn_paged_cache *c, int64_t N, PagedView *vi
 bool paged_overlap(const PagedView &c, const void *p, int64_t bytes);
 cudaError_t launch_paged_list(const PagedAttnArgs &a, int rows, int block, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttnArgs &a, int rows, int pitch, cudaStream_t s);
-cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int pitch, cudaStream_t s);
-// paged_few.cu: sequences of at most PG_FEW_ROWS rows, bf16
-cudaError_t launch_paged_few(const PagedAttnArgs &a, cudaStream_t s);
+cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int rows, int pitch, cudaStream_t s);
+// paged_few.cu: sequences of at most `rows` <= PG_FEW_ROWS rows, bf16
+cudaError_t launch_paged_few(const PagedAttnArgs &a, int rows, cudaStream_t s);
 // paged_tc.cu: sequences of more rows than that, bf16
 cudaError_t launch_paged_tc(const PagedAttnArgs &a, cudaStream_t s);
 // paged_simt.cu: any number of rows, plain FMA

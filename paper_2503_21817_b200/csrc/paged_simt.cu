@@ -59,9 +59,12 @@ template <typename T> __global__ void __launch_bounds__(THREADS) k_paged_simt(co
         const PagedTile e = a.tiles[t];
         if (e.blocks == 0) continue;
         const int live = min(ROWS, e.n * a.group - e.r0);
-        for (int h = (int)((u - e.u0) / e.blocks); h < c.heads && u < end; ++h) {
-            const int64_t first = e.u0 + (int64_t)h * e.blocks, last = first + e.blocks;
-            const int b0 = (int)(u - first), b1 = (int)(min(end, last) - first);
+        const int seg = e.blocks + PG_TILE_COST;
+        for (int h = (int)((u - e.u0) / seg); h < c.heads && u < end; ++h) {
+            const int64_t first = e.u0 + (int64_t)h * seg + PG_TILE_COST, last = first + e.blocks;   // units of the blocks
+            const int b0 = (int)max((int64_t)0, u - first), b1 = (int)(min(end, last) - first);
+            u = min(end, last);
+            if (b1 <= b0) continue;          // the run ends before the tile's first block
             const int r = e.r0 + row, limit = row < live ? e.len - e.n + r / a.group + 1 : 0;
             __syncthreads();
             for (int i = threadIdx.x; i < ROWS * (c.d / 4); i += THREADS) {
@@ -162,7 +165,6 @@ template <typename T> __global__ void __launch_bounds__(THREADS) k_paged_simt(co
                 cut.pieces = runs.of(last - 1) - run + 1;
                 a.cuts[run] = cut;
             }
-            u = min(end, last);
         }
     }
 }

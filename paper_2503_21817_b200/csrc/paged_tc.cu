@@ -51,7 +51,7 @@ template <bool WARP> struct PieceFeed {
         u = runs.begin(blockIdx.x);
         end = runs.begin(blockIdx.x + 1);
         if (u >= end) return;
-        for (int hi = p.a.head[0]; hi - t > 1;) {            // largest tile with u0 <= u
+        for (int hi = p.a.head[0]; hi - t > 1;) {            // largest tile with u0 <= u: it holds u
             const int mid = (t + hi) >> 1;
             if (p.a.tiles[mid].u0 <= u) t = mid; else hi = mid;
         }
@@ -59,13 +59,22 @@ template <bool WARP> struct PieceFeed {
     }
     __device__ bool take(Piece &w)
     {
-        if (u >= end) return false;
-        while (u >= e.u0 + (int64_t)e.blocks * p.a.c.heads) e = p.a.tiles[++t];
-        const int64_t in = u - e.u0;
-        w.blocks = pick(e.blocks);
-        w.h = pick((int)(in / e.blocks));
-        w.b0 = pick((int)(in - (int64_t)w.h * e.blocks));
-        w.b1 = pick((int)min((int64_t)w.blocks, w.b0 + (end - u)));
+        do {
+            if (u >= end) return false;
+            const int seg = e.blocks + PG_TILE_COST;
+            const int64_t in = u - e.u0;
+            if (e.blocks == 0 || in >= (int64_t)seg * p.a.c.heads) {
+                e = p.a.tiles[++t];
+                w.b0 = w.b1 = 0;
+                continue;
+            }
+            w.blocks = pick(e.blocks);
+            w.h = pick((int)(in / seg));
+            const int p0 = pick((int)(in - (int64_t)w.h * seg)), p1 = pick((int)min((int64_t)seg, p0 + (end - u)));
+            w.b0 = max(0, p0 - PG_TILE_COST);
+            w.b1 = max(0, p1 - PG_TILE_COST);
+            u += p1 - p0;
+        } while (w.b1 <= w.b0);              // the run may end before the tile's first block
         w.q0 = pick(e.q0); w.n = pick(e.n); w.len = pick(e.len); w.s = pick(e.s);
         w.t0 = pick(e.r0 / p.a.group);
         const int t1 = w.t0 + p.tokens, off = w.len - w.n;
@@ -73,7 +82,6 @@ template <bool WARP> struct PieceFeed {
         w.end1 = t1 < w.n ? max(0, off + min(t1 + p.tokens, w.n)) : 0;
         w.nb0 = ceil_div(w.end0, TILE);
         w.nb1 = ceil_div(w.end1, TILE);
-        u += w.b1 - w.b0;
         return true;
     }
     __device__ static int pick(int v) { return WARP ? uniform(v) : v; }
@@ -193,7 +201,6 @@ k_paged_tc(const __grid_constant__ PagedMaps tm, const __grid_constant__ PagedTc
         bool ok = true;
         PieceFeed<true> feed(p);
         Piece it;
-        int64_t u = feed.u;
         while (ok && feed.take(it)) {
             const int n = it.loads();
             pos += 2 * n;
@@ -201,10 +208,9 @@ k_paged_tc(const __grid_constant__ PagedMaps tm, const __grid_constant__ PagedTc
                 PagedCut cut = {};
                 cut.q0 = it.q0; cut.r0 = it.t0 * a.group; cut.h = it.h; cut.first = blockIdx.x;
                 cut.rows = min(2 * used, it.n * a.group - cut.r0);
-                cut.pieces = feed.runs.of(u + it.blocks - 1) - (int)blockIdx.x + 1;
+                cut.pieces = feed.runs.of(feed.u + (it.blocks - it.b1) - 1) - (int)blockIdx.x + 1;
                 a.cuts[blockIdx.x] = cut;
             }
-            u += n;
             if (!it.dirty_tail()) continue;
             const uint32_t s = (pos - 1) % SLOTS;
             ok = wait_warp<false>(smem_u32(&ctl->tail[s]), (seen >> s) & 1, waits, SITE_PRODUCER_EMPTY);
