@@ -10,8 +10,7 @@
 //     at the ends of runs cost 256 rows x 512 bytes each; runs of whole pairs would leave up to half of the SMs idle
 //     (32 pairs of rows and 8 heads on 148 SMs)
 //   * tokens see up to their own row: only the last blocks of a pair are masked
-#include "attention_tc.cuh"
-#include "paged.cuh"
+#include "paged_tma.cuh"
 
 namespace skipffn {
 
@@ -19,7 +18,7 @@ namespace {
 
 struct PagedTcParams {
     PagedAttnArgs a;
-    int32_t tokens, box, page_rows;          // tokens of a row tile; rows of a TMA box and of a page
+    int32_t tokens, box;                     // tokens of a row tile; rows of a TMA box
     float c2;
 };
 struct alignas(64) PagedMaps { CUtensorMap q, k, v; };
@@ -131,8 +130,7 @@ k_paged_tc(const __grid_constant__ PagedMaps tm, const __grid_constant__ PagedTc
     if (warp == FwdWarps::TMA) {
         uint32_t pos = 0, nq[2] = {0, 0};
         bool ok = true;
-        const int boxes = TILE / p.box;      // of a tile; lane i issues box i
-        const uint32_t box_bytes = (uint32_t)(p.box * DP * 2);
+        const PageBoxes boxes{a.c, p.box, lane};
         auto acquire = [&]() {               // next ring slot, free to be written
             const uint32_t s = pos % SLOTS;
             ok = ok && wait_warp<true>(smem_u32(&ctl->kv_empty[s]), ((pos / SLOTS) & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
@@ -152,47 +150,21 @@ k_paged_tc(const __grid_constant__ PagedMaps tm, const __grid_constant__ PagedTc
         PieceFeed<true> feed(p);
         Piece it;
         while (ok && feed.take(it)) {
-            // this lane's entry of the table for block j, looked up a block ahead and not touched until then
-            auto find = [&](int j, int &entry, int &row) {
-                const int r = j * TILE + lane * p.box;
-                row = -1;
-                if (lane < boxes && r < it.len) {
-                    const int k = div_by(r, a.c.page);
-                    entry = a.c.table[(int64_t)it.s * a.c.table_stride + k];
-                    row = r - k * p.page_rows;
-                }
-            };
-            auto load = [&](uint32_t dst, const CUtensorMap *map, uint32_t bar, int page, int row) {
-                const int n = __popc(__ballot_sync(0xffffffffu, row >= 0));
-                if (lane == 0) mbar_expect_tx(bar, (uint32_t)n * box_bytes);
-                __syncwarp();
-                if (row >= 0)
-#pragma unroll
-                    for (int s = 0; s < DP / 64; ++s)
-                        asm volatile(
-                            "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes "
-                            "[%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst + s * (TILE * 128) + lane * p.box * 128),
-                            "l"(map), "r"(64 * s), "r"(it.h), "r"(row), "r"(page), "r"(bar)
-                            : "memory");
-                __syncwarp();
-            };
-            int page = 0, row = -1, next_page = 0, next_row = -1;
-            find(it.b0, page, row);
+            PageBox box = boxes.find(it.s, it.len, it.b0 * TILE), next = box;
             for (int j = it.b0; j < it.b1 && ok; ++j) {
-                // a page that does not exist: the first one past the pool
-                if (row >= 0 && (page < 0 || page >= a.c.n_pages)) { page = (int)a.c.n_pages; row = 0; paged_report(a.c, SITE_PAGED_PAGE); }
+                boxes.check(box);
                 if (j == it.b0 && it.count(0)) load_q(it, 0);
-                if (j + 1 < it.b1) find(j + 1, next_page, next_row);
+                if (j + 1 < it.b1) next = boxes.find(it.s, it.len, (j + 1) * TILE);
                 uint32_t s = acquire();
                 if (!ok) break;
-                load(ring + s * T_BYTES, &tm.k, smem_u32(&ctl->kv_full[s]), page, row);
+                boxes.load<DP>(ring + s * T_BYTES, &tm.k, smem_u32(&ctl->kv_full[s]), box, it.h);
                 if (j == it.b0 && it.count(1)) load_q(it, 1);
                 s = acquire();
                 if (!ok) break;
                 // the tail warp passes a tile with rows to zero on to the MMA warp
-                load(ring + s * T_BYTES, &tm.v, smem_u32(j == it.b1 - 1 && it.dirty_tail() ? &ctl->tail[s] : &ctl->kv_full[s]), page, row);
+                boxes.load<DP>(ring + s * T_BYTES, &tm.v, smem_u32(j == it.b1 - 1 && it.dirty_tail() ? &ctl->tail[s] : &ctl->kv_full[s]), box, it.h);
                 if (lane == 0) ctl->issued = pos;
-                page = next_page; row = next_row;
+                box = next;
             }
         }
     } else if (warp == FwdWarps::TAIL) {
@@ -380,21 +352,6 @@ k_paged_tc(const __grid_constant__ PagedMaps tm, const __grid_constant__ PagedTc
     cta_teardown(waits.abort_flag, ctl->tmem_base, FwdWarps::MMA);
 }
 
-// pool of pages as [page][row][head][column]; box = 64 columns of `rows` rows of one head
-bool pool_map(CUtensorMap *m, const void *base, const PagedView &c, int rows)
-{
-    EncodeTiledFn enc = get_encode();
-    if (!enc) return false;
-    // a level of one entry may carry any stride
-    const int64_t width = (int64_t)c.d * 2, head = c.heads > 1 ? c.head_stride : width;
-    const int64_t page = c.n_pages > 1 ? c.page_stride : (int64_t)1 << 30;
-    cuuint64_t dims[4] = {(cuuint64_t)c.d, (cuuint64_t)c.heads, (cuuint64_t)c.page.d, (cuuint64_t)(c.n_pages > 0 ? c.n_pages : 1)};
-    cuuint64_t strides[3] = {(cuuint64_t)head, (cuuint64_t)c.row_stride, (cuuint64_t)page};
-    cuuint32_t box[4] = {64u, 1u, (cuuint32_t)rows, 1u}, es[4] = {1u, 1u, 1u, 1u};
-    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int DP> cudaError_t tc(const PagedAttnArgs &args, cudaStream_t s)
 {
     static int sms_of_device[64];
@@ -411,15 +368,11 @@ template <int DP> cudaError_t tc(const PagedAttnArgs &args, cudaStream_t s)
     p.a = args;
     p.a.runs = sms_of_device[dev];
     p.tokens = TILE / args.group;
-    p.page_rows = (int)args.c.page.d;
-    p.box = TILE;
-    while (p.page_rows % p.box) p.box /= 2;              // gcd(page_rows, 128), at least 8
+    p.box = box_rows(args.c);
     p.c2 = args.scale * LOG2E;
     PagedMaps tm;
-    // without pages no row is ever loaded: any address will do
-    const void *k = args.c.n_pages > 0 ? args.c.k : args.q, *v = args.c.n_pages > 0 ? args.c.v : args.q;
-    if (!head_map(&tm.q, args.q, args.c.d, args.hq, args.c.N, args.ldq, args.group, p.tokens) || !pool_map(&tm.k, k, args.c, p.box) ||
-        !pool_map(&tm.v, v, args.c, p.box))
+    if (!head_map(&tm.q, args.q, args.c.d, args.hq, args.c.N, args.ldq, args.group, p.tokens) || !pool_map(&tm.k, args.c.k, args.q, args.c, p.box) ||
+        !pool_map(&tm.v, args.c.v, args.q, args.c, p.box))
         return cudaErrorInvalidValue;
     cudaError_t e = launch_paged_list(p.a, 2 * p.tokens * args.group, TILE, s);
     if (e != cudaSuccess) return e;

@@ -2,82 +2,153 @@
 //
 //   weights[s, h, j] = prior + sum over new rows r of the head's group that see j of exp(scale q_r . k_j - lse_r)
 //
-// The forward's logarithms are given, so one pass over the keys suffices, and the sum over rows stays inside a warp: no
-// atomics, a fixed order.  Work is a line of units (sequence, head, 64 keys) that is cut into runs of equal cost, one per
-// CTA, two CTAs an SM; a CTA streams the steps of its units (64 keys x 32 rows; a unit's first step brings its keys, its
-// last one its priors) through a ring of asynchronous copies.  Keys are the rows of the products' accumulators (mma.sync), so a thread
-// adds its exponentials up as they come, and a warp's 16 keys stay in registers for all rows.  For few rows it is bound by
-// reading the keys, for many by the products (legacy matrix instructions: 64 x 32 x d multiply-adds a step) and the
-// exponentials.
-#include "paged.cuh"
-#include "paged_mma.cuh"
+// The forward's logarithms are given, so one pass over the keys suffices.  Scores are made with the keys on the
+// accumulator's rows (tcgen05.mma, 128 keys x up to 128 rows of queries), so a thread of the epilogue has one key and adds
+// its exponentials up in a register: no atomics, no shuffles, a fixed order.  Work is a line of units (sequence, head,
+// 128 keys), each with a step for every tile of query rows, cut into runs of equal steps, one CTA per SM:
+//   warp 0       key tiles through a ring (pages looked up a tile ahead), query tiles where they change
+//   warp 1       one product per step into one of four accumulators
+//   warps 2, 3   what needs no product: columns past a sequence's rows, sequences without new tokens
+//   warps 4..11  two groups that take units in turn: exponentials and sums
+// Bound by reading the keys for up to about 100 query rows a kv head, by the exponentials (16 a cycle and SM) beyond.  On the
+// legacy matrix instructions a step of 64 keys x 32 rows took 2 us from its copies to its sums however it was cut, with eight
+// warps an SM: 100 us for the batch of 48 conversations (238 MB), 250 us for 161 observing tokens of 40 heads.
+#include "paged_tma.cuh"
 
 namespace skipffn {
 
 namespace {
 
-constexpr int THREADS = 128, KEYS = 64, ROWS = 32, ZERO_COLS = 1024;
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr int WARPS = 12, THREADS = 32 * WARPS, ACCS = 4, FIRST = 4, ZERO_COLS = 1024;
 
-// What a stage of the ring holds, written when its copies are issued
-struct StepInfo { int s, h, j0, r0, rows, off, len, first, last; };
+struct WeightsParams {
+    PagedWeightsArgs a;
+    int32_t tokens, box;                     // tokens of a tile of query rows; rows of a TMA box
+};
+struct alignas(64) WeightsMaps { CUtensorMap q, k; };
 
 template <int DP> struct WeightsShape {
-    static constexpr int STAGES = DP == 128 ? 4 : 8;
-    static constexpr int KEY_BYTES = KEYS * DP * 2, ROW_BYTES = ROWS * DP * 2;
-    static constexpr int PRIOR = KEY_BYTES + ROW_BYTES, LSE = PRIOR + KEYS * 4, INFO = LSE + ROWS * 4, STAGE = INFO + 128;
-    static constexpr int SMEM = STAGES * STAGE;
+    static constexpr int T_BYTES = tile_bytes<DP>(), SLOTS = DP == 128 ? 4 : 8;
+    static constexpr int SMEM = (2 + SLOTS) * T_BYTES + 2048;
+};
+struct alignas(8) WeightsCtl {
+    uint64_t k_full[8], k_empty[8], q_full[2], q_empty[2], acc_full[ACCS], acc_empty[ACCS];
+    int64_t scan[WARPS], place[2];
+    uint32_t tmem_base;
+    volatile int abort_flag;
+    volatile uint32_t issued;
 };
 
-__device__ __forceinline__ void copy4(uint32_t dst, const void *src)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
+// One product: 128 keys from j0 on against `live` rows of queries, the tokens from t0 on
+struct Step {
+    int s, h, j0, t0, live, q0, off, len;    // len: rows that have a weight
+    int unit, count;                         // of this run: units before this one, steps up to this one
+    bool first, last, load_q;                // of the unit; other queries than the step before
+};
 
-template <int DP> __global__ void __launch_bounds__(THREADS, 2) k_paged_weights(const PagedWeightsArgs a, const int runs)
+// Walks the steps of this CTA's run, the same in every role
+struct Line {
+    const WeightsParams &p;
+    int64_t at, end;                         // first step of the unit, end of the run
+    int s, unit = 0, blocks, steps, tile = 0, units = 0, count = 0;
+    int held_s = -1, held_h = -1;            // whose only tile of queries is in shared memory
+    bool fresh = true;
+    PagedSeq q;
+    __device__ static int blocks_of(const PagedWeightsArgs &a, const PagedSeq &q) { return q.n > 0 ? (min(q.len, a.width) + TILE - 1) / TILE : 0; }
+    __device__ static int64_t cost_of(const WeightsParams &p, const PagedSeq &q)
+    {
+        return (int64_t)blocks_of(p.a, q) * p.a.c.heads * ceil_div(q.n, p.tokens);
+    }
+    __device__ void enter()
+    {
+        q = paged_seq(p.a.c, s, false);
+        blocks = blocks_of(p.a, q);
+        steps = ceil_div(q.n, p.tokens);
+    }
+    // the run's units are those whose first step lies in it
+    __device__ Line(const WeightsParams &p_, int64_t begin, int64_t end_, int seq, int64_t before) : p(p_), at(before), end(end_), s(seq)
+    {
+        if (begin >= end) { at = end; return; }
+        enter();
+        unit = (int)((begin - at + steps - 1) / steps);
+        at += (int64_t)unit * steps;
+        settle();
+    }
+    __device__ void settle()
+    {
+        while (unit == blocks * p.a.c.heads && at < end && s + 1 < p.a.c.n_seq) { ++s; enter(); unit = 0; }
+        if (unit == blocks * p.a.c.heads) at = end;
+        if (at < end) tile = max(0, unit % blocks * TILE - (q.len - q.n)) / p.tokens;     // tokens before it see none of the keys
+    }
+    __device__ bool next(Step &w)
+    {
+        if (at >= end) return false;
+        w.s = s; w.h = unit / blocks; w.j0 = (unit - w.h * blocks) * TILE; w.t0 = tile * p.tokens;
+        w.live = min(p.tokens, q.n - w.t0) * p.a.group;
+        w.q0 = q.q0; w.off = q.len - q.n; w.len = min(q.len, p.a.width);
+        w.unit = units; w.count = count++;
+        w.first = fresh;
+        w.last = fresh = ++tile == steps;
+        w.load_q = steps > 1 || s != held_s || w.h != held_h;
+        held_s = s; held_h = w.h;
+        if (fresh) { ++unit; ++units; at += steps; settle(); }
+        return true;
+    }
+};
+
+template <int DP>
+__global__ void __launch_bounds__(THREADS, 1) k_paged_weights(const __grid_constant__ WeightsMaps tm, const __grid_constant__ WeightsParams p)
 {
     using Sh = WeightsShape<DP>;
-    constexpr int CHUNKS = DP / 8, STEP = THREADS / CHUNKS;
-    extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int64_t scan[THREADS / 32], place[2];
-    pdl_enter();
+    constexpr int T_BYTES = Sh::T_BYTES, SLOTS = Sh::SLOTS;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    // of each epilogue warp (so that none waits for another): logarithms of the tile's rows of queries, and the last key
+    // that each sees, -1 for a row that gives nothing
+    __shared__ __align__(16) float lses[WARPS - FIRST][TILE];
+    __shared__ __align__(16) int sees[WARPS - FIRST][TILE];
+    const uint32_t q_tile = smem_u32(smem_raw), ring = q_tile + 2 * T_BYTES;
+    WeightsCtl *ctl = reinterpret_cast<WeightsCtl *>(smem_raw + (2 + SLOTS) * T_BYTES);
+    const PagedWeightsArgs &a = p.a;
     const PagedView &c = a.c;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, run = blockIdx.x;
-
-    // ---- columns past a sequence's rows
-    const int chunks = (a.width + ZERO_COLS - 1) / ZERO_COLS;
-    for (int64_t i = run; i < (int64_t)c.n_seq * c.heads * chunks; i += runs) {
-        const int64_t pair = i / chunks;
-        const int j0 = (int)(i - pair * chunks) * ZERO_COLS, j1 = min(a.width, j0 + ZERO_COLS);
-        const int len = min(max(c.lens[pair / c.heads], 0), c.capacity);
-        for (int j = max(j0, len) + tid; j < j1; j += THREADS) a.out[pair * a.width + j] = 0.0f;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < SLOTS; ++i) { mbar_init(smem_u32(&ctl->k_full[i]), 1); mbar_init(smem_u32(&ctl->k_empty[i]), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&ctl->q_full[i]), 1); mbar_init(smem_u32(&ctl->q_empty[i]), 1); }
+        for (int i = 0; i < ACCS; ++i) { mbar_init(smem_u32(&ctl->acc_full[i]), 1); mbar_init(smem_u32(&ctl->acc_empty[i]), 4); }
+        ctl->abort_flag = 0;
+        ctl->issued = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    const int used = a.group * p.tokens;     // rows of a tile that a box fills; the others stay zero
+    if (used < TILE) zero_smem(q_tile, 2 * T_BYTES);
+    fence_proxy_async_smem();
+    if (warp == 1) { tmem_alloc(smem_u32(&ctl->tmem_base), AT_TMEM_COLS); tmem_relinquish(); }
+    pdl_enter();
 
-    // ---- this CTA's run: units whose first step lies in it, in steps over the sequences
-    auto steps_of = [&](const PagedSeq &q) { return max(1, (q.n * a.group + ROWS - 1) / ROWS); };        // of one unit
-    auto blocks_of = [&](const PagedSeq &q) { return (min(q.len, a.width) + KEYS - 1) / KEYS; };
-    auto cost_of = [&](int s) {
+    // ---- this CTA's run
+    auto cost = [&](int s, bool report) {
         if (s >= c.n_seq) return (int64_t)0;
-        const PagedSeq q = paged_seq(c, s, run == 0);
-        if (run == 0 && q.len > a.width) paged_report(c, SITE_PAGED_WIDTH);
-        return (int64_t)blocks_of(q) * c.heads * steps_of(q);
+        const PagedSeq q = paged_seq(c, s, report);
+        if (report && q.len > a.width) paged_report(c, SITE_PAGED_WIDTH);
+        return Line::cost_of(p, q);
     };
     auto block_sum = [&](int64_t v) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         __syncthreads();
-        if (lane == 0) scan[warp] = v;
+        if (lane == 0) ctl->scan[warp] = v;
         __syncthreads();
-        return scan[0] + scan[1] + scan[2] + scan[3];
+        int64_t t = 0;
+        for (int i = 0; i < WARPS; ++i) t += ctl->scan[i];
+        return t;
     };
     int64_t mine = 0;
-    for (int s = tid; s < c.n_seq; s += THREADS) mine += cost_of(s);
-    const Runs line(block_sum(mine), runs);
-    const int64_t begin = line.begin(run), end = line.begin(run + 1);
-    if (begin >= end) return;
+    for (int s = tid; s < c.n_seq; s += THREADS) mine += cost(s, blockIdx.x == 0);
+    const Runs runs(block_sum(mine), (int)gridDim.x);
+    const int64_t begin = runs.begin(blockIdx.x), end = runs.begin(blockIdx.x + 1);
     int64_t before = 0;
-    for (int s0 = 0;; s0 += THREADS) {
-        const int64_t v = cost_of(s0 + tid);
+    for (int s0 = 0; s0 < c.n_seq && begin < end; s0 += THREADS) {
+        const int64_t v = cost(s0 + tid, false);
         int64_t x = v;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -86,171 +157,208 @@ template <int DP> __global__ void __launch_bounds__(THREADS, 2) k_paged_weights(
         }
         const int64_t total = block_sum(v);
         int64_t lo = before + x - v;
-        for (int i = 0; i < warp; ++i) lo += scan[i];
-        if (v > 0 && lo <= begin && begin < lo + v) { place[0] = s0 + tid; place[1] = lo; }
+        for (int i = 0; i < warp; ++i) lo += ctl->scan[i];
+        if (v > 0 && lo <= begin && begin < lo + v) { ctl->place[0] = s0 + tid; ctl->place[1] = lo; }
         before += total;
-        if (before > begin) break;           // the same in every thread; ends, since begin is inside the line
+        if (before > begin) break;           // the same in every thread
     }
+    tc_fence_before();
     __syncthreads();
+    tc_fence_after();
+    const Waits waits{&ctl->abort_flag, &ctl->issued, c.status, (uint32_t)WAIT_LIMIT_NS};
+    bool ok = true;
+    auto line = [&]() { return Line(p, begin, end, (int)ctl->place[0], ctl->place[1]); };
 
-    // ---- the ring
-    int s = (int)place[0], blocks, steps, unit, r0 = 0;
-    int64_t at = place[1];                   // first step of the unit
-    PagedSeq q;
-    auto enter = [&]() { q = paged_seq(c, s, false); blocks = blocks_of(q); steps = steps_of(q); };
-    auto first_row = [&](int j0) { return max(0, j0 - (q.len - q.n)) * a.group / ROWS * ROWS; };   // rows before it see none of the keys
-    // to a unit that exists, when the run has one left
-    auto settle = [&]() {
-        while (unit == blocks * c.heads && at < end && s + 1 < c.n_seq) { ++s; enter(); unit = 0; }
-        if (unit == blocks * c.heads) at = end;
-        if (at < end) r0 = first_row(unit % blocks * KEYS);
-    };
-    enter();
-    unit = (int)((begin - at + steps - 1) / steps);
-    at += (int64_t)unit * steps;
-    settle();
-    const uint32_t ring = smem_u32(smem);
-    int issued = 0;
-    bool fresh = true;                       // the unit's first step
-    auto issue = [&]() {
-        if (at < end) {
-            const int slot = issued % Sh::STAGES, h = unit / blocks, j0 = (unit - h * blocks) * KEYS, rows = q.n * a.group;
-            const int len = min(q.len, a.width);
-            const uint32_t dst = ring + slot * Sh::STAGE;
-            const int chunk = tid % CHUNKS, t0 = tid / CHUNKS;
-            const bool last = r0 + ROWS >= rows;
-            if (fresh) {
-                int64_t base = -1;           // lane i < 8: rows 8 i .. 8 i + 7
-                if (lane < KEYS / 8 && j0 + 8 * lane < len && rows > 0) {
-                    base = paged_row(c, s, j0 + 8 * lane);
-                    if (base >= 0) base += h * c.head_stride;
-                    else paged_report(c, SITE_PAGED_PAGE);
+    if (warp == 0) {
+        const PageBoxes boxes{c, p.box, lane};
+        Line walk = line();
+        Step w, n;
+        uint32_t k = 0, q = 0;               // tiles of keys, of queries so far
+        bool more = walk.next(w);
+        PageBox box = {0, -1}, next = box;
+        if (more) box = boxes.find(w.s, w.len, w.j0);
+        while (more && ok) {
+            const bool another = walk.next(n);
+            if (another && n.first) next = boxes.find(n.s, n.len, n.j0);
+            if (w.load_q) {
+                const uint32_t s = q & 1;
+                ok = wait_warp<true>(smem_u32(&ctl->q_empty[s]), ((q >> 1) & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
+                if (!ok) break;
+                if (lane == 0) {
+                    mbar_expect_tx(smem_u32(&ctl->q_full[s]), (uint32_t)(used * DP * 2));
+                    load_tile<DP>(q_tile + s * T_BYTES, &tm.q, w.h * a.group, w.q0 + w.t0, smem_u32(&ctl->q_full[s]));
                 }
-#pragma unroll
-                for (int i = 0; i < KEYS / STEP; ++i) {
-                    const int r = t0 + i * STEP;
-                    const int64_t g = __shfl_sync(0xffffffffu, base, r >> 3);
-                    const bool on = g >= 0 && j0 + r < len && chunk * 8 < c.d;
-                    copy16(dst + chunk_at<DP>(r, chunk), c.k + (on ? g + (r & 7) * c.row_stride + chunk * 16 : 0), on);
-                }
+                ++q;
             }
-            if (last && a.prior && tid < KEYS && j0 + tid < len)
-                copy4(dst + Sh::PRIOR + tid * 4, a.prior + ((int64_t)s * c.heads + h) * a.width + j0 + tid);
-            const int live = min(ROWS, rows - r0);
-#pragma unroll
-            for (int i = 0; i < ROWS / STEP; ++i) {
-                const int r = t0 + i * STEP;
-                if (r >= ((live + 15) & ~15)) break;
-                const bool on = r < live && chunk * 8 < c.d;
-                const bf16 *src = (const bf16 *)a.q;
-                if (on) src += (int64_t)(q.q0 + (r0 + r) / a.group) * a.ldq + (int64_t)(h * a.group + (r0 + r) % a.group) * c.d + chunk * 8;
-                copy16(dst + Sh::KEY_BYTES + chunk_at<DP>(r, chunk), src, on);
+            if (w.first) {
+                boxes.check(box);
+                const uint32_t s = k % SLOTS;
+                ok = wait_warp<true>(smem_u32(&ctl->k_empty[s]), ((k / SLOTS) & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
+                if (!ok) break;
+                boxes.load<DP>(ring + s * T_BYTES, &tm.k, smem_u32(&ctl->k_full[s]), box, w.h);
+                ++k;
+                if (lane == 0) ctl->issued = k;
             }
-            if (tid < ROWS) {
-                const int r = r0 + tid;
-                if (tid < live) copy4(dst + Sh::LSE + tid * 4, a.lse + (int64_t)(q.q0 + r / a.group) * a.hq + h * a.group + r % a.group);
-                else *reinterpret_cast<float *>(smem + slot * Sh::STAGE + Sh::LSE + tid * 4) = INFINITY;     // a row that is not there weighs nothing
+            if (another && n.first) box = next;
+            w = n;
+            more = another;
+        }
+    } else if (warp == 1) {
+        const uint32_t on = elect_one();     // the warp walks as one, one thread issues
+        const uint32_t q_desc = desc_rows(q_tile), k_desc = desc_rows(ring);
+        Line walk = line();
+        Step w;
+        uint32_t k = 0, q = 0;
+        while (ok && walk.next(w)) {
+            if (w.load_q) {
+                // the queries before these have no product left to come
+                if (q > 0) umma_commit_if(on, smem_u32(&ctl->q_empty[(q - 1) & 1]));
+                ok = wait_warp<true>(smem_u32(&ctl->q_full[q & 1]), (q >> 1) & 1, waits, SITE_MMA_FULL);
+                ++q;
             }
-            if (tid == 0) *reinterpret_cast<StepInfo *>(smem + slot * Sh::STAGE + Sh::INFO) = StepInfo{s, h, j0, r0, rows, q.len - q.n, len, fresh, last};
-            ++issued;
-            fresh = last;
-            r0 += ROWS;
-            if (last) {
-                ++unit;
-                at += steps;
-                settle();
+            if (w.first) {
+                ok = ok && wait_warp<true>(smem_u32(&ctl->k_full[k % SLOTS]), (k / SLOTS) & 1, waits, SITE_MMA_FULL);
+                ++k;
+            }
+            const uint32_t acc = w.count % ACCS, n = uniform(w.count) / ACCS;
+            ok = ok && wait_warp<true>(smem_u32(&ctl->acc_empty[acc]), (n & 1) ^ 1, waits, SITE_MMA_TMEM_EMPTY);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t ks = uniform((int)((k - 1) % SLOTS)), qs = uniform((int)((q - 1) & 1));
+            mma_rows_rows<DP>(on, tmem + uniform((int)acc) * TILE, k_desc + ks * (T_BYTES >> 4), q_desc + qs * (T_BYTES >> 4),
+                              idesc_rows(uniform(mma_cols(w.live))));
+            umma_commit_if(on, smem_u32(&ctl->acc_full[acc]));
+            if (w.last) umma_commit_if(on, smem_u32(&ctl->k_empty[ks]));
+        }
+    } else if (warp < FIRST) {
+        const int chunks = ceil_div(a.width, ZERO_COLS);
+        for (int64_t i = blockIdx.x; i < (int64_t)c.n_seq * c.heads * chunks; i += gridDim.x) {
+            const int64_t pair = i / chunks;
+            const int j0 = (int)(i - pair * chunks) * ZERO_COLS, j1 = min(a.width, j0 + ZERO_COLS);
+            const PagedSeq q = paged_seq(c, (int)(pair / c.heads), false);
+            const int from = q.n > 0 ? max(j0, q.len) : j0;
+            for (int j = from + tid - 64; j < j1; j += 64) {
+                const int64_t at = pair * a.width + j;
+                a.out[at] = j < q.len && a.prior ? a.prior[at] : 0.0f;
             }
         }
-        copy_commit();
-    };
+    } else {
+        const int g = (warp - FIRST) >> 2, mine = (warp & 3) * 32 + lane;      // group, key of the unit
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        Line walk = line();
+        Step w, n;
+        auto next = [&](Step &x) {           // this group's units
+            while (walk.next(x))
+                if ((x.unit & 1) == g) return true;
+            return false;
+        };
+        // a group sees every other unit: the queries are others when sequence, head or tile are
+        int held_s = -1, held_h = -1, held_t = -1;
+        auto changes = [&](const Step &x) { return x.s != held_s || x.h != held_h || x.t0 != held_t; };
+        float ahead[4], total = 0.0f, prior = 0.0f, *ls = lses[warp - FIRST];
+        int *see = sees[warp - FIRST];
+        bool odd = false;                    // the tile has rows that give nothing
+        auto look_up = [&](const Step &x) {
 #pragma unroll
-    for (int i = 0; i < Sh::STAGES - 1; ++i) issue();
-
-    // ---- arithmetic: a warp has 16 keys, a thread keys `key` and `key` + 8 of them
-    const int key = warp * 16 + (lane >> 2);
-    uint32_t kf[DP / 16][4];
-    float total[2] = {0.0f, 0.0f};
-    for (int done = 0;; ++done) {
-        if (done == issued) break;           // the ring is empty, and issue() had nothing to add
-        copy_wait<Sh::STAGES - 2>();
-        __syncthreads();                     // the step is there for every warp, and the slot refilled next is free
-        issue();
-        const int slot = done % Sh::STAGES;
-        const uint32_t src = ring + slot * Sh::STAGE, rt = src + Sh::KEY_BYTES;
-        const StepInfo t = *reinterpret_cast<const StepInfo *>(smem + slot * Sh::STAGE + Sh::INFO);
-        const float *lse = reinterpret_cast<const float *>(smem + slot * Sh::STAGE + Sh::LSE);
-        if (t.first) {
-            total[0] = total[1] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < DP / 16; ++k)
-                // rows of a: lanes 0-15 keys 0-15 of eight columns, lanes 16-31 of the next eight
-                ldsm_x4(src + chunk_at<DP>(warp * 16 + (lane & 15), 2 * k + (lane >> 4)), kf[k]);
-        }
-        // the first row of the step sees every key: no mask
-        const bool masked = t.j0 + KEYS - 1 > t.off + t.r0 / a.group;
-#pragma unroll
-        for (int n = 0; n < ROWS / 8; n += 2) {
-            if (t.r0 + 8 * n >= t.rows) break;
-            float x[2][4] = {};
-#pragma unroll
-            for (int k = 0; k < DP / 16; ++k) {
-                uint32_t b[4];
-                ldsm_x4(rt + chunk_at<DP>(n * 8 + (lane >> 4) * 8 + (lane & 7), 2 * k + ((lane >> 3) & 1)), b);
-                mma_16x8(x[0], kf[k], b[0], b[1]);
-                mma_16x8(x[1], kf[k], b[2], b[3]);
+            for (int i = 0; i < 4; ++i) {
+                const int r = lane + 32 * i;
+                ahead[i] = r < x.live ? a.lse[(int64_t)(x.q0 + x.t0 + r / a.group) * a.hq + x.h * a.group + r % a.group] : -INFINITY;
             }
+        };
+        bool more = next(w);
+        if (more) look_up(w);
+        while (more && ok) {
+            if (changes(w)) {
+                bool none = false;
+                __syncwarp();
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                const int i = 8 * (n + y) + 2 * (lane & 3);
-                const float2 l2 = *reinterpret_cast<const float2 *>(lse + i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float l = e & 1 ? l2.y : l2.x;
-                    // the difference first: it is small where the weight counts, so its rounding is too
-                    float w = fast_exp2(fmaf(x[y][e], a.scale, -l) * LOG2E);
-                    // a token without a logarithm saw nothing
-                    if (l == -INFINITY || (masked && t.j0 + key + 8 * (e >> 1) > t.off + (t.r0 + i + (e & 1)) / a.group)) w = 0.0f;
-                    total[e >> 1] += w;
+                for (int i = 0; i < 4; ++i) {
+                    const int r = lane + 32 * i;
+                    const bool empty = ahead[i] == -INFINITY;
+                    ls[r] = empty ? 0.0f : ahead[i];
+                    see[r] = empty ? -1 : w.off + w.t0 + r / a.group;
+                    none |= empty && r < w.live;
                 }
+                odd = __any_sync(0xffffffffu, none);
+                __syncwarp();
+                held_s = w.s; held_h = w.h; held_t = w.t0;
             }
-        }
-        if (t.last) {
-            const float *prior = reinterpret_cast<const float *>(smem + slot * Sh::STAGE + Sh::PRIOR);
-            float *out = a.out + ((int64_t)t.s * c.heads + t.h) * a.width + t.j0;
+            if (w.first) {
+                total = 0.0f;
+                prior = a.prior && w.j0 + mine < w.len ? a.prior[((int64_t)w.s * c.heads + w.h) * a.width + w.j0 + mine] : 0.0f;
+            }
+            const bool another = next(n);
+            if (another && changes(n)) look_up(n);
+            const uint32_t acc = w.count % ACCS;
+            ok = wait_warp<true>(smem_u32(&ctl->acc_full[acc]), (w.count / ACCS) & 1, waits, SITE_EPI_TMEM_FULL);
+            if (!ok) break;
+            tc_fence_after();
+            // every row of the tile sees every key, and gives something
+            const bool plain = w.j0 + TILE - 1 <= w.off + w.t0 && !odd;
+            const int key = w.j0 + mine;
+#pragma unroll 1
+            for (int c0 = 0; c0 < w.live; c0 += 16) {
+                uint32_t x[16];
+                tmem_ld16(tmem + lanes + acc * TILE + c0, x);
+                tmem_ld_wait(x);
+                float sum = 0.0f;
+                // the difference first: it is small where the weight counts, so its rounding is too
+                if (plain && c0 + 16 <= w.live) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float w = total[i] + __shfl_xor_sync(0xffffffffu, total[i], 1);
-                w += __shfl_xor_sync(0xffffffffu, w, 2);
-                const int k = key + 8 * i;
-                if ((lane & 3) == 0 && t.j0 + k < t.len) out[k] = a.prior ? prior[k] + w : w;
+                    for (int e = 0; e < 16; e += 4) {
+                        float l[4];
+                        load4(ls + c0 + e, l);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) sum += fast_exp2(fmaf(__uint_as_float(x[e + y]), a.scale, -l[y]) * LOG2E);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float v = fast_exp2(fmaf(__uint_as_float(x[e]), a.scale, -ls[c0 + e]) * LOG2E);
+                        sum += key <= see[c0 + e] ? v : 0.0f;
+                    }
+                }
+                total += sum;
             }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[acc]));
+            if (w.last && key < w.len) a.out[((int64_t)w.s * c.heads + w.h) * a.width + key] = prior + total;
+            w = n;
+            more = another;
         }
     }
-    copy_wait<0>();
+    cta_teardown(waits.abort_flag, ctl->tmem_base, 1);
 }
 
 template <int DP> cudaError_t weights(const PagedWeightsArgs &a, cudaStream_t s)
 {
     using Sh = WeightsShape<DP>;
-    static int runs_of_device[64];
+    static int sms_of_device[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    if (runs_of_device[dev] == 0) {
-        int sms = 0, per = 0;
+    if (sms_of_device[dev] == 0) {
+        int n = 0;
         cudaError_t e = cudaFuncSetAttribute(k_paged_weights<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::SMEM);
-        if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, k_paged_weights<DP>, THREADS, Sh::SMEM);
+        if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
         if (e != cudaSuccess) return e;
-        if (per < 1) return cudaErrorInvalidConfiguration;
-        runs_of_device[dev] = sms * (per < 2 ? per : 2);
+        sms_of_device[dev] = n;
     }
+    WeightsParams p = {};
+    p.a = a;
+    p.tokens = TILE / a.group;
+    p.box = box_rows(a.c);
+    WeightsMaps tm = {};
+    // a call without tokens has no products
+    if (a.c.N > 0 && (!head_map(&tm.q, a.q, a.c.d, a.hq, a.c.N, a.ldq, a.group, p.tokens) || !pool_map(&tm.k, a.c.k, a.q, a.c, p.box)))
+        return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)runs_of_device[dev]); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = Sh::SMEM; cfg.stream = s;
+    cfg.gridDim = dim3((unsigned)sms_of_device[dev]); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = Sh::SMEM; cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_paged_weights<DP>, a, runs_of_device[dev]);
+    return cudaLaunchKernelEx(&cfg, k_paged_weights<DP>, tm, p);
 }
 
 }  // namespace
