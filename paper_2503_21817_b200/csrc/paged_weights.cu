@@ -5,56 +5,58 @@
 // The forward's logarithms are given, so one pass over the keys suffices.  Scores are made with the keys on the
 // accumulator's rows (tcgen05.mma, 128 keys x up to 128 rows of queries), so a thread of the epilogue has one key and adds
 // its exponentials up in a register: no atomics, no shuffles, a fixed order.  Work is a line of units (sequence, head,
-// 128 keys), each with a step for every tile of query rows, cut into runs of equal steps, one CTA per SM:
-//   warp 0       key tiles through a ring (pages looked up a tile ahead), query tiles where they change
-//   warp 1       one product per step into one of four accumulators
-//   warps 2, 3   what needs no product: columns past a sequence's rows, sequences without new tokens
-//   warps 4..11  two groups that take units in turn: exponentials and sums
-// Bound by reading the keys for up to about 100 query rows a kv head, by the exponentials (16 a cycle and SM) beyond.  On the
-// legacy matrix instructions a step of 64 keys x 32 rows took 2 us from its copies to its sums however it was cut, with eight
-// warps an SM: 100 us for the batch of 48 conversations (238 MB), 250 us for 161 observing tokens of 40 heads.
+// 256 keys), each with a step for every tile of query rows, cut into runs of equal steps, one per CTA, one CTA per SM:
+//   warps 0, 2   key tiles of the first and second half of a unit (pages looked up a unit ahead), query tiles
+//   warp 1       the two products of a step
+//   warp 3       what needs no product: columns past a sequence's rows, sequences without new tokens
+//   warps 4..11  two groups, one for each half: exponentials and sums
+// Bound by reading the keys for up to about 100 query rows a kv head, by the exponentials (16 a cycle and SM) beyond.  A TMA
+// box costs its warp about 64 cycles whatever its size, so pages of 16 rows want the two warps (48 conversations: one warp
+// 82 us, two 71 us, with pages of 128 rows 58 us either way).  On the legacy matrix instructions a step of 64 keys x 32 rows
+// took 2 us from its copies to its sums however it was cut, with eight warps an SM: 100 us for the batch of 48
+// conversations (238 MB), 250 us for 161 observing tokens of 40 heads.
 #include "paged_tma.cuh"
 
 namespace skipffn {
 
 namespace {
 
-constexpr int WARPS = 12, THREADS = 32 * WARPS, ACCS = 4, FIRST = 4, ZERO_COLS = 1024;
+constexpr int WARPS = 12, THREADS = 32 * WARPS, FIRST = 4, FILL_COLS = 1024, UNIT = 2 * TILE;
 
 struct WeightsParams {
     PagedWeightsArgs a;
     int32_t tokens, box;                     // tokens of a tile of query rows; rows of a TMA box
+    int32_t q_slots, k_slots;                // tiles of queries, of each half's keys in shared memory
 };
 struct alignas(64) WeightsMaps { CUtensorMap q, k; };
 
 template <int DP> struct WeightsShape {
-    static constexpr int T_BYTES = tile_bytes<DP>(), SLOTS = DP == 128 ? 4 : 8;
-    static constexpr int SMEM = (2 + SLOTS) * T_BYTES + 2048;
+    static constexpr int T_BYTES = tile_bytes<DP>(), SLOTS = DP == 128 ? 6 : 10;       // of keys and of queries
+    static constexpr int SMEM = SLOTS * T_BYTES + 2048;
 };
 struct alignas(8) WeightsCtl {
-    uint64_t k_full[8], k_empty[8], q_full[2], q_empty[2], acc_full[ACCS], acc_empty[ACCS];
+    uint64_t full[10], empty[10], acc_full[2][2], acc_empty[2][2];      // accumulators of each group
     int64_t scan[WARPS], place[2];
     uint32_t tmem_base;
     volatile int abort_flag;
     volatile uint32_t issued;
 };
 
-// One product: 128 keys from j0 on against `live` rows of queries, the tokens from t0 on
+// Up to 256 keys from j0 on against `live` rows of queries, the tokens from t0 on
 struct Step {
     int s, h, j0, t0, live, q0, off, len;    // len: rows that have a weight
-    int unit, count;                         // of this run: units before this one, steps up to this one
     bool first, last, load_q;                // of the unit; other queries than the step before
+    __device__ bool half(int g) const { return j0 + g * TILE < len; }
 };
 
 // Walks the steps of this CTA's run, the same in every role
 struct Line {
     const WeightsParams &p;
     int64_t at, end;                         // first step of the unit, end of the run
-    int s, unit = 0, blocks, steps, tile = 0, units = 0, count = 0;
-    int held_s = -1, held_h = -1;            // whose only tile of queries is in shared memory
-    bool fresh = true;
+    int s, h = 0, b = 0, blocks, steps, tile = 0;
+    bool fresh = true, moved = true;         // a new unit, another (sequence, head)
     PagedSeq q;
-    __device__ static int blocks_of(const PagedWeightsArgs &a, const PagedSeq &q) { return q.n > 0 ? (min(q.len, a.width) + TILE - 1) / TILE : 0; }
+    __device__ static int blocks_of(const PagedWeightsArgs &a, const PagedSeq &q) { return q.n > 0 ? (min(q.len, a.width) + UNIT - 1) / UNIT : 0; }
     __device__ static int64_t cost_of(const WeightsParams &p, const PagedSeq &q)
     {
         return (int64_t)blocks_of(p.a, q) * p.a.c.heads * ceil_div(q.n, p.tokens);
@@ -64,34 +66,42 @@ struct Line {
         q = paged_seq(p.a.c, s, false);
         blocks = blocks_of(p.a, q);
         steps = ceil_div(q.n, p.tokens);
+        h = b = 0;
     }
     // the run's units are those whose first step lies in it
     __device__ Line(const WeightsParams &p_, int64_t begin, int64_t end_, int seq, int64_t before) : p(p_), at(before), end(end_), s(seq)
     {
         if (begin >= end) { at = end; return; }
         enter();
-        unit = (int)((begin - at + steps - 1) / steps);
-        at += (int64_t)unit * steps;
+        const int64_t unit = (begin - at + steps - 1) / steps;
+        at += unit * steps;
+        h = (int)(unit / blocks);
+        b = (int)(unit - (int64_t)h * blocks);
         settle();
     }
     __device__ void settle()
     {
-        while (unit == blocks * p.a.c.heads && at < end && s + 1 < p.a.c.n_seq) { ++s; enter(); unit = 0; }
-        if (unit == blocks * p.a.c.heads) at = end;
-        if (at < end) tile = max(0, unit % blocks * TILE - (q.len - q.n)) / p.tokens;     // tokens before it see none of the keys
+        if (b == blocks) { b = 0; ++h; moved = true; }
+        if (h == p.a.c.heads) {
+            do {
+                if (at >= end || s + 1 >= p.a.c.n_seq) { at = end; return; }
+                ++s;
+                enter();
+            } while (blocks == 0);
+        }
+        tile = max(0, b * UNIT - (q.len - q.n)) / p.tokens;           // tokens before it see none of the keys
     }
     __device__ bool next(Step &w)
     {
         if (at >= end) return false;
-        w.s = s; w.h = unit / blocks; w.j0 = (unit - w.h * blocks) * TILE; w.t0 = tile * p.tokens;
+        w.s = s; w.h = h; w.j0 = b * UNIT; w.t0 = tile * p.tokens;
         w.live = min(p.tokens, q.n - w.t0) * p.a.group;
         w.q0 = q.q0; w.off = q.len - q.n; w.len = min(q.len, p.a.width);
-        w.unit = units; w.count = count++;
         w.first = fresh;
         w.last = fresh = ++tile == steps;
-        w.load_q = steps > 1 || s != held_s || w.h != held_h;
-        held_s = s; held_h = w.h;
-        if (fresh) { ++unit; ++units; at += steps; settle(); }
+        w.load_q = steps > 1 || moved;
+        moved = false;
+        if (fresh) { ++b; at += steps; settle(); }
         return true;
     }
 };
@@ -106,21 +116,20 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_weights(const __grid_const
     // that each sees, -1 for a row that gives nothing
     __shared__ __align__(16) float lses[WARPS - FIRST][TILE];
     __shared__ __align__(16) int sees[WARPS - FIRST][TILE];
-    const uint32_t q_tile = smem_u32(smem_raw), ring = q_tile + 2 * T_BYTES;
-    WeightsCtl *ctl = reinterpret_cast<WeightsCtl *>(smem_raw + (2 + SLOTS) * T_BYTES);
+    const uint32_t ring = smem_u32(smem_raw);                // tiles of queries, of first halves, of second halves
+    WeightsCtl *ctl = reinterpret_cast<WeightsCtl *>(smem_raw + SLOTS * T_BYTES);
     const PagedWeightsArgs &a = p.a;
     const PagedView &c = a.c;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (int i = 0; i < SLOTS; ++i) { mbar_init(smem_u32(&ctl->k_full[i]), 1); mbar_init(smem_u32(&ctl->k_empty[i]), 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&ctl->q_full[i]), 1); mbar_init(smem_u32(&ctl->q_empty[i]), 1); }
-        for (int i = 0; i < ACCS; ++i) { mbar_init(smem_u32(&ctl->acc_full[i]), 1); mbar_init(smem_u32(&ctl->acc_empty[i]), 4); }
+        for (int i = 0; i < SLOTS; ++i) { mbar_init(smem_u32(&ctl->full[i]), 1); mbar_init(smem_u32(&ctl->empty[i]), 1); }
+        for (int i = 0; i < 4; ++i) { mbar_init(smem_u32(&ctl->acc_full[i >> 1][i & 1]), 1); mbar_init(smem_u32(&ctl->acc_empty[i >> 1][i & 1]), 4); }
         ctl->abort_flag = 0;
         ctl->issued = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     const int used = a.group * p.tokens;     // rows of a tile that a box fills; the others stay zero
-    if (used < TILE) zero_smem(q_tile, 2 * T_BYTES);
+    if (used < TILE) zero_smem(ring, p.q_slots * T_BYTES);
     fence_proxy_async_smem();
     if (warp == 1) { tmem_alloc(smem_u32(&ctl->tmem_base), AT_TMEM_COLS); tmem_relinquish(); }
     pdl_enter();
@@ -167,37 +176,52 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_weights(const __grid_const
     tc_fence_after();
     const Waits waits{&ctl->abort_flag, &ctl->issued, c.status, (uint32_t)WAIT_LIMIT_NS};
     bool ok = true;
+    // a place in one of the rings (queries, first halves, second halves): slot and parity
+    struct Ring {
+        int first, slots, at = 0;
+        uint32_t phase = 0;
+        __device__ Ring(int f, int n) : first(f), slots(n) {}
+        __device__ int slot() const { return first + at; }
+        __device__ void next() { if (++at == slots) { at = 0; phase ^= 1; } }
+    };
+    auto full = [&](int slot) { return smem_u32(&ctl->full[slot]); };
+    auto empty = [&](int slot) { return smem_u32(&ctl->empty[slot]); };
+    auto queries = [&]() { return Ring(0, p.q_slots); };
+    auto keys = [&](int g) { return Ring(p.q_slots + g * p.k_slots, p.k_slots); };
     auto line = [&]() { return Line(p, begin, end, (int)ctl->place[0], ctl->place[1]); };
 
-    if (warp == 0) {
+    if (warp == 0 || warp == 2) {
         const PageBoxes boxes{c, p.box, lane};
+        const int g = warp / 2;
         Line walk = line();
         Step w, n;
-        uint32_t k = 0, q = 0;               // tiles of keys, of queries so far
+        Ring q = queries(), k = keys(g);
+        uint32_t tiles = 0;
         bool more = walk.next(w);
         PageBox box = {0, -1}, next = box;
-        if (more) box = boxes.find(w.s, w.len, w.j0);
+        if (more) box = boxes.find(w.s, w.len, w.j0 + g * TILE);
         while (more && ok) {
             const bool another = walk.next(n);
-            if (another && n.first) next = boxes.find(n.s, n.len, n.j0);
-            if (w.load_q) {
-                const uint32_t s = q & 1;
-                ok = wait_warp<true>(smem_u32(&ctl->q_empty[s]), ((q >> 1) & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
+            if (another && n.first) next = boxes.find(n.s, n.len, n.j0 + g * TILE);
+            if (w.load_q && g == 0) {
+                const int s = q.slot();
+                ok = wait_warp<true>(empty(s), q.phase ^ 1, waits, SITE_PRODUCER_EMPTY);
                 if (!ok) break;
                 if (lane == 0) {
-                    mbar_expect_tx(smem_u32(&ctl->q_full[s]), (uint32_t)(used * DP * 2));
-                    load_tile<DP>(q_tile + s * T_BYTES, &tm.q, w.h * a.group, w.q0 + w.t0, smem_u32(&ctl->q_full[s]));
+                    mbar_expect_tx(full(s), (uint32_t)(used * DP * 2));
+                    load_tile<DP>(ring + s * T_BYTES, &tm.q, w.h * a.group, w.q0 + w.t0, full(s));
+                    ctl->issued = ++tiles;
                 }
-                ++q;
+                q.next();
             }
-            if (w.first) {
+            if (w.first && w.half(g)) {
                 boxes.check(box);
-                const uint32_t s = k % SLOTS;
-                ok = wait_warp<true>(smem_u32(&ctl->k_empty[s]), ((k / SLOTS) & 1) ^ 1, waits, SITE_PRODUCER_EMPTY);
+                const int s = k.slot();
+                ok = wait_warp<true>(empty(s), k.phase ^ 1, waits, SITE_PRODUCER_EMPTY);
                 if (!ok) break;
-                boxes.load<DP>(ring + s * T_BYTES, &tm.k, smem_u32(&ctl->k_full[s]), box, w.h);
-                ++k;
-                if (lane == 0) ctl->issued = k;
+                boxes.load<DP>(ring + s * T_BYTES, &tm.k, full(s), box, w.h);
+                k.next();
+                if (lane == 0 && g == 0) ctl->issued = ++tiles;
             }
             if (another && n.first) box = next;
             w = n;
@@ -205,68 +229,86 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_weights(const __grid_const
         }
     } else if (warp == 1) {
         const uint32_t on = elect_one();     // the warp walks as one, one thread issues
-        const uint32_t q_desc = desc_rows(q_tile), k_desc = desc_rows(ring);
+        const uint32_t desc = desc_rows(ring);
         Line walk = line();
-        Step w;
-        uint32_t k = 0, q = 0;
-        while (ok && walk.next(w)) {
+        Step w, n;
+        Ring q = queries(), k[2] = {keys(0), keys(1)};
+        int qs = 0, ks[2] = {0, 0};
+        uint32_t count[2] = {0, 0};
+        bool more = walk.next(w);
+        while (more && ok) {
+            const bool another = walk.next(n);
             if (w.load_q) {
-                // the queries before these have no product left to come
-                if (q > 0) umma_commit_if(on, smem_u32(&ctl->q_empty[(q - 1) & 1]));
-                ok = wait_warp<true>(smem_u32(&ctl->q_full[q & 1]), (q >> 1) & 1, waits, SITE_MMA_FULL);
-                ++q;
+                qs = uniform(q.slot());
+                ok = wait_warp<true>(full(qs), q.phase, waits, SITE_MMA_FULL);
+                q.next();
             }
-            if (w.first) {
-                ok = ok && wait_warp<true>(smem_u32(&ctl->k_full[k % SLOTS]), (k / SLOTS) & 1, waits, SITE_MMA_FULL);
-                ++k;
+            const uint32_t idesc = idesc_rows(uniform(mma_cols(w.live)));
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                if (!w.half(g)) continue;
+                if (w.first) {
+                    ks[g] = uniform(k[g].slot());
+                    ok = ok && wait_warp<true>(full(ks[g]), k[g].phase, waits, SITE_MMA_FULL);
+                    k[g].next();
+                }
+                const uint32_t acc = count[g] & 1;
+                ok = ok && wait_warp<true>(smem_u32(&ctl->acc_empty[g][acc]), (count[g] >> 1 & 1) ^ 1, waits, SITE_MMA_TMEM_EMPTY);
+                if (!ok) break;
+                ++count[g];
+                tc_fence_after();
+                mma_rows_rows<DP>(on, tmem + (2 * g + acc) * TILE, desc + ks[g] * (T_BYTES >> 4), desc + qs * (T_BYTES >> 4), idesc);
+                umma_commit_if(on, smem_u32(&ctl->acc_full[g][acc]));
+                if (w.last) umma_commit_if(on, empty(ks[g]));
             }
-            const uint32_t acc = w.count % ACCS, n = uniform(w.count) / ACCS;
-            ok = ok && wait_warp<true>(smem_u32(&ctl->acc_empty[acc]), (n & 1) ^ 1, waits, SITE_MMA_TMEM_EMPTY);
             if (!ok) break;
-            tc_fence_after();
-            const uint32_t ks = uniform((int)((k - 1) % SLOTS)), qs = uniform((int)((q - 1) & 1));
-            mma_rows_rows<DP>(on, tmem + uniform((int)acc) * TILE, k_desc + ks * (T_BYTES >> 4), q_desc + qs * (T_BYTES >> 4),
-                              idesc_rows(uniform(mma_cols(w.live))));
-            umma_commit_if(on, smem_u32(&ctl->acc_full[acc]));
-            if (w.last) umma_commit_if(on, smem_u32(&ctl->k_empty[ks]));
+            if (another && n.load_q) umma_commit_if(on, empty(qs));
+            w = n;
+            more = another;
         }
-    } else if (warp < FIRST) {
-        const int chunks = ceil_div(a.width, ZERO_COLS);
+    } else if (warp == 3) {
+        const int chunks = ceil_div(a.width, FILL_COLS);
         for (int64_t i = blockIdx.x; i < (int64_t)c.n_seq * c.heads * chunks; i += gridDim.x) {
             const int64_t pair = i / chunks;
-            const int j0 = (int)(i - pair * chunks) * ZERO_COLS, j1 = min(a.width, j0 + ZERO_COLS);
+            const int j0 = (int)(i - pair * chunks) * FILL_COLS, j1 = min(a.width, j0 + FILL_COLS);
             const PagedSeq q = paged_seq(c, (int)(pair / c.heads), false);
             const int from = q.n > 0 ? max(j0, q.len) : j0;
-            for (int j = from + tid - 64; j < j1; j += 64) {
+            for (int j = from + lane; j < j1; j += 32) {
                 const int64_t at = pair * a.width + j;
                 a.out[at] = j < q.len && a.prior ? a.prior[at] : 0.0f;
             }
         }
     } else {
-        const int g = (warp - FIRST) >> 2, mine = (warp & 3) * 32 + lane;      // group, key of the unit
+        const int g = (warp - FIRST) >> 2, mine = g * TILE + (warp & 3) * 32 + lane;        // group, key of the unit
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         Line walk = line();
         Step w, n;
-        auto next = [&](Step &x) {           // this group's units
+        auto next = [&](Step &x) {           // the steps in which this group has keys
             while (walk.next(x))
-                if ((x.unit & 1) == g) return true;
+                if (x.half(g)) return true;
             return false;
         };
-        // a group sees every other unit: the queries are others when sequence, head or tile are
+        // the lane looks after rows lane, lane + 32, .. of the queries: their tokens and heads in a tile
+        int row_t[4], row_h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { row_t[i] = (lane + 32 * i) / a.group; row_h[i] = lane + 32 * i - row_t[i] * a.group; }
+        // a group may pass steps over: the queries are others when sequence, head or tile are
         int held_s = -1, held_h = -1, held_t = -1;
         auto changes = [&](const Step &x) { return x.s != held_s || x.h != held_h || x.t0 != held_t; };
-        float ahead[4], total = 0.0f, prior = 0.0f, *ls = lses[warp - FIRST];
+        float ahead[4], total = 0.0f, prior = 0.0f, prior_ahead = 0.0f, *ls = lses[warp - FIRST];
         int *see = sees[warp - FIRST];
         bool odd = false;                    // the tile has rows that give nothing
+        uint32_t count = 0;
         auto look_up = [&](const Step &x) {
+            const float *src = a.lse + (int64_t)(x.q0 + x.t0) * a.hq + x.h * a.group;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = lane + 32 * i;
-                ahead[i] = r < x.live ? a.lse[(int64_t)(x.q0 + x.t0 + r / a.group) * a.hq + x.h * a.group + r % a.group] : -INFINITY;
-            }
+            for (int i = 0; i < 4; ++i) ahead[i] = lane + 32 * i < x.live ? src[(int64_t)row_t[i] * a.hq + row_h[i]] : -INFINITY;
+        };
+        auto prior_of = [&](const Step &x) {
+            return a.prior && x.j0 + mine < x.len ? a.prior[((int64_t)x.s * c.heads + x.h) * a.width + x.j0 + mine] : 0.0f;
         };
         bool more = next(w);
-        if (more) look_up(w);
+        if (more) { look_up(w); prior_ahead = prior_of(w); }
         while (more && ok) {
             if (changes(w)) {
                 bool none = false;
@@ -276,7 +318,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_weights(const __grid_const
                     const int r = lane + 32 * i;
                     const bool empty = ahead[i] == -INFINITY;
                     ls[r] = empty ? 0.0f : ahead[i];
-                    see[r] = empty ? -1 : w.off + w.t0 + r / a.group;
+                    see[r] = empty ? -1 : w.off + w.t0 + row_t[i];
                     none |= empty && r < w.live;
                 }
                 odd = __any_sync(0xffffffffu, none);
@@ -285,44 +327,69 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_weights(const __grid_const
             }
             if (w.first) {
                 total = 0.0f;
-                prior = a.prior && w.j0 + mine < w.len ? a.prior[((int64_t)w.s * c.heads + w.h) * a.width + w.j0 + mine] : 0.0f;
+                prior = prior_ahead;
             }
+            // what the group's next step needs from memory arrives during this one
             const bool another = next(n);
             if (another && changes(n)) look_up(n);
-            const uint32_t acc = w.count % ACCS;
-            ok = wait_warp<true>(smem_u32(&ctl->acc_full[acc]), (w.count / ACCS) & 1, waits, SITE_EPI_TMEM_FULL);
+            if (another && n.first) prior_ahead = prior_of(n);
+            const uint32_t acc = count & 1;
+            ok = wait_warp<true>(smem_u32(&ctl->acc_full[g][acc]), count >> 1 & 1, waits, SITE_EPI_TMEM_FULL);
             if (!ok) break;
+            ++count;
             tc_fence_after();
             // every row of the tile sees every key, and gives something
-            const bool plain = w.j0 + TILE - 1 <= w.off + w.t0 && !odd;
+            const bool plain = w.j0 + (g + 1) * TILE - 1 <= w.off + w.t0 && !odd;
             const int key = w.j0 + mine;
+            const uint32_t src = tmem + lanes + (2 * g + acc) * TILE;
+            // the difference first: it is small where the weight counts, so its rounding is too
+            auto weight = [&](uint32_t x, float l) { return fast_exp2(fmaf(__uint_as_float(x), a.scale, -l) * LOG2E); };
+            auto add_plain = [&](const uint32_t (&x)[32], int c0) {
+                float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    float l[4];
+                    load4(ls + c0 + e, l);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) sum[y & 1] += weight(x[e + y], l[y]);
+                }
+                total += sum[0] + sum[1];
+            };
+            int c0 = 0;
+            if (plain) {                     // 64 columns a turn, the second half arrives while the first is worked on
+                uint32_t x[32], y[32];
+                if (w.live >= 32) tmem_ld32(src, x);
 #pragma unroll 1
-            for (int c0 = 0; c0 < w.live; c0 += 16) {
+                for (; c0 + 64 <= w.live; c0 += 64) {
+                    tmem_ld_wait(x);
+                    tmem_ld32(src + c0 + 32, y);
+                    add_plain(x, c0);
+                    tmem_ld_wait(y);
+                    if (c0 + 96 <= w.live) tmem_ld32(src + c0 + 64, x);
+                    add_plain(y, c0 + 32);
+                }
+                if (c0 + 32 <= w.live) {
+                    tmem_ld_wait(x);
+                    add_plain(x, c0);
+                    c0 += 32;
+                }
+            }
+#pragma unroll 1
+            for (; c0 < w.live; c0 += 16) {  // masks, and what is left
                 uint32_t x[16];
-                tmem_ld16(tmem + lanes + acc * TILE + c0, x);
+                tmem_ld16(src + c0, x);
                 tmem_ld_wait(x);
                 float sum = 0.0f;
-                // the difference first: it is small where the weight counts, so its rounding is too
-                if (plain && c0 + 16 <= w.live) {
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        float l[4];
-                        load4(ls + c0 + e, l);
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) sum += fast_exp2(fmaf(__uint_as_float(x[e + y]), a.scale, -l[y]) * LOG2E);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float v = fast_exp2(fmaf(__uint_as_float(x[e]), a.scale, -ls[c0 + e]) * LOG2E);
-                        sum += key <= see[c0 + e] ? v : 0.0f;
-                    }
+                for (int e = 0; e < 16; ++e) {
+                    const float v = weight(x[e], ls[c0 + e]);
+                    sum += key <= see[c0 + e] ? v : 0.0f;
                 }
                 total += sum;
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[acc]));
+            if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[g][acc]));
             if (w.last && key < w.len) a.out[((int64_t)w.s * c.heads + w.h) * a.width + key] = prior + total;
             w = n;
             more = another;
@@ -348,6 +415,9 @@ template <int DP> cudaError_t weights(const PagedWeightsArgs &a, cudaStream_t s)
     p.a = a;
     p.tokens = TILE / a.group;
     p.box = box_rows(a.c);
+    // queries that stay (one tile a head) need a place to change them ahead; a chunk's come with every step
+    p.q_slots = a.c.max_new > p.tokens ? Sh::SLOTS - 2 : 2;
+    p.k_slots = (Sh::SLOTS - p.q_slots) / 2;
     WeightsMaps tm = {};
     // a call without tokens has no products
     if (a.c.N > 0 && (!head_map(&tm.q, a.q, a.c.d, a.hq, a.c.N, a.ldq, a.group, p.tokens) || !pool_map(&tm.k, a.c.k, a.q, a.c, p.box)))

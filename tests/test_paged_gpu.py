@@ -216,6 +216,23 @@ def test_weights_of_more_rows_than_their_width_are_reported():
     assert bool((part == full[..., :20]).all())
 
 
+@pytest.mark.parametrize("new,lens,hq,hk,d,page", [
+    ((130, 1, 70), (2500, 3000, 1200), 8, 8, 64, 16),        # several units for every CTA, of one and of several steps
+    ((90,), (30000,), 4, 1, 128, 64),
+    ((40, 200), (9000, 9001), 16, 4, 64, 32),
+])
+def test_weights_with_several_units_and_steps_per_cta(new, lens, hq, hk, d, page):
+    # small heads so that the statement in 64 bits stays quick; the logarithms are any numbers near the right ones
+    import torch
+    x = Batch(12, new, lens, hq, hk, d, page)
+    lse = torch.randn(x.cu[-1], hq, generator=torch.Generator().manual_seed(1)).cuda() + 8.0
+    lse[3] = float("-inf")
+    w = x.cache.weights(x.q, lse, width=max(lens))
+    x.cache.poll()
+    r_w, e_w = oc.weights(to_host(x.q), x.keys, to_host(lse), x.cu, lens, hk, x.scale, max(lens))
+    within(w, r_w, e_w, "weights")
+
+
 def test_long_cache_rows_against_64_bits():
     x = Batch(9, (1, 70), (70001, 9000), 4, 1, 128, 64)
     out, lse = x.cache.attention(x.q)
