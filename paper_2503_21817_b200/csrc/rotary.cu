@@ -7,8 +7,7 @@
 //
 // Angles: a frequency is kept as turns per position in 64-bit fixed point (a fraction of a full turn), so position *
 // frequency modulo one turn is one integer multiplication that drops what overflows: the angle's error does not grow
-// with the position beyond that of the frequency's last bit (2^-65 of a turn each position).  The quadrant is taken from
-// the top bits and the rest goes to sincospi.  A CTA computes the table of its tokens once, for all their heads.
+// with the position beyond that of the frequency's last bit (2^-65 of a turn each position).  A CTA computes the table of its tokens once, for all their heads.
 //
 // Bound by memory: every row is read and written once.  A group of lanes holds a row, each lane V pairs of it (two
 // 16-byte vectors where the sizes allow), so the sums of a row are shuffles inside the group.
@@ -24,8 +23,9 @@ namespace skipffn {
 
 constexpr int RT_MAX_D = 256, RT_MAX_PAIRS = RT_MAX_D / 2, RT_MAX_AXES = 4;
 constexpr int RT_THREADS = 256, RT_MAX_TOKENS = 32;          // tokens of a CTA's table
-constexpr int RT_FWD_ROWS = 4, RT_BWD_ROWS = 2;              // rows that a group of lanes has in flight
-constexpr int RT_MAX_PARTS = 444;                            // CTAs of the backward: partial sums of the gains' gradients
+constexpr int RT_FWD_ROWS = 2, RT_BWD_ROWS = 2;              // rows that a group of lanes has in flight
+constexpr int RT_TURN = 8;                                   // rows of a group in a turn
+constexpr int RT_MAX_PARTS = 296;                            // CTAs of the backward: partial sums of the gains' gradients
 
 struct RotaryTurns {                                         // by value in the kernels' parameters
     unsigned long long turns[RT_MAX_PAIRS];
@@ -44,20 +44,30 @@ struct RotaryArgs {
     RotaryRows rows[3];
     const int32_t *pos;
     int64_t ldpos, n;
-    int32_t d, rot;
+    int32_t d, rot, axes;                    // axes: 0 without rotation
     float eps;
     float *part;                             // backward: [CTAs][d]
     PagedView c;
 };
 
+// cos and sin of a 2^-64 turns.  The quadrant is the top bits; the rest, within an eighth of a turn, goes to the functions'
+// power series (terms 1 / n!): what they leave out is below 2^-29 there, so the error is that of the arithmetic, 4 x 2^-24.
 __device__ __forceinline__ float2 turn_to_cos_sin(unsigned long long a)
 {
     const int t = (int)(a >> 32);                            // signed 2^-32 turns
     const unsigned quad = ((unsigned)t + (1u << 29)) >> 30;
-    const int rest = t - (int)(quad << 30);                  // within an eighth of a turn
-    float s, c;
-    sincospif((float)rest * 4.656612873077393e-10f, &s, &c); // 2^-31: half turns
-    if (quad & 1) { const float x = c; c = -s; s = x; }
+    const int rest = t - (int)(quad << 30);
+    const float x = (float)rest * 1.4629180792671596e-9f;    // 2 pi 2^-32
+    const float z = x * x;
+    float s = fmaf(z, 2.7557319e-6f, -1.9841270e-4f), c = fmaf(z, -2.7557319e-7f, 2.4801587e-5f);     // 1/9!, 1/7!; 1/10!, 1/8!
+    s = fmaf(z, s, 8.3333333e-3f);                           // 1/5!
+    s = fmaf(z, s, -1.6666667e-1f);                          // 1/3!
+    s = fmaf(x * z, s, x);
+    c = fmaf(z, c, -1.3888889e-3f);                          // 1/6!
+    c = fmaf(z, c, 4.1666667e-2f);                           // 1/4!
+    c = fmaf(z, c, -0.5f);
+    c = fmaf(z, c, 1.0f);
+    if (quad & 1) { const float y = c; c = -s; s = y; }
     return quad & 2 ? make_float2(-c, -s) : make_float2(c, s);
 }
 
@@ -66,19 +76,38 @@ template <> struct Vec<bf16, 8> { typedef uint4 type; };
 template <> struct Vec<bf16, 4> { typedef uint2 type; };
 template <> struct Vec<float, 4> { typedef uint4 type; };
 
-template <typename T, int V> __device__ __forceinline__ void unpack(const typename Vec<T, V>::type &w, float (&f)[V])
+// V elements as V / 2 pairs of fp32 (one instruction for two products or sums) and back, rounded once
+__device__ __forceinline__ uint64_t widen(uint32_t w) { return pair2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ uint32_t narrow(uint64_t v)
 {
-    const T *e = reinterpret_cast<const T *>(&w);
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = to_f32(e[i]);
+    float a, b;
+    unpair2(v, a, b);
+    const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&t);
 }
-template <typename T, int V> __device__ __forceinline__ typename Vec<T, V>::type pack(const float (&f)[V])
+__device__ __forceinline__ void unpack(const uint4 &w, uint64_t (&f)[4]) { f[0] = widen(w.x); f[1] = widen(w.y); f[2] = widen(w.z); f[3] = widen(w.w); }
+__device__ __forceinline__ void unpack(const uint2 &w, uint64_t (&f)[2]) { f[0] = widen(w.x); f[1] = widen(w.y); }
+__device__ __forceinline__ void unpack(const uint4 &w, uint64_t (&f)[2])
 {
-    typename Vec<T, V>::type w;
-    T *e = reinterpret_cast<T *>(&w);
-#pragma unroll
-    for (int i = 0; i < V; ++i) e[i] = from_f32<T>(f[i]);
-    return w;
+    f[0] = pair2(__uint_as_float(w.x), __uint_as_float(w.y));
+    f[1] = pair2(__uint_as_float(w.z), __uint_as_float(w.w));
+}
+__device__ __forceinline__ void pack(const uint64_t (&f)[4], uint4 &w) { w = make_uint4(narrow(f[0]), narrow(f[1]), narrow(f[2]), narrow(f[3])); }
+template <typename T> __device__ __forceinline__ void pack(const uint64_t (&f)[2], uint2 &w) { w = make_uint2(narrow(f[0]), narrow(f[1])); }
+template <typename T> __device__ __forceinline__ void pack(const uint64_t (&f)[2], uint4 &w)
+{
+    float a, b, c, d;
+    unpair2(f[0], a, b);
+    unpair2(f[1], c, d);
+    w = make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+}
+template <typename T> __device__ __forceinline__ void pack(const uint64_t (&f)[4], uint4 &w) { pack(f, w); }
+__device__ __forceinline__ uint64_t both(float v) { return pair2(v, v); }
+__device__ __forceinline__ float sum2(uint64_t v)
+{
+    float a, b;
+    unpair2(v, a, b);
+    return a + b;
 }
 
 // Where a lane's V pairs are: elements e0 .. e0 + V - 1 and e1 .. e1 + V - 1 of the row, table entry p0 (below zero: columns
@@ -101,17 +130,26 @@ template <int V, bool INTER> __device__ __forceinline__ LanePairs lane_pairs(int
     return l;
 }
 
-// rotates the lane's pairs; sign -1 turns back
-template <int V, bool INTER> __device__ __forceinline__ void rotate(float (&lo)[V], float (&hi)[V], const float2 *cs, float sign)
+// Rotates the lane's pairs, whose cosines (then sines) stand at `cs` (`cs` + pairs); sign -1 turns back.
+template <int V, bool INTER> __device__ __forceinline__ void rotate(uint64_t (&lo)[V / 2], uint64_t (&hi)[V / 2], const float *cs, int pairs, float sign)
 {
+    if (INTER) {                             // a pair stands in one register pair: (a, b) c + (-b, a) s
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float2 t = cs[i];
-        float &a = INTER ? (2 * i < V ? lo[2 * i] : hi[2 * i - V]) : lo[i];
-        float &b = INTER ? (2 * i < V ? lo[2 * i + 1] : hi[2 * i + 1 - V]) : hi[i];
-        const float s = sign * t.y, x = a;
-        a = x * t.x - b * s;
-        b = b * t.x + x * s;
+        for (int i = 0; i < V; ++i) {
+            uint64_t &x = i < V / 2 ? lo[i] : hi[i - V / 2];
+            const float c = cs[i], s = sign * cs[pairs + i];
+            float a, b;
+            unpair2(x, a, b);
+            x = fma2(pair2(-b, a), both(s), mul2(x, both(c)));
+        }
+    } else {                                 // two pairs in two register pairs
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            const float2 cf = *reinterpret_cast<const float2 *>(cs + 2 * i), sf = *reinterpret_cast<const float2 *>(cs + pairs + 2 * i);
+            const uint64_t c = pair2(cf.x, cf.y), s = pair2(sign * sf.x, sign * sf.y), n = pair2(-sign * sf.x, -sign * sf.y), x = lo[i];
+            lo[i] = fma2(hi[i], n, mul2(x, c));
+            hi[i] = fma2(x, s, mul2(hi[i], c));
+        }
     }
 }
 
@@ -122,17 +160,27 @@ template <int L> __device__ __forceinline__ float group_sum(float v)
     return v;
 }
 
-// cos / sin of tokens t0 .. t0 + count - 1
-__device__ __forceinline__ void fill_table(float2 *table, const RotaryArgs &a, const RotaryTurns &f, int64_t t0, int count)
+// Cosines, then sines of the tokens whose positions stand at `pos` ([axis][RT_MAX_TOKENS]): a token's 2 x pairs floats.  A
+// thread has one pair, whose frequency it reads once (parameters read at 32 different places take 32 turns).
+__device__ __forceinline__ void fill_table(float *table, const RotaryArgs &a, const RotaryTurns &f, const int *pos, int count)
 {
     const int pairs = a.rot / 2;
     if (pairs == 0) return;
-    int t = threadIdx.x / pairs, p = threadIdx.x - t * pairs;
-    for (int i = threadIdx.x; i < count * pairs; i += RT_THREADS, p += RT_THREADS) {
-        while (p >= pairs) { p -= pairs; ++t; }
-        const long long pos = a.pos[f.axis[p] * a.ldpos + t0 + t];
-        table[i] = turn_to_cos_sin((unsigned long long)pos * f.turns[p]);
+    const int step = RT_THREADS / pairs, first = threadIdx.x / pairs, p = threadIdx.x - first * pairs;
+    if (first >= step) return;
+    const unsigned long long turns = f.turns[p];
+    pos += f.axis[p] * RT_MAX_TOKENS;
+    for (int t = first; t < count; t += step) {
+        const float2 cs = turn_to_cos_sin((unsigned long long)(long long)pos[t] * turns);
+        table[t * a.rot + p] = cs.x;
+        table[t * a.rot + pairs + p] = cs.y;
     }
+}
+
+__device__ __forceinline__ void load_positions(int *pos, const RotaryArgs &a, int64_t t0, int count)
+{
+    const int i = threadIdx.x % RT_MAX_TOKENS, axis = threadIdx.x / RT_MAX_TOKENS;
+    if (i < count && axis < a.axes) pos[threadIdx.x] = a.pos[axis * a.ldpos + t0 + i];
 }
 
 // Where the last row of a token's sequence puts it: byte offset of its cache row, -1 for none (token behind the last sequence: -2).
@@ -188,12 +236,13 @@ template <typename T, int V> __device__ __forceinline__ Row<T, V> load_row(const
 
 // Forward.  Every group of lanes has several rows in flight: their loads are issued before any of them is worked on.
 template <typename T, int V, int L, bool INTER, bool APPEND>
-__global__ void __launch_bounds__(RT_THREADS)
+__global__ void __launch_bounds__(RT_THREADS, 4)
 k_rotary_fwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ RotaryTurns f)
 {
     typedef typename Vec<T, V>::type W;
-    extern __shared__ float2 table[];
+    extern __shared__ __align__(16) float table[];
     __shared__ int64_t slot[RT_MAX_TOKENS];
+    __shared__ int pos[RT_MAX_AXES * RT_MAX_TOKENS];
     constexpr int GROUPS = RT_THREADS / L, U = RT_FWD_ROWS;
     int kind = 0, cta = blockIdx.x;
     while (cta >= a.rows[kind].ctas) cta -= a.rows[kind++].ctas;
@@ -204,25 +253,24 @@ k_rotary_fwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ Rotar
     const float inv_d = 1.0f / a.d;
     RowWalk walk(threadIdx.x / L, GROUPS, k.heads);
     pdl_enter();
-    float g0[V], g1[V];
+    uint64_t g0[V / 2] = {}, g1[V / 2] = {};
     if (k.gamma && l.on) {
         const Row<T, V> g = load_row<T, V>((const T *)k.gamma, l);
-        unpack<T, V>(g.w0, g0);
-        unpack<T, V>(g.w1, g1);
+        unpack(g.w0, g0);
+        unpack(g.w1, g1);
     }
-    if (kind < 2) fill_table(table, a, f, t0, count);
+    load_positions(pos, a, t0, kind < 2 ? count : 0);
     if (APPEND)
         for (int t = threadIdx.x >> 5; t < count; t += RT_THREADS / 32) {
             const int64_t r = append_row(a.c, t0 + t, threadIdx.x & 31, kind == 1);
             if ((threadIdx.x & 31) == 0) slot[t] = r;
         }
-    bool synced = false;
+    __syncthreads();
     // every lane of a warp takes part in the shuffles, so all walk the same number of rows
     for (int r0 = 0; r0 < rows; r0 += U * GROUPS) {
         Row<T, V> x[U];
         int at[U];                           // token of the CTA, -1: no row
         int64_t to[U];                       // element offset of the result's row (append, keys and values: byte offset)
-        if (APPEND && !synced) { __syncthreads(); synced = true; }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             at[u] = -1;
@@ -241,24 +289,27 @@ k_rotary_fwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ Rotar
             }
             walk.next();
         }
-        if (!synced) { __syncthreads(); synced = true; }       // the table is made while the first rows arrive
+        if (r0 == 0 && kind < 2) {           // the table is made while the first rows arrive
+            fill_table(table, a, f, pos, count);
+            __syncthreads();
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (kind < 2) {
-                float lo[V], hi[V];
-                unpack<T, V>(x[u].w0, lo);
-                unpack<T, V>(x[u].w1, hi);
+                uint64_t lo[V / 2], hi[V / 2];
+                unpack(x[u].w0, lo);
+                unpack(x[u].w1, hi);
                 if (k.gamma) {
-                    float ss = 0.0f;
+                    uint64_t ss = 0;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) ss = fmaf(lo[i], lo[i], fmaf(hi[i], hi[i], ss));
-                    const float r = rsqrtf(group_sum<L>(ss) * inv_d + a.eps);
+                    for (int i = 0; i < V / 2; ++i) ss = fma2(lo[i], lo[i], fma2(hi[i], hi[i], ss));
+                    const uint64_t r = both(rsqrtf(group_sum<L>(sum2(ss)) * inv_d + a.eps));
 #pragma unroll
-                    for (int i = 0; i < V; ++i) { lo[i] *= r * g0[i]; hi[i] *= r * g1[i]; }
+                    for (int i = 0; i < V / 2; ++i) { lo[i] = mul2(mul2(lo[i], g0[i]), r); hi[i] = mul2(mul2(hi[i], g1[i]), r); }
                 }
-                if (at[u] >= 0 && l.p0 >= 0) rotate<V, INTER>(lo, hi, table + at[u] * (a.rot / 2) + l.p0, 1.0f);
-                x[u].w0 = pack<T, V>(lo);
-                x[u].w1 = pack<T, V>(hi);
+                if (at[u] >= 0 && l.p0 >= 0) rotate<V, INTER>(lo, hi, table + at[u] * a.rot + l.p0, a.rot / 2, 1.0f);
+                pack<T>(lo, x[u].w0);
+                pack<T>(hi, x[u].w1);
             }
             if (to[u] >= 0) {
                 T *dst = APPEND && kind > 0 ? (T *)((kind == 1 ? a.c.k : a.c.v) + to[u]) : (T *)k.out + to[u];
@@ -272,29 +323,29 @@ k_rotary_fwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ Rotar
 // Backward.  CTAs of a kind walk blocks of its tokens; the gain's gradient is summed in registers (a lane's columns stay
 // the same), over the CTA's groups in shared memory, then over the CTAs by k_rotary_sum: a fixed order throughout.
 template <typename T, int V, int L, bool INTER>
-__global__ void __launch_bounds__(RT_THREADS)
+__global__ void __launch_bounds__(RT_THREADS, 2)
 k_rotary_bwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ RotaryTurns f)
 {
     typedef typename Vec<T, V>::type W;
-    extern __shared__ float2 table[];
+    extern __shared__ __align__(16) float table[];
+    __shared__ int pos[RT_MAX_AXES * RT_MAX_TOKENS];
     constexpr int GROUPS = RT_THREADS / L, U = RT_BWD_ROWS;
     const int kind = blockIdx.x >= a.rows[0].ctas, cta = blockIdx.x - (kind ? a.rows[0].ctas : 0);
     const RotaryRows &k = a.rows[kind];
     const LanePairs l = lane_pairs<V, INTER>(threadIdx.x % L, a.d, a.rot);
     const float inv_d = 1.0f / a.d;
     pdl_enter();
-    float acc[2][V] = {}, g0[V] = {}, g1[V] = {};
+    uint64_t acc[2][V / 2] = {}, g0[V / 2] = {}, g1[V / 2] = {};
     if (k.gamma && l.on) {
         const Row<T, V> g = load_row<T, V>((const T *)k.gamma, l);
-        unpack<T, V>(g.w0, g0);
-        unpack<T, V>(g.w1, g1);
+        unpack(g.w0, g0);
+        unpack(g.w1, g1);
     }
     for (int64_t t0 = (int64_t)cta * k.tokens; t0 < a.n; t0 += (int64_t)k.ctas * k.tokens) {
         const int count = (int)min((int64_t)k.tokens, a.n - t0), rows = count * k.heads;
         RowWalk walk(threadIdx.x / L, GROUPS, k.heads);
-        __syncthreads();                     // the table has been read
-        fill_table(table, a, f, t0, count);
-        bool synced = false;
+        load_positions(pos, a, t0, count);
+        __syncthreads();                     // they are there, and the table has been read
         for (int r0 = 0; r0 < rows; r0 += U * GROUPS) {
             Row<T, V> y[U], x[U];
             int at[U], head[U];
@@ -311,49 +362,54 @@ k_rotary_bwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ Rotar
                 }
                 walk.next();
             }
-            if (!synced) { __syncthreads(); synced = true; }
+            if (r0 == 0) {
+                fill_table(table, a, f, pos, count);
+                __syncthreads();
+            }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                float lo[V], hi[V];
-                unpack<T, V>(y[u].w0, lo);
-                unpack<T, V>(y[u].w1, hi);
-                if (at[u] >= 0 && l.p0 >= 0) rotate<V, INTER>(lo, hi, table + at[u] * (a.rot / 2) + l.p0, -1.0f);
+                uint64_t lo[V / 2], hi[V / 2];
+                unpack(y[u].w0, lo);
+                unpack(y[u].w1, hi);
+                if (at[u] >= 0 && l.p0 >= 0) rotate<V, INTER>(lo, hi, table + at[u] * a.rot + l.p0, a.rot / 2, -1.0f);
                 if (k.gamma) {
-                    float xl[V], xh[V];
-                    unpack<T, V>(x[u].w0, xl);
-                    unpack<T, V>(x[u].w1, xh);
-                    float ss = 0.0f, ux = 0.0f;
+                    uint64_t xl[V / 2], xh[V / 2], ss = 0, ux = 0;
+                    unpack(x[u].w0, xl);
+                    unpack(x[u].w1, xh);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        ss = fmaf(xl[i], xl[i], fmaf(xh[i], xh[i], ss));
-                        ux = fmaf(lo[i] * g0[i], xl[i], fmaf(hi[i] * g1[i], xh[i], ux));
+                    for (int i = 0; i < V / 2; ++i) {
+                        ss = fma2(xl[i], xl[i], fma2(xh[i], xh[i], ss));
+                        ux = fma2(mul2(lo[i], g0[i]), xl[i], fma2(mul2(hi[i], g1[i]), xh[i], ux));
                     }
-                    const float r = rsqrtf(group_sum<L>(ss) * inv_d + a.eps);
-                    const float m = group_sum<L>(ux) * inv_d * r * r;
+                    const float r = rsqrtf(group_sum<L>(sum2(ss)) * inv_d + a.eps);
+                    const uint64_t r2 = both(r), m = both(-group_sum<L>(sum2(ux)) * inv_d * r * r);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        acc[0][i] = fmaf(lo[i], xl[i] * r, acc[0][i]);
-                        acc[1][i] = fmaf(hi[i], xh[i] * r, acc[1][i]);
-                        lo[i] = r * (lo[i] * g0[i] - xl[i] * m);
-                        hi[i] = r * (hi[i] * g1[i] - xh[i] * m);
+                    for (int i = 0; i < V / 2; ++i) {
+                        acc[0][i] = fma2(lo[i], mul2(xl[i], r2), acc[0][i]);
+                        acc[1][i] = fma2(hi[i], mul2(xh[i], r2), acc[1][i]);
+                        lo[i] = mul2(r2, fma2(xl[i], m, mul2(lo[i], g0[i])));
+                        hi[i] = mul2(r2, fma2(xh[i], m, mul2(hi[i], g1[i])));
                     }
                 }
                 if (at[u] >= 0) {
                     T *dx = (T *)k.out + (t0 + at[u]) * k.ldo + (int64_t)head[u] * a.d;
-                    *reinterpret_cast<W *>(dx + l.e0) = pack<T, V>(lo);
-                    *reinterpret_cast<W *>(dx + l.e1) = pack<T, V>(hi);
+                    W w0, w1;
+                    pack<T>(lo, w0);
+                    pack<T>(hi, w1);
+                    *reinterpret_cast<W *>(dx + l.e0) = w0;
+                    *reinterpret_cast<W *>(dx + l.e1) = w1;
                 }
             }
         }
     }
     if (!k.gamma) return;
-    float *sums = reinterpret_cast<float *>(table);           // [groups][d]
+    float *sums = table;                     // [groups][d]
     __syncthreads();
     if (l.on)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            sums[(threadIdx.x / L) * a.d + l.e0 + i] = acc[0][i];
-            sums[(threadIdx.x / L) * a.d + l.e1 + i] = acc[1][i];
+        for (int i = 0; i < V / 2; ++i) {
+            *reinterpret_cast<uint64_t *>(sums + (threadIdx.x / L) * a.d + l.e0 + 2 * i) = acc[0][i];
+            *reinterpret_cast<uint64_t *>(sums + (threadIdx.x / L) * a.d + l.e1 + 2 * i) = acc[1][i];
         }
     __syncthreads();
     for (int c = threadIdx.x; c < a.d; c += RT_THREADS) {
@@ -415,7 +471,7 @@ template <typename T, int V, int L, bool INTER> static cudaError_t rotary_l(Rota
         if (k.ctas > 0 && k.tokens > tokens) tokens = k.tokens;
         ctas += k.ctas;
     }
-    const size_t table = (size_t)tokens * (a.rot / 2) * sizeof(float2);
+    const size_t table = (size_t)tokens * a.rot * sizeof(float);
     const dim3 grid((unsigned)ctas), block(RT_THREADS);
     if (mode == RT_FORWARD) return launch_smem(k_rotary_fwd<T, V, L, INTER, false>, grid, block, table, s, a, f);
     if (mode == RT_APPEND) return launch_smem(k_rotary_fwd<T, V, L, INTER, true>, grid, block, table, s, a, f);
@@ -442,20 +498,18 @@ static cudaError_t rotary_launch(RotaryMode mode, int dtype, bool inter, const R
     return inter ? rotary_v<bf16, 4, true>(mode, a, f, s) : rotary_v<bf16, 4, false>(mode, a, f, s);
 }
 
-// Tokens of a CTA's turn: two batches of rows per group of lanes, fewer while SMs would be left without work, never more than
-// the table holds.
-static int turn_tokens(int64_t n, int heads, int batch, int groups)
-{
-    int64_t t = 2 * batch * groups / heads;
-    while (t > 1 && (n + t - 1) / t * heads < (int64_t)148 * 4 * groups) t /= 2;
-    return (int)(t < 1 ? 1 : t > RT_MAX_TOKENS ? RT_MAX_TOKENS : t);
-}
-static void plan_rows(RotaryArgs *a, int dtype, int batch)
+// Tokens of a CTA's turn: as many as give every group of lanes RT_TURN rows, fewer while SMs would be left without work,
+// never more than the table holds.
+static void plan_rows(RotaryArgs *a, int dtype)
 {
     const int groups = RT_THREADS / lanes_of(a->d, pairs_per_lane(dtype, a->d, a->rot));
+    int64_t heads = 0, rows = (int64_t)RT_TURN * groups;
+    for (const RotaryRows &k : a->rows) heads += k.heads;
+    while (rows > groups && a->n * heads / rows < 4 * 148) rows /= 2;
     for (RotaryRows &k : a->rows) {
         if (k.heads == 0) continue;
-        k.tokens = turn_tokens(a->n, k.heads, batch, groups);
+        const int64_t t = rows / k.heads;
+        k.tokens = (int32_t)(t < 1 ? 1 : t > RT_MAX_TOKENS ? RT_MAX_TOKENS : t);
         k.ctas = (int32_t)((a->n + k.tokens - 1) / k.tokens);
     }
 }
@@ -512,7 +566,7 @@ RotaryArgs args_of(const skipffn_rotary *h, int64_t n, const void *q, int64_t ld
     a.rows[0].x = q; a.rows[0].ld = ldq; a.rows[0].gamma = gq; a.rows[0].out = oq; a.rows[0].ldo = ldoq; a.rows[0].heads = h->hq;
     a.rows[1].x = k; a.rows[1].ld = ldk; a.rows[1].gamma = gk; a.rows[1].out = ok; a.rows[1].ldo = ldok; a.rows[1].heads = h->hk;
     a.pos = pos; a.ldpos = ldpos; a.n = n;
-    a.d = h->d; a.rot = h->rot; a.eps = h->eps;
+    a.d = h->d; a.rot = h->rot; a.axes = h->rot ? h->axes : 0; a.eps = h->eps;
     return a;
 }
 
@@ -565,7 +619,7 @@ skipffn_status skipffn_rotary_forward(const skipffn_rotary *h, int32_t dtype, in
         !out_ok(ok, &c.k, {c.q, c.k}, positions, pb, gamma_q, gamma_k, gb, n) || tokens_overlap(oq, ok, n))
         return SKIPFFN_EINVAL;
     RotaryArgs a = args_of(h, n, q, ldq, k, ldk, positions, ldpos, gamma_q, gamma_k, q_out, ldqo, k_out, ldko);
-    plan_rows(&a, dtype, RT_FWD_ROWS);
+    plan_rows(&a, dtype);
     return rotary_launch(RT_FORWARD, dtype, h->inter, a, h->f, (cudaStream_t)stream) == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }
 
@@ -618,8 +672,8 @@ skipffn_status skipffn_rotary_backward(const skipffn_rotary *h, int32_t dtype, i
         a.rows[0].dy = dq_out; a.rows[0].lddy = lddqo;
         a.rows[1].dy = dk_out; a.rows[1].lddy = lddko;
         a.part = (float *)scratch;
-        plan_rows(&a, dtype, RT_BWD_ROWS);
-        // three CTAs an SM, shared out by the rows of a kind
+        plan_rows(&a, dtype);
+        // two CTAs an SM, shared out by the rows of a kind
         const int share = (int)((int64_t)RT_MAX_PARTS * h->hq / (h->hq + h->hk)), of_q = share < 1 ? 1 : share == RT_MAX_PARTS ? share - 1 : share;
         if (a.rows[0].ctas > of_q) a.rows[0].ctas = of_q;
         if (a.rows[1].ctas > RT_MAX_PARTS - of_q) a.rows[1].ctas = RT_MAX_PARTS - of_q;
@@ -657,7 +711,7 @@ skipffn_status skipffn_rotary_append(const skipffn_rotary *h, const skipffn_page
     RotaryArgs a = args_of(h, n, q, ldq, k, ldk, positions, ldpos, gamma_q, gamma_k, q_out, ldqo, nullptr, 0);
     a.rows[2].x = v; a.rows[2].ld = ldv; a.rows[2].heads = h->hk;
     a.c = view;
-    plan_rows(&a, cache->dtype, RT_FWD_ROWS);
+    plan_rows(&a, cache->dtype);
     return rotary_launch(RT_APPEND, cache->dtype, h->inter, a, h->f, (cudaStream_t)stream) == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }
 
@@ -676,7 +730,7 @@ skipffn_status skipffn_paged_append(const skipffn_paged_cache *cache, int64_t n,
     a.rows[1].x = k; a.rows[1].ld = ldk; a.rows[1].heads = view.heads;
     a.rows[2].x = v; a.rows[2].ld = ldv; a.rows[2].heads = view.heads;
     a.n = n; a.d = view.d; a.c = view;
-    plan_rows(&a, cache->dtype, RT_FWD_ROWS);
+    plan_rows(&a, cache->dtype);
     return rotary_launch(RT_APPEND, cache->dtype, false, a, RotaryTurns{}, (cudaStream_t)stream) == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }
 
