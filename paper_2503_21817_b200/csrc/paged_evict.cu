@@ -2,10 +2,11 @@
 // `recent` in any case), in their order, and move to the front of the same pages or to other ones.
 //
 // k_evict_select: one cluster of CTAs per (sequence, head).  The weight that separates kept from evicted rows is found by
-// four counts of eight bits each over the weights' order-preserving integer form; the CTAs' counts are added up through
-// distributed shared memory, one cluster barrier a count (two sets of bins take turns).  A CTA's part of the weights is read
-// once and stays in registers (up to HELD x 512 weights; what is beyond comes from L2 again).  Then every CTA numbers the
-// kept rows of its part.  Bound by the chain of barriers and shared-memory atomics: 16 381 rows of 8 heads in clusters of 16.
+// three counts of 11, 11 and 10 bits over the weights' order-preserving integer form (with 8 bits first, sign and exponent
+// alone, softmax weights crowd into a few bins and their atomic additions queue up).  A CTA counts its part, then adds its
+// bins that are not empty to every CTA's sums in distributed shared memory: one cluster barrier a count.  A CTA's part of the
+// weights is read once and stays in registers (up to HELD x 512; what is beyond comes from L2 again).  Then every CTA numbers
+// the kept rows of its part.  Bound by this chain of counts and barriers.
 // k_evict_move: a warp takes up to 32 rows; its lanes look up their places in parallel, then 16-byte pieces of keys and
 // values move, 8 in flight a lane.  Bound by memory.  In place, a pair's rows move in steps of its whole cluster: a row's
 // destination is never behind it (order is kept), so it is enough that a step has read all its rows before it writes any --
@@ -18,7 +19,8 @@ namespace skipffn {
 namespace {
 
 constexpr int THREADS = 512, WARPS = THREADS / 32, HELD = 8;         // select: weights that a thread holds
-constexpr int SPAN = THREADS * HELD;
+constexpr int SPAN = THREADS * HELD, PER = HELD * WARPS / 32;
+constexpr int BINS = 2048, OWN = BINS / THREADS;                     // bins of a count, of a thread
 constexpr int MOVE_THREADS = 256, PIECES = 8;                        // move: 16-byte pieces a lane holds
 
 // weights in ascending order as unsigned integers; NaN below everything, -0 = +0
@@ -29,35 +31,45 @@ __device__ __forceinline__ uint32_t order_of(float w)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-__device__ __forceinline__ uint32_t read_peer(const void *p, uint32_t rank)
+// adds to the same word of CTA `rank` of the cluster
+__device__ __forceinline__ void add_peer(uint32_t *p, uint32_t rank, uint32_t v)
 {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(mapa_rank(smem_u32(p), rank)) : "memory");
+    asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(mapa_rank(smem_u32(p), rank)), "r"(v) : "memory");
+}
+// inclusive sums over the lanes
+__device__ __forceinline__ uint32_t lane_scan(uint32_t v, int lane)
+{
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += x;
+    }
     return v;
 }
 
-__global__ void __launch_bounds__(THREADS) k_evict_select(const PagedEvictArgs a, const int size)
+__global__ void __launch_bounds__(THREADS, 2) k_evict_select(const PagedEvictArgs a, const int size)
 {
-    __shared__ uint32_t bins[2][256], all[256];
-    __shared__ uint32_t counts[2], picked[2], turn_counts[2];
+    static_assert(OWN == 4, "a thread's bins are one vector");
+    __shared__ __align__(16) uint32_t bins[BINS], sums[3][BINS];    // of this CTA; of the cluster, one set a count
+    __shared__ uint32_t before[2], picked[2], turn_counts[2], bin_sums[WARPS];
     __shared__ uint32_t warp_sums[HELD][WARPS][2];
     const PagedView &c = a.c;
     const uint32_t rank = cluster_ctarank();
     const int pair = blockIdx.x / size, s = pair / c.heads, h = pair - s * c.heads;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid < 256) bins[0][tid] = bins[1][tid] = 0;
+    auto own = [&](uint32_t *p) -> uint4 & { return *reinterpret_cast<uint4 *>(p + OWN * tid); };
+    own(bins) = own(sums[0]) = own(sums[1]) = own(sums[2]) = make_uint4(0, 0, 0, 0);
+    if (tid < 2) before[tid] = 0;
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // waited for before the first addition to a peer
     pdl_enter();
-    const int asked = c.lens[s];
-    int len = min(max(asked, 0), c.capacity);
-    const int m_all = min(len, a.width);
+    const int asked = c.lens[s], all = min(min(max(asked, 0), c.capacity), a.width);
     if (tid == 0 && rank == 0 && h == 0) {
-        if (len != asked) paged_report(c, SITE_PAGED_LENGTH);
-        else if (len > a.width) paged_report(c, SITE_PAGED_WIDTH);
-        a.lens_out[s] = min(m_all, a.budget);
-        if (min(m_all, a.budget) > a.dst.capacity) paged_report(a.dst, SITE_PAGED_ROOM);
+        if (asked < 0 || asked > c.capacity) paged_report(c, SITE_PAGED_LENGTH);
+        else if (asked > a.width) paged_report(c, SITE_PAGED_WIDTH);
+        a.lens_out[s] = min(all, a.budget);
+        if (min(all, a.budget) > a.dst.capacity) paged_report(a.dst, SITE_PAGED_ROOM);
     }
-    len = m_all;
-    const int m = min(len, a.budget);
+    const int len = all, m = min(len, a.budget);
     const float *w = a.weights + ((int64_t)s * c.heads + h) * a.width;
     int32_t *kept = a.kept + ((int64_t)s * c.heads + h) * a.budget;
     float *wout = a.weights_out + ((int64_t)s * c.heads + h) * a.budget;
@@ -65,53 +77,61 @@ __global__ void __launch_bounds__(THREADS) k_evict_select(const PagedEvictArgs a
     const int part = (len + size - 1) / size, lo = min(len, (int)rank * part), hi = min(len, lo + part);
     const bool cut = len > a.budget;
     const int first = a.sinks, past = len - a.recent;               // rows first .. past - 1 compete when there is a cut
-    uint32_t key[HELD];
+    float held[HELD];
 #pragma unroll
     for (int i = 0; i < HELD; ++i) {
         const int j = lo + i * THREADS + tid;
-        key[i] = cut && j < hi ? order_of(w[j]) : 0u;
+        held[i] = j < hi ? w[j] : 0.0f;
     }
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     uint32_t limit = 0, equal = 0;                                  // kept: order above `limit`, and the first `equal` at it
     if (cut) {
         uint32_t want = (uint32_t)(a.budget - a.sinks - a.recent);  // of past - first > want competitors
-        for (int shift = 24, turn = 0; shift >= 0; shift -= 8, turn ^= 1) {
-            __syncthreads();                                        // the bins of this turn are zero
-            const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-            auto count = [&](int j, uint32_t k) {
-                if (j >= first && j < past && (k & mask) == limit) atomicAdd(&bins[turn][(k >> shift) & 255], 1u);
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+            const uint32_t mask = pass == 0 ? 0u : 0xffffffffu << (pass == 1 ? 21 : 10), digits = pass == 2 ? 1023 : 2047;
+            uint32_t *mine = size == 1 ? sums[pass] : bins;
+            auto count = [&](int j, float x) {
+                const uint32_t k = order_of(x);
+                if (j >= first && j < past && (k & mask) == limit) atomicAdd(&mine[(k >> shift) & digits], 1u);
             };
 #pragma unroll
             for (int i = 0; i < HELD; ++i) {
                 const int j = lo + i * THREADS + tid;
-                if (j < hi) count(j, key[i]);
+                if (j < hi) count(j, held[i]);
             }
-            for (int j = lo + SPAN + tid; j < hi; j += THREADS) count(j, order_of(w[j]));
-            cluster_sync_all();
-            if (tid < 256) {
-                uint32_t n = 0;
-                for (int r = 0; r < size; ++r) n += read_peer(&bins[turn][tid], r);
-                all[tid] = n;
-                // the other set was read before this barrier and is next to be counted into
-                bins[turn ^ 1][tid] = 0;
-            }
+#pragma unroll 4
+            for (int j = lo + SPAN + tid; j < hi; j += THREADS) count(j, w[j]);
             __syncthreads();
-            if (tid < 32) {                                         // the bin that holds the want-th from above
-                uint32_t mine = 0;
-                for (int i = 0; i < 8; ++i) mine += all[255 - 8 * tid - i];
-                uint32_t above = mine;
+            if (size > 1) {
+                uint4 &v = own(bins);
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const uint32_t x = __shfl_up_sync(0xffffffffu, above, o);
-                    if (tid >= o) above += x;
+                for (int i = 0; i < OWN; ++i) {
+                    const uint32_t x = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+                    if (x)
+                        for (int r = 0; r < size; ++r) add_peer(&sums[pass][OWN * tid + i], r, x);
                 }
-                above -= mine;
-                // want = 0: nothing but the protected rows; the topmost bin, of which none is taken
-                if (want == 0 ? tid == 0 : above < want && want <= above + mine) {
-                    int b = 255 - 8 * tid;
-                    while (want > 0 && above + all[b] < want) above += all[b--];
-                    picked[0] = (uint32_t)b;
-                    picked[1] = want - above;
-                }
+                v = make_uint4(0, 0, 0, 0);
+                cluster_sync_all();
+            }
+            // from above: thread 0 has the four highest bins
+            const int top = BINS - OWN * (tid + 1);
+            const uint4 n = *reinterpret_cast<const uint4 *>(&sums[pass][top]);
+            const uint32_t here = n.x + n.y + n.z + n.w;
+            uint32_t above = lane_scan(here, lane);
+            if (lane == 31) bin_sums[warp] = above;
+            __syncthreads();
+            above -= here;
+            for (int i = 0; i < warp; ++i) above += bin_sums[i];
+            // the bin that holds the want-th from above; want = 0 (nothing but the protected rows): the topmost, none of it
+            if (want == 0 ? tid == 0 : above < want && want <= above + here) {
+                const uint32_t v[OWN] = {n.w, n.z, n.y, n.x};
+                int b = 0;
+#pragma unroll
+                for (int i = 0; i < OWN - 1; ++i)
+                    if (want > 0 && b == i && above + v[i] < want) { above += v[i]; ++b; }
+                picked[0] = (uint32_t)(top + OWN - 1 - b) & digits;
+                picked[1] = want - above;
             }
             __syncthreads();
             limit |= picked[0] << shift;
@@ -120,63 +140,67 @@ __global__ void __launch_bounds__(THREADS) k_evict_select(const PagedEvictArgs a
         equal = want;
     }
     // every row's state: kept for certain (bit 0), at the limit (bit 1)
-    auto state = [&](int j, uint32_t k) -> uint32_t {
+    auto state = [&](int j, float x) -> uint32_t {
         if (j >= hi) return 0u;
         if (!cut || j < first || j >= past) return 1u;
+        const uint32_t k = order_of(x);
         return k > limit ? 1u : k == limit ? 2u : 0u;
     };
-    uint32_t n0 = 0, n1 = 0;
-#pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-        const uint32_t x = state(lo + i * THREADS + tid, key[i]);
-        n0 += x & 1; n1 += x >> 1;
-    }
-    for (int j = lo + SPAN + tid; j < hi; j += THREADS) {
-        const uint32_t x = state(j, order_of(w[j]));
-        n0 += x & 1; n1 += x >> 1;
-    }
-    n0 = __reduce_add_sync(0xffffffffu, n0);
-    n1 = __reduce_add_sync(0xffffffffu, n1);
-    if (tid == 0) counts[0] = counts[1] = 0;
-    __syncthreads();
-    if (lane == 0) { atomicAdd(&counts[0], n0); atomicAdd(&counts[1], n1); }
-    cluster_sync_all();
+    // rows kept before this CTA's part
     uint32_t base0 = 0, base1 = 0;
-    for (uint32_t r = 0; r < rank; ++r) { base0 += read_peer(&counts[0], r); base1 += read_peer(&counts[1], r); }
-    for (int j0 = lo; j0 < hi; j0 += SPAN) {                        // one turn when the part fits the registers
-        uint32_t below0[HELD], below1[HELD];                        // within the warp
-        __syncthreads();
+    if (size > 1) {
+        uint32_t n0 = 0, n1 = 0;
 #pragma unroll
         for (int i = 0; i < HELD; ++i) {
-            const int j = j0 + i * THREADS + tid;
-            if (j0 > lo) key[i] = j < hi ? order_of(w[j]) : 0u;
-            const uint32_t x = state(j, key[i]);
+            const uint32_t x = state(lo + i * THREADS + tid, held[i]);
+            n0 += x & 1; n1 += x >> 1;
+        }
+#pragma unroll 4
+        for (int j = lo + SPAN + tid; j < hi; j += THREADS) {
+            const uint32_t x = state(j, w[j]);
+            n0 += x & 1; n1 += x >> 1;
+        }
+        n0 = __reduce_add_sync(0xffffffffu, n0);
+        n1 = __reduce_add_sync(0xffffffffu, n1);
+        if (lane == 0)
+            for (int r = rank + 1; r < size; ++r) { add_peer(&before[0], r, n0); add_peer(&before[1], r, n1); }
+        cluster_sync_all();
+        base0 = before[0];
+        base1 = before[1];
+    }
+    for (int j0 = lo; j0 < hi; j0 += SPAN) {                        // one turn when the part fits the registers
+        uint32_t below0[HELD], below1[HELD];                        // within the warp
+        if (j0 > lo) {
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                const int j = j0 + i * THREADS + tid;
+                held[i] = j < hi ? w[j] : 0.0f;
+            }
+            __syncthreads();                                        // the sums of the turn before have been read
+        }
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            const uint32_t x = state(j0 + i * THREADS + tid, held[i]);
             const uint32_t v0 = __ballot_sync(0xffffffffu, x & 1), v1 = __ballot_sync(0xffffffffu, x & 2), mask = (2u << lane) - 1;
             below0[i] = __popc(v0 & mask);
             below1[i] = __popc(v1 & mask);
             if (lane == 31) { warp_sums[i][warp][0] = below0[i]; warp_sums[i][warp][1] = below1[i]; }
         }
         __syncthreads();
-        if (tid < 32) {                                             // sums before each (slice of 512 rows, warp), four a lane
+        if (tid < 32) {                                             // sums before each (slice of rows, warp), PER a lane
             uint32_t *flat = &warp_sums[0][0][0];
-            uint32_t v[4][2], t0 = 0, t1 = 0;
+            uint32_t v[PER][2], t0 = 0, t1 = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[i][0] = flat[(4 * lane + i) * 2];
-                v[i][1] = flat[(4 * lane + i) * 2 + 1];
+            for (int i = 0; i < PER; ++i) {
+                v[i][0] = flat[(PER * lane + i) * 2];
+                v[i][1] = flat[(PER * lane + i) * 2 + 1];
                 t0 += v[i][0]; t1 += v[i][1];
             }
-            uint32_t x0 = t0, x1 = t1;
+            uint32_t x0 = lane_scan(t0, lane) - t0, x1 = lane_scan(t1, lane) - t1;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t y0 = __shfl_up_sync(0xffffffffu, x0, o), y1 = __shfl_up_sync(0xffffffffu, x1, o);
-                if (lane >= o) { x0 += y0; x1 += y1; }
-            }
-            x0 -= t0; x1 -= t1;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                flat[(4 * lane + i) * 2] = x0;
-                flat[(4 * lane + i) * 2 + 1] = x1;
+            for (int i = 0; i < PER; ++i) {
+                flat[(PER * lane + i) * 2] = x0;
+                flat[(PER * lane + i) * 2 + 1] = x1;
                 x0 += v[i][0]; x1 += v[i][1];
             }
             if (lane == 31) { turn_counts[0] = x0; turn_counts[1] = x1; }
@@ -185,18 +209,17 @@ __global__ void __launch_bounds__(THREADS) k_evict_select(const PagedEvictArgs a
 #pragma unroll
         for (int i = 0; i < HELD; ++i) {
             const int j = j0 + i * THREADS + tid;
-            const uint32_t x = state(j, key[i]);
+            const uint32_t x = state(j, held[i]);
             const uint32_t at_limit = base1 + warp_sums[i][warp][1] + below1[i];         // rows at the limit up to this one
             if (x == 1u || (x == 2u && at_limit <= equal)) {
                 const uint32_t r = base0 + warp_sums[i][warp][0] + below0[i] + min(at_limit, equal) - 1;
                 kept[r] = j;
-                wout[r] = w[j];
+                wout[r] = held[i];
             }
         }
         base0 += turn_counts[0]; base1 += turn_counts[1];
     }
     for (int r = m + (int)rank * THREADS + tid; r < a.budget; r += size * THREADS) { kept[r] = -1; wout[r] = 0.0f; }
-    cluster_sync_all();                                             // no CTA leaves while its counts are read
 }
 
 // pieces per row, rows of a warp's turn
