@@ -77,7 +77,7 @@ __device__ __forceinline__ int64_t paged_row(const PagedView &c, int s, int row)
 // A tile inside one run is written at once; the pieces of a cut one go to the run's two slots -- the piece a run begins
 // with (when it did not begin the tile) to slot 2b, the one it ends with to slot 2b + 1 -- and a second kernel adds them up
 // in the order of the runs, from the one that holds the first block to the one that holds the last.
-constexpr int PG_TILE_COST = 1;
+constexpr int PG_TILE_COST = 2;
 struct PagedTile { int q0, n, r0, len, s, blocks; int64_t u0; };   // u0: first unit (of head 0)
 struct PagedCut { int q0, r0, rows, h, pieces, first, pad[2]; };    // a tile that begins in run `first` and ends in a later one (pieces 0: none)
 
