@@ -184,72 +184,94 @@ __global__ void __launch_bounds__(LIST_THREADS) k_paged_list(const PagedAttnArgs
     }
 }
 
-// Adds the pieces of a cut tile up, in their order.  Listed tiles: cut blockIdx.x, a warp per row (SUBS = 1).  Few rows: the
-// cut of (sequence, head) blockIdx.x, all warps of the CTA for row blockIdx.y, each with every SUBS-th piece: one long
-// sequence leaves a hundred pieces a row.
+// Adds the pieces of a cut tile up, in their order.  Listed tiles: cut blockIdx.x, ROWS = 4 rows a warp (SUBS = 1).  Few rows:
+// the cut of (sequence, head) blockIdx.x, all warps of the CTA for row blockIdx.y, each with every SUBS-th piece: one long
+// sequence leaves a hundred pieces a row.  Bound by the latency of two dependent reads, and by CTAs that find nothing to do.
 constexpr int JOIN_THREADS = 256, JOIN_WARPS = JOIN_THREADS / 32;
-template <typename T, int SUBS> __global__ void __launch_bounds__(JOIN_THREADS) k_paged_join(const PagedAttnArgs a, int slot_rows, int pitch)
+template <typename T, int SUBS, int ROWS> __global__ void __launch_bounds__(JOIN_THREADS) k_paged_join(const PagedAttnArgs a, int slot_rows, int pitch)
 {
-    __shared__ float sums[JOIN_WARPS][PG_MAX_D + 4];
+    __shared__ float sums[SUBS > 1 ? JOIN_WARPS : 1][PG_MAX_D + 4];
     pdl_enter();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % SUBS;
-    const int row = blockIdx.y * (JOIN_WARPS / SUBS) + warp / SUBS;
+    const int row = (blockIdx.y * (JOIN_WARPS / SUBS) + warp / SUBS) * ROWS;
     if (SUBS > 1) {                          // sequences that another kernel has leave no word about their tiles
         const PagedSeq q = paged_seq(a.c, blockIdx.x / a.c.heads, false);
         if (row >= q.n * a.group || q.n * a.group > slot_rows) return;
     }
     const PagedCut cut = a.cuts[blockIdx.x];
     if (row >= cut.rows || cut.pieces == 0) return;              // with several warps a row: the same for all
+    const int rows = min(ROWS, cut.rows - row);
     auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * cut.first + 1 : 2 * (cut.first + i)) * slot_rows + row; };
     const float c2 = a.scale * 1.4426950408889634f;
-    float top = -INFINITY;
-    for (int i = lane; i < cut.pieces; i += 32) top = fmaxf(top, a.part_ml[slot(i)].x);
+    float top[ROWS];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    for (int r = 0; r < ROWS; ++r) top[r] = -INFINITY;
+    for (int i = lane; i < cut.pieces; i += 32)
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+            if (r < rows) top[r] = fmaxf(top[r], a.part_ml[slot(i) + r].x);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], o));
     const bool mine = 4 * lane < a.c.d;
-    float l = 0.0f, acc[4] = {};
+    float l[ROWS] = {}, acc[ROWS][4] = {};
     for (int i0 = sub; i0 < cut.pieces; i0 += 32 * SUBS) {
-        // each lane looks up one piece's weight, then all walk through them
+        // each lane looks up one piece's weights, then all walk through them
         const int i1 = i0 + lane * SUBS;
-        float2 ml = make_float2(-INFINITY, 0.0f);
-        if (i1 < cut.pieces) ml = a.part_ml[slot(i1)];
-        const float f = ml.x == -INFINITY ? 0.0f : exp2f((ml.x - top) * c2), fl = f * ml.y;
-        const int n = min(32, (cut.pieces - i0 + SUBS - 1) / SUBS);
-#pragma unroll 8
-        for (int i = 0; i < n; ++i) {
-            const float w = __shfl_sync(0xffffffffu, f, i);
-            l += __shfl_sync(0xffffffffu, fl, i);
-            if (w != 0.0f && mine) {         // a piece without keys for this row has written no sums
-                float v[4];
-                load4(a.part + slot(i0 + i * SUBS) * pitch + 4 * lane, v);
+        float f[ROWS], fl[ROWS];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, v[e], acc[e]);
+        for (int r = 0; r < ROWS; ++r) {
+            float2 ml = make_float2(-INFINITY, 0.0f);
+            if (i1 < cut.pieces && r < rows) ml = a.part_ml[slot(i1) + r];
+            f[r] = ml.x == -INFINITY ? 0.0f : exp2f((ml.x - top[r]) * c2);
+            fl[r] = f[r] * ml.y;
+        }
+        const int n = min(32, (cut.pieces - i0 + SUBS - 1) / SUBS);
+#pragma unroll(ROWS == 1 ? 8 : 2)
+        for (int i = 0; i < n; ++i) {
+            const float *src = a.part + slot(i0 + i * SUBS) * pitch + 4 * lane;
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const float w = __shfl_sync(0xffffffffu, f[r], i);
+                l[r] += __shfl_sync(0xffffffffu, fl[r], i);
+                if (w != 0.0f && mine) {     // a piece without keys for this row has written no sums
+                    float v[4];
+                    load4(src + r * pitch, v);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[r][e] = fmaf(w, v[e], acc[r][e]);
+                }
             }
         }
     }
     if (SUBS > 1) {
-        if (mine) store4(&sums[warp][4 * lane], acc);
-        if (lane == 0) sums[warp][PG_MAX_D] = l;
+        if (mine) store4(&sums[warp][4 * lane], acc[0]);
+        if (lane == 0) sums[warp][PG_MAX_D] = l[0];
         __syncthreads();
         if (sub != 0) return;
         for (int i = 1; i < SUBS; ++i) {
             float v[4];
             load4(&sums[warp + i][4 * lane], v);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] += v[e];
-            l += sums[warp + i][PG_MAX_D];
+            for (int e = 0; e < 4; ++e) acc[0][e] += v[e];
+            l[0] += sums[warp + i][PG_MAX_D];
         }
     }
-    const int r = cut.r0 + row;
-    const int64_t token = cut.q0 + r / a.group;
-    const int head = cut.h * a.group + r % a.group;
-    if (mine) {
-        const float inv = 1.0f / l;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = top == -INFINITY ? 0.0f : acc[e] * inv;
-        store4((T *)a.out + token * a.ldo + (int64_t)head * a.c.d + 4 * lane, acc);
+    for (int i = 0; i < ROWS; ++i) {
+        if (i >= rows) break;
+        const int r = cut.r0 + row + i;
+        const int64_t token = cut.q0 + r / a.group;
+        const int head = cut.h * a.group + r % a.group;
+        const bool none = top[i] == -INFINITY;
+        if (mine) {
+            const float inv = 1.0f / l[i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][e] = none ? 0.0f : acc[i][e] * inv;
+            store4((T *)a.out + token * a.ldo + (int64_t)head * a.c.d + 4 * lane, acc[i]);
+        }
+        if (lane == 0) a.lse[token * a.hq + head] = none ? -INFINITY : fmaf(top[i], a.scale, logf(l[i]));
     }
-    if (lane == 0) a.lse[token * a.hq + head] = top == -INFINITY ? -INFINITY : fmaf(top, a.scale, logf(l));
 }
 
 struct Scratch { size_t cuts, head, seq_tiles, tiles, ml, part, total; int64_t max_tiles; };
@@ -261,8 +283,8 @@ Scratch scratch_of(const skipffn_paged_cache *c, int group, int64_t N)
     const int64_t most = std::min<int64_t>(c->max_new, N) * group;
     const bool listed = simt(c) || most > PG_FEW_ROWS;
     // the largest of the kernels that the call may launch
-    const int64_t slots = simt(c) ? 2 * PG_SIMT_RUNS * PG_SIMT_ROWS : std::max(PG_FEW_SLOTS, listed ? 2 * PG_TC_RUNS * PG_TC_ROWS : 0);
-    const int64_t tile = simt(c) ? PG_SIMT_ROWS : 2 * (128 / group) * group;
+    const int64_t slots = simt(c) ? PG_SIMT_SLOTS : std::max(PG_FEW_SLOTS, listed ? 2 * PG_TC_RUNS * PG_TC_ROWS : 0);
+    const int64_t tile = simt(c) ? (most <= 16 ? 16 : 64) : 2 * (128 / group) * group;
     const int64_t pitch = !simt(c) && c->head_dim <= 64 ? 64 : 128;
     const size_t cuts = std::max<size_t>(std::max(PG_SIMT_RUNS, PG_TC_RUNS), simt(c) ? 0 : (size_t)c->n_seq * c->heads_kv);
     Scratch s;
@@ -288,16 +310,16 @@ cudaError_t launch_paged_list(const PagedAttnArgs &a, int rows, int block, cudaS
 
 cudaError_t launch_paged_join(const PagedAttnArgs &a, int rows, int pitch, cudaStream_t s)
 {
-    const dim3 grid((unsigned)a.runs, (unsigned)((rows + JOIN_WARPS - 1) / JOIN_WARPS));
-    return a.dtype == SKIPFFN_BF16 ? launch_pdl(k_paged_join<bf16, 1>, grid, dim3(JOIN_THREADS), s, a, rows, pitch)
-                                   : launch_pdl(k_paged_join<float, 1>, grid, dim3(JOIN_THREADS), s, a, rows, pitch);
+    const dim3 grid((unsigned)a.runs, (unsigned)((rows + 4 * JOIN_WARPS - 1) / (4 * JOIN_WARPS)));
+    return a.dtype == SKIPFFN_BF16 ? launch_pdl(k_paged_join<bf16, 1, 4>, grid, dim3(JOIN_THREADS), s, a, rows, pitch)
+                                   : launch_pdl(k_paged_join<float, 1, 4>, grid, dim3(JOIN_THREADS), s, a, rows, pitch);
 }
 
 cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int rows, int pitch, cudaStream_t s)
 {
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(a.c.max_new, a.c.N) * a.group), tiles = (int64_t)a.c.n_seq * a.c.heads;
     const dim3 grid((unsigned)tiles, (unsigned)std::min<int64_t>(most, rows));
-    return launch_pdl(k_paged_join<bf16, JOIN_WARPS>, grid, dim3(JOIN_THREADS), s, a, rows, pitch);
+    return launch_pdl(k_paged_join<bf16, JOIN_WARPS, 1>, grid, dim3(JOIN_THREADS), s, a, rows, pitch);
 }
 
 }  // namespace skipffn
@@ -352,7 +374,7 @@ skipffn_status skipffn_paged_attention(const skipffn_paged_cache *cache, int32_t
     cudaError_t e = cudaSuccess;
     if (a.simt) {
         a.min_rows = 0;
-        e = launch_paged_simt(a, s);
+        e = launch_paged_simt(a, (int)std::min<int64_t>(most, 64), s);
     } else {
         // Sequences of few rows are bound by reading their keys and have a kernel of their own.  Next to chunks these are
         // single tokens (16 rows, the fastest form; what has more joins the chunks); a single sequence that may be a chunk

@@ -130,8 +130,9 @@ struct PagedEvictArgs {
     int32_t elem_bytes;
 };
 
-// rows of a tile, runs of a launch (these size the scratch): plain FMA, two CTAs an SM; few rows, eight warps an SM
-constexpr int PG_SIMT_ROWS = 16, PG_SIMT_KEYS = 32, PG_SIMT_RUNS = 296;
+// rows of a tile, runs of a launch (these size the scratch): plain FMA, two CTAs an SM for 16 rows, one for 64; few rows,
+// eight warps an SM
+constexpr int PG_SIMT_KEYS = 64, PG_SIMT_RUNS = 296, PG_SIMT_SLOTS = 2 * 148 * 64;
 constexpr int PG_FEW_ROWS = 64, PG_FEW_SMS = 160, PG_FEW_SLOTS = 2 * PG_FEW_SMS * 8 * 16;
 constexpr int PG_TC_RUNS = 160, PG_TC_ROWS = 256;     // tensor-core kernel: one run per SM, two row tiles
 
@@ -147,8 +148,8 @@ cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int rows, int pitch, c
 cudaError_t launch_paged_few(const PagedAttnArgs &a, int rows, cudaStream_t s);
 // paged_tc.cu: sequences of more rows than that, bf16
 cudaError_t launch_paged_tc(const PagedAttnArgs &a, cudaStream_t s);
-// paged_simt.cu: any number of rows, plain FMA
-cudaError_t launch_paged_simt(const PagedAttnArgs &a, cudaStream_t s);
+// paged_simt.cu: sequences of at most `rows` rows, any number, plain FMA
+cudaError_t launch_paged_simt(const PagedAttnArgs &a, int rows, cudaStream_t s);
 cudaError_t launch_paged_weights_simt(const PagedWeightsArgs &a, cudaStream_t s);
 // paged_weights.cu (bf16)
 cudaError_t launch_paged_weights(const PagedWeightsArgs &a, cudaStream_t s);
