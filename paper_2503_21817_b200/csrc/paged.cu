@@ -126,11 +126,14 @@ template <typename T> __device__ void empty_rows(const PagedAttnArgs &a, const P
         }
 }
 
-// Lists the tiles of the sequences with more than min_rows rows, in order of the batch, with their first units.  One CTA:
-// a list of 10 000 tiles takes 10 turns.
+// Lists the tiles of the sequences with more than min_rows rows, in order of the batch, with their first units, and the tile
+// that each run begins in.  One CTA: a list of 10 000 tiles takes 10 turns.  Searches go through shared memory while the
+// sequences and tiles fit (a search through global memory costs 0.4 us a step).
+constexpr int LIST_NEAR = 2048;
 __global__ void __launch_bounds__(LIST_THREADS) k_paged_list(const PagedAttnArgs a, int rows, int block)
 {
-    __shared__ int64_t warp_sums[LIST_THREADS / 32];
+    __shared__ int64_t warp_sums[LIST_THREADS / 32], near_units[LIST_NEAR];
+    __shared__ int near_tiles[LIST_NEAR];
     pdl_enter();
     const PagedView &c = a.c;
     int64_t carry = 0, total;
@@ -142,7 +145,11 @@ __global__ void __launch_bounds__(LIST_THREADS) k_paged_list(const PagedAttnArgs
             n = r > a.min_rows ? (r + rows - 1) / rows : 0;
         }
         const int64_t before = block_exclusive(n, warp_sums, total);
-        if (s < c.n_seq) a.seq_tiles[s] = (int)min(carry + before, (int64_t)a.max_tiles);
+        if (s < c.n_seq) {
+            const int first = (int)min(carry + before, (int64_t)a.max_tiles);
+            a.seq_tiles[s] = first;
+            if (s < LIST_NEAR) near_tiles[s] = first;
+        }
         carry += total;
     }
     if (carry > a.max_tiles) {               // overlapping offsets: more rows than tokens
@@ -150,21 +157,21 @@ __global__ void __launch_bounds__(LIST_THREADS) k_paged_list(const PagedAttnArgs
         carry = a.max_tiles;
     }
     const int tiles = (int)carry;
-    if (threadIdx.x == 0) a.seq_tiles[c.n_seq] = tiles;
-    __syncthreads();                         // seq_tiles is read by every thread below
+    __syncthreads();                         // the first tiles are read by every thread below
+    const int *first_tile = c.n_seq <= LIST_NEAR ? near_tiles : a.seq_tiles;
     int64_t units = 0;
     for (int t0 = 0; t0 < tiles; t0 += LIST_THREADS) {
         const int t = t0 + threadIdx.x;
         PagedTile e = {};
         if (t < tiles) {
-            int lo = 0, hi = c.n_seq;        // largest s with seq_tiles[s] <= t
+            int lo = 0, hi = c.n_seq;        // largest s with first_tile[s] <= t
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (a.seq_tiles[mid] <= t) lo = mid; else hi = mid;
+                if (first_tile[mid] <= t) lo = mid; else hi = mid;
             }
             const PagedSeq q = paged_seq(c, lo, false);
             e.q0 = q.q0; e.n = q.n; e.len = q.len; e.s = lo;
-            e.r0 = (t - a.seq_tiles[lo]) * rows;
+            e.r0 = (t - first_tile[lo]) * rows;
             const int live = min(rows, q.n * a.group - e.r0);
             const int keys = max(0, q.len - q.n + (e.r0 + live - 1) / a.group + 1);
             e.blocks = (keys + block - 1) / block;
@@ -175,12 +182,23 @@ __global__ void __launch_bounds__(LIST_THREADS) k_paged_list(const PagedAttnArgs
         }
         const int64_t before = block_exclusive(e.blocks ? (int64_t)(e.blocks + PG_TILE_COST) * c.heads : 0, warp_sums, total);
         e.u0 = units + before;
-        if (t < tiles) a.tiles[t] = e;
+        if (t < tiles) {
+            a.tiles[t] = e;
+            if (t < LIST_NEAR) near_units[t] = e.u0;
+        }
         units += total;
     }
-    if (threadIdx.x == 0) {
-        a.head[0] = tiles;
-        *(int64_t *)(a.head + 2) = units;
+    if (threadIdx.x == 0) *(int64_t *)a.head = units;
+    __syncthreads();
+    const Runs runs(units, a.runs);
+    for (int b = threadIdx.x; b < runs.n; b += LIST_THREADS) {
+        const int64_t u = runs.begin(b);
+        int lo = 0;
+        for (int hi = tiles; hi - lo > 1;) { // largest tile with u0 <= u: it holds u
+            const int mid = (lo + hi) >> 1;
+            if ((tiles <= LIST_NEAR ? near_units[mid] : a.tiles[mid].u0) <= u) lo = mid; else hi = mid;
+        }
+        a.starts[b] = lo;
     }
 }
 
@@ -194,11 +212,11 @@ template <typename T, int SUBS, int ROWS> __global__ void __launch_bounds__(JOIN
     pdl_enter();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % SUBS;
     const int row = (blockIdx.y * (JOIN_WARPS / SUBS) + warp / SUBS) * ROWS;
+    const PagedCut cut = a.cuts[blockIdx.x];
     if (SUBS > 1) {                          // sequences that another kernel has leave no word about their tiles
         const PagedSeq q = paged_seq(a.c, blockIdx.x / a.c.heads, false);
         if (row >= q.n * a.group || q.n * a.group > slot_rows) return;
     }
-    const PagedCut cut = a.cuts[blockIdx.x];
     if (row >= cut.rows || cut.pieces == 0) return;              // with several warps a row: the same for all
     const int rows = min(ROWS, cut.rows - row);
     auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * cut.first + 1 : 2 * (cut.first + i)) * slot_rows + row; };
@@ -274,7 +292,7 @@ template <typename T, int SUBS, int ROWS> __global__ void __launch_bounds__(JOIN
     }
 }
 
-struct Scratch { size_t cuts, head, seq_tiles, tiles, ml, part, total; int64_t max_tiles; };
+struct Scratch { size_t cuts, head, starts, seq_tiles, tiles, ml, part, total; int64_t max_tiles; };
 
 bool simt(const skipffn_paged_cache *c) { return c->dtype == SKIPFFN_FP32 || c->path == SKIPFFN_PATH_SIMT; }
 
@@ -293,6 +311,7 @@ Scratch scratch_of(const skipffn_paged_cache *c, int group, int64_t N)
     auto take = [&](size_t bytes) { const size_t o = at; at = (at + bytes + 255) & ~(size_t)255; return o; };
     s.cuts = take(cuts * sizeof(PagedCut));
     s.head = take(64);
+    s.starts = take(std::max(PG_SIMT_RUNS, PG_TC_RUNS) * 4);
     s.seq_tiles = take(((size_t)c->n_seq + 1) * 4);
     s.tiles = take((size_t)s.max_tiles * sizeof(PagedTile));
     s.ml = take((size_t)slots * sizeof(float2));
@@ -367,7 +386,7 @@ skipffn_status skipffn_paged_attention(const skipffn_paged_cache *cache, int32_t
     a.hq = heads_q; a.group = heads_q / a.c.heads; a.dtype = cache->dtype; a.simt = simt(cache); a.scale = scale;
     char *base = (char *)scratch;
     a.part = (float *)(base + sc.part); a.part_ml = (float2 *)(base + sc.ml); a.cuts = (PagedCut *)(base + sc.cuts);
-    a.tiles = (PagedTile *)(base + sc.tiles); a.head = (int32_t *)(base + sc.head); a.seq_tiles = (int32_t *)(base + sc.seq_tiles);
+    a.tiles = (PagedTile *)(base + sc.tiles); a.head = (int64_t *)(base + sc.head); a.starts = (int32_t *)(base + sc.starts); a.seq_tiles = (int32_t *)(base + sc.seq_tiles);
     a.max_tiles = (int32_t)std::min<int64_t>(sc.max_tiles, INT_MAX);
     cudaStream_t s = (cudaStream_t)stream;
     const int64_t most = std::min<int64_t>(cache->max_new, n) * a.group;

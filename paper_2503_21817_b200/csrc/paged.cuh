@@ -94,7 +94,8 @@ struct PagedAttnArgs {
     float2 *part_ml;                         // [2 runs][rows] maximum (of scores as they are) and sum
     PagedCut *cuts;                          // listed tiles: [runs]; few rows: [sequence][head]
     PagedTile *tiles;                        // listed tiles
-    int32_t *head;                           // listed tiles: number; then units (int64) at head + 2
+    int64_t *head;                           // listed tiles: units
+    int32_t *starts;                         // [runs] tile that a run begins in
     int32_t *seq_tiles;                      // [n_seq + 1] first tile of each sequence
     int32_t max_tiles;
     int32_t min_rows;                        // listed tiles: sequences of at most this many rows are another kernel's

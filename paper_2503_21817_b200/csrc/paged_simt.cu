@@ -57,16 +57,12 @@ template <typename T, int R> __global__ void __launch_bounds__(THREADS, R == 1 ?
     float(*ps)[P_PITCH] = reinterpret_cast<float(*)[P_PITCH]>(vs + KEYS);
     pdl_enter();
     const PagedView &c = a.c;
-    const int tiles = a.head[0], run = blockIdx.x;
-    const Runs runs(*(const int64_t *)(a.head + 2), a.runs);
+    const int run = blockIdx.x;
+    const Runs runs(*a.head, a.runs);
     const int64_t begin = runs.begin(run), end = runs.begin(run + 1);
     if (threadIdx.x == 0) a.cuts[run].pieces = 0;
     if (begin >= end) return;
-    int t = 0;
-    for (int hi = tiles; hi - t > 1;) {      // largest tile with u0 <= begin
-        const int mid = (t + hi) >> 1;
-        if (a.tiles[mid].u0 <= begin) t = mid; else hi = mid;
-    }
+    int t = a.starts[run];
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     const float c2 = a.scale * LOG2E;
     for (int64_t u = begin; u < end; ++t) {

@@ -45,15 +45,12 @@ template <bool WARP> struct PieceFeed {
     int64_t u, end;
     int t = 0;
     PagedTile e;
-    __device__ explicit PieceFeed(const PagedTcParams &p_) : p(p_), runs(*(const int64_t *)(p_.a.head + 2), p_.a.runs)
+    __device__ explicit PieceFeed(const PagedTcParams &p_) : p(p_), runs(*p_.a.head, p_.a.runs)
     {
         u = runs.begin(blockIdx.x);
         end = runs.begin(blockIdx.x + 1);
         if (u >= end) return;
-        for (int hi = p.a.head[0]; hi - t > 1;) {            // largest tile with u0 <= u: it holds u
-            const int mid = (t + hi) >> 1;
-            if (p.a.tiles[mid].u0 <= u) t = mid; else hi = mid;
-        }
+        t = p.a.starts[blockIdx.x];
         e = p.a.tiles[t];
     }
     __device__ bool take(Piece &w)
