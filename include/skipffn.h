@@ -365,7 +365,7 @@ skipffn_status skipffn_kv_compact(const skipffn_saved *saved, const void *src, v
  * trusted: offsets outside the call's tokens, lengths beyond the table, more than max_new new tokens, page numbers
  * outside 0 .. n_pages - 1 never lead to an access outside the arrays; such a sequence (or page) is left out or cut, and
  * skipffn_paged_poll reports SKIPFFN_EINVAL with the site of one of the faults: 64 offsets, 65 length, 66 page, 67 no room for a row,
- * 68 more rows than weights.
+ * 68 more rows than weights; SKIPFFN_ETIMEOUT if a kernel gave up on a wait (results unfinished).
  * head_dim is a multiple of 8 up to 128, page_size a multiple of 8, heads_q / heads_kv at most 64, else EUNSUPPORTED.
  * All sums have a fixed order: equal calls give equal bits. */
 #define SKIPFFN_PAGED_STATUS_WORDS 64
@@ -412,8 +412,8 @@ skipffn_status skipffn_paged_weights(const skipffn_paged_cache *cache, int32_t h
  * the others those with the largest weights, `budget` in all (sinks + recent <= budget, else EINVAL; equal weights: the
  * lower row; NaN below everything); sequences of up to `budget` rows keep all.  The kept rows move, in their order, to the
  * front of `into`'s pages (its page_table; the same heads, head_dim, dtype and n_seq; its cu_new and lens are not used),
- * or of their own with into = NULL.  `into` must name other pages than `cache`, and a page that in-place eviction
- * changes must not be another sequence's; neither is checked.
+ * or of their own with into = NULL (or the same pages and table again).  Otherwise `into` must name other pages than
+ * `cache`, and a page that in-place eviction changes must not be another sequence's; neither is checked.
  *   weights     : [n_seq, heads_kv, width] fp32
  *   kept        : [n_seq, heads_kv, budget] int32 out, ascending former rows, -1 past the rows kept
  *   lens_out    : [n_seq] int32 out, min(lens, budget)

@@ -83,7 +83,7 @@ class PagedCache:
     tokens in the arrays of a call; ``lens``: int32 ``[n_seq]`` rows of each sequence, the new tokens among them as the last
     ones; ``max_new``: the most new tokens a sequence may have.  The three integer tensors live on the device and may be
     changed in place between calls and graph replays.  Work is enqueued on the current torch stream; calls that only
-    read the cache may overlap."""
+    read the cache may overlap.  Keep the object, and the tensors it was made of, as long as a captured call is replayed."""
 
     def __init__(self, k_pages, v_pages, page_table, cu_new, lens, max_new: int, path: int = PATH_DEFAULT):
         import torch
@@ -117,11 +117,19 @@ class PagedCache:
                               page_table.stride(0) if n_seq > 1 else width, cu_new.data_ptr(), lens.data_ptr(), self._status.data_ptr())
         self._ref = ctypes.byref(self._c)
         self._scratch_bytes = {}
+        self._made_on = torch._C._cuda_getCurrentRawStream(index)
+
+    def _on_this_stream(self):
+        """Calls on any stream report to the status block: its memory must outlive those calls too."""
+        torch = self._torch
+        if torch._C._cuda_getCurrentRawStream(self._index) != self._made_on and not torch.cuda.is_current_stream_capturing():
+            self._status.record_stream(torch.cuda.current_stream(self.device))
 
     def append(self, k, v) -> None:
         """Writes the new tokens' keys and values, ``[tokens, heads_kv, head_dim]``, to their rows (``skipffn_paged_append``)."""
         n = k.shape[0]
         args = [_heads(t, name, self._torch_dtype, self._index, n, self.heads_kv, self.head_dim) for t, name in ((k, "k"), (v, "v"))]
+        self._on_this_stream()
         st = _on_device(self._lib.skipffn_paged_append, self._index, self._ref, n, *args[0], *args[1])
         if st != 0:
             raise SkipFFNError(st, "skipffn_paged_append")
@@ -143,6 +151,7 @@ class PagedCache:
         if nbytes is None:
             nbytes = self._scratch_bytes[n, hq] = int(self._lib.skipffn_paged_attention_scratch_bytes(self._ref, hq, n))
         scratch = q.new_empty(max(nbytes, 16), dtype=self._torch.uint8)
+        self._on_this_stream()
         st = _on_device(self._lib.skipffn_paged_attention, self._index, self._ref, hq, d ** -0.5 if scale is None else float(scale), n, *aq,
                         *ao, al, scratch.data_ptr(), scratch.numel())
         if st != 0:
@@ -165,6 +174,7 @@ class PagedCache:
         if out is None:
             out = q.new_empty(*shape, dtype=self._torch.float32)
         ao = _floats(out, "out", shape, self._index)
+        self._on_this_stream()
         st = _on_device(self._lib.skipffn_paged_weights, self._index, self._ref, hq, self.head_dim ** -0.5 if scale is None else float(scale),
                         n, *aq, al, ap, ao, shape[2])
         if st != 0:
@@ -187,6 +197,7 @@ class PagedCache:
         kept = weights.new_empty(self.n_seq, self.heads_kv, max(budget, 0), dtype=torch.int32)
         lens = weights.new_empty(self.n_seq, dtype=torch.int32)
         new = weights.new_empty(self.n_seq, self.heads_kv, max(budget, 0))
+        self._on_this_stream()
         st = _on_device(self._lib.skipffn_paged_evict, self._index, self._ref, None if into is None else into._ref, aw, width, budget,
                         operator.index(sinks), operator.index(recent), kept.data_ptr(), lens.data_ptr(), new.data_ptr())
         if st != 0:
@@ -249,6 +260,8 @@ class RotaryQK:
         n, index, d = q.shape[0], q.get_device(), self.head_dim
         args = _heads(q, "q", q.dtype, index, n, self.heads_q, d) + _heads(k, "k", q.dtype, index, n, self.heads_kv, d)
         if self.rotary_dim:
+            if positions is None:
+                raise ValueError("positions are needed unless rotary_dim is 0")
             if positions.dim() == 1:
                 positions = positions[None]
             if positions.dtype is not torch.int32 or positions.get_device() != index or positions.dim() != 2 \
@@ -307,6 +320,7 @@ class RotaryQK:
             raise ValueError(f"q must be a {cache._torch_dtype} tensor on {cache.device}")
         d = self.head_dim
         out_q = q.new_empty(n, self.heads_q, d) if out_q is None else out_q
+        cache._on_this_stream()
         st = _on_device(self._lib.skipffn_rotary_append, index, self._handle, cache._ref, n, *args[:4],
                         *_heads(v, "v", q.dtype, index, n, self.heads_kv, d), *args[4:], *gammas,
                         *_heads(out_q, "out_q", q.dtype, index, n, self.heads_q, d))

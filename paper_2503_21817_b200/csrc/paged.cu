@@ -439,12 +439,17 @@ skipffn_status skipffn_paged_evict(const skipffn_paged_cache *cache, const skipf
     skipffn_status st = paged_view(cache, 0, &a.c);
     if (st != SKIPFFN_OK) return st;
     if (width < 0 || budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget) return SKIPFFN_EINVAL;
-    a.in_place = into == nullptr;
+    // the same pages through the same table are the same place, however they are named
+    a.in_place = !into || (into->k_pages == cache->k_pages && into->v_pages == cache->v_pages && into->page_table == cache->page_table);
     a.dst = a.c;
     if (into) {
         st = paged_view(into, 0, &a.dst);
         if (st != SKIPFFN_OK) return st;
         if (into->dtype != cache->dtype || into->heads_kv != cache->heads_kv || into->head_dim != cache->head_dim || into->n_seq != cache->n_seq)
+            return SKIPFFN_EINVAL;
+        // one pool seen with other strides has no order in which its rows could move
+        if (a.in_place && (into->page_stride != cache->page_stride || into->row_stride != cache->row_stride || into->head_stride != cache->head_stride ||
+                           into->page_size != cache->page_size || into->table_stride != cache->table_stride))
             return SKIPFFN_EINVAL;
     }
     if (a.c.n_seq == 0) return SKIPFFN_OK;

@@ -77,14 +77,17 @@ def test_rows_kept_and_moved(lens, budget, sinks, recent, kind, hk, d, page, dty
         for h in range(hk):
             m = new[s]
             want_w[s, h, :m] = w.cpu().numpy()[s, h, kept[s, h, :m]]
-    for into in (y.cache, None):
+    copies = x.k.clone(), x.v.clone()
+    for into in (y.cache, None, x.cache):                        # its own object: in place, too
+        if into is x.cache:
+            x.k.copy_(copies[0]), x.v.copy_(copies[1])
         got, got_lens, got_w = x.cache.evict(w, budget, sinks=sinks, recent=recent, into=into)
         x.cache.poll()
         assert np.array_equal(got.cpu().numpy(), kept)
         assert got_lens.tolist() == new
         assert np.array_equal(got_w.cpu().numpy(), want_w, equal_nan=True)
-        a, b = (y.k, y.v) if into is not None else (x.k, x.v)
-        c, e = moved if into is not None else in_place
+        a, b = (y.k, y.v) if into is y.cache else (x.k, x.v)
+        c, e = moved if into is y.cache else in_place
         assert _same_bits(a, c) and _same_bits(b, e)
 
 

@@ -29,6 +29,8 @@ CASES = [
     ((70, 40), (71, 45), 10, 2, 80, 16),                    # groups of 5
     ((50, 60), (20, 60), 4, 2, 128, 8),                     # a chunk whose first tokens see nothing
     ((20,), (100,), 64, 1, 32, 16),
+    ((150,) * 8, (150, 160, 170, 180, 190, 200, 210, 220), 32, 1, 64, 16),     # several tiles for every CTA
+    ((5, 7, 16), (1500, 40, 900), 8, 2, 64, 16),            # 20 to 64 rows over many blocks
 ]
 
 
@@ -240,6 +242,57 @@ def test_long_cache_rows_against_64_bits():
     r_out, r_lse, e_out, e_lse = x.want()
     within(out, r_out, e_out, "out")
     within(lse, r_lse, e_lse, "lse")
+
+
+@pytest.mark.parametrize("new", [(1, 3), (50, 3)])
+def test_pages_past_four_gigabytes(new):
+    # 40 000 pages of 64 rows: 5.2 GB for the keys alone; the sequences' pages are the last ones
+    import torch
+    import paper_2503_21817_b200 as sk
+    lens, hq, hk, d, page, pages = (200, 100), 8, 8, 128, 64, 40000
+    x = Batch(13, new, lens, hq, hk, d, page, spare=0)
+    k, v = (torch.empty(pages, page, hk, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    shift = pages - x.k.shape[0]
+    k[shift:], v[shift:] = x.k, x.v
+    table = torch.where(x.d_table >= 0, x.d_table + shift, x.d_table)
+    far = sk.PagedCache(k, v, table, x.d_cu, x.d_lens, max(new))
+    out, lse = far.attention(x.q)
+    want, lse2 = x.cache.attention(x.q)
+    assert torch.equal(out, want) and torch.equal(lse, lse2)
+    w = far.weights(x.q, lse, width=200)
+    assert torch.equal(w, x.cache.weights(x.q, lse, width=200))
+    n = x.cu[-1]
+    nk, nv = normal(1, n, hk, d), normal(2, n, hk, d)
+    far.append(nk, nv), x.cache.append(nk, nv)
+    kept = far.evict(w, 64, 2, 8)
+    assert all(torch.equal(a, b) for a, b in zip(kept, x.cache.evict(w, 64, 2, 8)))
+    far.poll(), x.cache.poll()
+    for a, b in ((k[shift:], x.k), (v[shift:], x.v)):
+        assert torch.equal(a.contiguous().view(torch.int16), b.contiguous().view(torch.int16))
+
+
+def test_no_tokens_no_sequences_no_pages():
+    import torch
+    import paper_2503_21817_b200 as sk
+    x = Batch(14, (1, 1), (20, 30), 4, 2, 64, 16)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    q0 = x.q[:0]
+    assert x.cache.attention(q0)[0].shape == (0, 4, 64)
+    none = sk.PagedCache(x.k, x.v, x.d_table[:0], i32(0), i32(), 1)
+    out, lse = none.attention(x.q, out=torch.full_like(x.q, 7.0))
+    assert bool((out == 7.0).all()) and none.weights(x.q, lse, width=9).shape == (0, 2, 9)
+    empty = sk.PagedCache(x.k[:0], x.v[:0], x.d_table[:, :0], x.d_cu, i32(0, 0), 1)
+    for new in (1, 60):                                          # the kernel for few rows, the one for chunks
+        e = sk.PagedCache(x.k[:0], x.v[:0], x.d_table[:, :0], i32(0, 0, new), i32(0, 0), new)
+        q = normal(5, new, 4, 64)
+        out, lse = e.attention(q)
+        assert bool((out == 0).all()) and bool((lse == float("-inf")).all())
+        e.poll()
+    w = empty.weights(x.q, lse[:2], width=5)
+    assert bool((w == 0).all())
+    kept, lens, ww = empty.evict(w, 3)
+    assert bool((kept == -1).all()) and lens.tolist() == [0, 0] and bool((ww == 0).all())
+    empty.poll()
 
 
 def test_a_key_that_scores_minus_infinity_has_probability_zero():

@@ -96,7 +96,8 @@ def test_evict_arguments_refused():
                dict(lens=None), dict(out=None), dict(kept=301 * M + 2), dict(kept=300 * M), dict(out=300 * M + 4), dict(lens=301 * M),
                dict(out=301 * M + 64), dict(kept=64 * M), dict(out=128 * M), dict(lens=202 * M), dict(into=_cache(**other, dtype=1)),
                dict(into=_cache(**other, heads_kv=4)), dict(into=_cache(**other, head_dim=64)), dict(into=_cache(**other, n_seq=1)),
-               dict(into=_cache(**other, n_pages=-1)), dict(into=_cache(**other), kept=500 * M)):
+               dict(into=_cache(**other, n_pages=-1)), dict(into=_cache(**other), kept=500 * M), dict(into=_cache(page_size=32, page_stride=32 * 1024)),
+               dict(into=_cache(table_stride=16))):
         assert e(**kw) == 1, kw
     assert lib.skipffn_paged_evict(_cache(n_seq=0, cu_new=None, lens=None), None, None, 0, 16, 0, 0, None, None, None, None) == 0
 

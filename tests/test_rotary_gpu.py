@@ -76,6 +76,17 @@ def test_default_and_restarted_frequencies_and_far_positions(dtype):
     _check(two, q, k, pos, g, dq, dk, [100.0 ** (-p / 16) for p in range(16)] * 2, [0] * 16 + [1] * 16, 64, False, dtype)
 
 
+def test_no_tokens():
+    import torch
+    import paper_2503_21817_b200 as sk
+    q, k, pos, g, dq, dk = _case(4, 5, 4, 2, 64, "bf16")
+    rot = sk.RotaryQK(4, 2, 64)
+    a = [t[:0] for t in (q, k)]
+    out = rot.forward(*a, pos[:, :0], *g)
+    back = rot.backward(dq[:0], dk[:0], *a, pos[:, :0], *g)
+    assert out[0].shape == (0, 4, 64) and back[1].shape == (0, 2, 64) and not back[2].any() and not back[3].any()
+
+
 def test_norm_of_small_and_zero_rows():
     import torch
     import paper_2503_21817_b200 as sk
