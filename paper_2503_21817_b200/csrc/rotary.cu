@@ -130,25 +130,36 @@ template <int V, bool INTER> __device__ __forceinline__ LanePairs lane_pairs(int
     return l;
 }
 
-// Rotates the lane's pairs, whose cosines (then sines) stand at `cs` (`cs` + pairs); sign -1 turns back.
+// Where the cosine of pair p stands in a token's part of the table (its sine `pairs` further): four of a lane's pairs
+// together, the lanes of a row side by side, so that a row's lanes read whole lines of banks.
+template <int V> __device__ __forceinline__ int table_at(int p, int pairs) { return (p % V / 4 * (pairs / V) + p / V) * 4 + p % 4; }
+
+// Rotates the lane's pairs, whose cosines start at `cs` (the place of the lane's first pair); sign -1 turns back.
 template <int V, bool INTER> __device__ __forceinline__ void rotate(uint64_t (&lo)[V / 2], uint64_t (&hi)[V / 2], const float *cs, int pairs, float sign)
 {
-    if (INTER) {                             // a pair stands in one register pair: (a, b) c + (-b, a) s
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            uint64_t &x = i < V / 2 ? lo[i] : hi[i - V / 2];
-            const float c = cs[i], s = sign * cs[pairs + i];
-            float a, b;
-            unpair2(x, a, b);
-            x = fma2(pair2(-b, a), both(s), mul2(x, both(c)));
-        }
-    } else {                                 // two pairs in two register pairs
+    for (int j = 0; j < V; j += 4) {
+        float c[4], s[4];
+        load4(cs + j * (pairs / V), c);
+        load4(cs + j * (pairs / V) + pairs, s);
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-            const float2 cf = *reinterpret_cast<const float2 *>(cs + 2 * i), sf = *reinterpret_cast<const float2 *>(cs + pairs + 2 * i);
-            const uint64_t c = pair2(cf.x, cf.y), s = pair2(sign * sf.x, sign * sf.y), n = pair2(-sign * sf.x, -sign * sf.y), x = lo[i];
-            lo[i] = fma2(hi[i], n, mul2(x, c));
-            hi[i] = fma2(x, s, mul2(hi[i], c));
+        for (int e = 0; e < 4; ++e) s[e] *= sign;
+        if (INTER) {                         // a pair stands in one register pair: (a, b) c + (-b, a) s
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint64_t &x = j + e < V / 2 ? lo[j + e] : hi[j + e - V / 2];
+                float a, b;
+                unpair2(x, a, b);
+                x = fma2(pair2(-b, a), both(s[e]), mul2(x, both(c[e])));
+            }
+        } else {                             // two pairs in two register pairs
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const int i = (j + e) / 2;
+                const uint64_t c2 = pair2(c[e], c[e + 1]), x = lo[i];
+                lo[i] = fma2(hi[i], pair2(-s[e], -s[e + 1]), mul2(x, c2));
+                hi[i] = fma2(x, pair2(s[e], s[e + 1]), mul2(hi[i], c2));
+            }
         }
     }
 }
@@ -162,18 +173,19 @@ template <int L> __device__ __forceinline__ float group_sum(float v)
 
 // Cosines, then sines of the tokens whose positions stand at `pos` ([axis][RT_MAX_TOKENS]): a token's 2 x pairs floats.  A
 // thread has one pair, whose frequency it reads once (parameters read at 32 different places take 32 turns).
-__device__ __forceinline__ void fill_table(float *table, const RotaryArgs &a, const RotaryTurns &f, const int *pos, int count)
+template <int V> __device__ __forceinline__ void fill_table(float *table, const RotaryArgs &a, const RotaryTurns &f, const int *pos, int count)
 {
     const int pairs = a.rot / 2;
     if (pairs == 0) return;
     const int step = RT_THREADS / pairs, first = threadIdx.x / pairs, p = threadIdx.x - first * pairs;
     if (first >= step) return;
+    const int at = table_at<V>(p, pairs);
     const unsigned long long turns = f.turns[p];
     pos += f.axis[p] * RT_MAX_TOKENS;
     for (int t = first; t < count; t += step) {
         const float2 cs = turn_to_cos_sin((unsigned long long)(long long)pos[t] * turns);
-        table[t * a.rot + p] = cs.x;
-        table[t * a.rot + pairs + p] = cs.y;
+        table[t * a.rot + at] = cs.x;
+        table[t * a.rot + pairs + at] = cs.y;
     }
 }
 
@@ -290,7 +302,7 @@ k_rotary_fwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ Rotar
             walk.next();
         }
         if (r0 == 0 && kind < 2) {           // the table is made while the first rows arrive
-            fill_table(table, a, f, pos, count);
+            fill_table<V>(table, a, f, pos, count);
             __syncthreads();
         }
 #pragma unroll
@@ -307,7 +319,7 @@ k_rotary_fwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ Rotar
 #pragma unroll
                     for (int i = 0; i < V / 2; ++i) { lo[i] = mul2(mul2(lo[i], g0[i]), r); hi[i] = mul2(mul2(hi[i], g1[i]), r); }
                 }
-                if (at[u] >= 0 && l.p0 >= 0) rotate<V, INTER>(lo, hi, table + at[u] * a.rot + l.p0, a.rot / 2, 1.0f);
+                if (at[u] >= 0 && l.p0 >= 0) rotate<V, INTER>(lo, hi, table + at[u] * a.rot + l.p0 / V * 4, a.rot / 2, 1.0f);
                 pack<T>(lo, x[u].w0);
                 pack<T>(hi, x[u].w1);
             }
@@ -363,7 +375,7 @@ k_rotary_bwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ Rotar
                 walk.next();
             }
             if (r0 == 0) {
-                fill_table(table, a, f, pos, count);
+                fill_table<V>(table, a, f, pos, count);
                 __syncthreads();
             }
 #pragma unroll
@@ -371,7 +383,7 @@ k_rotary_bwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ Rotar
                 uint64_t lo[V / 2], hi[V / 2];
                 unpack(y[u].w0, lo);
                 unpack(y[u].w1, hi);
-                if (at[u] >= 0 && l.p0 >= 0) rotate<V, INTER>(lo, hi, table + at[u] * a.rot + l.p0, a.rot / 2, -1.0f);
+                if (at[u] >= 0 && l.p0 >= 0) rotate<V, INTER>(lo, hi, table + at[u] * a.rot + l.p0 / V * 4, a.rot / 2, -1.0f);
                 if (k.gamma) {
                     uint64_t xl[V / 2], xh[V / 2], ss = 0, ux = 0;
                     unpack(x[u].w0, xl);
