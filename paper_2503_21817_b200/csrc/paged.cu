@@ -334,11 +334,11 @@ cudaError_t launch_paged_join(const PagedAttnArgs &a, int rows, int pitch, cudaS
                                    : launch_pdl(k_paged_join<float, 1, 4>, grid, dim3(JOIN_THREADS), s, a, rows, pitch);
 }
 
-cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int rows, int pitch, cudaStream_t s)
+cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int pitch, cudaStream_t s)
 {
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(a.c.max_new, a.c.N) * a.group), tiles = (int64_t)a.c.n_seq * a.c.heads;
-    const dim3 grid((unsigned)tiles, (unsigned)std::min<int64_t>(most, rows));
-    return launch_pdl(k_paged_join<bf16, JOIN_WARPS, 1>, grid, dim3(JOIN_THREADS), s, a, rows, pitch);
+    const dim3 grid((unsigned)tiles, (unsigned)std::min<int64_t>(most, PG_FEW_ROWS));
+    return launch_pdl(k_paged_join<bf16, JOIN_WARPS, 1>, grid, dim3(JOIN_THREADS), s, a, PG_FEW_ROWS, pitch);
 }
 
 }  // namespace skipffn
@@ -395,12 +395,11 @@ skipffn_status skipffn_paged_attention(const skipffn_paged_cache *cache, int32_t
         a.min_rows = 0;
         e = launch_paged_simt(a, (int)std::min<int64_t>(most, 64), s);
     } else {
-        // Sequences of few rows are bound by reading their keys and have a kernel of their own.  Next to chunks these are
-        // single tokens (16 rows, the fastest form; what has more joins the chunks); a single sequence that may be a chunk
-        // is not worth the launches that would find nothing to do.
+        // Sequences of few rows are bound by reading their keys and have a kernel of their own; a single sequence that may
+        // have more is not worth the launches that would find nothing to do.
         const bool listed = most > PG_FEW_ROWS, few = !listed || a.c.n_seq > 1;
-        a.min_rows = few ? 16 : 0;
-        if (few) e = launch_paged_few(a, listed ? 16 : (int)most, s);
+        a.min_rows = few ? PG_FEW_ROWS : 0;
+        if (few) e = launch_paged_few(a, s);
         if (e == cudaSuccess && listed) e = launch_paged_tc(a, s);
     }
     return e == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;

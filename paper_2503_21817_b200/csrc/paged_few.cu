@@ -1,17 +1,18 @@
-// Attention over a paged cache for sequences of at most 64 rows (new tokens x query heads of a kv head), bf16: the token that
-// is being answered, a handful of proposed ones.
+// Attention over a paged cache for sequences of at most 16 rows (new tokens x query heads of a kv head), bf16: the token that
+// is being answered, a few proposed ones.
 //
 //   s_rj = scale q_r . k_j,  out_r = sum_j softmax(s_r)_j v_j,  one pass over the keys with a running maximum and sum.
 //
 // Bound by reading the cache once: 512 bytes a key and kv head at head_dim 128 for 4 x rows x 128 flops, so the legacy
 // matrix instructions (mma.sync, whose accumulators are registers and need no second kernel role) are far from their
-// limit.  The keys of all sequences and heads, 16 to a unit, are one line that is cut into equal runs, one per stream: a
-// warp for tiles of up to 16 rows, two or four warps with 16 rows each for more (eight warps an SM).  Ragged batches and one
-// long sequence load every SM alike; a tile counts one unit more than it has, for its beginning and end.  A stream brings its
-// units through its own ring of asynchronous 16-byte copies and waits for no other: what the end of one tile costs (its
-// sums written, the next queries fetched) does not hold up the rest of the SM.  Rows come from their pages eight at a time (a
-// page holds whole groups of eight).  Before, four warps shared a unit of 64 keys and merged their sums at a tile's end:
-// 105 us for 48 conversations of 37 to 8877 rows (32 / 8 heads, head_dim 128).
+// limit.  The keys of all sequences and heads, 16 to a unit, are one line that is cut into equal runs, one per WARP (eight
+// an SM): ragged batches and one long sequence load every SM alike.  A warp brings its units through its own ring of
+// asynchronous 16-byte copies and waits for no other: what the end of one tile costs (its sums written, the next queries
+// fetched) does not hold up the rest of the SM.  Rows come from their pages eight at a time (a page holds whole groups of
+// eight).  Measured, 48 conversations of 37 to 8877 rows, 32 / 8 heads, head_dim 128: 80 us (5.8 TB/s while it streams, 5.5
+// over all); one of 130 001 rows 98 us.  Before, four warps shared a unit of 64 keys and merged their sums at a tile's end:
+// 105 us.  Two or four warps with 16 rows each behind one ring were slower than the tensor-core kernel (32 rows 144 us
+// against 128), which has everything beyond 16 rows.
 #include "paged.cuh"
 #include "paged_mma.cuh"
 
@@ -19,27 +20,27 @@ namespace skipffn {
 
 namespace {
 
-constexpr int WARPS = 8, THREADS = 32 * WARPS, KEYS = 16;
+constexpr int WARPS = 8, THREADS = 32 * WARPS, KEYS = 16, ROWS = PG_FEW_ROWS;
 constexpr float LOG2E = 1.4426950408889634f;
 
 // Blocks of keys of a sequence, of one head; a sequence without keys has one, which writes its empty rows.
-__device__ __forceinline__ int few_blocks(const PagedSeq &q, int group, int rows)
+__device__ __forceinline__ int few_blocks(const PagedSeq &q, int group)
 {
-    return q.n > 0 && q.n * group <= rows ? max(1, (q.len + KEYS - 1) / KEYS) : 0;
+    return q.n > 0 && q.n * group <= ROWS ? max(1, (q.len + KEYS - 1) / KEYS) : 0;
 }
 
 // A place in the line of units: block b of head h of sequence s
 struct Place {
     int s, h, b, blocks;
     PagedSeq q;
-    __device__ void enter(const PagedView &c, int group, int rows, int seq)
+    __device__ void enter(const PagedView &c, int group, int seq)
     {
         s = seq;
         q = paged_seq(c, s, false);
-        blocks = few_blocks(q, group, rows);
+        blocks = few_blocks(q, group);
     }
     // to the next block; the units that lie between.  The sequences end where the line does.
-    __device__ int step(const PagedView &c, int group, int rows)
+    __device__ int step(const PagedView &c, int group)
     {
         if (++b < blocks) return 1;
         b = 0;
@@ -47,36 +48,35 @@ struct Place {
             h = 0;
             do {
                 if (s + 1 >= c.n_seq) break;
-                enter(c, group, rows, s + 1);
+                enter(c, group, s + 1);
             } while (blocks == 0);
         }
         return 1 + PG_TILE_COST;
     }
 };
 
-// W warps make a stream
-template <int DP, int W> struct FewShape {
+template <int DP> struct FewShape {
     static constexpr int TILE = KEYS * DP * 2, STAGE = 2 * TILE;              // keys, then values
-    static constexpr int STAGES = (DP == 128 ? 3 : 6) * W, STREAMS = WARPS / W, ROWS = 16 * W;
-    static constexpr int SMEM = STREAMS * STAGES * STAGE;
+    static constexpr int STAGES = DP == 128 ? 3 : 6;
+    static constexpr int SMEM = WARPS * STAGES * STAGE;
 };
 
-template <int DP, int W>
+template <int DP>
 __global__ void __launch_bounds__(THREADS, 1) k_paged_few(const PagedAttnArgs a)
 {
-    using Sh = FewShape<DP, W>;
-    constexpr int CHUNKS = DP / 8, STEP = 32 * W / CHUNKS, STAGES = Sh::STAGES, STREAMS = Sh::STREAMS, ROWS = Sh::ROWS;
+    using Sh = FewShape<DP>;
+    constexpr int CHUNKS = DP / 8, STEP = 32 / CHUNKS, STAGES = Sh::STAGES;
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int64_t scan[WARPS], place_in[STREAMS];
-    __shared__ int place_seq[STREAMS];
+    __shared__ int64_t scan[WARPS], place_in[WARPS];
+    __shared__ int place_seq[WARPS];
     const PagedView &c = a.c;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, stream = warp / W, ctas = gridDim.x;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, ctas = gridDim.x;
     pdl_enter();
 
-    // ---- where the runs lie: sums of units over the sequences.  Run r is stream r / CTAs of CTA r % CTAs, so that a few runs
-    // are spread over the SMs.
+    // ---- where the runs lie: sums of units over the sequences.  Run r is warp r / CTAs of CTA r % CTAs, so that a few runs are
+    // spread over the SMs.
     auto units_of = [&](int s, bool report) {
-        const int b = s < c.n_seq ? few_blocks(paged_seq(c, s, report), a.group, ROWS) : 0;
+        const int b = s < c.n_seq ? few_blocks(paged_seq(c, s, report), a.group) : 0;
         return b ? (int64_t)(b + PG_TILE_COST) * c.heads : 0;
     };
     auto block_sum = [&](int64_t v) {
@@ -92,10 +92,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_few(const PagedAttnArgs a)
     };
     int64_t mine = 0;
     for (int s = tid; s < c.n_seq; s += THREADS) mine += units_of(s, blockIdx.x == 0);
-    const Runs runs(block_sum(mine), ctas * STREAMS);
+    const Runs runs(block_sum(mine), ctas * WARPS);
     if (runs.units == 0) return;
     int64_t before = 0;
-    const int64_t last_begin = min(runs.begin((STREAMS - 1) * ctas + (int)blockIdx.x), runs.units - 1);
+    const int64_t last_begin = min(runs.begin((WARPS - 1) * ctas + (int)blockIdx.x), runs.units - 1);
     for (int s0 = 0; s0 < c.n_seq; s0 += THREADS) {
         const int64_t v = units_of(s0 + tid, false);
         int64_t x = v;
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_few(const PagedAttnArgs a)
         const int64_t total = block_sum(v);
         int64_t lo = before + x - v;
         for (int i = 0; i < warp; ++i) lo += scan[i];
-        for (int w = 0; w < STREAMS; ++w) {
+        for (int w = 0; w < WARPS; ++w) {
             const int64_t u = runs.begin(w * ctas + (int)blockIdx.x);
             if (lo <= u && u < lo + v) { place_seq[w] = s0 + tid; place_in[w] = u - lo; }
         }
@@ -115,28 +115,23 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_few(const PagedAttnArgs a)
         if (before > last_begin) break;      // the same in every thread
     }
     __syncthreads();
-    const int run = stream * ctas + (int)blockIdx.x;
+    const int run = warp * ctas + (int)blockIdx.x;
     const int64_t begin = runs.begin(run), end = runs.begin(run + 1);
     if (run >= runs.n) return;               // no barrier of the CTA below
     Place at;
-    at.enter(c, a.group, ROWS, place_seq[stream]);
+    at.enter(c, a.group, place_seq[warp]);
     const int seg = at.blocks + PG_TILE_COST;
-    at.h = (int)(place_in[stream] / seg);
-    at.b = (int)(place_in[stream] - (int64_t)at.h * seg) - PG_TILE_COST;
+    at.h = (int)(place_in[warp] / seg);
+    at.b = (int)(place_in[warp] - (int64_t)at.h * seg) - PG_TILE_COST;
     int64_t u = begin;                       // of the next block
     if (at.b < 0) { u -= at.b; at.b = 0; }
     if (u >= end) return;                    // the run holds nothing but a tile's beginning
     int64_t item = u - at.b;                 // unit of the tile's first block
-    // the lanes of a stream together
-    auto sync = [&]() {
-        if (W == 1) __syncwarp();
-        else asm volatile("bar.sync %0, %1;" ::"r"(1 + stream), "n"(32 * W) : "memory");
-    };
 
     // ---- the ring.  A unit's pages are looked up when the one before it is issued: lanes 0 and 1 keep the entries for its
     // rows 0 .. 7 and 8 .. 15, which are touched a unit later.
-    const uint32_t ring = smem_u32(smem) + stream * STAGES * Sh::STAGE;
-    const int part = tid % (32 * W), chunk = part % CHUNKS, row0 = part / CHUNKS;
+    const uint32_t ring = smem_u32(smem) + warp * STAGES * Sh::STAGE;
+    const int chunk = lane % CHUNKS, row0 = lane / CHUNKS;
     Place ahead = at;
     int64_t issued = u;
     uint32_t fill = ring, use = ring;
@@ -160,9 +155,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_few(const PagedAttnArgs a)
             }
             const int64_t g[2] = {__shfl_sync(0xffffffffu, base, 0), __shfl_sync(0xffffffffu, base, 1)};
 #pragma unroll
-            for (int i = 0; i < (KEYS + STEP - 1) / STEP; ++i) {
+            for (int i = 0; i < KEYS / STEP; ++i) {
                 const int r = row0 + i * STEP;
-                if (KEYS % STEP && r >= KEYS) break;
                 const int64_t b = r < 8 ? g[0] : g[1];
                 const bool on = b >= 0 && r < left && chunk * 8 < c.d;
                 const int64_t off = on ? b + (r & 7) * c.row_stride + chunk * 16 : 0;
@@ -171,7 +165,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_few(const PagedAttnArgs a)
                 copy16(to + Sh::TILE, c.v + off, on);
             }
             fill = fill == ring + (STAGES - 1) * Sh::STAGE ? ring : fill + Sh::STAGE;
-            issued += ahead.step(c, a.group, ROWS);
+            issued += ahead.step(c, a.group);
             if (issued < end) find();
         }
         copy_commit();
@@ -181,7 +175,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_few(const PagedAttnArgs a)
     for (int i = 0; i < STAGES - 1; ++i) issue();
 
     // ---- arithmetic: a thread has rows r0 and r0 + 8
-    const int r0 = warp % W * 16 + (lane >> 2);
+    const int r0 = lane >> 2;
     const float c2 = a.scale * LOG2E;
     uint32_t qf[DP / 16][4];
     float o[DP / 8][4], m[2], l[2];
@@ -213,7 +207,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_few(const PagedAttnArgs a)
                 for (int e = 0; e < 4; ++e) o[n][e] = 0.0f;
         }
         copy_wait<STAGES - 2>();
-        sync();                              // the unit is there for every lane, and the slot refilled next is free
+        __syncwarp();                        // the unit is there for every lane, and the slot refilled next is free
         issue();
         const uint32_t kt = use, vt = use + Sh::TILE;
         use = use == ring + (STAGES - 1) * Sh::STAGE ? ring : use + Sh::STAGE;
@@ -306,27 +300,27 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_few(const PagedAttnArgs a)
                 if ((lane & 3) == 0) a.part_ml[to] = make_float2(m[i], l[i]);
             }
         }
-        if (item >= begin && part == 0) {    // the run that begins a tile says how many pieces it has
+        if (item >= begin && lane == 0) {    // the run that begins a tile says how many pieces it has
             PagedCut cut = {};
             cut.q0 = at.q.q0; cut.rows = at.q.n * a.group; cut.h = at.h; cut.first = run;
             cut.pieces = whole ? 0 : runs.of(last - 1) - run + 1;
             a.cuts[(int64_t)at.s * c.heads + at.h] = cut;
         }
-        u += at.step(c, a.group, ROWS);
+        u += at.step(c, a.group);
         fresh = true;
     }
     copy_wait<0>();
 }
 
-template <int DP, int W> cudaError_t few(const PagedAttnArgs &a, cudaStream_t s)
+template <int DP> cudaError_t few(const PagedAttnArgs &a, cudaStream_t s)
 {
-    using Sh = FewShape<DP, W>;
+    using Sh = FewShape<DP>;
     static int sms_of_device[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (sms_of_device[dev] == 0) {
         int n = 0;
-        cudaError_t e = cudaFuncSetAttribute(k_paged_few<DP, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::SMEM);
+        cudaError_t e = cudaFuncSetAttribute(k_paged_few<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::SMEM);
         if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
         if (e != cudaSuccess) return e;
         sms_of_device[dev] = n < PG_FEW_SMS ? n : PG_FEW_SMS;
@@ -337,16 +331,12 @@ template <int DP, int W> cudaError_t few(const PagedAttnArgs &a, cudaStream_t s)
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_paged_few<DP, W>, a);
-    return e != cudaSuccess ? e : launch_paged_join_few(a, Sh::ROWS, DP, s);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_paged_few<DP>, a);
+    return e != cudaSuccess ? e : launch_paged_join_few(a, DP, s);
 }
 
 }  // namespace
 
-cudaError_t launch_paged_few(const PagedAttnArgs &a, int rows, cudaStream_t s)
-{
-    if (a.c.d <= 64) return rows <= 16 ? few<64, 1>(a, s) : rows <= 32 ? few<64, 2>(a, s) : few<64, 4>(a, s);
-    return rows <= 16 ? few<128, 1>(a, s) : rows <= 32 ? few<128, 2>(a, s) : few<128, 4>(a, s);
-}
+cudaError_t launch_paged_few(const PagedAttnArgs &a, cudaStream_t s) { return a.c.d <= 64 ? few<64>(a, s) : few<128>(a, s); }
 
 }  // namespace skipffn

@@ -313,3 +313,45 @@ def test_a_key_that_scores_minus_infinity_has_probability_zero():
                 p = np.exp(s - s.max())
                 p /= p.sum()
                 assert np.allclose(to_host(out)[i, h], p @ v[:p.size], atol=2.0 ** -7 * np.abs(v).max())
+
+
+@pytest.mark.parametrize("tokens,lens,hq,hk,d", [
+    (8, range(129, 729, 4), 8, 2, 128),                      # 32 rows, 2 to 6 blocks, most of them within one run
+    (30, range(30, 780, 5), 4, 1, 64),                       # 120 rows, 1 to 7 blocks
+    (17, (257, 384, 385, 1000), 2, 2, 80),                   # 17 rows, all of them cut
+])
+def test_sequences_of_one_row_tile_over_several_blocks(tokens, lens, hq, hk, d):
+    import torch
+    lens = list(lens)
+    x = Batch(14, (tokens,) * len(lens), lens, hq, hk, d, 16)
+    out, lse = x.cache.attention(x.q)
+    x.cache.poll()
+    r_out, r_lse, e_out, e_lse = x.want()
+    within(out, r_out, e_out, "out")
+    within(lse, r_lse, e_lse, "lse")
+    # every other block scores minus infinity: half of a tile's blocks leave nothing, then the other half
+    for odd in (0, 1):
+        y = Batch(14, (tokens,) * len(lens), lens, hq, hk, d, 16)
+        y.q.abs_()
+        for s, n in enumerate(lens):
+            j = torch.arange(n, device="cuda")
+            j = j[j // 128 % 2 == odd]
+            y.k[y.d_table[s].long()[j // 16], j % 16] = float("-inf")
+            y.keys[s][j.cpu().numpy()] = -1e30
+        out, lse = y.cache.attention(y.q)
+        y.cache.poll()
+        q = to_host(y.q)
+        for s, n in enumerate(lens):
+            for i in (0, tokens - 1):
+                t, h = s * tokens + i, hq - 1
+                seen = np.arange(n - tokens + i + 1)
+                seen = seen[seen // 128 % 2 != odd]
+                if not seen.size:
+                    assert bool((out[t, h] == 0).all()) and lse[t, h].item() == float("-inf")
+                    continue
+                sc = y.scale * (y.keys[s][seen, h // (hq // hk)] @ q[t, h])
+                p = np.exp(sc - sc.max())
+                v = y.values[s][seen, h // (hq // hk)]
+                # weights and the result in bf16: half a step each, of values of at most the largest
+                assert np.allclose(to_host(out[t, h]), p / p.sum() @ v, rtol=0, atol=2.0 ** -7 * np.abs(v).max())
+                assert abs(lse[t, h].item() - sc.max() - np.log(p.sum())) < 1e-4 * max(1.0, abs(sc.max()))
