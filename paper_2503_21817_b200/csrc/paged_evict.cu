@@ -6,11 +6,15 @@
 // alone, softmax weights crowd into a few bins and their atomic additions queue up).  A CTA counts its part, then adds its
 // bins that are not empty to every CTA's sums in distributed shared memory: one cluster barrier a count.  A CTA's part of the
 // weights is read once and stays in registers (up to HELD x 512; what is beyond comes from L2 again).  Then every CTA numbers
-// the kept rows of its part.  Bound by this chain of counts and barriers.
+// the kept rows of its part.  Bound by this chain of counts and barriers: 22 us for 48 conversations of 37 to 8877 rows and 8
+// heads (8-bit counts 36 us, with a barrier for every read of a peer's bins 33 us), 9 us for the 8 heads of one prompt.
 // k_evict_move: a warp takes up to 32 rows; its lanes look up their places in parallel, then 16-byte pieces of keys and
-// values move, 8 in flight a lane.  Bound by memory.  In place, a pair's rows move in steps of its whole cluster: a row's
+// values move, 8 in flight a lane (4: 2 us less for the batch, 2 us more for one prompt; 16: 1 and 3 us more).  The three
+// reads that find the next rows run behind the pieces of these.  Bound by memory: 61 us for the batch's 345 MB (5.6 TB/s;
+// rows of a head are 256 bytes apart from their neighbours' in memory).  In place, a pair's rows move in steps of its whole cluster: a row's
 // destination is never behind it (order is kept), so it is enough that a step has read all its rows before it writes any --
 // later steps read only rows behind this step's destinations.
+#include <algorithm>
 #include "paged.cuh"
 #include "ptx.cuh"
 
@@ -230,21 +234,22 @@ template <bool IN_PLACE> __global__ void __launch_bounds__(MOVE_THREADS, 3) k_ev
     pdl_enter();
     const PagedView &c = a.c;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = MOVE_THREADS / 32, half = f.pieces.d / 2;
-    // in place: one cluster per pair, which takes its turns together; else a warp takes one turn of one pair
-    const int64_t id = (int64_t)blockIdx.x * warps + warp;
-    const int pair = IN_PLACE ? blockIdx.x / size : (int)(id / f.turns);
-    if (pair >= c.n_seq * c.heads) return;
-    const int s = pair / c.heads, h = pair - s * c.heads;
-    const int len = min(min(max(c.lens[s], 0), c.capacity), a.width), m = min(min(len, a.budget), a.dst.capacity);
-    const int32_t *kept = a.kept + (int64_t)pair * a.budget;
-    const int step = IN_PLACE ? size * warps * f.rows : 0x7fffffff;
-    for (int64_t r0 = IN_PLACE ? 0 : (id - (int64_t)pair * f.turns) * f.rows; r0 < m; r0 += step) {
-        const int64_t mine = r0 + (IN_PLACE ? ((int)(blockIdx.x % size) * warps + warp) * f.rows : 0);
-        // a lane's row: where it stands and where it goes
-        int64_t from = -1, dest = -1;
-        const int64_t r = mine + lane;
+    // In place, one cluster per pair, whose warps take `step` rows of it together.  Else the turns of all pairs are one line,
+    // of which every warp has its share.
+    const int64_t turns = (int64_t)c.n_seq * c.heads * f.turns, stride = (int64_t)gridDim.x * warps;
+    const int step = size * warps * f.rows, own = IN_PLACE ? ((int)(blockIdx.x % size) * warps + warp) * f.rows : 0;
+    int64_t at = IN_PLACE ? 0 : (int64_t)blockIdx.x * warps + warp;          // row of the pair; turn
+    // a lane's row of a turn: where it stands and where it goes.  False behind the last turn.
+    auto find = [&](int64_t t, int &h, int64_t &from, int64_t &dest) {
+        from = dest = -1;
+        if (!IN_PLACE && t >= turns) return false;
+        const int pair = IN_PLACE ? blockIdx.x / size : (int)(t / f.turns), s = pair / c.heads;
+        h = pair - s * c.heads;
+        const int m = min(min(min(min(max(c.lens[s], 0), c.capacity), a.width), a.budget), a.dst.capacity);
+        if (IN_PLACE && t >= m) return false;
+        const int64_t r = (IN_PLACE ? t + own : (t - (int64_t)pair * f.turns) * f.rows) + lane;
         if (lane < f.rows && r < m) {
-            const int j = kept[r];
+            const int j = a.kept[(int64_t)pair * a.budget + r];
             if (!IN_PLACE || j != r) {
                 from = paged_row(c, s, j);
                 dest = paged_row(a.dst, s, (int)r);
@@ -252,6 +257,12 @@ template <bool IN_PLACE> __global__ void __launch_bounds__(MOVE_THREADS, 3) k_ev
                 if (dest < 0) paged_report(a.dst, SITE_PAGED_PAGE);
             }
         }
+        return true;
+    };
+    int h, next_h = 0;
+    int64_t from, dest, next_from, next_dest;
+    bool more = find(at, h, from, dest);
+    while (more) {
         uint4 v[PIECES];
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -261,6 +272,8 @@ template <bool IN_PLACE> __global__ void __launch_bounds__(MOVE_THREADS, 3) k_ev
             if (row < f.rows && src >= 0 && to >= 0)
                 v[i] = __ldcs(reinterpret_cast<const uint4 *>((p < half ? c.k : c.v) + src + h * c.head_stride + (p < half ? p : p - half) * 16));
         }
+        at += IN_PLACE ? step : stride;
+        more = find(at, next_h, next_from, next_dest);              // three reads, one after the other, behind those of the rows
         if (IN_PLACE) cluster_sync_all();
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -269,6 +282,7 @@ template <bool IN_PLACE> __global__ void __launch_bounds__(MOVE_THREADS, 3) k_ev
             if (row < f.rows && to >= 0)
                 *reinterpret_cast<uint4 *>((p < half ? a.dst.k : a.dst.v) + to + h * a.dst.head_stride + (p < half ? p : p - half) * 16) = v[i];
         }
+        h = next_h; from = next_from; dest = next_dest;
     }
 }
 
@@ -302,8 +316,7 @@ cudaError_t launch_paged_evict(const PagedEvictArgs &a, cudaStream_t s)
     f.turns = (a.budget + f.rows - 1) / f.rows;
     if (a.in_place) return launch_clusters(k_evict_move<true>, (int64_t)pairs * size, MOVE_THREADS, size, s, a, f, size);
     const int64_t warps = (int64_t)pairs * f.turns, ctas = (warps + MOVE_THREADS / 32 - 1) / (MOVE_THREADS / 32);
-    if (ctas > 0x7fffffff) return cudaErrorInvalidValue;
-    return launch_clusters(k_evict_move<false>, ctas, MOVE_THREADS, 0, s, a, f, 0);
+    return launch_clusters(k_evict_move<false>, std::min<int64_t>(ctas, 3 * 148), MOVE_THREADS, 0, s, a, f, 0);
 }
 
 }  // namespace skipffn

@@ -11,8 +11,10 @@
 //   warp 3       what needs no product: columns past a sequence's rows, sequences without new tokens
 //   warps 4..11  two groups, one for each half: exponentials and sums
 // Bound by reading the keys for up to about 100 query rows a kv head, by the exponentials (16 a cycle and SM) beyond.  A TMA
-// box costs its warp about 64 cycles whatever its size, so pages of 16 rows want the two warps (48 conversations: one warp
-// 82 us, two 71 us, with pages of 128 rows 58 us either way).  On the legacy matrix instructions a step of 64 keys x 32 rows
+// box costs its warp about 64 cycles whatever its size, so pages of 16 rows want the two warps (with units of 128 keys, 48
+// conversations took 82 us from one warp, 71 us from two and 58 us from either with pages of 128 rows; with 256 it is 50 us
+// for 238 MB at 16 rows a page as at 128).  161 observing tokens of 40 heads take 55 us, a chunk of 2000 tokens over a
+// cache of 14 345 rows 518 us.  On the legacy matrix instructions a step of 64 keys x 32 rows
 // took 2 us from its copies to its sums however it was cut, with eight warps an SM: 100 us for the batch of 48
 // conversations (238 MB), 250 us for 161 observing tokens of 40 heads.
 #include "paged_tma.cuh"

@@ -10,7 +10,10 @@
 // with the position beyond that of the frequency's last bit (2^-65 of a turn each position).  A CTA computes the table of its tokens once, for all their heads.
 //
 // Bound by memory: every row is read and written once.  A group of lanes holds a row, each lane V pairs of it (two
-// 16-byte vectors where the sizes allow), so the sums of a row are shuffles inside the group.
+// 16-byte vectors where the sizes allow), so the sums of a row are shuffles inside the group.  Measured: forward of 4928
+// tokens, 32 / 8 heads, head_dim 128, normalised, bf16: 24 us for 101 MB (4.2 TB/s; 5.5 to 5.9 with four times the tokens,
+// the rest is launch and the first table); backward of 16 documents 117 us (576 MB, 4.9 TB/s); one token a warp, its
+// cosines in registers, was no faster (23.5 to 30 and 128 us).
 #include <math.h>
 
 #include <initializer_list>
