@@ -198,6 +198,8 @@ class PagedCache:
         lens = weights.new_empty(self.n_seq, dtype=torch.int32)
         new = weights.new_empty(self.n_seq, self.heads_kv, max(budget, 0))
         self._on_this_stream()
+        if into is not None:
+            into._on_this_stream()
         st = _on_device(self._lib.skipffn_paged_evict, self._index, self._ref, None if into is None else into._ref, aw, width, budget,
                         operator.index(sinks), operator.index(recent), kept.data_ptr(), lens.data_ptr(), new.data_ptr())
         if st != 0:
