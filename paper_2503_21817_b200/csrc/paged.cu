@@ -296,15 +296,21 @@ struct Scratch { size_t cuts, head, starts, seq_tiles, tiles, ml, part, total; i
 
 bool simt(const skipffn_paged_cache *c) { return c->dtype == SKIPFFN_FP32 || c->path == SKIPFFN_PATH_SIMT; }
 
+// rows of a sequence that the kernel of few rows takes
+int few_rows(const skipffn_paged_cache *c)
+{
+    return c->path == SKIPFFN_PATH_SIMT ? 0 : c->dtype == SKIPFFN_FP32 ? PG_FEW_ROWS_FP32 : PG_FEW_ROWS;
+}
+
 Scratch scratch_of(const skipffn_paged_cache *c, int group, int64_t N)
 {
     const int64_t most = std::min<int64_t>(c->max_new, N) * group;
-    const bool listed = simt(c) || most > PG_FEW_ROWS;
+    const bool listed = most > few_rows(c), few = c->path != SKIPFFN_PATH_SIMT;
     // the largest of the kernels that the call may launch
-    const int64_t slots = simt(c) ? PG_SIMT_SLOTS : std::max(PG_FEW_SLOTS, listed ? 2 * PG_TC_RUNS * PG_TC_ROWS : 0);
+    const int64_t slots = std::max(few ? PG_FEW_SLOTS : 0, !listed ? 0 : simt(c) ? PG_SIMT_SLOTS : 2 * PG_TC_RUNS * PG_TC_ROWS);
     const int64_t tile = simt(c) ? (most <= 16 ? 16 : 64) : 2 * (128 / group) * group;
     const int64_t pitch = !simt(c) && c->head_dim <= 64 ? 64 : 128;
-    const size_t cuts = std::max<size_t>(std::max(PG_SIMT_RUNS, PG_TC_RUNS), simt(c) ? 0 : (size_t)c->n_seq * c->heads_kv);
+    const size_t cuts = std::max<size_t>(std::max(PG_SIMT_RUNS, PG_TC_RUNS), few ? (size_t)c->n_seq * c->heads_kv : 0);
     Scratch s;
     s.max_tiles = listed ? N * group / tile + c->n_seq + 1 : 0;
     size_t at = 0;
@@ -334,11 +340,12 @@ cudaError_t launch_paged_join(const PagedAttnArgs &a, int rows, int pitch, cudaS
                                    : launch_pdl(k_paged_join<float, 1, 4>, grid, dim3(JOIN_THREADS), s, a, rows, pitch);
 }
 
-cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int pitch, cudaStream_t s)
+cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int rows, int pitch, cudaStream_t s)
 {
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(a.c.max_new, a.c.N) * a.group), tiles = (int64_t)a.c.n_seq * a.c.heads;
-    const dim3 grid((unsigned)tiles, (unsigned)std::min<int64_t>(most, PG_FEW_ROWS));
-    return launch_pdl(k_paged_join<bf16, JOIN_WARPS, 1>, grid, dim3(JOIN_THREADS), s, a, PG_FEW_ROWS, pitch);
+    const dim3 grid((unsigned)tiles, (unsigned)std::min<int64_t>(most, rows));
+    return a.dtype == SKIPFFN_BF16 ? launch_pdl(k_paged_join<bf16, JOIN_WARPS, 1>, grid, dim3(JOIN_THREADS), s, a, rows, pitch)
+                                   : launch_pdl(k_paged_join<float, JOIN_WARPS, 1>, grid, dim3(JOIN_THREADS), s, a, rows, pitch);
 }
 
 }  // namespace skipffn
@@ -391,17 +398,13 @@ skipffn_status skipffn_paged_attention(const skipffn_paged_cache *cache, int32_t
     cudaStream_t s = (cudaStream_t)stream;
     const int64_t most = std::min<int64_t>(cache->max_new, n) * a.group;
     cudaError_t e = cudaSuccess;
-    if (a.simt) {
-        a.min_rows = 0;
-        e = launch_paged_simt(a, (int)std::min<int64_t>(most, 64), s);
-    } else {
-        // Sequences of few rows are bound by reading their keys and have a kernel of their own; a single sequence that may
-        // have more is not worth the launches that would find nothing to do.
-        const bool listed = most > PG_FEW_ROWS, few = !listed || a.c.n_seq > 1;
-        a.min_rows = few ? PG_FEW_ROWS : 0;
-        if (few) e = launch_paged_few(a, s);
-        if (e == cudaSuccess && listed) e = launch_paged_tc(a, s);
-    }
+    // Sequences of few rows are bound by reading their keys and have a kernel of their own; a single sequence that may have
+    // more is not worth the launches that would find nothing to do.
+    const int rows = few_rows(cache);
+    const bool listed = most > rows, few = rows > 0 && (!listed || a.c.n_seq > 1);
+    a.min_rows = few ? rows : 0;
+    if (few) e = launch_paged_few(a, s);
+    if (e == cudaSuccess && listed) e = a.simt ? launch_paged_simt(a, (int)std::min<int64_t>(most, 64), s) : launch_paged_tc(a, s);
     return e == cudaSuccess ? SKIPFFN_OK : SKIPFFN_ECUDA;
 }
 

@@ -134,7 +134,7 @@ struct PagedEvictArgs {
 // rows of a tile, runs of a launch (these size the scratch): plain FMA, two CTAs an SM for 16 rows, one for 64; few rows,
 // eight warps an SM
 constexpr int PG_SIMT_KEYS = 64, PG_SIMT_RUNS = 296, PG_SIMT_SLOTS = 2 * 148 * 64;
-constexpr int PG_FEW_ROWS = 16, PG_FEW_SMS = 160, PG_FEW_SLOTS = 2 * PG_FEW_SMS * 8 * PG_FEW_ROWS;
+constexpr int PG_FEW_ROWS = 16, PG_FEW_ROWS_FP32 = 8, PG_FEW_SMS = 160, PG_FEW_SLOTS = 2 * PG_FEW_SMS * 8 * PG_FEW_ROWS;
 constexpr int PG_TC_RUNS = 160, PG_TC_ROWS = 256;     // tensor-core kernel: one run per SM, two row tiles
 
 // paged.cu
@@ -144,12 +144,12 @@ skipffn_status paged_view(const skipffn_paged_cache *c, int64_t N, PagedView *vi
 bool paged_overlap(const PagedView &c, const void *p, int64_t bytes);
 cudaError_t launch_paged_list(const PagedAttnArgs &a, int rows, int block, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttnArgs &a, int rows, int pitch, cudaStream_t s);
-cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int pitch, cudaStream_t s);
-// paged_few.cu: sequences of at most PG_FEW_ROWS rows, bf16
+cudaError_t launch_paged_join_few(const PagedAttnArgs &a, int rows, int pitch, cudaStream_t s);
+// paged_few.cu: sequences of at most PG_FEW_ROWS rows, bf16, or PG_FEW_ROWS_FP32
 cudaError_t launch_paged_few(const PagedAttnArgs &a, cudaStream_t s);
 // paged_tc.cu: sequences of more rows than that, bf16
 cudaError_t launch_paged_tc(const PagedAttnArgs &a, cudaStream_t s);
-// paged_simt.cu: sequences of at most `rows` rows, any number, plain FMA
+// paged_simt.cu: sequences of more than min_rows and at most `rows` rows, any number, plain FMA
 cudaError_t launch_paged_simt(const PagedAttnArgs &a, int rows, cudaStream_t s);
 cudaError_t launch_paged_weights_simt(const PagedWeightsArgs &a, cudaStream_t s);
 // paged_weights.cu (bf16)

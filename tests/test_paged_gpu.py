@@ -355,3 +355,25 @@ def test_sequences_of_one_row_tile_over_several_blocks(tokens, lens, hq, hk, d):
                 # weights and the result in bf16: half a step each, of values of at most the largest
                 assert np.allclose(to_host(out[t, h]), p / p.sum() @ v, rtol=0, atol=2.0 ** -7 * np.abs(v).max())
                 assert abs(lse[t, h].item() - sc.max() - np.log(p.sum())) < 1e-4 * max(1.0, abs(sc.max()))
+
+
+@pytest.mark.parametrize("path", [0, 1])
+@pytest.mark.parametrize("new,lens,hq,hk,d", [
+    ((1, 2, 0, 1), (9, 300, 8, 1), 1, 1, 128),               # 1 and 2 rows
+    ((3, 1, 2), (3, 500, 77), 1, 1, 40),                     # up to 4
+    ((1, 1), (2000, 17), 4, 1, 64),
+    ((1, 2, 1), (129, 7, 640), 6, 2, 72),                    # up to 6
+    ((8, 5), (8, 1000), 1, 1, 128),
+    ((2, 30, 1, 3), (200, 31, 900, 150), 4, 1, 96),          # 8 and fewer beside 12 and 120
+    ((3, 1), (2, 16), 2, 1, 64),                             # the first tokens see nothing
+])
+def test_few_rows_in_fp32(new, lens, hq, hk, d, path):
+    import torch
+    x = Batch(15, new, lens, hq, hk, d, 8, "fp32", path=path)
+    out, lse = x.cache.attention(x.q)
+    x.cache.poll()
+    r_out, r_lse, e_out, e_lse = x.want()
+    within(out, r_out, e_out, "out")
+    within(lse, r_lse, e_lse, "lse")
+    out2, lse2 = x.cache.attention(x.q)
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
