@@ -296,7 +296,7 @@ struct Scratch { size_t cuts, head, starts, seq_tiles, tiles, ml, part, total; i
 
 bool simt(const skipffn_paged_cache *c) { return c->dtype == SKIPFFN_FP32 || c->path == SKIPFFN_PATH_SIMT; }
 
-// rows of a sequence that the kernel of few rows takes
+// rows of a sequence that the kernel of few rows takes (0: that kernel is not asked for)
 int few_rows(const skipffn_paged_cache *c)
 {
     return c->path == SKIPFFN_PATH_SIMT ? 0 : c->dtype == SKIPFFN_FP32 ? PG_FEW_ROWS_FP32 : PG_FEW_ROWS;
@@ -305,7 +305,7 @@ int few_rows(const skipffn_paged_cache *c)
 Scratch scratch_of(const skipffn_paged_cache *c, int group, int64_t N)
 {
     const int64_t most = std::min<int64_t>(c->max_new, N) * group;
-    const bool listed = most > few_rows(c), few = c->path != SKIPFFN_PATH_SIMT;
+    const bool few = few_rows(c) > 0, listed = !few || most > few_rows(c);
     // the largest of the kernels that the call may launch
     const int64_t slots = std::max(few ? PG_FEW_SLOTS : 0, !listed ? 0 : simt(c) ? PG_SIMT_SLOTS : 2 * PG_TC_RUNS * PG_TC_ROWS);
     const int64_t tile = simt(c) ? (most <= 16 ? 16 : 64) : 2 * (128 / group) * group;
@@ -401,7 +401,7 @@ skipffn_status skipffn_paged_attention(const skipffn_paged_cache *cache, int32_t
     // Sequences of few rows are bound by reading their keys and have a kernel of their own; a single sequence that may have
     // more is not worth the launches that would find nothing to do.
     const int rows = few_rows(cache);
-    const bool listed = most > rows, few = rows > 0 && (!listed || a.c.n_seq > 1);
+    const bool listed = rows == 0 || most > rows, few = rows > 0 && (!listed || a.c.n_seq > 1);
     a.min_rows = few ? rows : 0;
     if (few) e = launch_paged_few(a, s);
     if (e == cudaSuccess && listed) e = a.simt ? launch_paged_simt(a, (int)std::min<int64_t>(most, 64), s) : launch_paged_tc(a, s);

@@ -377,3 +377,15 @@ def test_few_rows_in_fp32(new, lens, hq, hk, d, path):
     within(lse, r_lse, e_lse, "lse")
     out2, lse2 = x.cache.attention(x.q)
     assert torch.equal(out, out2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("dtype,path", [("bf16", 0), ("bf16", 1), ("fp32", 0), ("fp32", 1)])
+def test_more_new_tokens_than_the_most_are_reported_when_the_most_is_zero(dtype, path):
+    import torch
+    import paper_2503_21817_b200 as sk
+    x = Batch(16, (1, 2), (9, 20), 4, 2, 64, 8, dtype, max_new=0, path=path)
+    out, lse = torch.full_like(x.q, 7.0), torch.full((3, 4), 7.0, device="cuda")
+    x.cache.attention(x.q, out=out, lse=lse)
+    with pytest.raises(sk.SkipFFNError, match="site 64"):
+        x.cache.poll()
+    assert bool((out == 7.0).all()) and bool((lse == 7.0).all())
