@@ -114,15 +114,16 @@ __device__ int64_t block_exclusive(int64_t v, int64_t *warp_sums, int64_t &total
     return before + x - v;
 }
 
-template <typename T> __device__ void empty_rows(const PagedAttnArgs &a, const PagedTile &t, int rows)
+// Queries that see no row: zeros, and the logarithm of nothing.  A warp writes the rows first .. first + count - 1 of a sequence
+// whose tokens begin at q0, for all heads.
+template <typename T> __device__ void empty_rows(const PagedAttnArgs &a, int q0, int first, int count, int lane)
 {
-    // queries that see no row: zeros, and the logarithm of nothing
     for (int h = 0; h < a.c.heads; ++h)
-        for (int r = t.r0; r < t.r0 + rows; ++r) {
-            const int64_t token = t.q0 + r / a.group;
+        for (int r = first; r < first + count; ++r) {
+            const int64_t token = q0 + r / a.group;
             const int head = h * a.group + r % a.group;
-            for (int c = 0; c < a.c.d; ++c) ((T *)a.out)[token * a.ldo + (int64_t)head * a.c.d + c] = from_f32<T>(0.0f);
-            a.lse[token * a.hq + head] = -INFINITY;
+            for (int c = lane; c < a.c.d; c += 32) ((T *)a.out)[token * a.ldo + (int64_t)head * a.c.d + c] = from_f32<T>(0.0f);
+            if (lane == 0) a.lse[token * a.hq + head] = -INFINITY;
         }
 }
 
@@ -163,6 +164,7 @@ __global__ void __launch_bounds__(LIST_THREADS) k_paged_list(const PagedAttnArgs
     for (int t0 = 0; t0 < tiles; t0 += LIST_THREADS) {
         const int t = t0 + threadIdx.x;
         PagedTile e = {};
+        int empty = 0;                       // rows of a tile without keys
         if (t < tiles) {
             int lo = 0, hi = c.n_seq;        // largest s with first_tile[s] <= t
             while (hi - lo > 1) {
@@ -175,10 +177,13 @@ __global__ void __launch_bounds__(LIST_THREADS) k_paged_list(const PagedAttnArgs
             const int live = min(rows, q.n * a.group - e.r0);
             const int keys = max(0, q.len - q.n + (e.r0 + live - 1) / a.group + 1);
             e.blocks = (keys + block - 1) / block;
-            if (keys == 0) {
-                if (a.dtype == SKIPFFN_BF16) empty_rows<bf16>(a, e, live);
-                else empty_rows<float>(a, e, live);
-            }
+            if (keys == 0) empty = live;
+        }
+        for (unsigned todo = __ballot_sync(0xffffffffu, empty > 0); todo; todo &= todo - 1) {
+            const int from = __ffs(todo) - 1, lane = threadIdx.x & 31;
+            const int q0 = __shfl_sync(0xffffffffu, e.q0, from), r0 = __shfl_sync(0xffffffffu, e.r0, from), n = __shfl_sync(0xffffffffu, empty, from);
+            if (a.dtype == SKIPFFN_BF16) empty_rows<bf16>(a, q0, r0, n, lane);
+            else empty_rows<float>(a, q0, r0, n, lane);
         }
         const int64_t before = block_exclusive(e.blocks ? (int64_t)(e.blocks + PG_TILE_COST) * c.heads : 0, warp_sums, total);
         e.u0 = units + before;

@@ -389,3 +389,14 @@ def test_more_new_tokens_than_the_most_are_reported_when_the_most_is_zero(dtype,
     with pytest.raises(sk.SkipFFNError, match="site 64"):
         x.cache.poll()
     assert bool((out == 7.0).all()) and bool((lse == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype,path", [("bf16", 0), ("bf16", 1), ("fp32", 0)])
+def test_chunks_of_which_whole_tiles_see_nothing(dtype, path):
+    import torch
+    x = Batch(17, (600, 300, 40), (3, 0, 20), 8, 2, 64, 8, dtype, path=path)
+    out, lse = x.cache.attention(x.q, out=torch.full_like(x.q, 7.0))
+    x.cache.poll()
+    r_out, r_lse, e_out, e_lse = x.want()
+    within(out, r_out, e_out, "out")
+    within(lse, r_lse, e_lse, "lse")
