@@ -368,7 +368,7 @@ k_rotary_bwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ Rotar
             for (int u = 0; u < U; ++u) {
                 at[u] = -1;
                 head[u] = walk.h;
-                y[u] = x[u] = Row<T, V>{};   // a lane without a row adds nothing
+                y[u] = x[u] = Row<T, V>{};
                 if (walk.t < count && l.on) {
                     const int64_t tok = t0 + walk.t;
                     at[u] = walk.t;
@@ -396,7 +396,9 @@ k_rotary_bwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ Rotar
                         ss = fma2(xl[i], xl[i], fma2(xh[i], xh[i], ss));
                         ux = fma2(mul2(lo[i], g0[i]), xl[i], fma2(mul2(hi[i], g1[i]), xh[i], ux));
                     }
-                    const float r = rsqrtf(group_sum<L>(sum2(ss)) * inv_d + a.eps);
+                    const float inv = rsqrtf(group_sum<L>(sum2(ss)) * inv_d + a.eps);
+                    // lanes without a row add nothing: their zeros have no inverse norm when eps is 0
+                    const float r = at[u] >= 0 ? inv : 0.0f;
                     const uint64_t r2 = both(r), m = both(-group_sum<L>(sum2(ux)) * inv_d * r * r);
 #pragma unroll
                     for (int i = 0; i < V / 2; ++i) {
