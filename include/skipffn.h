@@ -363,9 +363,10 @@ skipffn_status skipffn_kv_compact(const skipffn_saved *saved, const void *src, v
  *   status           : device int32 [SKIPFFN_PAGED_STATUS_WORDS], zeroed once by the caller
  * The three integer arrays may change between a call's launch and the next, so captured calls follow them.  They are not
  * trusted: offsets outside the call's tokens, lengths beyond the table, more than max_new new tokens, page numbers
- * outside 0 .. n_pages - 1 never lead to an access outside the arrays; such a sequence (or page) is left out or cut, and
- * skipffn_paged_poll reports SKIPFFN_EINVAL with the site of one of the faults: 64 offsets, 65 length, 66 page, 67 no room for a row,
- * 68 more rows than weights; SKIPFFN_ETIMEOUT if a kernel gave up on a wait (results unfinished).
+ * outside 0 .. n_pages - 1 never lead to an access outside the arrays; such a sequence (or page) is left out or cut (by the
+ * append calls left out: none of its rows is written), and skipffn_paged_poll reports SKIPFFN_EINVAL with the site of one of
+ * the faults: 64 offsets, 65 length, 66 page, 67 no room for a row, 68 more rows than weights; SKIPFFN_ETIMEOUT if a kernel
+ * gave up on a wait (results unfinished).
  * head_dim is a multiple of 8 up to 128, page_size a multiple of 8, heads_q / heads_kv at most 64, else EUNSUPPORTED.
  * All sums have a fixed order: equal calls give equal bits. */
 #define SKIPFFN_PAGED_STATUS_WORDS 64
@@ -448,7 +449,8 @@ skipffn_status skipffn_paged_poll(const skipffn_paged_cache *cache, void *stream
  * gradient may stand on the upstream one or on the input; other overlaps are EINVAL.  dgamma_*: in dtype, fp32 with
  * dw_fp32, overwritten, either may be NULL; scratch (only with gammas): skipffn_rotary_scratch_bytes(handle) bytes.
  * append: the rotated keys and the values go to the rows of the cache that the new tokens are (cache->dtype is the dtype
- * of the call), the rotated queries to q_out; tokens behind the last sequence are left alone.
+ * of the call), the rotated queries to q_out, those of a sequence that the cache's integers leave out too; tokens that belong
+ * to no sequence are left alone.
  * Arithmetic is fp32 in a fixed order, results are rounded once. */
 typedef struct {
     int32_t heads_q, heads_kv, head_dim, rotary_dim;

@@ -198,8 +198,17 @@ __device__ __forceinline__ void load_positions(int *pos, const RotaryArgs &a, in
     if (i < count && axis < a.axes) pos[threadIdx.x] = a.pos[axis * a.ldpos + t0 + i];
 }
 
-// Where the last row of a token's sequence puts it: byte offset of its cache row, -1 for none (token behind the last sequence: -2).
-// One warp, every lane gets the answer.
+// Is the token one of sequence s, whose offsets and length are possible?
+__device__ __forceinline__ bool sound_seq(const PagedView &c, int s, int64_t token)
+{
+    const int a = c.cu[s], b = c.cu[s + 1];
+    const PagedSeq q = paged_seq(c, s, false);
+    return a <= token && token < b && q.q0 == a && q.n == b - a && q.len == c.lens[s];
+}
+
+// Byte offset of the cache row of a token, -1 for none, -2 for none of a token that belongs to no sequence.  A sequence whose
+// offsets or length are at fault has none for any of its tokens, since they may name older rows.  One warp, every lane gets
+// the answer.
 __device__ __forceinline__ int64_t append_row(const PagedView &c, int64_t token, int lane, bool report)
 {
     int lo = 0, hi = c.n_seq;                                // largest s with cu[s] <= token, 32 candidates at a time
@@ -211,14 +220,22 @@ __device__ __forceinline__ int64_t append_row(const PagedView &c, int64_t token,
         hi = min(hi, first + step);
         lo = first;
     }
-    const int a = c.cu[lo], b = c.cu[lo + 1];
-    if (token < a || token >= b) {
-        // behind the last sequence is where rows may stand that belong to none
-        if (report && lane == 0 && token < c.cu[c.n_seq]) paged_report(c, SITE_PAGED_OFFSETS);
-        return -2;
+    const bool spanned = c.cu[lo] <= token && token < c.cu[lo + 1];
+    // behind the last sequence is where rows may stand that belong to none
+    if (!spanned && token >= c.cu[c.n_seq]) return -2;
+    if (!sound_seq(c, lo, token)) {                          // the search wants ascending offsets: another may have the token
+        unsigned has = 0;
+        for (int s = lane; s - lane < c.n_seq && !has; s += 32) {
+            has = __ballot_sync(0xffffffffu, s < c.n_seq && sound_seq(c, s, token));
+            lo = s - lane + __ffs(has) - 1;
+        }
+        if (!has) {
+            if (report && lane == 0 && !spanned) paged_report(c, SITE_PAGED_OFFSETS);
+            return spanned ? -1 : -2;
+        }
     }
-    const int64_t row = (int64_t)c.lens[lo] - b + token;
-    if (row < 0 || row >= c.capacity) {
+    const int64_t row = (int64_t)c.lens[lo] - c.cu[lo + 1] + token;
+    if (row < 0) {
         if (report && lane == 0) paged_report(c, SITE_PAGED_ROOM);
         return -1;
     }
@@ -333,6 +350,9 @@ k_rotary_fwd(const __grid_constant__ RotaryArgs a, const __grid_constant__ Rotar
             }
         }
     }
+    // offsets and lengths at fault are reported whether or not a token of this call meets them; the values' CTAs have no table to make
+    if (APPEND && kind == 2 && cta == 0)
+        for (int s = threadIdx.x; s < a.c.n_seq; s += RT_THREADS) paged_seq(a.c, s, true);
 }
 
 // Backward.  CTAs of a kind walk blocks of its tokens; the gain's gradient is summed in registers (a lane's columns stay
