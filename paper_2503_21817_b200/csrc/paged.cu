@@ -360,7 +360,10 @@ using namespace skipffn;
 static skipffn_status check_heads(const PagedView &v, int32_t heads_q, float scale)
 {
     if (heads_q <= 0 || heads_q % v.heads || !(scale > 0.0f) || !isfinite(scale)) return SKIPFFN_EINVAL;
-    return heads_q / v.heads > 64 || heads_q > 65535 ? SKIPFFN_EUNSUPPORTED : SKIPFFN_OK;
+    const int group = heads_q / v.heads;
+    // the kernels count the rows of a sequence (new tokens x heads of a group) in 32 bits, and a tile or two beyond
+    const int64_t rows = std::min<int64_t>(v.max_new, v.N) * group;
+    return group > 64 || heads_q > 65535 || rows > INT_MAX - 4096 ? SKIPFFN_EUNSUPPORTED : SKIPFFN_OK;
 }
 
 extern "C" {
