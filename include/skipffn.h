@@ -368,7 +368,7 @@ skipffn_status skipffn_kv_compact(const skipffn_saved *saved, const void *src, v
  * the faults: 64 offsets, 65 length, 66 page, 67 no room for a row, 68 more rows than weights; SKIPFFN_ETIMEOUT if a kernel
  * gave up on a wait (results unfinished).
  * head_dim is a multiple of 8 up to 128, page_size a multiple of 8, heads_q / heads_kv at most 64, new tokens of a sequence
- * (min(max_new, n)) times heads_q / heads_kv below 2^31 - 4096, else EUNSUPPORTED.
+ * (min(max_new, n)) times heads_q / heads_kv below 2^31 - 4096, n_seq, width and budget below 2^31 - 8192, else EUNSUPPORTED.
  * All sums have a fixed order: equal calls give equal bits. */
 #define SKIPFFN_PAGED_STATUS_WORDS 64
 typedef struct {

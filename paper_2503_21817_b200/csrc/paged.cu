@@ -34,7 +34,8 @@ skipffn_status paged_view(const skipffn_paged_cache *c, int64_t N, PagedView *v)
         c->n_pages < 0 || c->n_seq < 0 || c->table_width < 0 || c->max_new < 0 || N < 0 || N > INT_MAX - 4096 ||
         (c->path != SKIPFFN_PATH_DEFAULT && c->path != SKIPFFN_PATH_SIMT) || !c->status || !is_aligned(c->status, 4))
         return SKIPFFN_EINVAL;
-    if (c->head_dim % 8 || c->head_dim > PG_MAX_D || c->page_size % 8 || c->page_size > (1 << 30) || c->n_pages > INT_MAX || c->heads_kv > 65535)
+    if (c->head_dim % 8 || c->head_dim > PG_MAX_D || c->page_size % 8 || c->page_size > (1 << 30) || c->n_pages > INT_MAX || c->heads_kv > 65535 ||
+        c->n_seq > PG_MAX_COUNT)
         return SKIPFFN_EUNSUPPORTED;
     const int64_t es = c->dtype == SKIPFFN_BF16 ? 2 : 4;
     for (const int64_t ld : {c->page_stride, c->row_stride, c->head_stride})
@@ -425,7 +426,7 @@ skipffn_status skipffn_paged_weights(const skipffn_paged_cache *cache, int32_t h
     if (st != SKIPFFN_OK) return st;
     if (width < 0) return SKIPFFN_EINVAL;
     if (a.c.n_seq == 0 || width == 0) return SKIPFFN_OK;
-    if (a.c.n_seq > 65535) return SKIPFFN_EUNSUPPORTED;
+    if (a.c.n_seq > 65535 || width > PG_MAX_COUNT) return SKIPFFN_EUNSUPPORTED;
     const int es = cache->dtype == SKIPFFN_BF16 ? 2 : 4;
     const int64_t bytes = (int64_t)a.c.n_seq * a.c.heads * width * 4, wl = (int64_t)heads_q * 4;
     if (ldq < 0 || ldq > (int64_t)1 << 36 || !weights || !is_aligned(weights, 4) || !is_aligned(prior, 4)) return SKIPFFN_EINVAL;
@@ -463,6 +464,7 @@ skipffn_status skipffn_paged_evict(const skipffn_paged_cache *cache, const skipf
             return SKIPFFN_EINVAL;
     }
     if (a.c.n_seq == 0) return SKIPFFN_OK;
+    if (width > PG_MAX_COUNT || budget > PG_MAX_COUNT) return SKIPFFN_EUNSUPPORTED;
     const int64_t pairs = (int64_t)a.c.n_seq * a.c.heads, wb = pairs * width * 4, kb = pairs * budget * 4, lb = (int64_t)a.c.n_seq * 4;
     if (pairs > INT_MAX / 16) return SKIPFFN_EUNSUPPORTED;
     if ((width > 0 && !weights) || !kept || !lens_out || !weights_out) return SKIPFFN_EINVAL;

@@ -11,6 +11,8 @@ namespace skipffn {
 enum : int { SITE_PAGED_OFFSETS = 64, SITE_PAGED_LENGTH = 65, SITE_PAGED_PAGE = 66, SITE_PAGED_ROOM = 67, SITE_PAGED_WIDTH = 68 };
 
 constexpr int PG_MAX_D = 128;
+// sequences of a call, columns of weights, rows that eviction keeps: loops step past them by up to eight CTAs' threads
+constexpr int PG_MAX_COUNT = 0x7fffffff - 8192;
 
 // x / divisor for 0 <= x < 2^31 by one multiplication (divisor >= 2)
 struct Divisor { uint32_t mul, shift, d; };
