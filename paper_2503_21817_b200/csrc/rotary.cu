@@ -581,15 +581,16 @@ skipffn_status check_call(const skipffn_rotary *h, int32_t dtype, int64_t n, con
     return SKIPFFN_OK;
 }
 
-// `out` may be `same` (in place), every other overlap with what the call reads is refused
-bool out_ok(const TokenArray &out, const TokenArray *same, std::initializer_list<TokenArray> in, const int32_t *pos, int64_t pos_bytes,
-            const void *gq, const void *gk, int64_t g_bytes, int64_t n)
+// `out` may stand on an array of its `own` rows (in place: a row is read before it is written, by the same lanes); every other
+// overlap with what the call reads is refused, also where an array of other rows is one of its own
+bool out_ok(const TokenArray &out, std::initializer_list<TokenArray> own, std::initializer_list<TokenArray> others, const int32_t *pos,
+            int64_t pos_bytes, const void *gq, const void *gk, int64_t g_bytes, int64_t n)
 {
     if (!token_array_ok(out, n)) return false;
-    for (const TokenArray &x : in) {
-        if (same && x.p == same->p && x.ld == same->ld && out.p == x.p && out.ld == x.ld && out.width == x.width) continue;
+    for (const TokenArray &x : own)
+        if (!(out.p == x.p && out.ld == x.ld && out.width == x.width) && tokens_overlap(out, x, n)) return false;
+    for (const TokenArray &x : others)
         if (tokens_overlap(out, x, n)) return false;
-    }
     const int64_t b = token_bytes(out, n);
     return !ranges_overlap(out.p, b, pos, pos_bytes) && !ranges_overlap(out.p, b, gq, g_bytes) && !ranges_overlap(out.p, b, gk, g_bytes);
 }
@@ -652,8 +653,8 @@ skipffn_status skipffn_rotary_forward(const skipffn_rotary *h, int32_t dtype, in
         if (ld < 0 || ld > (int64_t)1 << 36) return SKIPFFN_EINVAL;
     const TokenArray oq{q_out, ldqo * c.es, c.q.width}, ok{k_out, ldko * c.es, c.k.width};
     const int64_t pb = pos_bytes(h, n, ldpos), gb = (int64_t)h->d * c.es;
-    if (!out_ok(oq, &c.q, {c.q, c.k}, positions, pb, gamma_q, gamma_k, gb, n) ||
-        !out_ok(ok, &c.k, {c.q, c.k}, positions, pb, gamma_q, gamma_k, gb, n) || tokens_overlap(oq, ok, n))
+    if (!out_ok(oq, {c.q}, {c.k}, positions, pb, gamma_q, gamma_k, gb, n) || !out_ok(ok, {c.k}, {c.q}, positions, pb, gamma_q, gamma_k, gb, n) ||
+        tokens_overlap(oq, ok, n))
         return SKIPFFN_EINVAL;
     RotaryArgs a = args_of(h, n, q, ldq, k, ldk, positions, ldpos, gamma_q, gamma_k, q_out, ldqo, k_out, ldko);
     plan_rows(&a, dtype);
@@ -690,10 +691,8 @@ skipffn_status skipffn_rotary_backward(const skipffn_rotary *h, int32_t dtype, i
         const TokenArray oq{dq, lddq * es, c.q.width}, ok{dk, lddk * es, c.k.width};
         const int64_t pb = pos_bytes(h, n, ldpos), gb = (int64_t)h->d * es;
         if (!token_array_ok(gq, n) || !token_array_ok(gk, n)) return SKIPFFN_EINVAL;
-        // a result may stand where its own row was read, the upstream gradient or the input
-        const bool q_in = dq == q, k_in = dk == k;
-        if (!out_ok(oq, q_in ? &c.q : &gq, {c.q, c.k, gq, gk}, positions, pb, gamma_q, gamma_k, gb, n) ||
-            !out_ok(ok, k_in ? &c.k : &gk, {c.q, c.k, gq, gk}, positions, pb, gamma_q, gamma_k, gb, n) || tokens_overlap(oq, ok, n))
+        if (!out_ok(oq, {c.q, gq}, {c.k, gk}, positions, pb, gamma_q, gamma_k, gb, n) ||
+            !out_ok(ok, {c.k, gk}, {c.q, gq}, positions, pb, gamma_q, gamma_k, gb, n) || tokens_overlap(oq, ok, n))
             return SKIPFFN_EINVAL;
         if (norm) {
             const int64_t b = (int64_t)h->d * gs;
@@ -741,7 +740,7 @@ skipffn_status skipffn_rotary_append(const skipffn_rotary *h, const skipffn_page
         if (ld < 0 || ld > (int64_t)1 << 36) return SKIPFFN_EINVAL;
     const TokenArray va{v, ldv * c.es, c.k.width}, oq{q_out, ldqo * c.es, c.q.width};
     const int64_t pb = pos_bytes(h, n, ldpos), gb = (int64_t)h->d * c.es;
-    if (!token_array_ok(va, n) || !out_ok(oq, &c.q, {c.q, c.k, va}, positions, pb, gamma_q, gamma_k, gb, n)) return SKIPFFN_EINVAL;
+    if (!token_array_ok(va, n) || !out_ok(oq, {c.q}, {c.k, va}, positions, pb, gamma_q, gamma_k, gb, n)) return SKIPFFN_EINVAL;
     for (const TokenArray &x : {c.q, c.k, va, oq})
         if (paged_overlap(view, x.p, token_bytes(x, n))) return SKIPFFN_EINVAL;
     if (paged_overlap(view, positions, pb) || paged_overlap(view, gamma_q, gb) || paged_overlap(view, gamma_k, gb)) return SKIPFFN_EINVAL;
