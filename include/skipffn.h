@@ -395,6 +395,7 @@ typedef struct {
  * other, q or the cache (EINVAL).  scratch: device memory of skipffn_paged_attention_scratch_bytes(...) bytes, 16-byte
  * aligned, used by this call only.
  * Statistics and sums are fp32; bf16: the softmax weights are rounded to bf16 as operands of the second product, results once.
+ * A NaN among a token's scores gives NaN in its out and lse, minus infinity alone what no row gives.
  * What stands in the cache past a sequence's rows (unwritten memory, NaN) does not reach its results; inside a sequence a
  * non-finite value of a new token can reach earlier tokens of the same call (0 * inf). */
 size_t skipffn_paged_attention_scratch_bytes(const skipffn_paged_cache *cache, int32_t heads_q, int64_t n);

@@ -248,7 +248,7 @@ template <typename T, int SUBS, int ROWS> __global__ void __launch_bounds__(JOIN
         for (int r = 0; r < ROWS; ++r) {
             float2 ml = make_float2(-INFINITY, 0.0f);
             if (i1 < cut.pieces && r < rows) ml = a.part_ml[slot(i1) + r];
-            f[r] = ml.x == -INFINITY ? 0.0f : exp2f((ml.x - top[r]) * c2);
+            f[r] = ml.x == -INFINITY ? ml.y : exp2f((ml.x - top[r]) * c2);    // without a maximum the sum is 0, or NaN
             fl[r] = f[r] * ml.y;
         }
         const int n = min(32, (cut.pieces - i0 + SUBS - 1) / SUBS);
@@ -287,7 +287,7 @@ template <typename T, int SUBS, int ROWS> __global__ void __launch_bounds__(JOIN
         const int r = cut.r0 + row + i;
         const int64_t token = cut.q0 + r / a.group;
         const int head = cut.h * a.group + r % a.group;
-        const bool none = top[i] == -INFINITY;
+        const bool none = met_nothing(top[i], l[i]);
         if (mine) {
             const float inv = 1.0f / l[i];
 #pragma unroll

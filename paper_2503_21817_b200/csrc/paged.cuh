@@ -104,6 +104,10 @@ struct PagedAttnArgs {
     int32_t runs;
 };
 
+// Has a row with running maximum m and sum l met nothing but minus infinity?  The maximum alone does not say so: it passes NaN over, which
+// the sum does not.
+__device__ __forceinline__ bool met_nothing(float m, float l) { return m == -INFINITY && l == 0.0f; }
+
 // Runs over `units` by at most `ctas` CTAs: no run is empty, since the pieces of a tile are counted by their runs.
 struct Runs {
     int64_t units;

@@ -183,7 +183,7 @@ template <int DP> struct MmaRows {
             if (whole) {
                 bf16 *dst = (bf16 *)a.out + token * a.ldo + (int64_t)head * a.c.d;
                 const float inv = 1.0f / l[i];
-                const bool none = m[i] == -INFINITY;
+                const bool none = met_nothing(m[i], l[i]);
 #pragma unroll
                 for (int n = 0; n < DP / 8; ++n) {
                     const int col = 8 * n + 2 * (lane & 3);
@@ -309,7 +309,7 @@ template <int DP, int R> struct FmaRows {
             const int64_t token = at.q.q0 + r / a.group;
             const int head = at.h * a.group + r % a.group;
             if (whole) {
-                const bool none = m[r] == -INFINITY;
+                const bool none = met_nothing(m[r], l[r]);
                 const float inv = 1.0f / l[r];
                 if (lane < CHUNKS && col < a.c.d)
                     *reinterpret_cast<float4 *>((float *)a.out + token * a.ldo + (int64_t)head * a.c.d + col) =

@@ -176,17 +176,18 @@ template <typename T, int R> __global__ void __launch_bounds__(THREADS, R == 1 ?
                     const int64_t token = e.q0 + r / a.group;
                     const int head = h * a.group + r % a.group;
                     const float inv = 1.0f / l[i];
+                    const bool none = met_nothing(m[i], l[i]);
 #pragma unroll
                     for (int z = 0; z < 2; ++z) {
                         const int col = 64 * z + 4 * tx;
                         if (col < c.d) {
                             float v[4];
 #pragma unroll
-                            for (int w = 0; w < 4; ++w) v[w] = m[i] == -INFINITY ? 0.0f : acc[i][z][w] * inv;
+                            for (int w = 0; w < 4; ++w) v[w] = none ? 0.0f : acc[i][z][w] * inv;
                             store4((T *)a.out + token * a.ldo + (int64_t)head * c.d + col, v);
                         }
                     }
-                    if (tx == 0) a.lse[token * a.hq + head] = m[i] == -INFINITY ? -INFINITY : fmaf(m[i], a.scale, logf(l[i]));
+                    if (tx == 0) a.lse[token * a.hq + head] = none ? -INFINITY : fmaf(m[i], a.scale, logf(l[i]));
                 } else {
                     const int64_t at = (int64_t)(2 * run + (b0 == 0 ? 1 : 0)) * ROWS + row;
 #pragma unroll

@@ -310,7 +310,7 @@ k_paged_tc(const __grid_constant__ PagedMaps tm, const __grid_constant__ PagedTc
                 if (!ok) break;
                 tc_fence_after();
             }
-            const bool none = m == -INFINITY;        // nothing but keys it does not see, or minus infinity
+            const bool none = met_nothing(m, l);     // keys that it does not see among them
             if (whole) {
                 const float inv = none ? 0.0f : 1.0f / l;
                 bf16 *dst = live ? (bf16 *)a.out + tok * a.ldo + (int64_t)head * a.c.d : nullptr;
