@@ -59,7 +59,7 @@ __device__ __forceinline__ float2 turn_to_cos_sin(unsigned long long a)
 {
     const int t = (int)(a >> 32);                            // signed 2^-32 turns
     const unsigned quad = ((unsigned)t + (1u << 29)) >> 30;
-    const int rest = t - (int)(quad << 30);
+    const int rest = (int)((unsigned)t - (quad << 30));      // within 2^29 of zero; the difference of the signed ones would overflow
     const float x = (float)rest * 1.4629180792671596e-9f;    // 2 pi 2^-32
     const float z = x * x;
     float s = fmaf(z, 2.7557319e-6f, -1.9841270e-4f), c = fmaf(z, -2.7557319e-7f, 2.4801587e-5f);     // 1/9!, 1/7!; 1/10!, 1/8!
