@@ -486,11 +486,13 @@ skipffn_status skipffn_paged_evict(const skipffn_paged_cache *cache, const skipf
 skipffn_status skipffn_paged_poll(const skipffn_paged_cache *cache, void *stream, int32_t *site_out)
 {
     if (!cache || !cache->status) return SKIPFFN_EINVAL;
-    if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return SKIPFFN_ECUDA;
+    // on the caller's stream, not the default one: that may be busy, and a block cleared behind this call's back would lose what the
+    // next one reports
+    const cudaStream_t s = (cudaStream_t)stream;
     int32_t w[3] = {0, 0, 0};
-    if (cudaMemcpy(w, cache->status, sizeof(w), cudaMemcpyDeviceToHost) != cudaSuccess) return SKIPFFN_ECUDA;
+    if (cudaMemcpyAsync(w, cache->status, sizeof(w), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) return SKIPFFN_ECUDA;
     if (site_out) *site_out = w[ST_SITE];
-    if (w[ST_STATUS] != 0 && cudaMemset(cache->status + ST_STATUS, 0, 8) != cudaSuccess) return SKIPFFN_ECUDA;
+    if (w[ST_STATUS] != 0 && (cudaMemsetAsync(cache->status + ST_STATUS, 0, 8, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)) return SKIPFFN_ECUDA;
     return (skipffn_status)w[ST_STATUS];
 }
 
