@@ -61,6 +61,12 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedView &c, int s, bool re
     return r;
 }
 
+// Does paged_seq take offsets a, b and length l as they are?
+__device__ __forceinline__ bool paged_sound(const PagedView &c, int a, int b, int l)
+{
+    return a >= 0 && a <= b && b <= c.N && b - a <= c.max_new && l >= 0 && l <= c.capacity;
+}
+
 // Byte offset of row `row` (below the capacity), head 0, of sequence s; -1 if its page does not exist.
 __device__ __forceinline__ int64_t paged_row(const PagedView &c, int s, int row)
 {

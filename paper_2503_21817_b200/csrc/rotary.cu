@@ -198,14 +198,6 @@ __device__ __forceinline__ void load_positions(int *pos, const RotaryArgs &a, in
     if (i < count && axis < a.axes) pos[threadIdx.x] = a.pos[axis * a.ldpos + t0 + i];
 }
 
-// Is the token one of sequence s, whose offsets and length are possible?
-__device__ __forceinline__ bool sound_seq(const PagedView &c, int s, int64_t token)
-{
-    const int a = c.cu[s], b = c.cu[s + 1];
-    const PagedSeq q = paged_seq(c, s, false);
-    return a <= token && token < b && q.q0 == a && q.n == b - a && q.len == c.lens[s];
-}
-
 // Byte offset of the cache row of a token, -1 for none, -2 for none of a token that belongs to no sequence.  A sequence whose
 // offsets or length are at fault has none for any of its tokens, since they may name older rows.  One warp, every lane gets
 // the answer.
@@ -220,21 +212,29 @@ __device__ __forceinline__ int64_t append_row(const PagedView &c, int64_t token,
         hi = min(hi, first + step);
         lo = first;
     }
-    const bool spanned = c.cu[lo] <= token && token < c.cu[lo + 1];
+    int a = c.cu[lo], b = c.cu[lo + 1];
+    const bool spanned = a <= token && token < b;
     // behind the last sequence is where rows may stand that belong to none
     if (!spanned && token >= c.cu[c.n_seq]) return -2;
-    if (!sound_seq(c, lo, token)) {                          // the search wants ascending offsets: another may have the token
+    int len = c.lens[lo];
+    if (!spanned || !paged_sound(c, a, b, len)) {            // the search wants ascending offsets: another may have the token
         unsigned has = 0;
-        for (int s = lane; s - lane < c.n_seq && !has; s += 32) {
-            has = __ballot_sync(0xffffffffu, s < c.n_seq && sound_seq(c, s, token));
-            lo = s - lane + __ffs(has) - 1;
+        int s0 = -32;
+        while (!has) {
+            s0 += 32;
+            if (s0 >= c.n_seq) break;
+            lo = min(s0 + lane, c.n_seq - 1);
+            a = c.cu[lo]; b = c.cu[lo + 1]; len = c.lens[lo];
+            has = __ballot_sync(0xffffffffu, a <= token && token < b && paged_sound(c, a, b, len));
         }
         if (!has) {
             if (report && lane == 0 && !spanned) paged_report(c, SITE_PAGED_OFFSETS);
             return spanned ? -1 : -2;
         }
+        lo = s0 + __ffs(has) - 1;
+        b = c.cu[lo + 1]; len = c.lens[lo];
     }
-    const int64_t row = (int64_t)c.lens[lo] - c.cu[lo + 1] + token;
+    const int64_t row = (int64_t)len - b + token;
     if (row < 0) {
         if (report && lane == 0) paged_report(c, SITE_PAGED_ROOM);
         return -1;
