@@ -407,7 +407,9 @@ skipffn_status skipffn_paged_attention(const skipffn_paged_cache *cache, int32_t
  *     weights[s, h, j] = prior[s, h, j] + sum over new tokens i that see row j, and query heads g of kv head h,
  *                        of exp(scale q_ig . k_j - lse_ig)                                    for j < lens[s], else 0.
  * prior, weights: [n_seq, heads_kv, width] fp32; prior may be NULL (zero) or weights itself, else no overlap (EINVAL).
- * Tokens whose lse is minus infinity give nothing.  n_seq is at most 65535 (EUNSUPPORTED).  All arithmetic fp32. */
+ * Tokens whose lse is minus infinity give nothing, nor do weights below 2^-126.  width is at least the longest sequence's rows
+ * (site 68), so what eviction leaves is copied to the front of a wider array first.  n_seq is at most 65535 (EUNSUPPORTED).
+ * All arithmetic fp32. */
 skipffn_status skipffn_paged_weights(const skipffn_paged_cache *cache, int32_t heads_q, float scale, int64_t n, const void *q,
                                      int64_t ldq, const float *lse, const float *prior, float *weights, int32_t width, void *stream);
 

@@ -81,7 +81,8 @@ class PagedCache:
     memory order with contiguous rows of a head (views of one tensor that holds both, say).  ``page_table``: int32
     ``[n_seq, width]``, the pages of each sequence in order; ``cu_new``: int32 ``[n_seq + 1]`` offsets of each sequence's new
     tokens in the arrays of a call; ``lens``: int32 ``[n_seq]`` rows of each sequence, the new tokens among them as the last
-    ones; ``max_new``: the most new tokens a sequence may have.  The three integer tensors live on the device and may be
+    ones; ``max_new``: the most new tokens a sequence may have (it chooses the kernels: an object of its own for single tokens,
+    over the same tensors, is faster).  The three integer tensors live on the device and may be
     changed in place between calls and graph replays.  Work is enqueued on the current torch stream; calls that only
     read the cache may overlap.  Keep the object, and the tensors it was made of, as long as a captured call is replayed."""
 
@@ -185,7 +186,8 @@ class PagedCache:
         """Keeps at most ``budget`` rows of every sequence and kv head: the first ``sinks``, the last ``recent``, and those with
         the largest ``weights [n_seq, heads_kv, width]``; they move in their order to the front of ``into``'s pages, or of
         their own (``skipffn_paged_evict``).  Returns ``(kept [n_seq, heads_kv, budget] int32, lens [n_seq] int32, weights
-        [n_seq, heads_kv, budget])``; the ``lens`` of this object are left as they are."""
+        [n_seq, heads_kv, budget])``; the ``lens`` of this object are left as they are.  As ``prior`` of ``weights`` the last need
+        columns for the rows that follow: copy them to the front of a wider tensor of zeros."""
         torch = self._torch
         budget = operator.index(budget)
         if weights.dim() != 3:

@@ -10,10 +10,10 @@
 // heads (8-bit counts 36 us, with a barrier for every read of a peer's bins 33 us), 9 us for the 8 heads of one prompt.
 // k_evict_move: a warp takes up to 32 rows; its lanes look up their places in parallel, then 16-byte pieces of keys and
 // values move, 8 in flight a lane (4: 2 us less for the batch, 2 us more for one prompt; 16: 1 and 3 us more).  The three
-// reads that find the next rows run behind the pieces of these.  Bound by memory: 61 us for the batch's 345 MB (5.6 TB/s;
+// reads that find the next rows run behind the pieces of these.  Bound by memory: 61 us for the batch's 345 MB (5.7 TB/s;
 // rows of a head are 256 bytes apart from their neighbours' in memory).  In place, a pair's rows move in steps of its whole cluster: a row's
 // destination is never behind it (order is kept), so it is enough that a step has read all its rows before it writes any --
-// later steps read only rows behind this step's destinations.
+// later steps read only rows behind this step's destinations.  With its barriers the batch takes 95 us for 82, the one prompt 25 for 15.
 #include <algorithm>
 #include "paged.cuh"
 #include "ptx.cuh"

@@ -13,7 +13,7 @@
 // Bound by reading the keys for up to about 100 query rows a kv head, by the exponentials (16 a cycle and SM) beyond.  A TMA
 // box costs its warp about 64 cycles whatever its size, so pages of 16 rows want the two warps (with units of 128 keys, 48
 // conversations took 82 us from one warp, 71 us from two and 58 us from either with pages of 128 rows; with 256 it is 50 us
-// for 238 MB at 16 rows a page as at 128).  161 observing tokens of 40 heads take 55 us, a chunk of 2000 tokens over a
+// for 238 MB at 16 rows a page as at 128).  161 observing tokens of 40 heads take 57 us, a chunk of 2000 tokens over a
 // cache of 14 345 rows 518 us.  On the legacy matrix instructions a step of 64 keys x 32 rows
 // took 2 us from its copies to its sums however it was cut, with eight warps an SM: 100 us for the batch of 48
 // conversations (238 MB), 250 us for 161 observing tokens of 40 heads.

@@ -11,9 +11,10 @@
 //
 // Bound by memory: every row is read and written once.  A group of lanes holds a row, each lane V pairs of it (two
 // 16-byte vectors where the sizes allow), so the sums of a row are shuffles inside the group.  Measured: forward of 4928
-// tokens, 32 / 8 heads, head_dim 128, normalised, bf16: 24 us for 101 MB (4.2 TB/s; 5.5 to 5.9 with four times the tokens,
-// the rest is launch and the first table); backward of 16 documents 117 us (576 MB, 4.9 TB/s); one token a warp, its
-// cosines in registers, was no faster (23.5 to 30 and 128 us).
+// tokens, 32 / 8 heads, head_dim 128, normalised, bf16: 24 us for 101 MB (4.2 TB/s; 5.5 to 5.9 with four times the tokens; in
+// a row 22.8 us, the norm alone 18.2, the rotation alone 20.8: nothing is loaded behind either); backward of four documents of
+// 2344 tokens, 40 / 40 heads, 117 us (576 MB, 4.9 TB/s); one token a warp, its cosines in registers, was no faster (23.5 to 30
+// and 128 us).  4096 tokens of a prompt into the cache: 26.4 us, in fp32 37.2.
 #include <math.h>
 
 #include <initializer_list>
